@@ -49,8 +49,9 @@ typedef enum {
     SHARPV_ERR_CAPACITY = 4,      /* (status_word only) more survivors than `capacity` */
     SHARPV_ERR_CUDA = 5,          /* a CUDA runtime call or launch failed */
     SHARPV_ERR_TIMEOUT = 6,       /* (status_word only) reserved: a bounded device-side wait gave up; no kernel waits that way at present */
-    SHARPV_ERR_BOUNDS = 7         /* (status_word only, libraries built with -DSHARPV_DEBUG_BOUNDS) an index that a kernel was
-                                     about to gather from or scatter to lay outside its range; the access was skipped */
+    SHARPV_ERR_BOUNDS = 7         /* (status_word only) an index that a kernel was about to gather from or scatter to lay outside
+                                     its range; the access was skipped.  Checked in libraries built with -DSHARPV_DEBUG_BOUNDS,
+                                     and in every build by the entry points that say so */
 } sharpv_status;
 
 /* SHARPV_U8 (any one-byte element, e.g. an fp8 K/V cache) is accepted by sharpv_kv_compact only: rows are
@@ -338,6 +339,117 @@ sharpv_status sharpv_kv_compact_rope(
     const int32_t* kept_pos, const int32_t* kept_seq_offsets, const int32_t* seq_offsets, int32_t num_seqs,
     int64_t capacity, int32_t rotary_dim, double rope_base,
     void* workspace, size_t workspace_bytes, int32_t* status_word, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Decoding over the pruned cache (no counterpart in the paper, whose method ends with the smaller cache that
+ * "subsequent generation steps" read): attention over the cache's rows, the attention weight that every row
+ * collects, the choice of the rows that stay when a cache is over its budget, and the copy of rows into a cache
+ * whose sequences have room to grow.  The pruning entry points above never need attention scores; the two that
+ * follow the attention do not either: the weights are formed again from the queries and the log-sum-exp that
+ * any attention kernel returns.
+ *
+ * Shared by these entry points: sequence b's cached tokens are the cache rows [seq_begin[b], seq_begin[b] +
+ * seq_len[b]) of every plane, so sequences may be packed (seq_begin = kept_seq_offsets) or have free rows
+ * behind them; seq_len[b] may be 0.  A plane holds cache_tokens rows.  Its query nodes are the rows
+ * [node_offsets[b], node_offsets[b + 1]) of the query arrays, any number of them, 0 included; node_offsets is
+ * ascending and rows of the arrays that belong to no sequence are left untouched.  Table entries that reach
+ * outside the cache or the query arrays are cut to them and SHARPV_ERR_BOUNDS is written to status_word (in
+ * every build).  num_q_heads is a multiple of the layout's num_kv_heads; query head x reads KV head
+ * x / (num_q_heads / num_kv_heads).  SHARPV_F32 and SHARPV_BF16 caches (queries, drafted keys and values and
+ * the output have the cache's type), head_dim of at most 256.  num_seqs == 0 or total_nodes == 0 is valid and
+ * launches nothing.
+ *
+ * sharpv_tree_attention: attention of a step's query nodes.  Node i of a sequence sees every cached token
+ * of the sequence and those drafted tokens of the same sequence that its row of the tree mask marks:
+ *     s_j = scale * (q . k_j),  out = sum_j exp(s_j) v_j / sum_j exp(s_j),  lse = ln sum_j exp(s_j).
+ * draft_k, draft_v [dev] [total_nodes, num_kv_heads, head_dim]: the drafted tokens' own keys and values
+ *   (they are not in the cache yet), row strides ld_draft_k, ld_draft_v; both NULL: the cached tokens alone.
+ * tree_mask [dev] uint32[total_nodes, mask_words]: bit j % 32 of word j / 32 says that the node sees node j of
+ *   its sequence; bits that are not there count as 0.  NULL: node i sees the nodes 0 .. i (a chain, a chunk of
+ *   a prompt, or one decoded token).
+ * q [dev] [total_nodes, num_q_heads, head_dim], row stride ld_q; out [dev] the same shape, dense, 16-byte
+ *   aligned; out_lse [dev] float[total_nodes, num_q_heads].
+ * A row that sees nothing gives out = 0 and lse = -inf.  Keys and values that a row does not see never touch
+ * its result, whatever they hold (NaN and infinities included).  Scores, the softmax's maximum and sum and the
+ * weighted sums are fp32; out is rounded once.  scale > 0, finite.  Results do not depend on scheduling.
+ * workspace [dev]: sharpv_tree_attention_workspace_bytes() bytes, 256-byte aligned, contents undefined before
+ * and after; calls that may overlap on the GPU need a workspace each.
+ */
+size_t sharpv_tree_attention_workspace_bytes(int32_t num_seqs, int32_t head_dim);
+
+sharpv_status sharpv_tree_attention(
+    const void* q, int64_t ld_q,
+    const void* draft_k, int64_t ld_draft_k, const void* draft_v, int64_t ld_draft_v,
+    int32_t num_q_heads,
+    const void* kv, const sharpv_kv_layout* layout /* [host] */, int32_t layer, int64_t cache_tokens,
+    int32_t num_seqs, const int32_t* seq_begin, const int32_t* seq_len, const int32_t* node_offsets,
+    int64_t total_nodes, const uint32_t* tree_mask, int32_t mask_words, float scale,
+    void* out, float* out_lse,
+    void* workspace, size_t workspace_bytes, int32_t* status_word, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The attention weight that every cached token collects from a step's query nodes, summed over nodes and
+ * query heads:
+ *     out_mass[p] = decay * mass[p] + sum_nodes node_weight * sum_heads exp(scale * (q . k_p) - lse)
+ * for every cached row p of every sequence (rows outside the sequences are left untouched).  q, ld_q and the
+ * tables as in sharpv_tree_attention, lse [dev] float[total_nodes, num_q_heads] as it writes it (or as any other
+ * attention over at least these tokens returns it).
+ * node_weight [dev] float[total_nodes] or NULL (all 1): for example 1 for accepted nodes and 0 for the others;
+ *   a node of weight 0 is not looked at.  Rows whose lse is -inf (they saw nothing) add nothing.
+ * mass [dev] float[cache_tokens] or NULL: what the rows collected so far, row p at mass[p]; NULL and decay == 0
+ *   both mean that nothing is read and the sum starts at 0.  out_mass [dev] float[cache_tokens] may be mass.
+ * The sequences' cache rows must not overlap.  Sums are fp32 in a fixed order.
+ * workspace as above, sharpv_attention_mass_workspace_bytes() bytes.
+ */
+size_t sharpv_attention_mass_workspace_bytes(int32_t num_seqs, int64_t cache_tokens, int32_t num_kv_heads);
+
+sharpv_status sharpv_attention_mass(
+    const void* q, int64_t ld_q, const float* lse, const float* node_weight, int32_t num_q_heads,
+    const void* kv, const sharpv_kv_layout* layout /* [host] */, int32_t layer, int64_t cache_tokens,
+    int32_t num_seqs, const int32_t* seq_begin, const int32_t* seq_len, const int32_t* node_offsets,
+    int64_t total_nodes, float scale, float decay, const float* mass, float* out_mass,
+    void* workspace, size_t workspace_bytes, int32_t* status_word, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The cached tokens that stay when a sequence is over its budget.  Sequence b keeps the
+ * min(max(budget[b], 0), seq_len[b]) rows that come first under (protected before others, mass descending, row
+ * ascending); the first `sink` and the last `recent` rows of a sequence are protected.  -0 and +0 compare equal,
+ * NaN ranks above +inf.
+ * mass [dev] float[cache_tokens], row p of the cache at mass[p].
+ * out_kept_pos [dev] int32[capacity]: kept cache rows, sequence by sequence, ascending within a sequence, and
+ * out_kept_seq_offsets [dev] int32[num_seqs + 1]: the lists sharpv_kv_compact and sharpv_kv_append take (in
+ *   place compaction needs sequences in ascending order of their rows, as seq_begin has them in a packed cache).
+ * out_mass [dev] float[capacity] or NULL: mass of the kept rows, in the order of out_kept_pos (what the rows
+ *   of the compacted cache have collected); must not overlap mass.
+ * More survivors than `capacity`: SHARPV_ERR_CAPACITY in status_word, nothing written beyond it.
+ */
+sharpv_status sharpv_evict_select(
+    const float* mass, int64_t cache_tokens, int32_t num_seqs, const int32_t* seq_begin, const int32_t* seq_len,
+    const int32_t* budget, int32_t sink, int32_t recent,
+    int32_t* out_kept_pos, int32_t* out_kept_seq_offsets, float* out_mass, int64_t capacity,
+    int32_t* status_word, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * K/V rows into a cache whose sequences have room to grow.  For every layer in [layer_begin, layer_end), for K
+ * and V, for every KV head and every sequence b:
+ *     dst[dst_begin[b] + j - src_seq_offsets[b], :] = src[src_pos[j], :]
+ *         for src_seq_offsets[b] <= j < src_seq_offsets[b + 1]
+ * as a bit copy.  With the drafted tokens' K/V as the source, the accepted nodes as src_pos and dst_begin =
+ * seq_begin + seq_len this commits a step's accepted tokens; with a kept list as src_pos it compacts every
+ * sequence into a region of its own (sharpv_kv_compact packs them back to back).
+ * src_seq_offsets [dev] int32[num_seqs + 1], ascending, [0] = 0; src_pos [dev] int32[capacity]; `capacity` is a
+ * host-side upper bound on the rows and sizes the launch (more rows: SHARPV_ERR_CAPACITY in status_word, the
+ * surplus is not copied).  A plane holds src_tokens and dst_tokens rows; a row whose source or destination lies
+ * outside is not copied and SHARPV_ERR_BOUNDS is written to status_word (in every build).  The byte ranges of the
+ * two caches' planes must be disjoint, or SHARPV_ERR_INVALID_ARG is returned; destination rows of different
+ * sequences must not overlap.  Layouts as in sharpv_kv_compact, one-byte caches included.
+ */
+sharpv_status sharpv_kv_append(
+    const void* kv_src, const sharpv_kv_layout* src_layout /* [host] */, int64_t src_tokens,
+    void* kv_dst, const sharpv_kv_layout* dst_layout /* [host] */, int64_t dst_tokens,
+    int32_t layer_begin, int32_t layer_end,
+    const int32_t* src_pos, const int32_t* src_seq_offsets, const int32_t* dst_begin, int32_t num_seqs,
+    int64_t capacity, int32_t* status_word, void* cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -60,6 +60,9 @@ EXPORTS = (
     "sharpv_kv_calibrate_prune_noalloc",
     "sharpv_kv_prune_layers_workspace_bytes", "sharpv_kv_prune_layers", "sharpv_kv_compact",
     "sharpv_kv_compact_rope_workspace_bytes", "sharpv_kv_compact_rope",
+    "sharpv_tree_attention_workspace_bytes", "sharpv_tree_attention",
+    "sharpv_attention_mass_workspace_bytes", "sharpv_attention_mass",
+    "sharpv_evict_select", "sharpv_kv_append",
 )
 
 NOALLOC_MAX_SEQ_TOKENS = 262144
@@ -124,6 +127,21 @@ def lib():
     L.sharpv_kv_compact_rope.restype = C.c_int
     L.sharpv_kv_compact_rope.argtypes = [vp, C.POINTER(KVLayout), vp, C.POINTER(KVLayout), i32, i32, vp, vp, vp, i32,
                                          i64, i32, C.c_double, vp, sz, vp, vp]
+    lay = C.POINTER(KVLayout)
+    L.sharpv_tree_attention_workspace_bytes.restype = sz
+    L.sharpv_tree_attention_workspace_bytes.argtypes = [i32, i32]
+    L.sharpv_tree_attention.restype = C.c_int
+    L.sharpv_tree_attention.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, lay, i32, i64, i32, vp, vp, vp, i64, vp,
+                                        i32, f32, vp, vp, vp, sz, vp, vp]
+    L.sharpv_attention_mass_workspace_bytes.restype = sz
+    L.sharpv_attention_mass_workspace_bytes.argtypes = [i32, i64, i32]
+    L.sharpv_attention_mass.restype = C.c_int
+    L.sharpv_attention_mass.argtypes = [vp, i64, vp, vp, i32, vp, lay, i32, i64, i32, vp, vp, vp, i64, f32, f32, vp,
+                                        vp, vp, sz, vp, vp]
+    L.sharpv_evict_select.restype = C.c_int
+    L.sharpv_evict_select.argtypes = [vp, i64, i32, vp, vp, vp, i32, i32, vp, vp, vp, i64, vp, vp]
+    L.sharpv_kv_append.restype = C.c_int
+    L.sharpv_kv_append.argtypes = [vp, lay, i64, vp, lay, i64, i32, i32, vp, vp, vp, i32, i64, vp, vp]
     _lib = L
     return L
 
@@ -166,8 +184,11 @@ def _check(fn: str, rc: int):
 def _call(name: str, on: torch.Tensor, *args) -> int:
     """Calls the entry point `name` with the device of `on` current: kernels are launched on the current
     device, and the allocation-free entry point keys its built-in scratch on it."""
+    fn = getattr(_lib or lib(), name)
+    if on.device.index == torch.cuda.current_device():
+        return fn(*args)
     with torch.cuda.device(on.device):
-        return getattr(lib(), name)(*args)
+        return fn(*args)
 
 
 def _workspace(ws: Optional[torch.Tensor], nbytes: int, device) -> torch.Tensor:
@@ -489,4 +510,172 @@ def sharpv_kv_compact_rope(kv_src: torch.Tensor, kv_dst: torch.Tensor, kept_pos:
         _dev(seq_offsets, "seq_offsets", torch.int32), kept_seq_offsets.numel() - 1, capacity, int(rotary_dim),
         float(rope_base), ws.data_ptr(), ws.numel(), _dev(status_word, "status_word", torch.int32), _stream(stream))
     _check("sharpv_kv_compact_rope", rc)
+    return kv_dst
+
+
+# ------------------------------------------------------------------------------- decoding over the pruned cache
+def _on(t: torch.Tensor, name: str, device, dtype=None, shape=None) -> int:
+    """Address of a contiguous tensor of the given type and shape on the cache's device."""
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have the shape {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _heads(t: torch.Tensor, name: str, device, dtype, n: Optional[int], d: int, heads: Optional[int] = None) -> int:
+    """Row stride of a [nodes, heads, d] view whose heads lie next to each other."""
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, as the cache is")
+    if t.dim() != 3 or t.shape[2] != d or (n is not None and t.shape[0] != n) or \
+            (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must be [nodes, heads, head_dim]")
+    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d):
+        raise ValueError(f"{name} must have its heads next to each other")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * d
+
+
+def _queue(stream, device) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+
+
+def _cache(kv: torch.Tensor):
+    if not kv.is_cuda:
+        raise ValueError("kv must be a CUDA tensor")
+    return kv_layout(kv), kv.device
+
+
+def _sequences(seq_begin, seq_len, node_offsets, device):
+    B = seq_begin.numel()
+    return (B, _on(seq_begin, "seq_begin", device, torch.int32), _on(seq_len, "seq_len", device, torch.int32, (B,)),
+            _on(node_offsets, "node_offsets", device, torch.int32, (B + 1,)))
+
+
+def sharpv_tree_attention_workspace_bytes(num_seqs: int, head_dim: int) -> int:
+    return int(lib().sharpv_tree_attention_workspace_bytes(num_seqs, head_dim))
+
+
+def sharpv_tree_attention(q: torch.Tensor, kv: torch.Tensor, layer: int, seq_begin: torch.Tensor,
+                          seq_len: torch.Tensor, node_offsets: torch.Tensor, draft_k: Optional[torch.Tensor] = None,
+                          draft_v: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None,
+                          scale: Optional[float] = None, out: Optional[Dict[str, torch.Tensor]] = None,
+                          workspace=None, status_word=None, stream=None) -> Dict[str, torch.Tensor]:
+    """Attention of a step's query nodes q [nodes, q_heads, head_dim] over layer `layer` of the cache kv
+    [L, 2, H, T, head_dim] and the drafted tokens' own draft_k, draft_v [nodes, H, head_dim].  tree_mask: int32
+    [nodes, words], bit j of a row = the node sees node j of its sequence (None: nodes 0 .. i).  scale: None =
+    head_dim ** -0.5.  Returns dict(out [nodes, q_heads, head_dim], lse [nodes, q_heads])."""
+    lay, dev = _cache(kv)
+    D = lay.head_dim
+    ldq = _heads(q, "q", dev, kv.dtype, None, D)
+    N, HQ = q.shape[0], q.shape[1]
+    B, begin, length, offs = _sequences(seq_begin, seq_len, node_offsets, dev)
+    ldk = ldv = 0
+    if draft_k is not None:
+        ldk = _heads(draft_k, "draft_k", dev, kv.dtype, N, D, lay.num_kv_heads)
+    if draft_v is not None:
+        ldv = _heads(draft_v, "draft_v", dev, kv.dtype, N, D, lay.num_kv_heads)
+    words, mask = 0, None
+    if tree_mask is not None:
+        if tree_mask.dim() != 2 or tree_mask.shape[0] != N:
+            raise ValueError("tree_mask must be [nodes, words]")
+        words, mask = tree_mask.shape[1], _on(tree_mask, "tree_mask", dev, torch.int32)
+    if out is None:
+        out = {"out": torch.empty((N, HQ, D), dtype=q.dtype, device=dev),
+               "lse": torch.empty((N, HQ), dtype=torch.float32, device=dev)}
+    ws = _workspace(workspace, sharpv_tree_attention_workspace_bytes(B, D), dev)
+    rc = _call("sharpv_tree_attention", kv, q.data_ptr(), ldq,
+               None if draft_k is None else draft_k.data_ptr(), ldk, None if draft_v is None else draft_v.data_ptr(), ldv,
+               HQ, kv.data_ptr(), lay, layer, kv.shape[3], B, begin, length, offs, N, mask, words,
+               D ** -0.5 if scale is None else scale, _on(out["out"], "out", dev, q.dtype, (N, HQ, D)),
+               _on(out["lse"], "lse", dev, torch.float32, (N, HQ)), ws.data_ptr(), ws.numel(),
+               _dev(status_word, "status_word", torch.int32), _queue(stream, dev))
+    _check("sharpv_tree_attention", rc)
+    return out
+
+
+def sharpv_attention_mass_workspace_bytes(num_seqs: int, cache_tokens: int, num_kv_heads: int) -> int:
+    return int(lib().sharpv_attention_mass_workspace_bytes(num_seqs, cache_tokens, num_kv_heads))
+
+
+def sharpv_attention_mass(q: torch.Tensor, lse: torch.Tensor, kv: torch.Tensor, layer: int, seq_begin: torch.Tensor,
+                          seq_len: torch.Tensor, node_offsets: torch.Tensor, mass: Optional[torch.Tensor] = None,
+                          node_weight: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                          decay: float = 1.0, out: Optional[torch.Tensor] = None, workspace=None, status_word=None,
+                          stream=None) -> torch.Tensor:
+    """decay * mass + the attention weight that every cached row gets from the query nodes (summed over nodes and
+    query heads, nodes weighted by node_weight).  Returns out [T] (mass may be passed as out; without it a
+    tensor of zeros, so that rows outside the sequences have a value)."""
+    lay, dev = _cache(kv)
+    ldq = _heads(q, "q", dev, kv.dtype, None, lay.head_dim)
+    N, HQ = q.shape[0], q.shape[1]
+    B, begin, length, offs = _sequences(seq_begin, seq_len, node_offsets, dev)
+    T = kv.shape[3]
+    if out is None:
+        out = torch.zeros(T, dtype=torch.float32, device=dev)
+    ws = _workspace(workspace, sharpv_attention_mass_workspace_bytes(B, T, lay.num_kv_heads), dev)
+    rc = _call("sharpv_attention_mass", kv, q.data_ptr(), ldq, _on(lse, "lse", dev, torch.float32, (N, HQ)),
+               None if node_weight is None else _on(node_weight, "node_weight", dev, torch.float32, (N,)), HQ,
+               kv.data_ptr(), lay, layer, T, B, begin, length, offs, N,
+               lay.head_dim ** -0.5 if scale is None else scale, decay,
+               None if mass is None else _on(mass, "mass", dev, torch.float32, (T,)),
+               _on(out, "out", dev, torch.float32, (T,)), ws.data_ptr(), ws.numel(),
+               _dev(status_word, "status_word", torch.int32), _queue(stream, dev))
+    _check("sharpv_attention_mass", rc)
+    return out
+
+
+def sharpv_evict_select(mass: torch.Tensor, seq_begin: torch.Tensor, seq_len: torch.Tensor, budget: torch.Tensor,
+                        sink: int = 0, recent: int = 0, capacity: Optional[int] = None, want_mass: bool = True,
+                        out: Optional[Dict[str, torch.Tensor]] = None, status_word=None,
+                        stream=None) -> Dict[str, torch.Tensor]:
+    """The rows that stay of every sequence: its first `sink` and last `recent` rows before others, then the
+    highest mass.  capacity: None = the cache's rows.  Returns dict(kept_pos, kept_seq_offsets[, mass])."""
+    if not mass.is_cuda or mass.dim() != 1:
+        raise ValueError("mass must be a 1-D CUDA tensor")
+    dev, B = mass.device, seq_begin.numel()
+    if capacity is None:
+        capacity = mass.numel()
+    if out is None:
+        out = {"kept_pos": torch.empty(capacity, dtype=torch.int32, device=dev),
+               "kept_seq_offsets": torch.empty(B + 1, dtype=torch.int32, device=dev)}
+        if want_mass:
+            out["mass"] = torch.empty(capacity, dtype=torch.float32, device=dev)
+    kept_mass = out.get("mass")
+    rc = _call("sharpv_evict_select", mass, _on(mass, "mass", dev, torch.float32), mass.numel(), B,
+               _on(seq_begin, "seq_begin", dev, torch.int32), _on(seq_len, "seq_len", dev, torch.int32, (B,)),
+               _on(budget, "budget", dev, torch.int32, (B,)), sink, recent,
+               _on(out["kept_pos"], "kept_pos", dev, torch.int32, (capacity,)),
+               _on(out["kept_seq_offsets"], "kept_seq_offsets", dev, torch.int32, (B + 1,)),
+               None if kept_mass is None else _on(kept_mass, "out mass", dev, torch.float32, (capacity,)), capacity,
+               _dev(status_word, "status_word", torch.int32), _queue(stream, dev))
+    _check("sharpv_evict_select", rc)
+    return out
+
+
+def sharpv_kv_append(kv_src: torch.Tensor, kv_dst: torch.Tensor, src_pos: torch.Tensor, src_seq_offsets: torch.Tensor,
+                     dst_begin: torch.Tensor, capacity: Optional[int] = None, layer_begin: int = 0,
+                     layer_end: Optional[int] = None, status_word=None, stream=None) -> torch.Tensor:
+    """Copies, for every plane of the layers and every sequence b, the rows src_pos[src_seq_offsets[b] ..] of kv_src
+    [L, 2, H, T, D_h] to the rows of kv_dst from dst_begin[b] on.  Returns kv_dst."""
+    sl, dev = _cache(kv_src)
+    dl, ddev = _cache(kv_dst)
+    if dev != ddev or kv_src.dtype != kv_dst.dtype:
+        raise ValueError("kv_src and kv_dst must share device and dtype")
+    if capacity is None:
+        capacity = src_pos.numel()
+    if capacity > src_pos.numel():
+        raise ValueError("capacity is larger than src_pos")
+    B = dst_begin.numel()
+    rc = _call("sharpv_kv_append", kv_src, kv_src.data_ptr(), sl, kv_src.shape[3], kv_dst.data_ptr(), dl,
+               kv_dst.shape[3], layer_begin, kv_src.shape[0] if layer_end is None else layer_end,
+               _on(src_pos, "src_pos", dev, torch.int32), _on(src_seq_offsets, "src_seq_offsets", dev, torch.int32, (B + 1,)),
+               _on(dst_begin, "dst_begin", dev, torch.int32), B, capacity,
+               _dev(status_word, "status_word", torch.int32), _queue(stream, dev))
+    _check("sharpv_kv_append", rc)
     return kv_dst

@@ -3,9 +3,9 @@
 
 // 1xx: release build, 2xx: built with -DSHARPV_DEBUG_BOUNDS (every gather / scatter index range-checked)
 #ifdef SHARPV_DEBUG_BOUNDS
-extern "C" int sharpv_version(void) { return 201; }
+extern "C" int sharpv_version(void) { return 202; }
 #else
-extern "C" int sharpv_version(void) { return 101; }
+extern "C" int sharpv_version(void) { return 102; }
 #endif
 
 extern "C" const char* sharpv_status_string(sharpv_status s) {

@@ -1,0 +1,180 @@
+// What the operators that decode over a K/V cache share: the sequence tables (where a sequence's rows sit in
+// the cache, which query nodes are its own) with their range checks, and the split of an attention call into
+// units that the resident CTAs share evenly.
+#pragma once
+
+#include "common.cuh"
+
+namespace sharpv {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
+
+struct SeqTables {
+    const int32_t* begin;       // first cache row of sequence b
+    const int32_t* len;         // its rows
+    const int32_t* node_off;    // its nodes: [node_off[b], node_off[b + 1])
+    int num_seqs;
+    int64_t cache_tokens;       // rows a plane of the cache holds
+    int64_t total_nodes;
+};
+
+struct SeqInfo {
+    int64_t begin;
+    int len, node0, nodes;
+};
+
+// Entry b of the tables, cut to what the cache and the node arrays hold; `bad` is set if something was cut.
+__device__ __forceinline__ SeqInfo load_seq(const SeqTables& t, int b, bool& bad) {
+    SeqInfo s;
+    const int64_t begin = __ldg(t.begin + b), len = __ldg(t.len + b);
+    const int64_t n0 = __ldg(t.node_off + b), n1 = __ldg(t.node_off + b + 1);
+    s.begin = begin < 0 ? 0 : (begin > t.cache_tokens ? t.cache_tokens : begin);
+    int64_t l = begin < 0 || len < 0 ? 0 : len;
+    if (l > t.cache_tokens - s.begin) l = t.cache_tokens - s.begin;
+    s.len = (int)l;
+    const int64_t a = n0 < 0 ? 0 : (n0 > t.total_nodes ? t.total_nodes : n0);
+    const int64_t e = n1 < a ? a : (n1 > t.total_nodes ? t.total_nodes : n1);
+    s.node0 = (int)a;
+    s.nodes = (int)(e - a);
+    bad = bad || s.begin != begin || l != len || a != n0 || e != n1;
+    return s;
+}
+
+// The split of an attention call.  A segment is one (sequence, KV head, tile of `rows` query rows); a query
+// row is a (node, query head of the KV head's group) pair, nodes outermost.  A segment's keys are its cached rows
+// in tiles of `keys`, then its drafted tokens in tiles of `keys`; a unit is one such key tile of one segment,
+// numbered with the key tile innermost.  CTA c of G takes the units [c U / G, (c + 1) U / G): every CTA has the
+// same number of key tiles whatever the lengths, and the segments it shares with its neighbours are joined
+// from partial results afterwards.
+struct Split {
+    int rows, keys, group, heads;
+    int draft;                  // the drafted tokens' keys take part
+    __host__ __device__ int row_tiles(const SeqInfo& s) const {
+        return (int)(((int64_t)s.nodes * group + rows - 1) / rows);
+    }
+    __host__ __device__ int cache_tiles(const SeqInfo& s) const { return (s.len + keys - 1) / keys; }
+    // at least one (then empty), so that rows without any key are written as well
+    __host__ __device__ int key_tiles(const SeqInfo& s) const {
+        const int n = cache_tiles(s) + (draft ? (s.nodes + keys - 1) / keys : 0);
+        return n > 0 ? n : 1;
+    }
+    __host__ __device__ int64_t units(const SeqInfo& s) const {
+        return s.nodes == 0 ? 0 : (int64_t)row_tiles(s) * heads * key_tiles(s);
+    }
+};
+
+// The CTAs that take part: no more than there are units, so that each of them has at least one.
+__device__ __forceinline__ int64_t busy_ctas(int64_t units, int64_t ctas) { return units < ctas ? units : ctas; }
+
+// first unit of CTA c, and the CTA that owns unit u
+__device__ __forceinline__ int64_t cta_first_unit(int64_t c, int64_t units, int64_t ctas) { return c * units / ctas; }
+__device__ __forceinline__ int unit_owner(int64_t u, int64_t units, int64_t ctas) {
+    return (int)(((u + 1) * ctas - 1) / units);
+}
+
+struct PlanStart {
+    int64_t first, end;         // the CTA's units
+    int b;                      // sequence of the first one
+    int64_t before;             // units in front of that sequence
+};
+
+// Every thread of the block (NT threads) gets the plan of this CTA.  CTA 0 also writes prefix[0..num_seqs],
+// the units in front of every sequence, for the kernel that joins the partial results, and reports tables
+// that do not fit.  
+template <int NT>
+struct PlanScratch {
+    int64_t warp[NT / 32 + 1];
+    PlanStart start;
+};
+
+template <int NT>
+__device__ __forceinline__ PlanStart plan_cta(const SeqTables& t, const Split& sp, int cta, int ctas,
+                                              PlanScratch<NT>& sm, int64_t* prefix, int32_t* status_word) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int per = (t.num_seqs + NT - 1) / NT;
+    const int lo = min(t.num_seqs, (int)threadIdx.x * per), hi = min(t.num_seqs, lo + per);
+    int64_t sum = 0;
+    bool bad = false;
+    for (int b = lo; b < hi; ++b) sum += sp.units(load_seq(t, b, bad));
+    int64_t inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t n = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += n;
+    }
+    if (lane == 31) sm.warp[warp] = inc;
+    if (threadIdx.x == 0) sm.start = PlanStart{0, 0, 0, 0};
+    __syncthreads();
+    int64_t before = inc - sum, total = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) {
+        const int64_t v = sm.warp[w];
+        if (w < warp) before += v;
+        total += v;
+    }
+    const int64_t busy = busy_ctas(total, ctas);
+    const int64_t first = cta < busy ? cta_first_unit(cta, total, busy) : total;
+    int64_t run = before;
+    for (int b = lo; b < hi; ++b) {
+        const int64_t u = sp.units(load_seq(t, b, bad));
+        if (cta == 0 && prefix) prefix[b] = run;
+        if (first >= run && first < run + u) {
+            sm.start.b = b;
+            sm.start.before = run;
+        }
+        run += u;
+    }
+    if (threadIdx.x == 0) {
+        sm.start.first = first;
+        sm.start.end = cta < busy ? cta_first_unit(cta + 1, total, busy) : total;
+        if (cta == 0 && prefix) prefix[t.num_seqs] = total;
+    }
+    if (cta == 0 && bad) report(status_word, SHARPV_ERR_BOUNDS);
+    __syncthreads();
+    return sm.start;
+}
+
+// Where a portion (the units of one segment that one CTA works on) leaves its partial result: slot 1 of the CTA
+// if the portion starts at the segment's first key tile, else slot 0.  A CTA has at most one of each.
+__device__ __forceinline__ int portion_slot(int cta, int first_key_tile) { return cta * 2 + (first_key_tile == 0); }
+
+// 16 bytes from global to shared memory without passing registers; zeros where `valid` is false
+__device__ __forceinline__ void cp_async16(void* smem, const void* gmem, bool valid) {
+    const unsigned dst = (unsigned)__cvta_generic_to_shared(smem);
+    const int n = valid ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(gmem), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
+
+__device__ __forceinline__ bool finite_f32(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+// The layout checks of the calls that read a cache through its layout struct (the same as the compaction's).
+inline sharpv_status kv_layout_status(const void* kv, const sharpv_kv_layout* L, bool computes) {
+    if (!kv || !L) return SHARPV_ERR_INVALID_ARG;
+    if (computes ? !dtype_ok(L->dtype) : !copy_dtype_ok(L->dtype)) return SHARPV_ERR_UNSUPPORTED;
+    if (L->num_layers < 1 || L->num_kv_heads < 1 || L->head_dim < 1 || L->stride_layer < 0 || L->stride_kv < 0 ||
+        L->stride_head < 0 || L->stride_token < L->head_dim)
+        return SHARPV_ERR_INVALID_ARG;
+    const int64_t eb = elem_bytes(L->dtype);
+    if ((L->head_dim * eb) % 16 || (L->stride_layer * eb) % 16 || (L->stride_kv * eb) % 16 ||
+        (L->stride_head * eb) % 16 || (L->stride_token * eb) % 16 || !aligned16(kv))
+        return SHARPV_ERR_UNSUPPORTED;
+    return SHARPV_OK;
+}
+
+inline sharpv_status current_sms(int& sms) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) {
+        (void)cudaGetLastError();
+        return SHARPV_ERR_CUDA;
+    }
+    return SHARPV_OK;
+}
+
+}  // namespace sharpv

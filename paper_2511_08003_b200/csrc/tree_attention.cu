@@ -1,0 +1,426 @@
+// Attention of drafted tokens over a K/V cache (sharpv_tree_attention).
+//
+//   s_rj = scale q_r . k_j over the cached rows of the row's sequence and the drafted tokens its node sees,
+//   out_r = sum_j exp(s_rj - m_r) v_j / l_r,   l_r = sum_j exp(s_rj - m_r),   lse_r = m_r + ln l_r.
+//
+// Kernels:
+//   attn_simt_kernel      one pass over the keys with a running maximum and sum per row, on the fp32 units
+//   attn_join_kernel      (dependent launch) joins the partial results of segments that several CTAs share
+#include "tree_attention.cuh"
+
+#include <cuda_bf16.h>
+
+namespace sharpv {
+namespace {
+
+constexpr int kSimtThreads = 128;
+constexpr int kSimtKeys = 32;           // keys of a tile: one per lane
+
+template <int DT> struct Store;
+template <> struct Store<SHARPV_F32> {
+    using T = float;
+    __device__ __forceinline__ static T from(float x) { return x; }
+};
+template <> struct Store<SHARPV_BF16> {
+    using T = __nv_bfloat16;
+    __device__ __forceinline__ static T from(float x) { return __float2bfloat16_rn(x); }
+};
+
+template <int R, int DP>
+struct SimtShared {
+    float q[R][DP];
+    float k[2][kSimtKeys][DP + 4];      // 4 words of padding: lanes read 16 bytes of 32 rows without bank conflicts
+    float v[2][kSimtKeys][DP];
+    float p[R][kSimtKeys];
+    float alpha[R], m[R], l[R];
+    PlanScratch<kSimtThreads> plan;
+};
+
+// One tile of up to 32 rows of `src` (byte stride `row_bytes`, `valid` of them, D elements each) into shared memory
+// as fp32, the rest zero.
+template <int DT, int DP, int PITCH>
+__device__ __forceinline__ void simt_load(float (&dst)[kSimtKeys][PITCH], const char* src, int64_t row_bytes, int valid,
+                                          int D) {
+    using E = Elem<DT>;
+    constexpr int VPR = DP / E::kPerVec;
+    for (int x = threadIdx.x; x < kSimtKeys * VPR; x += kSimtThreads) {
+        const int j = x / VPR, c = (x % VPR) * E::kPerVec;
+        const bool there = j < valid && c < D;
+        const char* from = src + (there ? (int64_t)j * row_bytes + (int64_t)c * E::kBytes : 0);
+        if constexpr (DT == SHARPV_F32) {
+            cp_async16(&dst[j][c], from, there);
+        } else {
+            float w[E::kPerVec];
+            E::widen(there ? ld_stream(from) : make_uint4(0, 0, 0, 0), w);
+#pragma unroll
+            for (int i = 0; i < E::kPerVec; ++i) dst[j][c + i] = w[i];
+        }
+    }
+}
+
+// Warp w owns the rows w R/4 .. of the tile: lane = key when scores are formed, so a row's maximum and sum are warp
+// reductions; for the weighted sums a thread owns columns (col0, col0 + 128, ...) of RPT rows.
+template <int DT, int R, int DP>
+__global__ void __launch_bounds__(kSimtThreads)
+attn_simt_kernel(const __grid_constant__ AttnArgs a) {
+    using E = Elem<DT>;
+    using St = Store<DT>;
+    extern __shared__ __align__(16) char smem_raw[];
+    auto& sm = *reinterpret_cast<SimtShared<R, DP>*>(smem_raw);
+    constexpr int RW = R / 4;                               // rows of a warp
+    constexpr int COLS = DP < 128 ? DP : 128, CPT = DP / COLS, RG = kSimtThreads / COLS, RPT = R / RG;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int col0 = threadIdx.x % COLS, row0 = threadIdx.x / COLS * RPT;
+    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
+    cudaGridDependencySynchronize();
+    const PlanStart plan = plan_cta<kSimtThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, a.prefix, a.status_word);
+    int64_t u = plan.first;
+    const int64_t u_end = plan.end;
+    int b = plan.b;
+    int64_t before = plan.before;
+    bool bad = false;
+    while (u < u_end) {
+        const SeqInfo s = load_seq(a.seqs, b, bad);
+        const int64_t mine = a.split.units(s);
+        if (u - before >= mine) {               // on to the next sequence (those without nodes have no units)
+            before += mine;
+            ++b;
+            continue;
+        }
+        const int kt_all = a.split.key_tiles(s), kt_cache = a.split.cache_tiles(s), rts = a.split.row_tiles(s);
+        const int64_t seg = (u - before) / kt_all;
+        const int kt0 = (int)((u - before) % kt_all);
+        const int kt1 = (int)min((int64_t)kt_all, kt0 + (u_end - u));
+        const int h = (int)(seg / rts), rt = (int)(seg % rts);
+        const int r_base = rt * R, r_all = s.nodes * G;
+        u += kt1 - kt0;
+
+        auto load_tile = [&](int kt, int buf) {
+            const char *k, *v;
+            int64_t kb, vb;
+            int valid;
+            if (kt < kt_cache) {
+                const int64_t at = (int64_t)h * a.kv_head + (s.begin + (int64_t)kt * kSimtKeys) * a.kv_token;
+                k = a.cache_k + at; v = a.cache_v + at; kb = vb = a.kv_token;
+                valid = s.len - kt * kSimtKeys;
+            } else {
+                const int j0 = (kt - kt_cache) * kSimtKeys;
+                const int64_t hb = (int64_t)h * D * E::kBytes;
+                k = a.draft_k + (int64_t)(s.node0 + j0) * a.dk_node + hb; kb = a.dk_node;
+                v = a.draft_v + (int64_t)(s.node0 + j0) * a.dv_node + hb; vb = a.dv_node;
+                valid = a.split.draft ? s.nodes - j0 : 0;
+            }
+            simt_load<DT, DP>(sm.k[buf], k, kb, valid, D);
+            simt_load<DT, DP>(sm.v[buf], v, vb, valid, D);
+            cp_async_commit();
+        };
+
+        __syncthreads();                        // the previous portion's buffers are free
+        load_tile(kt0, 0);
+        constexpr int VPR = DP / E::kPerVec;
+        for (int x = threadIdx.x; x < R * VPR; x += kSimtThreads) {
+            const int r = x / VPR, c = (x % VPR) * E::kPerVec, row = r_base + r;
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (row < r_all && c < D)
+                w = ld_cached(a.q + (int64_t)(s.node0 + row / G) * a.q_node + ((int64_t)(h * G + row % G) * D + c) * E::kBytes);
+            float f[E::kPerVec];
+            E::widen(w, f);
+#pragma unroll
+            for (int i = 0; i < E::kPerVec; ++i) sm.q[r][c + i] = f[i];
+        }
+        float m[RW], l[RW], o[RPT][CPT];
+#pragma unroll
+        for (int i = 0; i < RW; ++i) { m[i] = neg_inf(); l[i] = 0.f; }
+#pragma unroll
+        for (int i = 0; i < RPT; ++i)
+#pragma unroll
+            for (int c = 0; c < CPT; ++c) o[i][c] = 0.f;
+
+        for (int kt = kt0; kt < kt1; ++kt) {
+            const int buf = (kt - kt0) & 1;
+            if (kt + 1 < kt1) {
+                load_tile(kt + 1, buf ^ 1);
+                cp_async_wait<1>();
+            } else {
+                cp_async_wait<0>();
+            }
+            __syncthreads();
+            float acc[RW];
+#pragma unroll
+            for (int i = 0; i < RW; ++i) acc[i] = 0.f;
+            for (int c = 0; c < D; c += 4) {
+                const float4 k4 = *reinterpret_cast<const float4*>(&sm.k[buf][lane][c]);
+#pragma unroll
+                for (int i = 0; i < RW; ++i) {
+                    const float4 q4 = *reinterpret_cast<const float4*>(&sm.q[warp * RW + i][c]);
+                    acc[i] = fmaf(q4.x, k4.x, fmaf(q4.y, k4.y, fmaf(q4.z, k4.z, fmaf(q4.w, k4.w, acc[i]))));
+                }
+            }
+            const bool drafted = kt >= kt_cache;
+            const int left = drafted ? 0 : s.len - kt * kSimtKeys;
+#pragma unroll
+            for (int i = 0; i < RW; ++i) {
+                const int row = r_base + warp * RW + i;
+                bool sees = lane < left;
+                if (drafted) {
+                    sees = false;
+                    if (a.split.draft && row < r_all)
+                        sees = draft_sees(a, s, row / G, (kt - kt_cache) * kSimtKeys) >> lane & 1;
+                }
+                const float x = sees ? acc[i] * a.scale_log2 : neg_inf();
+                float top = x;
+#pragma unroll
+                for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+                top = fmaxf(top, m[i]);
+                const float p = sees ? exp2f(x - (top == neg_inf() ? 0.f : top)) : 0.f;
+                const float al = m[i] == top ? 1.f : exp2f(m[i] - top);
+                l[i] = l[i] * al + warp_sum(p);
+                m[i] = top;
+                sm.p[warp * RW + i][lane] = sees ? p : -1.f;      // -1: not seen, its value row is not looked at
+                if (lane == 0) sm.alpha[warp * RW + i] = al;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < RPT; ++i) {
+                const float al = sm.alpha[row0 + i];
+#pragma unroll
+                for (int c = 0; c < CPT; ++c) o[i][c] *= al;
+            }
+            const bool whole = !drafted && left >= kSimtKeys;
+            for (int j = 0; j < kSimtKeys; j += 4) {
+                float v[4][CPT];
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+#pragma unroll
+                    for (int c = 0; c < CPT; ++c) v[y][c] = sm.v[buf][j + y][col0 + c * COLS];
+#pragma unroll
+                for (int i = 0; i < RPT; ++i) {
+                    const float4 p4 = *reinterpret_cast<const float4*>(&sm.p[row0 + i][j]);
+                    const float p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+#pragma unroll
+                        for (int c = 0; c < CPT; ++c) {
+                            const float n = fmaf(p[y], v[y][c], o[i][c]);
+                            o[i][c] = whole || !(p[y] < 0.f) ? n : o[i][c];
+                        }
+                }
+            }
+            __syncthreads();
+        }
+        if (lane == 0) {
+#pragma unroll
+            for (int i = 0; i < RW; ++i) { sm.m[warp * RW + i] = m[i]; sm.l[warp * RW + i] = l[i]; }
+        }
+        __syncthreads();
+        const bool complete = kt0 == 0 && kt1 == kt_all;
+        const int slot = portion_slot(blockIdx.x, kt0);
+        if (!complete && threadIdx.x < R) {
+            a.part_ml[((int64_t)slot * 2) * R + threadIdx.x] = sm.m[threadIdx.x];
+            a.part_ml[((int64_t)slot * 2 + 1) * R + threadIdx.x] = sm.l[threadIdx.x];
+        }
+        if (complete && threadIdx.x < R && r_base + (int)threadIdx.x < r_all) {
+            const int row = r_base + threadIdx.x;
+            a.lse[(int64_t)(s.node0 + row / G) * HQ + h * G + row % G] = row_lse(sm.m[threadIdx.x], sm.l[threadIdx.x]);
+        }
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+            const int row = r_base + row0 + i;
+            if (row >= r_all) continue;
+#pragma unroll
+            for (int c = 0; c < CPT; ++c) {
+                const int col = col0 + c * COLS;
+                if (col >= D) continue;
+                if (complete)
+                    reinterpret_cast<typename St::T*>(a.out)[((int64_t)(s.node0 + row / G) * HQ + h * G + row % G) * D + col] =
+                        St::from(o[i][c] * row_scale(sm.l[row0 + i]));
+                else
+                    a.part_o[((int64_t)slot * R + row0 + i) * D + col] = o[i][c];
+            }
+        }
+    }
+}
+
+// One warp per output row of a segment that more than one CTA worked on: the partial results' running maxima and sums
+// are brought to the common maximum, the weighted sums added in the order of the CTAs (fixed, so results do not
+// depend on scheduling), divided, rounded once.
+template <int DT>
+__global__ void __launch_bounds__(256)
+attn_join_kernel(const __grid_constant__ AttnArgs a) {
+    using St = Store<DT>;
+    const int lane = threadIdx.x & 31;
+    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G, R = a.split.rows;
+    const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    cudaGridDependencySynchronize();
+    const int64_t node = w / HQ;
+    if (node >= a.seqs.total_nodes) return;
+    const int qh = (int)(w % HQ), h = qh / G;
+    const int64_t units = a.prefix[a.seqs.num_seqs], busy = busy_ctas(units, a.ctas);
+    if (units == 0) return;
+    const int b = upper_segment(a.seqs.node_off, a.seqs.num_seqs, (int)node);
+    bool bad = false;
+    const SeqInfo s = load_seq(a.seqs, b, bad);
+    if (node < s.node0 || node >= s.node0 + s.nodes) return;       // no sequence's node: left as it is
+    const int row = (int)(node - s.node0) * G + qh % G;
+    const int rt = row / R, r = row % R;
+    const int kts = a.split.key_tiles(s);
+    const int64_t u0 = a.prefix[b] + ((int64_t)h * a.split.row_tiles(s) + rt) * kts;
+    const int c0 = unit_owner(u0, units, busy), c1 = unit_owner(u0 + kts - 1, units, busy);
+    if (c0 == c1) return;                                           // written by that CTA
+    float top = neg_inf();
+    for (int c = c0 + lane; c <= c1; c += 32) {
+        const int slot = c * 2 + (c == c0);
+        top = fmaxf(top, a.part_ml[(int64_t)slot * 2 * R + r]);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float base = top == neg_inf() ? 0.f : top;
+    float sum = 0.f;
+    float acc[kMaxHeadDim / 32];
+#pragma unroll
+    for (int i = 0; i < kMaxHeadDim / 32; ++i) acc[i] = 0.f;
+    for (int c = c0; c <= c1; c += 32) {
+        float f = 0.f;
+        if (c + lane <= c1) {
+            const int slot = (c + lane) * 2 + (c + lane == c0);
+            const float l = a.part_ml[((int64_t)slot * 2 + 1) * R + r];
+            f = exp2f(a.part_ml[(int64_t)slot * 2 * R + r] - base);
+            sum += l * f;
+        }
+        const int n = min(32, c1 - c + 1);
+        for (int i = 0; i < n; ++i) {
+            const float fi = __shfl_sync(0xffffffffu, f, i);
+            const float* o = a.part_o + ((int64_t)((c + i) * 2 + (c + i == c0)) * R + r) * D;
+#pragma unroll
+            for (int k = 0; k < kMaxHeadDim / 128; ++k) {
+                const int col = k * 128 + lane * 4;
+                if (col < D) {
+                    const float4 v = __ldcg(reinterpret_cast<const float4*>(o + col));
+                    acc[k * 4 + 0] = fmaf(fi, v.x, acc[k * 4 + 0]);
+                    acc[k * 4 + 1] = fmaf(fi, v.y, acc[k * 4 + 1]);
+                    acc[k * 4 + 2] = fmaf(fi, v.z, acc[k * 4 + 2]);
+                    acc[k * 4 + 3] = fmaf(fi, v.w, acc[k * 4 + 3]);
+                }
+            }
+        }
+    }
+    sum = warp_sum(sum);
+    const float inv = row_scale(sum);
+    auto* out = reinterpret_cast<typename St::T*>(a.out) + (node * HQ + qh) * D;
+#pragma unroll
+    for (int k = 0; k < kMaxHeadDim / 128; ++k) {
+        const int col = k * 128 + lane * 4;
+        if (col < D) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out[col + i] = St::from(acc[k * 4 + i] * inv);
+        }
+    }
+    if (lane == 0) a.lse[node * HQ + qh] = row_lse(top, sum);
+}
+
+template <int DT, int R, int DP>
+sharpv_status simt_launch(AttnArgs a, int sms, cudaStream_t stream) {
+    auto kern = attn_simt_kernel<DT, R, DP>;
+    const size_t smem = sizeof(SimtShared<R, DP>);
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SHARPV_ERR_CUDA;
+    }
+    const int per_sm = smem * 2 <= 220 * 1024 ? 2 : 1;
+    a.ctas = min(sms * per_sm, kMaxAttnCtas);
+    if (launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kSimtThreads), smem, stream, a) != cudaSuccess ||
+        launch_dependent(attn_join_kernel<DT>, dim3((unsigned)((a.seqs.total_nodes * a.split.heads * a.split.group + 7) / 8)),
+                         dim3(256), 0, stream, a) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SHARPV_ERR_CUDA;
+    }
+    return SHARPV_OK;
+}
+
+template <int DT, int R>
+sharpv_status simt_by_dim(const AttnArgs& a, int sms, cudaStream_t stream) {
+    if (a.head_dim <= 64) return simt_launch<DT, R, 64>(a, sms, stream);
+    if (a.head_dim <= 128) return simt_launch<DT, R, 128>(a, sms, stream);
+    return simt_launch<DT, R, 256>(a, sms, stream);
+}
+
+// query rows of a tile, and bytes of the workspace
+constexpr int kMaxTileRows = 32;
+size_t prefix_bytes(int32_t num_seqs) { return align_up((size_t)(num_seqs + 1) * 8, 256); }
+size_t part_ml_bytes() { return align_up((size_t)kMaxAttnCtas * 2 * 2 * kMaxTileRows * 4, 256); }
+size_t part_o_bytes(int32_t head_dim) { return align_up((size_t)kMaxAttnCtas * 2 * kMaxTileRows * head_dim * 4, 256); }
+
+}  // namespace
+}  // namespace sharpv
+
+using namespace sharpv;
+
+extern "C" size_t sharpv_tree_attention_workspace_bytes(int32_t num_seqs, int32_t head_dim) {
+    if (num_seqs < 0) num_seqs = 0;
+    if (head_dim < 1) head_dim = 1;
+    if (head_dim > kMaxHeadDim) head_dim = kMaxHeadDim;
+    return prefix_bytes(num_seqs) + part_ml_bytes() + part_o_bytes(head_dim);
+}
+
+extern "C" sharpv_status sharpv_tree_attention(
+    const void* q, int64_t ld_q, const void* draft_k, int64_t ld_draft_k, const void* draft_v, int64_t ld_draft_v,
+    int32_t num_q_heads, const void* kv, const sharpv_kv_layout* layout, int32_t layer, int64_t cache_tokens,
+    int32_t num_seqs, const int32_t* seq_begin, const int32_t* seq_len, const int32_t* node_offsets,
+    int64_t total_nodes, const uint32_t* tree_mask, int32_t mask_words, float scale, void* out, float* out_lse,
+    void* workspace, size_t workspace_bytes, int32_t* status_word, void* cuda_stream) {
+    const sharpv_status ls = kv_layout_status(kv, layout, true);
+    if (ls != SHARPV_OK) return ls;
+    const int D = layout->head_dim, H = layout->num_kv_heads;
+    const int64_t eb = elem_bytes(layout->dtype);
+    if (layer < 0 || layer >= layout->num_layers || cache_tokens < 0 || num_seqs < 0 || total_nodes < 0 ||
+        num_q_heads < 1 || num_q_heads % H != 0 || (draft_k == nullptr) != (draft_v == nullptr) ||
+        mask_words < 0 || !(scale > 0.f) || !(scale < __builtin_huge_valf()))
+        return SHARPV_ERR_INVALID_ARG;
+    if (D > kMaxHeadDim || cache_tokens >= (int64_t)1 << 31 || total_nodes * num_q_heads >= (int64_t)1 << 31)
+        return SHARPV_ERR_UNSUPPORTED;
+    if (num_seqs == 0 || total_nodes == 0) return SHARPV_OK;
+    if (!q || !seq_begin || !seq_len || !node_offsets || !out || !out_lse || (tree_mask && mask_words < 1) ||
+        ld_q < (int64_t)num_q_heads * D || (draft_k && (ld_draft_k < (int64_t)H * D || ld_draft_v < (int64_t)H * D)))
+        return SHARPV_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(out) || (ld_q * eb) % 16 ||
+        (draft_k && (!aligned16(draft_k) || !aligned16(draft_v) || (ld_draft_k * eb) % 16 || (ld_draft_v * eb) % 16)))
+        return SHARPV_ERR_UNSUPPORTED;
+    if (workspace_bytes < sharpv_tree_attention_workspace_bytes(num_seqs, D)) return SHARPV_ERR_WORKSPACE;
+    if (!workspace) return SHARPV_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(workspace) % 256) return SHARPV_ERR_UNSUPPORTED;
+
+    AttnArgs a = {};
+    a.q = (const char*)q;
+    a.q_node = ld_q * eb;
+    a.cache_k = (const char*)kv + (int64_t)layer * layout->stride_layer * eb;
+    a.cache_v = a.cache_k + layout->stride_kv * eb;
+    a.kv_head = layout->stride_head * eb;
+    a.kv_token = layout->stride_token * eb;
+    a.draft_k = (const char*)draft_k;
+    a.draft_v = (const char*)draft_v;
+    a.dk_node = ld_draft_k * eb;
+    a.dv_node = ld_draft_v * eb;
+    a.mask = tree_mask;
+    a.mask_words = mask_words;
+    a.head_dim = D;
+    a.scale_log2 = scale * kLog2e;
+    a.out = out;
+    a.lse = out_lse;
+    a.seqs = SeqTables{seq_begin, seq_len, node_offsets, num_seqs, cache_tokens, total_nodes};
+    const int group = num_q_heads / H;
+    // rows of a tile by the average rows of a (sequence, KV head)
+    const int64_t avg = total_nodes * group / num_seqs;
+    a.split = Split{avg <= 8 ? 8 : 32, kSimtKeys, group, H, draft_k != nullptr};
+    char* ws = (char*)workspace;
+    a.prefix = (int64_t*)ws;
+    a.part_ml = (float*)(ws + prefix_bytes(num_seqs));
+    a.part_o = (float*)(ws + prefix_bytes(num_seqs) + part_ml_bytes());
+    a.status_word = status_word;
+    int sms = 0;
+    const sharpv_status ss = current_sms(sms);
+    if (ss != SHARPV_OK) return ss;
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    if (layout->dtype == SHARPV_F32)
+        return avg <= 8 ? simt_by_dim<SHARPV_F32, 8>(a, sms, stream) : simt_by_dim<SHARPV_F32, 32>(a, sms, stream);
+    return avg <= 8 ? simt_by_dim<SHARPV_BF16, 8>(a, sms, stream) : simt_by_dim<SHARPV_BF16, 32>(a, sms, stream);
+}

@@ -1,0 +1,55 @@
+// Arguments that the kernels of the attention over a cache share.
+#pragma once
+
+#include "decode_common.cuh"
+
+namespace sharpv {
+
+constexpr int kMaxAttnCtas = 2 * 160;       // resident CTAs a call may use; sizes the workspace
+constexpr int kMaxHeadDim = 256;
+
+struct AttnArgs {
+    const char* q;              // [nodes, heads * group, D]; byte strides between nodes
+    int64_t q_node;
+    const char* cache_k;        // the layer's K and V blocks
+    const char* cache_v;
+    int64_t kv_head, kv_token;  // bytes
+    const char* draft_k;        // [nodes, heads, D], or null
+    const char* draft_v;
+    int64_t dk_node, dv_node;   // bytes
+    const uint32_t* mask;       // [nodes, mask_words]: bit j of a row = the node sees node j of its sequence; null: j <= i
+    int mask_words;
+    int head_dim;               // elements
+    float scale_log2;           // scale * log2(e): scores are kept in units of log 2
+    void* out;                  // [nodes, heads * group, D]
+    float* lse;                 // [nodes, heads * group]
+    SeqTables seqs;
+    Split split;
+    // workspace
+    int64_t* prefix;            // [num_seqs + 1]
+    float* part_ml;             // [slots][2][rows]: running maximum and sum of each row
+    float* part_o;              // [slots][rows][D]: weighted sums, not yet divided
+    int ctas;
+    int32_t* status_word;
+};
+
+// Which keys of the 32 from key0 on node `i` of a sequence sees, as bits (drafted tokens).
+__device__ __forceinline__ uint32_t draft_sees(const AttnArgs& a, const SeqInfo& s, int i, int key0) {
+    const int left = s.nodes - key0;
+    if (left <= 0) return 0u;
+    const uint32_t there = left >= 32 ? 0xffffffffu : (1u << left) - 1u;
+    uint32_t sees;
+    if (a.mask == nullptr) {
+        const int upto = i - key0;              // keys key0 .. i
+        sees = upto < 0 ? 0u : (upto >= 31 ? 0xffffffffu : (2u << upto) - 1u);
+    } else {
+        sees = key0 / 32 < a.mask_words ? __ldg(a.mask + ((int64_t)s.node0 + i) * a.mask_words + key0 / 32) : 0u;
+    }
+    return sees & there;
+}
+
+// out and lse of one row element from its weighted sum, running maximum (log 2 units) and sum
+__device__ __forceinline__ float row_scale(float l) { return l == 0.f ? 0.f : 1.0f / l; }
+__device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? neg_inf() : (m + log2f(l)) * kLn2; }
+
+}  // namespace sharpv
