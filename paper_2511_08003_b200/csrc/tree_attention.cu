@@ -319,7 +319,7 @@ attn_join_kernel(const __grid_constant__ AttnArgs a) {
 }
 
 template <int DT, int R, int DP>
-sharpv_status simt_launch(AttnArgs a, int sms, cudaStream_t stream) {
+sharpv_status simt_launch(AttnArgs& a, int sms, cudaStream_t stream) {
     auto kern = attn_simt_kernel<DT, R, DP>;
     const size_t smem = sizeof(SimtShared<R, DP>);
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
@@ -328,9 +328,17 @@ sharpv_status simt_launch(AttnArgs a, int sms, cudaStream_t stream) {
     }
     const int per_sm = smem * 2 <= 220 * 1024 ? 2 : 1;
     a.ctas = min(sms * per_sm, kMaxAttnCtas);
-    if (launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kSimtThreads), smem, stream, a) != cudaSuccess ||
-        launch_dependent(attn_join_kernel<DT>, dim3((unsigned)((a.seqs.total_nodes * a.split.heads * a.split.group + 7) / 8)),
-                         dim3(256), 0, stream, a) != cudaSuccess) {
+    if (launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kSimtThreads), smem, stream, a) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SHARPV_ERR_CUDA;
+    }
+    return SHARPV_OK;
+}
+
+template <int DT>
+sharpv_status join_launch(const AttnArgs& a, cudaStream_t stream) {
+    const int64_t rows = a.seqs.total_nodes * a.split.heads * a.split.group;
+    if (launch_dependent(attn_join_kernel<DT>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, stream, a) != cudaSuccess) {
         (void)cudaGetLastError();
         return SHARPV_ERR_CUDA;
     }
@@ -338,7 +346,7 @@ sharpv_status simt_launch(AttnArgs a, int sms, cudaStream_t stream) {
 }
 
 template <int DT, int R>
-sharpv_status simt_by_dim(const AttnArgs& a, int sms, cudaStream_t stream) {
+sharpv_status simt_by_dim(AttnArgs& a, int sms, cudaStream_t stream) {
     if (a.head_dim <= 64) return simt_launch<DT, R, 64>(a, sms, stream);
     if (a.head_dim <= 128) return simt_launch<DT, R, 128>(a, sms, stream);
     return simt_launch<DT, R, 256>(a, sms, stream);
@@ -410,7 +418,9 @@ extern "C" sharpv_status sharpv_tree_attention(
     const int group = num_q_heads / H;
     // rows of a tile by the average rows of a (sequence, KV head)
     const int64_t avg = total_nodes * group / num_seqs;
-    a.split = Split{avg <= 8 ? 8 : 32, kSimtKeys, group, H, draft_k != nullptr};
+    const bool bf16 = layout->dtype == SHARPV_BF16;
+    a.split = bf16 ? Split{avg <= 16 || D > 128 ? 16 : 32, kRowsTileKeys, group, H, draft_k != nullptr}
+                   : Split{avg <= 8 ? 8 : 32, kSimtKeys, group, H, draft_k != nullptr};
     char* ws = (char*)workspace;
     a.prefix = (int64_t*)ws;
     a.part_ml = (float*)(ws + prefix_bytes(num_seqs));
@@ -420,7 +430,11 @@ extern "C" sharpv_status sharpv_tree_attention(
     const sharpv_status ss = current_sms(sms);
     if (ss != SHARPV_OK) return ss;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    if (layout->dtype == SHARPV_F32)
-        return avg <= 8 ? simt_by_dim<SHARPV_F32, 8>(a, sms, stream) : simt_by_dim<SHARPV_F32, 32>(a, sms, stream);
-    return avg <= 8 ? simt_by_dim<SHARPV_BF16, 8>(a, sms, stream) : simt_by_dim<SHARPV_BF16, 32>(a, sms, stream);
+    sharpv_status st;
+    if (bf16) {
+        st = attn_rows_launch(a, sms, stream);
+        return st == SHARPV_OK ? join_launch<SHARPV_BF16>(a, stream) : st;
+    }
+    st = avg <= 8 ? simt_by_dim<SHARPV_F32, 8>(a, sms, stream) : simt_by_dim<SHARPV_F32, 32>(a, sms, stream);
+    return st == SHARPV_OK ? join_launch<SHARPV_F32>(a, stream) : st;
 }

@@ -1,6 +1,8 @@
 // Arguments that the kernels of the attention over a cache share.
 #pragma once
 
+#include <cuda.h>
+
 #include "decode_common.cuh"
 
 namespace sharpv {
@@ -32,6 +34,17 @@ struct AttnArgs {
     int ctas;
     int32_t* status_word;
 };
+
+// Tensor maps of a call (bf16): boxes of 64 columns and a key tile's rows.  draft_* repeat cache_* where there are none.
+struct AttnMaps {
+    CUtensorMap cache_k, cache_v, draft_k, draft_v;
+};
+sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps);
+
+// Few query rows, bf16: a.split has 16 or 32 rows (16 beyond head_dim 128) and kRowsTileKeys keys a tile.  Sets
+// a.ctas to what it launches.
+constexpr int kRowsTileKeys = 64;
+sharpv_status attn_rows_launch(AttnArgs& a, int sms, cudaStream_t stream);
 
 // Which keys of the 32 from key0 on node `i` of a sequence sees, as bits (drafted tokens).
 __device__ __forceinline__ uint32_t draft_sees(const AttnArgs& a, const SeqInfo& s, int i, int key0) {

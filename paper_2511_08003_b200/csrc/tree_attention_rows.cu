@@ -1,0 +1,432 @@
+// Attention of few query rows over a K/V cache in bf16: every K and V row is read once, and that is what bounds it.
+//
+// One CTA per SM takes its share of the key tiles (64 keys, K and V together 32 KB at head_dim 128).  One warp
+// keeps a ring of TMA tile loads in flight; two groups of four warps take the tiles in turn, every warp 16 keys of its
+// tile for all of the segment's 16 or 32 query rows: scores and weighted sums on the tensor cores (mma.sync: 16
+// rows fill it, and the time is that of the loads), running maximum, sum and result in registers.  A warp needs nobody
+// else until the end of its portion, where the eight results are joined through shared memory.
+#include "tma.cuh"
+#include "tree_attention.cuh"
+
+#include <cuda_bf16.h>
+
+namespace sharpv {
+namespace {
+
+constexpr int kKeys = kRowsTileKeys;            // of a tile
+constexpr int kWarps = 8;                       // that compute, in two groups of four
+constexpr int kThreads = kWarps * 32 + 32;
+constexpr int kMergeCols = 128;                 // columns that are joined at a time
+
+template <int MT, int DP>
+struct Cfg {
+    static constexpr int kHalves = DP / 64;                     // TMA boxes of 64 columns
+    static constexpr int kTileBytes = kKeys * DP * 2;           // K or V
+    static constexpr int kStages = DP == 64 ? 8 : (DP == 128 ? 4 : 2);
+    static constexpr bool kQInRegs = MT == 1 && DP <= 128;
+    static constexpr int kQPitch = DP * 2 + 16;                 // bytes; 16 more, so that 8 rows fall on 8 bank groups
+    static constexpr int kCols = DP < kMergeCols ? DP : kMergeCols;
+};
+
+template <int MT, int DP>
+struct Shared {
+    using C = Cfg<MT, DP>;
+    uint8_t tiles[C::kStages][2][C::kTileBytes];
+    float merge[kWarps][16][C::kCols + 4];
+    float m[kWarps][16], l[kWarps][16];
+    float top[16], sum[16];
+    uint8_t q[C::kQInRegs ? 16 : MT * 16 * C::kQPitch];
+    uint64_t full[C::kStages], empty[C::kStages];
+    int poison;
+    PlanScratch<kThreads> plan;
+};
+
+__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" :: "n"(kWarps * 32) : "memory"); }
+
+struct Portion {
+    SeqInfo s;
+    int h, rt, kt0, kt1, kt_all, kt_cache;
+};
+
+// The next portion of the CTA's units, or false.  u, b and before move on.
+__device__ __forceinline__ bool next_portion(const AttnArgs& a, Portion& p, int64_t& u, int64_t u_end, int& b, int64_t& before) {
+    bool bad = false;
+    while (u < u_end) {
+        p.s = load_seq(a.seqs, b, bad);
+        const int64_t mine = a.split.units(p.s);
+        if (u - before >= mine) {
+            before += mine;
+            ++b;
+            continue;
+        }
+        p.kt_all = a.split.key_tiles(p.s);
+        p.kt_cache = a.split.cache_tiles(p.s);
+        const int rts = a.split.row_tiles(p.s);
+        const int64_t seg = (u - before) / p.kt_all;
+        p.kt0 = (int)((u - before) % p.kt_all);
+        p.kt1 = (int)min((int64_t)p.kt_all, p.kt0 + (u_end - u));
+        p.h = (int)(seg / rts);
+        p.rt = (int)(seg % rts);
+        u += p.kt1 - p.kt0;
+        return true;
+    }
+    return false;
+}
+
+template <int MT, int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnMaps maps) {
+    using C = Cfg<MT, DP>;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    auto& sm = *reinterpret_cast<Shared<MT, DP>*>(smem_raw);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < C::kStages; ++i) {
+            mbar_init(&sm.full[i], 1);
+            mbar_init(&sm.empty[i], 4);
+        }
+        mbar_fence_init();
+        sm.poison = 0;
+    }
+    if (warp == kWarps && lane < 4) tma_prefetch(&maps.cache_k + lane);
+    cudaGridDependencySynchronize();
+    const PlanStart plan = plan_cta<kThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, a.prefix, a.status_word);
+    int64_t u = plan.first, before = plan.before;
+    int b = plan.b;
+    Portion p;
+    bool alive = true;                          // a wait that gave up: nothing is waited for any more, the result is void
+    uint32_t it = 0;                            // tiles of this CTA so far
+
+    if (warp == kWarps) {                       // the loads
+        if (lane != 0) return;
+        while (next_portion(a, p, u, plan.end, b, before)) {
+            for (int kt = p.kt0; kt < p.kt1 && alive; ++kt, ++it) {
+                const int stage = it % C::kStages;
+                if (it >= C::kStages) alive = mbar_wait(&sm.empty[stage], (it / C::kStages - 1) & 1);
+                if (!alive) break;
+                const bool drafted = kt >= p.kt_cache;
+                if (drafted && !a.split.draft) {            // the empty tile of rows without keys
+                    mbar_arrive(&sm.full[stage]);
+                    continue;
+                }
+                mbar_expect(&sm.full[stage], 2 * C::kTileBytes);
+                const CUtensorMap* mk = drafted ? &maps.draft_k : &maps.cache_k;
+                const CUtensorMap* mv = drafted ? &maps.draft_v : &maps.cache_v;
+                const int row = drafted ? p.s.node0 + (kt - p.kt_cache) * kKeys : (int)p.s.begin + kt * kKeys;
+#pragma unroll
+                for (int x = 0; x < C::kHalves; ++x)
+                    tma_load(sm.tiles[stage][0] + x * kKeys * 128, mk, &sm.full[stage], x * 64, row, p.h);
+#pragma unroll
+                for (int x = 0; x < C::kHalves; ++x)
+                    tma_load(sm.tiles[stage][1] + x * kKeys * 128, mv, &sm.full[stage], x * 64, row, p.h);
+            }
+        }
+        if (!alive) {
+            report(a.status_word, SHARPV_ERR_TIMEOUT);
+            for (int i = 0; i < C::kStages && (uint32_t)i < it; ++i) {      // copies in flight land before the CTA ends
+                const uint32_t last = it - 1 - i;
+                (void)mbar_wait(&sm.full[last % C::kStages], (last / C::kStages) & 1);
+            }
+        }
+        return;
+    }
+
+    const int group = warp >> 2, sub = warp & 3;        // tiles of this parity, 16 keys from sub * 16 on
+    const int qr = lane >> 2, qc = (lane & 3) * 2;      // fragment row (and row + 8), column (and column + 1)
+    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
+    constexpr int R = MT * 16;
+    while (next_portion(a, p, u, plan.end, b, before)) {
+        const int r_base = p.rt * R, r_all = p.s.nodes * G;
+        // the query rows, as fragments in registers or in shared memory
+        uint32_t qf[C::kQInRegs ? DP / 16 : 1][4];
+        auto q_row = [&](int row) -> const char* {
+            return a.q + (int64_t)(p.s.node0 + row / G) * a.q_node + (int64_t)(p.h * G + row % G) * D * 2;
+        };
+        if constexpr (C::kQInRegs) {
+            const bool in0 = r_base + qr < r_all, in1 = r_base + qr + 8 < r_all;
+            const char* q0 = q_row(in0 ? r_base + qr : 0);
+            const char* q1 = q_row(in1 ? r_base + qr + 8 : 0);
+#pragma unroll
+            for (int ks = 0; ks < DP / 16; ++ks) {
+                const int c = ks * 16 + qc;                 // D is a multiple of 8: c and c + 1 are both inside or not
+                qf[ks][0] = in0 && c < D ? __ldg((const uint32_t*)(q0 + c * 2)) : 0u;
+                qf[ks][1] = in1 && c < D ? __ldg((const uint32_t*)(q1 + c * 2)) : 0u;
+                qf[ks][2] = in0 && c + 8 < D ? __ldg((const uint32_t*)(q0 + c * 2 + 16)) : 0u;
+                qf[ks][3] = in1 && c + 8 < D ? __ldg((const uint32_t*)(q1 + c * 2 + 16)) : 0u;
+            }
+        } else {
+            for (int x = threadIdx.x; x < R * (DP / 8); x += kWarps * 32) {
+                const int r = x / (DP / 8), c = x % (DP / 8);
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (r_base + r < r_all && c * 8 < D) v = ld_cached(q_row(r_base + r) + c * 16);
+                *reinterpret_cast<uint4*>(sm.q + r * C::kQPitch + c * 16) = v;
+            }
+            consumer_sync();
+        }
+        float o[MT][DP / 8][4];
+        float m[MT][2], l[MT][2];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            m[t][0] = m[t][1] = neg_inf();
+            l[t][0] = l[t][1] = 0.f;
+#pragma unroll
+            for (int j = 0; j < DP / 8; ++j) o[t][j][0] = o[t][j][1] = o[t][j][2] = o[t][j][3] = 0.f;
+        }
+        bool poison = false;                    // a drafted value that is not finite was set aside
+
+        for (int kt = p.kt0; kt < p.kt1; ++kt, ++it) {
+            if ((int)(it & 1) != group) continue;
+            const int stage = it % C::kStages;
+            if (alive && !mbar_wait(&sm.full[stage], (it / C::kStages) & 1)) {
+                alive = false;
+                report(a.status_word, SHARPV_ERR_TIMEOUT);
+            }
+            const uint32_t ks_base = smem_u32(sm.tiles[stage][0]), vs_base = smem_u32(sm.tiles[stage][1]);
+            float s[MT][2][4];
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) s[t][n][0] = s[t][n][1] = s[t][n][2] = s[t][n][3] = 0.f;
+            const int krow = sub * 16 + (lane >> 4) * 8 + (lane & 7);
+#pragma unroll
+            for (int ks = 0; ks < DP / 16; ++ks) {
+                uint32_t k4[4];
+                const int c = (ks & 3) * 2 + ((lane >> 3) & 1);
+                ldmatrix4(k4, ks_base + (ks >> 2) * (kKeys * 128) + swizzle128(krow, c));
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    if constexpr (C::kQInRegs) {
+                        mma_bf16(s[t][0], qf[ks], k4[0], k4[1]);
+                        mma_bf16(s[t][1], qf[ks], k4[2], k4[3]);
+                    } else {
+                        uint32_t q4[4];
+                        ldmatrix4(q4, smem_u32(sm.q) + (t * 16 + (lane & 15)) * C::kQPitch + ks * 32 + (lane >> 4) * 16);
+                        mma_bf16(s[t][0], q4, k4[0], k4[1]);
+                        mma_bf16(s[t][1], q4, k4[2], k4[3]);
+                    }
+                }
+            }
+            const bool drafted = kt >= p.kt_cache;
+            const int left = drafted ? (a.split.draft ? p.s.nodes - (kt - p.kt_cache) * kKeys : 0)
+                                     : p.s.len - kt * kKeys;        // keys of the tile that are there
+            const bool masked = drafted || left < kKeys;
+            uint32_t pf[MT][4];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[t][n][i] *= a.scale_log2;
+                if (masked) {
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const int row = r_base + t * 16 + qr + half * 8;
+                        uint32_t sees;                              // the warp's 16 keys
+                        if (!drafted) {
+                            const int n = left - sub * 16;
+                            sees = n >= 16 ? 0xffffu : (n <= 0 ? 0u : (1u << n) - 1u);
+                        } else {
+                            const int key0 = (kt - p.kt_cache) * kKeys + (sub >> 1) * 32;
+                            sees = a.split.draft && row < r_all ? draft_sees(a, p.s, row / G, key0) >> ((sub & 1) * 16) : 0u;
+                        }
+#pragma unroll
+                        for (int n = 0; n < 2; ++n)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+                                if (!(sees >> (n * 8 + qc + i) & 1)) s[t][n][half * 2 + i] = neg_inf();
+                    }
+                }
+                float top[2];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float x = fmaxf(fmaxf(s[t][0][half * 2], s[t][0][half * 2 + 1]), fmaxf(s[t][1][half * 2], s[t][1][half * 2 + 1]));
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+                    top[half] = fmaxf(x, m[t][half]);
+                }
+                if (__any_sync(0xffffffffu, top[0] > m[t][0] || top[1] > m[t][1])) {
+                    const float a0 = m[t][0] == top[0] ? 1.f : ex2(m[t][0] - top[0]);
+                    const float a1 = m[t][1] == top[1] ? 1.f : ex2(m[t][1] - top[1]);
+                    m[t][0] = top[0];
+                    m[t][1] = top[1];
+                    l[t][0] *= a0;
+                    l[t][1] *= a1;
+#pragma unroll
+                    for (int j = 0; j < DP / 8; ++j) {
+                        o[t][j][0] *= a0;
+                        o[t][j][1] *= a0;
+                        o[t][j][2] *= a1;
+                        o[t][j][3] *= a1;
+                    }
+                }
+                const float b0 = m[t][0] == neg_inf() ? 0.f : m[t][0], b1 = m[t][1] == neg_inf() ? 0.f : m[t][1];
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const float p0 = ex2(s[t][n][0] - b0), p1 = ex2(s[t][n][1] - b0);
+                    const float p2 = ex2(s[t][n][2] - b1), p3 = ex2(s[t][n][3] - b1);
+                    l[t][0] += p0 + p1;
+                    l[t][1] += p2 + p3;
+                    // weights are rounded to bf16 for the product with the values; their sum is not
+                    pf[t][n * 2] = pack_bf16(p0, p1);
+                    pf[t][n * 2 + 1] = pack_bf16(p2, p3);
+                }
+            }
+            const int vrow = sub * 16 + (lane & 15);
+#pragma unroll
+            for (int j = 0; j < DP / 16; ++j) {
+                uint32_t v4[4];
+                const int c = (j & 3) * 2 + (lane >> 4);
+                ldmatrix4_trans(v4, vs_base + (j >> 2) * (kKeys * 128) + swizzle128(vrow, c));
+                if (masked) {
+                    // rows that are not there may hold anything, and so may drafted rows that some query rows do
+                    // not see: 0 times them would not be 0
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = sub * 16 + (i & 1) * 8 + qc;
+                        if (key >= left) v4[i] = 0u;
+                        else if (key + 1 >= left) v4[i] &= 0xffffu;
+                        if (drafted) {
+                            const uint32_t off = nonfinite_bf16(v4[i]);
+                            v4[i] &= ~off;
+                            poison |= off != 0;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    mma_bf16(o[t][j * 2], pf[t], v4[0], v4[1]);
+                    mma_bf16(o[t][j * 2 + 1], pf[t], v4[2], v4[3]);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.empty[stage]);
+        }
+
+        // ---- the eight warps' results are joined, 16 rows and up to 128 columns at a time
+        const bool complete = p.kt0 == 0 && p.kt1 == p.kt_all;
+        const int slot = portion_slot(blockIdx.x, p.kt0);
+        if (poison) sm.poison = 1;
+        for (int t = 0; t < MT; ++t) {
+            if (r_base + t * 16 >= r_all) break;            // the same for every thread
+            for (int c0 = 0; c0 < DP; c0 += C::kCols) {
+                float mm[2], ll[2];
+#pragma unroll
+                for (int x = 0; x < MT; ++x)
+                    if (x == t) { mm[0] = m[x][0]; mm[1] = m[x][1]; ll[0] = l[x][0]; ll[1] = l[x][1]; }
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    ll[half] += __shfl_xor_sync(0xffffffffu, ll[half], 1);
+                    ll[half] += __shfl_xor_sync(0xffffffffu, ll[half], 2);
+                    if ((lane & 3) == 0) { sm.m[warp][qr + half * 8] = mm[half]; sm.l[warp][qr + half * 8] = ll[half]; }
+                }
+#pragma unroll
+                for (int x = 0; x < MT; ++x)
+#pragma unroll
+                    for (int j = 0; j < DP / 8; ++j)
+                        if (x == t && j * 8 >= c0 && j * 8 < c0 + C::kCols) {
+                            *reinterpret_cast<float2*>(&sm.merge[warp][qr][j * 8 - c0 + qc]) = make_float2(o[x][j][0], o[x][j][1]);
+                            *reinterpret_cast<float2*>(&sm.merge[warp][qr + 8][j * 8 - c0 + qc]) = make_float2(o[x][j][2], o[x][j][3]);
+                        }
+                consumer_sync();
+                constexpr int V = C::kCols / 4;
+                for (int x = threadIdx.x; x < 16 * V; x += kWarps * 32) {
+                    const int r = x / V, c = c0 + (x % V) * 4, row = r_base + t * 16 + r;
+                    if (row >= r_all || c >= D) continue;
+                    float top = sm.m[0][r];
+#pragma unroll
+                    for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm.m[w][r]);
+                    const float base = top == neg_inf() ? 0.f : top;
+                    float sum = 0.f;
+                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) {
+                        const float f = ex2(sm.m[w][r] - base);
+                        const float4 v = *reinterpret_cast<const float4*>(&sm.merge[w][r][c - c0]);
+                        sum = fmaf(f, sm.l[w][r], sum);
+                        acc.x = fmaf(f, v.x, acc.x);
+                        acc.y = fmaf(f, v.y, acc.y);
+                        acc.z = fmaf(f, v.z, acc.z);
+                        acc.w = fmaf(f, v.w, acc.w);
+                    }
+                    if (sm.poison) {
+                        // what was set aside comes back to the rows that see it
+                        const int j0 = (max(p.kt0, p.kt_cache) - p.kt_cache) * kKeys, j1 = min(p.s.nodes, (p.kt1 - p.kt_cache) * kKeys);
+                        for (int j = j0; j < j1; ++j) {
+                            if (!(draft_sees(a, p.s, row / G, j & ~31) >> (j & 31) & 1)) continue;
+                            const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(
+                                a.draft_v + (int64_t)(p.s.node0 + j) * a.dv_node) + p.h * D + c;
+                            const float v0 = __bfloat162float(v[0]), v1 = __bfloat162float(v[1]);
+                            const float v2 = __bfloat162float(v[2]), v3 = __bfloat162float(v[3]);
+                            if (!finite_f32(v0)) acc.x += v0;
+                            if (!finite_f32(v1)) acc.y += v1;
+                            if (!finite_f32(v2)) acc.z += v2;
+                            if (!finite_f32(v3)) acc.w += v3;
+                        }
+                    }
+                    const int64_t at = (int64_t)(p.s.node0 + row / G) * HQ + p.h * G + row % G;
+                    if (complete) {
+                        const float inv = row_scale(sum);
+                        *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at * D + c) =
+                            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+                        if (c == 0) a.lse[at] = row_lse(top, sum);
+                    } else {
+                        *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * R + t * 16 + r) * D + c) = acc;
+                        if (c == 0) {
+                            a.part_ml[(int64_t)slot * 2 * R + t * 16 + r] = top;
+                            a.part_ml[((int64_t)slot * 2 + 1) * R + t * 16 + r] = sum;
+                        }
+                    }
+                }
+                consumer_sync();
+            }
+        }
+        if (threadIdx.x == 0) sm.poison = 0;
+        consumer_sync();
+    }
+}
+
+template <int MT, int DP>
+sharpv_status launch(const AttnArgs& a, cudaStream_t stream) {
+    using C = Cfg<MT, DP>;
+    auto kern = attn_rows_kernel<MT, DP>;
+    const size_t smem = sizeof(Shared<MT, DP>);
+    static_assert(sizeof(Shared<MT, DP>) <= 227 * 1024, "shared memory of one CTA");
+    AttnMaps maps;
+    const sharpv_status ms = encode_attn_maps(a, kKeys, maps);
+    if (ms != SHARPV_OK) return ms;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
+        launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kThreads), smem, stream, a, maps) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SHARPV_ERR_CUDA;
+    }
+    return SHARPV_OK;
+}
+
+}  // namespace
+
+sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps) {
+    const int D = a.head_dim, H = a.split.heads;
+    const int64_t T = a.seqs.cache_tokens > 0 ? a.seqs.cache_tokens : 1, N = a.seqs.total_nodes;
+    const int64_t most = (int64_t)1 << 40;              // what a tensor map's strides can say
+    if (a.kv_token >= most || a.kv_head >= most || a.dk_node >= most || a.dv_node >= most) return SHARPV_ERR_UNSUPPORTED;
+    bool ok = encode_rows_map(&maps.cache_k, a.cache_k, D, T, a.kv_token, H, a.kv_head, box_rows) &&
+              encode_rows_map(&maps.cache_v, a.cache_v, D, T, a.kv_token, H, a.kv_head, box_rows);
+    if (a.split.draft)
+        ok = ok && encode_rows_map(&maps.draft_k, a.draft_k, D, N, a.dk_node, H, (int64_t)D * 2, box_rows) &&
+             encode_rows_map(&maps.draft_v, a.draft_v, D, N, a.dv_node, H, (int64_t)D * 2, box_rows);
+    else {
+        maps.draft_k = maps.cache_k;
+        maps.draft_v = maps.cache_v;
+    }
+    return ok ? SHARPV_OK : SHARPV_ERR_CUDA;
+}
+
+sharpv_status attn_rows_launch(AttnArgs& a, int sms, cudaStream_t stream) {
+    a.ctas = sms < kMaxAttnCtas ? sms : kMaxAttnCtas;
+    const bool two = a.split.rows > 16;
+    if (a.head_dim <= 64) return two ? launch<2, 64>(a, stream) : launch<1, 64>(a, stream);
+    if (a.head_dim <= 128) return two ? launch<2, 128>(a, stream) : launch<1, 128>(a, stream);
+    return launch<1, 256>(a, stream);
+}
+
+}  // namespace sharpv
