@@ -74,25 +74,13 @@ mass_simt_kernel(const __grid_constant__ MassArgs a) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
     cudaGridDependencySynchronize();
-    const PlanStart plan = plan_cta<kMassThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, nullptr, a.status_word);
-    int64_t u = plan.first;
-    const int64_t u_end = plan.end;
-    int b = plan.b;
-    int64_t before = plan.before;
-    bool bad = false;
-    while (u < u_end) {
-        const SeqInfo s = load_seq(a.seqs, b, bad);
-        const int64_t mine = a.split.units(s);
-        if (u - before >= mine) {
-            before += mine;
-            ++b;
-            continue;
-        }
-        const int kt_all = a.split.key_tiles(s);
-        const int h = (int)((u - before) / kt_all);
-        const int kt0 = (int)((u - before) % kt_all);
-        const int kt1 = (int)min((int64_t)kt_all, kt0 + (u_end - u));
-        u += kt1 - kt0;
+    int64_t first, end;
+    const PlanStart plan = plan_cta<kMassThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
+    Walk walk(plan, first, end);
+    Portion part;
+    while (walk.next(a.seqs, a.split, part)) {
+        const SeqInfo& s = part.s;
+        const int h = part.h, kt0 = part.kt0, kt1 = part.kt1;
         if (s.len == 0) continue;
         auto load_keys = [&](int kt, int buf) {
             const char* src = a.cache_k + (int64_t)h * a.kv_head + (s.begin + (int64_t)kt * kMassKeys) * a.kv_token;

@@ -66,39 +66,57 @@ struct Split {
     }
 };
 
-// The CTAs that take part: no more than there are units, so that each of them has at least one.
-__device__ __forceinline__ int64_t busy_ctas(int64_t units, int64_t ctas) { return units < ctas ? units : ctas; }
-
-// first unit of CTA c, and the CTA that owns unit u
-__device__ __forceinline__ int64_t cta_first_unit(int64_t c, int64_t units, int64_t ctas) { return c * units / ctas; }
-__device__ __forceinline__ int unit_owner(int64_t u, int64_t units, int64_t ctas) {
-    return (int)(((u + 1) * ctas - 1) / units);
+// 64-bit division that takes the 32-bit one where the numbers allow it (nearly always: the 64-bit one is a routine of
+// its own, and several of them in a row cost a microsecond at the start of a kernel).
+__device__ __forceinline__ int64_t div64(int64_t a, int64_t b) {
+    return ((uint64_t)(a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
-struct PlanStart {
-    int64_t first, end;         // the CTA's units
-    int b;                      // sequence of the first one
-    int64_t before;             // units in front of that sequence
+// `units` dealt to `ctas` CTAs in contiguous runs whose lengths differ by one at most.  No more CTAs take part than
+// there are units, so each of those has at least one.
+struct Deal {
+    int64_t each, extra;        // the first `extra` CTAs have one unit more
+    int busy;                   // CTAs that take part
+    __device__ __forceinline__ Deal(int64_t units, int ctas) {
+        busy = units < ctas ? (int)units : ctas;
+        each = busy ? div64(units, busy) : 0;
+        extra = units - each * busy;
+    }
+    __device__ __forceinline__ int64_t first(int c) const { return c * each + (c < extra ? c : extra); }
+    __device__ __forceinline__ int owner(int64_t u) const {
+        const int64_t head = extra * (each + 1);
+        return (int)(u < head ? div64(u, each + 1) : extra + div64(u - head, each));
+    }
 };
 
-// Every thread of the block (NT threads) gets the plan of this CTA.  CTA 0 also writes prefix[0..num_seqs],
-// the units in front of every sequence, for the kernel that joins the partial results, and reports tables
-// that do not fit.  
+struct PlanStart {
+    SeqInfo s;                  // sequence of the CTA's first unit
+    int b;
+    int64_t before;             // units in front of that sequence
+    int64_t units;              // of the whole call
+};
+
 template <int NT>
 struct PlanScratch {
     int64_t warp[NT / 32 + 1];
     PlanStart start;
 };
 
+// Every thread of the block (NT threads) gets the plan of this CTA, `first` its first unit and `end` the one behind
+// its last.  CTA 0 reports tables that do not fit.
 template <int NT>
 __device__ __forceinline__ PlanStart plan_cta(const SeqTables& t, const Split& sp, int cta, int ctas,
-                                              PlanScratch<NT>& sm, int64_t* prefix, int32_t* status_word) {
+                                              PlanScratch<NT>& sm, int64_t& first, int64_t& end, int32_t* status_word) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per = (t.num_seqs + NT - 1) / NT;
     const int lo = min(t.num_seqs, (int)threadIdx.x * per), hi = min(t.num_seqs, lo + per);
     int64_t sum = 0;
     bool bad = false;
-    for (int b = lo; b < hi; ++b) sum += sp.units(load_seq(t, b, bad));
+    SeqInfo s = {};
+    for (int b = lo; b < hi; ++b) {
+        s = load_seq(t, b, bad);
+        sum += sp.units(s);
+    }
     int64_t inc = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -106,40 +124,83 @@ __device__ __forceinline__ PlanStart plan_cta(const SeqTables& t, const Split& s
         if (lane >= o) inc += n;
     }
     if (lane == 31) sm.warp[warp] = inc;
-    if (threadIdx.x == 0) sm.start = PlanStart{0, 0, 0, 0};
     __syncthreads();
-    int64_t before = inc - sum, total = 0;
+    int64_t run = inc - sum, total = 0;
 #pragma unroll
     for (int w = 0; w < NT / 32; ++w) {
         const int64_t v = sm.warp[w];
-        if (w < warp) before += v;
+        if (w < warp) run += v;
         total += v;
     }
-    const int64_t busy = busy_ctas(total, ctas);
-    const int64_t first = cta < busy ? cta_first_unit(cta, total, busy) : total;
-    int64_t run = before;
-    for (int b = lo; b < hi; ++b) {
-        const int64_t u = sp.units(load_seq(t, b, bad));
-        if (cta == 0 && prefix) prefix[b] = run;
-        if (first >= run && first < run + u) {
-            sm.start.b = b;
-            sm.start.before = run;
+    const Deal deal(total, ctas);
+    first = cta < deal.busy ? deal.first(cta) : total;
+    end = cta < deal.busy ? deal.first(cta + 1) : total;
+    if (first >= run && first < run + sum) {            // the sequence is among this thread's
+        int b = lo;
+        for (; per > 1; ++b) {
+            s = load_seq(t, b, bad);
+            const int64_t n = sp.units(s);
+            if (first < run + n) break;
+            run += n;
         }
-        run += u;
+        sm.start.s = s;
+        sm.start.b = b;
+        sm.start.before = run;
     }
-    if (threadIdx.x == 0) {
-        sm.start.first = first;
-        sm.start.end = cta < busy ? cta_first_unit(cta + 1, total, busy) : total;
-        if (cta == 0 && prefix) prefix[t.num_seqs] = total;
-    }
+    if (threadIdx.x == 0) sm.start.units = total;
     if (cta == 0 && bad) report(status_word, SHARPV_ERR_BOUNDS);
     __syncthreads();
     return sm.start;
 }
 
-// Where a portion (the units of one segment that one CTA works on) leaves its partial result: slot 1 of the CTA
-// if the portion starts at the segment's first key tile, else slot 0.  A CTA has at most one of each.
+// A portion: the units of one segment that one CTA works on.
+struct Portion {
+    SeqInfo s;
+    int h, rt;                          // KV head, row tile
+    int kt0, kt1;                       // key tiles of the portion
+    int kt_all, kt_cache;               // of the segment; of those, tiles of cached rows
+};
+
+// Walks the portions of a CTA's units [u, end).
+struct Walk {
+    int64_t u, end, before;
+    SeqInfo s;
+    int b;
+    __device__ __forceinline__ Walk(const PlanStart& p, int64_t first, int64_t last)
+        : u(first), end(last), before(p.before), s(p.s), b(p.b) {}
+    __device__ __forceinline__ bool next(const SeqTables& t, const Split& sp, Portion& p) {
+        if (u >= end) return false;
+        for (;;) {                              // sequences without nodes have no units
+            const int64_t mine = sp.units(s);
+            if (u - before < mine) break;
+            before += mine;
+            bool bad = false;
+            s = load_seq(t, ++b, bad);
+        }
+        p.s = s;
+        p.kt_all = sp.key_tiles(s);
+        p.kt_cache = sp.cache_tiles(s);
+        const int64_t seg = div64(u - before, p.kt_all);
+        p.kt0 = (int)(u - before - seg * p.kt_all);
+        p.kt1 = (int)min((int64_t)p.kt_all, p.kt0 + (end - u));
+        const int rts = sp.row_tiles(s);
+        p.h = (int)div64(seg, rts);
+        p.rt = (int)(seg - (int64_t)p.h * rts);
+        u += p.kt1 - p.kt0;
+        return true;
+    }
+};
+
+// Where a portion that is not a whole segment leaves its partial result: slot 1 of the CTA if it starts at the segment's
+// first key tile, else slot 0.  A CTA has at most one of each.
 __device__ __forceinline__ int portion_slot(int cta, int first_key_tile) { return cta * 2 + (first_key_tile == 0); }
+
+// The segment whose first units CTA c has and whose last ones it has not (at most one): the CTAs c .. last hold its parts.
+struct SharedSegment {
+    int node0, rows;                    // first node of the sequence, its query rows
+    int h, rt;
+    int last;                           // -1: there is none
+};
 
 // 16 bytes from global to shared memory without passing registers; zeros where `valid` is false
 __device__ __forceinline__ void cp_async16(void* smem, const void* gmem, bool valid) {

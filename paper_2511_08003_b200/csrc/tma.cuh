@@ -47,6 +47,11 @@ __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_u32(bar)) : "memory");
 }
 
+// one arrival when this thread's cp.async copies so far have landed
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" :: "r"(smem_u32(bar)) : "memory");
+}
+
 // Waits for the phase of the given parity to complete, at most kWaitTries times the hardware's own suspend time
 // (far beyond any kernel of this library); false if it did not.
 constexpr int kWaitTries = 1 << 18;

@@ -73,27 +73,16 @@ attn_simt_kernel(const __grid_constant__ AttnArgs a) {
     const int col0 = threadIdx.x % COLS, row0 = threadIdx.x / COLS * RPT;
     const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
     cudaGridDependencySynchronize();
-    const PlanStart plan = plan_cta<kSimtThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, a.prefix, a.status_word);
-    int64_t u = plan.first;
-    const int64_t u_end = plan.end;
-    int b = plan.b;
-    int64_t before = plan.before;
-    bool bad = false;
-    while (u < u_end) {
-        const SeqInfo s = load_seq(a.seqs, b, bad);
-        const int64_t mine = a.split.units(s);
-        if (u - before >= mine) {               // on to the next sequence (those without nodes have no units)
-            before += mine;
-            ++b;
-            continue;
-        }
-        const int kt_all = a.split.key_tiles(s), kt_cache = a.split.cache_tiles(s), rts = a.split.row_tiles(s);
-        const int64_t seg = (u - before) / kt_all;
-        const int kt0 = (int)((u - before) % kt_all);
-        const int kt1 = (int)min((int64_t)kt_all, kt0 + (u_end - u));
-        const int h = (int)(seg / rts), rt = (int)(seg % rts);
-        const int r_base = rt * R, r_all = s.nodes * G;
-        u += kt1 - kt0;
+    int64_t first, end;
+    const PlanStart plan = plan_cta<kSimtThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
+    Walk walk(plan, first, end);
+    Portion part;
+    SharedSegment shared = {0, 0, 0, 0, -1};
+    while (walk.next(a.seqs, a.split, part)) {
+        const SeqInfo& s = part.s;
+        const int kt_all = part.kt_all, kt_cache = part.kt_cache, kt0 = part.kt0, kt1 = part.kt1, h = part.h;
+        const int r_base = part.rt * R, r_all = s.nodes * G;
+        if (threadIdx.x == 0) note_shared(part, a.split, walk.u, plan.units, a.ctas, shared);
 
         auto load_tile = [&](int kt, int buf) {
             const char *k, *v;
@@ -239,83 +228,104 @@ attn_simt_kernel(const __grid_constant__ AttnArgs a) {
             }
         }
     }
+    if (threadIdx.x == 0) a.shared[blockIdx.x] = shared;
 }
 
-// One warp per output row of a segment that more than one CTA worked on: the partial results' running maxima and sums
-// are brought to the common maximum, the weighted sums added in the order of the CTAs (fixed, so results do not
-// depend on scheduling), divided, rounded once.
-template <int DT>
+// CTA (c, y) joins rows of the segment that the CTAs c .. last of the kernel before shared, WPR warps a row (a warp takes
+// every WPR-th part): the parts' running maxima and sums are brought to the common maximum, the weighted sums
+// added in a fixed order (results do not depend on scheduling), divided, rounded once.  What bounds it is the latency
+// of three dependent reads, hence eight parts' loads in flight a warp, and eight warps a row where a segment
+// has few rows (its parts are many then: up to one a CTA).
+constexpr int kJoinAhead = 8;
+template <int DT, int WPR>
 __global__ void __launch_bounds__(256)
 attn_join_kernel(const __grid_constant__ AttnArgs a) {
     using St = Store<DT>;
-    const int lane = threadIdx.x & 31;
+    constexpr int KD = kMaxHeadDim / 128, RPC = 8 / WPR;
+    __shared__ float4 part[WPR > 1 ? 8 : 1][KD][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x;
     const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G, R = a.split.rows;
-    const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int r = blockIdx.y * RPC + warp / WPR, w = warp % WPR;
     cudaGridDependencySynchronize();
-    const int64_t node = w / HQ;
-    if (node >= a.seqs.total_nodes) return;
-    const int qh = (int)(w % HQ), h = qh / G;
-    const int64_t units = a.prefix[a.seqs.num_seqs], busy = busy_ctas(units, a.ctas);
-    if (units == 0) return;
-    const int b = upper_segment(a.seqs.node_off, a.seqs.num_seqs, (int)node);
-    bool bad = false;
-    const SeqInfo s = load_seq(a.seqs, b, bad);
-    if (node < s.node0 || node >= s.node0 + s.nodes) return;       // no sequence's node: left as it is
-    const int row = (int)(node - s.node0) * G + qh % G;
-    const int rt = row / R, r = row % R;
-    const int kts = a.split.key_tiles(s);
-    const int64_t u0 = a.prefix[b] + ((int64_t)h * a.split.row_tiles(s) + rt) * kts;
-    const int c0 = unit_owner(u0, units, busy), c1 = unit_owner(u0 + kts - 1, units, busy);
-    if (c0 == c1) return;                                           // written by that CTA
+    const SharedSegment seg = a.shared[c0];
+    const int row = seg.rt * R + r;
+    if (seg.last < 0 || row >= seg.rows) return;            // with WPR = 8 the whole CTA, else warps of their own
+    const int c1 = seg.last;
     float top = neg_inf();
-    for (int c = c0 + lane; c <= c1; c += 32) {
-        const int slot = c * 2 + (c == c0);
-        top = fmaxf(top, a.part_ml[(int64_t)slot * 2 * R + r]);
-    }
+    for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(a.part_ml + (int64_t)(c * 2 + (c == c0)) * 2 * R + r));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float base = top == neg_inf() ? 0.f : top;
     float sum = 0.f;
-    float acc[kMaxHeadDim / 32];
+    float4 acc[KD];
 #pragma unroll
-    for (int i = 0; i < kMaxHeadDim / 32; ++i) acc[i] = 0.f;
+    for (int k = 0; k < KD; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int c = c0; c <= c1; c += 32) {
         float f = 0.f;
         if (c + lane <= c1) {
-            const int slot = (c + lane) * 2 + (c + lane == c0);
-            const float l = a.part_ml[((int64_t)slot * 2 + 1) * R + r];
-            f = exp2f(a.part_ml[(int64_t)slot * 2 * R + r] - base);
-            sum += l * f;
+            const float* ml = a.part_ml + (int64_t)((c + lane) * 2 + (c + lane == c0)) * 2 * R + r;
+            f = exp2f(__ldcg(ml) - base);
+            sum += __ldcg(ml + R) * f;
         }
         const int n = min(32, c1 - c + 1);
-        for (int i = 0; i < n; ++i) {
-            const float fi = __shfl_sync(0xffffffffu, f, i);
-            const float* o = a.part_o + ((int64_t)((c + i) * 2 + (c + i == c0)) * R + r) * D;
+        for (int i = w; i < n; i += kJoinAhead * WPR) {
 #pragma unroll
-            for (int k = 0; k < kMaxHeadDim / 128; ++k) {
+            for (int k = 0; k < KD; ++k) {
                 const int col = k * 128 + lane * 4;
-                if (col < D) {
-                    const float4 v = __ldcg(reinterpret_cast<const float4*>(o + col));
-                    acc[k * 4 + 0] = fmaf(fi, v.x, acc[k * 4 + 0]);
-                    acc[k * 4 + 1] = fmaf(fi, v.y, acc[k * 4 + 1]);
-                    acc[k * 4 + 2] = fmaf(fi, v.z, acc[k * 4 + 2]);
-                    acc[k * 4 + 3] = fmaf(fi, v.w, acc[k * 4 + 3]);
+                if (k * 128 >= D) break;
+                float4 v[kJoinAhead];
+#pragma unroll
+                for (int x = 0; x < kJoinAhead; ++x) {
+                    const int y = i + x * WPR;
+                    v[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (y < n && col < D)
+                        v[x] = __ldcg(reinterpret_cast<const float4*>(a.part_o + ((int64_t)((c + y) * 2 + (c + y == c0)) * R + r) * D + col));
+                }
+#pragma unroll
+                for (int x = 0; x < kJoinAhead; ++x) {
+                    const int y = i + x * WPR;
+                    const float fx = __shfl_sync(0xffffffffu, f, y & 31);
+                    if (y < n) {
+                        acc[k].x = fmaf(fx, v[x].x, acc[k].x);
+                        acc[k].y = fmaf(fx, v[x].y, acc[k].y);
+                        acc[k].z = fmaf(fx, v[x].z, acc[k].z);
+                        acc[k].w = fmaf(fx, v[x].w, acc[k].w);
+                    }
                 }
             }
         }
     }
-    sum = warp_sum(sum);
-    const float inv = row_scale(sum);
-    auto* out = reinterpret_cast<typename St::T*>(a.out) + (node * HQ + qh) * D;
+    sum = warp_sum(sum);                        // every warp of a row has all of it
+    if constexpr (WPR > 1) {
 #pragma unroll
-    for (int k = 0; k < kMaxHeadDim / 128; ++k) {
-        const int col = k * 128 + lane * 4;
-        if (col < D) {
+        for (int k = 0; k < KD; ++k) part[warp][k][lane] = acc[k];
+        __syncthreads();
+        if (w != 0) return;
+        for (int y = 1; y < WPR; ++y) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) out[col + i] = St::from(acc[k * 4 + i] * inv);
+            for (int k = 0; k < KD; ++k) {
+                const float4 v = part[warp + y][k][lane];
+                acc[k].x += v.x;
+                acc[k].y += v.y;
+                acc[k].z += v.z;
+                acc[k].w += v.w;
+            }
         }
     }
-    if (lane == 0) a.lse[node * HQ + qh] = row_lse(top, sum);
+    const float inv = row_scale(sum);
+    const int64_t at = (int64_t)(seg.node0 + row / G) * HQ + seg.h * G + row % G;
+    auto* out = reinterpret_cast<typename St::T*>(a.out) + at * D;
+#pragma unroll
+    for (int k = 0; k < KD; ++k) {
+        const int col = k * 128 + lane * 4;
+        if (col < D) {
+            out[col] = St::from(acc[k].x * inv);
+            out[col + 1] = St::from(acc[k].y * inv);
+            out[col + 2] = St::from(acc[k].z * inv);
+            out[col + 3] = St::from(acc[k].w * inv);
+        }
+    }
+    if (lane == 0) a.lse[at] = row_lse(top, sum);
 }
 
 template <int DT, int R, int DP>
@@ -337,8 +347,14 @@ sharpv_status simt_launch(AttnArgs& a, int sms, cudaStream_t stream) {
 
 template <int DT>
 sharpv_status join_launch(const AttnArgs& a, cudaStream_t stream) {
-    const int64_t rows = a.seqs.total_nodes * a.split.heads * a.split.group;
-    if (launch_dependent(attn_join_kernel<DT>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, stream, a) != cudaSuccess) {
+    // rows that any segment can have
+    const int64_t all = a.seqs.total_nodes * a.split.group;
+    const unsigned rows = (unsigned)(all < a.split.rows ? all : a.split.rows);
+    const cudaError_t e =
+        a.split.rows <= 32
+            ? launch_dependent(attn_join_kernel<DT, 8>, dim3((unsigned)a.ctas, rows), dim3(256), 0, stream, a)
+            : launch_dependent(attn_join_kernel<DT, 1>, dim3((unsigned)a.ctas, (rows + 7) / 8), dim3(256), 0, stream, a);
+    if (e != cudaSuccess) {
         (void)cudaGetLastError();
         return SHARPV_ERR_CUDA;
     }
@@ -354,7 +370,7 @@ sharpv_status simt_by_dim(AttnArgs& a, int sms, cudaStream_t stream) {
 
 // query rows of a tile, and bytes of the workspace
 constexpr int kMaxTileRows = 32;
-size_t prefix_bytes(int32_t num_seqs) { return align_up((size_t)(num_seqs + 1) * 8, 256); }
+size_t shared_bytes() { return align_up(kMaxAttnCtas * sizeof(SharedSegment), 256); }
 size_t part_ml_bytes() { return align_up((size_t)kMaxAttnCtas * 2 * 2 * kMaxTileRows * 4, 256); }
 size_t part_o_bytes(int32_t head_dim) { return align_up((size_t)kMaxAttnCtas * 2 * kMaxTileRows * head_dim * 4, 256); }
 
@@ -364,10 +380,10 @@ size_t part_o_bytes(int32_t head_dim) { return align_up((size_t)kMaxAttnCtas * 2
 using namespace sharpv;
 
 extern "C" size_t sharpv_tree_attention_workspace_bytes(int32_t num_seqs, int32_t head_dim) {
-    if (num_seqs < 0) num_seqs = 0;
+    (void)num_seqs;
     if (head_dim < 1) head_dim = 1;
     if (head_dim > kMaxHeadDim) head_dim = kMaxHeadDim;
-    return prefix_bytes(num_seqs) + part_ml_bytes() + part_o_bytes(head_dim);
+    return shared_bytes() + part_ml_bytes() + part_o_bytes(head_dim);
 }
 
 extern "C" sharpv_status sharpv_tree_attention(
@@ -422,9 +438,9 @@ extern "C" sharpv_status sharpv_tree_attention(
     a.split = bf16 ? Split{avg <= 16 || D > 128 ? 16 : 32, kRowsTileKeys, group, H, draft_k != nullptr}
                    : Split{avg <= 8 ? 8 : 32, kSimtKeys, group, H, draft_k != nullptr};
     char* ws = (char*)workspace;
-    a.prefix = (int64_t*)ws;
-    a.part_ml = (float*)(ws + prefix_bytes(num_seqs));
-    a.part_o = (float*)(ws + prefix_bytes(num_seqs) + part_ml_bytes());
+    a.shared = (SharedSegment*)ws;
+    a.part_ml = (float*)(ws + shared_bytes());
+    a.part_o = (float*)(ws + shared_bytes() + part_ml_bytes());
     a.status_word = status_word;
     int sms = 0;
     const sharpv_status ss = current_sms(sms);

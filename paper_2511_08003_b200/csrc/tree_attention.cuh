@@ -28,7 +28,7 @@ struct AttnArgs {
     SeqTables seqs;
     Split split;
     // workspace
-    int64_t* prefix;            // [num_seqs + 1]
+    SharedSegment* shared;      // [ctas]
     float* part_ml;             // [slots][2][rows]: running maximum and sum of each row
     float* part_o;              // [slots][rows][D]: weighted sums, not yet divided
     int ctas;
@@ -59,6 +59,17 @@ __device__ __forceinline__ uint32_t draft_sees(const AttnArgs& a, const SeqInfo&
         sees = key0 / 32 < a.mask_words ? __ldg(a.mask + ((int64_t)s.node0 + i) * a.mask_words + key0 / 32) : 0u;
     }
     return sees & there;
+}
+
+// What thread 0 of a CTA says of the segment it shares with the CTAs behind it: called for every portion.
+__device__ __forceinline__ void note_shared(const Portion& p, const Split& sp, int64_t next_unit, int64_t units, int ctas,
+                                            SharedSegment& seg) {
+    if (p.kt0 != 0 || p.kt1 == p.kt_all) return;
+    seg.node0 = p.s.node0;
+    seg.rows = p.s.nodes * sp.group;
+    seg.h = p.h;
+    seg.rt = p.rt;
+    seg.last = Deal(units, ctas).owner(next_unit + (p.kt_all - p.kt1) - 1);
 }
 
 // out and lse of one row element from its weighted sum, running maximum (log 2 units) and sum

@@ -35,43 +35,15 @@ struct Shared {
     float merge[kWarps][16][C::kCols + 4];
     float m[kWarps][16], l[kWarps][16];
     float top[16], sum[16];
-    uint8_t q[C::kQInRegs ? 16 : MT * 16 * C::kQPitch];
-    uint64_t full[C::kStages], empty[C::kStages];
-    int poison;
+    uint8_t q[2][MT * 16 * C::kQPitch];         // query rows of this portion and the next
+    Portion part[2];                            // kt1 < 0: there are no more
+    int64_t next_unit[2];
+    uint64_t full[C::kStages], empty[C::kStages], part_full[2], part_empty[2];
+    int poison, dead;
     PlanScratch<kThreads> plan;
 };
 
 __device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" :: "n"(kWarps * 32) : "memory"); }
-
-struct Portion {
-    SeqInfo s;
-    int h, rt, kt0, kt1, kt_all, kt_cache;
-};
-
-// The next portion of the CTA's units, or false.  u, b and before move on.
-__device__ __forceinline__ bool next_portion(const AttnArgs& a, Portion& p, int64_t& u, int64_t u_end, int& b, int64_t& before) {
-    bool bad = false;
-    while (u < u_end) {
-        p.s = load_seq(a.seqs, b, bad);
-        const int64_t mine = a.split.units(p.s);
-        if (u - before >= mine) {
-            before += mine;
-            ++b;
-            continue;
-        }
-        p.kt_all = a.split.key_tiles(p.s);
-        p.kt_cache = a.split.cache_tiles(p.s);
-        const int rts = a.split.row_tiles(p.s);
-        const int64_t seg = (u - before) / p.kt_all;
-        p.kt0 = (int)((u - before) % p.kt_all);
-        p.kt1 = (int)min((int64_t)p.kt_all, p.kt0 + (u_end - u));
-        p.h = (int)(seg / rts);
-        p.rt = (int)(seg % rts);
-        u += p.kt1 - p.kt0;
-        return true;
-    }
-    return false;
-}
 
 template <int MT, int DP>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -85,83 +57,101 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
             mbar_init(&sm.full[i], 1);
             mbar_init(&sm.empty[i], 4);
         }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sm.part_full[i], 33);        // 32 lanes' query rows have landed, and the portion is written
+            mbar_init(&sm.part_empty[i], kWarps);
+        }
         mbar_fence_init();
-        sm.poison = 0;
+        sm.poison = sm.dead = 0;
     }
     if (warp == kWarps && lane < 4) tma_prefetch(&maps.cache_k + lane);
     cudaGridDependencySynchronize();
-    const PlanStart plan = plan_cta<kThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, a.prefix, a.status_word);
-    int64_t u = plan.first, before = plan.before;
-    int b = plan.b;
-    Portion p;
+    int64_t first, end;
+    const PlanStart plan = plan_cta<kThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
     bool alive = true;                          // a wait that gave up: nothing is waited for any more, the result is void
-    uint32_t it = 0;                            // tiles of this CTA so far
+    uint32_t it = 0, pn = 0;                    // tiles and portions of this CTA so far
+    constexpr int R = MT * 16;
+    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
 
-    if (warp == kWarps) {                       // the loads
-        if (lane != 0) return;
-        while (next_portion(a, p, u, plan.end, b, before)) {
-            for (int kt = p.kt0; kt < p.kt1 && alive; ++kt, ++it) {
-                const int stage = it % C::kStages;
-                if (it >= C::kStages) alive = mbar_wait(&sm.empty[stage], (it / C::kStages - 1) & 1);
-                if (!alive) break;
-                const bool drafted = kt >= p.kt_cache;
-                if (drafted && !a.split.draft) {            // the empty tile of rows without keys
-                    mbar_arrive(&sm.full[stage]);
-                    continue;
+    if (warp == kWarps) {                       // portions, query rows and tiles ahead of the warps that compute
+        Walk walk(plan, first, end);
+        Portion p;
+        for (;; ++pn) {
+            const int slot = pn & 1;
+            const bool more = walk.next(a.seqs, a.split, p);
+            if (pn >= 2 && alive) alive = __all_sync(0xffffffffu, mbar_wait(&sm.part_empty[slot], ((pn >> 1) - 1) & 1));
+            if (more) {
+                const int r_base = p.rt * R, r_all = p.s.nodes * G;
+                for (int x = lane; x < R * (DP / 8); x += 32) {
+                    const int r = x / (DP / 8), c = x % (DP / 8), row = r_base + r;
+                    const bool there = row < r_all && c * 8 < D;
+                    const char* q = a.q;
+                    if (there) q += (int64_t)(p.s.node0 + row / G) * a.q_node + ((int64_t)(p.h * G + row % G) * D + c * 8) * 2;
+                    cp_async16(sm.q[slot] + r * C::kQPitch + c * 16, q, there);
                 }
-                mbar_expect(&sm.full[stage], 2 * C::kTileBytes);
-                const CUtensorMap* mk = drafted ? &maps.draft_k : &maps.cache_k;
-                const CUtensorMap* mv = drafted ? &maps.draft_v : &maps.cache_v;
-                const int row = drafted ? p.s.node0 + (kt - p.kt_cache) * kKeys : (int)p.s.begin + kt * kKeys;
-#pragma unroll
-                for (int x = 0; x < C::kHalves; ++x)
-                    tma_load(sm.tiles[stage][0] + x * kKeys * 128, mk, &sm.full[stage], x * 64, row, p.h);
-#pragma unroll
-                for (int x = 0; x < C::kHalves; ++x)
-                    tma_load(sm.tiles[stage][1] + x * kKeys * 128, mv, &sm.full[stage], x * 64, row, p.h);
             }
+            cp_async_arrive(&sm.part_full[slot]);
+            if (lane == 0) {
+                if (!more) p.kt1 = -1;
+                sm.part[slot] = p;
+                sm.next_unit[slot] = walk.u;
+                mbar_arrive(&sm.part_full[slot]);
+            }
+            if (!more) break;
+            if (lane == 0) {
+                for (int kt = p.kt0; kt < p.kt1; ++kt, ++it) {
+                    const int stage = it % C::kStages;
+                    if (alive && it >= C::kStages) alive = mbar_wait(&sm.empty[stage], (it / C::kStages - 1) & 1);
+                    if (!alive) break;
+                    const bool drafted = kt >= p.kt_cache;
+                    if (drafted && !a.split.draft) {            // the empty tile of rows without keys
+                        mbar_arrive(&sm.full[stage]);
+                        continue;
+                    }
+                    mbar_expect(&sm.full[stage], 2 * C::kTileBytes);
+                    const CUtensorMap* mk = drafted ? &maps.draft_k : &maps.cache_k;
+                    const CUtensorMap* mv = drafted ? &maps.draft_v : &maps.cache_v;
+                    const int row = drafted ? p.s.node0 + (kt - p.kt_cache) * kKeys : (int)p.s.begin + kt * kKeys;
+#pragma unroll
+                    for (int x = 0; x < C::kHalves; ++x)
+                        tma_load(sm.tiles[stage][0] + x * kKeys * 128, mk, &sm.full[stage], x * 64, row, p.h);
+#pragma unroll
+                    for (int x = 0; x < C::kHalves; ++x)
+                        tma_load(sm.tiles[stage][1] + x * kKeys * 128, mv, &sm.full[stage], x * 64, row, p.h);
+                }
+            }
+            alive = __all_sync(0xffffffffu, alive);
         }
-        if (!alive) {
+        if (!alive && lane == 0) {
             report(a.status_word, SHARPV_ERR_TIMEOUT);
             for (int i = 0; i < C::kStages && (uint32_t)i < it; ++i) {      // copies in flight land before the CTA ends
                 const uint32_t last = it - 1 - i;
                 (void)mbar_wait(&sm.full[last % C::kStages], (last / C::kStages) & 1);
             }
         }
+        cp_async_wait<0>();
         return;
     }
 
     const int group = warp >> 2, sub = warp & 3;        // tiles of this parity, 16 keys from sub * 16 on
     const int qr = lane >> 2, qc = (lane & 3) * 2;      // fragment row (and row + 8), column (and column + 1)
-    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
-    constexpr int R = MT * 16;
-    while (next_portion(a, p, u, plan.end, b, before)) {
+    SharedSegment shared = {0, 0, 0, 0, -1};
+    for (;; ++pn) {
+        const int at_part = pn & 1;
+        if (alive && !mbar_wait(&sm.part_full[at_part], (pn >> 1) & 1)) {
+            alive = false;
+            report(a.status_word, SHARPV_ERR_TIMEOUT);
+        }
+        if (!alive) sm.dead = 1;
+        consumer_sync();                        // all eight warps go on or none does
+        const Portion p = sm.part[at_part];
+        if (p.kt1 < 0 || sm.dead) break;
         const int r_base = p.rt * R, r_all = p.s.nodes * G;
-        // the query rows, as fragments in registers or in shared memory
+        const uint32_t q_base = smem_u32(sm.q[at_part]) + (lane & 15) * C::kQPitch + (lane >> 4) * 16;
         uint32_t qf[C::kQInRegs ? DP / 16 : 1][4];
-        auto q_row = [&](int row) -> const char* {
-            return a.q + (int64_t)(p.s.node0 + row / G) * a.q_node + (int64_t)(p.h * G + row % G) * D * 2;
-        };
         if constexpr (C::kQInRegs) {
-            const bool in0 = r_base + qr < r_all, in1 = r_base + qr + 8 < r_all;
-            const char* q0 = q_row(in0 ? r_base + qr : 0);
-            const char* q1 = q_row(in1 ? r_base + qr + 8 : 0);
 #pragma unroll
-            for (int ks = 0; ks < DP / 16; ++ks) {
-                const int c = ks * 16 + qc;                 // D is a multiple of 8: c and c + 1 are both inside or not
-                qf[ks][0] = in0 && c < D ? __ldg((const uint32_t*)(q0 + c * 2)) : 0u;
-                qf[ks][1] = in1 && c < D ? __ldg((const uint32_t*)(q1 + c * 2)) : 0u;
-                qf[ks][2] = in0 && c + 8 < D ? __ldg((const uint32_t*)(q0 + c * 2 + 16)) : 0u;
-                qf[ks][3] = in1 && c + 8 < D ? __ldg((const uint32_t*)(q1 + c * 2 + 16)) : 0u;
-            }
-        } else {
-            for (int x = threadIdx.x; x < R * (DP / 8); x += kWarps * 32) {
-                const int r = x / (DP / 8), c = x % (DP / 8);
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (r_base + r < r_all && c * 8 < D) v = ld_cached(q_row(r_base + r) + c * 16);
-                *reinterpret_cast<uint4*>(sm.q + r * C::kQPitch + c * 16) = v;
-            }
-            consumer_sync();
+            for (int ks = 0; ks < DP / 16; ++ks) ldmatrix4(qf[ks], q_base + ks * 32);
         }
         float o[MT][DP / 8][4];
         float m[MT][2], l[MT][2];
@@ -200,7 +190,7 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
                         mma_bf16(s[t][1], qf[ks], k4[2], k4[3]);
                     } else {
                         uint32_t q4[4];
-                        ldmatrix4(q4, smem_u32(sm.q) + (t * 16 + (lane & 15)) * C::kQPitch + ks * 32 + (lane >> 4) * 16);
+                        ldmatrix4(q4, q_base + t * 16 * C::kQPitch + ks * 32);
                         mma_bf16(s[t][0], q4, k4[0], k4[1]);
                         mma_bf16(s[t][1], q4, k4[2], k4[3]);
                     }
@@ -380,9 +370,14 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
                 consumer_sync();
             }
         }
-        if (threadIdx.x == 0) sm.poison = 0;
-        consumer_sync();
+        if (threadIdx.x == 0) {
+            sm.poison = 0;
+            note_shared(p, a.split, sm.next_unit[at_part], plan.units, a.ctas, shared);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.part_empty[at_part]);
     }
+    if (threadIdx.x == 0) a.shared[blockIdx.x] = shared;
 }
 
 template <int MT, int DP>
