@@ -375,7 +375,8 @@ sharpv_status sharpv_kv_compact_rope(
  * workspace [dev]: sharpv_tree_attention_workspace_bytes() bytes, 256-byte aligned, contents undefined before
  * and after; calls that may overlap on the GPU need a workspace each.
  */
-size_t sharpv_tree_attention_workspace_bytes(int32_t num_seqs, int32_t head_dim);
+size_t sharpv_tree_attention_workspace_bytes(int32_t num_seqs, int64_t total_nodes, int32_t num_q_heads,
+                                             int32_t num_kv_heads, int32_t head_dim, sharpv_dtype dtype);
 
 sharpv_status sharpv_tree_attention(
     const void* q, int64_t ld_q,

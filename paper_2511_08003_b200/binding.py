@@ -129,7 +129,7 @@ def lib():
                                          i64, i32, C.c_double, vp, sz, vp, vp]
     lay = C.POINTER(KVLayout)
     L.sharpv_tree_attention_workspace_bytes.restype = sz
-    L.sharpv_tree_attention_workspace_bytes.argtypes = [i32, i32]
+    L.sharpv_tree_attention_workspace_bytes.argtypes = [i32, i64, i32, i32, i32, C.c_int]
     L.sharpv_tree_attention.restype = C.c_int
     L.sharpv_tree_attention.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, lay, i32, i64, i32, vp, vp, vp, i64, vp,
                                         i32, f32, vp, vp, vp, sz, vp, vp]
@@ -557,8 +557,10 @@ def _sequences(seq_begin, seq_len, node_offsets, device):
             _on(node_offsets, "node_offsets", device, torch.int32, (B + 1,)))
 
 
-def sharpv_tree_attention_workspace_bytes(num_seqs: int, head_dim: int) -> int:
-    return int(lib().sharpv_tree_attention_workspace_bytes(num_seqs, head_dim))
+def sharpv_tree_attention_workspace_bytes(num_seqs: int, total_nodes: int, num_q_heads: int, num_kv_heads: int,
+                                          head_dim: int, dtype: int = BF16) -> int:
+    return int(lib().sharpv_tree_attention_workspace_bytes(num_seqs, total_nodes, num_q_heads, num_kv_heads, head_dim,
+                                                           dtype))
 
 
 def sharpv_tree_attention(q: torch.Tensor, kv: torch.Tensor, layer: int, seq_begin: torch.Tensor,
@@ -588,7 +590,7 @@ def sharpv_tree_attention(q: torch.Tensor, kv: torch.Tensor, layer: int, seq_beg
     if out is None:
         out = {"out": torch.empty((N, HQ, D), dtype=q.dtype, device=dev),
                "lse": torch.empty((N, HQ), dtype=torch.float32, device=dev)}
-    ws = _workspace(workspace, sharpv_tree_attention_workspace_bytes(B, D), dev)
+    ws = _workspace(workspace, sharpv_tree_attention_workspace_bytes(B, N, HQ, lay.num_kv_heads, D, lay.dtype), dev)
     rc = _call("sharpv_tree_attention", kv, q.data_ptr(), ldq,
                None if draft_k is None else draft_k.data_ptr(), ldk, None if draft_v is None else draft_v.data_ptr(), ldv,
                HQ, kv.data_ptr(), lay, layer, kv.shape[3], B, begin, length, offs, N, mask, words,

@@ -52,9 +52,14 @@ __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" :: "r"(smem_u32(bar)) : "memory");
 }
 
-// Waits for the phase of the given parity to complete, at most kWaitTries times the hardware's own suspend time
-// (far beyond any kernel of this library); false if it did not.
-constexpr int kWaitTries = 1 << 18;
+// Waits for the phase of the given parity to complete, for two seconds at most (far beyond any kernel of this library);
+// false if it did not.
+constexpr unsigned long long kWaitNs = 2000000000ull;
+__device__ __forceinline__ unsigned long long global_ns() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
 __device__ __forceinline__ bool mbar_try(uint64_t* bar, uint32_t parity) {
     uint32_t done;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
@@ -62,9 +67,15 @@ __device__ __forceinline__ bool mbar_try(uint64_t* bar, uint32_t parity) {
     return done != 0;
 }
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity) {
-    for (int i = 0; i < kWaitTries; ++i)
+    unsigned long long since = 0;
+    for (uint32_t i = 1;; ++i) {
         if (mbar_try(bar, parity)) return true;
-    return false;
+        if ((i & 63) == 0) {
+            const unsigned long long now = global_ns();
+            if (since == 0) since = now;
+            else if (now - since > kWaitNs) return false;
+        }
+    }
 }
 
 __device__ __forceinline__ void tma_prefetch(const CUtensorMap* map) {

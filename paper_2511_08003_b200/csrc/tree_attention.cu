@@ -368,22 +368,45 @@ sharpv_status simt_by_dim(AttnArgs& a, int sms, cudaStream_t stream) {
     return simt_launch<DT, R, 256>(a, sms, stream);
 }
 
-// query rows of a tile, and bytes of the workspace
-constexpr int kMaxTileRows = 32;
+// Which kernels a call takes, by the average query rows of a (sequence, KV head).  bf16: the row kernel reads K and V at
+// the memory's rate up to 16 rows; beyond 32 the tensor cores' kernel is ahead.
+constexpr int64_t kMaxRowsPath = 32;
+enum class Path { simt, rows, tc };
+struct Choice {
+    Path path;
+    int rows;               // of a tile
+    int max_ctas;           // sizes the workspace
+};
+Choice choose(sharpv_dtype dtype, int head_dim, int64_t avg_rows) {
+    if (dtype == SHARPV_F32) return {Path::simt, avg_rows <= 8 ? 8 : 32, kMaxAttnCtas};
+    if (head_dim > 128) return {Path::rows, 16, kMaxAttnCtas};
+    if (avg_rows <= 16) return {Path::rows, 16, kMaxAttnCtas};
+    if (avg_rows <= kMaxRowsPath) return {Path::rows, 32, kMaxAttnCtas};
+    return {Path::tc, kTcTileRows, kMaxTcCtas};
+}
+int64_t average_rows(int32_t num_seqs, int64_t total_nodes, int64_t group) {
+    return num_seqs > 0 ? total_nodes * group / num_seqs : 0;
+}
+
+// the parts of the workspace
 size_t shared_bytes() { return align_up(kMaxAttnCtas * sizeof(SharedSegment), 256); }
-size_t part_ml_bytes() { return align_up((size_t)kMaxAttnCtas * 2 * 2 * kMaxTileRows * 4, 256); }
-size_t part_o_bytes(int32_t head_dim) { return align_up((size_t)kMaxAttnCtas * 2 * kMaxTileRows * head_dim * 4, 256); }
+size_t part_ml_bytes(const Choice& c) { return align_up((size_t)c.max_ctas * 2 * 2 * c.rows * 4, 256); }
+size_t part_o_bytes(const Choice& c, int32_t head_dim) { return align_up((size_t)c.max_ctas * 2 * c.rows * head_dim * 4, 256); }
 
 }  // namespace
 }  // namespace sharpv
 
 using namespace sharpv;
 
-extern "C" size_t sharpv_tree_attention_workspace_bytes(int32_t num_seqs, int32_t head_dim) {
-    (void)num_seqs;
+extern "C" size_t sharpv_tree_attention_workspace_bytes(int32_t num_seqs, int64_t total_nodes, int32_t num_q_heads,
+                                                        int32_t num_kv_heads, int32_t head_dim, sharpv_dtype dtype) {
+    if (total_nodes < 0) total_nodes = 0;
+    if (num_kv_heads < 1) num_kv_heads = 1;
+    if (num_q_heads < 0) num_q_heads = 0;
     if (head_dim < 1) head_dim = 1;
     if (head_dim > kMaxHeadDim) head_dim = kMaxHeadDim;
-    return shared_bytes() + part_ml_bytes() + part_o_bytes(head_dim);
+    const Choice c = choose(dtype, head_dim, average_rows(num_seqs, total_nodes, num_q_heads / num_kv_heads));
+    return shared_bytes() + part_ml_bytes(c) + part_o_bytes(c, head_dim);
 }
 
 extern "C" sharpv_status sharpv_tree_attention(
@@ -409,7 +432,7 @@ extern "C" sharpv_status sharpv_tree_attention(
     if (!aligned16(q) || !aligned16(out) || (ld_q * eb) % 16 ||
         (draft_k && (!aligned16(draft_k) || !aligned16(draft_v) || (ld_draft_k * eb) % 16 || (ld_draft_v * eb) % 16)))
         return SHARPV_ERR_UNSUPPORTED;
-    if (workspace_bytes < sharpv_tree_attention_workspace_bytes(num_seqs, D)) return SHARPV_ERR_WORKSPACE;
+    if (workspace_bytes < sharpv_tree_attention_workspace_bytes(num_seqs, total_nodes, num_q_heads, H, D, layout->dtype)) return SHARPV_ERR_WORKSPACE;
     if (!workspace) return SHARPV_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) % 256) return SHARPV_ERR_UNSUPPORTED;
 
@@ -432,25 +455,23 @@ extern "C" sharpv_status sharpv_tree_attention(
     a.lse = out_lse;
     a.seqs = SeqTables{seq_begin, seq_len, node_offsets, num_seqs, cache_tokens, total_nodes};
     const int group = num_q_heads / H;
-    // rows of a tile by the average rows of a (sequence, KV head)
-    const int64_t avg = total_nodes * group / num_seqs;
-    const bool bf16 = layout->dtype == SHARPV_BF16;
-    a.split = bf16 ? Split{avg <= 16 || D > 128 ? 16 : 32, kRowsTileKeys, group, H, draft_k != nullptr}
-                   : Split{avg <= 8 ? 8 : 32, kSimtKeys, group, H, draft_k != nullptr};
+    const Choice ch = choose(layout->dtype, D, average_rows(num_seqs, total_nodes, group));
+    a.split = Split{ch.rows, ch.path == Path::tc ? kTcTileKeys : (ch.path == Path::rows ? kRowsTileKeys : kSimtKeys), group, H,
+                    draft_k != nullptr};
     char* ws = (char*)workspace;
     a.shared = (SharedSegment*)ws;
     a.part_ml = (float*)(ws + shared_bytes());
-    a.part_o = (float*)(ws + shared_bytes() + part_ml_bytes());
+    a.part_o = (float*)(ws + shared_bytes() + part_ml_bytes(ch));
     a.status_word = status_word;
     int sms = 0;
     const sharpv_status ss = current_sms(sms);
     if (ss != SHARPV_OK) return ss;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    sharpv_status st;
-    if (bf16) {
-        st = attn_rows_launch(a, sms, stream);
+    if (ch.path == Path::tc) return attn_tc_launch(a, sms, stream);
+    if (ch.path == Path::rows) {
+        const sharpv_status st = attn_rows_launch(a, sms, stream);
         return st == SHARPV_OK ? join_launch<SHARPV_BF16>(a, stream) : st;
     }
-    st = avg <= 8 ? simt_by_dim<SHARPV_F32, 8>(a, sms, stream) : simt_by_dim<SHARPV_F32, 32>(a, sms, stream);
+    const sharpv_status st = ch.rows == 8 ? simt_by_dim<SHARPV_F32, 8>(a, sms, stream) : simt_by_dim<SHARPV_F32, 32>(a, sms, stream);
     return st == SHARPV_OK ? join_launch<SHARPV_F32>(a, stream) : st;
 }

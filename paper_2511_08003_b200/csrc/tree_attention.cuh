@@ -46,6 +46,11 @@ sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps);
 constexpr int kRowsTileKeys = 64;
 sharpv_status attn_rows_launch(AttnArgs& a, int sms, cudaStream_t stream);
 
+// Many query rows, bf16, head_dim of at most 128: a.split has kTcTileRows rows and kTcTileKeys keys a tile.  Joins the parts
+// as well.
+constexpr int kTcTileRows = 256, kTcTileKeys = 128, kMaxTcCtas = 160;
+sharpv_status attn_tc_launch(AttnArgs& a, int sms, cudaStream_t stream);
+
 // Which keys of the 32 from key0 on node `i` of a sequence sees, as bits (drafted tokens).
 __device__ __forceinline__ uint32_t draft_sees(const AttnArgs& a, const SeqInfo& s, int i, int key0) {
     const int left = s.nodes - key0;

@@ -1,0 +1,590 @@
+// Attention of many query rows over a K/V cache in bf16 (drafted trees, chunks of a prompt) on the fifth-generation
+// tensor cores.
+//
+// A segment is up to 256 query rows of one (sequence, KV head), as two tiles of 128; a unit is 128 keys of it.  One
+// CTA per SM: a warp that loads (TMA ring of K and V tiles, 32 KB each at head_dim 128), a warp that issues
+// the products, two warpgroups that turn scores into weights, two warps that fetch query rows and clean the value tiles
+// that hold rows nobody may see.  Work goes in steps, each one stream's scores, weights and weighted sums:
+//   more than 128 rows   stream w owns row tile w; both take every key tile
+//   up to 128 rows       both streams own row tile 0 and take the key tiles in turn; joined in tensor memory at the end
+// While one stream's warpgroup works on its scores the tensor cores work for the other.  Scores, weights (bf16, in the
+// place of the scores they came from) and sums live in tensor memory: 2 x (128 + 128) columns.  A thread owns a
+// query row, so the softmax needs no shuffles.  Sums are rescaled only when a row's maximum has grown by more than 2^8
+// since they last were (weights then stay below 256, which bf16 and the fp32 sums hold as well as 1).
+#include "tcgen05.cuh"
+#include "tree_attention.cuh"
+
+#include <cuda_bf16.h>
+
+namespace sharpv {
+namespace {
+
+constexpr int kKeys = kTcTileKeys;              // 128
+constexpr int kRows = kTcTileRows;              // 256
+constexpr int kThreads = 384;
+constexpr int kLoadWarp = 8, kMmaWarp = 9, kAuxWarp = 10;       // warps 0-3, 4-7: the streams; 10, 11: aux
+constexpr uint32_t kCols = 512, kSumCol = 256;  // tensor memory: scores of stream w at 128 w, sums at 256 + DP w
+constexpr float kLazy = 8.f;
+
+template <int DP>
+struct Cfg {
+    static constexpr int kTileBytes = 128 * DP * 2;             // 128 rows of Q, K or V
+    static constexpr int kStages = DP == 64 ? 10 : 5;           // K and V tiles in turn
+    static constexpr int kHalf = 128 * 128;                     // bytes of a 64-column box
+};
+
+template <int DP>
+struct Shared {
+    using C = Cfg<DP>;
+    uint8_t q[2][C::kTileBytes];
+    uint8_t tiles[C::kStages][C::kTileBytes];
+    Portion part[2];                            // kt1 < 0: there are no more
+    int64_t next_unit[2];
+    float m[128], l[128];                       // of stream 1, when the streams share their rows
+    uint64_t full[C::kStages], empty[C::kStages];
+    uint64_t part_full[2], part_empty[2];
+    uint64_t clean[C::kStages];                 // value tiles: gone through (or nothing to do)
+    uint64_t q_full, q_empty;
+    uint64_t scores[2], weights[2], sums[2];    // per stream: products done, weights written, weighted sums added
+    uint64_t merge_full, merge_done, drain;
+    int poison[2];
+    uint32_t tmem;
+    PlanScratch<kThreads> plan;
+};
+
+// what every role derives from a portion
+struct Steps {
+    int tiles, n;               // key tiles, steps
+    bool pair;                  // two row tiles
+    __device__ __forceinline__ Steps(const Portion& p, int group) {
+        tiles = p.kt1 - p.kt0;
+        pair = p.s.nodes * group - p.rt * kRows > 128;
+        n = pair ? 2 * tiles : tiles;
+    }
+    __device__ __forceinline__ int tile(int step) const { return pair ? step >> 1 : step; }
+    __device__ __forceinline__ int of_stream(int w) const { return pair ? tiles : (tiles + 1 - w) >> 1; }
+};
+
+// Value tiles are the odd items of the ring; with an odd number of stages a stage holds one every other time.
+template <int STAGES>
+__device__ __forceinline__ uint32_t clean_phase(uint32_t item) { return STAGES % 2 ? item / STAGES >> 1 : item / STAGES; }
+
+// keys of tile kt that are there, and whether it has to be masked
+__device__ __forceinline__ int keys_left(const AttnArgs& a, const Portion& p, int kt) {
+    return kt < p.kt_cache ? p.s.len - kt * kKeys : (a.split.draft ? p.s.nodes - (kt - p.kt_cache) * kKeys : 0);
+}
+__device__ __forceinline__ bool tile_masked(const AttnArgs& a, const Portion& p, int kt) {
+    return kt >= p.kt_cache || keys_left(a, p, kt) < kKeys;
+}
+
+// Sums of two at a time (one instruction each on this architecture).
+__device__ __forceinline__ uint64_t pack2(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnMaps maps) {
+    using C = Cfg<DP>;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    auto& sm = *reinterpret_cast<Shared<DP>*>(smem_raw);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < C::kStages; ++i) {
+            mbar_init(&sm.full[i], 1);
+            mbar_init(&sm.empty[i], 1);
+            mbar_init(&sm.clean[i], 2);             // both aux warps
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sm.part_full[i], 1);
+            mbar_init(&sm.part_empty[i], 11);           // the warps that read it
+            mbar_init(&sm.scores[i], 1);
+            mbar_init(&sm.weights[i], 128);
+            mbar_init(&sm.sums[i], 1);
+        }
+        mbar_init(&sm.q_full, 64);
+        mbar_init(&sm.q_empty, 1);
+        mbar_init(&sm.merge_full, 128);
+        mbar_init(&sm.merge_done, 128);
+        mbar_init(&sm.drain, 1);
+        mbar_fence_init();
+    }
+    if (warp == kMmaWarp) tmem_alloc(&sm.tmem, kCols);
+    if (warp == kLoadWarp && lane < 4) tma_prefetch(&maps.cache_k + lane);
+    cudaGridDependencySynchronize();
+    int64_t first, end;
+    const PlanStart plan = plan_cta<kThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
+    tc_fence_after();
+    const uint32_t tmem = sm.tmem;
+    bool alive = true;          // a wait that gave up ends the role; the others then give up as well
+    auto wait = [&](uint64_t* bar, uint32_t phase) {            // by one thread
+        if (alive && !mbar_wait(bar, phase & 1)) alive = false;
+        return alive;
+    };
+    auto wait_warp = [&](uint64_t* bar, uint32_t phase) {       // by a whole warp, with one answer
+        if (alive) alive = __all_sync(0xffffffffu, mbar_wait(bar, phase & 1));
+        return alive;
+    };
+
+    if (warp >= kLoadWarp) {
+        fewer_registers<96>();
+        if (warp == kLoadWarp) {
+            if (lane == 0) {
+                Walk walk(plan, first, end);
+                Portion p;
+                uint32_t it = 0;
+                for (uint32_t pn = 0; alive; ++pn) {
+                    const int at = pn & 1;
+                    const bool more = walk.next(a.seqs, a.split, p);
+                    if (pn >= 2 && !wait(&sm.part_empty[at], (pn >> 1) - 1)) break;
+                    if (!more) p.kt1 = -1;
+                    sm.poison[at] = 0;
+                    sm.part[at] = p;
+                    sm.next_unit[at] = walk.u;
+                    mbar_arrive(&sm.part_full[at]);
+                    if (!more) break;
+                    for (int kt = p.kt0; kt < p.kt1 && alive; ++kt) {
+                        const bool drafted = kt >= p.kt_cache;
+                        const int row = drafted ? p.s.node0 + (kt - p.kt_cache) * kKeys : (int)p.s.begin + kt * kKeys;
+                        for (int v = 0; v < 2; ++v, ++it) {
+                            const int stage = it % C::kStages;
+                            if (it >= C::kStages && !wait(&sm.empty[stage], it / C::kStages - 1)) break;
+                            if (drafted && !a.split.draft) {        // the empty tile of rows without keys
+                                mbar_arrive(&sm.full[stage]);
+                                continue;
+                            }
+                            mbar_expect(&sm.full[stage], C::kTileBytes);
+                            const CUtensorMap* map = drafted ? (v ? &maps.draft_v : &maps.draft_k) : (v ? &maps.cache_v : &maps.cache_k);
+#pragma unroll
+                            for (int x = 0; x < DP / 64; ++x)
+                                tma_load(sm.tiles[stage] + x * C::kHalf, map, &sm.full[stage], x * 64, row, p.h);
+                        }
+                    }
+                }
+                if (!alive) {
+                    for (uint32_t i = 0; i < (uint32_t)C::kStages && i < it; ++i) {     // copies in flight land first
+                        const uint32_t last = it - 1 - i;
+                        (void)mbar_wait(&sm.full[last % C::kStages], (last / C::kStages) & 1);
+                    }
+                }
+            }
+        } else if (warp == kMmaWarp) {
+            if (lane == 0) {
+                uint32_t it0 = 0, steps0[2] = {0, 0};           // tiles and steps of the portions before
+                const uint32_t k_shape = mma_shape(128, false), v_shape = mma_shape(DP, true);
+                for (uint32_t pn = 0;; ++pn) {
+                    if (!wait(&sm.part_full[pn & 1], pn >> 1)) break;
+                    const Portion p = sm.part[pn & 1];
+                    if (p.kt1 < 0) break;
+                    const Steps st(p, G);
+                    if (!wait(&sm.q_full, pn)) break;
+                    auto scores = [&](int t) {                  // scores of step t
+                        const int j = st.tile(t), w = t & 1;
+                        const uint32_t item = it0 + 2 * j;
+                        if (!st.pair || w == 0) {
+                            if (!wait(&sm.full[item % C::kStages], item / C::kStages)) return;
+                        }
+                        tc_fence_after();
+                        const uint32_t qb = smem_u32(sm.q[st.pair ? w : 0]), kb = smem_u32(sm.tiles[item % C::kStages]);
+#pragma unroll
+                        for (int ks = 0; ks < DP / 16; ++ks) {
+                            const uint32_t off = (ks >> 2) * C::kHalf + (ks & 3) * 32;
+                            mma_ss(tmem + w * 128, smem_operand(qb + off, 1024, 16), smem_operand(kb + off, 1024, 16), k_shape, ks > 0);
+                        }
+                        mma_commit(&sm.scores[w]);
+                        if (!st.pair || w == 1) mma_commit(&sm.empty[item % C::kStages]);
+                        if (t == st.n - 1) mma_commit(&sm.q_empty);
+                    };
+                    scores(0);
+                    if (st.n > 1 && alive) scores(1);
+                    for (int t = 0; t < st.n && alive; ++t) {
+                        const int j = st.tile(t), w = t & 1;
+                        const uint32_t item = it0 + 2 * j + 1, mine = t >> 1;
+                        if (!st.pair || w == 0) {
+                            if (!wait(&sm.clean[item % C::kStages], clean_phase<C::kStages>(item)) ||
+                                !wait(&sm.full[item % C::kStages], item / C::kStages)) break;
+                        }
+                        if (!wait(&sm.weights[w], steps0[w] + mine)) break;
+                        tc_fence_after();
+                        const uint32_t vb = smem_u32(sm.tiles[item % C::kStages]);
+#pragma unroll
+                        for (int kk = 0; kk < kKeys / 16; ++kk)
+                            mma_ts(tmem + kSumCol + w * DP, tmem + w * 128 + kk * 8, smem_operand(vb + kk * 2048, 1024, C::kHalf), v_shape,
+                                   mine > 0 || kk > 0);
+                        mma_commit(&sm.sums[w]);
+                        if (!st.pair || w == 1) mma_commit(&sm.empty[item % C::kStages]);
+                        if (t + 2 < st.n) scores(t + 2);
+                    }
+                    if (!alive) break;
+                    it0 += 2 * st.tiles;
+                    steps0[0] += st.of_stream(0);
+                    steps0[1] += st.of_stream(1);
+                    mbar_arrive(&sm.part_empty[pn & 1]);
+                }
+                mma_commit(&sm.drain);              // the products in flight end before the tensor memory is given back
+                (void)mbar_wait(&sm.drain, 0);
+            }
+        } else {
+            // query rows, and value tiles with rows that are not there (or, drafted, that some query rows must not see):
+            // 0 times what such rows hold would not be 0 if that is not finite
+            const int t64 = threadIdx.x - kAuxWarp * 32;
+            uint32_t it0 = 0;
+            for (uint32_t pn = 0;; ++pn) {
+                if (!wait_warp(&sm.part_full[pn & 1], pn >> 1)) break;
+                const Portion p = sm.part[pn & 1];
+                if (p.kt1 < 0) break;
+                const Steps st(p, G);
+                if (pn > 0 && !wait_warp(&sm.q_empty, pn - 1)) break;
+                const int r_base = p.rt * kRows, rows = min(p.s.nodes * G - r_base, st.pair ? 256 : 128);
+                constexpr int CH = DP / 8;
+                for (int x = t64; x < (st.pair ? 256 : 128) * CH; x += 64) {
+                    const int r = x / CH, c = x % CH;
+                    const bool there = r < rows && c * 8 < D;
+                    const char* q = a.q;
+                    if (there) {
+                        const int row = r_base + r;
+                        q += (int64_t)(p.s.node0 + row / G) * a.q_node + ((int64_t)(p.h * G + row % G) * D + c * 8) * 2;
+                    }
+                    cp_async16(sm.q[r >> 7] + (c >> 3) * C::kHalf + swizzle128(r & 127, c & 7), q, there);
+                }
+                cp_async_wait_all();
+                async_proxy_fence();
+                mbar_arrive(&sm.q_full);
+                for (int kt = p.kt0; kt < p.kt1; ++kt) {
+                    const uint32_t item = it0 + 2 * (kt - p.kt0) + 1;
+                    if (!wait_warp(&sm.full[item % C::kStages], item / C::kStages)) break;
+                    if (tile_masked(a, p, kt)) {
+                        uint8_t* tile = sm.tiles[item % C::kStages];
+                        const int left = keys_left(a, p, kt);
+                        const bool drafted = kt >= p.kt_cache;
+                        bool odd = false;
+                        for (int x = t64; x < 128 * CH; x += 64) {
+                            const int key = (x >> 3) & 127;         // 128 rows of 8 chunks, then the next 64 columns
+                            uint4* at = reinterpret_cast<uint4*>(tile + x * 16);
+                            if (key >= left) {
+                                *at = make_uint4(0, 0, 0, 0);
+                            } else if (drafted) {
+                                const uint4 v = *at;
+                                const uint4 off = make_uint4(nonfinite_bf16(v.x), nonfinite_bf16(v.y), nonfinite_bf16(v.z), nonfinite_bf16(v.w));
+                                if (off.x | off.y | off.z | off.w) {
+                                    odd = true;
+                                    *at = make_uint4(v.x & ~off.x, v.y & ~off.y, v.z & ~off.z, v.w & ~off.w);
+                                }
+                            }
+                        }
+                        if (odd) sm.poison[pn & 1] = 1;
+                        async_proxy_fence();
+                        __syncwarp();
+                    }
+                    if (lane == 0) mbar_arrive(&sm.clean[item % C::kStages]);
+                }
+                if (!alive) break;
+                it0 += 2 * st.tiles;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.part_empty[pn & 1]);
+            }
+        }
+    } else {
+        more_registers<200>();
+        const int w = warp >> 2, r_in = threadIdx.x & 127;          // stream, row of its tile
+        const uint32_t lanes = (uint32_t)(warp & 3) * 32 << 16;
+        const uint32_t t_scores = tmem + lanes + w * 128, t_sums = tmem + lanes + kSumCol + w * DP;
+        const uint64_t c2 = pack2(a.scale_log2, a.scale_log2);
+        uint32_t steps = 0, merges = 0;
+        SharedSegment shared = {0, 0, 0, 0, -1};
+        for (uint32_t pn = 0;; ++pn) {
+            if (!wait_warp(&sm.part_full[pn & 1], pn >> 1)) break;
+            const Portion p = sm.part[pn & 1];
+            if (p.kt1 < 0) break;
+            const Steps st(p, G);
+            const int r_all = p.s.nodes * G, r_warp = p.rt * kRows + (st.pair ? w * 128 : 0) + (warp & 3) * 32;
+            const int row = r_warp + lane;
+            const bool work = r_warp < r_all;                       // some row of the warp is there
+            const int mine = st.of_stream(w);
+            float m2 = neg_inf(), l = 0.f;                          // maximum in log 2 units, as used; sum
+            for (int x = 0; x < mine; ++x) {
+                const int kt = p.kt0 + (st.pair ? x : 2 * x + w);
+                if (!wait_warp(&sm.scores[w], steps + x)) break;
+                if (work) {
+                    tc_fence_after();
+                    uint32_t s[4][32];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) tmem_ld32(s[i], t_scores + i * 32);
+                    tmem_wait_ld();
+                    if (tile_masked(a, p, kt)) {
+                        const int left = keys_left(a, p, kt);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t sees;
+                            if (kt < p.kt_cache) {
+                                const int n = left - i * 32;
+                                sees = n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u);
+                            } else {
+                                sees = a.split.draft && row < r_all ? draft_sees(a, p.s, row / G, (kt - p.kt_cache) * kKeys + i * 32) : 0u;
+                            }
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (!(sees >> k & 1)) s[i][k] = 0xff800000u;
+                        }
+                    }
+                    float top4[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        top4[i] = __uint_as_float(s[i][0]);
+#pragma unroll
+                        for (int k = 1; k < 32; ++k) top4[i] = fmaxf(top4[i], __uint_as_float(s[i][k]));
+                    }
+                    const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * a.scale_log2;
+                    const bool grows = top > m2 + kLazy;
+                    if (__any_sync(0xffffffffu, grows)) {
+                        const float next = grows ? top : m2;
+                        const float al = grows ? ex2(m2 - next) : 1.f;      // 0 where nothing was seen yet
+                        m2 = next;
+                        l *= al;
+                        if (x > 0) {
+                            if (!wait_warp(&sm.sums[w], steps + x - 1)) break;
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < DP; c += 32) {
+                                uint32_t o[32];
+                                tmem_ld32(o, t_sums + c);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * al);
+                                tmem_st32(t_sums + c, o);
+                            }
+                        }
+                    }
+                    const float base = m2 == neg_inf() ? 0.f : m2;
+                    const uint64_t nb = pack2(-base, -base);
+                    uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const uint64_t y = fma2(pack2(__uint_as_float(s[i][2 * k]), __uint_as_float(s[i][2 * k + 1])), c2, nb);
+                            float y0, y1;
+                            unpack2(y, y0, y1);
+                            y0 = ex2(y0);
+                            y1 = ex2(y1);
+                            sum2[k & 1] = add2(sum2[k & 1], pack2(y0, y1));
+                            // weights are rounded to bf16 for the product with the values; their sum is not
+                            pk[k] = pack_bf16(y0, y1);
+                        }
+                        tmem_st16(t_scores + i * 16, pk);
+                    }
+                    float s0, s1;
+                    unpack2(add2(sum2[0], sum2[1]), s0, s1);
+                    l += s0 + s1;
+                    tmem_wait_st();
+                    tc_fence_before();
+                }
+                mbar_arrive(&sm.weights[w]);
+            }
+            if (!alive) break;
+            // ---- the portion's result
+            if (mine > 0 && !wait_warp(&sm.sums[w], steps + mine - 1)) break;
+            tc_fence_after();
+            steps += mine;
+            float f0 = 1.f, f1 = 0.f;
+            if (!st.pair) {
+                if (w == 1) {
+                    sm.m[r_in] = m2;
+                    sm.l[r_in] = l;
+                    mbar_arrive(&sm.merge_full);
+                    if (!wait_warp(&sm.merge_done, merges)) break;
+                } else {
+                    if (!wait_warp(&sm.merge_full, merges)) break;
+                    tc_fence_after();
+                    const float m1 = sm.m[r_in], l1 = sm.l[r_in], top = fmaxf(m2, m1), base = top == neg_inf() ? 0.f : top;
+                    f0 = ex2(m2 - base);
+                    f1 = ex2(m1 - base);
+                    l = st.of_stream(1) > 0 ? l * f0 + l1 * f1 : l * f0;
+                    m2 = top;
+                }
+                ++merges;
+            }
+            if (w == 0 || st.pair) {
+                const bool both = !st.pair && st.of_stream(1) > 0;
+                const bool complete = p.kt0 == 0 && p.kt1 == p.kt_all;
+                const int slot = portion_slot(blockIdx.x, p.kt0);
+                const int r = row - p.rt * kRows;
+                const float inv = row_scale(l);
+                const int64_t at = (int64_t)(p.s.node0 + row / G) * HQ + p.h * G + row % G;
+                const bool poison = sm.poison[pn & 1] != 0;
+                if (work) {
+#pragma unroll 1
+                    for (int c = 0; c < DP; c += 32) {
+                        if (c >= D) break;
+                        uint32_t o[32];
+                        tmem_ld32(o, t_sums + c);
+                        tmem_wait_ld();
+                        if (both) {
+                            uint32_t o1[32];
+                            tmem_ld32(o1, t_sums + DP + c);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                o[k] = __float_as_uint(__uint_as_float(o[k]) * f0 + __uint_as_float(o1[k]) * f1);
+                        }
+                        if (row < r_all) {
+                            if (poison) {           // drafted values that were set aside come back to the rows that see them
+                                const int j0 = (max(p.kt0, p.kt_cache) - p.kt_cache) * kKeys;
+                                const int j1 = min(p.s.nodes, (p.kt1 - p.kt_cache) * kKeys);
+#pragma unroll 1
+                                for (int j = j0; j < j1; ++j) {
+                                    if (!(draft_sees(a, p.s, row / G, j & ~31) >> (j & 31) & 1)) continue;
+                                    const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(
+                                        a.draft_v + (int64_t)(p.s.node0 + j) * a.dv_node) + p.h * D + c;
+#pragma unroll
+                                    for (int k = 0; k < 32; ++k) {
+                                        if (c + k >= D) break;
+                                        const float y = __bfloat162float(v[k]);
+                                        if (!finite_f32(y)) o[k] = __float_as_uint(__uint_as_float(o[k]) + y);
+                                    }
+                                }
+                            }
+#pragma unroll
+                            for (int k = 0; k < 32; k += 8) {
+                                if (c + k >= D) break;
+                                float y[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(o[k + i]);
+                                if (complete) {
+                                    *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at * D + c + k) =
+                                        make_uint4(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
+                                                   pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
+                                } else {            // four columns of all rows next to each other: whole lines a warp
+                                    float4* to = reinterpret_cast<float4*>(a.part_o) + ((int64_t)slot * (D / 4) + (c + k) / 4) * kRows + r;
+                                    __stcg(to, make_float4(y[0], y[1], y[2], y[3]));
+                                    __stcg(to + kRows, make_float4(y[4], y[5], y[6], y[7]));
+                                }
+                            }
+                        }
+                    }
+                    if (row < r_all) {
+                        if (complete) {
+                            a.lse[at] = row_lse(m2, l);
+                        } else {
+                            a.part_ml[(int64_t)slot * 2 * kRows + r] = m2;
+                            a.part_ml[((int64_t)slot * 2 + 1) * kRows + r] = l;
+                        }
+                    }
+                }
+                if (!st.pair) {
+                    tc_fence_before();
+                    mbar_arrive(&sm.merge_done);
+                }
+            }
+            if (threadIdx.x == 0) note_shared(p, a.split, sm.next_unit[pn & 1], plan.units, a.ctas, shared);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.part_empty[pn & 1]);
+        }
+        if (threadIdx.x == 0) a.shared[blockIdx.x] = shared;
+    }
+    if (!alive) report(a.status_word, SHARPV_ERR_TIMEOUT);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == kMmaWarp) tmem_free(tmem, kCols);
+}
+
+// Joins a segment's parts: CTA (c, y, z) takes 32 rows (lane = row) and eight groups of four columns (one a warp) of
+// the segment that CTA c begins; the parts are added in the order of the CTAs.
+constexpr int kJoinAhead = 8;
+__global__ void __launch_bounds__(256)
+attn_tc_join_kernel(const __grid_constant__ AttnArgs a) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x;
+    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
+    const int r = blockIdx.y * 32 + lane, c4 = blockIdx.z * 8 + warp;
+    cudaGridDependencySynchronize();
+    const SharedSegment seg = a.shared[c0];
+    const int row = seg.rt * kRows + r;
+    if (seg.last < 0 || row >= seg.rows || c4 * 4 >= D) return;
+    const int c1 = seg.last;
+    float top = neg_inf();
+#pragma unroll 8
+    for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(a.part_ml + (int64_t)(c * 2 + (c == c0)) * 2 * kRows + r));
+    const float base = top == neg_inf() ? 0.f : top;
+    float sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = c0; i <= c1; i += kJoinAhead) {
+        float4 v[kJoinAhead];
+        float m[kJoinAhead], l[kJoinAhead];
+#pragma unroll
+        for (int x = 0; x < kJoinAhead; ++x) {
+            const int c = i + x;
+            v[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+            m[x] = neg_inf();
+            l[x] = 0.f;
+            if (c <= c1) {
+                const int64_t slot = c * 2 + (c == c0);
+                v[x] = __ldcg(reinterpret_cast<const float4*>(a.part_o) + (slot * (D / 4) + c4) * kRows + r);
+                m[x] = __ldcg(a.part_ml + slot * 2 * kRows + r);
+                l[x] = __ldcg(a.part_ml + (slot * 2 + 1) * kRows + r);
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < kJoinAhead; ++x) {
+            if (i + x > c1) break;
+            const float f = ex2(m[x] - base);
+            sum = fmaf(f, l[x], sum);
+            acc.x = fmaf(f, v[x].x, acc.x);
+            acc.y = fmaf(f, v[x].y, acc.y);
+            acc.z = fmaf(f, v[x].z, acc.z);
+            acc.w = fmaf(f, v[x].w, acc.w);
+        }
+    }
+    const float inv = row_scale(sum);
+    const int64_t at = (int64_t)(seg.node0 + row / G) * HQ + seg.h * G + row % G;
+    *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at * D + c4 * 4) =
+        make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    if (c4 == 0) a.lse[at] = row_lse(top, sum);
+}
+
+template <int DP>
+sharpv_status launch(const AttnArgs& a, cudaStream_t stream) {
+    auto kern = attn_tc_kernel<DP>;
+    const size_t smem = sizeof(Shared<DP>);
+    static_assert(sizeof(Shared<DP>) <= 227 * 1024, "shared memory of one CTA");
+    static_assert(kSumCol + 2 * DP <= kCols, "tensor memory");
+    AttnMaps maps;
+    const sharpv_status ms = encode_attn_maps(a, kKeys, maps);
+    if (ms != SHARPV_OK) return ms;
+    const int64_t all = a.seqs.total_nodes * a.split.group;
+    const unsigned rows = (unsigned)(all < kRows ? all : kRows);
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
+        launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kThreads), smem, stream, a, maps) != cudaSuccess ||
+        launch_dependent(attn_tc_join_kernel, dim3((unsigned)a.ctas, (rows + 31) / 32, (unsigned)(a.head_dim + 31) / 32), dim3(256), 0,
+                         stream, a) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SHARPV_ERR_CUDA;
+    }
+    return SHARPV_OK;
+}
+
+}  // namespace
+
+sharpv_status attn_tc_launch(AttnArgs& a, int sms, cudaStream_t stream) {
+    a.ctas = sms < kMaxTcCtas ? sms : kMaxTcCtas;
+    return a.head_dim <= 64 ? launch<64>(a, stream) : launch<128>(a, stream);
+}
+
+}  // namespace sharpv

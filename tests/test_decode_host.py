@@ -78,8 +78,8 @@ def test_attention_mass_refusals(L, change, status):
 
 
 def test_workspace_queries(L):
-    a = L.sharpv_tree_attention_workspace_bytes(1, 64)
-    assert 0 < a <= L.sharpv_tree_attention_workspace_bytes(1, 128) <= L.sharpv_tree_attention_workspace_bytes(5000, 128)
+    a = L.sharpv_tree_attention_workspace_bytes(1, 1, 14, 2, 64, 1)
+    assert 0 < a <= L.sharpv_tree_attention_workspace_bytes(1, 1, 14, 2, 128, 1) <= L.sharpv_tree_attention_workspace_bytes(1, 500, 14, 2, 128, 1)
     assert a % 256 == 0
     assert L.sharpv_attention_mass_workspace_bytes(2, 1000, 4) >= 16000
 

@@ -82,7 +82,8 @@ class Case:
         out = {"out": mem.empty(self.q.shape, self.dtype), "lse": mem.empty((N, self.H * self.G), torch.float32)}
         out["out"].fill_(7.0)
         out["lse"].fill_(7.0)
-        ws = mem.empty(sv.sharpv_tree_attention_workspace_bytes(len(self.length), self.D), torch.uint8)
+        ws = mem.empty(sv.sharpv_tree_attention_workspace_bytes(len(self.length), N, self.H * self.G, self.H, self.D,
+                                                               sv.BF16 if self.bf16 else sv.F32), torch.uint8)
         status = torch.zeros(1, dtype=torch.int32, device="cuda")
         got = sv.sharpv_tree_attention(self.q, self.kv, self.layer, *self.tables, self.dk, self.dv, self.tree,
                                        scale=scale, out=out, workspace=ws, status_word=status)
@@ -227,7 +228,7 @@ def test_tree_attention_same_bits_again_captured_and_on_a_stream(nodes):
         again = sv.sharpv_tree_attention(*args)
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(first["out"], again["out"]) and torch.equal(first["lse"], again["lse"])
-    ws = torch.full((sv.sharpv_tree_attention_workspace_bytes(2, 128),), 0xFF, dtype=torch.uint8, device="cuda")
+    ws = torch.full((sv.sharpv_tree_attention_workspace_bytes(2, sum(nodes), 14, 2, 128),), 0xFF, dtype=torch.uint8, device="cuda")
     out = {k: torch.zeros_like(v) for k, v in first.items()}
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
