@@ -400,9 +400,9 @@ sharpv_status sharpv_tree_attention(
  * mass [dev] float[cache_tokens] or NULL: what the rows collected so far, row p at mass[p]; NULL and decay == 0
  *   both mean that nothing is read and the sum starts at 0.  out_mass [dev] float[cache_tokens] may be mass.
  * The sequences' cache rows must not overlap.  Sums are fp32 in a fixed order.
- * workspace as above, sharpv_attention_mass_workspace_bytes() bytes.
+ * workspace as above, sharpv_attention_mass_workspace_bytes() bytes (0 for SHARPV_BF16 caches: may be NULL).
  */
-size_t sharpv_attention_mass_workspace_bytes(int32_t num_seqs, int64_t cache_tokens, int32_t num_kv_heads);
+size_t sharpv_attention_mass_workspace_bytes(int64_t cache_tokens, int32_t num_kv_heads, sharpv_dtype dtype);
 
 sharpv_status sharpv_attention_mass(
     const void* q, int64_t ld_q, const float* lse, const float* node_weight, int32_t num_q_heads,

@@ -134,7 +134,7 @@ def lib():
     L.sharpv_tree_attention.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, lay, i32, i64, i32, vp, vp, vp, i64, vp,
                                         i32, f32, vp, vp, vp, sz, vp, vp]
     L.sharpv_attention_mass_workspace_bytes.restype = sz
-    L.sharpv_attention_mass_workspace_bytes.argtypes = [i32, i64, i32]
+    L.sharpv_attention_mass_workspace_bytes.argtypes = [i64, i32, C.c_int]
     L.sharpv_attention_mass.restype = C.c_int
     L.sharpv_attention_mass.argtypes = [vp, i64, vp, vp, i32, vp, lay, i32, i64, i32, vp, vp, vp, i64, f32, f32, vp,
                                         vp, vp, sz, vp, vp]
@@ -601,8 +601,8 @@ def sharpv_tree_attention(q: torch.Tensor, kv: torch.Tensor, layer: int, seq_beg
     return out
 
 
-def sharpv_attention_mass_workspace_bytes(num_seqs: int, cache_tokens: int, num_kv_heads: int) -> int:
-    return int(lib().sharpv_attention_mass_workspace_bytes(num_seqs, cache_tokens, num_kv_heads))
+def sharpv_attention_mass_workspace_bytes(cache_tokens: int, num_kv_heads: int, dtype: int = BF16) -> int:
+    return int(lib().sharpv_attention_mass_workspace_bytes(cache_tokens, num_kv_heads, dtype))
 
 
 def sharpv_attention_mass(q: torch.Tensor, lse: torch.Tensor, kv: torch.Tensor, layer: int, seq_begin: torch.Tensor,
@@ -620,13 +620,15 @@ def sharpv_attention_mass(q: torch.Tensor, lse: torch.Tensor, kv: torch.Tensor, 
     T = kv.shape[3]
     if out is None:
         out = torch.zeros(T, dtype=torch.float32, device=dev)
-    ws = _workspace(workspace, sharpv_attention_mass_workspace_bytes(B, T, lay.num_kv_heads), dev)
+    need = 0 if lay.dtype == BF16 else sharpv_attention_mass_workspace_bytes(T, lay.num_kv_heads, lay.dtype)
+    ws = _workspace(workspace, need, dev) if need else None
     rc = _call("sharpv_attention_mass", kv, q.data_ptr(), ldq, _on(lse, "lse", dev, torch.float32, (N, HQ)),
                None if node_weight is None else _on(node_weight, "node_weight", dev, torch.float32, (N,)), HQ,
                kv.data_ptr(), lay, layer, T, B, begin, length, offs, N,
                lay.head_dim ** -0.5 if scale is None else scale, decay,
                None if mass is None else _on(mass, "mass", dev, torch.float32, (T,)),
-               _on(out, "out", dev, torch.float32, (T,)), ws.data_ptr(), ws.numel(),
+               _on(out, "out", dev, torch.float32, (T,)), None if ws is None else ws.data_ptr(),
+               0 if ws is None else ws.numel(),
                _dev(status_word, "status_word", torch.int32), _queue(stream, dev))
     _check("sharpv_attention_mass", rc)
     return out

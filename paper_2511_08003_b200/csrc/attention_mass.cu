@@ -6,10 +6,10 @@
 // others: keys are spread over CTAs, a key's sum over the rows of one KV head stays in a register, and the KV heads'
 // sums are added in a second, small kernel in the order of the heads (no atomics: the order is fixed).
 //
-// Kernels:
+// Kernels (fp32 caches; bf16 ones take the kernel of attention_mass_rows.cu):
 //   mass_simt_kernel      (sequence, KV head, 32 keys) a step, lane = key, on the fp32 units
 //   mass_join_kernel      (dependent launch) adds the heads' sums and what the rows collected before
-#include "decode_common.cuh"
+#include "attention_mass.cuh"
 
 namespace sharpv {
 namespace {
@@ -18,24 +18,6 @@ constexpr int kMassThreads = 128;
 constexpr int kMassKeys = 32;
 constexpr int kNodeWindow = 512;        // nodes whose weights are looked at together
 constexpr int kMaxMassHeadDim = 256;
-
-struct MassArgs {
-    const char* q;
-    int64_t q_node;
-    const float* lse;           // [nodes, heads * group]
-    const float* weight;        // [nodes] or null
-    const char* cache_k;
-    int64_t kv_head, kv_token;
-    int head_dim;
-    float scale_log2, decay;
-    const float* mass;          // null: nothing collected yet
-    float* out;
-    float* part;                // [heads][cache_tokens]
-    SeqTables seqs;
-    Split split;                // rows: all of a sequence's in one tile
-    int ctas;
-    int32_t* status_word;
-};
 
 // The nodes [w0, w0 + kNodeWindow) of a sequence that count, as a list in ascending order.  Returns their number.
 template <int NT>
@@ -217,8 +199,8 @@ sharpv_status mass_by_dim(const MassArgs& a, int sms, cudaStream_t stream) {
 
 using namespace sharpv;
 
-extern "C" size_t sharpv_attention_mass_workspace_bytes(int32_t num_seqs, int64_t cache_tokens, int32_t num_kv_heads) {
-    (void)num_seqs;
+extern "C" size_t sharpv_attention_mass_workspace_bytes(int64_t cache_tokens, int32_t num_kv_heads, sharpv_dtype dtype) {
+    if (dtype == SHARPV_BF16) return 0;
     if (cache_tokens < 1) cache_tokens = 1;
     if (num_kv_heads < 1) num_kv_heads = 1;
     return align_up((size_t)cache_tokens * num_kv_heads * 4, 256);
@@ -245,9 +227,10 @@ extern "C" sharpv_status sharpv_attention_mass(
         ld_q < (int64_t)num_q_heads * D)
         return SHARPV_ERR_INVALID_ARG;
     if (!aligned16(q) || (ld_q * eb) % 16) return SHARPV_ERR_UNSUPPORTED;
-    if (workspace_bytes < sharpv_attention_mass_workspace_bytes(num_seqs, cache_tokens, H)) return SHARPV_ERR_WORKSPACE;
-    if (!workspace) return SHARPV_ERR_INVALID_ARG;
-    if (reinterpret_cast<uintptr_t>(workspace) % 256) return SHARPV_ERR_UNSUPPORTED;
+    const size_t need = sharpv_attention_mass_workspace_bytes(cache_tokens, H, layout->dtype);
+    if (workspace_bytes < need) return SHARPV_ERR_WORKSPACE;
+    if (need > 0 && !workspace) return SHARPV_ERR_INVALID_ARG;
+    if (need > 0 && reinterpret_cast<uintptr_t>(workspace) % 256) return SHARPV_ERR_UNSUPPORTED;
 
     MassArgs a = {};
     a.q = (const char*)q;
@@ -271,11 +254,9 @@ extern "C" sharpv_status sharpv_attention_mass(
     sharpv_status st = current_sms(sms);
     if (st != SHARPV_OK) return st;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    const int64_t avg = total_nodes * group / num_seqs;
-    if (layout->dtype == SHARPV_F32)
-        st = avg <= 8 ? mass_by_dim<SHARPV_F32, 8>(a, sms, stream) : mass_by_dim<SHARPV_F32, 32>(a, sms, stream);
-    else
-        st = avg <= 8 ? mass_by_dim<SHARPV_BF16, 8>(a, sms, stream) : mass_by_dim<SHARPV_BF16, 32>(a, sms, stream);
+    if (layout->dtype == SHARPV_BF16) return mass_rows_launch(a, sms, stream);
+    st = total_nodes * group / num_seqs <= 8 ? mass_by_dim<SHARPV_F32, 8>(a, sms, stream)
+                                             : mass_by_dim<SHARPV_F32, 32>(a, sms, stream);
     if (st != SHARPV_OK) return st;
     const int y = num_seqs < 1024 ? num_seqs : 1024;
     int64_t x = (cache_tokens / num_seqs + 255) / 256;

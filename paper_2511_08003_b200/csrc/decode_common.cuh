@@ -66,6 +66,12 @@ struct Split {
     }
 };
 
+// The split of a call that gives every cached row a value: a unit is `keys` rows of one sequence.
+struct KeySplit {
+    int keys;
+    __host__ __device__ int64_t units(const SeqInfo& s) const { return (s.len + keys - 1) / keys; }
+};
+
 // 64-bit division that takes the 32-bit one where the numbers allow it (nearly always: the 64-bit one is a routine of
 // its own, and several of them in a row cost a microsecond at the start of a kernel).
 __device__ __forceinline__ int64_t div64(int64_t a, int64_t b) {
@@ -104,8 +110,8 @@ struct PlanScratch {
 
 // Every thread of the block (NT threads) gets the plan of this CTA, `first` its first unit and `end` the one behind
 // its last.  CTA 0 reports tables that do not fit.
-template <int NT>
-__device__ __forceinline__ PlanStart plan_cta(const SeqTables& t, const Split& sp, int cta, int ctas,
+template <int NT, class S>
+__device__ __forceinline__ PlanStart plan_cta(const SeqTables& t, const S& sp, int cta, int ctas,
                                               PlanScratch<NT>& sm, int64_t& first, int64_t& end, int32_t* status_word) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per = (t.num_seqs + NT - 1) / NT;

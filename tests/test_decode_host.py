@@ -69,7 +69,10 @@ def test_tree_attention_refusals(L, change, status):
     assert _attn(L, **change) == status
 
 
-@pytest.mark.parametrize("change,status", COMMON + [
+@pytest.mark.parametrize("change,status", [c for c in COMMON if "ws" not in c[0] and "wsb" not in c[0]] + [
+    (dict(lay=_layout(dtype=0, d=64), ldq=28 * 64, ws=None), S.ERR_INVALID_ARG),
+    (dict(lay=_layout(dtype=0, d=64), ldq=28 * 64, ws=P + 16), S.ERR_UNSUPPORTED),
+    (dict(lay=_layout(dtype=0, d=64), ldq=28 * 64, wsb=64), S.ERR_WORKSPACE),
     (dict(decay=-0.5), S.ERR_INVALID_ARG), (dict(decay=float("nan")), S.ERR_INVALID_ARG), (dict(decay=INF), S.ERR_INVALID_ARG),
     (dict(tokens=0), S.OK),
 ])
@@ -81,7 +84,7 @@ def test_workspace_queries(L):
     a = L.sharpv_tree_attention_workspace_bytes(1, 1, 14, 2, 64, 1)
     assert 0 < a <= L.sharpv_tree_attention_workspace_bytes(1, 1, 14, 2, 128, 1) <= L.sharpv_tree_attention_workspace_bytes(1, 500, 14, 2, 128, 1)
     assert a % 256 == 0
-    assert L.sharpv_attention_mass_workspace_bytes(2, 1000, 4) >= 16000
+    assert L.sharpv_attention_mass_workspace_bytes(1000, 4, 0) >= 16000 and L.sharpv_attention_mass_workspace_bytes(1000, 4, 1) == 0
 
 
 @pytest.mark.parametrize("change,status", [

@@ -263,7 +263,7 @@ def _mass_case(dtype, H, G, D, lens, nodes, decay, weights, seed=0, spread=1.0):
     mem = Guarded()
     out = mem.empty(T, torch.float32)
     out.fill_(-3.0)
-    ws = mem.empty(sv.sharpv_attention_mass_workspace_bytes(len(lens), T, H), torch.uint8)
+    ws = mem.empty(sv.sharpv_attention_mass_workspace_bytes(T, H, sv.BF16 if c.bf16 else sv.F32), torch.uint8)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     res = sv.sharpv_attention_mass(c.q, got["lse"], c.kv, c.layer, *c.tables, mass=hist,
                                    node_weight=None if w is None else torch.from_numpy(w).cuda(), decay=decay, out=out,
@@ -306,7 +306,9 @@ def test_attention_mass_sums_to_the_number_of_rows():
     out = mass.clone()
     twice = sv.sharpv_attention_mass(c.q, got["lse"], c.kv, c.layer, *c.tables, mass=out, out=out)     # in place
     used = torch.cat([torch.arange(b, b + n) for b, n in zip(c.begin, c.length)]).cuda()
-    assert torch.equal(twice[used], mass[used] + mass[used])
+    # the weights are the same bits; query rows that do not fit at a time add to the old value one lot after the other,
+    # here two: (m + s0) + s1 against 2 (s0 + s1), all positive, three roundings of u each against one
+    assert bool(((twice[used] - 2 * mass[used]).abs() <= 4 * ref.U * twice[used]).all())
 
 
 def test_attention_mass_history_is_not_read_when_it_decays_to_nothing():
