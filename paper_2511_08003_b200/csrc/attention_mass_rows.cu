@@ -17,8 +17,8 @@ constexpr int kKeys = 32;               // of a tile
 constexpr int kWarps = 8, kPairs = 4;
 constexpr int kThreads = kWarps * 32 + 32;
 constexpr int kRingBytes = 96 * 1024;
-constexpr int kQueryBytes = 112 * 1024; // query rows, their weights and log-sum-exps
-constexpr int kListMax = 1024;          // nodes of a pass
+constexpr int kQueryBytes = 108 * 1024; // query rows, their weights and log-sum-exps
+constexpr int kRowsMax = 512;           // query rows of a head in a pass
 
 template <int DP>
 struct Cfg {
@@ -37,11 +37,12 @@ struct Shared {
     using C = Cfg<DP>;
     uint8_t tiles[C::kStages][C::kTileBytes];
     uint64_t full[C::kStages], empty[C::kStages];
-    int list[kListMax];
+    int list[kRowsMax + 1];                                 // nodes of a pass that count
+    int64_t row_at[kRowsMax];                               // byte offset of a query row (of head 0 of its group), -1: none
     int scan[kWarps];
-    int dead;
+    int dead, unseen;
     PlanScratch<kThreads> plan;
-    __align__(16) uint8_t query[kQueryBytes];               // [heads][rows] pitch, then log-sum-exps, then weights
+    __align__(16) uint8_t query[kQueryBytes];               // [heads][rows] pitch, then log-sum-exps [heads][rows], weights [rows]
 };
 
 __device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" :: "n"(kWarps * 32) : "memory"); }
@@ -73,6 +74,33 @@ struct KeyWalk {
     }
 };
 
+// The weights of N blocks of eight query rows for the warp's 16 keys, added to the thread's two keys.
+template <int N, int DP>
+__device__ __forceinline__ void weigh(const uint32_t (&kf)[DP / 16][4], uint32_t qb, const float* lse2, const float* weight, int nb,
+                                      float scale_log2, float& sum0, float& sum1) {
+    float c[N][4];
+#pragma unroll
+    for (int j = 0; j < N; ++j) c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < DP / 16; ks += 2) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            uint32_t q4[4];
+            ldmatrix4(q4, qb + (nb + j) * 8 * Cfg<DP>::kPitch + ks * 32);
+            mma_bf16(c[j], kf[ks], q4[0], q4[1]);
+            mma_bf16(c[j], kf[ks + 1], q4[2], q4[3]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const float2 ls = *reinterpret_cast<const float2*>(lse2 + (nb + j) * 8), wt = *reinterpret_cast<const float2*>(weight + (nb + j) * 8);
+        sum0 = fmaf(wt.x, ex2(fmaf(c[j][0], scale_log2, -ls.x)), sum0);
+        sum0 = fmaf(wt.y, ex2(fmaf(c[j][1], scale_log2, -ls.y)), sum0);
+        sum1 = fmaf(wt.x, ex2(fmaf(c[j][2], scale_log2, -ls.x)), sum1);
+        sum1 = fmaf(wt.y, ex2(fmaf(c[j][3], scale_log2, -ls.y)), sum1);
+    }
+}
+
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1)
 mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUtensorMap map, const Pass ps) {
@@ -88,7 +116,7 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
             mbar_init(&sm.empty[i], 2);
         }
         mbar_fence_init();
-        sm.dead = 0;
+        sm.dead = sm.unseen = 0;
     }
     if (warp == kWarps && lane == 0) tma_prefetch(&map);
     cudaGridDependencySynchronize();
@@ -153,8 +181,8 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
 
         for (int rp = 0;; ++rp) {
             // ---- the nodes of this pass: rows [rp * rows, ...) of the rows of the nodes that count, node by node
-            const int64_t row0 = (int64_t)rp * ps.rows;
-            const int k0 = (int)(row0 / G);                             // first node of the pass, in order of those that count
+            const int row0 = rp * ps.rows;
+            const int k0 = row0 / G;                                    // first node of the pass, in order of those that count
             consumer_sync();
             if (sm.dead) return;
             int seen = 0;
@@ -173,46 +201,63 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
                         if (w < warp) at += sm.scan[w];
                         seen += sm.scan[w];
                     }
-                    if (on && at >= k0 && at - k0 < kListMax) sm.list[at - k0] = x;
+                    if (on && at >= k0 && at - k0 < kRowsMax + 1) sm.list[at - k0] = x;
                     consumer_sync();
                 }
             }
-            const int64_t all_rows = (int64_t)seen * G;
-            const int rows = (int)max((int64_t)0, min((int64_t)ps.rows, all_rows - row0));       // of this pass, a head
+            const int all_rows = seen * G;
+            const int rows = max(0, min(ps.rows, all_rows - row0));     // of this pass, a head
             const int blocks = (rows + 7) / 8;
+            for (int r = tid; r < blocks * 8; r += kWarps * 32) {
+                int64_t at = -1;
+                float wt = 0.f;
+                if (r < rows) {
+                    const int k = (row0 + r) / G, g = row0 + r - k * G;
+                    const int64_t node = s.node0 + (a.weight == nullptr ? k : sm.list[k - k0]);
+                    at = node * a.q_node + (int64_t)g * D * 2;
+                    wt = a.weight == nullptr ? 1.f : __ldg(a.weight + node);
+                }
+                sm.row_at[r] = at;
+                weight[r] = wt;
+            }
+            consumer_sync();
             for (int hp = 0; hp < head_passes; ++hp) {
                 const int h0 = hp * ps.heads, hn = min(H - h0, ps.heads);
                 if (hp > 0) consumer_sync();
                 constexpr int CH = DP / 8;
-                for (int x = tid; x < hn * blocks * 8 * CH; x += kWarps * 32) {
-                    const int c = x % CH, hr = x / CH, r = hr % (blocks * 8), h = hr / (blocks * 8);
-                    const int64_t row = row0 + r;
-                    bool there = r < rows && c * 8 < D;
-                    const char* q = a.q;
-                    if (there) {
-                        const int k = (int)(row / G), g = (int)(row - (int64_t)k * G);
-                        const int64_t node = s.node0 + (a.weight == nullptr ? k : sm.list[k - k0]);
-                        there = __ldg(a.lse + node * HQ + (h0 + h) * G + g) != neg_inf();
-                        q += node * a.q_node + ((int64_t)((h0 + h) * G + g) * D + c * 8) * 2;
+                for (int h = 0; h < hn; ++h) {
+                    for (int r = tid / CH; r < blocks * 8; r += kWarps * 32 / CH) {
+                        const int c = tid % CH;
+                        const int64_t at = sm.row_at[r];
+                        const bool there = at >= 0 && c * 8 < D;
+                        cp_async16(sm.query + (size_t)(h * ps.rows + r) * C::kPitch + c * 16,
+                                   there ? a.q + at + (int64_t)(h0 + h) * G * D * 2 + c * 16 : a.q, there);
                     }
-                    cp_async16(sm.query + (size_t)(h * ps.rows + r) * C::kPitch + c * 16, q, there);
-                }
-                for (int x = tid; x < hn * blocks * 8; x += kWarps * 32) {
-                    const int r = x % (blocks * 8), h = x / (blocks * 8);
-                    const int64_t row = row0 + r;
-                    float ls = 0.f, wt = 0.f;
-                    if (r < rows) {
-                        const int k = (int)(row / G), g = (int)(row - (int64_t)k * G);
-                        const int64_t node = s.node0 + (a.weight == nullptr ? k : sm.list[k - k0]);
-                        ls = __ldg(a.lse + node * HQ + (h0 + h) * G + g);
-                        wt = a.weight == nullptr ? 1.f : __ldg(a.weight + node);
-                        if (ls == neg_inf()) ls = wt = 0.f;             // saw nothing: its query row is zero here
+                    for (int r = tid; r < blocks * 8; r += kWarps * 32) {
+                        float ls = 0.f;
+                        if (r < rows) {
+                            const int k = (row0 + r) / G, g = row0 + r - k * G;
+                            const int64_t node = s.node0 + (a.weight == nullptr ? k : sm.list[k - k0]);
+                            ls = __ldg(a.lse + node * HQ + (h0 + h) * G + g);
+                            if (ls == neg_inf()) sm.unseen = 1;
+                        }
+                        lse2[h * ps.rows + r] = ls * kLog2e;
                     }
-                    lse2[h * ps.rows + r] = ls * kLog2e;
-                    weight[h * ps.rows + r] = wt;
                 }
                 cp_async_wait_all();
                 consumer_sync();
+                if (sm.unseen) {
+                    // rows that saw nothing add nothing, whatever their queries hold: a zero row under a log-sum-exp of +inf
+                    for (int x = tid; x < hn * blocks * 8; x += kWarps * 32) {
+                        const int r = x % (blocks * 8), h = x / (blocks * 8);
+                        if (lse2[h * ps.rows + r] != neg_inf()) continue;
+                        lse2[h * ps.rows + r] = -neg_inf();
+                        for (int c = 0; c < CH; ++c)
+                            *reinterpret_cast<uint4*>(sm.query + (size_t)(h * ps.rows + r) * C::kPitch + c * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    consumer_sync();
+                    if (tid == 0) sm.unseen = 0;
+                }
                 const bool fresh = rp == 0 && hp == 0;
                 for (int kt = walk.kt0; kt < walk.kt1; kt += kPairs) {
                     const int n = min(kPairs, walk.kt1 - kt);
@@ -247,22 +292,15 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
                             if (lane == 0) mbar_arrive(&sm.empty[stage]);
                             const uint32_t qb = smem_u32(sm.query) + (uint32_t)(h * ps.rows + (lane & 7)) * C::kPitch + (lane >> 3) * 16;
                             const float* hl = lse2 + h * ps.rows + (lane & 3) * 2;
-                            const float* hw = weight + h * ps.rows + (lane & 3) * 2;
-                            for (int nb = 0; nb < blocks; ++nb) {
-                                float c[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                                for (int ks = 0; ks < DP / 16; ks += 2) {
-                                    uint32_t q4[4];
-                                    ldmatrix4(q4, qb + nb * 8 * C::kPitch + ks * 32);
-                                    mma_bf16(c, kf[ks], q4[0], q4[1]);
-                                    mma_bf16(c, kf[ks + 1], q4[2], q4[3]);
-                                }
-                                const float2 ls = *reinterpret_cast<const float2*>(hl + nb * 8), wt = *reinterpret_cast<const float2*>(hw + nb * 8);
-                                sum0 = fmaf(wt.x, ex2(fmaf(c[0], a.scale_log2, -ls.x)), sum0);
-                                sum0 = fmaf(wt.y, ex2(fmaf(c[1], a.scale_log2, -ls.y)), sum0);
-                                sum1 = fmaf(wt.x, ex2(fmaf(c[2], a.scale_log2, -ls.x)), sum1);
-                                sum1 = fmaf(wt.y, ex2(fmaf(c[3], a.scale_log2, -ls.y)), sum1);
+                            const float* hw = weight + (lane & 3) * 2;
+                            // four blocks of eight query rows at a time: products of one block wait for one another
+                            int nb = 0;
+                            for (; nb + 4 <= blocks; nb += 4) weigh<4, DP>(kf, qb, hl, hw, nb, a.scale_log2, sum0, sum1);
+                            if (nb + 2 <= blocks) {
+                                weigh<2, DP>(kf, qb, hl, hw, nb, a.scale_log2, sum0, sum1);
+                                nb += 2;
                             }
+                            if (nb < blocks) weigh<1, DP>(kf, qb, hl, hw, nb, a.scale_log2, sum0, sum1);
                         }
                         it += hn * n;
                     }
@@ -273,7 +311,7 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
                     if (writes && my_key < s.len) a.out[s.begin + my_key] = old + ((lane & 3) == 0 ? sum0 : sum1);
                 }
             }
-            if (row0 + ps.rows >= all_rows) break;
+            if (all_rows - row0 <= ps.rows) break;
         }
 
     }
@@ -310,7 +348,7 @@ sharpv_status mass_rows_launch(MassArgs& a, int sms, cudaStream_t stream) {
     const int64_t fit = kQueryBytes / ((int64_t)ps.heads * row_bytes) / 8 * 8;
     const int64_t can = (a.seqs.total_nodes * a.split.group + 7) / 8 * 8;
     ps.rows = (int)(can < fit ? (can > 8 ? can : 8) : fit);
-    if (ps.rows > kListMax) ps.rows = kListMax;
+    if (ps.rows > kRowsMax) ps.rows = kRowsMax;
     if (DP == 64) return launch<64>(a, ps, stream);
     if (DP == 128) return launch<128>(a, ps, stream);
     return launch<256>(a, ps, stream);
