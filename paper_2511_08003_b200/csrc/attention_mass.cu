@@ -18,6 +18,7 @@ constexpr int kMassThreads = 128;
 constexpr int kMassKeys = 32;
 constexpr int kNodeWindow = 512;        // nodes whose weights are looked at together
 constexpr int kMaxMassHeadDim = 256;
+constexpr int64_t kMaxRowsPath = 32;    // bf16: average rows up to which the row kernel is taken
 
 // The nodes [w0, w0 + kNodeWindow) of a sequence that count, as a list in ascending order.  Returns their number.
 template <int NT>
@@ -254,8 +255,13 @@ extern "C" sharpv_status sharpv_attention_mass(
     sharpv_status st = current_sms(sms);
     if (st != SHARPV_OK) return st;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    if (layout->dtype == SHARPV_BF16) return mass_rows_launch(a, sms, stream);
-    st = total_nodes * group / num_seqs <= 8 ? mass_by_dim<SHARPV_F32, 8>(a, sms, stream)
+    const int64_t avg = total_nodes * group / num_seqs;     // query rows of a (sequence, KV head)
+    if (layout->dtype == SHARPV_BF16) {
+        const int64_t most = (int64_t)1 << 40;              // what a tensor map's strides can say
+        if (a.kv_token >= most || a.kv_head >= most) return SHARPV_ERR_UNSUPPORTED;
+        return avg > kMaxRowsPath && D <= 128 ? mass_tc_launch(a, avg, sms, stream) : mass_rows_launch(a, sms, stream);
+    }
+    st = avg <= 8 ? mass_by_dim<SHARPV_F32, 8>(a, sms, stream)
                                              : mass_by_dim<SHARPV_F32, 32>(a, sms, stream);
     if (st != SHARPV_OK) return st;
     const int y = num_seqs < 1024 ? num_seqs : 1024;

@@ -23,7 +23,32 @@ struct MassArgs {
     int32_t* status_word;
 };
 
-// bf16 caches: one kernel that writes a.out
+// units in their order; all of a portion belong to one sequence
+struct KeyWalk {
+    int64_t u, end, before;
+    SeqInfo s;
+    int b, kt0, kt1;
+    __device__ __forceinline__ KeyWalk(const PlanStart& p, int64_t first, int64_t last)
+        : u(first), end(last), before(p.before), s(p.s), b(p.b) {}
+    __device__ __forceinline__ bool next(const SeqTables& t, const KeySplit& sp) {
+        if (u >= end) return false;
+        for (;;) {
+            const int64_t mine = sp.units(s);
+            if (u - before < mine) break;
+            before += mine;
+            bool bad = false;
+            s = load_seq(t, ++b, bad);
+        }
+        kt0 = (int)(u - before);
+        kt1 = (int)min(sp.units(s), kt0 + (end - u));
+        u += kt1 - kt0;
+        return true;
+    }
+};
+
+// bf16 caches: kernels that write a.out.  Few query rows a (sequence, KV head), any head_dim; many of them, head_dim of at
+// most 128.
 sharpv_status mass_rows_launch(MassArgs& a, int sms, cudaStream_t stream);
+sharpv_status mass_tc_launch(MassArgs& a, int64_t avg_rows, int sms, cudaStream_t stream);
 
 }  // namespace sharpv

@@ -51,29 +51,6 @@ __device__ __forceinline__ bool counts(const MassArgs& a, int64_t node) {
     return a.weight == nullptr || __ldg(a.weight + node) != 0.f;
 }
 
-// units in their order; all of a portion belong to one sequence
-struct KeyWalk {
-    int64_t u, end, before;
-    SeqInfo s;
-    int b, kt0, kt1;
-    __device__ __forceinline__ KeyWalk(const PlanStart& p, int64_t first, int64_t last)
-        : u(first), end(last), before(p.before), s(p.s), b(p.b) {}
-    __device__ __forceinline__ bool next(const SeqTables& t, const KeySplit& sp) {
-        if (u >= end) return false;
-        for (;;) {
-            const int64_t mine = sp.units(s);
-            if (u - before < mine) break;
-            before += mine;
-            bool bad = false;
-            s = load_seq(t, ++b, bad);
-        }
-        kt0 = (int)(u - before);
-        kt1 = (int)min(sp.units(s), kt0 + (end - u));
-        u += kt1 - kt0;
-        return true;
-    }
-};
-
 // The weights of N blocks of eight query rows for the warp's 16 keys, added to the thread's two keys.
 template <int N, int DP>
 __device__ __forceinline__ void weigh(const uint32_t (&kf)[DP / 16][4], uint32_t qb, const float* lse2, const float* weight, int nb,
@@ -336,8 +313,6 @@ sharpv_status launch(const MassArgs& a, const Pass& ps, cudaStream_t stream) {
 }  // namespace
 
 sharpv_status mass_rows_launch(MassArgs& a, int sms, cudaStream_t stream) {
-    const int64_t most = (int64_t)1 << 40;              // what a tensor map's strides can say
-    if (a.kv_token >= most || a.kv_head >= most) return SHARPV_ERR_UNSUPPORTED;
     a.ctas = sms;
     const int DP = a.head_dim <= 64 ? 64 : (a.head_dim <= 128 ? 128 : 256);
     const int row_bytes = DP * 2 + 16 + 8;
