@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import enum
+import functools
 import os
 from typing import Dict, Optional
 
@@ -185,7 +186,7 @@ def _call(name: str, on: torch.Tensor, *args) -> int:
     """Calls the entry point `name` with the device of `on` current: kernels are launched on the current
     device, and the allocation-free entry point keys its built-in scratch on it."""
     fn = getattr(_lib or lib(), name)
-    if on.device.index == torch.cuda.current_device():
+    if on.get_device() == torch._C._cuda_getDevice():
         return fn(*args)
     with torch.cuda.device(on.device):
         return fn(*args)
@@ -199,14 +200,19 @@ def _workspace(ws: Optional[torch.Tensor], nbytes: int, device) -> torch.Tensor:
     return ws
 
 
+_KV_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
 def kv_layout(kv: torch.Tensor) -> KVLayout:
     """Layout struct of a 5-D view [L, 2, H, T, D_h] (any strides, contiguous last axis).  One-byte
     caches (uint8 / int8 / fp8 tensors) are described as U8: compaction only copies bits."""
-    if kv.dim() != 5 or kv.shape[1] != 2 or kv.stride(4) != 1:
+    n, st = kv.shape, kv.stride()
+    if len(n) != 5 or n[1] != 2 or st[4] != 1:
         raise ValueError("K/V cache must be a [L, 2, H, T, D_h] view with a contiguous last axis")
-    code = U8 if kv.element_size() == 1 else _dtype_code(kv)
-    return KVLayout(kv.shape[0], kv.shape[2], kv.shape[4], code,
-                    kv.stride(0), kv.stride(1), kv.stride(2), kv.stride(3))
+    code = _KV_CODES.get(kv.dtype)
+    if code is None:
+        code = U8 if kv.element_size() == 1 else _dtype_code(kv)
+    return KVLayout(n[0], n[2], n[4], code, st[0], st[1], st[2], st[3])
 
 
 # ------------------------------------------------------------------------------- entry points
@@ -514,49 +520,56 @@ def sharpv_kv_compact_rope(kv_src: torch.Tensor, kv_dst: torch.Tensor, kept_pos:
 
 
 # ------------------------------------------------------------------------------- decoding over the pruned cache
-def _on(t: torch.Tensor, name: str, device, dtype=None, shape=None) -> int:
-    """Address of a contiguous tensor of the given type and shape on the cache's device."""
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}")
-    if dtype is not None and t.dtype != dtype:
+# These calls are short on the device, so what the wrappers cost per call counts: every tensor is checked by one
+# condition, and what is wrong with it is found out only when the condition fails.
+_I32, _F32 = torch.int32, torch.float32
+
+
+def _refuse(t, name, device, dtype, n):
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise ValueError(f"{name} must be a tensor on {device}")
+    if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} must have the shape {tuple(shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{name} must have {n} elements")
+    raise ValueError(f"{name} must be contiguous")
+
+
+def _on(t: torch.Tensor, name: str, device, dtype, n: Optional[int] = None) -> int:
+    """Address of a contiguous tensor of the given type and number of elements on the cache's device."""
+    if t.device != device or t.dtype is not dtype or not t.is_contiguous() or (n is not None and t.numel() != n):
+        _refuse(t, name, device, dtype, n)
     return t.data_ptr()
 
 
-def _heads(t: torch.Tensor, name: str, device, dtype, n: Optional[int], d: int, heads: Optional[int] = None) -> int:
+def _heads(t: torch.Tensor, name: str, device, dtype, n: Optional[int], heads: Optional[int], d: int) -> int:
     """Row stride of a [nodes, heads, d] view whose heads lie next to each other."""
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, as the cache is")
-    if t.dim() != 3 or t.shape[2] != d or (n is not None and t.shape[0] != n) or \
-            (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} must be [nodes, heads, head_dim]")
-    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d):
-        raise ValueError(f"{name} must have its heads next to each other")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * d
+    s, st = t.shape, t.stride()
+    if t.device != device or t.dtype is not dtype or len(s) != 3 or s[2] != d or (n is not None and s[0] != n) or \
+            (heads is not None and s[1] != heads) or st[2] != 1 or (st[1] != d and s[1] > 1):
+        if t.device != device:
+            raise ValueError(f"{name} must be on {device}")
+        if t.dtype is not dtype:
+            raise TypeError(f"{name} must be {dtype}, as the cache is")
+        raise ValueError(f"{name} must be [nodes, heads, head_dim] with its heads next to each other")
+    return st[0] if s[0] > 1 else s[1] * d
+
+
+def _cache(kv: torch.Tensor):
+    if not kv.is_cuda:
+        raise ValueError("the K/V cache must be a CUDA tensor")
+    return kv_layout(kv), kv.device
 
 
 def _queue(stream, device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
 
-def _cache(kv: torch.Tensor):
-    if not kv.is_cuda:
-        raise ValueError("kv must be a CUDA tensor")
-    return kv_layout(kv), kv.device
+def _status(status_word, device):
+    return None if status_word is None else _on(status_word, "status_word", device, _I32)
 
 
-def _sequences(seq_begin, seq_len, node_offsets, device):
-    B = seq_begin.numel()
-    return (B, _on(seq_begin, "seq_begin", device, torch.int32), _on(seq_len, "seq_len", device, torch.int32, (B,)),
-            _on(node_offsets, "node_offsets", device, torch.int32, (B + 1,)))
-
-
+@functools.lru_cache(maxsize=None)
 def sharpv_tree_attention_workspace_bytes(num_seqs: int, total_nodes: int, num_q_heads: int, num_kv_heads: int,
                                           head_dim: int, dtype: int = BF16) -> int:
     return int(lib().sharpv_tree_attention_workspace_bytes(num_seqs, total_nodes, num_q_heads, num_kv_heads, head_dim,
@@ -573,31 +586,37 @@ def sharpv_tree_attention(q: torch.Tensor, kv: torch.Tensor, layer: int, seq_beg
     [nodes, words], bit j of a row = the node sees node j of its sequence (None: nodes 0 .. i).  scale: None =
     head_dim ** -0.5.  Returns dict(out [nodes, q_heads, head_dim], lse [nodes, q_heads])."""
     lay, dev = _cache(kv)
-    D = lay.head_dim
-    ldq = _heads(q, "q", dev, kv.dtype, None, D)
-    N, HQ = q.shape[0], q.shape[1]
-    B, begin, length, offs = _sequences(seq_begin, seq_len, node_offsets, dev)
-    ldk = ldv = 0
+    dtype, D, H = kv.dtype, lay.head_dim, lay.num_kv_heads
+    ldq = _heads(q, "q", dev, dtype, None, None, D)
+    N, HQ = q.shape[:2]
+    B = seq_begin.numel()
+    ldk = ldv = words = 0
+    dk = dv = mask = None
     if draft_k is not None:
-        ldk = _heads(draft_k, "draft_k", dev, kv.dtype, N, D, lay.num_kv_heads)
+        ldk, dk = _heads(draft_k, "draft_k", dev, dtype, N, H, D), draft_k.data_ptr()
     if draft_v is not None:
-        ldv = _heads(draft_v, "draft_v", dev, kv.dtype, N, D, lay.num_kv_heads)
-    words, mask = 0, None
+        ldv, dv = _heads(draft_v, "draft_v", dev, dtype, N, H, D), draft_v.data_ptr()
     if tree_mask is not None:
         if tree_mask.dim() != 2 or tree_mask.shape[0] != N:
             raise ValueError("tree_mask must be [nodes, words]")
-        words, mask = tree_mask.shape[1], _on(tree_mask, "tree_mask", dev, torch.int32)
+        words, mask = tree_mask.shape[1], _on(tree_mask, "tree_mask", dev, _I32)
     if out is None:
-        out = {"out": torch.empty((N, HQ, D), dtype=q.dtype, device=dev),
-               "lse": torch.empty((N, HQ), dtype=torch.float32, device=dev)}
-    ws = _workspace(workspace, sharpv_tree_attention_workspace_bytes(B, N, HQ, lay.num_kv_heads, D, lay.dtype), dev)
-    rc = _call("sharpv_tree_attention", kv, q.data_ptr(), ldq,
-               None if draft_k is None else draft_k.data_ptr(), ldk, None if draft_v is None else draft_v.data_ptr(), ldv,
-               HQ, kv.data_ptr(), lay, layer, kv.shape[3], B, begin, length, offs, N, mask, words,
-               D ** -0.5 if scale is None else scale, _on(out["out"], "out", dev, q.dtype, (N, HQ, D)),
-               _on(out["lse"], "lse", dev, torch.float32, (N, HQ)), ws.data_ptr(), ws.numel(),
-               _dev(status_word, "status_word", torch.int32), _queue(stream, dev))
-    _check("sharpv_tree_attention", rc)
+        o = torch.empty_like(q, memory_format=torch.contiguous_format)
+        lse = torch.empty((N, HQ), dtype=_F32, device=dev)
+        out = {"out": o, "lse": lse}
+        po, pl = o.data_ptr(), lse.data_ptr()
+    else:
+        if out["out"].shape != q.shape or out["lse"].shape != q.shape[:2]:
+            raise ValueError("out must be [nodes, q_heads, head_dim], lse [nodes, q_heads]")
+        po, pl = _on(out["out"], "out", dev, dtype), _on(out["lse"], "lse", dev, _F32)
+    ws = _workspace(workspace, sharpv_tree_attention_workspace_bytes(B, N, HQ, H, D, lay.dtype), dev)
+    rc = _call("sharpv_tree_attention", kv, q.data_ptr(), ldq, dk, ldk, dv, ldv, HQ, kv.data_ptr(), lay, layer,
+               kv.shape[3], B, _on(seq_begin, "seq_begin", dev, _I32), _on(seq_len, "seq_len", dev, _I32, B),
+               _on(node_offsets, "node_offsets", dev, _I32, B + 1), N, mask, words,
+               D ** -0.5 if scale is None else scale, po, pl, ws.data_ptr(), ws.numel(), _status(status_word, dev),
+               _queue(stream, dev))
+    if rc:
+        _check("sharpv_tree_attention", rc)
     return out
 
 
@@ -614,23 +633,27 @@ def sharpv_attention_mass(q: torch.Tensor, lse: torch.Tensor, kv: torch.Tensor, 
     query heads, nodes weighted by node_weight).  Returns out [T] (mass may be passed as out; without it a
     tensor of zeros, so that rows outside the sequences have a value)."""
     lay, dev = _cache(kv)
-    ldq = _heads(q, "q", dev, kv.dtype, None, lay.head_dim)
-    N, HQ = q.shape[0], q.shape[1]
-    B, begin, length, offs = _sequences(seq_begin, seq_len, node_offsets, dev)
-    T = kv.shape[3]
+    D, T = lay.head_dim, kv.shape[3]
+    ldq = _heads(q, "q", dev, kv.dtype, None, None, D)
+    N, HQ = q.shape[:2]
+    if lse.shape != q.shape[:2]:
+        raise ValueError("lse must be [nodes, q_heads]")
+    B = seq_begin.numel()
     if out is None:
-        out = torch.zeros(T, dtype=torch.float32, device=dev)
-    need = 0 if lay.dtype == BF16 else sharpv_attention_mass_workspace_bytes(T, lay.num_kv_heads, lay.dtype)
-    ws = _workspace(workspace, need, dev) if need else None
-    rc = _call("sharpv_attention_mass", kv, q.data_ptr(), ldq, _on(lse, "lse", dev, torch.float32, (N, HQ)),
-               None if node_weight is None else _on(node_weight, "node_weight", dev, torch.float32, (N,)), HQ,
-               kv.data_ptr(), lay, layer, T, B, begin, length, offs, N,
-               lay.head_dim ** -0.5 if scale is None else scale, decay,
-               None if mass is None else _on(mass, "mass", dev, torch.float32, (T,)),
-               _on(out, "out", dev, torch.float32, (T,)), None if ws is None else ws.data_ptr(),
-               0 if ws is None else ws.numel(),
-               _dev(status_word, "status_word", torch.int32), _queue(stream, dev))
-    _check("sharpv_attention_mass", rc)
+        out = torch.zeros(T, dtype=_F32, device=dev)
+    ws, need = None, 0
+    if lay.dtype != BF16:
+        need = sharpv_attention_mass_workspace_bytes(T, lay.num_kv_heads, lay.dtype)
+        ws = _workspace(workspace, need, dev)
+        need = ws.numel()
+    rc = _call("sharpv_attention_mass", kv, q.data_ptr(), ldq, _on(lse, "lse", dev, _F32),
+               None if node_weight is None else _on(node_weight, "node_weight", dev, _F32, N), HQ, kv.data_ptr(), lay,
+               layer, T, B, _on(seq_begin, "seq_begin", dev, _I32), _on(seq_len, "seq_len", dev, _I32, B),
+               _on(node_offsets, "node_offsets", dev, _I32, B + 1), N, D ** -0.5 if scale is None else scale, decay,
+               None if mass is None else _on(mass, "mass", dev, _F32, T), _on(out, "out", dev, _F32, T),
+               None if ws is None else ws.data_ptr(), need, _status(status_word, dev), _queue(stream, dev))
+    if rc:
+        _check("sharpv_attention_mass", rc)
     return out
 
 
@@ -642,23 +665,23 @@ def sharpv_evict_select(mass: torch.Tensor, seq_begin: torch.Tensor, seq_len: to
     highest mass.  capacity: None = the cache's rows.  Returns dict(kept_pos, kept_seq_offsets[, mass])."""
     if not mass.is_cuda or mass.dim() != 1:
         raise ValueError("mass must be a 1-D CUDA tensor")
-    dev, B = mass.device, seq_begin.numel()
+    dev, B, T = mass.device, seq_begin.numel(), mass.numel()
     if capacity is None:
-        capacity = mass.numel()
+        capacity = T
     if out is None:
-        out = {"kept_pos": torch.empty(capacity, dtype=torch.int32, device=dev),
-               "kept_seq_offsets": torch.empty(B + 1, dtype=torch.int32, device=dev)}
+        pos = torch.empty(capacity, dtype=_I32, device=dev)
+        out = {"kept_pos": pos, "kept_seq_offsets": seq_begin.new_empty(B + 1)}
         if want_mass:
-            out["mass"] = torch.empty(capacity, dtype=torch.float32, device=dev)
+            out["mass"] = mass.new_empty(capacity)
     kept_mass = out.get("mass")
-    rc = _call("sharpv_evict_select", mass, _on(mass, "mass", dev, torch.float32), mass.numel(), B,
-               _on(seq_begin, "seq_begin", dev, torch.int32), _on(seq_len, "seq_len", dev, torch.int32, (B,)),
-               _on(budget, "budget", dev, torch.int32, (B,)), sink, recent,
-               _on(out["kept_pos"], "kept_pos", dev, torch.int32, (capacity,)),
-               _on(out["kept_seq_offsets"], "kept_seq_offsets", dev, torch.int32, (B + 1,)),
-               None if kept_mass is None else _on(kept_mass, "out mass", dev, torch.float32, (capacity,)), capacity,
-               _dev(status_word, "status_word", torch.int32), _queue(stream, dev))
-    _check("sharpv_evict_select", rc)
+    rc = _call("sharpv_evict_select", mass, _on(mass, "mass", dev, _F32), T, B,
+               _on(seq_begin, "seq_begin", dev, _I32), _on(seq_len, "seq_len", dev, _I32, B),
+               _on(budget, "budget", dev, _I32, B), sink, recent, _on(out["kept_pos"], "kept_pos", dev, _I32, capacity),
+               _on(out["kept_seq_offsets"], "kept_seq_offsets", dev, _I32, B + 1),
+               None if kept_mass is None else _on(kept_mass, "out mass", dev, _F32, capacity), capacity,
+               _status(status_word, dev), _queue(stream, dev))
+    if rc:
+        _check("sharpv_evict_select", rc)
     return out
 
 
@@ -669,17 +692,17 @@ def sharpv_kv_append(kv_src: torch.Tensor, kv_dst: torch.Tensor, src_pos: torch.
     [L, 2, H, T, D_h] to the rows of kv_dst from dst_begin[b] on.  Returns kv_dst."""
     sl, dev = _cache(kv_src)
     dl, ddev = _cache(kv_dst)
-    if dev != ddev or kv_src.dtype != kv_dst.dtype:
+    if dev != ddev or kv_src.dtype is not kv_dst.dtype:
         raise ValueError("kv_src and kv_dst must share device and dtype")
     if capacity is None:
         capacity = src_pos.numel()
-    if capacity > src_pos.numel():
+    elif capacity > src_pos.numel():
         raise ValueError("capacity is larger than src_pos")
     B = dst_begin.numel()
     rc = _call("sharpv_kv_append", kv_src, kv_src.data_ptr(), sl, kv_src.shape[3], kv_dst.data_ptr(), dl,
-               kv_dst.shape[3], layer_begin, kv_src.shape[0] if layer_end is None else layer_end,
-               _on(src_pos, "src_pos", dev, torch.int32), _on(src_seq_offsets, "src_seq_offsets", dev, torch.int32, (B + 1,)),
-               _on(dst_begin, "dst_begin", dev, torch.int32), B, capacity,
-               _dev(status_word, "status_word", torch.int32), _queue(stream, dev))
-    _check("sharpv_kv_append", rc)
+               kv_dst.shape[3], layer_begin, sl.num_layers if layer_end is None else layer_end,
+               _on(src_pos, "src_pos", dev, _I32), _on(src_seq_offsets, "src_seq_offsets", dev, _I32, B + 1),
+               _on(dst_begin, "dst_begin", dev, _I32), B, capacity, _status(status_word, dev), _queue(stream, dev))
+    if rc:
+        _check("sharpv_kv_append", rc)
     return kv_dst
