@@ -7,10 +7,11 @@
 
 namespace sharpv {
 
-// A map over bf16 planes [heads][rows][D] (byte strides between rows and heads) whose box is 64 elements of
-// `box_rows` rows, laid out in shared memory with the 128-byte swizzle; elements outside read as zero.
-inline bool encode_rows_map(CUtensorMap* map, const void* base, int D, int64_t rows, int64_t row_bytes, int heads,
-                            int64_t head_bytes, int box_rows) {
+// A map over bf16 rows of D elements in two levels (inner count and byte stride, outer count and byte stride) whose box is
+// 64 elements of box_inner x box_outer rows, laid out in shared memory with the 128-byte swizzle; elements outside
+// read as zero.
+inline bool encode_map(CUtensorMap* map, const void* base, int D, int64_t inner, int64_t inner_bytes, int64_t outer,
+                       int64_t outer_bytes, int box_inner, int box_outer) {
     using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -25,13 +26,23 @@ inline bool encode_rows_map(CUtensorMap* map, const void* base, int D, int64_t r
         return reinterpret_cast<Encode>(fn);
     }();
     if (!encode) return false;
-    // a stride that no element needs (one row, one head) may be anything the map accepts
-    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)rows, (cuuint64_t)heads};
-    const cuuint64_t strides[2] = {(cuuint64_t)row_bytes, heads > 1 ? (cuuint64_t)head_bytes : 16u};
-    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, ones[3] = {1, 1, 1};
+    // a stride that no element needs may be anything the map accepts
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)inner, (cuuint64_t)outer};
+    const cuuint64_t strides[2] = {inner > 1 ? (cuuint64_t)inner_bytes : 16u, outer > 1 ? (cuuint64_t)outer_bytes : 16u};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_inner, (cuuint32_t)box_outer}, ones[3] = {1, 1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, ones,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// [heads][rows][D]: a box is box_rows rows of one head
+inline bool encode_rows_map(CUtensorMap* map, const void* base, int D, int64_t rows, int64_t row_bytes, int heads,
+                            int64_t head_bytes, int box_rows) {
+    return encode_map(map, base, D, rows, row_bytes, heads, head_bytes, box_rows, 1);
+}
+// [nodes][heads][D], heads next to each other: a box is box_heads heads of box_nodes nodes
+inline bool encode_heads_map(CUtensorMap* map, const void* base, int D, int heads, int64_t nodes, int64_t node_bytes, int box_heads,
+                             int box_nodes) {
+    return encode_map(map, base, D, heads, (int64_t)D * 2, nodes, node_bytes, box_heads, box_nodes);
 }
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }

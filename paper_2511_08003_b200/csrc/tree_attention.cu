@@ -375,14 +375,15 @@ enum class Path { simt, rows, tc };
 struct Choice {
     Path path;
     int rows;               // of a tile
+    int places;             // for rows in a partial result
     int max_ctas;           // sizes the workspace
 };
-Choice choose(sharpv_dtype dtype, int head_dim, int64_t avg_rows) {
-    if (dtype == SHARPV_F32) return {Path::simt, avg_rows <= 8 ? 8 : 32, kMaxAttnCtas};
-    if (head_dim > 128) return {Path::rows, 16, kMaxAttnCtas};
-    if (avg_rows <= 16) return {Path::rows, 16, kMaxAttnCtas};
-    if (avg_rows <= kMaxRowsPath) return {Path::rows, 32, kMaxAttnCtas};
-    return {Path::tc, kTcTileRows, kMaxTcCtas};
+Choice choose(sharpv_dtype dtype, int head_dim, int group, int64_t avg_rows) {
+    const int few = dtype == SHARPV_F32 ? 8 : 16;
+    if (dtype == SHARPV_BF16 && head_dim <= 128 && group <= 128 && avg_rows > kMaxRowsPath)
+        return {Path::tc, tc_rows(group), kTcPlaces, kMaxTcCtas};
+    const int rows = avg_rows <= few || (dtype == SHARPV_BF16 && head_dim > 128) ? few : 32;
+    return {dtype == SHARPV_F32 ? Path::simt : Path::rows, rows, rows, kMaxAttnCtas};
 }
 int64_t average_rows(int32_t num_seqs, int64_t total_nodes, int64_t group) {
     return num_seqs > 0 ? total_nodes * group / num_seqs : 0;
@@ -390,8 +391,8 @@ int64_t average_rows(int32_t num_seqs, int64_t total_nodes, int64_t group) {
 
 // the parts of the workspace
 size_t shared_bytes() { return align_up(kMaxAttnCtas * sizeof(SharedSegment), 256); }
-size_t part_ml_bytes(const Choice& c) { return align_up((size_t)c.max_ctas * 2 * 2 * c.rows * 4, 256); }
-size_t part_o_bytes(const Choice& c, int32_t head_dim) { return align_up((size_t)c.max_ctas * 2 * c.rows * head_dim * 4, 256); }
+size_t part_ml_bytes(const Choice& c) { return align_up((size_t)c.max_ctas * 2 * 2 * c.places * 4, 256); }
+size_t part_o_bytes(const Choice& c, int32_t head_dim) { return align_up((size_t)c.max_ctas * 2 * c.places * head_dim * 4, 256); }
 
 }  // namespace
 }  // namespace sharpv
@@ -405,7 +406,8 @@ extern "C" size_t sharpv_tree_attention_workspace_bytes(int32_t num_seqs, int64_
     if (num_q_heads < 0) num_q_heads = 0;
     if (head_dim < 1) head_dim = 1;
     if (head_dim > kMaxHeadDim) head_dim = kMaxHeadDim;
-    const Choice c = choose(dtype, head_dim, average_rows(num_seqs, total_nodes, num_q_heads / num_kv_heads));
+    const int group = num_q_heads / num_kv_heads;
+    const Choice c = choose(dtype, head_dim, group > 0 ? group : 1, average_rows(num_seqs, total_nodes, group));
     return shared_bytes() + part_ml_bytes(c) + part_o_bytes(c, head_dim);
 }
 
@@ -455,7 +457,7 @@ extern "C" sharpv_status sharpv_tree_attention(
     a.lse = out_lse;
     a.seqs = SeqTables{seq_begin, seq_len, node_offsets, num_seqs, cache_tokens, total_nodes};
     const int group = num_q_heads / H;
-    const Choice ch = choose(layout->dtype, D, average_rows(num_seqs, total_nodes, group));
+    const Choice ch = choose(layout->dtype, D, group, average_rows(num_seqs, total_nodes, group));
     a.split = Split{ch.rows, ch.path == Path::tc ? kTcTileKeys : (ch.path == Path::rows ? kRowsTileKeys : kSimtKeys), group, H,
                     draft_k != nullptr};
     char* ws = (char*)workspace;

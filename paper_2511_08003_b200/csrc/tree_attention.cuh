@@ -37,7 +37,7 @@ struct AttnArgs {
 
 // Tensor maps of a call (bf16): boxes of 64 columns and a key tile's rows.  draft_* repeat cache_* where there are none.
 struct AttnMaps {
-    CUtensorMap cache_k, cache_v, draft_k, draft_v;
+    CUtensorMap cache_k, cache_v, draft_k, draft_v, query;      // query: boxes of whole nodes' rows of one KV head (tcgen05 kernel)
 };
 sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps);
 
@@ -46,9 +46,10 @@ sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps);
 constexpr int kRowsTileKeys = 64;
 sharpv_status attn_rows_launch(AttnArgs& a, int sms, cudaStream_t stream);
 
-// Many query rows, bf16, head_dim of at most 128: a.split has kTcTileRows rows and kTcTileKeys keys a tile.  Joins the parts
-// as well.
-constexpr int kTcTileRows = 256, kTcTileKeys = 128, kMaxTcCtas = 160;
+// Many query rows, bf16, head_dim and group of at most 128: a.split has tc_rows(group) rows and kTcTileKeys keys a tile.
+// A partial result has room for kTcPlaces rows.  Joins the parts as well.
+constexpr int kTcPlaces = 256, kTcTileKeys = 128, kMaxTcCtas = 160;
+inline int tc_rows(int group) { return 2 * (128 / group * group); }
 sharpv_status attn_tc_launch(AttnArgs& a, int sms, cudaStream_t stream);
 
 // Which keys of the 32 from key0 on node `i` of a sequence sees, as bits (drafted tokens).

@@ -413,6 +413,8 @@ sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps) 
         maps.draft_k = maps.cache_k;
         maps.draft_v = maps.cache_v;
     }
+    if (ok && box_rows == kTcTileKeys)
+        ok = encode_heads_map(&maps.query, a.q, D, H * a.split.group, N, a.q_node, a.split.group, a.split.rows / (2 * a.split.group));
     return ok ? SHARPV_OK : SHARPV_ERR_CUDA;
 }
 

@@ -1,10 +1,11 @@
 // Attention of many query rows over a K/V cache in bf16 (drafted trees, chunks of a prompt) on the fifth-generation
 // tensor cores.
 //
-// A segment is up to 256 query rows of one (sequence, KV head), as two tiles of 128; a unit is 128 keys of it.  One
+// A segment is up to 256 query rows of one (sequence, KV head), as two tiles of up to 128 (as many whole nodes as
+// fit, so that one TMA box fetches them); a unit is 128 keys of it.  One
 // CTA per SM: a warp that loads (TMA ring of K and V tiles, 32 KB each at head_dim 128), a warp that issues
-// the products, two warpgroups that turn scores into weights, two warps that fetch query rows and clean the value tiles
-// that hold rows nobody may see.  Work goes in steps, each one stream's scores, weights and weighted sums:
+// the products, two warpgroups that turn scores into weights, two warps that clean the value tiles that hold rows
+// nobody may see.  Work goes in steps, each one stream's scores, weights and weighted sums:
 //   more than 128 rows   stream w owns row tile w; both take every key tile
 //   up to 128 rows       both streams own row tile 0 and take the key tiles in turn; joined in tensor memory at the end
 // While one stream's warpgroup works on its scores the tensor cores work for the other.  Scores, weights (bf16, in the
@@ -20,7 +21,7 @@ namespace sharpv {
 namespace {
 
 constexpr int kKeys = kTcTileKeys;              // 128
-constexpr int kRows = kTcTileRows;              // 256
+constexpr int kRows = 256;                      // places for query rows: 128 a stream
 constexpr int kThreads = 384;
 constexpr int kLoadWarp = 8, kMmaWarp = 9, kAuxWarp = 10;       // warps 0-3, 4-7: the streams; 10, 11: aux
 constexpr uint32_t kCols = 512, kSumCol = 256;  // tensor memory: scores of stream w at 128 w, sums at 256 + DP w
@@ -45,7 +46,7 @@ struct Shared {
     uint64_t part_full[2], part_empty[2];
     uint64_t clean[C::kStages];                 // value tiles: gone through (or nothing to do)
     uint64_t q_full, q_empty;
-    uint64_t scores[2], weights[2], sums[2];    // per stream: products done, weights written, weighted sums added
+    uint64_t scores[2], weights[2][2], sums[2]; // per stream: products done, each half of the weights written, weighted sums added
     uint64_t merge_full, merge_done, drain;
     int poison[2];
     uint32_t tmem;
@@ -56,9 +57,9 @@ struct Shared {
 struct Steps {
     int tiles, n;               // key tiles, steps
     bool pair;                  // two row tiles
-    __device__ __forceinline__ Steps(const Portion& p, int group) {
+    __device__ __forceinline__ Steps(const Portion& p, const Split& sp) {
         tiles = p.kt1 - p.kt0;
-        pair = p.s.nodes * group - p.rt * kRows > 128;
+        pair = p.s.nodes * sp.group - p.rt * sp.rows > sp.rows / 2;
         n = pair ? 2 * tiles : tiles;
     }
     __device__ __forceinline__ int tile(int step) const { return pair ? step >> 1 : step; }
@@ -95,6 +96,12 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnMaps maps) {
@@ -113,10 +120,11 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
             mbar_init(&sm.part_full[i], 1);
             mbar_init(&sm.part_empty[i], 11);           // the warps that read it
             mbar_init(&sm.scores[i], 1);
-            mbar_init(&sm.weights[i], 128);
+            mbar_init(&sm.weights[i][0], 4);
+            mbar_init(&sm.weights[i][1], 4);
             mbar_init(&sm.sums[i], 1);
         }
-        mbar_init(&sm.q_full, 64);
+        mbar_init(&sm.q_full, 1);
         mbar_init(&sm.q_empty, 1);
         mbar_init(&sm.merge_full, 128);
         mbar_init(&sm.merge_done, 128);
@@ -124,7 +132,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
         mbar_fence_init();
     }
     if (warp == kMmaWarp) tmem_alloc(&sm.tmem, kCols);
-    if (warp == kLoadWarp && lane < 4) tma_prefetch(&maps.cache_k + lane);
+    if (warp == kLoadWarp && lane < 5) tma_prefetch(&maps.cache_k + lane);
     cudaGridDependencySynchronize();
     int64_t first, end;
     const PlanStart plan = plan_cta<kThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
@@ -157,6 +165,15 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                     sm.next_unit[at] = walk.u;
                     mbar_arrive(&sm.part_full[at]);
                     if (!more) break;
+                    // query rows: whole nodes, the group's heads of each next to each other
+                    const Steps st(p, a.split);
+                    if (pn > 0 && !wait(&sm.q_empty, pn - 1)) break;
+                    const int nodes = a.split.rows / (2 * G);
+                    mbar_expect(&sm.q_full, (st.pair ? 2 : 1) * (DP / 64) * (a.split.rows / 2) * 128);
+                    for (int w = 0; w < (st.pair ? 2 : 1); ++w)
+#pragma unroll
+                        for (int x = 0; x < DP / 64; ++x)
+                            tma_load(sm.q[w] + x * C::kHalf, &maps.query, &sm.q_full, x * 64, p.h * G, p.s.node0 + (p.rt * 2 + w) * nodes);
                     for (int kt = p.kt0; kt < p.kt1 && alive; ++kt) {
                         const bool drafted = kt >= p.kt_cache;
                         const int row = drafted ? p.s.node0 + (kt - p.kt_cache) * kKeys : (int)p.s.begin + kt * kKeys;
@@ -190,7 +207,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                     if (!wait(&sm.part_full[pn & 1], pn >> 1)) break;
                     const Portion p = sm.part[pn & 1];
                     if (p.kt1 < 0) break;
-                    const Steps st(p, G);
+                    const Steps st(p, a.split);
                     if (!wait(&sm.q_full, pn)) break;
                     auto scores = [&](int t) {                  // scores of step t
                         const int j = st.tile(t), w = t & 1;
@@ -218,13 +235,16 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                             if (!wait(&sm.clean[item % C::kStages], clean_phase<C::kStages>(item)) ||
                                 !wait(&sm.full[item % C::kStages], item / C::kStages)) break;
                         }
-                        if (!wait(&sm.weights[w], steps0[w] + mine)) break;
-                        tc_fence_after();
                         const uint32_t vb = smem_u32(sm.tiles[item % C::kStages]);
+                        for (int half = 0; half < 2; ++half) {          // the first half while the second is being weighed
+                            if (!wait(&sm.weights[w][half], steps0[w] + mine)) break;
+                            tc_fence_after();
 #pragma unroll
-                        for (int kk = 0; kk < kKeys / 16; ++kk)
-                            mma_ts(tmem + kSumCol + w * DP, tmem + w * 128 + kk * 8, smem_operand(vb + kk * 2048, 1024, C::kHalf), v_shape,
-                                   mine > 0 || kk > 0);
+                            for (int kk = 0; kk < kKeys / 32; ++kk)
+                                mma_ts(tmem + kSumCol + w * DP, tmem + w * 128 + half * 32 + kk * 8,
+                                       smem_operand(vb + (half * 4 + kk) * 2048, 1024, C::kHalf), v_shape, mine > 0 || half > 0 || kk > 0);
+                        }
+                        if (!alive) break;
                         mma_commit(&sm.sums[w]);
                         if (!st.pair || w == 1) mma_commit(&sm.empty[item % C::kStages]);
                         if (t + 2 < st.n) scores(t + 2);
@@ -239,34 +259,20 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                 (void)mbar_wait(&sm.drain, 0);
             }
         } else {
-            // query rows, and value tiles with rows that are not there (or, drafted, that some query rows must not see):
-            // 0 times what such rows hold would not be 0 if that is not finite
+            // value tiles with rows that are not there (or, drafted, that some query rows must not see): 0 times what such
+            // rows hold would not be 0 if that is not finite
             const int t64 = threadIdx.x - kAuxWarp * 32;
             uint32_t it0 = 0;
             for (uint32_t pn = 0;; ++pn) {
                 if (!wait_warp(&sm.part_full[pn & 1], pn >> 1)) break;
                 const Portion p = sm.part[pn & 1];
                 if (p.kt1 < 0) break;
-                const Steps st(p, G);
-                if (pn > 0 && !wait_warp(&sm.q_empty, pn - 1)) break;
-                const int r_base = p.rt * kRows, rows = min(p.s.nodes * G - r_base, st.pair ? 256 : 128);
                 constexpr int CH = DP / 8;
-                for (int x = t64; x < (st.pair ? 256 : 128) * CH; x += 64) {
-                    const int r = x / CH, c = x % CH;
-                    const bool there = r < rows && c * 8 < D;
-                    const char* q = a.q;
-                    if (there) {
-                        const int row = r_base + r;
-                        q += (int64_t)(p.s.node0 + row / G) * a.q_node + ((int64_t)(p.h * G + row % G) * D + c * 8) * 2;
-                    }
-                    cp_async16(sm.q[r >> 7] + (c >> 3) * C::kHalf + swizzle128(r & 127, c & 7), q, there);
-                }
-                cp_async_wait_all();
-                async_proxy_fence();
-                mbar_arrive(&sm.q_full);
                 for (int kt = p.kt0; kt < p.kt1; ++kt) {
-                    const uint32_t item = it0 + 2 * (kt - p.kt0) + 1;
-                    if (!wait_warp(&sm.full[item % C::kStages], item / C::kStages)) break;
+                    const uint32_t item = it0 + 2 * (kt - p.kt0) + 1, key_item = item - 1;
+                    // the key tile's arrival as well: a phase that is waited for has to be the next one of its barrier
+                    if (!wait_warp(&sm.full[key_item % C::kStages], key_item / C::kStages) ||
+                        !wait_warp(&sm.full[item % C::kStages], item / C::kStages)) break;
                     if (tile_masked(a, p, kt)) {
                         uint8_t* tile = sm.tiles[item % C::kStages];
                         const int left = keys_left(a, p, kt);
@@ -293,7 +299,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                     if (lane == 0) mbar_arrive(&sm.clean[item % C::kStages]);
                 }
                 if (!alive) break;
-                it0 += 2 * st.tiles;
+                it0 += 2 * (p.kt1 - p.kt0);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm.part_empty[pn & 1]);
             }
@@ -310,10 +316,12 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
             if (!wait_warp(&sm.part_full[pn & 1], pn >> 1)) break;
             const Portion p = sm.part[pn & 1];
             if (p.kt1 < 0) break;
-            const Steps st(p, G);
-            const int r_all = p.s.nodes * G, r_warp = p.rt * kRows + (st.pair ? w * 128 : 0) + (warp & 3) * 32;
-            const int row = r_warp + lane;
-            const bool work = r_warp < r_all;                       // some row of the warp is there
+            const Steps st(p, a.split);
+            const int tile_rows = a.split.rows / 2;
+            const int r_tile = p.rt * a.split.rows + (st.pair ? w * tile_rows : 0);
+            const int row = r_tile + r_in;
+            const int r_all = r_in < tile_rows ? p.s.nodes * G : 0;                     // the thread has a row if row < r_all
+            const bool work = (warp & 3) * 32 < min(tile_rows, p.s.nodes * G - r_tile);     // some thread of the warp has one
             const int mine = st.of_stream(w);
             float m2 = neg_inf(), l = 0.f;                          // maximum in log 2 units, as used; sum
             for (int x = 0; x < mine; ++x) {
@@ -346,7 +354,8 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                     for (int i = 0; i < 4; ++i) {
                         top4[i] = __uint_as_float(s[i][0]);
 #pragma unroll
-                        for (int k = 1; k < 32; ++k) top4[i] = fmaxf(top4[i], __uint_as_float(s[i][k]));
+                        for (int k = 1; k < 31; k += 2) top4[i] = max3(top4[i], __uint_as_float(s[i][k]), __uint_as_float(s[i][k + 1]));
+                        top4[i] = fmaxf(top4[i], __uint_as_float(s[i][31]));
                     }
                     const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * a.scale_log2;
                     const bool grows = top > m2 + kLazy;
@@ -387,14 +396,23 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                             pk[k] = pack_bf16(y0, y1);
                         }
                         tmem_st16(t_scores + i * 16, pk);
+                        if (i & 1) {
+                            tmem_wait_st();
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&sm.weights[w][i >> 1]);
+                        }
                     }
                     float s0, s1;
                     unpack2(add2(sum2[0], sum2[1]), s0, s1);
                     l += s0 + s1;
-                    tmem_wait_st();
-                    tc_fence_before();
+                } else {
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(&sm.weights[w][0]);
+                        mbar_arrive(&sm.weights[w][1]);
+                    }
                 }
-                mbar_arrive(&sm.weights[w]);
             }
             if (!alive) break;
             // ---- the portion's result
@@ -423,7 +441,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                 const bool both = !st.pair && st.of_stream(1) > 0;
                 const bool complete = p.kt0 == 0 && p.kt1 == p.kt_all;
                 const int slot = portion_slot(blockIdx.x, p.kt0);
-                const int r = row - p.rt * kRows;
+                const int r = (st.pair ? w * 128 : 0) + r_in;
                 const float inv = row_scale(l);
                 const int64_t at = (int64_t)(p.s.node0 + row / G) * HQ + p.h * G + row % G;
                 const bool poison = sm.poison[pn & 1] != 0;
@@ -516,8 +534,8 @@ attn_tc_join_kernel(const __grid_constant__ AttnArgs a) {
     const int r = blockIdx.y * 32 + lane, c4 = blockIdx.z * 8 + warp;
     cudaGridDependencySynchronize();
     const SharedSegment seg = a.shared[c0];
-    const int row = seg.rt * kRows + r;
-    if (seg.last < 0 || row >= seg.rows || c4 * 4 >= D) return;
+    const int tile_rows = a.split.rows / 2, row = seg.rt * a.split.rows + (r >> 7) * tile_rows + (r & 127);
+    if (seg.last < 0 || (r & 127) >= tile_rows || row >= seg.rows || c4 * 4 >= D) return;
     const int c1 = seg.last;
     float top = neg_inf();
 #pragma unroll 8
@@ -569,7 +587,7 @@ sharpv_status launch(const AttnArgs& a, cudaStream_t stream) {
     const sharpv_status ms = encode_attn_maps(a, kKeys, maps);
     if (ms != SHARPV_OK) return ms;
     const int64_t all = a.seqs.total_nodes * a.split.group;
-    const unsigned rows = (unsigned)(all < kRows ? all : kRows);
+    const unsigned rows = (unsigned)(all <= a.split.rows / 2 ? all : kRows);        // places that any segment can use
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
         launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kThreads), smem, stream, a, maps) != cudaSuccess ||
         launch_dependent(attn_tc_join_kernel, dim3((unsigned)a.ctas, (rows + 31) / 32, (unsigned)(a.head_dim + 31) / 32), dim3(256), 0,
