@@ -23,7 +23,7 @@ constexpr int kRowsMax = 512;           // query rows of a head in a pass
 template <int DP>
 struct Cfg {
     static constexpr int kTileBytes = kKeys * DP * 2;
-    static constexpr int kStages = kRingBytes / kTileBytes;
+    static constexpr int kStages = kRingBytes / kTileBytes / kPairs;        // of a pair's own ring
     static constexpr int kPitch = DP * 2 + 16;              // of a query row: 8 rows fall on 8 bank groups
 };
 
@@ -35,8 +35,8 @@ struct Pass {
 template <int DP>
 struct Shared {
     using C = Cfg<DP>;
-    uint8_t tiles[C::kStages][C::kTileBytes];
-    uint64_t full[C::kStages], empty[C::kStages];
+    uint8_t tiles[kPairs][C::kStages][C::kTileBytes];       // every pair waits for every use of its stages, in order
+    uint64_t full[kPairs][C::kStages], empty[kPairs][C::kStages];
     int list[kRowsMax + 1];                                 // nodes of a pass that count
     int64_t row_at[kRowsMax];                               // byte offset of a query row (of head 0 of its group), -1: none
     int scan[kWarps];
@@ -88,9 +88,9 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
     const int D = a.head_dim, G = a.split.group, H = a.split.heads, HQ = H * G;
     const KeySplit split{kKeys};
     if (threadIdx.x == 0) {
-        for (int i = 0; i < C::kStages; ++i) {
-            mbar_init(&sm.full[i], 1);
-            mbar_init(&sm.empty[i], 2);
+        for (int i = 0; i < kPairs * C::kStages; ++i) {
+            mbar_init(&sm.full[0][i], 1);
+            mbar_init(&sm.empty[0][i], 2);
         }
         mbar_fence_init();
         sm.dead = sm.unseen = 0;
@@ -101,10 +101,10 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
     const PlanStart plan = plan_cta<kThreads>(a.seqs, split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
     KeyWalk walk(plan, first, end);
     const int head_passes = (H + ps.heads - 1) / ps.heads;
-    uint32_t it = 0;
     bool alive = true;
 
     if (warp == kWarps) {
+        uint32_t it[kPairs] = {};                       // tiles of every pair so far
         while (walk.next(a.seqs, split)) {
             // how often the portion is gone through: by the number of nodes that count
             int active = 0;
@@ -122,15 +122,18 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
                         for (int kt = walk.kt0; kt < walk.kt1; kt += kPairs) {
                             const int n = min(kPairs, walk.kt1 - kt);
                             for (int h = h0; h < h1; ++h)
-                                for (int t = 0; t < n && alive; ++t, ++it) {
-                                    const int stage = it % C::kStages;
-                                    if (it >= C::kStages) alive = mbar_wait(&sm.empty[stage], (it / C::kStages - 1) & 1);
+#pragma unroll
+                                for (int t = 0; t < kPairs; ++t) {
+                                    if (t >= n || !alive) break;
+                                    const int stage = it[t] % C::kStages;
+                                    if (it[t] >= C::kStages) alive = mbar_wait(&sm.empty[t][stage], (it[t] / C::kStages - 1) & 1);
                                     if (!alive) break;
-                                    mbar_expect(&sm.full[stage], C::kTileBytes);
+                                    mbar_expect(&sm.full[t][stage], C::kTileBytes);
 #pragma unroll
                                     for (int x = 0; x < DP / 64; ++x)
-                                        tma_load(sm.tiles[stage] + x * kKeys * 128, &map, &sm.full[stage], x * 64,
+                                        tma_load(sm.tiles[t][stage] + x * kKeys * 128, &map, &sm.full[t][stage], x * 64,
                                                  (int)walk.s.begin + (kt + t) * kKeys, h);
+                                    ++it[t];
                                 }
                         }
                     }
@@ -140,16 +143,20 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
         }
         if (!alive && lane == 0) {
             report(a.status_word, SHARPV_ERR_TIMEOUT);
-            for (uint32_t i = 0; i < (uint32_t)C::kStages && i < it; ++i) {         // copies in flight land before the CTA ends
-                const uint32_t last = it - 1 - i;
-                (void)mbar_wait(&sm.full[last % C::kStages], (last / C::kStages) & 1);
-            }
+            // copies in flight land before the CTA ends
+#pragma unroll
+            for (int t = 0; t < kPairs; ++t)
+                for (uint32_t i = 0; i < (uint32_t)C::kStages && i < it[t]; ++i) {
+                    const uint32_t last = it[t] - 1 - i;
+                    (void)mbar_wait(&sm.full[t][last % C::kStages], (last / C::kStages) & 1);
+                }
         }
         return;
     }
 
     const int pair = warp >> 1, sub = warp & 1;
     const int tid = threadIdx.x;
+    uint32_t it = 0;                            // the pair's tiles so far
     float* const lse2 = reinterpret_cast<float*>(sm.query + (size_t)ps.heads * ps.rows * C::kPitch);
     float* const weight = lse2 + ps.heads * ps.rows;
     while (walk.next(a.seqs, split)) {
@@ -238,12 +245,9 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
                 const bool fresh = rp == 0 && hp == 0;
                 for (int kt = walk.kt0; kt < walk.kt1; kt += kPairs) {
                     const int n = min(kPairs, walk.kt1 - kt);
-                    if (rows > 0 && pair >= n) {
-                        it += hn * n;
-                        continue;
-                    }
+                    if (pair >= n) continue;
                     const int key = p0 + (kt - walk.kt0 + pair) * kKeys;            // of the sequence
-                    const bool writes = pair < n && (lane & 3) < 2;                 // lane 0 of four: key, lane 1: key + 8
+                    const bool writes = (lane & 3) < 2;                             // lane 0 of four: key, lane 1: key + 8
                     const int my_key = key + (lane & 3) * 8;
                     float old = 0.f;
                     if (writes && my_key < s.len) {
@@ -252,21 +256,20 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
                     }
                     float sum0 = 0.f, sum1 = 0.f;
                     if (rows > 0) {
-                        for (int h = 0; h < hn; ++h) {
-                            const uint32_t item = it + h * n + pair;
-                            const int stage = item % C::kStages;
-                            if (alive && !mbar_wait(&sm.full[stage], (item / C::kStages) & 1)) {
+                        for (int h = 0; h < hn; ++h, ++it) {
+                            const int stage = it % C::kStages;
+                            if (alive && !mbar_wait(&sm.full[pair][stage], (it / C::kStages) & 1)) {
                                 alive = false;
                                 sm.dead = 1;
                                 report(a.status_word, SHARPV_ERR_TIMEOUT);
                             }
-                            const uint32_t kb = smem_u32(sm.tiles[stage]);
+                            const uint32_t kb = smem_u32(sm.tiles[pair][stage]);
                             uint32_t kf[DP / 16][4];
 #pragma unroll
                             for (int ks = 0; ks < DP / 16; ++ks)
                                 ldmatrix4(kf[ks], kb + (ks >> 2) * (kKeys * 128) + swizzle128(sub * 16 + (lane & 15), (ks & 3) * 2 + (lane >> 4)));
                             __syncwarp();
-                            if (lane == 0) mbar_arrive(&sm.empty[stage]);
+                            if (lane == 0) mbar_arrive(&sm.empty[pair][stage]);
                             const uint32_t qb = smem_u32(sm.query) + (uint32_t)(h * ps.rows + (lane & 7)) * C::kPitch + (lane >> 3) * 16;
                             const float* hl = lse2 + h * ps.rows + (lane & 3) * 2;
                             const float* hw = weight + (lane & 3) * 2;
@@ -279,7 +282,6 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
                             }
                             if (nb < blocks) weigh<1, DP>(kf, qb, hl, hw, nb, a.scale_log2, sum0, sum1);
                         }
-                        it += hn * n;
                     }
                     sum0 += __shfl_xor_sync(0xffffffffu, sum0, 1);
                     sum0 += __shfl_xor_sync(0xffffffffu, sum0, 2);

@@ -46,7 +46,7 @@ struct Shared {
     uint64_t part_full[2], part_empty[2];
     uint64_t clean[C::kStages];                 // value tiles: gone through (or nothing to do)
     uint64_t q_full, q_empty;
-    uint64_t scores[2], weights[2][2], sums[2]; // per stream: products done, each half of the weights written, weighted sums added
+    uint64_t scores[2], weights[2][2], sums[2]; // per stream: products done, each half of the weights written, a portion's weighted sums added
     uint64_t merge_full, merge_done, drain;
     int poison[2];
     uint32_t tmem;
@@ -62,13 +62,25 @@ struct Steps {
         pair = p.s.nodes * sp.group - p.rt * sp.rows > sp.rows / 2;
         n = pair ? 2 * tiles : tiles;
     }
-    __device__ __forceinline__ int tile(int step) const { return pair ? step >> 1 : step; }
     __device__ __forceinline__ int of_stream(int w) const { return pair ? tiles : (tiles + 1 - w) >> 1; }
 };
 
-// Value tiles are the odd items of the ring; with an odd number of stages a stage holds one every other time.
+// Every second item of the ring (key tiles are the even ones, value tiles the odd ones): its stage, and how often the
+// ring has gone round.
 template <int STAGES>
-__device__ __forceinline__ uint32_t clean_phase(uint32_t item) { return STAGES % 2 ? item / STAGES >> 1 : item / STAGES; }
+struct Ring {
+    int stage;
+    uint32_t round;
+    __device__ __forceinline__ void next() {
+        stage += 2;
+        if (stage >= STAGES) {
+            stage -= STAGES;
+            ++round;
+        }
+    }
+    // uses of the stage for a tile of the same kind so far: with an odd number of stages every other round is one
+    __device__ __forceinline__ uint32_t use() const { return STAGES % 2 ? round >> 1 : round; }
+};
 
 // keys of tile kt that are there, and whether it has to be masked
 __device__ __forceinline__ int keys_left(const AttnArgs& a, const Portion& p, int kt) {
@@ -200,64 +212,82 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                 }
             }
         } else if (warp == kMmaWarp) {
-            if (lane == 0) {
-                uint32_t it0 = 0, steps0[2] = {0, 0};           // tiles and steps of the portions before
-                const uint32_t k_shape = mma_shape(128, false), v_shape = mma_shape(DP, true);
-                for (uint32_t pn = 0;; ++pn) {
-                    if (!wait(&sm.part_full[pn & 1], pn >> 1)) break;
-                    const Portion p = sm.part[pn & 1];
-                    if (p.kt1 < 0) break;
-                    const Steps st(p, a.split);
-                    if (!wait(&sm.q_full, pn)) break;
-                    auto scores = [&](int t) {                  // scores of step t
-                        const int j = st.tile(t), w = t & 1;
-                        const uint32_t item = it0 + 2 * j;
-                        if (!st.pair || w == 0) {
-                            if (!wait(&sm.full[item % C::kStages], item / C::kStages)) return;
-                        }
-                        tc_fence_after();
-                        const uint32_t qb = smem_u32(sm.q[st.pair ? w : 0]), kb = smem_u32(sm.tiles[item % C::kStages]);
+            // The whole warp walks and waits, one thread issues.  The tensor cores queue only a few products, so what
+            // happens between two batches is kept short: one wait that is mostly over, one commit.
+            constexpr uint32_t k_shape = mma_shape(128, false), v_shape = mma_shape(DP, true);
+            const uint64_t q_op = smem_operand(smem_u32(sm.q[0]), 1024, 16), k_op = smem_operand(smem_u32(sm.tiles[0]), 1024, 16);
+            const uint64_t v_op = smem_operand(smem_u32(sm.tiles[0]), 1024, C::kHalf);
+            Ring<C::kStages> kr{0, 0}, vr{1, 0};                        // where the next key and value tile to wait for are
+            uint32_t steps0[2] = {0, 0};                                // steps of the portions before
+            for (uint32_t pn = 0;; ++pn) {
+                if (!wait_warp(&sm.part_full[pn & 1], pn >> 1)) break;
+                const Portion& p = sm.part[pn & 1];
+                if (p.kt1 < 0) break;
+                const Steps st(p, a.split);
+                const bool pair = __shfl_sync(0xffffffffu, (int)st.pair, 0) != 0;
+                const int n = __shfl_sync(0xffffffffu, st.n, 0);
+                if (!wait_warp(&sm.q_full, pn)) break;
+                auto scores = [&](int t) {                              // scores of step t
+                    const int w = t & 1;
+                    if (!pair || w == 0) {
+                        if (!wait_warp(&sm.full[kr.stage], kr.round)) return;
+                    }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t q = q_op + (pair ? w : 0) * (C::kTileBytes >> 4), k = k_op + kr.stage * (C::kTileBytes >> 4);
 #pragma unroll
                         for (int ks = 0; ks < DP / 16; ++ks) {
-                            const uint32_t off = (ks >> 2) * C::kHalf + (ks & 3) * 32;
-                            mma_ss(tmem + w * 128, smem_operand(qb + off, 1024, 16), smem_operand(kb + off, 1024, 16), k_shape, ks > 0);
+                            const uint32_t off = ((ks >> 2) * C::kHalf + (ks & 3) * 32) >> 4;
+                            mma_ss(tmem + w * 128, q + off, k + off, k_shape, ks > 0);
                         }
                         mma_commit(&sm.scores[w]);
-                        if (!st.pair || w == 1) mma_commit(&sm.empty[item % C::kStages]);
-                        if (t == st.n - 1) mma_commit(&sm.q_empty);
-                    };
-                    scores(0);
-                    if (st.n > 1 && alive) scores(1);
-                    for (int t = 0; t < st.n && alive; ++t) {
-                        const int j = st.tile(t), w = t & 1;
-                        const uint32_t item = it0 + 2 * j + 1, mine = t >> 1;
-                        if (!st.pair || w == 0) {
-                            if (!wait(&sm.clean[item % C::kStages], clean_phase<C::kStages>(item)) ||
-                                !wait(&sm.full[item % C::kStages], item / C::kStages)) break;
-                        }
-                        const uint32_t vb = smem_u32(sm.tiles[item % C::kStages]);
-                        for (int half = 0; half < 2; ++half) {          // the first half while the second is being weighed
-                            if (!wait(&sm.weights[w][half], steps0[w] + mine)) break;
-                            tc_fence_after();
+                        if (!pair || w == 1) mma_commit(&sm.empty[kr.stage]);
+                        if (t == n - 1) mma_commit(&sm.q_empty);
+                    }
+                    __syncwarp();
+                    if (!pair || w == 1) kr.next();
+                };
+                scores(0);
+                if (n > 1 && alive) scores(1);
+                for (int t = 0; t < n && alive; ++t) {
+                    const int w = t & 1, mine = t >> 1;
+                    if (!pair || w == 0) {
+                        if (!wait_warp(&sm.clean[vr.stage], vr.use())) break;
+                    }
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {              // the first half while the second is being weighed
+                        if (!wait_warp(&sm.weights[w][half], steps0[w] + mine)) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint64_t v = v_op + vr.stage * (C::kTileBytes >> 4) + half * (kKeys / 2 * 128 >> 4);
 #pragma unroll
                             for (int kk = 0; kk < kKeys / 32; ++kk)
-                                mma_ts(tmem + kSumCol + w * DP, tmem + w * 128 + half * 32 + kk * 8,
-                                       smem_operand(vb + (half * 4 + kk) * 2048, 1024, C::kHalf), v_shape, mine > 0 || half > 0 || kk > 0);
+                                mma_ts(tmem + kSumCol + w * DP, tmem + w * 128 + half * 32 + kk * 8, v + kk * (16 * 128 >> 4), v_shape,
+                                       mine > 0 || half > 0 || kk > 0);
+                            // a step's scores say that the weighted sums of the step before are in; of the last step this does
+                            if (half == 1 && t + 2 >= n) mma_commit(&sm.sums[w]);
                         }
-                        if (!alive) break;
-                        mma_commit(&sm.sums[w]);
-                        if (!st.pair || w == 1) mma_commit(&sm.empty[item % C::kStages]);
-                        if (t + 2 < st.n) scores(t + 2);
+                        __syncwarp();
                     }
                     if (!alive) break;
-                    it0 += 2 * st.tiles;
-                    steps0[0] += st.of_stream(0);
-                    steps0[1] += st.of_stream(1);
-                    mbar_arrive(&sm.part_empty[pn & 1]);
+                    const int v_stage = vr.stage;
+                    const bool v_done = !pair || w == 1;
+                    if (v_done) vr.next();
+                    if (t + 2 < n) scores(t + 2);
+                    if (v_done && elect_one()) mma_commit(&sm.empty[v_stage]);
+                    __syncwarp();
                 }
-                mma_commit(&sm.drain);              // the products in flight end before the tensor memory is given back
-                (void)mbar_wait(&sm.drain, 0);
+                if (!alive) break;
+                steps0[0] += st.of_stream(0);
+                steps0[1] += st.of_stream(1);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.part_empty[pn & 1]);
             }
+            // the products in flight end before the tensor memory is given back
+            __syncwarp();
+            if (elect_one()) mma_commit(&sm.drain);
+            __syncwarp();
+            (void)mbar_wait(&sm.drain, 0);
         } else {
             // value tiles with rows that are not there (or, drafted, that some query rows must not see): 0 times what such
             // rows hold would not be 0 if that is not finite
@@ -310,7 +340,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
         const uint32_t lanes = (uint32_t)(warp & 3) * 32 << 16;
         const uint32_t t_scores = tmem + lanes + w * 128, t_sums = tmem + lanes + kSumCol + w * DP;
         const uint64_t c2 = pack2(a.scale_log2, a.scale_log2);
-        uint32_t steps = 0, merges = 0;
+        uint32_t steps = 0, merges = 0, summed = 0;
         SharedSegment shared = {0, 0, 0, 0, -1};
         for (uint32_t pn = 0;; ++pn) {
             if (!wait_warp(&sm.part_full[pn & 1], pn >> 1)) break;
@@ -364,9 +394,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                         const float al = grows ? ex2(m2 - next) : 1.f;      // 0 where nothing was seen yet
                         m2 = next;
                         l *= al;
-                        if (x > 0) {
-                            if (!wait_warp(&sm.sums[w], steps + x - 1)) break;
-                            tc_fence_after();
+                        if (x > 0) {            // the sums of step x - 1 are in: its products came before this step's scores
 #pragma unroll 1
                             for (int c = 0; c < DP; c += 32) {
                                 uint32_t o[32];
@@ -416,7 +444,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
             }
             if (!alive) break;
             // ---- the portion's result
-            if (mine > 0 && !wait_warp(&sm.sums[w], steps + mine - 1)) break;
+            if (mine > 0 && !wait_warp(&sm.sums[w], summed++)) break;
             tc_fence_after();
             steps += mine;
             float f0 = 1.f, f1 = 0.f;
