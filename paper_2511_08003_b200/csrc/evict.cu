@@ -3,7 +3,10 @@
 // A sequence's k-th key is found by counting, eight bits at a time from the top (the key is the monotone 32-bit
 // image of the mass), by a cluster of CTAs that share the sequence's rows in contiguous slices: every CTA counts
 // its slice in shared memory, and all read one another's counts.  The rows above the k-th key stay, and of those equal
-// to it the first ones; the slices' counts give every CTA the place where its survivors go.
+// to it the first ones; the warps' and slices' counts give every warp the place where its survivors go.
+// What bounds it is latency (four rounds of counting with two barriers of the cluster each): the keys are read from
+// memory once and kept in shared memory (slices too long for that are read again every round), and lanes of a warp
+// that count the same digit (weights span few powers of two) count it with one atomic.
 #include <cooperative_groups.h>
 
 #include "decode_common.cuh"
@@ -14,6 +17,7 @@ namespace {
 constexpr int kEvictThreads = 512;
 constexpr int kEvictCluster = 8;
 constexpr int kBins = 256;
+constexpr int kKeyRoom = 24 * 1024;     // keys of a slice in shared memory: 96 KB, two CTAs on an SM
 
 struct EvictArgs {
     const float* mass;
@@ -27,6 +31,7 @@ struct EvictArgs {
     int32_t* kept_offsets;
     float* out_mass;
     int64_t capacity;
+    int key_room;               // keys of a slice that shared memory holds
     int32_t* status_word;
 };
 
@@ -49,10 +54,12 @@ __global__ void __cluster_dims__(kEvictCluster, 1, 1) __launch_bounds__(kEvictTh
 evict_select_kernel(const __grid_constant__ EvictArgs a) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
+    extern __shared__ uint32_t keys[];
+    constexpr int kWarps = kEvictThreads / 32;
     __shared__ int hist[2][kBins];
     __shared__ int total[kBins];
     __shared__ int counts[2];                   // rows of the slice above the k-th key, and equal to it
-    __shared__ int scan[kEvictThreads / 32 + 1];
+    __shared__ int warp_up[kWarps], warp_eq[kWarps];
     __shared__ int64_t base_part[kEvictThreads / 32];
     __shared__ int pick[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -98,16 +105,26 @@ evict_select_kernel(const __grid_constant__ EvictArgs a) {
     // contiguous slice of this CTA
     const int lo = (int)((int64_t)len * rank / kEvictCluster), hi = (int)((int64_t)len * (rank + 1) / kEvictCluster);
     const float* mass = a.mass + begin;
+    const bool kept_here = hi - lo <= a.key_room;
+    if (kept_here) {
+#pragma unroll 4
+        for (int i = lo + tid; i < hi; i += kEvictThreads) keys[i - lo] = mass_key(__ldg(mass + i));
+        __syncthreads();
+    }
+    auto key_of = [&](int i) { return kept_here ? keys[i - lo] : mass_key(__ldg(mass + i)); };
     uint32_t prefix = 0, need = (uint32_t)want;                      // the k-th key's known bits; rank among those that share them
     if (choose) {                                                    // the same in every CTA of the cluster
 #pragma unroll 1
         for (int pass = 0; pass < 4; ++pass) {
             const int shift = 24 - 8 * pass;
             int* h = hist[pass & 1];
-            for (int i = lo + tid; i < hi; i += kEvictThreads) {
-                const bool in = (i < s_end || i >= r_begin) == among_guarded;
-                const uint32_t key = mass_key(__ldg(mass + i));
-                if (in && (pass == 0 || key >> (shift + 8) == prefix)) atomicAdd(&h[(key >> shift) & 255], 1);
+            for (int i0 = lo; i0 < hi; i0 += kEvictThreads) {
+                const int i = i0 + tid;
+                const uint32_t key = i < hi ? key_of(i) : 0u;
+                const bool in = i < hi && (i < s_end || i >= r_begin) == among_guarded && (pass == 0 || key >> (shift + 8) == prefix);
+                const int digit = in ? (int)(key >> shift & 255) : kBins;
+                const uint32_t same = __match_any_sync(0xffffffffu, digit);
+                if (in && lane == __ffs(same) - 1) atomicAdd(&h[digit], __popc(same));
             }
             cluster.sync();
             if (tid < kBins) {
@@ -148,42 +165,51 @@ evict_select_kernel(const __grid_constant__ EvictArgs a) {
         const bool guard = i < s_end || i >= r_begin;
         if (guard != among_guarded) return guard ? 2 : 0;
         if (!choose) return want > 0 ? 2 : 0;
-        const uint32_t key = mass_key(__ldg(mass + i));
+        const uint32_t key = key_of(i);
         return key > prefix ? 2 : (key == prefix ? 1 : 0);
     };
-    int above = 0, equal = 0;
-    for (int i = lo + tid; i < hi; i += kEvictThreads) {
-        const int st = state(i);
-        above += st == 2;
-        equal += st == 1;
+    // contiguous piece of this warp, counted first, written then
+    const int n = hi - lo;
+    const int w_lo = lo + (int)((int64_t)n * warp / kWarps), w_hi = lo + (int)((int64_t)n * (warp + 1) / kWarps);
+    int up = 0, eq = 0;
+    for (int x = w_lo; x < w_hi; x += 32) {
+        const int st = x + lane < w_hi ? state(x + lane) : 0;
+        up += __popc(__ballot_sync(0xffffffffu, st == 2));
+        eq += __popc(__ballot_sync(0xffffffffu, st == 1));
     }
-    if (tid < 2) counts[tid] = 0;
+    if (lane == 0) { warp_up[warp] = up; warp_eq[warp] = eq; }
     __syncthreads();
-    above = warp_sum_int(above);
-    equal = warp_sum_int(equal);
-    if (lane == 0) { atomicAdd(&counts[0], above); atomicAdd(&counts[1], equal); }     // integers: order does not matter
+    int up_before = 0, eq_before = 0, up_all = 0, eq_all = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) { up_before += warp_up[w]; eq_before += warp_eq[w]; }
+        up_all += warp_up[w];
+        eq_all += warp_eq[w];
+    }
+    if (tid == 0) { counts[0] = up_all; counts[1] = eq_all; }
     cluster.sync();
-    int eq_before = 0, up_before = 0;
-    for (int r = 0; r < rank; ++r) {
+#pragma unroll
+    for (int r = 0; r < kEvictCluster; ++r) {
         const int* c = cluster.map_shared_rank(counts, r);
-        up_before += c[0];
-        eq_before += c[1];
+        const int c0 = c[0], c1 = c[1];
+        if (r < rank) { up_before += c0; eq_before += c1; }
     }
     cluster.sync();                             // nobody leaves while its counts are read
     int64_t at = base + up_before + min(eq_before, (int)need);
-    for (int x0 = lo; x0 < hi; x0 += kEvictThreads) {
-        const int i = x0 + tid;
-        const int st = i < hi ? state(i) : 0;
-        int eqs, stay_all;
-        const int eq_rank = eq_before + block_exclusive_scan<kEvictThreads>(st == 1, scan, eqs);
-        const int stays = st == 2 || (st == 1 && eq_rank < (int)need);
-        const int64_t j = at + block_exclusive_scan<kEvictThreads>(stays, scan, stay_all);
+    for (int x = w_lo; x < w_hi; x += 32) {
+        const int i = x + lane;
+        const int st = i < w_hi ? state(i) : 0;
+        const uint32_t below = (1u << lane) - 1u;
+        const uint32_t equal = __ballot_sync(0xffffffffu, st == 1);
+        const bool stays = st == 2 || (st == 1 && eq_before + __popc(equal & below) < (int)need);
+        const uint32_t all = __ballot_sync(0xffffffffu, stays);
+        const int64_t j = at + __popc(all & below);
         if (stays && j < a.capacity) {
             a.kept_pos[j] = (int32_t)(begin + i);
             if (a.out_mass) a.out_mass[j] = __ldg(mass + i);
         }
-        at += stay_all;
-        eq_before += eqs;
+        at += __popc(all);
+        eq_before += __popc(equal);
     }
 }
 
@@ -206,9 +232,13 @@ extern "C" sharpv_status sharpv_evict_select(
     if (!seq_begin || !seq_len || !budget || (cache_tokens > 0 && !mass) || (capacity > 0 && !out_kept_pos))
         return SHARPV_ERR_INVALID_ARG;
     if (out_mass && mass && out_mass < mass + cache_tokens && mass < out_mass + capacity) return SHARPV_ERR_INVALID_ARG;
+    // room for a slice of the longest sequence that the cache can hold, up to kKeyRoom
+    const int64_t slice = (cache_tokens + kEvictCluster - 1) / kEvictCluster + 1;
+    const int room = (int)(slice < kKeyRoom ? slice : kKeyRoom);
     EvictArgs a = {mass, cache_tokens, num_seqs, seq_begin, seq_len, budget, sink, recent,
-                   out_kept_pos, out_kept_seq_offsets, out_mass, capacity, status_word};
-    if (launch_dependent(evict_select_kernel, dim3((unsigned)num_seqs * kEvictCluster), dim3(kEvictThreads), 0, stream, a) !=
+                   out_kept_pos, out_kept_seq_offsets, out_mass, capacity, room, status_word};
+    if (cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeyRoom * 4) != cudaSuccess ||
+        launch_dependent(evict_select_kernel, dim3((unsigned)num_seqs * kEvictCluster), dim3(kEvictThreads), (size_t)room * 4, stream, a) !=
         cudaSuccess) {
         (void)cudaGetLastError();
         return SHARPV_ERR_CUDA;

@@ -231,25 +231,28 @@ attn_simt_kernel(const __grid_constant__ AttnArgs a) {
     if (threadIdx.x == 0) a.shared[blockIdx.x] = shared;
 }
 
-// CTA (c, y) joins rows of the segment that the CTAs c .. last of the kernel before shared, WPR warps a row (a warp takes
-// every WPR-th part): the parts' running maxima and sums are brought to the common maximum, the weighted sums
+// CTA (x, y) joins 8 / W rows of the x-th segment that several CTAs of the kernel before shared, W warps a row (one takes
+// every W-th part): the parts' running maxima and sums are brought to the common maximum, the weighted sums
 // added in a fixed order (results do not depend on scheduling), divided, rounded once.  What bounds it is the latency
-// of three dependent reads, hence eight parts' loads in flight a warp, and eight warps a row where a segment
-// has few rows (its parts are many then: up to one a CTA).
+// of a few dependent reads, hence eight parts' loads in flight a warp, and W = 8 where a segment may have many parts.
+// With few parts a segment one warp a row keeps all CTAs resident at once: 16 sequences of one token 36 us a call with eight,
+// 27 with one.
 constexpr int kJoinAhead = 8;
-template <int DT, int WPR>
+template <int DT, int W>
 __global__ void __launch_bounds__(256)
 attn_join_kernel(const __grid_constant__ AttnArgs a) {
     using St = Store<DT>;
-    constexpr int KD = kMaxHeadDim / 128, RPC = 8 / WPR;
-    __shared__ float4 part[WPR > 1 ? 8 : 1][KD][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x;
+    constexpr int KD = kMaxHeadDim / 128;
+    __shared__ float4 part[W > 1 ? W : 1][KD][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G, R = a.split.rows;
-    const int r = blockIdx.y * RPC + warp / WPR, w = warp % WPR;
+    const int r = blockIdx.y * (8 / W) + warp / W, w = warp % W;
     cudaGridDependencySynchronize();
+    const int c0 = find_shared(a, blockIdx.x);
+    if (c0 < 0) return;
     const SharedSegment seg = a.shared[c0];
     const int row = seg.rt * R + r;
-    if (seg.last < 0 || row >= seg.rows) return;            // with WPR = 8 the whole CTA, else warps of their own
+    if (seg.last < 0 || row >= seg.rows) return;            // with W = 8 the whole CTA, else a warp of its own
     const int c1 = seg.last;
     float top = neg_inf();
     for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(a.part_ml + (int64_t)(c * 2 + (c == c0)) * 2 * R + r));
@@ -268,7 +271,7 @@ attn_join_kernel(const __grid_constant__ AttnArgs a) {
             sum += __ldcg(ml + R) * f;
         }
         const int n = min(32, c1 - c + 1);
-        for (int i = w; i < n; i += kJoinAhead * WPR) {
+        for (int i = w; i < n; i += kJoinAhead * W) {
 #pragma unroll
             for (int k = 0; k < KD; ++k) {
                 const int col = k * 128 + lane * 4;
@@ -276,14 +279,14 @@ attn_join_kernel(const __grid_constant__ AttnArgs a) {
                 float4 v[kJoinAhead];
 #pragma unroll
                 for (int x = 0; x < kJoinAhead; ++x) {
-                    const int y = i + x * WPR;
+                    const int y = i + x * W;
                     v[x] = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (y < n && col < D)
                         v[x] = __ldcg(reinterpret_cast<const float4*>(a.part_o + ((int64_t)((c + y) * 2 + (c + y == c0)) * R + r) * D + col));
                 }
 #pragma unroll
                 for (int x = 0; x < kJoinAhead; ++x) {
-                    const int y = i + x * WPR;
+                    const int y = i + x * W;
                     const float fx = __shfl_sync(0xffffffffu, f, y & 31);
                     if (y < n) {
                         acc[k].x = fmaf(fx, v[x].x, acc[k].x);
@@ -295,16 +298,16 @@ attn_join_kernel(const __grid_constant__ AttnArgs a) {
             }
         }
     }
-    sum = warp_sum(sum);                        // every warp of a row has all of it
-    if constexpr (WPR > 1) {
+    sum = warp_sum(sum);                    // every warp of a row has all of it
+    if constexpr (W > 1) {
 #pragma unroll
-        for (int k = 0; k < KD; ++k) part[warp][k][lane] = acc[k];
+        for (int k = 0; k < KD; ++k) part[w][k][lane] = acc[k];
         __syncthreads();
         if (w != 0) return;
-        for (int y = 1; y < WPR; ++y) {
+        for (int y = 1; y < W; ++y) {
 #pragma unroll
             for (int k = 0; k < KD; ++k) {
-                const float4 v = part[warp + y][k][lane];
+                const float4 v = part[y][k][lane];
                 acc[k].x += v.x;
                 acc[k].y += v.y;
                 acc[k].z += v.z;
@@ -350,10 +353,9 @@ sharpv_status join_launch(const AttnArgs& a, cudaStream_t stream) {
     // rows that any segment can have
     const int64_t all = a.seqs.total_nodes * a.split.group;
     const unsigned rows = (unsigned)(all < a.split.rows ? all : a.split.rows);
-    const cudaError_t e =
-        a.split.rows <= 32
-            ? launch_dependent(attn_join_kernel<DT, 8>, dim3((unsigned)a.ctas, rows), dim3(256), 0, stream, a)
-            : launch_dependent(attn_join_kernel<DT, 1>, dim3((unsigned)a.ctas, (rows + 7) / 8), dim3(256), 0, stream, a);
+    const unsigned x = (unsigned)join_ctas(a);
+    const cudaError_t e = many_parts(a) ? launch_dependent(attn_join_kernel<DT, 8>, dim3(x, rows), dim3(256), 0, stream, a)
+                                             : launch_dependent(attn_join_kernel<DT, 1>, dim3(x, (rows + 7) / 8), dim3(256), 0, stream, a);
     if (e != cudaSuccess) {
         (void)cudaGetLastError();
         return SHARPV_ERR_CUDA;
@@ -460,6 +462,8 @@ extern "C" sharpv_status sharpv_tree_attention(
     const Choice ch = choose(layout->dtype, D, group, average_rows(num_seqs, total_nodes, group));
     a.split = Split{ch.rows, ch.path == Path::tc ? kTcTileKeys : (ch.path == Path::rows ? kRowsTileKeys : kSimtKeys), group, H,
                     draft_k != nullptr};
+    const int64_t segments = (total_nodes * group / ch.rows + num_seqs) * H;     // rounding a sequence's last tile up adds one at most
+    a.max_segments = (int)(segments < kMaxAttnCtas ? segments : kMaxAttnCtas);
     char* ws = (char*)workspace;
     a.shared = (SharedSegment*)ws;
     a.part_ml = (float*)(ws + shared_bytes());

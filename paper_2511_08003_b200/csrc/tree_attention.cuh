@@ -32,6 +32,7 @@ struct AttnArgs {
     float* part_ml;             // [slots][2][rows]: running maximum and sum of each row
     float* part_o;              // [slots][rows][D]: weighted sums, not yet divided
     int ctas;
+    int max_segments;           // that there can be
     int32_t* status_word;
 };
 
@@ -76,6 +77,30 @@ __device__ __forceinline__ void note_shared(const Portion& p, const Split& sp, i
     seg.h = p.h;
     seg.rt = p.rt;
     seg.last = Deal(units, ctas).owner(next_unit + (p.kt_all - p.kt1) - 1);
+}
+
+// Whether segments have many parts each.  Then there are few shared segments, and a joining kernel has a CTA row for
+// each, found among the CTAs' notes; else one for every CTA of the kernel before, most of which have something to join.
+__host__ __device__ inline bool many_parts(const AttnArgs& a) { return a.ctas >= 8 * a.max_segments; }
+__host__ __device__ inline int join_ctas(const AttnArgs& a) { return many_parts(a) ? a.max_segments : a.ctas; }
+
+// The first CTA of the x-th shared segment, -1 if there are fewer.  By a whole warp.
+__device__ __forceinline__ int find_shared(const AttnArgs& a, int x) {
+    if (!many_parts(a)) return x;
+    const int lane = threadIdx.x & 31;
+    constexpr int N = (kMaxAttnCtas + 31) / 32;
+    int last[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) last[k] = k * 32 + lane < a.ctas ? __ldcg(&a.shared[k * 32 + lane].last) : -1;
+    int found = -1, count = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const uint32_t valid = __ballot_sync(0xffffffffu, last[k] >= 0);
+        const uint32_t mine = __ballot_sync(0xffffffffu, last[k] >= 0 && count + __popc(valid & ((1u << lane) - 1u)) == x);
+        if (mine) found = k * 32 + __ffs(mine) - 1;
+        count += __popc(valid);
+    }
+    return found;
 }
 
 // out and lse of one row element from its weighted sum, running maximum (log 2 units) and sum

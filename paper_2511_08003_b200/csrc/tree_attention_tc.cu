@@ -552,24 +552,23 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
     if (warp == kMmaWarp) tmem_free(tmem, kCols);
 }
 
-// Joins a segment's parts: CTA (c, y, z) takes 32 rows (lane = row) and eight groups of four columns (one a warp) of
-// the segment that CTA c begins; the parts are added in the order of the CTAs.
-constexpr int kJoinAhead = 8;
+// Joins the parts of the segments that several CTAs shared: CTA (x, y, z) takes 32 places (lane = place) and eight groups of
+// four columns (one a warp) of the x-th.  The parts are added in the order of the CTAs, with a running maximum.
+constexpr int kJoinAhead = 12;
 __global__ void __launch_bounds__(256)
 attn_tc_join_kernel(const __grid_constant__ AttnArgs a) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x;
-    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G, tile_rows = a.split.rows / 2;
     const int r = blockIdx.y * 32 + lane, c4 = blockIdx.z * 8 + warp;
+    if (c4 * 4 >= D) return;
     cudaGridDependencySynchronize();
+    const int c0 = find_shared(a, blockIdx.x);
+    if (c0 < 0) return;
     const SharedSegment seg = a.shared[c0];
-    const int tile_rows = a.split.rows / 2, row = seg.rt * a.split.rows + (r >> 7) * tile_rows + (r & 127);
-    if (seg.last < 0 || (r & 127) >= tile_rows || row >= seg.rows || c4 * 4 >= D) return;
+    const int row = seg.rt * a.split.rows + (r >> 7) * tile_rows + (r & 127);
+    if (seg.last < 0 || (r & 127) >= tile_rows || row >= seg.rows) return;
     const int c1 = seg.last;
-    float top = neg_inf();
-#pragma unroll 8
-    for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(a.part_ml + (int64_t)(c * 2 + (c == c0)) * 2 * kRows + r));
-    const float base = top == neg_inf() ? 0.f : top;
-    float sum = 0.f;
+    float top = neg_inf(), sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i = c0; i <= c1; i += kJoinAhead) {
         float4 v[kJoinAhead];
@@ -587,6 +586,16 @@ attn_tc_join_kernel(const __grid_constant__ AttnArgs a) {
                 l[x] = __ldcg(a.part_ml + (slot * 2 + 1) * kRows + r);
             }
         }
+        float next_top = top;
+#pragma unroll
+        for (int x = 0; x < kJoinAhead; ++x) next_top = fmaxf(next_top, m[x]);
+        const float base = next_top == neg_inf() ? 0.f : next_top, old = ex2(top - base);
+        sum *= old;
+        acc.x *= old;
+        acc.y *= old;
+        acc.z *= old;
+        acc.w *= old;
+        top = next_top;
 #pragma unroll
         for (int x = 0; x < kJoinAhead; ++x) {
             if (i + x > c1) break;
@@ -618,7 +627,7 @@ sharpv_status launch(const AttnArgs& a, cudaStream_t stream) {
     const unsigned rows = (unsigned)(all <= a.split.rows / 2 ? all : kRows);        // places that any segment can use
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
         launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kThreads), smem, stream, a, maps) != cudaSuccess ||
-        launch_dependent(attn_tc_join_kernel, dim3((unsigned)a.ctas, (rows + 31) / 32, (unsigned)(a.head_dim + 31) / 32), dim3(256), 0,
+        launch_dependent(attn_tc_join_kernel, dim3((unsigned)join_ctas(a), (rows + 31) / 32, (unsigned)(a.head_dim + 31) / 32), dim3(256), 0,
                          stream, a) != cudaSuccess) {
         (void)cudaGetLastError();
         return SHARPV_ERR_CUDA;
