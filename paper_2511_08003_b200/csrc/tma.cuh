@@ -126,6 +126,12 @@ __device__ __forceinline__ uint32_t nonfinite_bf16(uint32_t x) {
     return ((x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
 
+// whether one of eight bf16 is infinite or NaN: an exponent of ones carries into the sign's place
+__device__ __forceinline__ bool any_nonfinite(const uint4& v) {
+    auto carry = [](uint32_t x) { return (x & 0x7f807f80u) + 0x00800080u; };
+    return ((carry(v.x) | carry(v.y) | carry(v.z) | carry(v.w)) & 0x80008000u) != 0;
+}
+
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

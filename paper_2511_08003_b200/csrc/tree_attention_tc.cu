@@ -308,6 +308,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                         const int left = keys_left(a, p, kt);
                         const bool drafted = kt >= p.kt_cache;
                         bool odd = false;
+#pragma unroll 8
                         for (int x = t64; x < 128 * CH; x += 64) {
                             const int key = (x >> 3) & 127;         // 128 rows of 8 chunks, then the next 64 columns
                             uint4* at = reinterpret_cast<uint4*>(tile + x * 16);
@@ -315,10 +316,10 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                                 *at = make_uint4(0, 0, 0, 0);
                             } else if (drafted) {
                                 const uint4 v = *at;
-                                const uint4 off = make_uint4(nonfinite_bf16(v.x), nonfinite_bf16(v.y), nonfinite_bf16(v.z), nonfinite_bf16(v.w));
-                                if (off.x | off.y | off.z | off.w) {
+                                if (any_nonfinite(v)) {
                                     odd = true;
-                                    *at = make_uint4(v.x & ~off.x, v.y & ~off.y, v.z & ~off.z, v.w & ~off.w);
+                                    *at = make_uint4(v.x & ~nonfinite_bf16(v.x), v.y & ~nonfinite_bf16(v.y), v.z & ~nonfinite_bf16(v.z),
+                                                     v.w & ~nonfinite_bf16(v.w));
                                 }
                             }
                         }
@@ -356,6 +357,20 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
             float m2 = neg_inf(), l = 0.f;                          // maximum in log 2 units, as used; sum
             for (int x = 0; x < mine; ++x) {
                 const int kt = p.kt0 + (st.pair ? x : 2 * x + w);
+                const bool masked = tile_masked(a, p, kt);
+                uint32_t sees[4] = {~0u, ~0u, ~0u, ~0u};            // the keys that the row sees, looked up ahead of the scores
+                if (work && masked) {
+                    const int left = keys_left(a, p, kt);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (kt < p.kt_cache) {
+                            const int n = left - i * 32;
+                            sees[i] = n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u);
+                        } else {
+                            sees[i] = a.split.draft && row < r_all ? draft_sees(a, p.s, row / G, (kt - p.kt_cache) * kKeys + i * 32) : 0u;
+                        }
+                    }
+                }
                 if (!wait_warp(&sm.scores[w], steps + x)) break;
                 if (work) {
                     tc_fence_after();
@@ -363,20 +378,13 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
 #pragma unroll
                     for (int i = 0; i < 4; ++i) tmem_ld32(s[i], t_scores + i * 32);
                     tmem_wait_ld();
-                    if (tile_masked(a, p, kt)) {
-                        const int left = keys_left(a, p, kt);
+                    if (masked) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            uint32_t sees;
-                            if (kt < p.kt_cache) {
-                                const int n = left - i * 32;
-                                sees = n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u);
-                            } else {
-                                sees = a.split.draft && row < r_all ? draft_sees(a, p.s, row / G, (kt - p.kt_cache) * kKeys + i * 32) : 0u;
-                            }
+                            if (__all_sync(0xffffffffu, sees[i] == ~0u)) continue;
 #pragma unroll
                             for (int k = 0; k < 32; ++k)
-                                if (!(sees >> k & 1)) s[i][k] = 0xff800000u;
+                                if (!(sees[i] >> k & 1)) s[i][k] = 0xff800000u;
                         }
                     }
                     float top4[4];
