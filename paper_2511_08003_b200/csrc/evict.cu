@@ -5,8 +5,8 @@
 // its slice in shared memory, and all read one another's counts.  The rows above the k-th key stay, and of those equal
 // to it the first ones; the warps' and slices' counts give every warp the place where its survivors go.
 // What bounds it is latency (four rounds of counting with two barriers of the cluster each): the keys are read from
-// memory once and kept in shared memory (slices too long for that are read again every round), and lanes of a warp
-// that count the same digit (weights span few powers of two) count it with one atomic.
+// memory once and kept in shared memory (slices too long for that are read again every round), and in the first round
+// lanes of a warp that count the same digit (weights span few powers of two) count it with one atomic.
 #include <cooperative_groups.h>
 
 #include "decode_common.cuh"
@@ -122,9 +122,13 @@ evict_select_kernel(const __grid_constant__ EvictArgs a) {
                 const int i = i0 + tid;
                 const uint32_t key = i < hi ? key_of(i) : 0u;
                 const bool in = i < hi && (i < s_end || i >= r_begin) == among_guarded && (pass == 0 || key >> (shift + 8) == prefix);
-                const int digit = in ? (int)(key >> shift & 255) : kBins;
-                const uint32_t same = __match_any_sync(0xffffffffu, digit);
-                if (in && lane == __ffs(same) - 1) atomicAdd(&h[digit], __popc(same));
+                if (pass == 0) {
+                    const int digit = in ? (int)(key >> 24) : kBins;
+                    const uint32_t same = __match_any_sync(0xffffffffu, digit);
+                    if (in && lane == __ffs(same) - 1) atomicAdd(&h[digit], __popc(same));
+                } else if (in) {
+                    atomicAdd(&h[key >> shift & 255], 1);
+                }
             }
             cluster.sync();
             if (tid < kBins) {
@@ -132,7 +136,7 @@ evict_select_kernel(const __grid_constant__ EvictArgs a) {
 #pragma unroll
                 for (int r = 0; r < kEvictCluster; ++r) t += cluster.map_shared_rank(h, r)[tid];
                 total[tid] = t;
-            } else {
+            } else if (tid < 2 * kBins) {
                 hist[(pass + 1) & 1][tid - kBins] = 0;               // read by nobody since the sync of the pass before
             }
             __syncthreads();
@@ -172,6 +176,7 @@ evict_select_kernel(const __grid_constant__ EvictArgs a) {
     const int n = hi - lo;
     const int w_lo = lo + (int)((int64_t)n * warp / kWarps), w_hi = lo + (int)((int64_t)n * (warp + 1) / kWarps);
     int up = 0, eq = 0;
+#pragma unroll 4
     for (int x = w_lo; x < w_hi; x += 32) {
         const int st = x + lane < w_hi ? state(x + lane) : 0;
         up += __popc(__ballot_sync(0xffffffffu, st == 2));

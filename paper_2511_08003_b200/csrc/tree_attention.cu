@@ -77,12 +77,12 @@ attn_simt_kernel(const __grid_constant__ AttnArgs a) {
     const PlanStart plan = plan_cta<kSimtThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
     Walk walk(plan, first, end);
     Portion part;
-    SharedSegment shared = {0, 0, 0, 0, -1};
+    bool any = false;
     while (walk.next(a.seqs, a.split, part)) {
         const SeqInfo& s = part.s;
         const int kt_all = part.kt_all, kt_cache = part.kt_cache, kt0 = part.kt0, kt1 = part.kt1, h = part.h;
         const int r_base = part.rt * R, r_all = s.nodes * G;
-        if (threadIdx.x == 0) note_shared(part, a.split, walk.u, plan.units, a.ctas, shared);
+        any = true;
 
         auto load_tile = [&](int kt, int buf) {
             const char *k, *v;
@@ -228,7 +228,7 @@ attn_simt_kernel(const __grid_constant__ AttnArgs a) {
             }
         }
     }
-    if (threadIdx.x == 0) a.shared[blockIdx.x] = shared;
+    if (threadIdx.x == 0) note_shared(a, any, part, end, plan.units);
 }
 
 // CTA (x, y) joins 8 / W rows of the x-th segment that several CTAs of the kernel before shared, W warps a row (one takes

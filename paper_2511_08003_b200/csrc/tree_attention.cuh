@@ -68,15 +68,14 @@ __device__ __forceinline__ uint32_t draft_sees(const AttnArgs& a, const SeqInfo&
     return sees & there;
 }
 
-// What thread 0 of a CTA says of the segment it shares with the CTAs behind it: called for every portion.
-__device__ __forceinline__ void note_shared(const Portion& p, const Split& sp, int64_t next_unit, int64_t units, int ctas,
-                                            SharedSegment& seg) {
-    if (p.kt0 != 0 || p.kt1 == p.kt_all) return;
-    seg.node0 = p.s.node0;
-    seg.rows = p.s.nodes * sp.group;
-    seg.h = p.h;
-    seg.rt = p.rt;
-    seg.last = Deal(units, ctas).owner(next_unit + (p.kt_all - p.kt1) - 1);
+// What a CTA says of the segment that it shares with the CTAs behind it, by one thread: `last` is its last portion (the only
+// one that can start a segment without ending it), `any` whether it has one.
+__device__ __forceinline__ void note_shared(const AttnArgs& a, bool any, const Portion& last, int64_t end, int64_t units) {
+    SharedSegment seg = {0, 0, 0, 0, -1};
+    if (any && last.kt0 == 0 && last.kt1 < last.kt_all)
+        seg = SharedSegment{last.s.node0, last.s.nodes * a.split.group, last.h, last.rt,
+                            Deal(units, a.ctas).owner(end + (last.kt_all - last.kt1) - 1)};
+    a.shared[blockIdx.x] = seg;
 }
 
 // Whether segments have many parts each.  Then there are few shared segments, and a joining kernel has a CTA row for

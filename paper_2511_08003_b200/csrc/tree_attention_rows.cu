@@ -37,7 +37,6 @@ struct Shared {
     float top[16], sum[16];
     uint8_t q[2][MT * 16 * C::kQPitch];         // query rows of this portion and the next
     Portion part[2];                            // kt1 < 0: there are no more
-    int64_t next_unit[2];
     uint64_t full[C::kStages], empty[C::kStages], part_full[2], part_empty[2];
     int poison, dead;
     PlanScratch<kThreads> plan;
@@ -75,9 +74,10 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
 
     if (warp == kWarps) {                       // portions, query rows and tiles ahead of the warps that compute
         Walk walk(plan, first, end);
-        Portion p;
+        Portion p, last;
         for (;; ++pn) {
             const int slot = pn & 1;
+            last = p;
             const bool more = walk.next(a.seqs, a.split, p);
             if (pn >= 2 && alive) alive = __all_sync(0xffffffffu, mbar_wait(&sm.part_empty[slot], ((pn >> 1) - 1) & 1));
             if (more) {
@@ -94,7 +94,6 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
             if (lane == 0) {
                 if (!more) p.kt1 = -1;
                 sm.part[slot] = p;
-                sm.next_unit[slot] = walk.u;
                 mbar_arrive(&sm.part_full[slot]);
             }
             if (!more) break;
@@ -129,13 +128,13 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
                 (void)mbar_wait(&sm.full[last % C::kStages], (last / C::kStages) & 1);
             }
         }
+        if (lane == 0) note_shared(a, pn > 0, last, end, plan.units);
         cp_async_wait<0>();
         return;
     }
 
     const int group = warp >> 2, sub = warp & 3;        // tiles of this parity, 16 keys from sub * 16 on
     const int qr = lane >> 2, qc = (lane & 3) * 2;      // fragment row (and row + 8), column (and column + 1)
-    SharedSegment shared = {0, 0, 0, 0, -1};
     for (;; ++pn) {
         const int at_part = pn & 1;
         if (alive && !mbar_wait(&sm.part_full[at_part], (pn >> 1) & 1)) {
@@ -315,7 +314,8 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
                     for (int j = 0; j < DP / 8; ++j)
                         if (x == t && j * 8 >= c0 && j * 8 < c0 + C::kCols) {
                             *reinterpret_cast<float2*>(&sm.merge[warp][qr][j * 8 - c0 + qc]) = make_float2(o[x][j][0], o[x][j][1]);
-                            *reinterpret_cast<float2*>(&sm.merge[warp][qr + 8][j * 8 - c0 + qc]) = make_float2(o[x][j][2], o[x][j][3]);
+                            if (r_base + t * 16 + 8 < r_all)        // rows 8 to 15 hold something
+                                *reinterpret_cast<float2*>(&sm.merge[warp][qr + 8][j * 8 - c0 + qc]) = make_float2(o[x][j][2], o[x][j][3]);
                         }
                 consumer_sync();
                 constexpr int V = C::kCols / 4;
@@ -370,14 +370,10 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
                 consumer_sync();
             }
         }
-        if (threadIdx.x == 0) {
-            sm.poison = 0;
-            note_shared(p, a.split, sm.next_unit[at_part], plan.units, a.ctas, shared);
-        }
+        if (threadIdx.x == 0) sm.poison = 0;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.part_empty[at_part]);
     }
-    if (threadIdx.x == 0) a.shared[blockIdx.x] = shared;
 }
 
 template <int MT, int DP>

@@ -40,7 +40,6 @@ struct Shared {
     uint8_t q[2][C::kTileBytes];
     uint8_t tiles[C::kStages][C::kTileBytes];
     Portion part[2];                            // kt1 < 0: there are no more
-    int64_t next_unit[2];
     float m[128], l[128];                       // of stream 1, when the streams share their rows
     uint64_t full[C::kStages], empty[C::kStages];
     uint64_t part_full[2], part_empty[2];
@@ -165,16 +164,17 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
         if (warp == kLoadWarp) {
             if (lane == 0) {
                 Walk walk(plan, first, end);
-                Portion p;
+                Portion p, last;
                 uint32_t it = 0;
                 for (uint32_t pn = 0; alive; ++pn) {
                     const int at = pn & 1;
+                    last = p;
                     const bool more = walk.next(a.seqs, a.split, p);
+                    if (!more) note_shared(a, pn > 0, last, end, plan.units);
                     if (pn >= 2 && !wait(&sm.part_empty[at], (pn >> 1) - 1)) break;
                     if (!more) p.kt1 = -1;
                     sm.poison[at] = 0;
                     sm.part[at] = p;
-                    sm.next_unit[at] = walk.u;
                     mbar_arrive(&sm.part_full[at]);
                     if (!more) break;
                     // query rows: whole nodes, the group's heads of each next to each other
@@ -205,6 +205,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                     }
                 }
                 if (!alive) {
+                    a.shared[blockIdx.x].last = -1;
                     for (uint32_t i = 0; i < (uint32_t)C::kStages && i < it; ++i) {     // copies in flight land first
                         const uint32_t last = it - 1 - i;
                         (void)mbar_wait(&sm.full[last % C::kStages], (last / C::kStages) & 1);
@@ -342,7 +343,6 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
         const uint32_t t_scores = tmem + lanes + w * 128, t_sums = tmem + lanes + kSumCol + w * DP;
         const uint64_t c2 = pack2(a.scale_log2, a.scale_log2);
         uint32_t steps = 0, merges = 0, summed = 0;
-        SharedSegment shared = {0, 0, 0, 0, -1};
         for (uint32_t pn = 0;; ++pn) {
             if (!wait_warp(&sm.part_full[pn & 1], pn >> 1)) break;
             const Portion p = sm.part[pn & 1];
@@ -545,12 +545,10 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                     mbar_arrive(&sm.merge_done);
                 }
             }
-            if (threadIdx.x == 0) note_shared(p, a.split, sm.next_unit[pn & 1], plan.units, a.ctas, shared);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&sm.part_empty[pn & 1]);
         }
-        if (threadIdx.x == 0) a.shared[blockIdx.x] = shared;
     }
     if (!alive) report(a.status_word, SHARPV_ERR_TIMEOUT);
     __syncwarp();
