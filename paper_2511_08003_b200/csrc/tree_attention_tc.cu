@@ -45,7 +45,7 @@ struct Shared {
     uint64_t part_full[2], part_empty[2];
     uint64_t clean[C::kStages];                 // value tiles: gone through (or nothing to do)
     uint64_t q_full, q_empty;
-    uint64_t scores[2], weights[2][2], sums[2]; // per stream: products done, each half of the weights written, a portion's weighted sums added
+    uint64_t scores[2], weights[2], sums[2];    // per stream: scores formed, weights written, a portion's weighted sums added
     uint64_t merge_full, merge_done, drain;
     int poison[2];
     uint32_t tmem;
@@ -131,8 +131,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
             mbar_init(&sm.part_full[i], 1);
             mbar_init(&sm.part_empty[i], 11);           // the warps that read it
             mbar_init(&sm.scores[i], 1);
-            mbar_init(&sm.weights[i][0], 4);
-            mbar_init(&sm.weights[i][1], 4);
+            mbar_init(&sm.weights[i], 4);
             mbar_init(&sm.sums[i], 1);
         }
         mbar_init(&sm.q_full, 1);
@@ -154,8 +153,8 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
         if (alive && !mbar_wait(bar, phase & 1)) alive = false;
         return alive;
     };
-    auto wait_warp = [&](uint64_t* bar, uint32_t phase) {       // by a whole warp, with one answer
-        if (alive) alive = __all_sync(0xffffffffu, mbar_wait(bar, phase & 1));
+    auto wait_warp = [&](uint64_t* bar, uint32_t phase) {       // by a whole warp: its lanes ask together and get one answer
+        if (alive) alive = mbar_wait(bar, phase & 1);
         return alive;
     };
 
@@ -255,22 +254,17 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                     if (!pair || w == 0) {
                         if (!wait_warp(&sm.clean[vr.stage], vr.use())) break;
                     }
+                    if (!wait_warp(&sm.weights[w], steps0[w] + mine)) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t v = v_op + vr.stage * (C::kTileBytes >> 4);
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {              // the first half while the second is being weighed
-                        if (!wait_warp(&sm.weights[w][half], steps0[w] + mine)) break;
-                        tc_fence_after();
-                        if (elect_one()) {
-                            const uint64_t v = v_op + vr.stage * (C::kTileBytes >> 4) + half * (kKeys / 2 * 128 >> 4);
-#pragma unroll
-                            for (int kk = 0; kk < kKeys / 32; ++kk)
-                                mma_ts(tmem + kSumCol + w * DP, tmem + w * 128 + half * 32 + kk * 8, v + kk * (16 * 128 >> 4), v_shape,
-                                       mine > 0 || half > 0 || kk > 0);
-                            // a step's scores say that the weighted sums of the step before are in; of the last step this does
-                            if (half == 1 && t + 2 >= n) mma_commit(&sm.sums[w]);
-                        }
-                        __syncwarp();
+                        for (int kk = 0; kk < kKeys / 16; ++kk)
+                            mma_ts(tmem + kSumCol + w * DP, tmem + w * 128 + kk * 8, v + kk * (16 * 128 >> 4), v_shape, mine > 0 || kk > 0);
+                        // a step's scores say that the weighted sums of the step before are in; of the last step this does
+                        if (t + 2 >= n) mma_commit(&sm.sums[w]);
                     }
-                    if (!alive) break;
+                    __syncwarp();
                     const int v_stage = vr.stage;
                     const bool v_done = !pair || w == 1;
                     if (v_done) vr.next();
@@ -432,22 +426,17 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                             pk[k] = pack_bf16(y0, y1);
                         }
                         tmem_st16(t_scores + i * 16, pk);
-                        if (i & 1) {
-                            tmem_wait_st();
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(&sm.weights[w][i >> 1]);
-                        }
                     }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sm.weights[w]);
                     float s0, s1;
                     unpack2(add2(sum2[0], sum2[1]), s0, s1);
                     l += s0 + s1;
                 } else {
                     __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(&sm.weights[w][0]);
-                        mbar_arrive(&sm.weights[w][1]);
-                    }
+                    if (lane == 0) mbar_arrive(&sm.weights[w]);
                 }
             }
             if (!alive) break;
