@@ -370,9 +370,12 @@ sharpv_status simt_by_dim(AttnArgs& a, int sms, cudaStream_t stream) {
     return simt_launch<DT, R, 256>(a, sms, stream);
 }
 
-// Which kernels a call takes, by the average query rows of a (sequence, KV head).  bf16: the row kernel reads K and V at
-// the memory's rate up to 16 rows; beyond 32 the tensor cores' kernel is ahead.
-constexpr int64_t kMaxRowsPath = 32;
+// Which kernels a call takes, by type, head_dim and the average query rows of a (sequence, KV head).  Up to 16 rows one
+// row tile of the row kernel takes them all and K and V are read once; with more it would read them again for every 16,
+// and the tensor cores' kernel is ahead at once (21 rows, 4 KV heads x 128, us: 50,432 rows 36 against 55, the ragged
+// batch of 16 34 against 54, 6,272 rows 19 against 23; 56 rows: 37 / 77, 36 / 84, 19 / 34).  It holds up to 128 columns and
+// groups of up to 128 heads; beyond, the row kernel takes any number of rows.
+constexpr int64_t kMaxRowsPath = 16;
 enum class Path { simt, rows, tc };
 struct Choice {
     Path path;
@@ -381,11 +384,9 @@ struct Choice {
     int max_ctas;           // sizes the workspace
 };
 Choice choose(sharpv_dtype dtype, int head_dim, int group, int64_t avg_rows) {
-    const int few = dtype == SHARPV_F32 ? 8 : 16;
-    if (dtype == SHARPV_BF16 && head_dim <= 128 && group <= 128 && avg_rows > kMaxRowsPath)
-        return {Path::tc, tc_rows(group), kTcPlaces, kMaxTcCtas};
-    const int rows = avg_rows <= few || (dtype == SHARPV_BF16 && head_dim > 128) ? few : 32;
-    return {dtype == SHARPV_F32 ? Path::simt : Path::rows, rows, rows, kMaxAttnCtas};
+    if (dtype == SHARPV_F32) return avg_rows <= 8 ? Choice{Path::simt, 8, 8, kMaxAttnCtas} : Choice{Path::simt, 32, 32, kMaxAttnCtas};
+    if (head_dim <= 128 && group <= 128 && avg_rows > kMaxRowsPath) return {Path::tc, tc_rows(group), kTcPlaces, kMaxTcCtas};
+    return {Path::rows, kRowsTileRows, kRowsTileRows, kMaxAttnCtas};
 }
 int64_t average_rows(int32_t num_seqs, int64_t total_nodes, int64_t group) {
     return num_seqs > 0 ? total_nodes * group / num_seqs : 0;

@@ -42,9 +42,8 @@ struct AttnMaps {
 };
 sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps);
 
-// Few query rows, bf16: a.split has 16 or 32 rows (16 beyond head_dim 128) and kRowsTileKeys keys a tile.  Sets
-// a.ctas to what it launches.
-constexpr int kRowsTileKeys = 64;
+// Few query rows, bf16: a.split has kRowsTileRows rows and kRowsTileKeys keys a tile.  Sets a.ctas to what it launches.
+constexpr int kRowsTileRows = 16, kRowsTileKeys = 64;
 sharpv_status attn_rows_launch(AttnArgs& a, int sms, cudaStream_t stream);
 
 // Many query rows, bf16, head_dim and group of at most 128: a.split has tc_rows(group) rows and kTcTileKeys keys a tile.

@@ -119,6 +119,8 @@ SHAPES = [
     (1, 7, 136, [77], [6]),
     (1, 4, 128, [1500, 3], [130, 64]),
     (1, 2, 64, [640], [300]),
+    (1, 100, 128, [200, 9], [2, 1]),             # a node fills most of a row tile
+    (1, 130, 64, [70, 300], [2, 3]),             # more heads in a group than a row tile holds
 ]
 
 
