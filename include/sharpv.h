@@ -48,7 +48,8 @@ typedef enum {
     SHARPV_ERR_WORKSPACE = 3,     /* workspace smaller than the matching *_workspace_bytes() */
     SHARPV_ERR_CAPACITY = 4,      /* (status_word only) more survivors than `capacity` */
     SHARPV_ERR_CUDA = 5,          /* a CUDA runtime call or launch failed */
-    SHARPV_ERR_TIMEOUT = 6,       /* (status_word only) reserved: a bounded device-side wait gave up; no kernel waits that way at present */
+    SHARPV_ERR_TIMEOUT = 6,       /* (status_word only) a bounded device-side wait of an attention or attention-weight kernel (for its own
+                                     copies and products, two seconds) gave up; the call's outputs are void */
     SHARPV_ERR_BOUNDS = 7         /* (status_word only) an index that a kernel was about to gather from or scatter to lay outside
                                      its range; the access was skipped.  Checked in libraries built with -DSHARPV_DEBUG_BOUNDS,
                                      and in every build by the entry points that say so */
@@ -369,6 +370,7 @@ sharpv_status sharpv_kv_compact_rope(
  *   a prompt, or one decoded token).
  * q [dev] [total_nodes, num_q_heads, head_dim], row stride ld_q; out [dev] the same shape, dense, 16-byte
  *   aligned; out_lse [dev] float[total_nodes, num_q_heads].
+ * out and out_lse must not overlap the inputs.
  * A row that sees nothing gives out = 0 and lse = -inf.  Keys and values that a row does not see never touch
  * its result, whatever they hold (NaN and infinities included).  Scores, the softmax's maximum and sum and the
  * weighted sums are fp32; out is rounded once.  scale > 0, finite.  Results do not depend on scheduling.
@@ -398,7 +400,8 @@ sharpv_status sharpv_tree_attention(
  * node_weight [dev] float[total_nodes] or NULL (all 1): for example 1 for accepted nodes and 0 for the others;
  *   a node of weight 0 is not looked at.  Rows whose lse is -inf (they saw nothing) add nothing.
  * mass [dev] float[cache_tokens] or NULL: what the rows collected so far, row p at mass[p]; NULL and decay == 0
- *   both mean that nothing is read and the sum starts at 0.  out_mass [dev] float[cache_tokens] may be mass.
+ *   both mean that nothing is read and the sum starts at 0.  out_mass [dev] float[cache_tokens] may be mass, but not
+ *   overlap it otherwise (SHARPV_ERR_INVALID_ARG).
  * The sequences' cache rows must not overlap.  Sums are fp32 in a fixed order.
  * workspace as above, sharpv_attention_mass_workspace_bytes() bytes (0 for SHARPV_BF16 caches: may be NULL).
  */

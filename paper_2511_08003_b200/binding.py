@@ -565,6 +565,14 @@ def _queue(stream, device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
 
+def _lend(stream, *tensors):
+    """Memory that a wrapper allocates belongs to the current stream: a call on another stream has to say that it uses it."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
 def _status(status_word, device):
     return None if status_word is None else _on(status_word, "status_word", device, _I32)
 
@@ -605,11 +613,13 @@ def sharpv_tree_attention(q: torch.Tensor, kv: torch.Tensor, layer: int, seq_beg
         lse = torch.empty((N, HQ), dtype=_F32, device=dev)
         out = {"out": o, "lse": lse}
         po, pl = o.data_ptr(), lse.data_ptr()
+        _lend(stream, o, lse)
     else:
         if out["out"].shape != q.shape or out["lse"].shape != q.shape[:2]:
             raise ValueError("out must be [nodes, q_heads, head_dim], lse [nodes, q_heads]")
         po, pl = _on(out["out"], "out", dev, dtype), _on(out["lse"], "lse", dev, _F32)
     ws = _workspace(workspace, sharpv_tree_attention_workspace_bytes(B, N, HQ, H, D, lay.dtype), dev)
+    _lend(stream, ws)
     rc = _call("sharpv_tree_attention", kv, q.data_ptr(), ldq, dk, ldk, dv, ldv, HQ, kv.data_ptr(), lay, layer,
                kv.shape[3], B, _on(seq_begin, "seq_begin", dev, _I32), _on(seq_len, "seq_len", dev, _I32, B),
                _on(node_offsets, "node_offsets", dev, _I32, B + 1), N, mask, words,
@@ -640,12 +650,17 @@ def sharpv_attention_mass(q: torch.Tensor, lse: torch.Tensor, kv: torch.Tensor, 
         raise ValueError("lse must be [nodes, q_heads]")
     B = seq_begin.numel()
     if out is None:
-        out = torch.zeros(T, dtype=_F32, device=dev)
+        if stream is None:
+            out = torch.zeros(T, dtype=_F32, device=dev)
+        else:
+            with torch.cuda.stream(stream):     # the zeros have to be there before the call
+                out = torch.zeros(T, dtype=_F32, device=dev)
     ws, need = None, 0
     if lay.dtype != BF16:
         need = sharpv_attention_mass_workspace_bytes(T, lay.num_kv_heads, lay.dtype)
         ws = _workspace(workspace, need, dev)
         need = ws.numel()
+        _lend(stream, ws)
     rc = _call("sharpv_attention_mass", kv, q.data_ptr(), ldq, _on(lse, "lse", dev, _F32),
                None if node_weight is None else _on(node_weight, "node_weight", dev, _F32, N), HQ, kv.data_ptr(), lay,
                layer, T, B, _on(seq_begin, "seq_begin", dev, _I32), _on(seq_len, "seq_len", dev, _I32, B),
@@ -673,6 +688,7 @@ def sharpv_evict_select(mass: torch.Tensor, seq_begin: torch.Tensor, seq_len: to
         out = {"kept_pos": pos, "kept_seq_offsets": seq_begin.new_empty(B + 1)}
         if want_mass:
             out["mass"] = mass.new_empty(capacity)
+        _lend(stream, *out.values())
     kept_mass = out.get("mass")
     rc = _call("sharpv_evict_select", mass, _on(mass, "mass", dev, _F32), T, B,
                _on(seq_begin, "seq_begin", dev, _I32), _on(seq_len, "seq_len", dev, _I32, B),

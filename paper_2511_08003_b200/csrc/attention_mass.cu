@@ -230,6 +230,7 @@ extern "C" sharpv_status sharpv_attention_mass(
     if (!seq_begin || !seq_len || !node_offsets || !out_mass || (total_nodes > 0 && (!q || !lse)) ||
         ld_q < (int64_t)num_q_heads * D)
         return SHARPV_ERR_INVALID_ARG;
+    if (mass && mass != out_mass && mass < out_mass + cache_tokens && out_mass < mass + cache_tokens) return SHARPV_ERR_INVALID_ARG;
     if (!aligned16(q) || (ld_q * eb) % 16) return SHARPV_ERR_UNSUPPORTED;
     const size_t need = sharpv_attention_mass_workspace_bytes(cache_tokens, H, layout->dtype);
     if (workspace_bytes < need) return SHARPV_ERR_WORKSPACE;

@@ -370,7 +370,7 @@ sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps) 
     const int D = a.head_dim, H = a.split.heads;
     const int64_t T = a.seqs.cache_tokens > 0 ? a.seqs.cache_tokens : 1, N = a.seqs.total_nodes;
     const int64_t most = (int64_t)1 << 40;              // what a tensor map's strides can say
-    if (a.kv_token >= most || a.kv_head >= most || a.dk_node >= most || a.dv_node >= most) return SHARPV_ERR_UNSUPPORTED;
+    if (a.kv_token >= most || a.kv_head >= most || a.dk_node >= most || a.dv_node >= most || a.q_node >= most) return SHARPV_ERR_UNSUPPORTED;
     bool ok = encode_rows_map(&maps.cache_k, a.cache_k, D, T, a.kv_token, H, a.kv_head, box_rows) &&
               encode_rows_map(&maps.cache_v, a.cache_v, D, T, a.kv_token, H, a.kv_head, box_rows);
     if (a.split.draft)

@@ -74,7 +74,7 @@ def test_tree_attention_refusals(L, change, status):
     (dict(lay=_layout(dtype=0, d=64), ldq=28 * 64, ws=P + 16), S.ERR_UNSUPPORTED),
     (dict(lay=_layout(dtype=0, d=64), ldq=28 * 64, wsb=64), S.ERR_WORKSPACE),
     (dict(decay=-0.5), S.ERR_INVALID_ARG), (dict(decay=float("nan")), S.ERR_INVALID_ARG), (dict(decay=INF), S.ERR_INVALID_ARG),
-    (dict(tokens=0), S.OK),
+    (dict(mass=P + 256), S.ERR_INVALID_ARG), (dict(tokens=0), S.OK),
 ])
 def test_attention_mass_refusals(L, change, status):
     assert _mass(L, **change) == status

@@ -324,6 +324,92 @@ def test_attention_mass_history_is_not_read_when_it_decays_to_nothing():
     assert bool((sv.sharpv_attention_mass(c.q, empty, c.kv, c.layer, *c.tables) == 0).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nodes", [[3, 1], [40, 30]])
+def test_attention_mass_rows_that_saw_nothing(nodes, dtype):
+    """A row whose log-sum-exp is -inf adds nothing, whatever its query holds."""
+    c = Case(dtype, 2, 4, 128, [100, 333], nodes, spare=0)
+    lse = sv.sharpv_tree_attention(c.q, c.kv, c.layer, *c.tables, c.dk, c.dv, c.tree)["lse"]
+    dead = torch.tensor([0, int(c.offsets[1])], device="cuda")
+    w = torch.ones(c.q.shape[0], device="cuda")
+    w[dead] = 0
+    want = sv.sharpv_attention_mass(c.q, lse, c.kv, c.layer, *c.tables, node_weight=w)
+    lse[dead] = float("-inf")
+    c.q[dead] = NAN
+    got = sv.sharpv_attention_mass(c.q, lse, c.kv, c.layer, *c.tables)
+    # the same rows weighed, in another order where rows of weight 0 are left out: 2 (rows + 2) u of the sum
+    rows = 8 * (max(nodes) + 1)
+    assert bool(((got - want).abs() <= 2 * (rows + 2) * ref.U * want).all())
+    alive = torch.isfinite(want)
+    assert bool(alive.all()) and float(want.sum()) > 0
+
+
+# ------------------------------------------------------------------------------------------ far rows, other streams
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("nodes", [1, 40])
+def test_rows_more_than_32_bits_away(nodes, dtype):
+    """A cache whose rows lie 32 KB apart, used at its far end, more than 4 GB behind its start."""
+    D, rows = 128, 170000
+    es = 4 if dtype == "f32" else 2
+    step = 32768 // es
+    big = torch.empty(rows * step, dtype=DT[dtype], device="cuda")
+    kv = big.as_strided((1, 2, 2, rows, D), (0, 2 * D, D, step, 1))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    begin, n = rows - 400, 390
+    near = torch.randn((1, 2, 2, n, D), device="cuda", generator=g).to(DT[dtype])
+    sv.sharpv_kv_append(near, kv, torch.arange(n, dtype=torch.int32, device="cuda"), _i32([0, n]), _i32([begin]))
+    assert torch.equal(kv[:, :, :, begin:begin + n], near)
+    q = torch.randn((nodes, 6, D), device="cuda", generator=g).to(DT[dtype])
+    far = sv.sharpv_tree_attention(q, kv, 0, _i32([begin]), _i32([n]), _i32([0, nodes]))
+    here = sv.sharpv_tree_attention(q, near, 0, _i32([0]), _i32([n]), _i32([0, nodes]))
+    assert torch.equal(far["out"], here["out"]) and torch.equal(far["lse"], here["lse"])
+    m_far = sv.sharpv_attention_mass(q, far["lse"], kv, 0, _i32([begin]), _i32([n]), _i32([0, nodes]))
+    m_here = sv.sharpv_attention_mass(q, far["lse"], near, 0, _i32([0]), _i32([n]), _i32([0, nodes]))
+    assert torch.equal(m_far[begin:begin + n], m_here) and float(m_far[:begin].abs().sum()) == 0
+
+
+def test_calls_on_a_stream_that_is_not_the_current_one():
+    c = Case("bf16", 2, 7, 128, [900, 41], [9, 2], spare=0)
+    f = Case("f32", 2, 7, 64, [900, 41], [9, 2], spare=0)
+    side = torch.cuda.Stream()
+    for x in (c, f):
+        here = sv.sharpv_tree_attention(x.q, x.kv, x.layer, *x.tables, x.dk, x.dv, x.tree)
+        m_here = sv.sharpv_attention_mass(x.q, here["lse"], x.kv, x.layer, *x.tables)
+        k_here = sv.sharpv_evict_select(m_here, x.tables[0], x.tables[1], _i32([300, 20]), 2, 4, 320)
+        torch.cuda.synchronize()
+        for _ in range(20):                     # what the wrappers allocate is in use until the stream is done with it
+            there = sv.sharpv_tree_attention(x.q, x.kv, x.layer, *x.tables, x.dk, x.dv, x.tree, stream=side)
+            m = sv.sharpv_attention_mass(x.q, there["lse"], x.kv, x.layer, *x.tables, stream=side)
+            k = sv.sharpv_evict_select(m, x.tables[0], x.tables[1], _i32([300, 20]), 2, 4, 320, stream=side)
+            junk = [torch.full((1 << 20,), NAN, device="cuda") for _ in range(4)]
+        torch.cuda.synchronize()
+        del junk
+        assert torch.equal(here["out"], there["out"]) and torch.equal(m_here, m) and torch.equal(k_here["kept_pos"], k["kept_pos"])
+
+
+def test_two_captured_graphs_share_a_workspace_one_after_the_other():
+    a = Case("bf16", 2, 7, 128, [2000, 33], [1, 1], spare=0)
+    b = Case("bf16", 2, 7, 128, [1500, 700], [30, 41], spare=0, seed=3)
+    want = [sv.sharpv_tree_attention(x.q, x.kv, x.layer, *x.tables, x.dk, x.dv, x.tree) for x in (a, b)]
+    need = max(sv.sharpv_tree_attention_workspace_bytes(2, x.q.shape[0], 14, 2, 128) for x in (a, b))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    outs, graphs = [], []
+    for x, w in zip((a, b), want):
+        out = {k: torch.zeros_like(v) for k, v in w.items()}
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            sv.sharpv_tree_attention(x.q, x.kv, x.layer, *x.tables, x.dk, x.dv, x.tree, out=out, workspace=ws)
+        outs.append(out)
+        graphs.append(graph)
+    for order in ((0, 1, 0), (1, 1, 0)):
+        for i in order:
+            outs[i]["out"].zero_()
+            graphs[i].replay()
+        for i in (0, 1):
+            assert torch.equal(outs[i]["out"], want[i]["out"]) or i not in order
+            assert torch.equal(outs[i]["lse"], want[i]["lse"])
+
+
 # ------------------------------------------------------------------------------------------ eviction
 @pytest.mark.parametrize("lens,budget,sink,recent", [
     ([100], [40], 4, 16),
@@ -363,6 +449,15 @@ def test_evict_select(kind, lens, budget, sink, recent):
         mem.check("evict, short")
         assert status.item() == sv.Status.ERR_CAPACITY
         assert np.array_equal(got["kept_pos"].cpu().numpy(), kept[:-1])
+
+
+def test_evict_select_longer_than_shared_memory_holds():
+    g = np.random.default_rng(2)
+    n = 300001
+    mass = np.exp(2 * g.standard_normal(n)).astype(np.float32).round(2)
+    kept, offsets = ref.evict(mass, [0], [n], [77777], 4, 1000)
+    got = sv.sharpv_evict_select(torch.from_numpy(mass).cuda(), _i32([0]), _i32([n]), _i32([77777]), 4, 1000, 77777)
+    assert np.array_equal(got["kept_pos"].cpu().numpy(), kept) and got["kept_seq_offsets"].tolist() == [0, 77777]
 
 
 def test_evict_select_tables_outside_the_mass():
