@@ -263,7 +263,7 @@ extern "C" sharpv_status sharpv_attention_mass(
     if (layout->dtype == SHARPV_BF16) {
         const int64_t most = (int64_t)1 << 40;              // what a tensor map's strides can say
         if (a.kv_token >= most || a.kv_head >= most) return SHARPV_ERR_UNSUPPORTED;
-        return avg > kMaxRowsPath && D <= 128 ? mass_tc_launch(a, avg, sms, stream) : mass_rows_launch(a, sms, stream);
+        return avg > kMaxRowsPath && D <= 128 ? mass_tc_launch(a, sms, stream) : mass_rows_launch(a, sms, stream);
     }
     st = avg <= 8 ? mass_by_dim<SHARPV_F32, 8>(a, sms, stream)
                                              : mass_by_dim<SHARPV_F32, 32>(a, sms, stream);

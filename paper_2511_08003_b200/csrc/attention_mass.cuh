@@ -49,6 +49,6 @@ struct KeyWalk {
 // bf16 caches: kernels that write a.out.  Few query rows a (sequence, KV head), any head_dim; many of them, head_dim of at
 // most 128.
 sharpv_status mass_rows_launch(MassArgs& a, int sms, cudaStream_t stream);
-sharpv_status mass_tc_launch(MassArgs& a, int64_t avg_rows, int sms, cudaStream_t stream);
+sharpv_status mass_tc_launch(MassArgs& a, int sms, cudaStream_t stream);
 
 }  // namespace sharpv

@@ -86,7 +86,7 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
     auto& sm = *reinterpret_cast<Shared<DP>*>(smem_raw);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int D = a.head_dim, G = a.split.group, H = a.split.heads, HQ = H * G;
-    const KeySplit split{kKeys};
+    const KeySplit split{kKeys, G, a.weight != nullptr};
     if (threadIdx.x == 0) {
         for (int i = 0; i < kPairs * C::kStages; ++i) {
             mbar_init(&sm.full[0][i], 1);
@@ -209,6 +209,16 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
                 const int h0 = hp * ps.heads, hn = min(H - h0, ps.heads);
                 if (hp > 0) consumer_sync();
                 constexpr int CH = DP / 8;
+                for (int h = 0; h < hn; ++h)            // log-sum-exps first, then the query rows, all on their way at the same time
+                    for (int r = tid; r < blocks * 8; r += kWarps * 32) {
+                        if (r < rows) {
+                            const int k = (row0 + r) / G, g = row0 + r - k * G;
+                            const int64_t node = s.node0 + (a.weight == nullptr ? k : sm.list[k - k0]);
+                            cp_async4(&lse2[h * ps.rows + r], a.lse + node * HQ + (h0 + h) * G + g);
+                        } else {
+                            lse2[h * ps.rows + r] = 0.f;
+                        }
+                    }
                 for (int h = 0; h < hn; ++h) {
                     for (int r = tid / CH; r < blocks * 8; r += kWarps * 32 / CH) {
                         const int c = tid % CH;
@@ -217,18 +227,14 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
                         cp_async16(sm.query + (size_t)(h * ps.rows + r) * C::kPitch + c * 16,
                                    there ? a.q + at + (int64_t)(h0 + h) * G * D * 2 + c * 16 : a.q, there);
                     }
-                    for (int r = tid; r < blocks * 8; r += kWarps * 32) {
-                        float ls = 0.f;
-                        if (r < rows) {
-                            const int k = (row0 + r) / G, g = row0 + r - k * G;
-                            const int64_t node = s.node0 + (a.weight == nullptr ? k : sm.list[k - k0]);
-                            ls = __ldg(a.lse + node * HQ + (h0 + h) * G + g);
-                            if (ls == neg_inf()) sm.unseen = 1;
-                        }
-                        lse2[h * ps.rows + r] = ls * kLog2e;
-                    }
                 }
                 cp_async_wait_all();
+                for (int h = 0; h < hn; ++h)
+                    for (int r = tid; r < blocks * 8; r += kWarps * 32) {       // the thread's own
+                        const float ls = lse2[h * ps.rows + r];
+                        if (ls == neg_inf()) sm.unseen = 1;
+                        lse2[h * ps.rows + r] = ls * kLog2e;
+                    }
                 consumer_sync();
                 if (sm.unseen) {
                     // rows that saw nothing add nothing, whatever their queries hold: a zero row under a log-sum-exp of +inf

@@ -16,24 +16,34 @@ namespace {
 
 constexpr int kKeys = 128;
 constexpr int kWeighWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kThreads = 320, kWeighThreads = 256;
-constexpr int kStages = 3;
-constexpr int kRowsMax = 480;           // query rows in shared memory, all heads of a pass together
+constexpr int kStages = 5;              // of the ring: 64 columns of a key tile each, 16 KB
+constexpr int kRowsMax = 512;           // query rows in shared memory, all heads of a pass together
 constexpr int kBlock = 32;              // columns a warp weighs at a time; rows of a head are padded to it
 
+// What of a sequence's query rows is in shared memory at a time: `heads` KV heads, `rows` rows of each (a multiple of
+// kBlock).  As many heads as fit with all their rows, in even lots; if not even one does, its rows one lot after the other.
 struct Pass {
-    int heads, rows;                    // KV heads at a time, rows of each (a multiple of kBlock)
+    int heads, rows;
+    __device__ __forceinline__ Pass(int all_rows, int num_heads) {
+        const int need = max((all_rows + kBlock - 1) / kBlock, 1) * kBlock;
+        heads = need >= kRowsMax ? 1 : min(kRowsMax / need, num_heads);
+        const int lots = (num_heads + heads - 1) / heads;
+        heads = (num_heads + lots - 1) / lots;
+        rows = min(need, kRowsMax / heads / kBlock * kBlock);
+    }
 };
 
 template <int DP>
 struct Shared {
     uint8_t query[kRowsMax * DP * 2];                       // [heads][64-column halves][rows] 128 bytes, swizzled
-    uint8_t tiles[kStages][kKeys * DP * 2];
+    uint8_t tiles[kStages][kKeys * 128];
     float lse2[kRowsMax], weight[kRowsMax];                 // [heads][rows], [rows]
     int list[kRowsMax + 1];                                 // nodes of a pass that count
     float half[kKeys];                                      // sums of the second warp of every lane quarter
     uint64_t full[kStages], empty[kStages], scored[2], weighed[2], ready, taken, drain;
     int scan[kWeighWarps];
-    int rows, last;                                         // of the pass that is ready: rows of a head, whether it is a portion's last
+    int rows, room, heads, last;                            // of the pass that is ready: rows of a head, places for them, heads, whether
+                                                            // it is a portion's last
     int dead, unseen;
     uint32_t tmem;
     PlanScratch<kThreads> plan;
@@ -47,12 +57,12 @@ __device__ __forceinline__ bool counts(const MassArgs& a, int64_t node) {
 
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1)
-mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUtensorMap map, const Pass ps) {
+mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUtensorMap map) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     auto& sm = *reinterpret_cast<Shared<DP>*>(smem_raw);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tid = threadIdx.x;
     const int D = a.head_dim, G = a.split.group, H = a.split.heads, HQ = H * G;
-    const KeySplit split{kKeys};
+    const KeySplit split{kKeys, G, a.weight != nullptr};
     if (tid == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(&sm.full[i], 1);
@@ -76,7 +86,6 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
     tc_fence_after();
     const uint32_t tmem = sm.tmem;
     KeyWalk walk(plan, first, end);
-    const int head_passes = (H + ps.heads - 1) / ps.heads;
     bool alive = true;          // a wait that gave up ends the role; the others then give up as well
     auto wait = [&](uint64_t* bar, uint32_t phase) {
         if (alive && !mbar_wait(bar, phase & 1)) alive = false;
@@ -93,19 +102,20 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
                 for (int x = 0; x < walk.s.nodes; x += 32)
                     active += __popc(__ballot_sync(0xffffffffu, x + lane < walk.s.nodes && counts(a, walk.s.node0 + x + lane)));
             }
-            const int row_passes = (active * G + ps.rows - 1) / ps.rows;
+            const Pass ps(active * G, H);
+            const int row_passes = (active * G + ps.rows - 1) / ps.rows, head_passes = (H + ps.heads - 1) / ps.heads;
             if (lane == 0) {
                 for (int pass = 0; pass < row_passes * head_passes && alive; ++pass) {
                     const int h0 = pass % head_passes * ps.heads, h1 = min(H, h0 + ps.heads);
                     for (int kt = walk.kt0; kt < walk.kt1 && alive; ++kt)
-                        for (int h = h0; h < h1; ++h, ++it) {
-                            const int stage = it % kStages;
-                            if (it >= kStages && !wait(&sm.empty[stage], it / kStages - 1)) break;
-                            mbar_expect(&sm.full[stage], kKeys * DP * 2);
+                        for (int h = h0; h < h1; ++h)
 #pragma unroll
-                            for (int x = 0; x < DP / 64; ++x)
-                                tma_load(sm.tiles[stage] + x * kKeys * 128, &map, &sm.full[stage], x * 64, (int)walk.s.begin + kt * kKeys, h);
-                        }
+                            for (int x = 0; x < DP / 64; ++x, ++it) {
+                                const int stage = it % kStages;
+                                if (it >= kStages && !wait(&sm.empty[stage], it / kStages - 1)) break;
+                                mbar_expect(&sm.full[stage], kKeys * 128);
+                                tma_load(sm.tiles[stage], &map, &sm.full[stage], x * 64, (int)walk.s.begin + kt * kKeys, h);
+                            }
                 }
             }
             alive = __all_sync(0xffffffffu, alive);
@@ -121,36 +131,38 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
             uint32_t it = 0, step = 0, pass = 0;
             bool issued = false;
             while (alive && walk.next(a.seqs, split)) {
-                for (bool last = false; !last && alive;) {
-                    for (int hp = 0; hp < head_passes; ++hp, ++pass) {
-                        if (!wait(&sm.ready, pass)) break;
-                        const int rows = sm.rows, h0 = hp * ps.heads, hn = min(H - h0, ps.heads);
-                        last = sm.last != 0;
-                        mbar_arrive(&sm.taken);
-                        if (rows == 0) continue;
-                        const int cols = (rows + kBlock - 1) / kBlock * kBlock;
-                        for (int kt = walk.kt0; kt < walk.kt1 && alive; ++kt)
-                            for (int h = 0; h < hn && alive; ++h, ++it) {
-                                const int stage = it % kStages;
-                                if (!wait(&sm.full[stage], it / kStages)) break;
-                                for (int c = 0; c < cols; c += 256, ++step) {
-                                    const int w = step & 1, n = min(256, cols - c);
-                                    if (step >= 2 && !wait(&sm.weighed[w], (step >> 1) - 1)) break;
-                                    tc_fence_after();
-                                    const uint32_t kb = smem_u32(sm.tiles[stage]);
-                                    const uint32_t qb = smem_u32(sm.query) + (uint32_t)(h * (DP / 64) * ps.rows + c) * 128;
-                                    const uint32_t shape = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(n / 8) << 17 | 128u / 16 << 24;
+                for (bool last = false; !last && alive; ++pass) {
+                    if (!wait(&sm.ready, pass)) break;
+                    const int rows = sm.rows, room = sm.room, hn = sm.heads;
+                    last = sm.last != 0;
+                    mbar_arrive(&sm.taken);
+                    if (rows == 0) continue;
+                    const int cols = (rows + kBlock - 1) / kBlock * kBlock;
+                    for (int kt = walk.kt0; kt < walk.kt1 && alive; ++kt)
+                        for (int h = 0; h < hn && alive; ++h, it += DP / 64) {
 #pragma unroll
-                                    for (int ks = 0; ks < DP / 16; ++ks)
-                                        mma_ss(tmem + w * 256, smem_operand(kb + (ks >> 2) * kKeys * 128 + (ks & 3) * 32, 1024, 16),
-                                               smem_operand(qb + (ks >> 2) * ps.rows * 128 + (ks & 3) * 32, 1024, 16), shape, ks > 0);
-                                    mma_commit(&sm.scored[w]);
-                                    issued = true;
+                            for (int x = 0; x < DP / 64; ++x) wait(&sm.full[(it + x) % kStages], (it + x) / kStages);
+                            for (int c = 0; c < cols && alive; c += 256, ++step) {
+                                const int w = step & 1, n = min(256, cols - c);
+                                if (step >= 2 && !wait(&sm.weighed[w], (step >> 1) - 1)) break;
+                                tc_fence_after();
+                                const uint32_t qb = smem_u32(sm.query) + (uint32_t)(h * (DP / 64) * room + c) * 128;
+                                const uint32_t shape = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(n / 8) << 17 | 128u / 16 << 24;
+#pragma unroll
+                                for (int x = 0; x < DP / 64; ++x) {
+                                    const uint32_t kb = smem_u32(sm.tiles[(it + x) % kStages]);
+#pragma unroll
+                                    for (int ks = 0; ks < 4; ++ks)
+                                        mma_ss(tmem + w * 256, smem_operand(kb + ks * 32, 1024, 16),
+                                               smem_operand(qb + x * room * 128 + ks * 32, 1024, 16), shape, x > 0 || ks > 0);
                                 }
-                                if (alive) mma_commit(&sm.empty[stage]);
+                                mma_commit(&sm.scored[w]);
+                                issued = true;
                             }
-                        if (!alive) break;
-                    }
+                            if (!alive) break;
+#pragma unroll
+                            for (int x = 0; x < DP / 64; ++x) mma_commit(&sm.empty[(it + x) % kStages]);
+                        }
                 }
             }
             if (!alive && issued) {
@@ -165,6 +177,17 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
         uint32_t step = 0, pass = 0;
         while (walk.next(a.seqs, split)) {
             const SeqInfo& s = walk.s;
+            // the nodes that count: how many, and what that leaves of the rows in shared memory at a time
+            int seen = 0;
+            if (a.weight == nullptr) {
+                seen = s.nodes;
+            } else {
+                for (int x = lane; x < s.nodes; x += 32) seen += counts(a, s.node0 + x);
+                seen = warp_sum_int(seen);
+            }
+            const int all_rows = seen * G;
+            const Pass ps(all_rows, H);
+            const int head_passes = (H + ps.heads - 1) / ps.heads;
             bool over = false;
             for (int rp = 0; !over; ++rp) {
                 const int row0 = rp * ps.rows, k0 = row0 / G;       // first row, first node of the pass (of those that count)
@@ -173,33 +196,43 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
                     alive = false;
                     break;
                 }
-                int seen = 0;
-                if (a.weight == nullptr) {
-                    seen = s.nodes;
-                } else {
+                if (a.weight != nullptr) {
+                    int before = 0;
                     for (int x0 = 0; x0 < s.nodes; x0 += kWeighThreads) {
                         const int x = x0 + tid;
                         const bool on = x < s.nodes && counts(a, s.node0 + x);
                         const uint32_t mask = __ballot_sync(0xffffffffu, on);
                         if (lane == 0) sm.scan[warp] = __popc(mask);
                         weigh_sync();
-                        int at = seen + __popc(mask & ((1u << lane) - 1u));
+                        int at = before + __popc(mask & ((1u << lane) - 1u));
 #pragma unroll
                         for (int w = 0; w < kWeighWarps; ++w) {
                             if (w < warp) at += sm.scan[w];
-                            seen += sm.scan[w];
+                            before += sm.scan[w];
                         }
                         if (on && at >= k0 && at - k0 <= kRowsMax) sm.list[at - k0] = x;
                         weigh_sync();
                     }
                 }
-                const int all_rows = seen * G;
                 over = all_rows - row0 <= ps.rows;
                 const int rows = max(0, min(ps.rows, all_rows - row0)), cols = (rows + kBlock - 1) / kBlock * kBlock;
                 for (int hp = 0; hp < head_passes; ++hp) {
                     const int h0 = hp * ps.heads, hn = min(H - h0, ps.heads);
                     if (hp > 0) weigh_sync();
                     constexpr int CH = DP / 8;
+                    // log-sum-exps and weights first, then the query rows, all on their way at the same time
+                    for (int r = tid; r < cols; r += kWeighThreads) {
+                        if (r < rows) {
+                            const int k = (row0 + r) / G, g = row0 + r - k * G;
+                            const int64_t node = s.node0 + (a.weight == nullptr ? k : sm.list[k - k0]);
+                            for (int h = 0; h < hn; ++h) cp_async4(&sm.lse2[h * ps.rows + r], a.lse + node * HQ + (h0 + h) * G + g);
+                            if (a.weight != nullptr) cp_async4(&sm.weight[r], a.weight + node);
+                            else sm.weight[r] = 1.f;
+                        } else {
+                            for (int h = 0; h < hn; ++h) sm.lse2[h * ps.rows + r] = 0.f;
+                            sm.weight[r] = 0.f;
+                        }
+                    }
                     // query rows: CH threads a row, so that a row's place is found once for its chunks
                     for (int r = tid / CH; r < cols; r += kWeighThreads / CH) {
                         const int c = tid % CH;
@@ -214,24 +247,13 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
                             cp_async16(sm.query + (size_t)((h * (DP / 64) + (c >> 3)) * ps.rows) * 128 + swizzle128(r, c & 7),
                                        q + (there ? (int64_t)h * G * D * 2 : 0), there);
                     }
-                    for (int r = tid; r < cols; r += kWeighThreads) {
-                        int64_t node = 0;
-                        int g = 0;
-                        float wt = 0.f;
-                        if (r < rows) {
-                            const int k = (row0 + r) / G;
-                            g = row0 + r - k * G;
-                            node = s.node0 + (a.weight == nullptr ? k : sm.list[k - k0]);
-                            wt = a.weight == nullptr ? 1.f : __ldg(a.weight + node);
-                        }
-                        sm.weight[r] = wt;
+                    cp_async_wait_all();
+                    for (int r = tid; r < cols; r += kWeighThreads)             // the thread's own
                         for (int h = 0; h < hn; ++h) {
-                            const float ls = r < rows ? __ldg(a.lse + node * HQ + (h0 + h) * G + g) : 0.f;
+                            const float ls = sm.lse2[h * ps.rows + r];
                             if (ls == neg_inf()) sm.unseen = 1;
                             sm.lse2[h * ps.rows + r] = ls * kLog2e;
                         }
-                    }
-                    cp_async_wait_all();
                     weigh_sync();
                     if (sm.unseen) {
                         // rows that saw nothing add nothing, whatever their queries hold: a zero row under a log-sum-exp of +inf
@@ -249,7 +271,9 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
                     if (tid == 0) {
                         if (pass > 0 && !wait(&sm.taken, pass - 1)) sm.dead = 1;
                         sm.rows = rows;
-                        sm.last = over;
+                        sm.room = ps.rows;
+                        sm.heads = hn;
+                        sm.last = over && hp == head_passes - 1;
                     }
                     async_proxy_fence();
                     mbar_arrive(&sm.ready);
@@ -314,7 +338,7 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
 }
 
 template <int DP>
-sharpv_status launch(const MassArgs& a, const Pass& ps, cudaStream_t stream) {
+sharpv_status launch(const MassArgs& a, cudaStream_t stream) {
     auto kern = mass_tc_kernel<DP>;
     const size_t smem = sizeof(Shared<DP>);
     static_assert(sizeof(Shared<DP>) <= 227 * 1024, "shared memory of one CTA");
@@ -322,7 +346,7 @@ sharpv_status launch(const MassArgs& a, const Pass& ps, cudaStream_t stream) {
     if (!encode_rows_map(&map, a.cache_k, a.head_dim, a.seqs.cache_tokens, a.kv_token, a.split.heads, a.kv_head, kKeys))
         return SHARPV_ERR_CUDA;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
-        launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kThreads), smem, stream, a, map, ps) != cudaSuccess) {
+        launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kThreads), smem, stream, a, map) != cudaSuccess) {
         (void)cudaGetLastError();
         return SHARPV_ERR_CUDA;
     }
@@ -331,17 +355,9 @@ sharpv_status launch(const MassArgs& a, const Pass& ps, cudaStream_t stream) {
 
 }  // namespace
 
-sharpv_status mass_tc_launch(MassArgs& a, int64_t avg_rows, int sms, cudaStream_t stream) {
+sharpv_status mass_tc_launch(MassArgs& a, int sms, cudaStream_t stream) {
     a.ctas = sms;
-    // As many heads at a time as leave room for half as many rows again as the average (half of it where nodes have
-    // weights: part of them, usually most, count for nothing); sequences that have more rows are gone through again.
-    const int64_t room = a.weight == nullptr ? avg_rows + avg_rows / 2 : avg_rows / 2;
-    const int64_t want = (room + kBlock - 1) / kBlock * kBlock;
-    Pass ps;
-    ps.heads = (int)(want >= kRowsMax ? 1 : kRowsMax / want);
-    if (ps.heads > a.split.heads) ps.heads = a.split.heads;
-    ps.rows = kRowsMax / ps.heads / kBlock * kBlock;
-    return a.head_dim <= 64 ? launch<64>(a, ps, stream) : launch<128>(a, ps, stream);
+    return a.head_dim <= 64 ? launch<64>(a, stream) : launch<128>(a, stream);
 }
 
 }  // namespace sharpv

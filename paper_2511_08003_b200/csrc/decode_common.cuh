@@ -46,10 +46,17 @@ __device__ __forceinline__ SeqInfo load_seq(const SeqTables& t, int b, bool& bad
 // The split of an attention call.  A segment is one (sequence, KV head, tile of `rows` query rows); a query
 // row is a (node, query head of the KV head's group) pair, nodes outermost.  A segment's keys are its cached rows
 // in tiles of `keys`, then its drafted tokens in tiles of `keys`; a unit is one such key tile of one segment,
-// numbered with the key tile innermost.  CTA c of G takes the units [c U / G, (c + 1) U / G): every CTA has the
-// same number of key tiles whatever the lengths, and the segments it shares with its neighbours are joined
-// from partial results afterwards.
+// numbered with the key tile innermost.  Units are dealt to the CTAs in one of two ways, and the segments that several
+// CTAs share are joined from partial results afterwards:
+//   pieces  every segment is cut into even pieces of a cost of at most m, one CTA each, m as small as the CTAs allow;
+//   runs    CTA c of G takes the units [c U / G, (c + 1) U / G), whose numbers differ by one at most, but many CTAs
+//           end one segment and begin the next, which costs them about kSwitch.
+// Pieces are taken where m is no more than a run's cost and that (and there are at most 32 sequences: one a lane).
+// Against runs alone, us: tree of 64 nodes over 50,432 rows 58.9 -> 57.0, ragged trees 47.1 -> 46.0, one token over 50,432
+// rows 29.3 -> 28.7, weight of ragged trees 26.3 -> 24.4; a chunk of 509 nodes over 10,944 rows keeps runs.
 struct Split {
+    static constexpr uint32_t kSwitch = 3;      // what ending one segment and beginning another costs, in tiles
+    __host__ __device__ uint32_t cost(const SeqInfo&) const { return 1; }
     int rows, keys, group, heads;
     int draft;                  // the drafted tokens' keys take part
     __host__ __device__ int row_tiles(const SeqInfo& s) const {
@@ -61,15 +68,24 @@ struct Split {
         const int n = cache_tiles(s) + (draft ? (s.nodes + keys - 1) / keys : 0);
         return n > 0 ? n : 1;
     }
-    __host__ __device__ int64_t units(const SeqInfo& s) const {
-        return s.nodes == 0 ? 0 : (int64_t)row_tiles(s) * heads * key_tiles(s);
-    }
+    __host__ __device__ int64_t segments(const SeqInfo& s) const { return (int64_t)row_tiles(s) * heads; }
+    __host__ __device__ int tiles(const SeqInfo& s) const { return key_tiles(s); }
+    __host__ __device__ int64_t units(const SeqInfo& s) const { return segments(s) * key_tiles(s); }
 };
 
-// The split of a call that gives every cached row a value: a unit is `keys` rows of one sequence.
+// The split of a call that gives every cached row a value: a unit is `keys` rows of one sequence.  Its cost goes by the
+// query rows that weigh them (a KV head's, `share` halvings for nodes that count for nothing), from the 64 on that
+// take longer than the keys' loads.
 struct KeySplit {
-    int keys;
-    __host__ __device__ int64_t units(const SeqInfo& s) const { return (s.len + keys - 1) / keys; }
+    int keys, group, share;
+    static constexpr uint32_t kSwitch = 12;
+    __host__ __device__ int64_t segments(const SeqInfo& s) const { return s.len > 0; }
+    __host__ __device__ int tiles(const SeqInfo& s) const { return (s.len + keys - 1) / keys; }
+    __host__ __device__ int64_t units(const SeqInfo& s) const { return tiles(s); }
+    __host__ __device__ uint32_t cost(const SeqInfo& s) const {
+        const int64_t rows = ((int64_t)s.nodes * group >> share) / 32;
+        return rows < 1 ? 2u : (rows > 62 ? 64u : (uint32_t)rows + 1u);
+    }
 };
 
 // 64-bit division that takes the 32-bit one where the numbers allow it (nearly always: the 64-bit one is a routine of
@@ -100,6 +116,7 @@ struct PlanStart {
     int b;
     int64_t before;             // units in front of that sequence
     int64_t units;              // of the whole call
+    int last;                   // pieces: the CTA that ends the segment; -1: runs
 };
 
 template <int NT>
@@ -114,6 +131,64 @@ template <int NT, class S>
 __device__ __forceinline__ PlanStart plan_cta(const SeqTables& t, const S& sp, int cta, int ctas,
                                               PlanScratch<NT>& sm, int64_t& first, int64_t& end, int32_t* status_word) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (t.num_seqs <= 32) {                     // a sequence a lane, every warp on its own with the same result, in 32 bits
+        bool bad = false;
+        SeqInfo s = {};
+        if (lane < t.num_seqs) s = load_seq(t, lane, bad);
+        const int64_t wide = sp.units(s);
+        if (__all_sync(0xffffffffu, wide < (1 << 20))) {
+            const uint32_t segments = (uint32_t)sp.segments(s), tiles = (uint32_t)sp.tiles(s), units = (uint32_t)wide, cost = sp.cost(s);
+            const uint32_t total = __reduce_add_sync(0xffffffffu, units), costs = __reduce_add_sync(0xffffffffu, units * cost);
+            auto pieces = [&](uint32_t m) { return segments * min(tiles, (tiles * cost + m - 1) / m); };
+            uint32_t lo = costs > (uint32_t)ctas ? (costs + ctas - 1) / ctas : 1, hi = lo + S::kSwitch;
+            const bool cut = __reduce_add_sync(0xffffffffu, pieces(hi)) <= (uint32_t)ctas;
+            while (cut && lo < hi) {
+                const uint32_t m = (lo + hi) >> 1;
+                if (__reduce_add_sync(0xffffffffu, pieces(m)) <= (uint32_t)ctas) hi = m; else lo = m + 1;
+            }
+            // the lane's sequence has the CTAs (pieces) or the units (runs) [inc - mine, inc)
+            const uint32_t mine = cut ? pieces(hi) : units;
+            uint32_t inc = mine, units_inc = units;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t n = __shfl_up_sync(0xffffffffu, inc, o), u = __shfl_up_sync(0xffffffffu, units_inc, o);
+                if (lane >= o) {
+                    inc += n;
+                    units_inc += u;
+                }
+            }
+            const uint32_t busy = total < (uint32_t)ctas ? total : ctas, each = busy ? total / busy : 0, extra = total - each * busy;
+            auto run_first = [&](uint32_t c) { return c * each + (c < extra ? c : extra); };
+            const uint32_t at = cut ? (uint32_t)cta : ((uint32_t)cta < busy ? run_first(cta) : total);
+            const uint32_t found = __ballot_sync(0xffffffffu, at >= inc - mine && at < inc);
+            const int b = found ? __ffs(found) - 1 : 0;
+            PlanStart p;
+            p.s.begin = __shfl_sync(0xffffffffu, s.begin, b);
+            p.s.len = __shfl_sync(0xffffffffu, s.len, b);
+            p.s.node0 = __shfl_sync(0xffffffffu, s.node0, b);
+            p.s.nodes = __shfl_sync(0xffffffffu, s.nodes, b);
+            p.b = b;
+            p.before = __shfl_sync(0xffffffffu, units_inc - units, b);
+            p.units = total;
+            p.last = cut ? 0 : -1;
+            first = end = total;
+            if (found && !cut) {
+                first = at;
+                end = run_first(cta + 1);
+            }
+            const uint32_t cta_first = __shfl_sync(0xffffffffu, inc - mine, b);
+            if (found && cut) {
+                const uint32_t n = (uint32_t)sp.tiles(p.s), of = min(n, (n * sp.cost(p.s) + hi - 1) / hi), local = at - cta_first;
+                const uint32_t segment = local / of, piece = local - segment * of;
+                first = p.before + segment * n + n * piece / of;
+                end = p.before + segment * n + n * (piece + 1) / of;
+                p.last = cta + (int)(of - 1 - piece);
+            }
+            if (cta == 0 && warp == 0 && bad) report(status_word, SHARPV_ERR_BOUNDS);
+            __syncthreads();                    // what was set up in front of the plan is seen
+            return p;
+        }
+    }
     const int per = (t.num_seqs + NT - 1) / NT;
     const int lo = min(t.num_seqs, (int)threadIdx.x * per), hi = min(t.num_seqs, lo + per);
     int64_t sum = 0;
@@ -153,7 +228,10 @@ __device__ __forceinline__ PlanStart plan_cta(const SeqTables& t, const S& sp, i
         sm.start.b = b;
         sm.start.before = run;
     }
-    if (threadIdx.x == 0) sm.start.units = total;
+    if (threadIdx.x == 0) {
+        sm.start.units = total;
+        sm.start.last = -1;
+    }
     if (cta == 0 && bad) report(status_word, SHARPV_ERR_BOUNDS);
     __syncthreads();
     return sm.start;
@@ -213,6 +291,9 @@ __device__ __forceinline__ void cp_async16(void* smem, const void* gmem, bool va
     const unsigned dst = (unsigned)__cvta_generic_to_shared(smem);
     const int n = valid ? 16 : 0;
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(gmem), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async4(void* smem, const void* gmem) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"((unsigned)__cvta_generic_to_shared(smem)), "l"(gmem) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }

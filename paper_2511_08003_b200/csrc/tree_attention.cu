@@ -228,7 +228,7 @@ attn_simt_kernel(const __grid_constant__ AttnArgs a) {
             }
         }
     }
-    if (threadIdx.x == 0) note_shared(a, any, part, end, plan.units);
+    if (threadIdx.x == 0) note_shared(a, any, part, end, plan);
 }
 
 // CTA (x, y) joins 8 / W rows of the x-th segment that several CTAs of the kernel before shared, W warps a row (one takes

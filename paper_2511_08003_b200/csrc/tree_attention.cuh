@@ -69,11 +69,11 @@ __device__ __forceinline__ uint32_t draft_sees(const AttnArgs& a, const SeqInfo&
 
 // What a CTA says of the segment that it shares with the CTAs behind it, by one thread: `last` is its last portion (the only
 // one that can start a segment without ending it), `any` whether it has one.
-__device__ __forceinline__ void note_shared(const AttnArgs& a, bool any, const Portion& last, int64_t end, int64_t units) {
+__device__ __forceinline__ void note_shared(const AttnArgs& a, bool any, const Portion& last, int64_t end, const PlanStart& plan) {
     SharedSegment seg = {0, 0, 0, 0, -1};
     if (any && last.kt0 == 0 && last.kt1 < last.kt_all)
         seg = SharedSegment{last.s.node0, last.s.nodes * a.split.group, last.h, last.rt,
-                            Deal(units, a.ctas).owner(end + (last.kt_all - last.kt1) - 1)};
+                            plan.last >= 0 ? plan.last : Deal(plan.units, a.ctas).owner(end + (last.kt_all - last.kt1) - 1)};
     a.shared[blockIdx.x] = seg;
 }
 

@@ -128,7 +128,7 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
                 (void)mbar_wait(&sm.full[last % C::kStages], (last / C::kStages) & 1);
             }
         }
-        if (lane == 0) note_shared(a, pn > 0, last, end, plan.units);
+        if (lane == 0) note_shared(a, pn > 0, last, end, plan);
         cp_async_wait<0>();
         return;
     }

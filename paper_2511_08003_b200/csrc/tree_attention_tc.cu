@@ -169,7 +169,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                     const int at = pn & 1;
                     last = p;
                     const bool more = walk.next(a.seqs, a.split, p);
-                    if (!more) note_shared(a, pn > 0, last, end, plan.units);
+                    if (!more) note_shared(a, pn > 0, last, end, plan);
                     if (pn >= 2 && !wait(&sm.part_empty[at], (pn >> 1) - 1)) break;
                     if (!more) p.kt1 = -1;
                     sm.poison[at] = 0;
