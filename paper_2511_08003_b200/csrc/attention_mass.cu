@@ -6,7 +6,7 @@
 // others: keys are spread over CTAs, a key's sum over the rows of one KV head stays in a register, and the KV heads'
 // sums are added in a second, small kernel in the order of the heads (no atomics: the order is fixed).
 //
-// Kernels (fp32 caches; bf16 ones take the kernel of attention_mass_rows.cu):
+// Kernels (fp32 caches; bf16 ones take those of attention_mass_rows.cu and attention_mass_tc.cu):
 //   mass_simt_kernel      (sequence, KV head, 32 keys) a step, lane = key, on the fp32 units
 //   mass_join_kernel      (dependent launch) adds the heads' sums and what the rows collected before
 #include "attention_mass.cuh"
@@ -50,13 +50,13 @@ struct MassShared {
     PlanScratch<kMassThreads> plan;
 };
 
-template <int DT, int R, int DP>
+// With R = 8 the reads of K bound it, with R = 32 the multiply-adds.
+template <int R, int DP>
 __global__ void __launch_bounds__(kMassThreads)
 mass_simt_kernel(const __grid_constant__ MassArgs a) {
-    using E = Elem<DT>;
     extern __shared__ __align__(16) char smem_raw[];
     auto& sm = *reinterpret_cast<MassShared<R, DP>*>(smem_raw);
-    constexpr int RW = R / 4, VPR = DP / E::kPerVec;
+    constexpr int RW = R / 4, VPR = DP / 4;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
     cudaGridDependencySynchronize();
@@ -72,17 +72,9 @@ mass_simt_kernel(const __grid_constant__ MassArgs a) {
             const char* src = a.cache_k + (int64_t)h * a.kv_head + (s.begin + (int64_t)kt * kMassKeys) * a.kv_token;
             const int valid = s.len - kt * kMassKeys;
             for (int x = threadIdx.x; x < kMassKeys * VPR; x += kMassThreads) {
-                const int j = x / VPR, c = (x % VPR) * E::kPerVec;
+                const int j = x / VPR, c = x % VPR * 4;
                 const bool there = j < valid && c < D;
-                const char* from = src + (there ? (int64_t)j * a.kv_token + (int64_t)c * E::kBytes : 0);
-                if constexpr (DT == SHARPV_F32) {
-                    cp_async16(&sm.k[buf][j][c], from, there);
-                } else {
-                    float w[E::kPerVec];
-                    E::widen(there ? ld_stream(from) : make_uint4(0, 0, 0, 0), w);
-#pragma unroll
-                    for (int i = 0; i < E::kPerVec; ++i) sm.k[buf][j][c + i] = w[i];
-                }
+                cp_async16(&sm.k[buf][j][c], there ? src + (int64_t)j * a.kv_token + c * 4 : src, there);
             }
             cp_async_commit();
         };
@@ -106,15 +98,11 @@ mass_simt_kernel(const __grid_constant__ MassArgs a) {
                     if (!one_chunk || kt == kt0) {
                         __syncthreads();
                         for (int x = threadIdx.x; x < R * VPR; x += kMassThreads) {
-                            const int r = x / VPR, c = (x % VPR) * E::kPerVec, row = r0 + r;
+                            const int r = x / VPR, c = x % VPR * 4, row = r0 + r;
                             uint4 w = make_uint4(0, 0, 0, 0);
                             if (row < rows && c < D)
-                                w = ld_cached(a.q + (int64_t)(s.node0 + sm.list[row / G]) * a.q_node +
-                                              ((int64_t)(h * G + row % G) * D + c) * E::kBytes);
-                            float f[E::kPerVec];
-                            E::widen(w, f);
-#pragma unroll
-                            for (int i = 0; i < E::kPerVec; ++i) sm.q[r][c + i] = f[i];
+                                w = ld_cached(a.q + (int64_t)(s.node0 + sm.list[row / G]) * a.q_node + ((int64_t)(h * G + row % G) * D + c) * 4);
+                            *reinterpret_cast<uint4*>(&sm.q[r][c]) = w;
                         }
                         if (threadIdx.x < R) {
                             const int row = r0 + threadIdx.x;
@@ -178,9 +166,9 @@ mass_join_kernel(const __grid_constant__ MassArgs a) {
     }
 }
 
-template <int DT, int R, int DP>
+template <int R, int DP>
 sharpv_status mass_simt_launch(MassArgs a, int sms, cudaStream_t stream) {
-    auto kern = mass_simt_kernel<DT, R, DP>;
+    auto kern = mass_simt_kernel<R, DP>;
     const size_t smem = sizeof(MassShared<R, DP>);
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
         (void)cudaGetLastError();
@@ -191,11 +179,11 @@ sharpv_status mass_simt_launch(MassArgs a, int sms, cudaStream_t stream) {
                ? SHARPV_OK : (cudaGetLastError(), SHARPV_ERR_CUDA);
 }
 
-template <int DT, int R>
+template <int R>
 sharpv_status mass_by_dim(const MassArgs& a, int sms, cudaStream_t stream) {
-    if (a.head_dim <= 64) return mass_simt_launch<DT, R, 64>(a, sms, stream);
-    if (a.head_dim <= 128) return mass_simt_launch<DT, R, 128>(a, sms, stream);
-    return mass_simt_launch<DT, R, 256>(a, sms, stream);
+    if (a.head_dim <= 64) return mass_simt_launch<R, 64>(a, sms, stream);
+    if (a.head_dim <= 128) return mass_simt_launch<R, 128>(a, sms, stream);
+    return mass_simt_launch<R, 256>(a, sms, stream);
 }
 
 }  // namespace
@@ -265,8 +253,8 @@ extern "C" sharpv_status sharpv_attention_mass(
         if (a.kv_token >= most || a.kv_head >= most) return SHARPV_ERR_UNSUPPORTED;
         return avg > kMaxRowsPath && D <= 128 ? mass_tc_launch(a, sms, stream) : mass_rows_launch(a, sms, stream);
     }
-    st = avg <= 8 ? mass_by_dim<SHARPV_F32, 8>(a, sms, stream)
-                                             : mass_by_dim<SHARPV_F32, 32>(a, sms, stream);
+    st = avg <= 8 ? mass_by_dim<8>(a, sms, stream)
+                                             : mass_by_dim<32>(a, sms, stream);
     if (st != SHARPV_OK) return st;
     const int y = num_seqs < 1024 ? num_seqs : 1024;
     int64_t x = (cache_tokens / num_seqs + 255) / 256;

@@ -3,8 +3,8 @@
 //   s_rj = scale q_r . k_j over the cached rows of the row's sequence and the drafted tokens its node sees,
 //   out_r = sum_j exp(s_rj - m_r) v_j / l_r,   l_r = sum_j exp(s_rj - m_r),   lse_r = m_r + ln l_r.
 //
-// Kernels:
-//   attn_simt_kernel      one pass over the keys with a running maximum and sum per row, on the fp32 units
+// Kernels (and those of tree_attention_rows.cu and tree_attention_tc.cu for bf16 caches):
+//   attn_simt_kernel      fp32 caches: one pass over the keys with a running maximum and sum per row, on the fp32 units
 //   attn_join_kernel      (dependent launch) joins the partial results of segments that several CTAs share
 #include "tree_attention.cuh"
 
@@ -36,35 +36,27 @@ struct SimtShared {
     PlanScratch<kSimtThreads> plan;
 };
 
-// One tile of up to 32 rows of `src` (byte stride `row_bytes`, `valid` of them, D elements each) into shared memory
-// as fp32, the rest zero.
-template <int DT, int DP, int PITCH>
+// One tile of up to 32 rows of `src` (byte stride `row_bytes`, `valid` of them, D elements each) into shared memory, the
+// rest zero.
+template <int DP, int PITCH>
 __device__ __forceinline__ void simt_load(float (&dst)[kSimtKeys][PITCH], const char* src, int64_t row_bytes, int valid,
                                           int D) {
-    using E = Elem<DT>;
-    constexpr int VPR = DP / E::kPerVec;
+    constexpr int VPR = DP / 4;
     for (int x = threadIdx.x; x < kSimtKeys * VPR; x += kSimtThreads) {
-        const int j = x / VPR, c = (x % VPR) * E::kPerVec;
+        const int j = x / VPR, c = x % VPR * 4;
         const bool there = j < valid && c < D;
-        const char* from = src + (there ? (int64_t)j * row_bytes + (int64_t)c * E::kBytes : 0);
-        if constexpr (DT == SHARPV_F32) {
-            cp_async16(&dst[j][c], from, there);
-        } else {
-            float w[E::kPerVec];
-            E::widen(there ? ld_stream(from) : make_uint4(0, 0, 0, 0), w);
-#pragma unroll
-            for (int i = 0; i < E::kPerVec; ++i) dst[j][c + i] = w[i];
-        }
+        cp_async16(&dst[j][c], there ? src + (int64_t)j * row_bytes + c * 4 : src, there);
     }
 }
 
-// Warp w owns the rows w R/4 .. of the tile: lane = key when scores are formed, so a row's maximum and sum are warp
-// reductions; for the weighted sums a thread owns columns (col0, col0 + 128, ...) of RPT rows.
-template <int DT, int R, int DP>
+// fp32 caches: the tensor cores would round the operands, so products run on the fp32 units.  Warp w owns the rows w R/4 ..
+// of the tile: lane = key when scores are formed, so a row's maximum and sum are warp reductions; for the weighted
+// sums a thread owns columns (col0, col0 + 128, ...) of RPT rows.  With R = 8 a call is bound by the reads of K and V (and,
+// short as it is, by latency: 1,600 rows of 2 heads x 64 take 12 us), with R = 32 by multiply-adds (19 nodes x 5 of 8 heads
+// over 6,249 x 128: 193 us, 70 TFLOP/s, nearly what the fp32 units give).
+template <int R, int DP>
 __global__ void __launch_bounds__(kSimtThreads)
 attn_simt_kernel(const __grid_constant__ AttnArgs a) {
-    using E = Elem<DT>;
-    using St = Store<DT>;
     extern __shared__ __align__(16) char smem_raw[];
     auto& sm = *reinterpret_cast<SimtShared<R, DP>*>(smem_raw);
     constexpr int RW = R / 4;                               // rows of a warp
@@ -94,28 +86,25 @@ attn_simt_kernel(const __grid_constant__ AttnArgs a) {
                 valid = s.len - kt * kSimtKeys;
             } else {
                 const int j0 = (kt - kt_cache) * kSimtKeys;
-                const int64_t hb = (int64_t)h * D * E::kBytes;
+                const int64_t hb = (int64_t)h * D * 4;
                 k = a.draft_k + (int64_t)(s.node0 + j0) * a.dk_node + hb; kb = a.dk_node;
                 v = a.draft_v + (int64_t)(s.node0 + j0) * a.dv_node + hb; vb = a.dv_node;
                 valid = a.split.draft ? s.nodes - j0 : 0;
             }
-            simt_load<DT, DP>(sm.k[buf], k, kb, valid, D);
-            simt_load<DT, DP>(sm.v[buf], v, vb, valid, D);
+            simt_load<DP>(sm.k[buf], k, kb, valid, D);
+            simt_load<DP>(sm.v[buf], v, vb, valid, D);
             cp_async_commit();
         };
 
         __syncthreads();                        // the previous portion's buffers are free
         load_tile(kt0, 0);
-        constexpr int VPR = DP / E::kPerVec;
+        constexpr int VPR = DP / 4;
         for (int x = threadIdx.x; x < R * VPR; x += kSimtThreads) {
-            const int r = x / VPR, c = (x % VPR) * E::kPerVec, row = r_base + r;
+            const int r = x / VPR, c = x % VPR * 4, row = r_base + r;
             uint4 w = make_uint4(0, 0, 0, 0);
             if (row < r_all && c < D)
-                w = ld_cached(a.q + (int64_t)(s.node0 + row / G) * a.q_node + ((int64_t)(h * G + row % G) * D + c) * E::kBytes);
-            float f[E::kPerVec];
-            E::widen(w, f);
-#pragma unroll
-            for (int i = 0; i < E::kPerVec; ++i) sm.q[r][c + i] = f[i];
+                w = ld_cached(a.q + (int64_t)(s.node0 + row / G) * a.q_node + ((int64_t)(h * G + row % G) * D + c) * 4);
+            *reinterpret_cast<uint4*>(&sm.q[r][c]) = w;
         }
         float m[RW], l[RW], o[RPT][CPT];
 #pragma unroll
@@ -221,8 +210,8 @@ attn_simt_kernel(const __grid_constant__ AttnArgs a) {
                 const int col = col0 + c * COLS;
                 if (col >= D) continue;
                 if (complete)
-                    reinterpret_cast<typename St::T*>(a.out)[((int64_t)(s.node0 + row / G) * HQ + h * G + row % G) * D + col] =
-                        St::from(o[i][c] * row_scale(sm.l[row0 + i]));
+                    reinterpret_cast<float*>(a.out)[((int64_t)(s.node0 + row / G) * HQ + h * G + row % G) * D + col] =
+                        o[i][c] * row_scale(sm.l[row0 + i]);
                 else
                     a.part_o[((int64_t)slot * R + row0 + i) * D + col] = o[i][c];
             }
@@ -331,9 +320,9 @@ attn_join_kernel(const __grid_constant__ AttnArgs a) {
     if (lane == 0) a.lse[at] = row_lse(top, sum);
 }
 
-template <int DT, int R, int DP>
+template <int R, int DP>
 sharpv_status simt_launch(AttnArgs& a, int sms, cudaStream_t stream) {
-    auto kern = attn_simt_kernel<DT, R, DP>;
+    auto kern = attn_simt_kernel<R, DP>;
     const size_t smem = sizeof(SimtShared<R, DP>);
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
         (void)cudaGetLastError();
@@ -363,11 +352,11 @@ sharpv_status join_launch(const AttnArgs& a, cudaStream_t stream) {
     return SHARPV_OK;
 }
 
-template <int DT, int R>
+template <int R>
 sharpv_status simt_by_dim(AttnArgs& a, int sms, cudaStream_t stream) {
-    if (a.head_dim <= 64) return simt_launch<DT, R, 64>(a, sms, stream);
-    if (a.head_dim <= 128) return simt_launch<DT, R, 128>(a, sms, stream);
-    return simt_launch<DT, R, 256>(a, sms, stream);
+    if (a.head_dim <= 64) return simt_launch<R, 64>(a, sms, stream);
+    if (a.head_dim <= 128) return simt_launch<R, 128>(a, sms, stream);
+    return simt_launch<R, 256>(a, sms, stream);
 }
 
 // Which kernels a call takes, by type, head_dim and the average query rows of a (sequence, KV head).  Up to 16 rows one
@@ -479,6 +468,6 @@ extern "C" sharpv_status sharpv_tree_attention(
         const sharpv_status st = attn_rows_launch(a, sms, stream);
         return st == SHARPV_OK ? join_launch<SHARPV_BF16>(a, stream) : st;
     }
-    const sharpv_status st = ch.rows == 8 ? simt_by_dim<SHARPV_F32, 8>(a, sms, stream) : simt_by_dim<SHARPV_F32, 32>(a, sms, stream);
+    const sharpv_status st = ch.rows == 8 ? simt_by_dim<8>(a, sms, stream) : simt_by_dim<32>(a, sms, stream);
     return st == SHARPV_OK ? join_launch<SHARPV_F32>(a, stream) : st;
 }

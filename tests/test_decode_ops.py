@@ -21,6 +21,11 @@ def _f64(t):
     return t.detach().double().cpu().numpy()
 
 
+def _needs_capture():
+    if sv.lib().sharpv_version() >= 200 and sv.lib_path() != sv._build.LIB_PATH:
+        pytest.skip("with the range-checking library every call is followed by a synchronise, which a capture refuses")
+
+
 class Case:
     """A cache with every row outside the sequences NaN, gaps between the sequences, nodes behind the last sequence."""
 
@@ -221,6 +226,7 @@ def test_tree_attention_tables_outside_the_cache(dtype):
 
 @pytest.mark.parametrize("nodes", [[1, 1], [20, 33], [200, 30]])
 def test_tree_attention_same_bits_again_captured_and_on_a_stream(nodes):
+    _needs_capture()
     c = Case("bf16", 2, 7, 128, [3000, 411], nodes, spare=0)
     args = (c.q, c.kv, c.layer, *c.tables, c.dk, c.dv, c.tree)
     first = sv.sharpv_tree_attention(*args)
@@ -388,6 +394,7 @@ def test_calls_on_a_stream_that_is_not_the_current_one():
 
 
 def test_two_captured_graphs_share_a_workspace_one_after_the_other():
+    _needs_capture()
     a = Case("bf16", 2, 7, 128, [2000, 33], [1, 1], spare=0)
     b = Case("bf16", 2, 7, 128, [1500, 700], [30, 41], spare=0, seed=3)
     want = [sv.sharpv_tree_attention(x.q, x.kv, x.layer, *x.tables, x.dk, x.dv, x.tree) for x in (a, b)]
