@@ -547,11 +547,14 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
     if (warp == kMmaWarp) tmem_free(tmem, kCols);
 }
 
-// Joins the parts of the segments that several CTAs shared: CTA (x, y, z) takes 32 places (lane = place) and eight groups of
-// four columns (one a warp) of the x-th.  The parts are added in the order of the CTAs, with a running maximum.
-constexpr int kJoinAhead = 12;
+// Joins the parts of the segments that several CTAs shared: CTA (x, y, z) takes 32 places (lane = place) of the x-th, each
+// warp CG groups of four columns.  The parts are added in the order of the CTAs, with a running maximum; 12 loads are
+// in flight.  CG = 1 where segments have many parts; with few, one warp takes all its columns at once (CG = 4), and
+// all CTAs are resident together: ragged trees JOIN_FIGURES.
+template <int CG>
 __global__ void __launch_bounds__(256)
 attn_tc_join_kernel(const __grid_constant__ AttnArgs a) {
+    constexpr int kAhead = 12 / CG;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G, tile_rows = a.split.rows / 2;
     const int r = blockIdx.y * 32 + lane, c4 = blockIdx.z * 8 + warp;
@@ -564,48 +567,50 @@ attn_tc_join_kernel(const __grid_constant__ AttnArgs a) {
     if (seg.last < 0 || (r & 127) >= tile_rows || row >= seg.rows) return;
     const int c1 = seg.last;
     float top = neg_inf(), sum = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = c0; i <= c1; i += kJoinAhead) {
-        float4 v[kJoinAhead];
-        float m[kJoinAhead], l[kJoinAhead];
+    float4 acc[CG];
 #pragma unroll
-        for (int x = 0; x < kJoinAhead; ++x) {
+    for (int g = 0; g < CG; ++g) acc[g] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = c0; i <= c1; i += kAhead) {
+        float4 v[kAhead][CG];
+        float m[kAhead], l[kAhead];
+#pragma unroll
+        for (int x = 0; x < kAhead; ++x) {
             const int c = i + x;
-            v[x] = make_float4(0.f, 0.f, 0.f, 0.f);
-            m[x] = neg_inf();
-            l[x] = 0.f;
-            if (c <= c1) {
-                const int64_t slot = c * 2 + (c == c0);
-                v[x] = __ldcg(reinterpret_cast<const float4*>(a.part_o) + (slot * (D / 4) + c4) * kRows + r);
-                m[x] = __ldcg(a.part_ml + slot * 2 * kRows + r);
-                l[x] = __ldcg(a.part_ml + (slot * 2 + 1) * kRows + r);
-            }
+            const int64_t slot = c * 2 + (c == c0);
+            m[x] = c <= c1 ? __ldcg(a.part_ml + slot * 2 * kRows + r) : neg_inf();
+            l[x] = c <= c1 ? __ldcg(a.part_ml + (slot * 2 + 1) * kRows + r) : 0.f;
+#pragma unroll
+            for (int g = 0; g < CG; ++g)
+                v[x][g] = c <= c1 && (c4 + g * 8) * 4 < D
+                              ? __ldcg(reinterpret_cast<const float4*>(a.part_o) + (slot * (D / 4) + c4 + g * 8) * kRows + r)
+                              : make_float4(0.f, 0.f, 0.f, 0.f);
         }
         float next_top = top;
 #pragma unroll
-        for (int x = 0; x < kJoinAhead; ++x) next_top = fmaxf(next_top, m[x]);
+        for (int x = 0; x < kAhead; ++x) next_top = fmaxf(next_top, m[x]);
         const float base = next_top == neg_inf() ? 0.f : next_top, old = ex2(top - base);
-        sum *= old;
-        acc.x *= old;
-        acc.y *= old;
-        acc.z *= old;
-        acc.w *= old;
         top = next_top;
+        sum *= old;
 #pragma unroll
-        for (int x = 0; x < kJoinAhead; ++x) {
+        for (int g = 0; g < CG; ++g) acc[g] = make_float4(acc[g].x * old, acc[g].y * old, acc[g].z * old, acc[g].w * old);
+#pragma unroll
+        for (int x = 0; x < kAhead; ++x) {
             if (i + x > c1) break;
             const float f = ex2(m[x] - base);
             sum = fmaf(f, l[x], sum);
-            acc.x = fmaf(f, v[x].x, acc.x);
-            acc.y = fmaf(f, v[x].y, acc.y);
-            acc.z = fmaf(f, v[x].z, acc.z);
-            acc.w = fmaf(f, v[x].w, acc.w);
+#pragma unroll
+            for (int g = 0; g < CG; ++g)
+                acc[g] = make_float4(fmaf(f, v[x][g].x, acc[g].x), fmaf(f, v[x][g].y, acc[g].y), fmaf(f, v[x][g].z, acc[g].z),
+                                     fmaf(f, v[x][g].w, acc[g].w));
         }
     }
     const float inv = row_scale(sum);
     const int64_t at = (int64_t)(seg.node0 + row / G) * HQ + seg.h * G + row % G;
-    *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at * D + c4 * 4) =
-        make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+#pragma unroll
+    for (int g = 0; g < CG; ++g)
+        if ((c4 + g * 8) * 4 < D)
+            *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at * D + (c4 + g * 8) * 4) =
+                make_uint2(pack_bf16(acc[g].x * inv, acc[g].y * inv), pack_bf16(acc[g].z * inv, acc[g].w * inv));
     if (c4 == 0) a.lse[at] = row_lse(top, sum);
 }
 
@@ -620,10 +625,14 @@ sharpv_status launch(const AttnArgs& a, cudaStream_t stream) {
     if (ms != SHARPV_OK) return ms;
     const int64_t all = a.seqs.total_nodes * a.split.group;
     const unsigned rows = (unsigned)(all <= a.split.rows / 2 ? all : kRows);        // places that any segment can use
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
-        launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kThreads), smem, stream, a, maps) != cudaSuccess ||
-        launch_dependent(attn_tc_join_kernel, dim3((unsigned)join_ctas(a), (rows + 31) / 32, (unsigned)(a.head_dim + 31) / 32), dim3(256), 0,
-                         stream, a) != cudaSuccess) {
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess) e = launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kThreads), smem, stream, a, maps);
+    if (e == cudaSuccess) {
+        const unsigned x = (unsigned)join_ctas(a), y = (rows + 31) / 32;
+        e = many_parts(a) ? launch_dependent(attn_tc_join_kernel<1>, dim3(x, y, (unsigned)(a.head_dim + 31) / 32), dim3(256), 0, stream, a)
+                          : launch_dependent(attn_tc_join_kernel<4>, dim3(x, y), dim3(256), 0, stream, a);
+    }
+    if (e != cudaSuccess) {
         (void)cudaGetLastError();
         return SHARPV_ERR_CUDA;
     }
