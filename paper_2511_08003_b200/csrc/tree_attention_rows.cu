@@ -82,13 +82,14 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
             if (pn >= 2 && alive) alive = __all_sync(0xffffffffu, mbar_wait(&sm.part_empty[slot], ((pn >> 1) - 1) & 1));
             if (more) {
                 const int r_base = p.rt * kRows, r_all = p.s.nodes * G;
-                for (int x = lane; x < kRows * (DP / 8); x += 32) {
-                    const int r = x / (DP / 8), c = x % (DP / 8), row = r_base + r;
-                    const bool there = row < r_all && c * 8 < D;
-                    const char* q = a.q;
-                    if (there) q += (int64_t)(p.s.node0 + row / G) * a.q_node + ((int64_t)(p.h * G + row % G) * D + c * 8) * 2;
-                    cp_async16(sm.q[slot] + r * C::kQPitch + c * 16, q, there);
-                }
+                // two lanes a row, every second chunk each
+                const int r = lane >> 1, row = r_base + r;
+                const bool there = row < r_all;
+                const int node = there ? row / G : 0, g = there ? row - node * G : 0;
+                const char* q = a.q + (int64_t)(p.s.node0 + node) * a.q_node + (int64_t)(p.h * G + g) * D * 2;
+                uint8_t* to = sm.q[slot] + r * C::kQPitch;
+#pragma unroll
+                for (int c = lane & 1; c < DP / 8; c += 2) cp_async16(to + c * 16, c * 8 < D ? q + c * 16 : q, there && c * 8 < D);
             }
             cp_async_arrive(&sm.part_full[slot]);
             if (lane == 0) {
