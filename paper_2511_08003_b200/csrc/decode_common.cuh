@@ -116,7 +116,9 @@ struct PlanStart {
     int b;
     int64_t before;             // units in front of that sequence
     int64_t units;              // of the whole call
-    int last;                   // pieces: the CTA that ends the segment; -1: runs
+    // pieces (segments >= 0): how many segments there are, the number of the CTA's if it begins one (else -1) and the CTA that
+    // ends it
+    int segments, ordinal, last;
 };
 
 template <int NT>
@@ -148,13 +150,15 @@ __device__ __forceinline__ PlanStart plan_cta(const SeqTables& t, const S& sp, i
             }
             // the lane's sequence has the CTAs (pieces) or the units (runs) [inc - mine, inc)
             const uint32_t mine = cut ? pieces(hi) : units;
-            uint32_t inc = mine, units_inc = units;
+            uint32_t inc = mine, units_inc = units, segments_inc = segments;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const uint32_t n = __shfl_up_sync(0xffffffffu, inc, o), u = __shfl_up_sync(0xffffffffu, units_inc, o);
+                const uint32_t g = __shfl_up_sync(0xffffffffu, segments_inc, o);
                 if (lane >= o) {
                     inc += n;
                     units_inc += u;
+                    segments_inc += g;
                 }
             }
             const uint32_t busy = total < (uint32_t)ctas ? total : ctas, each = busy ? total / busy : 0, extra = total - each * busy;
@@ -170,19 +174,24 @@ __device__ __forceinline__ PlanStart plan_cta(const SeqTables& t, const S& sp, i
             p.b = b;
             p.before = __shfl_sync(0xffffffffu, units_inc - units, b);
             p.units = total;
-            p.last = cut ? 0 : -1;
+            p.segments = cut ? (int)__shfl_sync(0xffffffffu, segments_inc, 31) : -1;
+            p.ordinal = p.last = -1;
             first = end = total;
             if (found && !cut) {
                 first = at;
                 end = run_first(cta + 1);
             }
             const uint32_t cta_first = __shfl_sync(0xffffffffu, inc - mine, b);
+            const uint32_t segments_before = __shfl_sync(0xffffffffu, segments_inc - segments, b);
             if (found && cut) {
                 const uint32_t n = (uint32_t)sp.tiles(p.s), of = min(n, (n * sp.cost(p.s) + hi - 1) / hi), local = at - cta_first;
                 const uint32_t segment = local / of, piece = local - segment * of;
                 first = p.before + segment * n + n * piece / of;
                 end = p.before + segment * n + n * (piece + 1) / of;
-                p.last = cta + (int)(of - 1 - piece);
+                if (piece == 0) {
+                    p.ordinal = (int)(segments_before + segment);
+                    p.last = cta + (int)of - 1;
+                }
             }
             if (cta == 0 && warp == 0 && bad) report(status_word, SHARPV_ERR_BOUNDS);
             __syncthreads();                    // what was set up in front of the plan is seen
@@ -230,7 +239,7 @@ __device__ __forceinline__ PlanStart plan_cta(const SeqTables& t, const S& sp, i
     }
     if (threadIdx.x == 0) {
         sm.start.units = total;
-        sm.start.last = -1;
+        sm.start.segments = sm.start.ordinal = sm.start.last = -1;
     }
     if (cta == 0 && bad) report(status_word, SHARPV_ERR_BOUNDS);
     __syncthreads();
@@ -279,11 +288,15 @@ struct Walk {
 // first key tile, else slot 0.  A CTA has at most one of each.
 __device__ __forceinline__ int portion_slot(int cta, int first_key_tile) { return cta * 2 + (first_key_tile == 0); }
 
-// The segment whose first units CTA c has and whose last ones it has not (at most one): the CTAs c .. last hold its parts.
+// A segment whose first units CTA `first` has and whose last ones it has not (at most one a CTA): the CTAs first .. last hold
+// its parts.  Noted at the segment's number where segments are cut into pieces, else at the CTA's.
 struct SharedSegment {
     int node0, rows;                    // first node of the sequence, its query rows
     int h, rt;
-    int last;                           // -1: there is none
+    int first, last;                    // last -1: there is none
+};
+struct SharedHead {
+    int pieces, segments;               // whether the notes go by segment, and how many there are
 };
 
 // 16 bytes from global to shared memory without passing registers; zeros where `valid` is false

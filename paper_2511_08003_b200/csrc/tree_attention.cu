@@ -223,7 +223,8 @@ attn_simt_kernel(const __grid_constant__ AttnArgs a) {
 // CTA (x, y) joins 8 / W rows of the x-th segment that several CTAs of the kernel before shared, W warps a row (one takes
 // every W-th part): the parts' running maxima and sums are brought to the common maximum, the weighted sums
 // added in a fixed order (results do not depend on scheduling), divided, rounded once.  What bounds it is the latency
-// of a few dependent reads, hence eight parts' loads in flight a warp, and W = 8 where a segment may have many parts.
+// of dependent reads, hence all loads of 8 W parts in flight together (one token over 50,432 rows 28.6 -> 26.4 us, with
+// the notes found by segment), and W = 8 where a segment may have many parts.
 // With few parts a segment one warp a row keeps all CTAs resident at once: 16 sequences of one token 36 us a call with eight,
 // 27 with one.
 constexpr int kJoinAhead = 8;
@@ -237,57 +238,60 @@ attn_join_kernel(const __grid_constant__ AttnArgs a) {
     const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G, R = a.split.rows;
     const int r = blockIdx.y * (8 / W) + warp / W, w = warp % W;
     cudaGridDependencySynchronize();
-    const int c0 = find_shared(a, blockIdx.x);
-    if (c0 < 0) return;
-    const SharedSegment seg = a.shared[c0];
+    SharedSegment seg;
+    if (!find_shared(a, blockIdx.x, seg)) return;
     const int row = seg.rt * R + r;
-    if (seg.last < 0 || row >= seg.rows) return;            // with W = 8 the whole CTA, else a warp of its own
-    const int c1 = seg.last;
-    float top = neg_inf();
-    for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, __ldcg(a.part_ml + (int64_t)(c * 2 + (c == c0)) * 2 * R + r));
+    if (row >= seg.rows) return;                            // with W = 8 the whole CTA, else a warp of its own
+    const int n = seg.last - seg.first + 1;                 // parts
+    auto slot = [&](int p) { return (int64_t)((seg.first + p) * 2 + (p == 0)); };
+    auto load = [&](int p, int k) {
+        const int col = k * 128 + lane * 4;
+        return p < n && col < D ? __ldcg(reinterpret_cast<const float4*>(a.part_o + (slot(p) * R + r) * D + col))
+                                : make_float4(0.f, 0.f, 0.f, 0.f);
+    };
+    // everything that is read for up to 64 parts is on its way before any of it is used
+    float m[2], l[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int p = k * 32 + lane;
+        m[k] = p < n ? __ldcg(a.part_ml + slot(p) * 2 * R + r) : neg_inf();
+        l[k] = p < n ? __ldcg(a.part_ml + (slot(p) * 2 + 1) * R + r) : 0.f;
+    }
+    float4 v[kJoinAhead][KD];
+#pragma unroll
+    for (int x = 0; x < kJoinAhead; ++x)
+#pragma unroll
+        for (int k = 0; k < KD; ++k) v[x][k] = k * 128 < D ? load(w + x * W, k) : make_float4(0.f, 0.f, 0.f, 0.f);
+    float top = fmaxf(m[0], m[1]);
+    for (int p = 64 + lane; p < n; p += 32) top = fmaxf(top, __ldcg(a.part_ml + slot(p) * 2 * R + r));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float base = top == neg_inf() ? 0.f : top;
-    float sum = 0.f;
+    const float f[2] = {exp2f(m[0] - base), exp2f(m[1] - base)};
+    float sum = l[0] * f[0] + l[1] * f[1];
+    for (int p = 64 + lane; p < n; p += 32)
+        sum = fmaf(__ldcg(a.part_ml + (slot(p) * 2 + 1) * R + r), exp2f(__ldcg(a.part_ml + slot(p) * 2 * R + r) - base), sum);
+    sum = warp_sum(sum);                        // every warp of a row has all of it
     float4 acc[KD];
 #pragma unroll
     for (int k = 0; k < KD; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c = c0; c <= c1; c += 32) {
-        float f = 0.f;
-        if (c + lane <= c1) {
-            const float* ml = a.part_ml + (int64_t)((c + lane) * 2 + (c + lane == c0)) * 2 * R + r;
-            f = exp2f(__ldcg(ml) - base);
-            sum += __ldcg(ml + R) * f;
-        }
-        const int n = min(32, c1 - c + 1);
-        for (int i = w; i < n; i += kJoinAhead * W) {
+    auto add = [&](float fp, const float4& y, float4& to) {
+        to = make_float4(fmaf(fp, y.x, to.x), fmaf(fp, y.y, to.y), fmaf(fp, y.z, to.z), fmaf(fp, y.w, to.w));
+    };
 #pragma unroll
-            for (int k = 0; k < KD; ++k) {
-                const int col = k * 128 + lane * 4;
-                if (k * 128 >= D) break;
-                float4 v[kJoinAhead];
+    for (int x = 0; x < kJoinAhead; ++x) {
+        const int p = w + x * W;                // under 64
+        const float fp = __shfl_sync(0xffffffffu, x * W < 32 ? f[0] : f[1], p & 31);
+        if (p < n) {
 #pragma unroll
-                for (int x = 0; x < kJoinAhead; ++x) {
-                    const int y = i + x * W;
-                    v[x] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (y < n && col < D)
-                        v[x] = __ldcg(reinterpret_cast<const float4*>(a.part_o + ((int64_t)((c + y) * 2 + (c + y == c0)) * R + r) * D + col));
-                }
-#pragma unroll
-                for (int x = 0; x < kJoinAhead; ++x) {
-                    const int y = i + x * W;
-                    const float fx = __shfl_sync(0xffffffffu, f, y & 31);
-                    if (y < n) {
-                        acc[k].x = fmaf(fx, v[x].x, acc[k].x);
-                        acc[k].y = fmaf(fx, v[x].y, acc[k].y);
-                        acc[k].z = fmaf(fx, v[x].z, acc[k].z);
-                        acc[k].w = fmaf(fx, v[x].w, acc[k].w);
-                    }
-                }
-            }
+            for (int k = 0; k < KD; ++k) add(fp, v[x][k], acc[k]);
         }
     }
-    sum = warp_sum(sum);                    // every warp of a row has all of it
+    for (int p = w + kJoinAhead * W; p < n; p += W) {
+        const float fp = exp2f(__ldcg(a.part_ml + slot(p) * 2 * R + r) - base);
+#pragma unroll
+        for (int k = 0; k < KD; ++k) add(fp, load(p, k), acc[k]);
+    }
     if constexpr (W > 1) {
 #pragma unroll
         for (int k = 0; k < KD; ++k) part[w][k][lane] = acc[k];
@@ -295,13 +299,7 @@ attn_join_kernel(const __grid_constant__ AttnArgs a) {
         if (w != 0) return;
         for (int y = 1; y < W; ++y) {
 #pragma unroll
-            for (int k = 0; k < KD; ++k) {
-                const float4 v = part[y][k][lane];
-                acc[k].x += v.x;
-                acc[k].y += v.y;
-                acc[k].z += v.z;
-                acc[k].w += v.w;
-            }
+            for (int k = 0; k < KD; ++k) add(1.f, part[y][k][lane], acc[k]);
         }
     }
     const float inv = row_scale(sum);
@@ -382,7 +380,7 @@ int64_t average_rows(int32_t num_seqs, int64_t total_nodes, int64_t group) {
 }
 
 // the parts of the workspace
-size_t shared_bytes() { return align_up(kMaxAttnCtas * sizeof(SharedSegment), 256); }
+size_t shared_bytes() { return 256 + align_up(kMaxAttnCtas * sizeof(SharedSegment), 256); }
 size_t part_ml_bytes(const Choice& c) { return align_up((size_t)c.max_ctas * 2 * 2 * c.places * 4, 256); }
 size_t part_o_bytes(const Choice& c, int32_t head_dim) { return align_up((size_t)c.max_ctas * 2 * c.places * head_dim * 4, 256); }
 
@@ -455,7 +453,8 @@ extern "C" sharpv_status sharpv_tree_attention(
     const int64_t segments = (total_nodes * group / ch.rows + num_seqs) * H;     // rounding a sequence's last tile up adds one at most
     a.max_segments = (int)(segments < kMaxAttnCtas ? segments : kMaxAttnCtas);
     char* ws = (char*)workspace;
-    a.shared = (SharedSegment*)ws;
+    a.head = (SharedHead*)ws;
+    a.shared = (SharedSegment*)(ws + 256);
     a.part_ml = (float*)(ws + shared_bytes());
     a.part_o = (float*)(ws + shared_bytes() + part_ml_bytes(ch));
     a.status_word = status_word;

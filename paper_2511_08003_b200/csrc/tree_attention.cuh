@@ -28,6 +28,7 @@ struct AttnArgs {
     SeqTables seqs;
     Split split;
     // workspace
+    SharedHead* head;
     SharedSegment* shared;      // [ctas]
     float* part_ml;             // [slots][2][rows]: running maximum and sum of each row
     float* part_o;              // [slots][rows][D]: weighted sums, not yet divided
@@ -70,11 +71,14 @@ __device__ __forceinline__ uint32_t draft_sees(const AttnArgs& a, const SeqInfo&
 // What a CTA says of the segment that it shares with the CTAs behind it, by one thread: `last` is its last portion (the only
 // one that can start a segment without ending it), `any` whether it has one.
 __device__ __forceinline__ void note_shared(const AttnArgs& a, bool any, const Portion& last, int64_t end, const PlanStart& plan) {
-    SharedSegment seg = {0, 0, 0, 0, -1};
+    const bool pieces = plan.segments >= 0;
+    if (blockIdx.x == 0) *a.head = SharedHead{pieces, plan.segments};
+    SharedSegment seg = {0, 0, 0, 0, 0, -1};
     if (any && last.kt0 == 0 && last.kt1 < last.kt_all)
-        seg = SharedSegment{last.s.node0, last.s.nodes * a.split.group, last.h, last.rt,
-                            plan.last >= 0 ? plan.last : Deal(plan.units, a.ctas).owner(end + (last.kt_all - last.kt1) - 1)};
-    a.shared[blockIdx.x] = seg;
+        seg = SharedSegment{last.s.node0, last.s.nodes * a.split.group, last.h, last.rt, (int)blockIdx.x,
+                            pieces ? plan.last : Deal(plan.units, a.ctas).owner(end + (last.kt_all - last.kt1) - 1)};
+    if (!pieces) a.shared[blockIdx.x] = seg;
+    else if (plan.ordinal >= 0) a.shared[plan.ordinal] = seg;
 }
 
 // Whether segments have many parts each.  Then there are few shared segments, and a joining kernel has a CTA row for
@@ -82,9 +86,12 @@ __device__ __forceinline__ void note_shared(const AttnArgs& a, bool any, const P
 __host__ __device__ inline bool many_parts(const AttnArgs& a) { return a.ctas >= 8 * a.max_segments; }
 __host__ __device__ inline int join_ctas(const AttnArgs& a) { return many_parts(a) ? a.max_segments : a.ctas; }
 
-// The first CTA of the x-th shared segment, -1 if there are fewer.  By a whole warp.
-__device__ __forceinline__ int find_shared(const AttnArgs& a, int x) {
-    if (!many_parts(a)) return x;
+// The x-th shared segment; false if there is none.  By a whole warp.
+__device__ __forceinline__ bool find_shared(const AttnArgs& a, int x, SharedSegment& seg) {
+    const int2 head = __ldcg(reinterpret_cast<const int2*>(a.head));
+    seg = a.shared[x];
+    if (head.x) return x < head.y && seg.last >= 0;
+    if (!many_parts(a)) return seg.last >= 0;
     const int lane = threadIdx.x & 31;
     constexpr int N = (kMaxAttnCtas + 31) / 32;
     int last[N];
@@ -98,7 +105,8 @@ __device__ __forceinline__ int find_shared(const AttnArgs& a, int x) {
         if (mine) found = k * 32 + __ffs(mine) - 1;
         count += __popc(valid);
     }
-    return found;
+    if (found >= 0) seg = a.shared[found];
+    return found >= 0;
 }
 
 // out and lse of one row element from its weighted sum, running maximum (log 2 units) and sum

@@ -204,7 +204,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                     }
                 }
                 if (!alive) {
-                    a.shared[blockIdx.x].last = -1;
+                    note_shared(a, false, p, end, plan);            // nothing to join
                     for (uint32_t i = 0; i < (uint32_t)C::kStages && i < it; ++i) {     // copies in flight land first
                         const uint32_t last = it - 1 - i;
                         (void)mbar_wait(&sm.full[last % C::kStages], (last / C::kStages) & 1);
@@ -560,12 +560,10 @@ attn_tc_join_kernel(const __grid_constant__ AttnArgs a) {
     const int r = blockIdx.y * 32 + lane, c4 = blockIdx.z * 8 + warp;
     if (c4 * 4 >= D) return;
     cudaGridDependencySynchronize();
-    const int c0 = find_shared(a, blockIdx.x);
-    if (c0 < 0) return;
-    const SharedSegment seg = a.shared[c0];
-    const int row = seg.rt * a.split.rows + (r >> 7) * tile_rows + (r & 127);
-    if (seg.last < 0 || (r & 127) >= tile_rows || row >= seg.rows) return;
-    const int c1 = seg.last;
+    SharedSegment seg;
+    if (!find_shared(a, blockIdx.x, seg)) return;
+    const int row = seg.rt * a.split.rows + (r >> 7) * tile_rows + (r & 127), c0 = seg.first, c1 = seg.last;
+    if ((r & 127) >= tile_rows || row >= seg.rows) return;
     float top = neg_inf(), sum = 0.f;
     float4 acc[CG];
 #pragma unroll

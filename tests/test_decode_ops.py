@@ -165,6 +165,18 @@ def test_tree_attention_layouts_and_ranges(kind, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("H,G,D,lens,nodes", [
+    (1, 2, 256, [12007], [1]),                      # parts of one segment for every warp of a joining CTA many times over
+    (2, 1, 200, [6001, 0, 5003], [2, 3, 1]),
+    (1, 4, 128, [4000] + [3] * 30, [1] * 31),       # one sequence in many parts among whole ones
+    (1, 4, 128, [9000] + [70] * 39, [1] * 40),      # the same with more sequences than lanes
+    (1, 4, 128, [9000, 300, 0, 5], [40, 3, 0, 1]),
+])
+def test_tree_attention_segments_in_many_parts(H, G, D, lens, nodes, dtype):
+    Case(dtype, H, G, D, lens, nodes, seed=D + len(lens)).check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("nodes", [[6, 3], [90, 40]])
 @pytest.mark.parametrize("value", [NAN, float("inf"), float("-inf")])
 def test_tree_attention_ignores_what_is_not_seen(value, nodes, dtype):
