@@ -10,6 +10,8 @@
 
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 namespace sharpv {
 namespace {
 
@@ -26,13 +28,16 @@ template <> struct Store<SHARPV_BF16> {
     __device__ __forceinline__ static T from(float x) { return __float2bfloat16_rn(x); }
 };
 
+constexpr int kSimtRows = 8;            // of a warp
+
 template <int R, int DP>
 struct SimtShared {
-    float q[R][DP];
-    float k[2][kSimtKeys][DP + 4];      // 4 words of padding: lanes read 16 bytes of 32 rows without bank conflicts
+    static constexpr int kParts = 4 * kSimtRows / R;        // warps that share the rows and split a tile's keys
+    float q[R][DP + 4];                 // 4 words of padding: 16 bytes of up to 32 rows are read without bank conflicts
+    float k[2][kSimtKeys][DP + 4];      // at a portion's end also the weighted sums of warps that split keys
     float v[2][kSimtKeys][DP];
     float p[R][kSimtKeys];
-    float alpha[R], m[R], l[R];
+    float m[kParts][R], l[kParts][R];
     PlanScratch<kSimtThreads> plan;
 };
 
@@ -49,20 +54,29 @@ __device__ __forceinline__ void simt_load(float (&dst)[kSimtKeys][PITCH], const 
     }
 }
 
-// fp32 caches: the tensor cores would round the operands, so products run on the fp32 units.  Warp w owns the rows w R/4 ..
-// of the tile: lane = key when scores are formed, so a row's maximum and sum are warp reductions; for the weighted
-// sums a thread owns columns (col0, col0 + 128, ...) of RPT rows.  With R = 8 a call is bound by the reads of K and V (and,
-// short as it is, by latency: 1,600 rows of 2 heads x 64 take 12 us), with R = 32 by multiply-adds (19 nodes x 5 of 8 heads
-// over 6,249 x 128: 193 us, 70 TFLOP/s, nearly what the fp32 units give).
+__device__ __forceinline__ void simt_columns(float (&to)[4], const float* from) {
+    const float4 x = *reinterpret_cast<const float4*>(from);
+    to[0] = x.x; to[1] = x.y; to[2] = x.z; to[3] = x.w;
+}
+__device__ __forceinline__ void simt_columns(float (&to)[2], const float* from) {
+    const float2 x = *reinterpret_cast<const float2*>(from);
+    to[0] = x.x; to[1] = x.y;
+}
+
+// fp32 caches: the tensor cores would round the operands, so products run on the fp32 units.  A warp owns 8 rows: with R = 32
+// each warp others and all of a tile's keys, with R = 8 all warps the same and a quarter of the keys each (K and V then
+// leave shared memory once), joined at a portion's end.  For scores a lane forms RS rows x KS keys (so that reads of shared
+// memory keep up with the multiply-adds); for the weighted sums it owns DP / 32 columns of the 8 rows.
 template <int R, int DP>
 __global__ void __launch_bounds__(kSimtThreads)
 attn_simt_kernel(const __grid_constant__ AttnArgs a) {
     extern __shared__ __align__(16) char smem_raw[];
     auto& sm = *reinterpret_cast<SimtShared<R, DP>*>(smem_raw);
-    constexpr int RW = R / 4;                               // rows of a warp
-    constexpr int COLS = DP < 128 ? DP : 128, CPT = DP / COLS, RG = kSimtThreads / COLS, RPT = R / RG;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int col0 = threadIdx.x % COLS, row0 = threadIdx.x / COLS * RPT;
+    constexpr int RW = kSimtRows, PARTS = SimtShared<R, DP>::kParts, KW = kSimtKeys / PARTS;   // rows and keys of a warp
+    constexpr int LK = PARTS == 1 ? 16 : 8, KS = KW / LK, RS = RW * LK / 32;                    // lanes along keys; keys, rows of a lane
+    constexpr int VW = DP < 128 ? 2 : 4, NV = DP / 32 / VW;                                     // columns: NV times VW neighbours
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kl = lane % LK, rl = lane / LK;
+    const int row0 = PARTS == 1 ? warp * RW : 0, key0 = PARTS == 1 ? 0 : warp * KW;
     const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
     cudaGridDependencySynchronize();
     int64_t first, end;
@@ -106,114 +120,175 @@ attn_simt_kernel(const __grid_constant__ AttnArgs a) {
                 w = ld_cached(a.q + (int64_t)(s.node0 + row / G) * a.q_node + ((int64_t)(h * G + row % G) * D + c) * 4);
             *reinterpret_cast<uint4*>(&sm.q[r][c]) = w;
         }
-        float m[RW], l[RW], o[RPT][CPT];
+        float m[RS], l[RS], o[RW][NV][VW];
 #pragma unroll
-        for (int i = 0; i < RW; ++i) { m[i] = neg_inf(); l[i] = 0.f; }
+        for (int i = 0; i < RS; ++i) { m[i] = neg_inf(); l[i] = 0.f; }
 #pragma unroll
-        for (int i = 0; i < RPT; ++i)
+        for (int i = 0; i < RW; ++i)
 #pragma unroll
-            for (int c = 0; c < CPT; ++c) o[i][c] = 0.f;
+            for (int n = 0; n < NV; ++n)
+#pragma unroll
+                for (int c = 0; c < VW; ++c) o[i][n][c] = 0.f;
+        const bool busy = r_base + row0 < r_all;
 
         for (int kt = kt0; kt < kt1; ++kt) {
             const int buf = (kt - kt0) & 1;
-            if (kt + 1 < kt1) {
-                load_tile(kt + 1, buf ^ 1);
-                cp_async_wait<1>();
-            } else {
-                cp_async_wait<0>();
-            }
-            __syncthreads();
-            float acc[RW];
+            cp_async_wait<0>();
+            __syncthreads();                    // the tile is there, and nobody reads the other buffer any more
+            if (kt + 1 < kt1) load_tile(kt + 1, buf ^ 1);
+            if (!busy) continue;
+            float acc[RS][KS];
 #pragma unroll
-            for (int i = 0; i < RW; ++i) acc[i] = 0.f;
+            for (int i = 0; i < RS; ++i)
+#pragma unroll
+                for (int y = 0; y < KS; ++y) acc[i][y] = 0.f;
+#pragma unroll 4
             for (int c = 0; c < D; c += 4) {
-                const float4 k4 = *reinterpret_cast<const float4*>(&sm.k[buf][lane][c]);
+                float4 k4[KS];
 #pragma unroll
-                for (int i = 0; i < RW; ++i) {
-                    const float4 q4 = *reinterpret_cast<const float4*>(&sm.q[warp * RW + i][c]);
-                    acc[i] = fmaf(q4.x, k4.x, fmaf(q4.y, k4.y, fmaf(q4.z, k4.z, fmaf(q4.w, k4.w, acc[i]))));
+                for (int y = 0; y < KS; ++y) k4[y] = *reinterpret_cast<const float4*>(&sm.k[buf][key0 + y * LK + kl][c]);
+#pragma unroll
+                for (int i = 0; i < RS; ++i) {
+                    const float4 q4 = *reinterpret_cast<const float4*>(&sm.q[row0 + rl * RS + i][c]);
+#pragma unroll
+                    for (int y = 0; y < KS; ++y)
+                        acc[i][y] = fmaf(q4.x, k4[y].x, fmaf(q4.y, k4[y].y, fmaf(q4.z, k4[y].z, fmaf(q4.w, k4[y].w, acc[i][y]))));
                 }
             }
             const bool drafted = kt >= kt_cache;
             const int left = drafted ? 0 : s.len - kt * kSimtKeys;
+            float al[RS];
+            bool grown = false;
 #pragma unroll
-            for (int i = 0; i < RW; ++i) {
-                const int row = r_base + warp * RW + i;
-                bool sees = lane < left;
-                if (drafted) {
-                    sees = false;
-                    if (a.split.draft && row < r_all)
-                        sees = draft_sees(a, s, row / G, (kt - kt_cache) * kSimtKeys) >> lane & 1;
+            for (int i = 0; i < RS; ++i) {
+                const int r = row0 + rl * RS + i, row = r_base + r;
+                uint32_t sees = left >= 32 ? 0xffffffffu : (1u << left) - 1u;
+                if (drafted) sees = a.split.draft && row < r_all ? draft_sees(a, s, row / G, (kt - kt_cache) * kSimtKeys) : 0u;
+                float x[KS], top = m[i];
+#pragma unroll
+                for (int y = 0; y < KS; ++y) {
+                    x[y] = sees >> (key0 + y * LK + kl) & 1 ? acc[i][y] * a.scale_log2 : neg_inf();
+                    top = fmaxf(top, x[y]);
                 }
-                const float x = sees ? acc[i] * a.scale_log2 : neg_inf();
-                float top = x;
 #pragma unroll
-                for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-                top = fmaxf(top, m[i]);
-                const float p = sees ? exp2f(x - (top == neg_inf() ? 0.f : top)) : 0.f;
-                const float al = m[i] == top ? 1.f : exp2f(m[i] - top);
-                l[i] = l[i] * al + warp_sum(p);
+                for (int w = LK / 2; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+                const float base = top == neg_inf() ? 0.f : top;
+                al[i] = m[i] == top ? 1.f : exp2f(m[i] - top);
+                grown = grown || al[i] != 1.f;
+                float sum = 0.f;
+#pragma unroll
+                for (int y = 0; y < KS; ++y) {
+                    const int key = key0 + y * LK + kl;
+                    const bool seen = sees >> key & 1;
+                    const float p = seen ? exp2f(x[y] - base) : 0.f;
+                    sum += p;
+                    sm.p[r][key] = seen || !drafted ? p : -1.f;     // -1: its value row is not looked at
+                }
+                l[i] = l[i] * al[i] + sum;                          // of the lane's keys
                 m[i] = top;
-                sm.p[warp * RW + i][lane] = sees ? p : -1.f;      // -1: not seen, its value row is not looked at
-                if (lane == 0) sm.alpha[warp * RW + i] = al;
             }
-            __syncthreads();
+            __syncwarp();
+            if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
-            for (int i = 0; i < RPT; ++i) {
-                const float al = sm.alpha[row0 + i];
+                for (int i = 0; i < RW; ++i) {
+                    const float f = __shfl_sync(0xffffffffu, al[i % RS], i / RS * LK);
 #pragma unroll
-                for (int c = 0; c < CPT; ++c) o[i][c] *= al;
+                    for (int n = 0; n < NV; ++n)
+#pragma unroll
+                        for (int c = 0; c < VW; ++c) o[i][n][c] *= f;
+                }
             }
-            const bool whole = !drafted && left >= kSimtKeys;
-            for (int j = 0; j < kSimtKeys; j += 4) {
-                float v[4][CPT];
-#pragma unroll
-                for (int y = 0; y < 4; ++y)
-#pragma unroll
-                    for (int c = 0; c < CPT; ++c) v[y][c] = sm.v[buf][j + y][col0 + c * COLS];
-#pragma unroll
-                for (int i = 0; i < RPT; ++i) {
-                    const float4 p4 = *reinterpret_cast<const float4*>(&sm.p[row0 + i][j]);
-                    const float p[4] = {p4.x, p4.y, p4.z, p4.w};
+            auto weigh = [&](auto select) {
+#pragma unroll 2
+                for (int j = key0; j < key0 + KW; j += 4) {
+                    float v[4][NV][VW];
 #pragma unroll
                     for (int y = 0; y < 4; ++y)
 #pragma unroll
-                        for (int c = 0; c < CPT; ++c) {
-                            const float n = fmaf(p[y], v[y][c], o[i][c]);
-                            o[i][c] = whole || !(p[y] < 0.f) ? n : o[i][c];
-                        }
-                }
-            }
-            __syncthreads();
-        }
-        if (lane == 0) {
+                        for (int n = 0; n < NV; ++n) simt_columns(v[y][n], &sm.v[buf][j + y][n * 128 + lane * VW]);
 #pragma unroll
-            for (int i = 0; i < RW; ++i) { sm.m[warp * RW + i] = m[i]; sm.l[warp * RW + i] = l[i]; }
+                    for (int i = 0; i < RW; ++i) {
+                        const float4 p4 = *reinterpret_cast<const float4*>(&sm.p[row0 + i][j]);
+                        const float p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+                        for (int y = 0; y < 4; ++y)
+#pragma unroll
+                            for (int n = 0; n < NV; ++n)
+#pragma unroll
+                                for (int c = 0; c < VW; ++c) {
+                                    const float x = fmaf(p[y], v[y][n][c], o[i][n][c]);
+                                    o[i][n][c] = (!decltype(select)::value || !(p[y] < 0.f)) ? x : o[i][n][c];
+                                }
+                    }
+                }
+            };
+            // cached rows behind the sequence's end are zeros in shared memory; drafted ones that a row does not see are
+            // others' and may hold anything
+            if (drafted) weigh(std::true_type{}); else weigh(std::false_type{});
+            __syncwarp();
         }
-        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < RS; ++i) {
+#pragma unroll
+            for (int w = LK / 2; w > 0; w >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
+            if (kl == 0) {
+                sm.m[PARTS == 1 ? 0 : warp][row0 + rl * RS + i] = m[i];
+                sm.l[PARTS == 1 ? 0 : warp][row0 + rl * RS + i] = l[i];
+            }
+        }
         const bool complete = kt0 == 0 && kt1 == kt_all;
         const int slot = portion_slot(blockIdx.x, kt0);
-        if (!complete && threadIdx.x < R) {
-            a.part_ml[((int64_t)slot * 2) * R + threadIdx.x] = sm.m[threadIdx.x];
-            a.part_ml[((int64_t)slot * 2 + 1) * R + threadIdx.x] = sm.l[threadIdx.x];
-        }
-        if (complete && threadIdx.x < R && r_base + (int)threadIdx.x < r_all) {
-            const int row = r_base + threadIdx.x;
-            a.lse[(int64_t)(s.node0 + row / G) * HQ + h * G + row % G] = row_lse(sm.m[threadIdx.x], sm.l[threadIdx.x]);
-        }
+        auto write = [&](int r, const float (&x)[NV][VW], float top, float sum) {
+            const int row = r_base + r;
+            if (row >= r_all) return;
+            const int64_t at = (int64_t)(s.node0 + row / G) * HQ + h * G + row % G;
+            const float f = complete ? row_scale(sum) : 1.f;
+            float* to = complete ? reinterpret_cast<float*>(a.out) + at * D : a.part_o + ((int64_t)slot * R + r) * D;
 #pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-            const int row = r_base + row0 + i;
-            if (row >= r_all) continue;
-#pragma unroll
-            for (int c = 0; c < CPT; ++c) {
-                const int col = col0 + c * COLS;
+            for (int n = 0; n < NV; ++n) {
+                const int col = n * 128 + lane * VW;
                 if (col >= D) continue;
-                if (complete)
-                    reinterpret_cast<float*>(a.out)[((int64_t)(s.node0 + row / G) * HQ + h * G + row % G) * D + col] =
-                        o[i][c] * row_scale(sm.l[row0 + i]);
-                else
-                    a.part_o[((int64_t)slot * R + row0 + i) * D + col] = o[i][c];
+                if constexpr (VW == 4) *reinterpret_cast<float4*>(to + col) = make_float4(x[n][0] * f, x[n][1] * f, x[n][2] * f, x[n][3] * f);
+                else *reinterpret_cast<float2*>(to + col) = make_float2(x[n][0] * f, x[n][1] * f);
+            }
+            if (lane != 0) return;
+            if (complete) {
+                a.lse[at] = row_lse(top, sum);
+            } else {
+                a.part_ml[(int64_t)slot * 2 * R + r] = top;
+                a.part_ml[((int64_t)slot * 2 + 1) * R + r] = sum;
+            }
+        };
+        if constexpr (PARTS == 1) {
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < RW; ++i) write(row0 + i, o[i], sm.m[0][row0 + i], sm.l[0][row0 + i]);
+        } else {
+            float (*sums)[RW][DP] = reinterpret_cast<float (*)[RW][DP]>(&sm.k[0][0][0]);
+            static_assert(sizeof(float) * PARTS * RW * DP <= sizeof(sm.k), "");
+            __syncthreads();                    // K is no longer read
+#pragma unroll
+            for (int i = 0; i < RW; ++i)
+#pragma unroll
+                for (int n = 0; n < NV; ++n)
+#pragma unroll
+                    for (int c = 0; c < VW; ++c) sums[warp][i][n * 128 + lane * VW + c] = o[i][n][c];
+            __syncthreads();
+            for (int r = warp; r < RW; r += 4) {
+                float top = neg_inf(), sum = 0.f, x[NV][VW] = {};
+#pragma unroll
+                for (int w = 0; w < PARTS; ++w) top = fmaxf(top, sm.m[w][r]);
+                const float base = top == neg_inf() ? 0.f : top;
+#pragma unroll
+                for (int w = 0; w < PARTS; ++w) {
+                    const float f = exp2f(sm.m[w][r] - base);
+                    sum = fmaf(sm.l[w][r], f, sum);
+#pragma unroll
+                    for (int n = 0; n < NV; ++n)
+#pragma unroll
+                        for (int c = 0; c < VW; ++c) x[n][c] = fmaf(f, sums[w][r][n * 128 + lane * VW + c], x[n][c]);
+                }
+                write(r, x, top, sum);
             }
         }
     }
