@@ -66,9 +66,12 @@ __device__ __forceinline__ void simt_columns(float (&to)[2], const float* from) 
 // fp32 caches: the tensor cores would round the operands, so products run on the fp32 units.  A warp owns 8 rows: with R = 32
 // each warp others and all of a tile's keys, with R = 8 all warps the same and a quarter of the keys each (K and V then
 // leave shared memory once), joined at a portion's end.  For scores a lane forms RS rows x KS keys (so that reads of shared
-// memory keep up with the multiply-adds); for the weighted sums it owns DP / 32 columns of the 8 rows.
+// memory keep up with the multiply-adds); for the weighted sums it owns DP / 32 columns of the 8 rows.  What bounds it is
+// latency with the few warps that shared memory has room for (three CTAs an SM with R = 8: 63 us against 73 with two).
+// Measured: one token over 1,600 rows of 2 x 64 9.4 us, over 50,432 of 4 x 128 63 us (3.3 TB/s); a tree of 64 over 6,272 of
+// 4 x 128, 7 query heads each, 230 us (25 TFLOP/s of the fp32 units' 72); 19 nodes over 6,249 of 8 x 128, 5 each, 110 us.
 template <int R, int DP>
-__global__ void __launch_bounds__(kSimtThreads)
+__global__ void __launch_bounds__(kSimtThreads, DP > 128 ? 2 : 3)
 attn_simt_kernel(const __grid_constant__ AttnArgs a) {
     extern __shared__ __align__(16) char smem_raw[];
     auto& sm = *reinterpret_cast<SimtShared<R, DP>*>(smem_raw);
@@ -401,7 +404,7 @@ sharpv_status simt_launch(AttnArgs& a, int sms, cudaStream_t stream) {
         (void)cudaGetLastError();
         return SHARPV_ERR_CUDA;
     }
-    const int per_sm = smem * 2 <= 220 * 1024 ? 2 : 1;
+    const int per_sm = min(3, max(1, (int)(220 * 1024 / smem)));
     a.ctas = min(sms * per_sm, kMaxAttnCtas);
     if (launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kSimtThreads), smem, stream, a) != cudaSuccess) {
         (void)cudaGetLastError();
@@ -448,7 +451,7 @@ struct Choice {
 Choice choose(sharpv_dtype dtype, int head_dim, int group, int64_t avg_rows) {
     if (dtype == SHARPV_F32) return avg_rows <= 8 ? Choice{Path::simt, 8, 8, kMaxAttnCtas} : Choice{Path::simt, 32, 32, kMaxAttnCtas};
     if (head_dim <= 128 && group <= 128 && avg_rows > kMaxRowsPath) return {Path::tc, tc_rows(group), kTcPlaces, kMaxTcCtas};
-    return {Path::rows, kRowsTileRows, kRowsTileRows, kMaxAttnCtas};
+    return {Path::rows, kRowsTileRows, kRowsTileRows, kMaxRowsCtas};
 }
 int64_t average_rows(int32_t num_seqs, int64_t total_nodes, int64_t group) {
     return num_seqs > 0 ? total_nodes * group / num_seqs : 0;

@@ -7,7 +7,8 @@
 
 namespace sharpv {
 
-constexpr int kMaxAttnCtas = 2 * 160;       // resident CTAs a call may use; sizes the workspace
+constexpr int kMaxAttnCtas = 3 * 160;       // resident CTAs a call may use; sizes the workspace
+constexpr int kMaxRowsCtas = 160;           // of them the row kernel's
 constexpr int kMaxHeadDim = 256;
 
 struct AttnArgs {

