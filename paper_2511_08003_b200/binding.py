@@ -192,9 +192,22 @@ def _call(name: str, on: torch.Tensor, *args) -> int:
         return fn(*args)
 
 
-def _workspace(ws: Optional[torch.Tensor], nbytes: int, device) -> torch.Tensor:
+def _empty(shape, dtype, device, stream, result: bool = True) -> torch.Tensor:
+    """Memory that a call needs, from the pool of the stream that the call runs on: what a block of another stream's
+    pool was freed of may still be queued there, and nothing orders that before this call.  A result is also noted
+    for the caller's current stream, where it is used: freed, it goes back only behind what was queued there by then."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if result:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _workspace(ws: Optional[torch.Tensor], nbytes: int, device, stream=None) -> torch.Tensor:
     if ws is None:
-        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+        return _empty(max(nbytes, 256), torch.uint8, device, stream, result=False)
     if not ws.is_cuda or ws.dtype != torch.uint8 or not ws.is_contiguous():
         raise ValueError("workspace must be a contiguous CUDA uint8 tensor")
     return ws
@@ -233,17 +246,17 @@ def sharpv_score_frames(tokens: torch.Tensor, video_frame_offsets: torch.Tensor,
     out = dict(out) if out else {}
     n = total_frames * f
     if "importance" not in out:
-        out["importance"] = torch.empty(n, dtype=torch.float32, device=dev)
+        out["importance"] = _empty(n, torch.float32, dev, stream)
     if "ratio" not in out:
-        out["ratio"] = torch.empty(total_frames, dtype=torch.float32, device=dev)
+        out["ratio"] = _empty(total_frames, torch.float32, dev, stream)
     if "k" not in out:
-        out["k"] = torch.empty(total_frames, dtype=torch.int32, device=dev)
+        out["k"] = _empty(total_frames, torch.int32, dev, stream)
     if want_spatial and "spatial" not in out:
-        out["spatial"] = torch.empty(n, dtype=torch.float32, device=dev)
+        out["spatial"] = _empty(n, torch.float32, dev, stream)
     if want_temporal and "temporal" not in out:
-        out["temporal"] = torch.empty(n, dtype=torch.float32, device=dev)
+        out["temporal"] = _empty(n, torch.float32, dev, stream)
     nbytes = sharpv_score_frames_workspace_bytes(total_frames, f, d)
-    ws = _workspace(workspace, nbytes, dev)
+    ws = _workspace(workspace, nbytes, dev, stream)
     rc = _call("sharpv_score_frames", tokens,
         _dev(tokens, "tokens"), _dtype_code(tokens), ld, video_frame_offsets.numel() - 1,
         _dev(video_frame_offsets, "video_frame_offsets", torch.int32), total_frames, f, d, float(w),
@@ -267,20 +280,20 @@ def _select(fn_name, importance, k, K, total_frames, f, tokens, capacity, gather
     if capacity is None:
         capacity = total_frames * f
     if "kept_index" not in out:
-        out["kept_index"] = torch.empty(max(capacity, 1), dtype=torch.int32, device=dev)
+        out["kept_index"] = _empty(max(capacity, 1), torch.int32, dev, stream)
     if "kept_offsets" not in out:
-        out["kept_offsets"] = torch.empty(total_frames + 1, dtype=torch.int32, device=dev)
+        out["kept_offsets"] = _empty(total_frames + 1, torch.int32, dev, stream)
     if "num_kept" not in out:
-        out["num_kept"] = torch.empty(1, dtype=torch.int32, device=dev)
+        out["num_kept"] = _empty(1, torch.int32, dev, stream)
     tok_ptr, tok_dt, ld, d, out_tok_ptr = None, 0, 0, 0, None
     if gather:
         if tokens is None:
             raise ValueError("gather=True needs tokens")
         ld, d, tok_dt = _rows(tokens, "tokens"), tokens.shape[1], _dtype_code(tokens)
         if "tokens" not in out:
-            out["tokens"] = torch.empty((max(capacity, 1), d), dtype=tokens.dtype, device=dev)
+            out["tokens"] = _empty((max(capacity, 1), d), tokens.dtype, dev, stream)
         tok_ptr, out_tok_ptr = _dev(tokens, "tokens"), _dev(out["tokens"], "out tokens")
-    ws = _workspace(workspace, sharpv_select_tokens_workspace_bytes(total_frames, f), dev)
+    ws = _workspace(workspace, sharpv_select_tokens_workspace_bytes(total_frames, f), dev, stream)
     common = (total_frames, f, tok_ptr, tok_dt, ld, d, _dev(out["kept_index"], "kept_index", torch.int32),
               _dev(out["kept_offsets"], "kept_offsets", torch.int32), out_tok_ptr, capacity,
               _dev(out["num_kept"], "num_kept", torch.int32), ws.data_ptr(), ws.numel(),
@@ -331,7 +344,7 @@ def sharpv_prune_frames(tokens: torch.Tensor, video_frame_offsets: torch.Tensor,
     n = total_frames * f
     if capacity is None:
         capacity = n
-    new = lambda shape, dt: torch.empty(shape, dtype=dt, device=dev)
+    new = lambda shape, dt: _empty(shape, dt, dev, stream)
     out.setdefault("importance", new(n, torch.float32))
     out.setdefault("ratio", new(total_frames, torch.float32))
     out.setdefault("k", new(total_frames, torch.int32))
@@ -344,7 +357,7 @@ def sharpv_prune_frames(tokens: torch.Tensor, video_frame_offsets: torch.Tensor,
     out.setdefault("num_kept", new(1, torch.int32))
     if gather:
         out.setdefault("tokens", new((max(capacity, 1), d), tokens.dtype))
-    ws = _workspace(workspace, sharpv_prune_frames_workspace_bytes(total_frames, f, d), dev)
+    ws = _workspace(workspace, sharpv_prune_frames_workspace_bytes(total_frames, f, d), dev, stream)
     rc = _call("sharpv_prune_frames", tokens,
                _dev(tokens, "tokens"), _dtype_code(tokens), ld, video_frame_offsets.numel() - 1,
                _dev(video_frame_offsets, "video_frame_offsets", torch.int32), total_frames, f, d, float(w),
@@ -376,13 +389,13 @@ def _calibrate(fn_name, hidden, visual, seq_offsets, vis_begin, vis_count, vis_o
     if capacity is None:
         capacity = total_seq_tokens
     if "cos" not in out:
-        out["cos"] = torch.empty(max(total_visual, 1), dtype=torch.float32, device=dev)
+        out["cos"] = _empty(max(total_visual, 1), torch.float32, dev, stream)
     if "kept_pos" not in out:
-        out["kept_pos"] = torch.empty(max(capacity, 1), dtype=torch.int32, device=dev)
+        out["kept_pos"] = _empty(max(capacity, 1), torch.int32, dev, stream)
     if "kept_seq_offsets" not in out:
-        out["kept_seq_offsets"] = torch.empty(B + 1, dtype=torch.int32, device=dev)
+        out["kept_seq_offsets"] = _empty(B + 1, torch.int32, dev, stream)
     if want_mean_cos and "mean_cos" not in out:
-        out["mean_cos"] = torch.empty(B, dtype=torch.float32, device=dev)
+        out["mean_cos"] = _empty(B, torch.float32, dev, stream)
     head = (_dev(hidden, "hidden"), ldh, _dev(visual, "visual"), ldv, _dtype_code(hidden), hidden.shape[1], B,
             _dev(seq_offsets, "seq_offsets", torch.int32), _dev(vis_begin, "vis_begin", torch.int32),
             _dev(vis_count, "vis_count", torch.int32), _dev(vis_offsets, "vis_offsets", torch.int32),
@@ -391,7 +404,7 @@ def _calibrate(fn_name, hidden, visual, seq_offsets, vis_begin, vis_count, vis_o
             _dev(out["kept_seq_offsets"], "kept_seq_offsets", torch.int32), capacity)
     tail = (_dev(status_word, "status_word", torch.int32), _stream(stream))
     if fn_name == "sharpv_kv_calibrate_prune":
-        ws = _workspace(workspace, sharpv_kv_calibrate_prune_workspace_bytes(total_seq_tokens, B), dev)
+        ws = _workspace(workspace, sharpv_kv_calibrate_prune_workspace_bytes(total_seq_tokens, B), dev, stream)
         rc = _call("sharpv_kv_calibrate_prune", hidden, *head, ws.data_ptr(), ws.numel(), *tail)
     else:
         rc = _call("sharpv_kv_calibrate_prune_noalloc", hidden, *head, *tail)
@@ -464,13 +477,13 @@ def sharpv_kv_prune_layers(hidden_layers: torch.Tensor, visual: torch.Tensor, se
     total_visual = visual.shape[0]
     if capacity is None:
         capacity = total_seq_tokens
-    out = {"cos": torch.empty((n, max(total_visual, 1)), dtype=torch.float32, device=dev),
-           "kept_pos": torch.empty((n, max(capacity, 1)), dtype=torch.int32, device=dev),
-           "kept_seq_offsets": torch.empty((n, B + 1), dtype=torch.int32, device=dev)}
+    out = {"cos": _empty((n, max(total_visual, 1)), torch.float32, dev, stream),
+           "kept_pos": _empty((n, max(capacity, 1)), torch.int32, dev, stream),
+           "kept_seq_offsets": _empty((n, B + 1), torch.int32, dev, stream)}
     if want_mean_cos or mode == PRUNE_PER_LAYER:
-        out["mean_cos"] = torch.empty((n, B), dtype=torch.float32, device=dev)
+        out["mean_cos"] = _empty((n, B), torch.float32, dev, stream)
     if mode == PRUNE_PER_LAYER:
-        out["first_discard"] = torch.empty(B, dtype=torch.int32, device=dev)
+        out["first_discard"] = _empty(B, torch.int32, dev, stream)
     if total_visual == 0 or capacity == 0:
         raise ValueError("sharpv_kv_prune_layers wrapper needs total_visual > 0 and capacity > 0")
     if (kv_src is None) != (kv_dst is None):
@@ -480,7 +493,7 @@ def sharpv_kv_prune_layers(hidden_layers: torch.Tensor, visual: torch.Tensor, se
     else:
         L = kv_layers if kv_layers is not None else layer_begin + n
         sl = dl = KVLayout(L, 1, 16, _dtype_code(visual), 16, 16, 16, 16)
-    ws = _workspace(workspace, sharpv_kv_prune_layers_workspace_bytes(total_seq_tokens, B, n), dev)
+    ws = _workspace(workspace, sharpv_kv_prune_layers_workspace_bytes(total_seq_tokens, B, n), dev, stream)
     rc = _call("sharpv_kv_prune_layers", hidden_layers,
         _dev(hidden_layers, "hidden_layers"), hidden_layers.stride(0), hidden_layers.stride(1),
         _dev(visual, "visual"), ldv, _dtype_code(visual), visual.shape[1], B,
@@ -509,7 +522,7 @@ def sharpv_kv_compact_rope(kv_src: torch.Tensor, kv_dst: torch.Tensor, kept_pos:
     sl, dl = kv_layout(kv_src), kv_layout(kv_dst)
     if layer_end is None:
         layer_end = kv_src.shape[0]
-    ws = _workspace(workspace, sharpv_kv_compact_rope_workspace_bytes(capacity, rotary_dim), kv_src.device)
+    ws = _workspace(workspace, sharpv_kv_compact_rope_workspace_bytes(capacity, rotary_dim), kv_src.device, stream)
     rc = _call("sharpv_kv_compact_rope", kv_src,
         _dev(kv_src, "kv_src"), C.byref(sl), _dev(kv_dst, "kv_dst"), C.byref(dl), layer_begin, layer_end,
         _dev(kept_pos, "kept_pos", torch.int32), _dev(kept_seq_offsets, "kept_seq_offsets", torch.int32),
@@ -565,14 +578,6 @@ def _queue(stream, device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
 
-def _lend(stream, *tensors):
-    """Memory that a wrapper allocates belongs to the current stream: a call on another stream has to say that it uses it."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
-
-
 def _status(status_word, device):
     return None if status_word is None else _on(status_word, "status_word", device, _I32)
 
@@ -609,17 +614,14 @@ def sharpv_tree_attention(q: torch.Tensor, kv: torch.Tensor, layer: int, seq_beg
             raise ValueError("tree_mask must be [nodes, words]")
         words, mask = tree_mask.shape[1], _on(tree_mask, "tree_mask", dev, _I32)
     if out is None:
-        o = torch.empty_like(q, memory_format=torch.contiguous_format)
-        lse = torch.empty((N, HQ), dtype=_F32, device=dev)
+        o, lse = _empty(q.shape, dtype, dev, stream), _empty((N, HQ), _F32, dev, stream)
         out = {"out": o, "lse": lse}
         po, pl = o.data_ptr(), lse.data_ptr()
-        _lend(stream, o, lse)
     else:
         if out["out"].shape != q.shape or out["lse"].shape != q.shape[:2]:
             raise ValueError("out must be [nodes, q_heads, head_dim], lse [nodes, q_heads]")
         po, pl = _on(out["out"], "out", dev, dtype), _on(out["lse"], "lse", dev, _F32)
-    ws = _workspace(workspace, sharpv_tree_attention_workspace_bytes(B, N, HQ, H, D, lay.dtype), dev)
-    _lend(stream, ws)
+    ws = _workspace(workspace, sharpv_tree_attention_workspace_bytes(B, N, HQ, H, D, lay.dtype), dev, stream)
     rc = _call("sharpv_tree_attention", kv, q.data_ptr(), ldq, dk, ldk, dv, ldv, HQ, kv.data_ptr(), lay, layer,
                kv.shape[3], B, _on(seq_begin, "seq_begin", dev, _I32), _on(seq_len, "seq_len", dev, _I32, B),
                _on(node_offsets, "node_offsets", dev, _I32, B + 1), N, mask, words,
@@ -650,17 +652,17 @@ def sharpv_attention_mass(q: torch.Tensor, lse: torch.Tensor, kv: torch.Tensor, 
         raise ValueError("lse must be [nodes, q_heads]")
     B = seq_begin.numel()
     if out is None:
+        out = _empty(T, _F32, dev, stream)
         if stream is None:
-            out = torch.zeros(T, dtype=_F32, device=dev)
+            out.zero_()
         else:
-            with torch.cuda.stream(stream):     # the zeros have to be there before the call
-                out = torch.zeros(T, dtype=_F32, device=dev)
+            with torch.cuda.stream(stream):
+                out.zero_()
     ws, need = None, 0
     if lay.dtype != BF16:
         need = sharpv_attention_mass_workspace_bytes(T, lay.num_kv_heads, lay.dtype)
-        ws = _workspace(workspace, need, dev)
+        ws = _workspace(workspace, need, dev, stream)
         need = ws.numel()
-        _lend(stream, ws)
     rc = _call("sharpv_attention_mass", kv, q.data_ptr(), ldq, _on(lse, "lse", dev, _F32),
                None if node_weight is None else _on(node_weight, "node_weight", dev, _F32, N), HQ, kv.data_ptr(), lay,
                layer, T, B, _on(seq_begin, "seq_begin", dev, _I32), _on(seq_len, "seq_len", dev, _I32, B),
@@ -684,11 +686,9 @@ def sharpv_evict_select(mass: torch.Tensor, seq_begin: torch.Tensor, seq_len: to
     if capacity is None:
         capacity = T
     if out is None:
-        pos = torch.empty(capacity, dtype=_I32, device=dev)
-        out = {"kept_pos": pos, "kept_seq_offsets": seq_begin.new_empty(B + 1)}
+        out = {"kept_pos": _empty(capacity, _I32, dev, stream), "kept_seq_offsets": _empty(B + 1, _I32, dev, stream)}
         if want_mass:
-            out["mass"] = mass.new_empty(capacity)
-        _lend(stream, *out.values())
+            out["mass"] = _empty(capacity, _F32, dev, stream)
     kept_mass = out.get("mass")
     rc = _call("sharpv_evict_select", mass, _on(mass, "mass", dev, _F32), T, B,
                _on(seq_begin, "seq_begin", dev, _I32), _on(seq_len, "seq_len", dev, _I32, B),
