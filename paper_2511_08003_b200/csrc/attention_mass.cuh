@@ -2,6 +2,7 @@
 #pragma once
 
 #include "decode_common.cuh"
+#include "tma.cuh"
 
 namespace sharpv {
 
@@ -22,6 +23,15 @@ struct MassArgs {
     int ctas;
     int32_t* status_word;
 };
+
+// bf16 kernels: a query row's log-sum-exp in units of log 2.  Places without a row and rows that saw nothing have kNoRow and
+// are left out by selection: their product with a key that is not finite need not be 0.
+constexpr float kNoRow = 3.402823466e38f;
+__device__ __forceinline__ float lse_log2(float lse) { return lse == neg_inf() ? kNoRow : lse * kLog2e; }
+__device__ __forceinline__ float add_weight(float sum, float weight, float product, float scale_log2, float lse2) {
+    const float x = fmaf(weight, ex2(fmaf(product, scale_log2, -lse2)), sum);
+    return lse2 != kNoRow ? x : sum;
+}
 
 // units in their order; all of a portion belong to one sequence
 struct KeyWalk {

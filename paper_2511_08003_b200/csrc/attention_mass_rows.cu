@@ -43,7 +43,7 @@ struct Shared {
     int list[kRowsMax + 1];                                 // nodes of a pass that count
     int64_t row_at[kRowsMax];                               // byte offset of a query row (of head 0 of its group), -1: none
     int scan[kWarps];
-    int dead, unseen;
+    int dead;
     PlanScratch<kThreads> plan;
     __align__(16) uint8_t query[kQueryBytes];               // [heads][rows] pitch, then log-sum-exps [heads][rows], weights [rows]
 };
@@ -74,10 +74,10 @@ __device__ __forceinline__ void weigh(const uint32_t (&kf)[DP / 16][4], uint32_t
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         const float2 ls = *reinterpret_cast<const float2*>(lse2 + (nb + j) * 8), wt = *reinterpret_cast<const float2*>(weight + (nb + j) * 8);
-        sum0 = fmaf(wt.x, ex2(fmaf(c[j][0], scale_log2, -ls.x)), sum0);
-        sum0 = fmaf(wt.y, ex2(fmaf(c[j][1], scale_log2, -ls.y)), sum0);
-        sum1 = fmaf(wt.x, ex2(fmaf(c[j][2], scale_log2, -ls.x)), sum1);
-        sum1 = fmaf(wt.y, ex2(fmaf(c[j][3], scale_log2, -ls.y)), sum1);
+        sum0 = add_weight(sum0, wt.x, c[j][0], scale_log2, ls.x);
+        sum0 = add_weight(sum0, wt.y, c[j][1], scale_log2, ls.y);
+        sum1 = add_weight(sum1, wt.x, c[j][2], scale_log2, ls.x);
+        sum1 = add_weight(sum1, wt.y, c[j][3], scale_log2, ls.y);
     }
 }
 
@@ -96,7 +96,7 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
             mbar_init(&sm.empty[0][i], 2);
         }
         mbar_fence_init();
-        sm.dead = sm.unseen = 0;
+        sm.dead = 0;
     }
     if (warp == kWarps && lane == 0) tma_prefetch(&map);
     cudaGridDependencySynchronize();
@@ -219,7 +219,7 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
                             const int64_t node = s.node0 + (a.weight == nullptr ? k : sm.list[k - k0]);
                             cp_async4(&lse2[h * ps.rows + r], a.lse + node * HQ + (h0 + h) * G + g);
                         } else {
-                            lse2[h * ps.rows + r] = 0.f;
+                            lse2[h * ps.rows + r] = kNoRow;
                         }
                     }
                 for (int h = 0; h < hn; ++h) {
@@ -234,23 +234,9 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
                 cp_async_wait_all();
                 for (int h = 0; h < hn; ++h)
                     for (int r = tid; r < blocks * 8; r += kWarps * 32) {       // the thread's own
-                        const float ls = lse2[h * ps.rows + r];
-                        if (ls == neg_inf()) sm.unseen = 1;
-                        lse2[h * ps.rows + r] = ls * kLog2e;
+                        if (r < rows) lse2[h * ps.rows + r] = lse_log2(lse2[h * ps.rows + r]);
                     }
                 consumer_sync();
-                if (sm.unseen) {
-                    // rows that saw nothing add nothing, whatever their queries hold: a zero row under a log-sum-exp of +inf
-                    for (int x = tid; x < hn * blocks * 8; x += kWarps * 32) {
-                        const int r = x % (blocks * 8), h = x / (blocks * 8);
-                        if (lse2[h * ps.rows + r] != neg_inf()) continue;
-                        lse2[h * ps.rows + r] = -neg_inf();
-                        for (int c = 0; c < CH; ++c)
-                            *reinterpret_cast<uint4*>(sm.query + (size_t)(h * ps.rows + r) * C::kPitch + c * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    consumer_sync();
-                    if (tid == 0) sm.unseen = 0;
-                }
                 const bool fresh = rp == 0 && hp == 0;
                 for (int kt = walk.kt0; kt < walk.kt1; kt += kPairs) {
                     const int n = min(kPairs, walk.kt1 - kt);

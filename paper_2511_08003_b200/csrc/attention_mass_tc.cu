@@ -48,7 +48,7 @@ struct Shared {
     int scan[kWeighWarps];
     int rows, room, heads, last;                            // of the pass that is ready: rows of a head, places for them, heads, whether
                                                             // it is a portion's last
-    int dead, unseen;
+    int dead;
     uint32_t tmem;
     PlanScratch<kThreads> plan;
 };
@@ -80,7 +80,7 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
         mbar_init(&sm.taken, 1);
         mbar_init(&sm.drain, 1);
         mbar_fence_init();
-        sm.dead = sm.unseen = 0;
+        sm.dead = 0;
     }
     if (warp == kMmaWarp) tmem_alloc(&sm.tmem, 512);
     if (warp == kLoadWarp && lane == 0) tma_prefetch(&map);
@@ -233,7 +233,7 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
                             if (a.weight != nullptr) cp_async4(&sm.weight[r], a.weight + node);
                             else sm.weight[r] = 1.f;
                         } else {
-                            for (int h = 0; h < hn; ++h) sm.lse2[h * ps.rows + r] = 0.f;
+                            for (int h = 0; h < hn; ++h) sm.lse2[h * ps.rows + r] = kNoRow;
                             sm.weight[r] = 0.f;
                         }
                     }
@@ -252,26 +252,9 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
                                        q + (there ? (int64_t)h * G * D * 2 : 0), there);
                     }
                     cp_async_wait_all();
-                    for (int r = tid; r < cols; r += kWeighThreads)             // the thread's own
-                        for (int h = 0; h < hn; ++h) {
-                            const float ls = sm.lse2[h * ps.rows + r];
-                            if (ls == neg_inf()) sm.unseen = 1;
-                            sm.lse2[h * ps.rows + r] = ls * kLog2e;
-                        }
+                    for (int r = tid; r < rows; r += kWeighThreads)             // the thread's own
+                        for (int h = 0; h < hn; ++h) sm.lse2[h * ps.rows + r] = lse_log2(sm.lse2[h * ps.rows + r]);
                     weigh_sync();
-                    if (sm.unseen) {
-                        // rows that saw nothing add nothing, whatever their queries hold: a zero row under a log-sum-exp of +inf
-                        for (int x = tid; x < hn * cols; x += kWeighThreads) {
-                            const int r = x % cols, h = x / cols;
-                            if (sm.lse2[h * ps.rows + r] != neg_inf()) continue;
-                            sm.lse2[h * ps.rows + r] = -neg_inf();
-                            for (int c = 0; c < CH; ++c)
-                                *reinterpret_cast<uint4*>(sm.query + (size_t)((h * (DP / 64) + (c >> 3)) * ps.rows) * 128 +
-                                                          swizzle128(r, c & 7)) = make_uint4(0, 0, 0, 0);
-                        }
-                        weigh_sync();
-                        if (tid == 0) sm.unseen = 0;
-                    }
                     if (tid == 0) {
                         if (pass > 0 && !wait(&sm.taken, pass - 1)) sm.dead = 1;
                         sm.rows = rows;
@@ -310,10 +293,10 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
 #pragma unroll
                                         for (int k = 0; k < 8; ++k) {
                                             const float4 l4 = ls[k], w4 = wt[k];
-                                            sum[0] = fmaf(w4.x, ex2(fmaf(__uint_as_float(v[4 * k]), a.scale_log2, -l4.x)), sum[0]);
-                                            sum[1] = fmaf(w4.y, ex2(fmaf(__uint_as_float(v[4 * k + 1]), a.scale_log2, -l4.y)), sum[1]);
-                                            sum[0] = fmaf(w4.z, ex2(fmaf(__uint_as_float(v[4 * k + 2]), a.scale_log2, -l4.z)), sum[0]);
-                                            sum[1] = fmaf(w4.w, ex2(fmaf(__uint_as_float(v[4 * k + 3]), a.scale_log2, -l4.w)), sum[1]);
+                                            sum[0] = add_weight(sum[0], w4.x, __uint_as_float(v[4 * k]), a.scale_log2, l4.x);
+                                            sum[1] = add_weight(sum[1], w4.y, __uint_as_float(v[4 * k + 1]), a.scale_log2, l4.y);
+                                            sum[0] = add_weight(sum[0], w4.z, __uint_as_float(v[4 * k + 2]), a.scale_log2, l4.z);
+                                            sum[1] = add_weight(sum[1], w4.w, __uint_as_float(v[4 * k + 3]), a.scale_log2, l4.w);
                                         }
                                     }
                                     tc_fence_before();
