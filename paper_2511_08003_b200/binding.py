@@ -582,7 +582,7 @@ def _status(status_word, device):
     return None if status_word is None else _on(status_word, "status_word", device, _I32)
 
 
-@functools.lru_cache(maxsize=None)
+@functools.lru_cache(maxsize=256)       # a server's steps differ in their nodes without end
 def sharpv_tree_attention_workspace_bytes(num_seqs: int, total_nodes: int, num_q_heads: int, num_kv_heads: int,
                                           head_dim: int, dtype: int = BF16) -> int:
     return int(lib().sharpv_tree_attention_workspace_bytes(num_seqs, total_nodes, num_q_heads, num_kv_heads, head_dim,

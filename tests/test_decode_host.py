@@ -129,3 +129,9 @@ def test_wrappers_refuse_what_is_not_on_the_gpu():
         sv.sharpv_evict_select(torch.zeros(8), i, i, i)
     with pytest.raises(ValueError):
         sv.sharpv_kv_append(kv, kv.clone(), i, torch.zeros(2, dtype=torch.int32), i)
+
+
+def test_workspace_sizes_that_are_kept_stay_few(L):
+    sizes = {n: sv.sharpv_tree_attention_workspace_bytes(3, n, 28, 4, 128) for n in range(1, 3000)}
+    assert sv.sharpv_tree_attention_workspace_bytes.cache_info().currsize <= 1000
+    assert all(L.sharpv_tree_attention_workspace_bytes(3, n, 28, 4, 128, 1) == b for n, b in sizes.items())
