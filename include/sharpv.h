@@ -357,8 +357,7 @@ sharpv_status sharpv_kv_compact_rope(
  * outside the cache or the query arrays are cut to them and SHARPV_ERR_BOUNDS is written to status_word (in
  * every build).  num_q_heads is a multiple of the layout's num_kv_heads; query head x reads KV head
  * x / (num_q_heads / num_kv_heads).  SHARPV_F32 and SHARPV_BF16 caches (queries, drafted keys and values and
- * the output have the cache's type), head_dim of at most 256.  num_seqs == 0 or total_nodes == 0 is valid and
- * launches nothing.
+ * the output have the cache's type), head_dim of at most 256.  num_seqs == 0 is valid and launches nothing.
  *
  * sharpv_tree_attention: attention of a step's query nodes.  Node i of a sequence sees every cached token
  * of the sequence and those drafted tokens of the same sequence that its row of the tree mask marks:
@@ -372,8 +371,12 @@ sharpv_status sharpv_kv_compact_rope(
  *   aligned; out_lse [dev] float[total_nodes, num_q_heads].
  * out and out_lse must not overlap the inputs.
  * A row that sees nothing gives out = 0 and lse = -inf.  Keys and values that a row does not see never touch
- * its result, whatever they hold (NaN and infinities included).  Scores, the softmax's maximum and sum and the
- * weighted sums are fp32; out is rounded once.  scale > 0, finite.  Results do not depend on scheduling.
+ * its result, whatever they hold (NaN and infinities included).  Scores, the softmax's maximum and sum, the
+ * weighted sums and lse are fp32; out is rounded to the storage type.  SHARPV_BF16: the weights exp(s_j - m) are also
+ * rounded, to bf16, before they multiply the values (the sum that divides is taken of the unrounded ones), so a
+ * component of out is off by up to 2^-8 sum_j p_j |v_j| / sum_j p_j for that and 2^-8 |out| for its own rounding;
+ * SHARPV_F32 rounds nothing below fp32.  scale > 0, finite.  Results do not depend on scheduling.
+ * total_nodes == 0 is valid and launches nothing.
  * workspace [dev]: sharpv_tree_attention_workspace_bytes() bytes, 256-byte aligned, contents undefined before
  * and after; calls that may overlap on the GPU need a workspace each.
  */
@@ -398,10 +401,14 @@ sharpv_status sharpv_tree_attention(
  * tables as in sharpv_tree_attention, lse [dev] float[total_nodes, num_q_heads] as it writes it (or as any other
  * attention over at least these tokens returns it).
  * node_weight [dev] float[total_nodes] or NULL (all 1): for example 1 for accepted nodes and 0 for the others;
- *   a node of weight 0 is not looked at.  Rows whose lse is -inf (they saw nothing) add nothing.
+ *   a node of weight 0 is not looked at.  Rows whose lse is -inf (they saw nothing) add nothing.  A sequence without
+ *   nodes that count gets decay * mass, also where total_nodes == 0.
  * mass [dev] float[cache_tokens] or NULL: what the rows collected so far, row p at mass[p]; NULL and decay == 0
  *   both mean that nothing is read and the sum starts at 0.  out_mass [dev] float[cache_tokens] may be mass, but not
  *   overlap it otherwise (SHARPV_ERR_INVALID_ARG).
+ * Only cached tokens collect weight: what the tokens of one step (drafted ones, a chunk of a prompt) give each other is
+ * not counted.  A row that joins a sequence starts with what the caller has put at its place of mass (0, say), and
+ * sharpv_evict_select's `recent` is what keeps such rows until later steps have looked at them.
  * The sequences' cache rows must not overlap.  Sums are fp32 in a fixed order.
  * workspace as above, sharpv_attention_mass_workspace_bytes() bytes (0 for SHARPV_BF16 caches: may be NULL).
  */
@@ -424,8 +431,10 @@ sharpv_status sharpv_attention_mass(
  * out_kept_seq_offsets [dev] int32[num_seqs + 1]: the lists sharpv_kv_compact and sharpv_kv_append take (in
  *   place compaction needs sequences in ascending order of their rows, as seq_begin has them in a packed cache).
  * out_mass [dev] float[capacity] or NULL: mass of the kept rows, in the order of out_kept_pos (what the rows
- *   of the compacted cache have collected); must not overlap mass.
+ *   of the compacted cache have collected): entry j belongs to the row that kept_pos[j] is copied to; must not overlap
+ *   mass.
  * More survivors than `capacity`: SHARPV_ERR_CAPACITY in status_word, nothing written beyond it.
+ * num_seqs == 0: out_kept_seq_offsets[0] = 0.
  */
 sharpv_status sharpv_evict_select(
     const float* mass, int64_t cache_tokens, int32_t num_seqs, const int32_t* seq_begin, const int32_t* seq_len,

@@ -51,3 +51,23 @@ def test_attention_mass_of_rows_that_saw_nothing_over_any_keys(group, nodes, dty
     for b in range(2):
         rows = slice(int(c.begin[b]), int(c.begin[b] + c.length[b]))
         assert torch.equal(mass[rows], 0.5 * hist[rows])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_mass_without_nodes(dtype):
+    """Without nodes, or with none that counts, a row gets decay * mass; rows outside the sequences stay."""
+    c = Case(dtype, 2, 4, 128, [70, 0, 333], [0, 0, 0], spare=0, tree=None)
+    hist = torch.rand(c.kv.shape[3], device="cuda")
+    inside = torch.cat([torch.arange(b, b + n) for b, n in zip(c.begin, c.length)]).cuda()
+    want = torch.full_like(hist, -3.0)
+    want[inside] = 0.25 * hist[inside]
+    out = torch.full_like(hist, -3.0)
+    sv.sharpv_attention_mass(c.q, torch.empty((0, 8), device="cuda"), c.kv, c.layer, *c.tables, mass=hist, decay=0.25, out=out)
+    assert torch.equal(out, want)
+    for nodes in ([3, 1, 4], [90, 3, 70]):
+        c = Case(dtype, 2, 4, 128, [70, 0, 333], nodes, spare=0, tree=None)
+        lse = torch.zeros(c.q.shape[:2], device="cuda")
+        out.fill_(-3.0)
+        sv.sharpv_attention_mass(c.q, lse, c.kv, c.layer, *c.tables, mass=hist, decay=0.25, out=out,
+                                 node_weight=torch.zeros(c.q.shape[0], device="cuda"))
+        assert torch.equal(out, want)
