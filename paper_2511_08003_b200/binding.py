@@ -559,7 +559,7 @@ def _heads(t: torch.Tensor, name: str, device, dtype, n: Optional[int], heads: O
     """Row stride of a [nodes, heads, d] view whose heads lie next to each other."""
     s, st = t.shape, t.stride()
     if t.device != device or t.dtype is not dtype or len(s) != 3 or s[2] != d or (n is not None and s[0] != n) or \
-            (heads is not None and s[1] != heads) or st[2] != 1 or (st[1] != d and s[1] > 1):
+            (heads is not None and s[1] != heads) or (s[0] > 0 and (st[2] != 1 or (st[1] != d and s[1] > 1))):
         if t.device != device:
             raise ValueError(f"{name} must be on {device}")
         if t.dtype is not dtype:

@@ -135,3 +135,13 @@ def test_workspace_sizes_that_are_kept_stay_few(L):
     sizes = {n: sv.sharpv_tree_attention_workspace_bytes(3, n, 28, 4, 128) for n in range(1, 3000)}
     assert sv.sharpv_tree_attention_workspace_bytes.cache_info().currsize <= 1000
     assert all(L.sharpv_tree_attention_workspace_bytes(3, n, 28, 4, 128, 1) == b for n, b in sizes.items())
+
+
+def test_query_arrays_without_nodes_have_no_strides_that_matter():
+    cpu, f32 = torch.device("cpu"), torch.float32
+    for t in (torch.empty((5, 24, 64))[:0, 3:11], torch.empty((0, 8, 64)).transpose(0, 1).contiguous().transpose(0, 1)):
+        assert sv._heads(t, "q", cpu, f32, None, None, 64) == 8 * 64
+    with pytest.raises(ValueError):
+        sv._heads(torch.empty((0, 8, 32)), "q", cpu, f32, None, None, 64)
+    with pytest.raises(ValueError):
+        sv._heads(torch.empty((8, 5, 64)).transpose(0, 1), "q", cpu, f32, None, None, 64)
