@@ -1,6 +1,7 @@
 """Refusals of the operators that decode over a cache: nothing here needs a GPU, every call returns before any launch."""
 import ctypes as C
 
+import numpy as np
 import pytest
 import torch
 
@@ -139,7 +140,8 @@ def test_workspace_sizes_that_are_kept_stay_few(L):
 
 def test_query_arrays_without_nodes_have_no_strides_that_matter():
     cpu, f32 = torch.device("cpu"), torch.float32
-    for t in (torch.empty((5, 24, 64))[:0, 3:11], torch.empty((0, 8, 64)).transpose(0, 1).contiguous().transpose(0, 1)):
+    for t in (torch.empty((5, 24, 64))[:0, 3:11], torch.from_numpy(np.zeros((0, 8, 64), np.float32)),    # strides of 0
+              torch.empty((4, 64, 8)).transpose(1, 2)[:0]):
         assert sv._heads(t, "q", cpu, f32, None, None, 64) == 8 * 64
     with pytest.raises(ValueError):
         sv._heads(torch.empty((0, 8, 32)), "q", cpu, f32, None, None, 64)
