@@ -144,9 +144,9 @@ mass_rows_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUt
             alive = __all_sync(0xffffffffu, alive);
             if (!alive) break;
         }
-        if (!alive && lane == 0) {
-            report(a.status_word, SHARPV_ERR_TIMEOUT);
-            // copies in flight land before the CTA ends
+        if (lane == 0) {
+            if (!alive) report(a.status_word, SHARPV_ERR_TIMEOUT);
+            // copies in flight land before the CTA ends, also where the warps that wanted them gave up
 #pragma unroll
             for (int t = 0; t < kPairs; ++t)
                 for (uint32_t i = 0; i < (uint32_t)C::kStages && i < it[t]; ++i) {

@@ -124,8 +124,9 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
             }
             alive = __all_sync(0xffffffffu, alive);
         }
-        if (!alive && lane == 0) {
-            for (uint32_t i = 0; i < (uint32_t)kStages && i < it; ++i) {            // copies in flight land before the CTA ends
+        if (lane == 0) {
+            // copies in flight land before the CTA ends, also where the warps that wanted them gave up
+            for (uint32_t i = 0; i < (uint32_t)kStages && i < it; ++i) {
                 const uint32_t last = it - 1 - i;
                 (void)mbar_wait(&sm.full[last % kStages], (last / kStages) & 1);
             }
@@ -169,7 +170,7 @@ mass_tc_kernel(const __grid_constant__ MassArgs a, const __grid_constant__ CUten
                         }
                 }
             }
-            if (!alive && issued) {
+            if (issued) {
                 // the products in flight end before the tensor memory is given back
                 mma_commit(&sm.drain);
                 (void)mbar_wait(&sm.drain, 0);

@@ -82,7 +82,8 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
             const int slot = pn & 1;
             last = p;
             const bool more = walk.next(a.seqs, a.split, p);
-            if (pn >= 2 && alive) alive = __all_sync(0xffffffffu, mbar_wait(&sm.part_empty[slot], ((pn >> 1) - 1) & 1));
+            if (pn >= 2) alive = __all_sync(0xffffffffu, mbar_wait(&sm.part_empty[slot], ((pn >> 1) - 1) & 1));
+            if (!alive) break;                  // the place may still be read: the others give up on the portion that does not come
             if (more) {
                 const int r_base = p.rt * kRows, r_all = p.s.nodes * G;
                 // two lanes a row, every second chunk each
@@ -104,7 +105,7 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
             if (lane == 0) {
                 for (int kt = p.kt0; kt < p.kt1; ++kt, ++it) {
                     const int stage = it % C::kStages;
-                    if (alive && it >= C::kStages) alive = mbar_wait(&sm.empty[stage], (it / C::kStages - 1) & 1);
+                    if (it >= C::kStages) alive = mbar_wait(&sm.empty[stage], (it / C::kStages - 1) & 1);
                     if (!alive) break;
                     const bool drafted = kt >= p.kt_cache;
                     if (drafted && !a.split.draft) {            // the empty tile of rows without keys
@@ -124,15 +125,17 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Att
                 }
             }
             alive = __all_sync(0xffffffffu, alive);
+            if (!alive) break;
         }
-        if (!alive && lane == 0) {
-            report(a.status_word, SHARPV_ERR_TIMEOUT);
-            for (int i = 0; i < C::kStages && (uint32_t)i < it; ++i) {      // copies in flight land before the CTA ends
-                const uint32_t last = it - 1 - i;
-                (void)mbar_wait(&sm.full[last % C::kStages], (last / C::kStages) & 1);
+        if (lane == 0) {
+            if (!alive) report(a.status_word, SHARPV_ERR_TIMEOUT);
+            note_shared(a, alive && pn > 0, last, end, plan);
+            // copies in flight land before the CTA ends, also where the warps that wanted them gave up
+            for (int i = 0; i < C::kStages && (uint32_t)i < it; ++i) {
+                const uint32_t at = it - 1 - i;
+                (void)mbar_wait(&sm.full[at % C::kStages], (at / C::kStages) & 1);
             }
         }
-        if (lane == 0) note_shared(a, pn > 0, last, end, plan);
         cp_async_wait<0>();
         return;
     }

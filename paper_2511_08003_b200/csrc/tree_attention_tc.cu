@@ -168,7 +168,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
             if (lane == 0) {
                 Walk walk(plan, first, end);
                 Portion p, last;
-                uint32_t it = 0;
+                uint32_t it = 0, queries = 0;                       // tiles, and portions whose query rows were asked for
                 for (uint32_t pn = 0; alive; ++pn) {
                     const int at = pn & 1;
                     last = p;
@@ -184,6 +184,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                     const Steps st(p, a.split);
                     if (pn > 0 && !wait(&sm.q_empty, pn - 1)) break;
                     const int nodes = a.split.rows / (2 * G);
+                    ++queries;
                     mbar_expect(&sm.q_full, (st.pair ? 2 : 1) * (DP / 64) * (a.split.rows / 2) * 128);
                     for (int w = 0; w < (st.pair ? 2 : 1); ++w)
 #pragma unroll
@@ -207,13 +208,13 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                         }
                     }
                 }
-                if (!alive) {
-                    note_shared(a, false, p, end, plan);            // nothing to join
-                    for (uint32_t i = 0; i < (uint32_t)C::kStages && i < it; ++i) {     // copies in flight land first
-                        const uint32_t last = it - 1 - i;
-                        (void)mbar_wait(&sm.full[last % C::kStages], (last / C::kStages) & 1);
-                    }
+                if (!alive) note_shared(a, false, p, end, plan);    // nothing to join
+                // copies in flight land before the CTA ends, also where the warps that wanted them gave up
+                for (uint32_t i = 0; i < (uint32_t)C::kStages && i < it; ++i) {
+                    const uint32_t at = it - 1 - i;
+                    (void)mbar_wait(&sm.full[at % C::kStages], (at / C::kStages) & 1);
                 }
+                if (queries > 0) (void)mbar_wait(&sm.q_full, (queries - 1) & 1);
             }
         } else if (warp == kMmaWarp) {
             // The whole warp walks and waits, one thread issues.  The tensor cores queue only a few products, so what
