@@ -358,6 +358,8 @@ sharpv_status sharpv_kv_compact_rope(
  * every build).  num_q_heads is a multiple of the layout's num_kv_heads; query head x reads KV head
  * x / (num_q_heads / num_kv_heads).  SHARPV_F32 and SHARPV_BF16 caches (queries, drafted keys and values and
  * the output have the cache's type), head_dim of at most 256.  num_seqs == 0 is valid and launches nothing.
+ * kv is never NULL.  A call of the attention or of the collected weight is laid out for the average number of nodes a
+ * sequence, which is all the host knows: sequences with many nodes and a majority with few are faster in two calls.
  *
  * sharpv_tree_attention: attention of a step's query nodes.  Node i of a sequence sees every cached token
  * of the sequence and those drafted tokens of the same sequence that its row of the tree mask marks:

@@ -20,7 +20,9 @@ constexpr int kNodeWindow = 512;        // nodes whose weights are looked at tog
 constexpr int kMaxMassHeadDim = 256;
 // bf16: average query rows of a (sequence, KV head) up to which the row kernel is taken.  It spreads keys finer (32 a unit
 // against 128), the tensor cores' kernel weighs more rows at once; 56 rows, 4 KV heads x 128, us: 50,432 rows 17.1 against
-// 17.8, 6,272 rows 7.7 / 9.4, the ragged batch of 16 21.4 / 18.7; 84 rows: 19.3 / 18.1, 8.5 / 9.8, 23.4 / 19.4.
+// 17.8, 6,272 rows 7.7 / 9.4, the ragged batch of 16 21.4 / 18.7; 84 rows: 19.3 / 18.1, 8.5 / 9.8, 23.4 / 19.4.  As with the
+// attention, an average over unlike sequences finds the kernel of the small ones: 63 single nodes over 2,000 rows each and 64
+// nodes over 50,432 121 us in one call, 30 + 32 in two; fp32 (6,272 rows in place of 50,432) 993, 89 + 106 in two.
 constexpr int64_t kMaxRowsPath = 64;
 
 // The nodes [w0, w0 + kNodeWindow) of a sequence that count, as a list in ascending order.  Returns their number.

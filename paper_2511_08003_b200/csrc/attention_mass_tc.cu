@@ -10,8 +10,8 @@
 // heads at a time as fit; K is read once unless one head's rows alone do not fit.
 //
 // What bounds it are the exponentials, one a (key, query row).  Measured (4 KV heads x 128, 7 query heads each): 64 nodes over
-// 50,432 rows 32 us (0.71 PFLOP/s); accepted nodes of 16 ragged sequences 24.5 us; 509 nodes over 10,944 rows, in several
-// passes, 143 us (0.28 PFLOP/s).
+// 50,432 rows 32 us (0.71 PFLOP/s); accepted nodes of 16 ragged sequences 23.5 us; 509 nodes over 10,944 rows, in several
+// passes, 144 us (0.28 PFLOP/s).
 #include "attention_mass.cuh"
 #include "tcgen05.cuh"
 

@@ -53,7 +53,8 @@ __device__ __forceinline__ SeqInfo load_seq(const SeqTables& t, int b, bool& bad
 //           end one segment and begin the next, which costs them about kSwitch.
 // Pieces are taken where m is no more than a run's cost and that (and there are at most 32 sequences: one a lane).
 // Against runs alone, us: tree of 64 nodes over 50,432 rows 58.9 -> 57.0, ragged trees 47.1 -> 46.0, one token over 50,432
-// rows 29.3 -> 28.7, weight of ragged trees 26.3 -> 24.4; a chunk of 509 nodes over 10,944 rows keeps runs.
+// rows 29.3 -> 28.7, weight of ragged trees 26.3 -> 24.4; a chunk of 509 nodes over 10,944 rows keeps runs.  kSwitch was chosen
+// on these, which are bf16; the fp32 kernels use it as it is, although a tile of theirs (32 keys) takes another time.
 struct Split {
     static constexpr uint32_t kSwitch = 3;      // what ending one segment and beginning another costs, in tiles
     __host__ __device__ uint32_t cost(const SeqInfo&) const { return 1; }

@@ -4,9 +4,10 @@
 // image of the mass), by a cluster of CTAs that share the sequence's rows in contiguous slices: every CTA counts
 // its slice in shared memory, and all read one another's counts.  The rows above the k-th key stay, and of those equal
 // to it the first ones; the warps' and slices' counts give every warp the place where its survivors go.
-// What bounds it is latency (four rounds of counting with two barriers of the cluster each): the keys are read from
-// memory once and kept in shared memory (slices too long for that are read again every round), and in the first round
-// lanes of a warp that count the same digit (weights span few powers of two) count it with one atomic.
+// What bounds it is latency: a CTA walks its slice seven times (once to read it, a time a round, once to count the survivors,
+// once to write them), with a barrier of the cluster a round and two behind the count.  The keys are read from memory
+// once and kept in shared memory (slices too long for that are read again every time), and in the first round lanes of a
+// warp that count the same digit (weights span few powers of two) count it with one atomic.
 #include <cooperative_groups.h>
 
 #include "decode_common.cuh"
@@ -49,7 +50,9 @@ __device__ __forceinline__ void seq_rows(const EvictArgs& a, int b, int64_t& beg
     keep = min(max(__ldg(a.budget + b), 0), len);
 }
 
-// One cluster per sequence.  Measured: 16 ragged sequences (37,712 rows) 10.5 us, one of 50,432 rows 21 us (2.3 us a round).
+// One cluster per sequence.  Measured: 16 ragged sequences (37,712 rows) 10.5 us, one of 50,432 rows 21 us.  Of that, by time
+// stamps from cold caches (10.9 and 22.3 us): tables and slice read 1.7 and 3.2, four rounds 5.0 and 10.6, survivors counted
+// and exchanged 2.3 and 3.3, written 0.5 and 5.1.
 __global__ void __cluster_dims__(kEvictCluster, 1, 1) __launch_bounds__(kEvictThreads)
 evict_select_kernel(const __grid_constant__ EvictArgs a) {
     namespace cg = cooperative_groups;

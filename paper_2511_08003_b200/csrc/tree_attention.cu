@@ -439,7 +439,11 @@ sharpv_status simt_by_dim(AttnArgs& a, int sms, cudaStream_t stream) {
 // row tile of the row kernel takes them all and K and V are read once; with more it would read them again for every 16,
 // and the tensor cores' kernel is ahead at once (21 rows, 4 KV heads x 128, us: 50,432 rows 36 against 55, the ragged
 // batch of 16 34 against 54, 6,272 rows 19 against 23; 56 rows: 37 / 77, 36 / 84, 19 / 34).  It holds up to 128 columns and
-// groups of up to 128 heads; beyond, the row kernel takes any number of rows.
+// groups of up to 128 heads; beyond, the row kernel takes any number of rows, 16 at a time (4 x 256, 7 query heads each, 6,272
+// rows: one token 18 us, 64 nodes 120, a chunk of 509 926).
+// The host knows the average alone.  One large sequence among many small ones is taken by the kernel of the small ones: 63
+// tokens over 2,000 rows each and a tree of 64 over 50,432 (4 x 128) 399 us in one call, 50 + 58 in two; with 15 tokens,
+// where the average is over 16, 77 in one and 22 + 58 in two.
 constexpr int64_t kMaxRowsPath = 16;
 enum class Path { simt, rows, tc };
 struct Choice {
