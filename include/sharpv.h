@@ -55,9 +55,11 @@ typedef enum {
                                      and in every build by the entry points that say so */
 } sharpv_status;
 
-/* SHARPV_U8 (any one-byte element, e.g. an fp8 K/V cache) is accepted by sharpv_kv_compact only: rows are
- * copied bit for bit, never interpreted.  Scores and cosines need SHARPV_F32 or SHARPV_BF16. */
-typedef enum { SHARPV_F32 = 0, SHARPV_BF16 = 1, SHARPV_U8 = 2 } sharpv_dtype;
+/* SHARPV_U8 (any one-byte element, e.g. an fp8 K/V cache) is accepted by sharpv_kv_compact and sharpv_kv_append only: rows are
+ * copied bit for bit, never interpreted.  Scores and cosines need SHARPV_F32 or SHARPV_BF16.  SHARPV_E4M3 (8-bit floats, 4 bits of
+ * exponent, 3 of mantissa, largest value 448, no infinities) and SHARPV_I8 (-128 .. 127) are the codes of caches in 8 bits
+ * with scales, which sharpv_kv_append_q8 and sharpv_tree_attention_q8 take. */
+typedef enum { SHARPV_F32 = 0, SHARPV_BF16 = 1, SHARPV_U8 = 2, SHARPV_E4M3 = 3, SHARPV_I8 = 4 } sharpv_dtype;
 
 /* How threshold_t * f (Eq. 5, 6) becomes an integer budget.  The paper is silent;
  * FLOOR never keeps more than the computed ratio and is the default of the binding. */
@@ -465,6 +467,98 @@ sharpv_status sharpv_kv_append(
     int32_t layer_begin, int32_t layer_end,
     const int32_t* src_pos, const int32_t* src_seq_offsets, const int32_t* dst_begin, int32_t num_seqs,
     int64_t capacity, int32_t* status_word, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * What a layer does to the queries and keys of a step before the attention (no counterpart in the paper): the norm of every
+ * head and the rotation by the token's position, in one pass.  For every token and head, in fp32 and rounded once:
+ *     y = x / sqrt(mean(x^2) + eps) * weight                                   (norm = 1; norm = 0: y = x)
+ *     out_i = y_i cos a_i - y_{i+h} sin a_i,  out_{i+h} = y_{i+h} cos a_i + y_i sin a_i      for i < h = rotary_dim / 2,
+ *     a_i = positions[pair_axis[i]][token] * rope_base^(-i / h),
+ * and out = y from rotary_dim on (the pairing of sharpv_kv_compact_rope).  pair_axis [host] uint8[rotary_dim / 2] says
+ * which of the num_axes positions of a token (time, height, width of a video's token, say) turns which pair, in blocks or
+ * in turn, as the model has it; a text token's axes all hold the same number.  One axis is the usual rotation.
+ *
+ * q [dev] [num_tokens, num_q_heads, head_dim], token stride ld_q, head stride head_q (elements); k the same with num_kv_heads:
+ *   views of a fused projection are fine.  Outputs have strides of their own (keys can go straight to where the
+ *   attention or sharpv_kv_append reads them).  An output may be its own input (same pointer and strides); otherwise outputs
+ *   overlap neither inputs nor each other.
+ * q_weight, k_weight [dev] [head_dim] of the same type, or NULL: ones (they must be NULL where norm = 0).
+ * positions [dev] int32[num_axes, num_tokens], row stride ld_positions; any value.  Angles are formed and reduced in
+ *   64 bits, their sine and cosine taken in fp32.
+ * SHARPV_F32 and SHARPV_BF16; head_dim of at most 256, head_dim and rotary_dim / 2 elements multiples of 16 bytes; at most 8
+ * axes and 4096 heads in all.  rotary_dim = 0 is the norm alone (norm = 0 and rotary_dim = 0: SHARPV_ERR_INVALID_ARG).
+ * num_tokens == 0 is valid and launches nothing.
+ */
+sharpv_status sharpv_qk_norm_rope(
+    const void* q, int64_t ld_q, int64_t head_q, const void* k, int64_t ld_k, int64_t head_k, sharpv_dtype dtype,
+    int64_t num_tokens, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+    int32_t norm, const void* q_weight, const void* k_weight, float eps,
+    const int32_t* positions, int64_t ld_positions, int32_t num_axes, const uint8_t* pair_axis /* [host] */,
+    int32_t rotary_dim, double rope_base,
+    void* out_q, int64_t ld_out_q, int64_t head_out_q, void* out_k, int64_t ld_out_k, int64_t head_out_k,
+    void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A cache in 8 bits: codes (SHARPV_E4M3 or SHARPV_I8) in the library's layout, and a scale for each block of block_tokens
+ * rows of a plane: a byte x at scales + layer * stride_layer + kv * stride_kv + head * stride_head + row / block_tokens
+ * (strides in bytes) that stands for 2^(x - 127).  A row's values are its codes times its block's scale.  Scales are used from
+ * 2^-48 to 2^48; a byte outside 79 .. 175 is read as the nearest of these.  Being powers of two they cost e4m3 codes
+ * nothing and int8 codes up to one bit, and make everything else exact: rows in 8 bits widen to bf16 without rounding, and a
+ * block whose scale has to grow is rounded once more where its codes lose a bit, not where they do not.
+ */
+typedef struct {
+    int32_t block_tokens;                               /* a power of two from 1 to 256 */
+    int64_t stride_layer, stride_kv, stride_head;       /* bytes; a plane's blocks lie next to each other */
+} sharpv_kv_scales;
+
+/* ------------------------------------------------------------------------------------------
+ * K/V rows into a cache in 8 bits whose sequences have room to grow: sharpv_kv_append with the rows of src (SHARPV_F32,
+ * SHARPV_BF16, or another cache in 8 bits with src_scales) rounded to dst's codes.  With a kept list as src_pos it prunes and
+ * quantises the cache that a prompt left in one pass; with accepted nodes it commits a step's tokens; from a cache in
+ * 8 bits it copies, forks or compacts sequences.
+ *   Every block of dst that receives rows gets the least scale 2^e (e from -48 to 48) with |value| <= 448 * 2^e (SHARPV_E4M3;
+ * 127 * 2^e for SHARPV_I8) for all the finite values that it receives; codes are the nearest to value / 2^e, ties to even.
+ * Values that are too large for 2^48 and infinities become the largest code of their sign (-128 for SHARPV_I8's negative ones),
+ * NaN stays NaN (SHARPV_I8: 0).
+ *   Rows that lie in front of dst_begin[b] in the same block are taken to be sequence b's own and keep their values: if their
+ * scale is the larger one it stays, otherwise their codes are rounded to the new one.  So sequences begin at multiples of
+ * block_tokens, and destination blocks of different sequences must not be the same.  Rows of a block behind the last one written
+ * are left as they are: they are free.
+ * Tables, capacity, status_word and the disjointness of the two caches as in sharpv_kv_append; src_scales_layout and src_scales
+ * are NULL for SHARPV_F32 and SHARPV_BF16 sources.  head_dim is a multiple of 16 and at most 1024 (of 256 with SHARPV_F32
+ * sources).  The scales of dst and src must not overlap.
+ */
+sharpv_status sharpv_kv_append_q8(
+    const void* kv_src, const sharpv_kv_layout* src_layout /* [host] */, const uint8_t* src_scales,
+    const sharpv_kv_scales* src_scales_layout /* [host] */, int64_t src_tokens,
+    void* kv_dst, const sharpv_kv_layout* dst_layout /* [host] */, uint8_t* dst_scales,
+    const sharpv_kv_scales* dst_scales_layout /* [host] */, int64_t dst_tokens,
+    int32_t layer_begin, int32_t layer_end,
+    const int32_t* src_pos, const int32_t* src_seq_offsets, const int32_t* dst_begin, int32_t num_seqs,
+    int64_t capacity, int32_t* status_word, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * sharpv_tree_attention over a cache in 8 bits: the attention of the query nodes over the values that the cache stands for and
+ * the drafted tokens.  q, draft_k, draft_v and out are SHARPV_BF16; the layout's dtype is SHARPV_E4M3 or SHARPV_I8, head_dim a
+ * multiple of 16.  All else as there: tables, masks, rows that see nothing, errors, workspace.
+ * Scores, the softmax's maximum and sum, the weighted sums and lse are fp32.  Weights are rounded to 16 bits before they multiply
+ * the values, so a component of out is off by up to 2^-8 sum_j p_j |v_j| / sum_j p_j for that and 2^-8 |out| for its own
+ * rounding.  (Up to 16 average query rows a sequence and KV head, and where head_dim is over 128, cached values are weighted in
+ * fp16 relative to the largest weight times scale, which is eight times as exact.)
+ */
+size_t sharpv_tree_attention_q8_workspace_bytes(int32_t num_seqs, int64_t total_nodes, int32_t num_q_heads,
+                                                int32_t num_kv_heads, int32_t head_dim);
+
+sharpv_status sharpv_tree_attention_q8(
+    const void* q, int64_t ld_q,
+    const void* draft_k, int64_t ld_draft_k, const void* draft_v, int64_t ld_draft_v,
+    int32_t num_q_heads,
+    const void* kv, const sharpv_kv_layout* layout /* [host] */, const uint8_t* scales,
+    const sharpv_kv_scales* scales_layout /* [host] */, int32_t layer, int64_t cache_tokens,
+    int32_t num_seqs, const int32_t* seq_begin, const int32_t* seq_len, const int32_t* node_offsets,
+    int64_t total_nodes, const uint32_t* tree_mask, int32_t mask_words, float scale,
+    void* out, float* out_lse,
+    void* workspace, size_t workspace_bytes, int32_t* status_word, void* cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -30,7 +30,7 @@ class Status(enum.IntEnum):
     ERR_BOUNDS = 7
 
 
-F32, BF16, U8 = 0, 1, 2
+F32, BF16, U8, E4M3, I8 = 0, 1, 2, 3, 4
 ROUND_FLOOR, ROUND_NEAREST, ROUND_CEIL = 0, 1, 2
 DISSIM, ONE_MINUS_COS = 0, 1
 PRUNE_PER_TOKEN, PRUNE_PER_LAYER = 0, 1
@@ -49,6 +49,11 @@ class KVLayout(C.Structure):
                 ("stride_head", C.c_int64), ("stride_token", C.c_int64)]
 
 
+class KVScales(C.Structure):
+    _fields_ = [("block_tokens", C.c_int32), ("stride_layer", C.c_int64), ("stride_kv", C.c_int64),
+                ("stride_head", C.c_int64)]
+
+
 # ------------------------------------------------------------------------------- loading
 _lib = None
 
@@ -64,6 +69,8 @@ EXPORTS = (
     "sharpv_tree_attention_workspace_bytes", "sharpv_tree_attention",
     "sharpv_attention_mass_workspace_bytes", "sharpv_attention_mass",
     "sharpv_evict_select", "sharpv_kv_append",
+    "sharpv_qk_norm_rope", "sharpv_kv_append_q8",
+    "sharpv_tree_attention_q8_workspace_bytes", "sharpv_tree_attention_q8",
 )
 
 NOALLOC_MAX_SEQ_TOKENS = 262144
@@ -143,6 +150,17 @@ def lib():
     L.sharpv_evict_select.argtypes = [vp, i64, i32, vp, vp, vp, i32, i32, vp, vp, vp, i64, vp, vp]
     L.sharpv_kv_append.restype = C.c_int
     L.sharpv_kv_append.argtypes = [vp, lay, i64, vp, lay, i64, i32, i32, vp, vp, vp, i32, i64, vp, vp]
+    L.sharpv_qk_norm_rope.restype = C.c_int
+    L.sharpv_qk_norm_rope.argtypes = [vp, i64, i64, vp, i64, i64, C.c_int, i64, i32, i32, i32, i32, vp, vp, f32, vp, i64, i32,
+                                      C.c_char_p, i32, C.c_double, vp, i64, i64, vp, i64, i64, vp]
+    scl = C.POINTER(KVScales)
+    L.sharpv_kv_append_q8.restype = C.c_int
+    L.sharpv_kv_append_q8.argtypes = [vp, lay, vp, scl, i64, vp, lay, vp, scl, i64, i32, i32, vp, vp, vp, i32, i64, vp, vp]
+    L.sharpv_tree_attention_q8_workspace_bytes.restype = sz
+    L.sharpv_tree_attention_q8_workspace_bytes.argtypes = [i32, i64, i32, i32, i32]
+    L.sharpv_tree_attention_q8.restype = C.c_int
+    L.sharpv_tree_attention_q8.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, lay, vp, scl, i32, i64, i32, vp, vp, vp, i64,
+                                           vp, i32, f32, vp, vp, vp, sz, vp, vp]
     _lib = L
     return L
 
@@ -589,20 +607,11 @@ def sharpv_tree_attention_workspace_bytes(num_seqs: int, total_nodes: int, num_q
                                                            dtype))
 
 
-def sharpv_tree_attention(q: torch.Tensor, kv: torch.Tensor, layer: int, seq_begin: torch.Tensor,
-                          seq_len: torch.Tensor, node_offsets: torch.Tensor, draft_k: Optional[torch.Tensor] = None,
-                          draft_v: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None,
-                          scale: Optional[float] = None, out: Optional[Dict[str, torch.Tensor]] = None,
-                          workspace=None, status_word=None, stream=None) -> Dict[str, torch.Tensor]:
-    """Attention of a step's query nodes q [nodes, q_heads, head_dim] over layer `layer` of the cache kv
-    [L, 2, H, T, head_dim] and the drafted tokens' own draft_k, draft_v [nodes, H, head_dim].  tree_mask: int32
-    [nodes, words], bit j of a row = the node sees node j of its sequence (None: nodes 0 .. i).  scale: None =
-    head_dim ** -0.5.  Returns dict(out [nodes, q_heads, head_dim], lse [nodes, q_heads])."""
-    lay, dev = _cache(kv)
-    dtype, D, H = kv.dtype, lay.head_dim, lay.num_kv_heads
+def _attention_arrays(q, kv, lay, dev, dtype, draft_k, draft_v, tree_mask, out, stream):
+    """What both attentions check and pass alike: (q, ld_q, draft_k, ld, draft_v, ld), (mask, words), out with its addresses."""
+    D, H = lay.head_dim, lay.num_kv_heads
     ldq = _heads(q, "q", dev, dtype, None, None, D)
     N, HQ = q.shape[:2]
-    B = seq_begin.numel()
     ldk = ldv = words = 0
     dk = dv = mask = None
     if draft_k is not None:
@@ -621,10 +630,25 @@ def sharpv_tree_attention(q: torch.Tensor, kv: torch.Tensor, layer: int, seq_beg
         if out["out"].shape != q.shape or out["lse"].shape != q.shape[:2]:
             raise ValueError("out must be [nodes, q_heads, head_dim], lse [nodes, q_heads]")
         po, pl = _on(out["out"], "out", dev, dtype), _on(out["lse"], "lse", dev, _F32)
-    ws = _workspace(workspace, sharpv_tree_attention_workspace_bytes(B, N, HQ, H, D, lay.dtype), dev, stream)
-    rc = _call("sharpv_tree_attention", kv, q.data_ptr(), ldq, dk, ldk, dv, ldv, HQ, kv.data_ptr(), lay, layer,
+    return (q.data_ptr(), ldq, dk, ldk, dv, ldv, HQ), (mask, words), out, po, pl
+
+
+def sharpv_tree_attention(q: torch.Tensor, kv: torch.Tensor, layer: int, seq_begin: torch.Tensor,
+                          seq_len: torch.Tensor, node_offsets: torch.Tensor, draft_k: Optional[torch.Tensor] = None,
+                          draft_v: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None,
+                          scale: Optional[float] = None, out: Optional[Dict[str, torch.Tensor]] = None,
+                          workspace=None, status_word=None, stream=None) -> Dict[str, torch.Tensor]:
+    """Attention of a step's query nodes q [nodes, q_heads, head_dim] over layer `layer` of the cache kv
+    [L, 2, H, T, head_dim] and the drafted tokens' own draft_k, draft_v [nodes, H, head_dim].  tree_mask: int32
+    [nodes, words], bit j of a row = the node sees node j of its sequence (None: nodes 0 .. i).  scale: None =
+    head_dim ** -0.5.  Returns dict(out [nodes, q_heads, head_dim], lse [nodes, q_heads])."""
+    lay, dev = _cache(kv)
+    arrays, mask, out, po, pl = _attention_arrays(q, kv, lay, dev, kv.dtype, draft_k, draft_v, tree_mask, out, stream)
+    D, B, (N, HQ) = lay.head_dim, seq_begin.numel(), q.shape[:2]
+    ws = _workspace(workspace, sharpv_tree_attention_workspace_bytes(B, N, HQ, lay.num_kv_heads, D, lay.dtype), dev, stream)
+    rc = _call("sharpv_tree_attention", kv, *arrays, kv.data_ptr(), lay, layer,
                kv.shape[3], B, _on(seq_begin, "seq_begin", dev, _I32), _on(seq_len, "seq_len", dev, _I32, B),
-               _on(node_offsets, "node_offsets", dev, _I32, B + 1), N, mask, words,
+               _on(node_offsets, "node_offsets", dev, _I32, B + 1), N, *mask,
                D ** -0.5 if scale is None else scale, po, pl, ws.data_ptr(), ws.numel(), _status(status_word, dev),
                _queue(stream, dev))
     if rc:
@@ -722,3 +746,129 @@ def sharpv_kv_append(kv_src: torch.Tensor, kv_dst: torch.Tensor, src_pos: torch.
     if rc:
         _check("sharpv_kv_append", rc)
     return kv_dst
+
+
+# ------------------------------------------------------------------------------- queries and keys of a step
+def sharpv_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, pair_axis, rope_base: float,
+                        norm: bool = False, q_weight: Optional[torch.Tensor] = None,
+                        k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                        out: Optional[Dict[str, torch.Tensor]] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """Norm of every head (norm=True; weights [head_dim] or None) and its rotation by the token's positions int32 [axes,
+    tokens] (or [tokens]): q [tokens, q_heads, head_dim], k [tokens, heads, head_dim], any token and head strides.
+    pair_axis: for each of the rotary_dim / 2 pairs the axis whose position turns it (bytes or a sequence of ints).
+    Returns dict(q, k), dense unless `out` holds them; out may hold q and k themselves."""
+    if not q.is_cuda:
+        raise ValueError("q must be a CUDA tensor")
+    dev, dtype = q.device, q.dtype
+    if q.dim() != 3 or k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
+        raise ValueError("q and k must be [tokens, heads, head_dim] of the same tokens and head_dim")
+    N, HQ, D = q.shape
+    H = k.shape[1]
+    if k.device != dev or k.dtype is not dtype:
+        raise ValueError("q and k must share device and dtype")
+    if out is None:
+        out = {"q": _empty(q.shape, dtype, dev, stream), "k": _empty(k.shape, dtype, dev, stream)}
+    oq, ok = out["q"], out["k"]
+    for t, like in ((oq, q), (ok, k)):
+        if t.device != dev or t.dtype is not dtype or t.shape != like.shape:
+            raise ValueError("out must hold q and k of the inputs' shapes, dtype and device")
+    if positions.dim() == 1:
+        positions = positions[None]
+    if positions.dim() != 2 or positions.shape[1] != N or positions.device != dev or (N > 1 and positions.stride(1) != 1):
+        raise ValueError(f"positions must be [axes, tokens] on {dev} with a contiguous last axis")
+    if positions.dtype is not _I32:
+        raise TypeError("positions must be int32")
+    pairs = pair_axis if isinstance(pair_axis, bytes) else bytes(pair_axis)
+    rows = []
+    for t in (q, k, oq, ok):
+        s = t.stride()
+        if N and t.shape[1] and s[2] != 1:
+            raise ValueError("q and k must have a contiguous last axis")
+        # a stride that nothing needs may be anything that the call accepts
+        head = s[1] if t.shape[1] > 1 else D
+        rows.append((t.data_ptr(), s[0] if N > 1 else max(D, head), head))
+    w = [None if t is None else _on(t, name, dev, dtype, D) for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight"))]
+    rc = _call("sharpv_qk_norm_rope", q, *rows[0], *rows[1], _dtype_code(q), N, HQ, H, D, 1 if norm else 0, w[0], w[1], eps,
+               positions.data_ptr(), positions.stride(0) if positions.shape[0] > 1 else N, positions.shape[0], pairs, 2 * len(pairs),
+               rope_base, *rows[2], *rows[3], _queue(stream, dev))
+    if rc:
+        _check("sharpv_qk_norm_rope", rc)
+    return out
+
+
+# ------------------------------------------------------------------------------- a cache in 8 bits
+_Q8_CODES = {torch.float8_e4m3fn: E4M3, torch.int8: I8}
+
+
+def _q8_cache(kv: torch.Tensor, scales: torch.Tensor, block_tokens: int, name: str):
+    """Layouts of a cache in 8 bits and of its scales [L, 2, H, blocks]: bytes x (uint8 or float8_e8m0fnu) for 2 ** (x - 127)."""
+    lay, dev = _cache(kv)
+    code = _Q8_CODES.get(kv.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float8_e4m3fn or int8")
+    lay.dtype = code
+    s, st = scales.shape, scales.stride()
+    if scales.device != dev or scales.element_size() != 1:
+        raise ValueError(f"the scales of {name} must be one byte each and on {dev}")
+    if len(s) != 4 or s[:3] != kv.shape[:3] or block_tokens < 1 or s[3] * block_tokens < kv.shape[3] or (s[3] > 1 and st[3] != 1):
+        raise ValueError(f"the scales of {name} must be [L, 2, H, blocks] with a contiguous last axis and a block for every "
+                         "block_tokens rows")
+    return lay, KVScales(block_tokens, st[0], st[1], st[2]), dev
+
+
+def sharpv_kv_append_q8(kv_src: torch.Tensor, kv_dst: torch.Tensor, dst_scales: torch.Tensor, block_tokens: int,
+                        src_pos: torch.Tensor, src_seq_offsets: torch.Tensor, dst_begin: torch.Tensor,
+                        src_scales: Optional[torch.Tensor] = None, src_block_tokens: Optional[int] = None,
+                        capacity: Optional[int] = None, layer_begin: int = 0, layer_end: Optional[int] = None,
+                        status_word=None, stream=None) -> torch.Tensor:
+    """sharpv_kv_append into a cache in 8 bits kv_dst [L, 2, H, T, D_h] (float8_e4m3fn or int8) with dst_scales [L, 2, H, blocks]:
+    rows of kv_src (float32, bfloat16, or another cache in 8 bits with src_scales) rounded to codes.  Returns kv_dst."""
+    dl, ds, dev = _q8_cache(kv_dst, dst_scales, block_tokens, "kv_dst")
+    if kv_src.device != dev:
+        raise ValueError("kv_src and kv_dst must be on the same device")
+    if src_scales is not None:
+        sl, ss, _ = _q8_cache(kv_src, src_scales, block_tokens if src_block_tokens is None else src_block_tokens, "kv_src")
+    else:
+        sl, ss = kv_layout(kv_src), None
+        if kv_src.dtype not in _KV_CODES:
+            raise TypeError("kv_src must be float32 or bfloat16, or a cache in 8 bits with src_scales")
+    if capacity is None:
+        capacity = src_pos.numel()
+    elif capacity > src_pos.numel():
+        raise ValueError("capacity is larger than src_pos")
+    B = dst_begin.numel()
+    rc = _call("sharpv_kv_append_q8", kv_src, kv_src.data_ptr(), sl, None if ss is None else src_scales.data_ptr(), ss,
+               kv_src.shape[3], kv_dst.data_ptr(), dl, dst_scales.data_ptr(), ds, kv_dst.shape[3], layer_begin,
+               sl.num_layers if layer_end is None else layer_end, _on(src_pos, "src_pos", dev, _I32),
+               _on(src_seq_offsets, "src_seq_offsets", dev, _I32, B + 1), _on(dst_begin, "dst_begin", dev, _I32), B, capacity,
+               _status(status_word, dev), _queue(stream, dev))
+    if rc:
+        _check("sharpv_kv_append_q8", rc)
+    return kv_dst
+
+
+@functools.lru_cache(maxsize=256)
+def sharpv_tree_attention_q8_workspace_bytes(num_seqs: int, total_nodes: int, num_q_heads: int, num_kv_heads: int,
+                                             head_dim: int) -> int:
+    return int(lib().sharpv_tree_attention_q8_workspace_bytes(num_seqs, total_nodes, num_q_heads, num_kv_heads, head_dim))
+
+
+def sharpv_tree_attention_q8(q: torch.Tensor, kv: torch.Tensor, scales: torch.Tensor, block_tokens: int, layer: int,
+                             seq_begin: torch.Tensor, seq_len: torch.Tensor, node_offsets: torch.Tensor,
+                             draft_k: Optional[torch.Tensor] = None, draft_v: Optional[torch.Tensor] = None,
+                             tree_mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                             out: Optional[Dict[str, torch.Tensor]] = None, workspace=None, status_word=None,
+                             stream=None) -> Dict[str, torch.Tensor]:
+    """sharpv_tree_attention over a cache in 8 bits (float8_e4m3fn or int8) with its scales [L, 2, H, blocks]; q, draft_k, draft_v
+    and out are bfloat16.  Returns dict(out [nodes, q_heads, head_dim], lse [nodes, q_heads])."""
+    lay, sc, dev = _q8_cache(kv, scales, block_tokens, "kv")
+    arrays, mask, out, po, pl = _attention_arrays(q, kv, lay, dev, torch.bfloat16, draft_k, draft_v, tree_mask, out, stream)
+    D, B, (N, HQ) = lay.head_dim, seq_begin.numel(), q.shape[:2]
+    ws = _workspace(workspace, sharpv_tree_attention_q8_workspace_bytes(B, N, HQ, lay.num_kv_heads, D), dev, stream)
+    rc = _call("sharpv_tree_attention_q8", kv, *arrays, kv.data_ptr(), lay, scales.data_ptr(), sc, layer, kv.shape[3], B,
+               _on(seq_begin, "seq_begin", dev, _I32), _on(seq_len, "seq_len", dev, _I32, B),
+               _on(node_offsets, "node_offsets", dev, _I32, B + 1), N, *mask, D ** -0.5 if scale is None else scale, po, pl,
+               ws.data_ptr(), ws.numel(), _status(status_word, dev), _queue(stream, dev))
+    if rc:
+        _check("sharpv_tree_attention_q8", rc)
+    return out

@@ -317,9 +317,10 @@ __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_gr
 __device__ __forceinline__ bool finite_f32(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
 // The layout checks of the calls that read a cache through its layout struct (the same as the compaction's).
-inline sharpv_status kv_layout_status(const void* kv, const sharpv_kv_layout* L, bool computes) {
+template <class Ok>
+inline sharpv_status kv_layout_status_if(const void* kv, const sharpv_kv_layout* L, Ok ok) {
     if (!kv || !L) return SHARPV_ERR_INVALID_ARG;
-    if (computes ? !dtype_ok(L->dtype) : !copy_dtype_ok(L->dtype)) return SHARPV_ERR_UNSUPPORTED;
+    if (!ok(L->dtype)) return SHARPV_ERR_UNSUPPORTED;
     if (L->num_layers < 1 || L->num_kv_heads < 1 || L->head_dim < 1 || L->stride_layer < 0 || L->stride_kv < 0 ||
         L->stride_head < 0 || L->stride_token < L->head_dim)
         return SHARPV_ERR_INVALID_ARG;
@@ -328,6 +329,10 @@ inline sharpv_status kv_layout_status(const void* kv, const sharpv_kv_layout* L,
         (L->stride_head * eb) % 16 || (L->stride_token * eb) % 16 || !aligned16(kv))
         return SHARPV_ERR_UNSUPPORTED;
     return SHARPV_OK;
+}
+
+inline sharpv_status kv_layout_status(const void* kv, const sharpv_kv_layout* L, bool computes) {
+    return kv_layout_status_if(kv, L, computes ? dtype_ok : copy_dtype_ok);
 }
 
 inline sharpv_status current_sms(int& sms) {

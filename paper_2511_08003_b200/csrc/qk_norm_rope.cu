@@ -1,0 +1,264 @@
+// Norm of every query and key head and its position rotation in one pass (sharpv_qk_norm_rope):
+//
+//   y = x / sqrt(mean(x^2) + eps) * weight            (left out where the call wants the rotation alone)
+//   out_i = y_i cos a_i - y_{i+R/2} sin a_i,  out_{i+R/2} = y_{i+R/2} cos a_i + y_i sin a_i,  i < R/2,
+//   a_i = positions[axis_i] * base^(-2i/R);  the elements from R on are y.
+//
+// Every row (a token's head) is read and written once, by LP neighbouring lanes.  A lane holds a vector of the first half
+// of the rotated part and its partner of the second half, so the rotation needs no exchange and the norm LP - 1
+// shuffles at most.  The angles of a token are the same for all its heads: a CTA takes whole tokens and keeps their cosines and
+// sines in shared memory, in the order in which the lanes of a row read them (neighbouring 16 bytes).  Angles are
+// formed in turns and reduced in 64 bits (a position of 2^31 is off by 2^-23 of a turn at most); their sine and cosine are
+// taken in fp32, as the products are; the one rounding to the storage type is the last.
+//
+// HBM bounds it for prompts, latency (positions, sine, one row) for the tokens of a step.
+#include "decode_common.cuh"
+
+#include <cuda_bf16.h>
+
+#include <cmath>
+
+namespace sharpv {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kAhead = 2;               // rows of a lane that are loaded before the first is worked on
+constexpr int kMaxPairs = 128;          // head_dim of at most 256
+constexpr int kMaxAxes = 8;
+constexpr int kMaxTileTokens = 16;
+
+struct NormRopeArgs {
+    const char* q;
+    const char* k;
+    char* out_q;
+    char* out_k;
+    int64_t q_token, q_head, k_token, k_head, oq_token, oq_head, ok_token, ok_head;     // bytes
+    const char* q_weight;               // or null: ones
+    const char* k_weight;
+    const int32_t* positions;           // [axes][ld_positions]
+    int64_t ld_positions, tokens;
+    int q_heads, all_heads;             // all_heads: with the key heads
+    int row_vecs, half_vecs, units, half;       // 16-byte vectors of a row, of half of the rotated part; lanes at work; pairs
+    int tile_tokens;
+    int norm;
+    float eps, inv_d;
+    double freq[kMaxPairs];             // turns a position
+    uint8_t axis[kMaxPairs];
+};
+
+template <int DT>
+__device__ __forceinline__ uint4 narrow(const float (&x)[Elem<DT>::kPerVec]) {
+    if constexpr (DT == SHARPV_F32) {
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// 128 bits that are not read again; not by way of the read-only path, since an output may be its own input
+__device__ __forceinline__ uint4 ld_once(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
+template <int DT, int LP>
+__global__ void __launch_bounds__(kThreads, 4)
+qk_norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
+    using E = Elem<DT>;
+    constexpr int P = E::kPerVec, kGroups = kThreads / LP, kRound = kGroups * kAhead;
+    extern __shared__ float4 table[];   // [tokens][P / 2][half_vecs]: cosine and sine of two pairs
+    const int u = threadIdx.x % LP, group = threadIdx.x / LP;
+    // the lane's two vectors: a pair of the rotated part, or two neighbours behind it
+    const bool pair = u < a.half_vecs, busy = u < a.units;
+    const int v0 = pair ? u : 2 * u, v1 = pair ? u + a.half_vecs : v0 + 1;
+    const bool second = busy && v1 < a.row_vecs;
+    cudaGridDependencySynchronize();
+    const int64_t token0 = (int64_t)blockIdx.x * a.tile_tokens;
+    const int tokens = (int)min((int64_t)a.tile_tokens, a.tokens - token0), rows = tokens * a.all_heads;
+    bool first = true;
+    for (int r0 = blockIdx.y * kRound; r0 < rows; r0 += gridDim.y * kRound) {
+        uint4 x0[kAhead], x1[kAhead];
+#pragma unroll
+        for (int y = 0; y < kAhead; ++y) {
+            const int r = r0 + y * kGroups + group;
+            x0[y] = x1[y] = make_uint4(0, 0, 0, 0);
+            if (r < rows && busy) {
+                const int t = r / a.all_heads, h = r - t * a.all_heads;
+                const char* row = h < a.q_heads ? a.q + (token0 + t) * a.q_token + h * a.q_head
+                                                : a.k + (token0 + t) * a.k_token + (h - a.q_heads) * a.k_head;
+                x0[y] = ld_once(row + v0 * 16);
+                if (second) x1[y] = ld_once(row + v1 * 16);
+            }
+        }
+        if (first) {                    // while the rows are on their way
+            first = false;
+            const int step = a.half > 0 ? kThreads / a.half : 0;
+            if (threadIdx.x < step * a.half) {
+                const int i = threadIdx.x % a.half;
+                const double freq = a.freq[i];
+                const int32_t* at = a.positions + a.axis[i] * a.ld_positions + token0;
+                float2* to = reinterpret_cast<float2*>(table) + ((i % P >> 1) * a.half_vecs + i / P) * 2 + (i & 1);
+                for (int t = threadIdx.x / a.half; t < tokens; t += step) {
+                    const double turns = __ldg(at + t) * freq;
+                    float s, c;
+                    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+                    to[t * (P / 2) * a.half_vecs * 2] = make_float2(c, s);
+                }
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int y = 0; y < kAhead; ++y) {
+            const int r = r0 + y * kGroups + group;
+            const int t = r / a.all_heads, h = r - t * a.all_heads;
+            const bool is_q = h < a.q_heads;
+            float p[P], n[P];
+            E::widen(x0[y], p);
+            E::widen(x1[y], n);
+            if (a.norm) {
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < P; ++e) sum = fmaf(p[e], p[e], fmaf(n[e], n[e], sum));
+#pragma unroll
+                for (int o = LP / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                const float f = rsqrtf(fmaf(sum, a.inv_d, a.eps));
+                const char* weight = is_q ? a.q_weight : a.k_weight;
+                float w[P];
+#pragma unroll
+                for (int e = 0; e < P; ++e) w[e] = 1.f;
+                if (weight && busy) E::widen(ld_cached(weight + v0 * 16), w);
+#pragma unroll
+                for (int e = 0; e < P; ++e) p[e] *= f * w[e];
+                if (weight && second) E::widen(ld_cached(weight + v1 * 16), w);
+#pragma unroll
+                for (int e = 0; e < P; ++e) n[e] *= f * w[e];
+            }
+            if (r >= rows || !busy) continue;
+            if (pair) {
+                const float4* cs = table + t * (P / 2) * a.half_vecs + u;
+#pragma unroll
+                for (int e = 0; e < P; e += 2) {
+                    const float4 w = cs[(e >> 1) * a.half_vecs];
+                    const float a0 = p[e], a1 = p[e + 1];
+                    p[e] = fmaf(a0, w.x, -n[e] * w.y);
+                    n[e] = fmaf(n[e], w.x, a0 * w.y);
+                    p[e + 1] = fmaf(a1, w.z, -n[e + 1] * w.w);
+                    n[e + 1] = fmaf(n[e + 1], w.z, a1 * w.w);
+                }
+            }
+            char* row = is_q ? a.out_q + (token0 + t) * a.oq_token + h * a.oq_head
+                             : a.out_k + (token0 + t) * a.ok_token + (h - a.q_heads) * a.ok_head;
+            st_stream(row + v0 * 16, narrow<DT>(p));
+            if (second) st_stream(row + v1 * 16, narrow<DT>(n));
+        }
+    }
+}
+
+template <int DT, int LP>
+sharpv_status launch(NormRopeArgs& a, int sms, cudaStream_t stream) {
+    constexpr int kRound = kThreads / LP * kAhead;
+    // about four rounds a CTA, so that the angles are formed while others stream; with few tokens a CTA each, and with fewer
+    // still several CTAs share a token's heads and form its angles each
+    int64_t tile = (4 * kRound + a.all_heads - 1) / a.all_heads;
+    const int64_t share = a.tokens / (2 * sms);
+    if (tile > share) tile = share;
+    if (tile > kMaxTileTokens) tile = kMaxTileTokens;
+    if (tile < 1) tile = 1;
+    a.tile_tokens = (int)tile;
+    const int64_t ctas = (a.tokens + tile - 1) / tile;
+    int y = 1;
+    if (tile == 1) {
+        y = (a.all_heads + kRound - 1) / kRound;
+        const int64_t room = 4 * sms / ctas;
+        if (y > room) y = room > 1 ? (int)room : 1;
+    }
+    const size_t smem = (size_t)tile * a.half * sizeof(float2);
+    if (launch_dependent(qk_norm_rope_kernel<DT, LP>, dim3((unsigned)ctas, (unsigned)y), dim3(kThreads), smem, stream, a) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SHARPV_ERR_CUDA;
+    }
+    return SHARPV_OK;
+}
+
+template <int DT>
+sharpv_status by_lanes(NormRopeArgs& a, int sms, cudaStream_t stream) {
+    if (a.units <= 2) return launch<DT, 2>(a, sms, stream);
+    if (a.units <= 4) return launch<DT, 4>(a, sms, stream);
+    if (a.units <= 8) return launch<DT, 8>(a, sms, stream);
+    if (a.units <= 16) return launch<DT, 16>(a, sms, stream);
+    return launch<DT, 32>(a, sms, stream);
+}
+
+}  // namespace
+}  // namespace sharpv
+
+using namespace sharpv;
+
+extern "C" sharpv_status sharpv_qk_norm_rope(
+    const void* q, int64_t ld_q, int64_t head_q, const void* k, int64_t ld_k, int64_t head_k, sharpv_dtype dtype,
+    int64_t num_tokens, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t norm, const void* q_weight,
+    const void* k_weight, float eps, const int32_t* positions, int64_t ld_positions, int32_t num_axes,
+    const uint8_t* pair_axis, int32_t rotary_dim, double rope_base, void* out_q, int64_t ld_out_q, int64_t head_out_q,
+    void* out_k, int64_t ld_out_k, int64_t head_out_k, void* cuda_stream) {
+    if (!dtype_ok(dtype)) return SHARPV_ERR_UNSUPPORTED;
+    if (num_tokens < 0 || num_q_heads < 1 || num_kv_heads < 1 || head_dim < 1 || rotary_dim < 0 || rotary_dim > head_dim ||
+        rotary_dim % 2 || (norm != 0 && norm != 1) || (norm && (!(eps >= 0.f) || !(eps < __builtin_huge_valf()))) ||
+        (!norm && (q_weight || k_weight)) || (rotary_dim > 0 && (num_axes < 1 || !pair_axis || !(rope_base > 0.0) || !(rope_base < __builtin_huge_val()))))
+        return SHARPV_ERR_INVALID_ARG;
+    if (rotary_dim == 0 && !norm) return SHARPV_ERR_INVALID_ARG;
+    const int64_t eb = elem_bytes(dtype), row = head_dim * eb;
+    if (head_dim > 2 * kMaxPairs || row % 16 || (rotary_dim / 2 * eb) % 16 || num_axes > kMaxAxes ||
+        (int64_t)num_q_heads + num_kv_heads > 4096 || num_tokens >= (int64_t)1 << 31)
+        return SHARPV_ERR_UNSUPPORTED;
+    for (int i = 0; i < rotary_dim / 2; ++i)
+        if (pair_axis[i] >= num_axes) return SHARPV_ERR_INVALID_ARG;
+    if (num_tokens == 0) return SHARPV_OK;
+    if (!q || !k || !out_q || !out_k || (rotary_dim > 0 && (!positions || (num_axes > 1 && ld_positions < num_tokens))))
+        return SHARPV_ERR_INVALID_ARG;
+    const int64_t strides[8] = {ld_q, head_q, ld_k, head_k, ld_out_q, head_out_q, ld_out_k, head_out_k};
+    for (int i = 0; i < 8; ++i) {
+        if (strides[i] < head_dim) return SHARPV_ERR_INVALID_ARG;
+        if ((strides[i] * eb) % 16) return SHARPV_ERR_UNSUPPORTED;
+    }
+    if (!aligned16(q) || !aligned16(k) || !aligned16(out_q) || !aligned16(out_k) || !aligned16(q_weight) || !aligned16(k_weight))
+        return SHARPV_ERR_UNSUPPORTED;
+    NormRopeArgs a = {};
+    a.q = (const char*)q;
+    a.k = (const char*)k;
+    a.out_q = (char*)out_q;
+    a.out_k = (char*)out_k;
+    a.q_token = ld_q * eb;      a.q_head = head_q * eb;
+    a.k_token = ld_k * eb;      a.k_head = head_k * eb;
+    a.oq_token = ld_out_q * eb; a.oq_head = head_out_q * eb;
+    a.ok_token = ld_out_k * eb; a.ok_head = head_out_k * eb;
+    a.q_weight = (const char*)q_weight;
+    a.k_weight = (const char*)k_weight;
+    a.positions = positions;
+    a.ld_positions = ld_positions;
+    a.tokens = num_tokens;
+    a.q_heads = num_q_heads;
+    a.all_heads = num_q_heads + num_kv_heads;
+    a.half = rotary_dim / 2;
+    a.row_vecs = (int)(row / 16);
+    a.half_vecs = (int)(a.half * eb / 16);
+    a.units = a.half_vecs + (a.row_vecs - 2 * a.half_vecs + 1) / 2;
+    a.norm = norm;
+    a.eps = eps;
+    a.inv_d = 1.0f / (float)head_dim;
+    for (int i = 0; i < a.half; ++i) {
+        a.axis[i] = pair_axis[i];
+        a.freq[i] = std::pow(rope_base, -(double)i / a.half) / 6.283185307179586;
+    }
+    int sms = 0;
+    const sharpv_status st = current_sms(sms);
+    if (st != SHARPV_OK) return st;
+    return dtype == SHARPV_F32 ? by_lanes<SHARPV_F32>(a, sms, (cudaStream_t)cuda_stream)
+                               : by_lanes<SHARPV_BF16>(a, sms, (cudaStream_t)cuda_stream);
+}

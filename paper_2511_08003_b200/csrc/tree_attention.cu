@@ -6,6 +6,7 @@
 // Kernels (and those of tree_attention_rows.cu and tree_attention_tc.cu for bf16 caches):
 //   attn_simt_kernel      fp32 caches: one pass over the keys with a running maximum and sum per row, on the fp32 units
 //   attn_join_kernel      (dependent launch) joins the partial results of segments that several CTAs share
+#include "q8.cuh"
 #include "tree_attention.cuh"
 
 #include <cuda_bf16.h>
@@ -453,6 +454,7 @@ struct Choice {
     int max_ctas;           // sizes the workspace
 };
 Choice choose(sharpv_dtype dtype, int head_dim, int group, int64_t avg_rows) {
+    if (q8_dtype_ok(dtype)) return {Path::rows, kRowsTileRows, kRowsTileRows, kMaxRowsCtas};
     if (dtype == SHARPV_F32) return avg_rows <= 8 ? Choice{Path::simt, 8, 8, kMaxAttnCtas} : Choice{Path::simt, 32, 32, kMaxAttnCtas};
     if (head_dim <= 128 && group <= 128 && avg_rows > kMaxRowsPath) return {Path::tc, tc_rows(group), kTcPlaces, kMaxTcCtas};
     return {Path::rows, kRowsTileRows, kRowsTileRows, kMaxRowsCtas};
@@ -466,13 +468,8 @@ size_t shared_bytes() { return 256 + align_up(kMaxAttnCtas * sizeof(SharedSegmen
 size_t part_ml_bytes(const Choice& c) { return align_up((size_t)c.max_ctas * 2 * 2 * c.places * 4, 256); }
 size_t part_o_bytes(const Choice& c, int32_t head_dim) { return align_up((size_t)c.max_ctas * 2 * c.places * head_dim * 4, 256); }
 
-}  // namespace
-}  // namespace sharpv
-
-using namespace sharpv;
-
-extern "C" size_t sharpv_tree_attention_workspace_bytes(int32_t num_seqs, int64_t total_nodes, int32_t num_q_heads,
-                                                        int32_t num_kv_heads, int32_t head_dim, sharpv_dtype dtype) {
+size_t workspace_bytes(int32_t num_seqs, int64_t total_nodes, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                       sharpv_dtype dtype) {
     if (total_nodes < 0) total_nodes = 0;
     if (num_kv_heads < 1) num_kv_heads = 1;
     if (num_q_heads < 0) num_q_heads = 0;
@@ -483,16 +480,16 @@ extern "C" size_t sharpv_tree_attention_workspace_bytes(int32_t num_seqs, int64_
     return shared_bytes() + part_ml_bytes(c) + part_o_bytes(c, head_dim);
 }
 
-extern "C" sharpv_status sharpv_tree_attention(
+// Both entry points, behind the checks of the cache.  eb: bytes of an element of q, of drafted rows and of out.
+sharpv_status attend(
     const void* q, int64_t ld_q, const void* draft_k, int64_t ld_draft_k, const void* draft_v, int64_t ld_draft_v,
-    int32_t num_q_heads, const void* kv, const sharpv_kv_layout* layout, int32_t layer, int64_t cache_tokens,
+    int32_t num_q_heads, const void* kv, const sharpv_kv_layout* layout, const uint8_t* scales,
+    const sharpv_kv_scales* scales_layout, int64_t eb, int32_t layer, int64_t cache_tokens,
     int32_t num_seqs, const int32_t* seq_begin, const int32_t* seq_len, const int32_t* node_offsets,
     int64_t total_nodes, const uint32_t* tree_mask, int32_t mask_words, float scale, void* out, float* out_lse,
-    void* workspace, size_t workspace_bytes, int32_t* status_word, void* cuda_stream) {
-    const sharpv_status ls = kv_layout_status(kv, layout, true);
-    if (ls != SHARPV_OK) return ls;
+    void* workspace, size_t workspace_size, int32_t* status_word, void* cuda_stream) {
     const int D = layout->head_dim, H = layout->num_kv_heads;
-    const int64_t eb = elem_bytes(layout->dtype);
+    const int64_t kv_eb = elem_bytes(layout->dtype);
     if (layer < 0 || layer >= layout->num_layers || cache_tokens < 0 || num_seqs < 0 || total_nodes < 0 ||
         num_q_heads < 1 || num_q_heads % H != 0 || (draft_k == nullptr) != (draft_v == nullptr) ||
         mask_words < 0 || !(scale > 0.f) || !(scale < __builtin_huge_valf()))
@@ -506,17 +503,17 @@ extern "C" sharpv_status sharpv_tree_attention(
     if (!aligned16(q) || !aligned16(out) || (ld_q * eb) % 16 ||
         (draft_k && (!aligned16(draft_k) || !aligned16(draft_v) || (ld_draft_k * eb) % 16 || (ld_draft_v * eb) % 16)))
         return SHARPV_ERR_UNSUPPORTED;
-    if (workspace_bytes < sharpv_tree_attention_workspace_bytes(num_seqs, total_nodes, num_q_heads, H, D, layout->dtype)) return SHARPV_ERR_WORKSPACE;
+    if (workspace_size < workspace_bytes(num_seqs, total_nodes, num_q_heads, H, D, layout->dtype)) return SHARPV_ERR_WORKSPACE;
     if (!workspace) return SHARPV_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) % 256) return SHARPV_ERR_UNSUPPORTED;
 
     AttnArgs a = {};
     a.q = (const char*)q;
     a.q_node = ld_q * eb;
-    a.cache_k = (const char*)kv + (int64_t)layer * layout->stride_layer * eb;
-    a.cache_v = a.cache_k + layout->stride_kv * eb;
-    a.kv_head = layout->stride_head * eb;
-    a.kv_token = layout->stride_token * eb;
+    a.cache_k = (const char*)kv + (int64_t)layer * layout->stride_layer * kv_eb;
+    a.cache_v = a.cache_k + layout->stride_kv * kv_eb;
+    a.kv_head = layout->stride_head * kv_eb;
+    a.kv_token = layout->stride_token * kv_eb;
     a.draft_k = (const char*)draft_k;
     a.draft_v = (const char*)draft_v;
     a.dk_node = ld_draft_k * eb;
@@ -540,15 +537,64 @@ extern "C" sharpv_status sharpv_tree_attention(
     a.part_ml = (float*)(ws + shared_bytes());
     a.part_o = (float*)(ws + shared_bytes() + part_ml_bytes(ch));
     a.status_word = status_word;
+    if (scales) {
+        a.k_scales = scales + layer * scales_layout->stride_layer;
+        a.v_scales = a.k_scales + scales_layout->stride_kv;
+        a.scale_head = scales_layout->stride_head;
+        a.scale_shift = log2_of(scales_layout->block_tokens);
+    }
     int sms = 0;
     const sharpv_status ss = current_sms(sms);
     if (ss != SHARPV_OK) return ss;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     if (ch.path == Path::tc) return attn_tc_launch(a, sms, stream);
     if (ch.path == Path::rows) {
-        const sharpv_status st = attn_rows_launch(a, sms, stream);
+        const sharpv_status st = scales ? attn_rows_q8_launch(a, layout->dtype, sms, stream) : attn_rows_launch(a, sms, stream);
         return st == SHARPV_OK ? join_launch<SHARPV_BF16>(a, stream) : st;
     }
     const sharpv_status st = ch.rows == 8 ? simt_by_dim<8>(a, sms, stream) : simt_by_dim<32>(a, sms, stream);
     return st == SHARPV_OK ? join_launch<SHARPV_F32>(a, stream) : st;
+}
+
+}  // namespace
+}  // namespace sharpv
+
+using namespace sharpv;
+
+extern "C" size_t sharpv_tree_attention_workspace_bytes(int32_t num_seqs, int64_t total_nodes, int32_t num_q_heads,
+                                                        int32_t num_kv_heads, int32_t head_dim, sharpv_dtype dtype) {
+    return workspace_bytes(num_seqs, total_nodes, num_q_heads, num_kv_heads, head_dim, q8_dtype_ok(dtype) ? SHARPV_BF16 : dtype);
+}
+
+extern "C" size_t sharpv_tree_attention_q8_workspace_bytes(int32_t num_seqs, int64_t total_nodes, int32_t num_q_heads,
+                                                           int32_t num_kv_heads, int32_t head_dim) {
+    return workspace_bytes(num_seqs, total_nodes, num_q_heads, num_kv_heads, head_dim, SHARPV_E4M3);
+}
+
+extern "C" sharpv_status sharpv_tree_attention(
+    const void* q, int64_t ld_q, const void* draft_k, int64_t ld_draft_k, const void* draft_v, int64_t ld_draft_v,
+    int32_t num_q_heads, const void* kv, const sharpv_kv_layout* layout, int32_t layer, int64_t cache_tokens,
+    int32_t num_seqs, const int32_t* seq_begin, const int32_t* seq_len, const int32_t* node_offsets,
+    int64_t total_nodes, const uint32_t* tree_mask, int32_t mask_words, float scale, void* out, float* out_lse,
+    void* workspace, size_t workspace_bytes, int32_t* status_word, void* cuda_stream) {
+    const sharpv_status ls = kv_layout_status(kv, layout, true);
+    if (ls != SHARPV_OK) return ls;
+    return attend(q, ld_q, draft_k, ld_draft_k, draft_v, ld_draft_v, num_q_heads, kv, layout, nullptr, nullptr,
+                  elem_bytes(layout->dtype), layer, cache_tokens, num_seqs, seq_begin, seq_len, node_offsets, total_nodes, tree_mask,
+                  mask_words, scale, out, out_lse, workspace, workspace_bytes, status_word, cuda_stream);
+}
+
+extern "C" sharpv_status sharpv_tree_attention_q8(
+    const void* q, int64_t ld_q, const void* draft_k, int64_t ld_draft_k, const void* draft_v, int64_t ld_draft_v,
+    int32_t num_q_heads, const void* kv, const sharpv_kv_layout* layout, const uint8_t* scales,
+    const sharpv_kv_scales* scales_layout, int32_t layer, int64_t cache_tokens, int32_t num_seqs, const int32_t* seq_begin,
+    const int32_t* seq_len, const int32_t* node_offsets, int64_t total_nodes, const uint32_t* tree_mask, int32_t mask_words,
+    float scale, void* out, float* out_lse, void* workspace, size_t workspace_bytes, int32_t* status_word, void* cuda_stream) {
+    sharpv_status st = kv_layout_status_if(kv, layout, q8_dtype_ok);
+    if (st != SHARPV_OK) return st;
+    st = kv_scales_status(scales, scales_layout);
+    if (st != SHARPV_OK) return st;
+    return attend(q, ld_q, draft_k, ld_draft_k, draft_v, ld_draft_v, num_q_heads, kv, layout, scales, scales_layout,
+                  elem_bytes(SHARPV_BF16), layer, cache_tokens, num_seqs, seq_begin, seq_len, node_offsets, total_nodes, tree_mask,
+                  mask_words, scale, out, out_lse, workspace, workspace_bytes, status_word, cuda_stream);
 }

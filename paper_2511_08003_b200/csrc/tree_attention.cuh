@@ -36,17 +36,25 @@ struct AttnArgs {
     int ctas;
     int max_segments;           // that there can be
     int32_t* status_word;
+    // caches in 8 bits: the layer's scales of K and V, bytes between heads, log2 of a block's rows
+    const uint8_t* k_scales;
+    const uint8_t* v_scales;
+    int64_t scale_head;
+    int scale_shift;
 };
 
 // Tensor maps of a call (bf16): boxes of 64 columns and a key tile's rows.  draft_* repeat cache_* where there are none.
 struct AttnMaps {
     CUtensorMap cache_k, cache_v, draft_k, draft_v, query;      // query: boxes of whole nodes' rows of one KV head (tcgen05 kernel)
 };
-sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps);
+// box_bytes: a cache in 8 bits, boxes of so many bytes of cache_k and cache_v
+sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps, int box_bytes = 0);
 
 // Few query rows, bf16: a.split has kRowsTileRows rows and kRowsTileKeys keys a tile.  Sets a.ctas to what it launches.
 constexpr int kRowsTileRows = 16, kRowsTileKeys = 64;
 sharpv_status attn_rows_launch(AttnArgs& a, int sms, cudaStream_t stream);
+// the same for a cache in 8 bits
+sharpv_status attn_rows_q8_launch(AttnArgs& a, sharpv_dtype code, int sms, cudaStream_t stream);
 
 // Many query rows, bf16, head_dim and group of at most 128: a.split has tc_rows(group) rows and kTcTileKeys keys a tile.
 // A partial result has room for kTcPlaces rows.  Joins the parts as well.

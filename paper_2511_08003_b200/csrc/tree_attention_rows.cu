@@ -373,13 +373,15 @@ sharpv_status launch(const AttnArgs& a, cudaStream_t stream) {
 
 }  // namespace
 
-sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps) {
+sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps, int box_bytes) {
     const int D = a.head_dim, H = a.split.heads;
     const int64_t T = a.seqs.cache_tokens > 0 ? a.seqs.cache_tokens : 1, N = a.seqs.total_nodes;
     const int64_t most = (int64_t)1 << 40;              // what a tensor map's strides can say
     if (a.kv_token >= most || a.kv_head >= most || a.dk_node >= most || a.dv_node >= most || a.q_node >= most) return SHARPV_ERR_UNSUPPORTED;
-    bool ok = encode_rows_map(&maps.cache_k, a.cache_k, D, T, a.kv_token, H, a.kv_head, box_rows) &&
-              encode_rows_map(&maps.cache_v, a.cache_v, D, T, a.kv_token, H, a.kv_head, box_rows);
+    bool ok = box_bytes ? encode_codes_map(&maps.cache_k, a.cache_k, D, T, a.kv_token, H, a.kv_head, box_rows, box_bytes) &&
+                              encode_codes_map(&maps.cache_v, a.cache_v, D, T, a.kv_token, H, a.kv_head, box_rows, box_bytes)
+                        : encode_rows_map(&maps.cache_k, a.cache_k, D, T, a.kv_token, H, a.kv_head, box_rows) &&
+                              encode_rows_map(&maps.cache_v, a.cache_v, D, T, a.kv_token, H, a.kv_head, box_rows);
     if (a.split.draft)
         ok = ok && encode_rows_map(&maps.draft_k, a.draft_k, D, N, a.dk_node, H, (int64_t)D * 2, box_rows) &&
              encode_rows_map(&maps.draft_v, a.draft_v, D, N, a.dv_node, H, (int64_t)D * 2, box_rows);
