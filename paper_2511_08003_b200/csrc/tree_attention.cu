@@ -454,7 +454,6 @@ struct Choice {
     int max_ctas;           // sizes the workspace
 };
 Choice choose(sharpv_dtype dtype, int head_dim, int group, int64_t avg_rows) {
-    if (q8_dtype_ok(dtype)) return {Path::rows, kRowsTileRows, kRowsTileRows, kMaxRowsCtas};
     if (dtype == SHARPV_F32) return avg_rows <= 8 ? Choice{Path::simt, 8, 8, kMaxAttnCtas} : Choice{Path::simt, 32, 32, kMaxAttnCtas};
     if (head_dim <= 128 && group <= 128 && avg_rows > kMaxRowsPath) return {Path::tc, tc_rows(group), kTcPlaces, kMaxTcCtas};
     return {Path::rows, kRowsTileRows, kRowsTileRows, kMaxRowsCtas};
@@ -547,7 +546,7 @@ sharpv_status attend(
     const sharpv_status ss = current_sms(sms);
     if (ss != SHARPV_OK) return ss;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    if (ch.path == Path::tc) return attn_tc_launch(a, sms, stream);
+    if (ch.path == Path::tc) return attn_tc_launch(a, layout->dtype, sms, stream);
     if (ch.path == Path::rows) {
         const sharpv_status st = scales ? attn_rows_q8_launch(a, layout->dtype, sms, stream) : attn_rows_launch(a, sms, stream);
         return st == SHARPV_OK ? join_launch<SHARPV_BF16>(a, stream) : st;

@@ -56,11 +56,11 @@ sharpv_status attn_rows_launch(AttnArgs& a, int sms, cudaStream_t stream);
 // the same for a cache in 8 bits
 sharpv_status attn_rows_q8_launch(AttnArgs& a, sharpv_dtype code, int sms, cudaStream_t stream);
 
-// Many query rows, bf16, head_dim and group of at most 128: a.split has tc_rows(group) rows and kTcTileKeys keys a tile.
+// Many query rows, bf16 or codes with scales, head_dim and group of at most 128: a.split has tc_rows(group) rows and kTcTileKeys keys a tile.
 // A partial result has room for kTcPlaces rows.  Joins the parts as well.
 constexpr int kTcPlaces = 256, kTcTileKeys = 128, kMaxTcCtas = 160;
 inline int tc_rows(int group) { return 2 * (128 / group * group); }
-sharpv_status attn_tc_launch(AttnArgs& a, int sms, cudaStream_t stream);
+sharpv_status attn_tc_launch(AttnArgs& a, sharpv_dtype dtype, int sms, cudaStream_t stream);
 
 // Which keys of the 32 from key0 on node `i` of a sequence sees, as bits (drafted tokens).
 __device__ __forceinline__ uint32_t draft_sees(const AttnArgs& a, const SeqInfo& s, int i, int key0) {

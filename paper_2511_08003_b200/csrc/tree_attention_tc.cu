@@ -13,9 +13,14 @@
 // query row, so the softmax needs no shuffles.  Sums are rescaled only when a row's maximum has grown by more than 2^8
 // since they last were (weights then stay below 256, which bf16 and the fp32 sums hold as well as 1).
 //
+// Caches in 8 bits (CODE): their tiles go by TMA into a ring of their own, and a warpgroup of four more warps, a key a thread,
+// widens them to bf16 with the key's scale (exactly: scales are powers of two) into the ring that the products read, which
+// also stands in for the cleaning.  All else is the same code: the products see what a bf16 cache would hold.
+//
 // What bounds it is the hand-over between a stream's scores and its products.  Measured with the join (4 KV heads x 128, 7
 // query heads each): a tree of 64 over 50,432 rows 57 us (0.81 PFLOP/s, tensor pipe 48 % active), trees of 5 to 41 over 37,712
 // ragged rows 40.5 us, a chunk of 509 over 10,944 rows 91 us (0.9 PFLOP/s of what its rows see).
+#include "q8.cuh"
 #include "tcgen05.cuh"
 #include "tree_attention.cuh"
 
@@ -26,34 +31,52 @@ namespace {
 
 constexpr int kKeys = kTcTileKeys;              // 128
 constexpr int kRows = 256;                      // places for query rows: 128 a stream
-constexpr int kThreads = 384;
-constexpr int kLoadWarp = 8, kMmaWarp = 9, kAuxWarp = 10;       // warps 0-3, 4-7: the streams; 10, 11: aux
+constexpr int kLoadWarp = 8, kMmaWarp = 9;      // warps 0-3, 4-7: the streams
 constexpr uint32_t kCols = 512, kSumCol = 256;  // tensor memory: scores of stream w at 128 w, sums at 256 + DP w
 constexpr float kLazy = 8.f;
 
-template <int DP>
+template <int DP, int CODE>
 struct Cfg {
+    static constexpr bool kQ8 = CODE != SHARPV_BF16;
     static constexpr int kTileBytes = 128 * DP * 2;             // 128 rows of Q, K or V
-    static constexpr int kStages = DP == 64 ? 10 : 5;           // K and V tiles in turn
+    static constexpr int kStages = kQ8 ? (DP == 64 ? 8 : 4) : (DP == 64 ? 10 : 5);      // K and V tiles in turn
     static constexpr int kHalf = 128 * 128;                     // bytes of a 64-column box
+    static constexpr int kThreads = kQ8 ? 512 : 384;
+    static constexpr int kAuxWarp = kQ8 ? 12 : 10, kAuxWarps = kQ8 ? 4 : 2;
+    // registers of the streams' threads and of the others', at most what the CTA was launched with together
+    static constexpr int kStreamRegs = kQ8 ? 192 : 200, kOtherRegs = kQ8 ? 64 : 96;
+    static_assert(!kQ8 || 256 * kStreamRegs + 256 * kOtherRegs <= 512 * 128, "registers");
+    static_assert(!kQ8 || kStages % 2 == 0, "a stage of the ring holds keys or values, not both in turn");
 };
 
+template <int DP, int CODE>
+struct CodeTiles {
+    static constexpr int kStages = DP == 64 ? 4 : 2;            // K and V in turn
+    uint8_t codes[kStages][128 * DP];
+    uint64_t full8[kStages], empty8[kStages];
+};
 template <int DP>
+struct CodeTiles<DP, SHARPV_BF16> {
+    static constexpr int kStages = 0;
+};
+
+template <int DP, int CODE>
 struct Shared {
-    using C = Cfg<DP>;
+    using C = Cfg<DP, CODE>;
     uint8_t q[2][C::kTileBytes];
     uint8_t tiles[C::kStages][C::kTileBytes];
+    CodeTiles<DP, CODE> c8;
     Portion part[2];                            // kt1 < 0: there are no more
     float m[128], l[128];                       // of stream 1, when the streams share their rows
     uint64_t full[C::kStages], empty[C::kStages];
     uint64_t part_full[2], part_empty[2];
-    uint64_t clean[C::kStages];                 // value tiles: gone through (or nothing to do)
+    uint64_t clean[C::kStages];                 // value tiles: gone through (or nothing to do); 8 bits: any tile, there to be read
     uint64_t q_full, q_empty;
     uint64_t scores[2], weights[2], sums[2];    // per stream: scores formed, weights written, a portion's weighted sums added
     uint64_t merge_full, merge_done, drain;
     int poison[2];
     uint32_t tmem;
-    PlanScratch<kThreads> plan;
+    PlanScratch<C::kThreads> plan;
 };
 
 // what every role derives from a portion
@@ -117,23 +140,199 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
-template <int DP>
-__global__ void __launch_bounds__(kThreads, 1)
+// Four codes times 2^e as bf16, exactly: `f` and, where a second factor is needed, `f2` hold the power of two.
+//   e4m3: a code's exponent and mantissa in the places of bf16's are 2^-120 of its value, subnormal ones too
+//   int8: 128 + the low seven bits, and 128 or 256 by the sign, are bf16 numbers; their difference is the value
+template <int CODE>
+__device__ __forceinline__ void bf16_of(uint32_t codes, __nv_bfloat162 f, bool twice, __nv_bfloat162 f2, uint32_t& lo, uint32_t& hi) {
+    __nv_bfloat162 x[2];
+    if constexpr (CODE == SHARPV_E4M3) {
+        const uint32_t up = (codes >> 4 & 0x07070707u) | (codes & 0x80808080u), down = codes << 4 & 0xf0f0f0f0u;
+        const uint32_t a = __byte_perm(down, up, 0x5140), b = __byte_perm(down, up, 0x7362);
+        x[0] = *reinterpret_cast<const __nv_bfloat162*>(&a);
+        x[1] = *reinterpret_cast<const __nv_bfloat162*>(&b);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t w = __byte_perm(codes, 0x43434343u, i ? 0x4342 : 0x4140);
+            const uint32_t m = w & 0xff7fff7fu, s = w & 0xff80ff80u;
+            x[i] = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&m), *reinterpret_cast<const __nv_bfloat162*>(&s));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        x[i] = __hmul2(x[i], f);
+        if (twice) x[i] = __hmul2(x[i], f2);
+    }
+    lo = *reinterpret_cast<const uint32_t*>(&x[0]);
+    hi = *reinterpret_cast<const uint32_t*>(&x[1]);
+}
+
+// e4m3's NaN, which the above takes for 480: the bytes that are it, and such halves made NaN
+__device__ __forceinline__ uint32_t nan_codes(uint32_t codes) { return ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ void keep_nan(uint32_t codes, uint32_t& lo, uint32_t& hi) {
+    const uint32_t n = nan_codes(codes);
+    lo |= (n & 0x80u ? 0x7fffu : 0u) | (n & 0x8000u ? 0x7fff0000u : 0u);
+    hi |= (n & 0x800000u ? 0x7fffu : 0u) | (n & 0x80000000u ? 0x7fff0000u : 0u);
+}
+
+// The row of a tile of codes that this thread owns, times 2^e, to a tile of bf16; zeros where the row is not there.
+template <int DP, int CODE>
+__device__ __forceinline__ void widen_row(const uint8_t* codes, uint8_t* tile, int row, bool there, int e) {
+    using C = Cfg<DP, CODE>;
+    constexpr int kFree = CODE == SHARPV_E4M3 ? 120 : 0;
+    const int e1 = min(e + kFree, 127), e2 = e + kFree - e1;
+    const __nv_bfloat162 f = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)((e1 + 127) << 7)));
+    const __nv_bfloat162 f2 = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)((e2 + 127) << 7)));
+    const bool twice = __any_sync(0xffffffffu, there && e2 > 0);
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+        if (there) {
+            const uint4 w = *reinterpret_cast<const uint4*>(codes + (DP == 64 ? swizzle64(row, c) : swizzle128(row, c)));
+            if (twice) {
+                bf16_of<CODE>(w.x, f, true, f2, lo.x, lo.y);
+                bf16_of<CODE>(w.y, f, true, f2, lo.z, lo.w);
+                bf16_of<CODE>(w.z, f, true, f2, hi.x, hi.y);
+                bf16_of<CODE>(w.w, f, true, f2, hi.z, hi.w);
+            } else {
+                bf16_of<CODE>(w.x, f, false, f2, lo.x, lo.y);
+                bf16_of<CODE>(w.y, f, false, f2, lo.z, lo.w);
+                bf16_of<CODE>(w.z, f, false, f2, hi.x, hi.y);
+                bf16_of<CODE>(w.w, f, false, f2, hi.z, hi.w);
+            }
+            if (CODE == SHARPV_E4M3 && (nan_codes(w.x) | nan_codes(w.y) | nan_codes(w.z) | nan_codes(w.w))) {
+                keep_nan(w.x, lo.x, lo.y);
+                keep_nan(w.y, lo.z, lo.w);
+                keep_nan(w.z, hi.x, hi.y);
+                keep_nan(w.w, hi.z, hi.w);
+            }
+        }
+        uint8_t* to = tile + (c >> 2) * C::kHalf;
+        *reinterpret_cast<uint4*>(to + swizzle128(row, (c & 3) * 2)) = lo;
+        *reinterpret_cast<uint4*>(to + swizzle128(row, (c & 3) * 2 + 1)) = hi;
+    }
+}
+
+// The warps that widen tiles of codes: every item of the ring (keys, values, keys, ...) in turn, 128 threads, a row each.
+// Drafted tiles, which are bf16, are brought by TMA, asked for by one thread up to two items ahead, and cleaned as in a bf16 cache.
+template <int DP, int CODE, class Wait>
+__device__ __forceinline__ void widen_tiles(const AttnArgs& a, const AttnMaps& maps, Shared<DP, CODE>& sm, Wait& wait_warp, bool& alive) {
+    using C = Cfg<DP, CODE>;
+    constexpr uint32_t kCodeStages = CodeTiles<DP, CODE>::kStages;
+    const int t = threadIdx.x - C::kAuxWarp * 32, lane = threadIdx.x & 31;
+    uint32_t it = 0, codes = 0;                     // items of the ring, and tiles of codes so far
+    uint32_t asked = 0;                             // thread 0: the first item that no drafted tile was asked for
+    uint32_t uses = 0;                              // a bit a stage: parity of the drafted tiles it has had
+    for (uint32_t pn = 0;; ++pn) {
+        if (!wait_warp(&sm.part_full[pn & 1], pn >> 1)) break;
+        const Portion p = sm.part[pn & 1];
+        if (p.kt1 < 0) break;
+        const uint8_t* ks = a.k_scales + p.h * a.scale_head;
+        const uint8_t* vs = a.v_scales + p.h * a.scale_head;
+        auto scale_of = [&](const uint8_t* scales, int kt) {
+            const int key = kt * kKeys + t;
+            return kt < p.kt1 && kt < p.kt_cache && key < p.s.len ? (uint32_t)__ldg(scales + ((p.s.begin + key) >> a.scale_shift)) : 127u;
+        };
+        uint32_t next_k = scale_of(ks, p.kt0), next_v = scale_of(vs, p.kt0);
+        for (int kt = p.kt0; kt < p.kt1 && alive; ++kt) {
+            const int k_exponent = scale_exponent(next_k), v_exponent = scale_exponent(next_v);
+            next_k = scale_of(ks, kt + 1);
+            next_v = scale_of(vs, kt + 1);
+            const bool cached = kt < p.kt_cache;
+            const int left = keys_left(a, p, kt);
+#pragma unroll 1
+            for (int v = 0; v < 2; ++v, ++it) {
+                const int stage = it % C::kStages;
+                uint8_t* tile = sm.tiles[stage];
+                if (it >= (uint32_t)C::kStages && !wait_warp(&sm.empty[stage], it / C::kStages - 1)) break;
+                if (cached) {
+                    const int from = codes % kCodeStages;
+                    if (!wait_warp(&sm.c8.full8[from], codes / kCodeStages)) break;
+                    ++codes;
+                    widen_row<DP, CODE>(sm.c8.codes[from], tile, t, t < left, v ? v_exponent : k_exponent);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sm.c8.empty8[from]);
+                } else if (a.split.draft) {
+                    if (t == 0) {
+                        const uint32_t last = it + 2 * (p.kt1 - kt) - v;        // behind the portion's last item
+                        for (uint32_t i = asked > it ? asked : it; i < last && i <= it + 2; ++i) {
+                            const int at = i % C::kStages;
+                            if (i > it && i >= (uint32_t)C::kStages && !mbar_try(&sm.empty[at], (i / C::kStages - 1) & 1)) break;
+                            const int ahead = v + (int)(i - it), row = p.s.node0 + (kt + ahead / 2 - p.kt_cache) * kKeys;
+                            mbar_expect(&sm.full[at], C::kTileBytes);
+#pragma unroll
+                            for (int x = 0; x < DP / 64; ++x)
+                                tma_load(sm.tiles[at] + x * C::kHalf, ahead % 2 ? &maps.draft_v : &maps.draft_k, &sm.full[at], x * 64, row, p.h);
+                            asked = i + 1;
+                        }
+                    }
+                    __syncwarp();
+                    if (!wait_warp(&sm.full[stage], uses >> stage & 1)) break;
+                    uses ^= 1u << stage;
+                    if (v) {
+                        bool odd = false;
+#pragma unroll 8
+                        for (int x = t; x < 128 * (DP / 8); x += 128) {
+                            const int key = (x >> 3) & 127;         // 128 rows of 8 chunks, then the next 64 columns
+                            uint4* at = reinterpret_cast<uint4*>(tile + x * 16);
+                            if (key >= left) {
+                                *at = make_uint4(0, 0, 0, 0);
+                            } else {
+                                const uint4 w = *at;
+                                if (any_nonfinite(w)) {
+                                    odd = true;
+                                    *at = make_uint4(w.x & ~nonfinite_bf16(w.x), w.y & ~nonfinite_bf16(w.y), w.z & ~nonfinite_bf16(w.z),
+                                                     w.w & ~nonfinite_bf16(w.w));
+                                }
+                            }
+                        }
+                        if (odd) sm.poison[pn & 1] = 1;
+                    }
+                } else if (v) {                     // the empty tile of rows without keys
+                    for (int x = t; x < 128 * (DP / 8); x += 128) *reinterpret_cast<uint4*>(tile + x * 16) = make_uint4(0, 0, 0, 0);
+                }
+                async_proxy_fence();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.clean[stage]);
+            }
+        }
+        if (!alive) break;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.part_empty[pn & 1]);
+    }
+    // given up: drafted tiles in flight land before the CTA ends
+    if (!alive && t == 0)
+        for (uint32_t i = it; i < asked; ++i) {
+            (void)mbar_wait(&sm.full[i % C::kStages], uses >> (i % C::kStages) & 1);
+            uses ^= 1u << (i % C::kStages);
+        }
+}
+
+template <int DP, int CODE>
+__global__ void __launch_bounds__(Cfg<DP, CODE>::kThreads, 1)
 attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnMaps maps) {
-    using C = Cfg<DP>;
+    using C = Cfg<DP, CODE>;
+    [[maybe_unused]] constexpr int kThreads = C::kThreads, kAuxWarp = C::kAuxWarp, kCodeStages = CodeTiles<DP, CODE>::kStages;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    auto& sm = *reinterpret_cast<Shared<DP>*>(smem_raw);
+    auto& sm = *reinterpret_cast<Shared<DP, CODE>*>(smem_raw);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::kStages; ++i) {
             mbar_init(&sm.full[i], 1);
             mbar_init(&sm.empty[i], 1);
-            mbar_init(&sm.clean[i], 2);             // both aux warps
+            mbar_init(&sm.clean[i], C::kAuxWarps);
+        }
+        if constexpr (C::kQ8) {
+            for (uint32_t i = 0; i < kCodeStages; ++i) {
+                mbar_init(&sm.c8.full8[i], 1);
+                mbar_init(&sm.c8.empty8[i], C::kAuxWarps);
+            }
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sm.part_full[i], 1);
-            mbar_init(&sm.part_empty[i], 11);           // the warps that read it
+            mbar_init(&sm.part_empty[i], 9 + C::kAuxWarps);         // the warps that read it
             mbar_init(&sm.scores[i], 1);
             mbar_init(&sm.weights[i], 4);
             mbar_init(&sm.sums[i], 1);
@@ -163,7 +362,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
     };
 
     if (warp >= kLoadWarp) {
-        fewer_registers<96>();
+        fewer_registers<C::kOtherRegs>();
         if (warp == kLoadWarp) {
             if (lane == 0) {
                 Walk walk(plan, first, end);
@@ -190,29 +389,47 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
 #pragma unroll
                         for (int x = 0; x < DP / 64; ++x)
                             tma_load(sm.q[w] + x * C::kHalf, &maps.query, &sm.q_full, x * 64, p.h * G, p.s.node0 + (p.rt * 2 + w) * nodes);
-                    for (int kt = p.kt0; kt < p.kt1 && alive; ++kt) {
-                        const bool drafted = kt >= p.kt_cache;
-                        const int row = drafted ? p.s.node0 + (kt - p.kt_cache) * kKeys : (int)p.s.begin + kt * kKeys;
-                        for (int v = 0; v < 2; ++v, ++it) {
-                            const int stage = it % C::kStages;
-                            if (it >= C::kStages && !wait(&sm.empty[stage], it / C::kStages - 1)) break;
-                            if (drafted && !a.split.draft) {        // the empty tile of rows without keys
-                                mbar_arrive(&sm.full[stage]);
-                                continue;
+                    if constexpr (C::kQ8) {                 // codes; drafted tiles are asked for where tiles are widened
+                        for (int kt = p.kt0; kt < p.kt1 && kt < p.kt_cache && alive; ++kt)
+                            for (int v = 0; v < 2; ++v, ++it) {
+                                const int stage = it % kCodeStages;
+                                if (it >= kCodeStages && !wait(&sm.c8.empty8[stage], it / kCodeStages - 1)) break;
+                                mbar_expect(&sm.c8.full8[stage], 128 * DP);
+                                tma_load(sm.c8.codes[stage], v ? &maps.cache_v : &maps.cache_k, &sm.c8.full8[stage], 0,
+                                         (int)p.s.begin + kt * kKeys, p.h);
                             }
-                            mbar_expect(&sm.full[stage], C::kTileBytes);
-                            const CUtensorMap* map = drafted ? (v ? &maps.draft_v : &maps.draft_k) : (v ? &maps.cache_v : &maps.cache_k);
+                    } else {
+                        for (int kt = p.kt0; kt < p.kt1 && alive; ++kt) {
+                            const bool drafted = kt >= p.kt_cache;
+                            const int row = drafted ? p.s.node0 + (kt - p.kt_cache) * kKeys : (int)p.s.begin + kt * kKeys;
+                            for (int v = 0; v < 2; ++v, ++it) {
+                                const int stage = it % C::kStages;
+                                if (it >= C::kStages && !wait(&sm.empty[stage], it / C::kStages - 1)) break;
+                                if (drafted && !a.split.draft) {        // the empty tile of rows without keys
+                                    mbar_arrive(&sm.full[stage]);
+                                    continue;
+                                }
+                                mbar_expect(&sm.full[stage], C::kTileBytes);
+                                const CUtensorMap* map = drafted ? (v ? &maps.draft_v : &maps.draft_k) : (v ? &maps.cache_v : &maps.cache_k);
 #pragma unroll
-                            for (int x = 0; x < DP / 64; ++x)
-                                tma_load(sm.tiles[stage] + x * C::kHalf, map, &sm.full[stage], x * 64, row, p.h);
+                                for (int x = 0; x < DP / 64; ++x)
+                                    tma_load(sm.tiles[stage] + x * C::kHalf, map, &sm.full[stage], x * 64, row, p.h);
+                            }
                         }
                     }
                 }
                 if (!alive) note_shared(a, false, p, end, plan);    // nothing to join
                 // copies in flight land before the CTA ends, also where the warps that wanted them gave up
-                for (uint32_t i = 0; i < (uint32_t)C::kStages && i < it; ++i) {
-                    const uint32_t at = it - 1 - i;
-                    (void)mbar_wait(&sm.full[at % C::kStages], (at / C::kStages) & 1);
+                if constexpr (C::kQ8) {
+                    for (uint32_t i = 0; i < kCodeStages && i < it; ++i) {
+                        const uint32_t at = it - 1 - i;
+                        (void)mbar_wait(&sm.c8.full8[at % kCodeStages], (at / kCodeStages) & 1);
+                    }
+                } else {
+                    for (uint32_t i = 0; i < (uint32_t)C::kStages && i < it; ++i) {
+                        const uint32_t at = it - 1 - i;
+                        (void)mbar_wait(&sm.full[at % C::kStages], (at / C::kStages) & 1);
+                    }
                 }
                 if (queries > 0) (void)mbar_wait(&sm.q_full, (queries - 1) & 1);
             }
@@ -235,7 +452,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                 auto scores = [&](int t) {                              // scores of step t
                     const int w = t & 1;
                     if (!pair || w == 0) {
-                        if (!wait_warp(&sm.full[kr.stage], kr.round)) return;
+                        if (!wait_warp(C::kQ8 ? &sm.clean[kr.stage] : &sm.full[kr.stage], kr.round)) return;
                     }
                     tc_fence_after();
                     if (elect_one()) {
@@ -288,6 +505,8 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
             if (elect_one()) mma_commit(&sm.drain);
             __syncwarp();
             (void)mbar_wait(&sm.drain, 0);
+        } else if constexpr (C::kQ8) {
+            if (warp >= kAuxWarp) widen_tiles<DP, CODE>(a, maps, sm, wait_warp, alive);
         } else {
             // value tiles with rows that are not there (or, drafted, that some query rows must not see): 0 times what such
             // rows hold would not be 0 if that is not finite
@@ -336,7 +555,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
             }
         }
     } else {
-        more_registers<200>();
+        more_registers<C::kStreamRegs>();
         const int w = warp >> 2, r_in = threadIdx.x & 127;          // stream, row of its tile
         const uint32_t lanes = (uint32_t)(warp & 3) * 32 << 16;
         const uint32_t t_scores = tmem + lanes + w * 128, t_sums = tmem + lanes + kSumCol + w * DP;
@@ -617,14 +836,15 @@ attn_tc_join_kernel(const __grid_constant__ AttnArgs a) {
     if (c4 == 0) a.lse[at] = row_lse(top, sum);
 }
 
-template <int DP>
+template <int DP, int CODE>
 sharpv_status launch(const AttnArgs& a, cudaStream_t stream) {
-    auto kern = attn_tc_kernel<DP>;
-    const size_t smem = sizeof(Shared<DP>);
-    static_assert(sizeof(Shared<DP>) <= 227 * 1024, "shared memory of one CTA");
+    constexpr int kThreads = Cfg<DP, CODE>::kThreads;
+    auto kern = attn_tc_kernel<DP, CODE>;
+    const size_t smem = sizeof(Shared<DP, CODE>);
+    static_assert(sizeof(Shared<DP, CODE>) <= 227 * 1024, "shared memory of one CTA");
     static_assert(kSumCol + 2 * DP <= kCols, "tensor memory");
     AttnMaps maps;
-    const sharpv_status ms = encode_attn_maps(a, kKeys, maps);
+    const sharpv_status ms = encode_attn_maps(a, kKeys, maps, Cfg<DP, CODE>::kQ8 ? DP : 0);
     if (ms != SHARPV_OK) return ms;
     const int64_t all = a.seqs.total_nodes * a.split.group;
     const unsigned rows = (unsigned)(all <= a.split.rows / 2 ? all : kRows);        // places that any segment can use
@@ -644,9 +864,11 @@ sharpv_status launch(const AttnArgs& a, cudaStream_t stream) {
 
 }  // namespace
 
-sharpv_status attn_tc_launch(AttnArgs& a, int sms, cudaStream_t stream) {
+sharpv_status attn_tc_launch(AttnArgs& a, sharpv_dtype dtype, int sms, cudaStream_t stream) {
     a.ctas = sms < kMaxTcCtas ? sms : kMaxTcCtas;
-    return a.head_dim <= 64 ? launch<64>(a, stream) : launch<128>(a, stream);
+    if (dtype == SHARPV_E4M3) return a.head_dim <= 64 ? launch<64, SHARPV_E4M3>(a, stream) : launch<128, SHARPV_E4M3>(a, stream);
+    if (dtype == SHARPV_I8) return a.head_dim <= 64 ? launch<64, SHARPV_I8>(a, stream) : launch<128, SHARPV_I8>(a, stream);
+    return a.head_dim <= 64 ? launch<64, SHARPV_BF16>(a, stream) : launch<128, SHARPV_BF16>(a, stream);
 }
 
 }  // namespace sharpv
