@@ -140,11 +140,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
-// Four codes times 2^e as bf16, exactly: `f` and, where a second factor is needed, `f2` hold the power of two.
+// Four codes times a power of two as bf16, exactly; `f` holds it (and f2 a second factor, where one is not enough).
 //   e4m3: a code's exponent and mantissa in the places of bf16's are 2^-120 of its value, subnormal ones too
 //   int8: 128 + the low seven bits, and 128 or 256 by the sign, are bf16 numbers; their difference is the value
-template <int CODE>
-__device__ __forceinline__ void bf16_of(uint32_t codes, __nv_bfloat162 f, bool twice, __nv_bfloat162 f2, uint32_t& lo, uint32_t& hi) {
+template <int CODE, bool TWICE>
+__device__ __forceinline__ void bf16_of(uint32_t codes, __nv_bfloat162 f, __nv_bfloat162 f2, uint32_t& lo, uint32_t& hi) {
     __nv_bfloat162 x[2];
     if constexpr (CODE == SHARPV_E4M3) {
         const uint32_t up = (codes >> 4 & 0x07070707u) | (codes & 0x80808080u), down = codes << 4 & 0xf0f0f0f0u;
@@ -162,55 +162,68 @@ __device__ __forceinline__ void bf16_of(uint32_t codes, __nv_bfloat162 f, bool t
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         x[i] = __hmul2(x[i], f);
-        if (twice) x[i] = __hmul2(x[i], f2);
+        if constexpr (TWICE) x[i] = __hmul2(x[i], f2);
     }
     lo = *reinterpret_cast<const uint32_t*>(&x[0]);
     hi = *reinterpret_cast<const uint32_t*>(&x[1]);
 }
 
-// e4m3's NaN, which the above takes for 480: the bytes that are it, and such halves made NaN
-__device__ __forceinline__ uint32_t nan_codes(uint32_t codes) { return ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// e4m3's NaN, which the above takes for 480: a carry into the signs' places of codes that are it, and such halves made NaN
+__device__ __forceinline__ uint32_t nan_carry(uint32_t codes) { return (codes & 0x7f7f7f7fu) + 0x01010101u; }
 __device__ __forceinline__ void keep_nan(uint32_t codes, uint32_t& lo, uint32_t& hi) {
-    const uint32_t n = nan_codes(codes);
+    const uint32_t n = nan_carry(codes);
     lo |= (n & 0x80u ? 0x7fffu : 0u) | (n & 0x8000u ? 0x7fff0000u : 0u);
     hi |= (n & 0x800000u ? 0x7fffu : 0u) | (n & 0x80000000u ? 0x7fff0000u : 0u);
 }
 
-// The row of a tile of codes that this thread owns, times 2^e, to a tile of bf16; zeros where the row is not there.
-template <int DP, int CODE>
-__device__ __forceinline__ void widen_row(const uint8_t* codes, uint8_t* tile, int row, bool there, int e) {
-    using C = Cfg<DP, CODE>;
+// 64 columns of a row of codes to their places in 64 columns of a tile of bf16.
+template <int CODE, bool TWICE, bool NAN_TOO>
+__device__ __forceinline__ void write_columns(const uint4 (&w)[4], uint8_t* tile, int row, __nv_bfloat162 f, __nv_bfloat162 f2) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        uint4 lo, hi;
+        bf16_of<CODE, TWICE>(w[c].x, f, f2, lo.x, lo.y);
+        bf16_of<CODE, TWICE>(w[c].y, f, f2, lo.z, lo.w);
+        bf16_of<CODE, TWICE>(w[c].z, f, f2, hi.x, hi.y);
+        bf16_of<CODE, TWICE>(w[c].w, f, f2, hi.z, hi.w);
+        if constexpr (NAN_TOO) {
+            keep_nan(w[c].x, lo.x, lo.y);
+            keep_nan(w[c].y, lo.z, lo.w);
+            keep_nan(w[c].z, hi.x, hi.y);
+            keep_nan(w[c].w, hi.z, hi.w);
+        }
+        *reinterpret_cast<uint4*>(tile + swizzle128(row, c * 2)) = lo;
+        *reinterpret_cast<uint4*>(tile + swizzle128(row, c * 2 + 1)) = hi;
+    }
+}
+
+// The row of a tile of codes that this thread owns, times 2^e, to a tile of bf16; zeros where the row is not there.  `read` is
+// called as soon as the codes are in registers.
+template <int DP, int CODE, class Read>
+__device__ __forceinline__ void widen_row(const uint8_t* codes, uint8_t* tile, int row, bool there, int e, Read read) {
     constexpr int kFree = CODE == SHARPV_E4M3 ? 120 : 0;
     const int e1 = min(e + kFree, 127), e2 = e + kFree - e1;
     const __nv_bfloat162 f = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)((e1 + 127) << 7)));
-    const __nv_bfloat162 f2 = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)((e2 + 127) << 7)));
-    const bool twice = __any_sync(0xffffffffu, there && e2 > 0);
 #pragma unroll
-    for (int c = 0; c < DP / 16; ++c) {
-        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-        if (there) {
-            const uint4 w = *reinterpret_cast<const uint4*>(codes + (DP == 64 ? swizzle64(row, c) : swizzle128(row, c)));
-            if (twice) {
-                bf16_of<CODE>(w.x, f, true, f2, lo.x, lo.y);
-                bf16_of<CODE>(w.y, f, true, f2, lo.z, lo.w);
-                bf16_of<CODE>(w.z, f, true, f2, hi.x, hi.y);
-                bf16_of<CODE>(w.w, f, true, f2, hi.z, hi.w);
-            } else {
-                bf16_of<CODE>(w.x, f, false, f2, lo.x, lo.y);
-                bf16_of<CODE>(w.y, f, false, f2, lo.z, lo.w);
-                bf16_of<CODE>(w.z, f, false, f2, hi.x, hi.y);
-                bf16_of<CODE>(w.w, f, false, f2, hi.z, hi.w);
-            }
-            if (CODE == SHARPV_E4M3 && (nan_codes(w.x) | nan_codes(w.y) | nan_codes(w.z) | nan_codes(w.w))) {
-                keep_nan(w.x, lo.x, lo.y);
-                keep_nan(w.y, lo.z, lo.w);
-                keep_nan(w.z, hi.x, hi.y);
-                keep_nan(w.w, hi.z, hi.w);
-            }
+    for (int half = 0; half < DP / 64; ++half) {
+        uint4 w[4];
+        uint32_t carry = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            w[c] = *reinterpret_cast<const uint4*>(codes + (DP == 64 ? swizzle64(row, c) : swizzle128(row, half * 4 + c)));
+        if (!there) w[0] = w[1] = w[2] = w[3] = make_uint4(0, 0, 0, 0);
+        if constexpr (CODE == SHARPV_E4M3) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) carry |= nan_carry(w[c].x) | nan_carry(w[c].y) | nan_carry(w[c].z) | nan_carry(w[c].w);
         }
-        uint8_t* to = tile + (c >> 2) * C::kHalf;
-        *reinterpret_cast<uint4*>(to + swizzle128(row, (c & 3) * 2)) = lo;
-        *reinterpret_cast<uint4*>(to + swizzle128(row, (c & 3) * 2 + 1)) = hi;
+        if (half == DP / 64 - 1) read();
+        uint8_t* to = tile + half * Cfg<DP, CODE>::kHalf;
+        if (__all_sync(0xffffffffu, e2 == 0 && (carry & 0x80808080u) == 0)) {
+            write_columns<CODE, false, false>(w, to, row, f, f);
+        } else {
+            const __nv_bfloat162 f2 = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)((e2 + 127) << 7)));
+            write_columns<CODE, true, CODE == SHARPV_E4M3>(w, to, row, f, f2);
+        }
     }
 }
 
@@ -224,36 +237,57 @@ __device__ __forceinline__ void widen_tiles(const AttnArgs& a, const AttnMaps& m
     uint32_t it = 0, codes = 0;                     // items of the ring, and tiles of codes so far
     uint32_t asked = 0;                             // thread 0: the first item that no drafted tile was asked for
     uint32_t uses = 0;                              // a bit a stage: parity of the drafted tiles it has had
+    auto ready = [&] {                              // the tile of item `it` may be read by the products
+        async_proxy_fence();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.clean[it % C::kStages]);
+    };
+    auto free_tile = [&] { return it < (uint32_t)C::kStages || wait_warp(&sm.empty[it % C::kStages], it / C::kStages - 1); };
     for (uint32_t pn = 0;; ++pn) {
         if (!wait_warp(&sm.part_full[pn & 1], pn >> 1)) break;
-        const Portion p = sm.part[pn & 1];
+        const Portion& p = sm.part[pn & 1];
         if (p.kt1 < 0) break;
-        const uint8_t* ks = a.k_scales + p.h * a.scale_head;
-        const uint8_t* vs = a.v_scales + p.h * a.scale_head;
-        auto scale_of = [&](const uint8_t* scales, int kt) {
-            const int key = kt * kKeys + t;
-            return kt < p.kt1 && kt < p.kt_cache && key < p.s.len ? (uint32_t)__ldg(scales + ((p.s.begin + key) >> a.scale_shift)) : 127u;
-        };
-        uint32_t next_k = scale_of(ks, p.kt0), next_v = scale_of(vs, p.kt0);
-        for (int kt = p.kt0; kt < p.kt1 && alive; ++kt) {
-            const int k_exponent = scale_exponent(next_k), v_exponent = scale_exponent(next_v);
-            next_k = scale_of(ks, kt + 1);
-            next_v = scale_of(vs, kt + 1);
-            const bool cached = kt < p.kt_cache;
+        {
+            // the row's key in the sequence, its scales a tile ahead
+            const int end = min(p.kt1, p.kt_cache), len = p.s.len;
+            const int64_t begin = p.s.begin;
+            const uint8_t* ks = a.k_scales + p.h * a.scale_head;
+            const uint8_t* vs = a.v_scales + p.h * a.scale_head;
+            int key = p.kt0 * kKeys + t;
+            uint32_t next_k = 127, next_v = 127;
+            auto look_up = [&] {
+                if (key < len) {
+                    next_k = __ldg(ks + ((begin + key) >> a.scale_shift));
+                    next_v = __ldg(vs + ((begin + key) >> a.scale_shift));
+                }
+            };
+            if (p.kt0 < end) look_up();
+            for (int kt = p.kt0; kt < end && alive; ++kt) {
+                const bool there = key < len;
+                int e = scale_exponent(next_k), then = scale_exponent(next_v);
+                key += kKeys;
+                if (kt + 1 < end) look_up();
+#pragma unroll 1
+                for (int v = 0; v < 2; ++v, ++it, ++codes) {
+                    const uint32_t from = codes % kCodeStages;
+                    if (!free_tile() || !wait_warp(&sm.c8.full8[from], codes / kCodeStages)) break;
+                    widen_row<DP, CODE>(sm.c8.codes[from], sm.tiles[it % C::kStages], t, there, e, [&] {
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sm.c8.empty8[from]);
+                    });
+                    ready();
+                    e = then;
+                }
+            }
+        }
+        for (int kt = max(p.kt0, p.kt_cache); kt < p.kt1 && alive; ++kt) {
             const int left = keys_left(a, p, kt);
 #pragma unroll 1
             for (int v = 0; v < 2; ++v, ++it) {
                 const int stage = it % C::kStages;
                 uint8_t* tile = sm.tiles[stage];
-                if (it >= (uint32_t)C::kStages && !wait_warp(&sm.empty[stage], it / C::kStages - 1)) break;
-                if (cached) {
-                    const int from = codes % kCodeStages;
-                    if (!wait_warp(&sm.c8.full8[from], codes / kCodeStages)) break;
-                    ++codes;
-                    widen_row<DP, CODE>(sm.c8.codes[from], tile, t, t < left, v ? v_exponent : k_exponent);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sm.c8.empty8[from]);
-                } else if (a.split.draft) {
+                if (!free_tile()) break;
+                if (a.split.draft) {
                     if (t == 0) {
                         const uint32_t last = it + 2 * (p.kt1 - kt) - v;        // behind the portion's last item
                         for (uint32_t i = asked > it ? asked : it; i < last && i <= it + 2; ++i) {
@@ -272,7 +306,7 @@ __device__ __forceinline__ void widen_tiles(const AttnArgs& a, const AttnMaps& m
                     uses ^= 1u << stage;
                     if (v) {
                         bool odd = false;
-#pragma unroll 8
+#pragma unroll 4
                         for (int x = t; x < 128 * (DP / 8); x += 128) {
                             const int key = (x >> 3) & 127;         // 128 rows of 8 chunks, then the next 64 columns
                             uint4* at = reinterpret_cast<uint4*>(tile + x * 16);
@@ -292,9 +326,7 @@ __device__ __forceinline__ void widen_tiles(const AttnArgs& a, const AttnMaps& m
                 } else if (v) {                     // the empty tile of rows without keys
                     for (int x = t; x < 128 * (DP / 8); x += 128) *reinterpret_cast<uint4*>(tile + x * 16) = make_uint4(0, 0, 0, 0);
                 }
-                async_proxy_fence();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sm.clean[stage]);
+                ready();
             }
         }
         if (!alive) break;
