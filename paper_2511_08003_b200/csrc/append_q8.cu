@@ -7,14 +7,21 @@
 // A block needs its largest value before its first code, so a team of threads takes whole blocks: it loads up to kVecs 16-byte
 // vectors a thread, keeps them in registers, finds the blocks' largest values (bits of non-negative floats order as
 // integers: one warp reduction and one atomic of shared memory a warp), and writes codes from the registers: every
-// row is read once.  Blocks that are larger than what a team holds are read twice, the second time out of L2.
-// Maxima do not depend on the order of atomics, multiplying by a power of two is exact, and one rounding remains.
+// row is read once, and one barrier a plane is enough.  Blocks that are larger than what a team holds are read twice, the second
+// time out of L2.  Maxima do not depend on the order of atomics, multiplying by a power of two is exact, and one rounding remains.
 //
 // A team is a CTA where sequences receive many rows, and a warp where they receive a few (accepted tokens: 224 planes x
-// 16 sequences of 1 to 6 rows are 3,584 small pieces, which have to be resident together).
+// 16 sequences of 1 to 6 rows are 3,584 small pieces, which have to be resident together).  Where there are many tiles a team
+// takes several planes of one: what the tables say of the tile holds for all of them.
+//
+// The arithmetic is kept to about two instructions an element either way, or it would be what bounds it: largest values are found
+// two at a time in the source's own type, products with powers of two are formed two at a time, and rounding to whole
+// numbers is the addition of a number whose last place is 1.
 //
 // HBM bounds long lists, latency (tables, rows, maximum, codes) short ones.
 #include "q8.cuh"
+
+#include <cuda_bf16.h>
 
 namespace sharpv {
 namespace {
@@ -32,7 +39,9 @@ struct AppendQ8Args {
     int64_t src_tokens, dst_tokens;
     int src_shift, dst_shift;           // log2 of the blocks' rows
     int num_kv_heads, layer_begin, planes, row_vecs, code_vecs;     // 16-byte vectors of a source row, of a row of codes
+    uint32_t row_inverse;               // 2^32 / row_vecs, rounded up: the high word of a product with it is the quotient; 0 for 1
     int tile_rows;                      // a multiple of the block's rows
+    int team_planes;                    // that a team takes of a tile, one after the other
     const int32_t* src_pos;
     const int32_t* offsets;
     const int32_t* dst_begin;
@@ -41,12 +50,46 @@ struct AppendQ8Args {
     int32_t* status_word;
 };
 
-template <int SRC> struct Source {      // a 16-byte vector as fp32
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
+__device__ __forceinline__ uint32_t bits_of(__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); }
+__device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); }
+
+// Low bytes of four words.
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+
+// What a source's 16-byte vector gives: its largest finite |value| (bits of fp32, without the source's scale), whether something
+// in it is not finite, and its values as fp32.
+template <int SRC> struct Source {
     static constexpr int kPerVec = Elem<SRC>::kPerVec;
+    static constexpr bool kCodes = false;
     __device__ __forceinline__ static void widen(const uint4& v, float (&x)[kPerVec]) { Elem<SRC>::widen(v, x); }
+    __device__ __forceinline__ static uint32_t top(const uint4& v, bool& odd) {
+        uint32_t m;
+        if constexpr (SRC == SHARPV_F32) {
+            m = max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu));
+        } else {
+            const uint32_t t = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+            m = max(t & 0xffff0000u, t << 16);
+        }
+        odd = m >= 0x7f800000u;
+        if (odd) {
+            float x[kPerVec];
+            widen(v, x);
+            m = 0;
+#pragma unroll
+            for (int e = 0; e < kPerVec; ++e) {
+                const uint32_t y = __float_as_uint(x[e]) & 0x7fffffffu;
+                m = max(m, y < 0x7f800000u ? y : 0u);
+            }
+        }
+        return m;
+    }
 };
 template <int CODE> struct CodeSource {
     static constexpr int kPerVec = 16;
+    static constexpr bool kCodes = true;
     __device__ __forceinline__ static void widen(const uint4& v, float (&x)[16]) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -57,15 +100,92 @@ template <int CODE> struct CodeSource {
             for (int j = 0; j < 4; ++j) x[4 * i + j] = y[j];
         }
     }
+    __device__ __forceinline__ static uint32_t top(const uint4& v, bool& odd) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t m = 0;                         // two at a time, the larger magnitude of codes in halves of a word
+        odd = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (CODE == SHARPV_E4M3) {
+                m = __vmaxu2(__vmaxu2(w[i] & 0x007f007fu, w[i] >> 8 & 0x007f007fu), m);
+            } else {                            // |x| of signed bytes in the high places of halves
+                m = __vmaxu2(__vmaxu2(__vabs2(w[i] & 0xff00ff00u), __vabs2(w[i] << 8 & 0xff00ff00u)), m);
+            }
+        }
+        m = max(m >> 16, m & 0xffffu);
+        if constexpr (CODE == SHARPV_E4M3) {
+            odd = m == 0x7fu;
+            if (odd) {                          // NaN: the largest of the others
+                m = 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t y = w[i / 4] >> (i % 4 * 8) & 0x7fu;
+                    m = max(m, y < 0x7fu ? y : 0u);
+                }
+            }
+            return __float_as_uint(__half2float(__low2half(as_half2(half2_of_e4m3((uint16_t)m)))));
+        } else {
+            return __float_as_uint((float)(m >> 8));
+        }
+    }
 };
 template <> struct Source<SHARPV_E4M3> : CodeSource<SHARPV_E4M3> {};
 template <> struct Source<SHARPV_I8> : CodeSource<SHARPV_I8> {};
 
-template <int CODE, int P>
-__device__ __forceinline__ void store_codes(uint8_t* to, const float (&x)[P], float f) {
+// The codes of a vector's values times 2^k.  `plain`: everything in it is finite and no product is beyond the largest code.
+template <int SRC, int CODE>
+__device__ __forceinline__ void store_codes(uint8_t* to, const uint4& v, int k, bool plain) {
+    using S = Source<SRC>;
+    constexpr int P = S::kPerVec;
     uint32_t w[P / 4];
+    if constexpr (SRC == CODE) {
+        // fp16 holds the codes and the products that round to something; 2^-24 takes what is below to 0 as well, and k > 15 only
+        // goes with codes under 2^-7 (e4m3) or none (int8)
+        const uint32_t c[4] = {v.x, v.y, v.z, v.w};
+        const __half2 f = __float2half2_rn(power_of_two(min(max(k, -24), 15)));
+        const bool more = CODE == SHARPV_E4M3 && k > 15;
+        const __half2 g = __float2half2_rn(power_of_two(min(max(k - 15, 0), 2)));
 #pragma unroll
-    for (int i = 0; i < P / 4; ++i) w[i] = to_codes<CODE>(x[4 * i] * f, x[4 * i + 1] * f, x[4 * i + 2] * f, x[4 * i + 3] * f);
+        for (int i = 0; i < 4; ++i) {
+            uint32_t lo, hi;
+            halves_of<CODE>(c[i], lo, hi);
+            if constexpr (CODE == SHARPV_E4M3) {
+                __half2 a = __hmul2(as_half2(lo), f), b = __hmul2(as_half2(hi), f);
+                if (more) {
+                    a = __hmul2(a, g);
+                    b = __hmul2(b, g);
+                }
+                asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f16x2 l, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 h, %2;\n\tmov.b32 %0, {l, h};\n\t}"
+                    : "=r"(w[i]) : "r"(bits_of(a)), "r"(bits_of(b)));
+            } else {
+                const __half2 one = __float2half2_rn(1536.f);       // whole numbers from here to 2048
+                const uint32_t a = bits_of(__hfma2(as_half2(lo), f, one)), b = bits_of(__hfma2(as_half2(hi), f, one));
+                w[i] = __byte_perm(a, b, 0x6420);
+            }
+        }
+    } else {
+        const float f = power_of_two(k);
+        float x[P];
+        if constexpr (SRC == SHARPV_BF16) {
+            const __nv_bfloat162 f2 = __float2bfloat162_rn(f);
+            const __nv_bfloat162 y[4] = {__hmul2(as_bf162(v.x), f2), __hmul2(as_bf162(v.y), f2), __hmul2(as_bf162(v.z), f2), __hmul2(as_bf162(v.w), f2)};
+            S::widen(*reinterpret_cast<const uint4*>(y), x);
+        } else {
+            S::widen(v, x);
+#pragma unroll
+            for (int e = 0; e < P; ++e) x[e] *= f;
+        }
+        if (CODE == SHARPV_I8 && plain) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) x[i] += 12582912.f;         // 1.5 * 2^23: its last place is 1
+#pragma unroll
+            for (int i = 0; i < P / 4; ++i)
+                w[i] = low_bytes(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < P / 4; ++i) w[i] = to_codes<CODE>(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+        }
+    }
     if constexpr (P == 4) __stcs(reinterpret_cast<uint32_t*>(to), w[0]);
     else if constexpr (P == 8) __stcs(reinterpret_cast<uint2*>(to), make_uint2(w[0], w[1]));
     else st_stream(to, make_uint4(w[0], w[1], w[2], w[3]));
@@ -73,9 +193,7 @@ __device__ __forceinline__ void store_codes(uint8_t* to, const float (&x)[P], fl
 
 struct Team {
     int from[kMaxTileRows];             // source row of a row of the tile; -1: none
-    float unit[kMaxTileRows];           // scale of that row (sources in 8 bits)
-    uint32_t top[kMaxTileRows];         // of the tile's blocks: bits of the largest value, then the exponent
-    int old;                            // of the first block, where rows lie in front
+    uint32_t top[3][kMaxTileRows];      // of the tile's blocks: bits of the largest value; a plane after the other
 };
 
 template <int SRC, int CODE, int TEAM, int VECS>
@@ -83,26 +201,27 @@ __global__ void __launch_bounds__(kThreads, VECS > 4 ? 3 : 4)
 kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
     using S = Source<SRC>;
     constexpr int P = S::kPerVec, kTeams = kThreads / TEAM;
-    constexpr bool kCodes = SRC == SHARPV_E4M3 || SRC == SHARPV_I8;
     __shared__ Team teams[kTeams];
     auto sync = [] { if constexpr (TEAM == 32) __syncwarp(); else __syncthreads(); };
     const int tid = threadIdx.x % TEAM, lane = threadIdx.x & 31;
     Team& sm = teams[threadIdx.x / TEAM];
-    const int plane = blockIdx.y * kTeams + threadIdx.x / TEAM;
+    const int plane0 = (blockIdx.y * kTeams + threadIdx.x / TEAM) * a.team_planes;
     cudaGridDependencySynchronize();
-    if (plane >= a.planes) return;
-    const int h = plane % a.num_kv_heads, kv = (plane / a.num_kv_heads) & 1, l = a.layer_begin + plane / (2 * a.num_kv_heads);
+    if (plane0 >= a.planes) return;
     const int64_t all = __ldg(a.offsets + a.num_seqs);
     const int64_t n = min(max(all, (int64_t)0), a.capacity);
-    const bool speaks = plane == 0 && tid == 0;
+    const bool speaks = plane0 == 0 && tid == 0;
     if (speaks && blockIdx.x == 0 && all > a.capacity) report(a.status_word, SHARPV_ERR_CAPACITY);
     // sequence b has the CTAs from offsets[b] / tile_rows + b on: enough for its tiles but one, which its last CTA takes as well
     auto offset = [&](int b) { return min(max((int64_t)__ldg(a.offsets + b), (int64_t)0), n); };
     auto first_cta = [&](int b) { return (int64_t)((uint32_t)offset(b) / (uint32_t)a.tile_rows) + b; };
     int b = 0;
-    for (int hi = a.num_seqs; hi - b > 1;) {
-        const int mid = (b + hi) >> 1;
-        if (first_cta(mid) <= blockIdx.x) b = mid; else hi = mid;
+    for (int left = a.num_seqs; left > 1;) {                // a warp narrows 32 ways a round
+        const int step = (left + 31) / 32, at = lane * step;
+        const uint32_t not_behind = __ballot_sync(0xffffffffu, at < left && first_cta(b + at) <= blockIdx.x);
+        const int skip = max(__popc(not_behind) - 1, 0) * step;
+        b += skip;
+        left = min(step, left - skip);
     }
     const int64_t j0 = offset(b), j1 = max(offset(b + 1), j0), begin = __ldg(a.dst_begin + b);
     // rows of dst [lo, hi) of this sequence; row t holds list entry j0 + t - begin
@@ -114,11 +233,8 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
     const int64_t tiles = (hi - base + a.tile_rows - 1) / a.tile_rows;
     const int64_t mine = blockIdx.x - first_cta(b), ctas = first_cta(b + 1) - first_cta(b);
     if (mine < 0) return;               // offsets that do not begin at 0
-    const char* s = a.src + l * a.src_layer + kv * a.src_kv + h * a.src_head;
-    const uint8_t* ss = kCodes ? a.src_scales + l * a.ss_layer + kv * a.ss_kv + h * a.ss_head : nullptr;
-    uint8_t* d = a.dst + l * a.dst_layer + kv * a.dst_kv + h * a.dst_head;
-    uint8_t* ds = a.dst_scales + l * a.ds_layer + kv * a.ds_kv + h * a.ds_head;
 
+    int turn = 0;                       // which of the three lists of largest values
     for (int64_t tile = mine; tile < (mine + 1 == ctas ? tiles : min(tiles, mine + 1)); ++tile) {
         const int64_t row0 = base + tile * a.tile_rows;
         const int rows = (int)min((int64_t)a.tile_rows, hi - row0), blocks = (rows + block_rows - 1) >> a.dst_shift;
@@ -129,96 +245,116 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
             if (r >= lead) {
                 const int64_t f = __ldg(a.src_pos + j0 + (row0 + r - begin));
                 if (f >= 0 && f < a.src_tokens) from = (int)f;
-                else if (plane == 0) report(a.status_word, SHARPV_ERR_BOUNDS);
+                else if (plane0 == 0) report(a.status_word, SHARPV_ERR_BOUNDS);
             }
             sm.from[r] = from;
-            if constexpr (kCodes) sm.unit[r] = from >= 0 ? power_of_two(scale_exponent(__ldg(ss + (from >> a.src_shift)))) : 0.f;
         }
-        for (int i = tid; i < blocks; i += TEAM) sm.top[i] = 0;
-        if (tid == 0 && lead > 0) sm.old = scale_exponent(ds[row0 >> a.dst_shift]);
+        for (int i = tid; i < blocks; i += TEAM) sm.top[0][i] = sm.top[1][i] = sm.top[2][i] = 0;
         sync();
-        const int vecs = rows * a.row_vecs, block_vecs = a.row_vecs << a.dst_shift;
-        const bool whole_warps = block_vecs % 32 == 0;
-        uint4 v[VECS];
-        unsigned there = 0;
-        auto load = [&](int q0) {
-            there = 0;
+        const int vecs = (rows - lead) * a.row_vecs;
+        const bool aligned = blocks == 1 || (((lead * a.row_vecs) | (a.row_vecs << a.dst_shift)) & 31) == 0;    // a warp's vectors lie in one block
+        uint8_t* const d_tile = a.dst + row0 * a.dst_token;
+        uint8_t* const ds_tile = a.dst_scales + (row0 >> a.dst_shift);
+        for (int plane = plane0; plane < min(plane0 + a.team_planes, a.planes); ++plane) {
+            const int h = plane % a.num_kv_heads, kv = (plane / a.num_kv_heads) & 1, l = a.layer_begin + plane / (2 * a.num_kv_heads);
+            const char* s = a.src + l * a.src_layer + kv * a.src_kv + h * a.src_head;
+            uint8_t* d = d_tile + l * a.dst_layer + kv * a.dst_kv + h * a.dst_head;
+            uint8_t* ds = ds_tile + l * a.ds_layer + kv * a.ds_kv + h * a.ds_head;
+            uint32_t* tops = sm.top[turn];
+            const int old = lead > 0 ? scale_exponent(*ds) : kScaleLeast;       // of the first block's rows in front
+            uint4 v[VECS];
+            int unit[S::kCodes ? VECS : 1];         // exponent of the source's scale
+            unsigned there = 0, odd = 0;
+            auto row_of = [&](int q) { return lead + (a.row_inverse ? (int)__umulhi((uint32_t)q, a.row_inverse) : q); };
+            auto load = [&](int q0) {
+                there = 0;
 #pragma unroll
-            for (int u = 0; u < VECS; ++u) {
-                const int q = q0 + u * TEAM + tid, r = q / a.row_vecs;
-                if (q < vecs && sm.from[r] >= 0) {
-                    v[u] = ld_stream(s + sm.from[r] * a.src_token + (int64_t)(q - r * a.row_vecs) * 16);
-                    there |= 1u << u;
-                }
-            }
-        };
-        for (int q0 = 0; q0 < vecs; q0 += VECS * TEAM) {
-            load(q0);
-#pragma unroll
-            for (int u = 0; u < VECS; ++u) {
-                const int q = q0 + u * TEAM + tid;
-                uint32_t top = 0;
-                if (there >> u & 1) {
-                    float x[P];
-                    S::widen(v[u], x);
-#pragma unroll
-                    for (int e = 0; e < P; ++e) {
-                        const uint32_t m = __float_as_uint(x[e]) & 0x7fffffffu;
-                        top = max(top, m < 0x7f800000u ? m : 0u);
+                for (int u = 0; u < VECS; ++u) {
+                    const int q = q0 + u * TEAM + tid, r = row_of(q);
+                    if (q < vecs) {
+                        const int from = sm.from[r];
+                        if (from >= 0) {
+                            there |= 1u << u;
+                            v[u] = ld_stream(s + from * a.src_token + (q - (r - lead) * a.row_vecs) * 16);
+                            if constexpr (S::kCodes)
+                                unit[u] = scale_exponent(__ldg(a.src_scales + l * a.ss_layer + kv * a.ss_kv + h * a.ss_head + (from >> a.src_shift)));
+                        }
                     }
-                    if constexpr (kCodes) top = __float_as_uint(__uint_as_float(top) * sm.unit[q / a.row_vecs]);
                 }
-                if (whole_warps) {              // the warp's 32 vectors lie in one block
-                    top = __reduce_max_sync(0xffffffffu, top);
-                    if (lane == 0 && top) atomicMax(&sm.top[q / block_vecs], top);
-                } else if (top) {
-                    atomicMax(&sm.top[q / block_vecs], top);
-                }
-            }
-        }
-        sync();
-        for (int i = tid; i < blocks; i += TEAM) {
-            int e = exponent_for<CODE>(sm.top[i]);
-            if (i == 0 && lead > 0) e = max(e, sm.old);
-            sm.top[i] = (uint32_t)e;
-            ds[(row0 >> a.dst_shift) + i] = (uint8_t)(e + 127);
-        }
-        sync();
-        for (int q0 = 0; q0 < vecs; q0 += VECS * TEAM) {
-            if (vecs > VECS * TEAM) load(q0);
+            };
+            for (int q0 = 0; q0 < vecs; q0 += VECS * TEAM) {
+                load(q0);
 #pragma unroll
-            for (int u = 0; u < VECS; ++u) {
-                const int q = q0 + u * TEAM + tid;
-                if (!(there >> u & 1)) continue;
-                const int r = q / a.row_vecs;
-                float x[P], f = power_of_two(-(int)sm.top[r >> a.dst_shift]);
-                S::widen(v[u], x);
-                if constexpr (kCodes) f *= sm.unit[r];
-                store_codes<CODE>(d + (row0 + r) * a.dst_token + (int64_t)(q - r * a.row_vecs) * P, x, f);
+                for (int u = 0; u < VECS; ++u) {
+                    uint32_t top = 0;
+                    if (there >> u & 1) {
+                        bool strange;
+                        top = S::top(v[u], strange);
+                        if (strange) odd |= 1u << u;
+                        if constexpr (S::kCodes) top = __float_as_uint(__uint_as_float(top) * power_of_two(unit[u]));
+                    }
+                    if (aligned) {
+                        top = __reduce_max_sync(0xffffffffu, top);
+                        if (lane == 0 && top) atomicMax(&tops[row_of(q0 + u * TEAM + tid) >> a.dst_shift], top);
+                    } else if (top) {
+                        atomicMax(&tops[row_of(q0 + u * TEAM + tid) >> a.dst_shift], top);
+                    }
+                }
             }
-        }
-        if (lead > 0 && (int)sm.top[0] != sm.old) {         // rows in front, by the new scale
-            const float f = power_of_two(sm.old - (int)sm.top[0]);
-            for (int q = tid; q < lead * a.code_vecs; q += TEAM) {
-                const int r = q / a.code_vecs;
-                uint4* at = reinterpret_cast<uint4*>(d + (row0 + r) * a.dst_token) + (q - r * a.code_vecs);
-                float x[16];
-                CodeSource<CODE>::widen(*at, x);
-                store_codes<CODE>(reinterpret_cast<uint8_t*>(at), x, f);
+            sync();
+            // the list after the next: nobody reads it any more, and nobody adds to it before the next barrier
+            for (int i = tid; i < blocks; i += TEAM) sm.top[turn == 0 ? 2 : turn - 1][i] = 0;
+            auto exponent = [&](int block) {
+                const int e = exponent_for<CODE>(tops[block]);
+                return block == 0 ? max(e, old) : e;
+            };
+            for (int i = tid; i < blocks; i += TEAM) ds[i] = (uint8_t)(exponent(i) + 127);
+            for (int q0 = 0; q0 < vecs; q0 += VECS * TEAM) {
+                if (vecs > VECS * TEAM) load(q0);
+#pragma unroll
+                for (int u = 0; u < VECS; ++u) {
+                    if (!(there >> u & 1)) continue;
+                    const int q = q0 + u * TEAM + tid, r = row_of(q), e = exponent(r >> a.dst_shift);
+                    // several goes: what was seen in a vector is not kept, so each is taken for strange
+                    const bool plain = !(odd >> u & 1) && e < kScaleMost && vecs <= VECS * TEAM;
+                    store_codes<SRC, CODE>(d + r * a.dst_token + (q - (r - lead) * a.row_vecs) * P, v[u], (S::kCodes ? unit[S::kCodes ? u : 0] : 0) - e, plain);
+                }
             }
+            if (lead > 0 && exponent(0) != old) {                   // rows in front, by the new scale
+                const int k = old - exponent(0), all_vecs = lead * a.code_vecs;
+                constexpr int kAhead = 4;
+                for (int q0 = tid; q0 < all_vecs; q0 += kAhead * TEAM) {
+                    uint4 w[kAhead];
+                    uint8_t* at[kAhead];
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        const int q = q0 + u * TEAM, r = q / a.code_vecs;
+                        at[u] = d + r * a.dst_token + (q - r * a.code_vecs) * 16;
+                        if (q < all_vecs) w[u] = *reinterpret_cast<const uint4*>(at[u]);
+                    }
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u)
+                        if (q0 + u * TEAM < all_vecs) store_codes<CODE, CODE>(at[u], w[u], k, false);
+                }
+            }
+            turn = turn == 2 ? 0 : turn + 1;
         }
     }
 }
 
 template <int SRC, int CODE, int TEAM, int VECS>
-sharpv_status launch(AppendQ8Args& a, cudaStream_t stream) {
+sharpv_status launch(AppendQ8Args& a, int sms, cudaStream_t stream) {
     const int block_rows = 1 << a.dst_shift;
     int rows = VECS * TEAM / a.row_vecs / block_rows * block_rows;      // what a team holds, in whole blocks; one at least
     if (rows < block_rows) rows = block_rows;
     if (rows > kMaxTileRows) rows = kMaxTileRows;
     a.tile_rows = rows;
     const int64_t ctas = a.capacity / rows + a.num_seqs;
-    const int y = (a.planes + kThreads / TEAM - 1) / (kThreads / TEAM);
+    // several planes a team as long as there are sixteen times as many teams as SMs hold
+    constexpr int kTeams = kThreads / TEAM;
+    a.team_planes = 1;
+    while (a.team_planes < 8 && ctas * a.planes / (2 * a.team_planes) >= (int64_t)sms * kTeams * 4 * 16) a.team_planes *= 2;
+    const int y = (a.planes + kTeams * a.team_planes - 1) / (kTeams * a.team_planes);
     if (ctas >= (int64_t)1 << 31 || y > 65535) return SHARPV_ERR_UNSUPPORTED;
     if (launch_dependent(kv_append_q8_kernel<SRC, CODE, TEAM, VECS>, dim3((unsigned)ctas, (unsigned)y), dim3(kThreads), 0, stream, a) !=
         cudaSuccess) {
@@ -229,18 +365,18 @@ sharpv_status launch(AppendQ8Args& a, cudaStream_t stream) {
 }
 
 template <int SRC, int CODE>
-sharpv_status by_size(AppendQ8Args& a, cudaStream_t stream) {
+sharpv_status by_size(AppendQ8Args& a, int sms, cudaStream_t stream) {
     // a warp a piece where a sequence's rows are no more than a warp takes in two goes; else a CTA, with eight vectors a thread
     // where four do not hold a block
     const int64_t vecs = a.capacity / a.num_seqs * a.row_vecs;
-    if (vecs <= 2 * 4 * 32) return launch<SRC, CODE, 32, 4>(a, stream);
-    if ((a.row_vecs << a.dst_shift) <= 4 * kThreads) return launch<SRC, CODE, kThreads, 4>(a, stream);
-    return launch<SRC, CODE, kThreads, 8>(a, stream);
+    if (vecs <= 2 * 4 * 32) return launch<SRC, CODE, 32, 4>(a, sms, stream);
+    if ((a.row_vecs << a.dst_shift) <= 4 * kThreads) return launch<SRC, CODE, kThreads, 4>(a, sms, stream);
+    return launch<SRC, CODE, kThreads, 8>(a, sms, stream);
 }
 
 template <int SRC>
-sharpv_status by_code(AppendQ8Args& a, sharpv_dtype code, cudaStream_t stream) {
-    return code == SHARPV_E4M3 ? by_size<SRC, SHARPV_E4M3>(a, stream) : by_size<SRC, SHARPV_I8>(a, stream);
+sharpv_status by_code(AppendQ8Args& a, sharpv_dtype code, int sms, cudaStream_t stream) {
+    return code == SHARPV_E4M3 ? by_size<SRC, SHARPV_E4M3>(a, sms, stream) : by_size<SRC, SHARPV_I8>(a, sms, stream);
 }
 
 // the bytes that the scales of `rows` rows of the planes of the layers span
@@ -327,11 +463,15 @@ extern "C" sharpv_status sharpv_kv_append_q8(
     a.num_seqs = num_seqs;
     a.capacity = capacity;
     a.status_word = status_word;
+    a.row_inverse = row_vecs == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + row_vecs - 1) / row_vecs);
+    int sms = 0;
+    st = current_sms(sms);
+    if (st != SHARPV_OK) return st;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     switch (src_layout->dtype) {
-        case SHARPV_F32: return by_code<SHARPV_F32>(a, dst_layout->dtype, stream);
-        case SHARPV_BF16: return by_code<SHARPV_BF16>(a, dst_layout->dtype, stream);
-        case SHARPV_E4M3: return by_code<SHARPV_E4M3>(a, dst_layout->dtype, stream);
-        default: return by_code<SHARPV_I8>(a, dst_layout->dtype, stream);
+        case SHARPV_F32: return by_code<SHARPV_F32>(a, dst_layout->dtype, sms, stream);
+        case SHARPV_BF16: return by_code<SHARPV_BF16>(a, dst_layout->dtype, sms, stream);
+        case SHARPV_E4M3: return by_code<SHARPV_E4M3>(a, dst_layout->dtype, sms, stream);
+        default: return by_code<SHARPV_I8>(a, dst_layout->dtype, sms, stream);
     }
 }
