@@ -525,8 +525,8 @@ typedef struct {
  * block_tokens, and destination blocks of different sequences must not be the same.  Rows of a block behind the last one written
  * are left as they are: they are free.
  * Tables, capacity, status_word and the disjointness of the two caches as in sharpv_kv_append; src_scales_layout and src_scales
- * are NULL for SHARPV_F32 and SHARPV_BF16 sources.  head_dim is a multiple of 16 and at most 1024 (of 256 with SHARPV_F32
- * sources).  The scales of dst and src must not overlap.
+ * are NULL for SHARPV_F32 and SHARPV_BF16 sources.  head_dim is a multiple of 16 and at most 1024 (512 with SHARPV_F32
+ * sources), token strides are under 2 GB.  The scales of dst and src must not overlap.
  */
 sharpv_status sharpv_kv_append_q8(
     const void* kv_src, const sharpv_kv_layout* src_layout /* [host] */, const uint8_t* src_scales,

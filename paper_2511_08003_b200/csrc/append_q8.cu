@@ -29,17 +29,27 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxTileRows = 256;
 
+// Where planes lie, in bytes, and how far the next one is: in the same block, from the last K head to the first of V, from the
+// last of V to the next layer's first.
+struct Planes {
+    int64_t layer, kv, head, step[3];
+    __device__ __forceinline__ int64_t at(int l, int v, int h) const { return l * layer + v * kv + h * head; }
+};
+inline Planes planes_of(int64_t layer, int64_t kv, int64_t head, int heads) {
+    return {layer, kv, head, {head, kv - (heads - 1) * head, layer - kv - (heads - 1) * head}};
+}
+
 struct AppendQ8Args {
     const char* src;
     uint8_t* dst;
     const uint8_t* src_scales;
     uint8_t* dst_scales;
-    int64_t src_layer, src_kv, src_head, src_token, dst_layer, dst_kv, dst_head, dst_token;    // bytes
-    int64_t ss_layer, ss_kv, ss_head, ds_layer, ds_kv, ds_head;
+    Planes src_to, dst_to, ss_to, ds_to;
+    uint32_t src_token, dst_token;      // bytes
     int64_t src_tokens, dst_tokens;
     int src_shift, dst_shift;           // log2 of the blocks' rows
     int num_kv_heads, layer_begin, planes, row_vecs, code_vecs;     // 16-byte vectors of a source row, of a row of codes
-    uint32_t row_inverse;               // 2^32 / row_vecs, rounded up: the high word of a product with it is the quotient; 0 for 1
+    int go_rows;                        // rows that a team's threads hold one vector each of
     int tile_rows;                      // a multiple of the block's rows
     int team_planes;                    // that a team takes of a tile, one after the other
     const int32_t* src_pos;
@@ -230,10 +240,13 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
     if (lo >= hi) return;
     const int block_rows = 1 << a.dst_shift;
     const int64_t base = lo >> a.dst_shift << a.dst_shift;         // first row of the sequence's first block
-    const int64_t tiles = (hi - base + a.tile_rows - 1) / a.tile_rows;
+    const int64_t tiles = ((uint32_t)(hi - base) + a.tile_rows - 1) / (uint32_t)a.tile_rows;
     const int64_t mine = blockIdx.x - first_cta(b), ctas = first_cta(b + 1) - first_cta(b);
     if (mine < 0) return;               // offsets that do not begin at 0
 
+    // a thread has one column vector of every go_rows-th row
+    const int y0 = tid / a.row_vecs, col = tid - y0 * a.row_vecs;
+    const bool active = y0 < a.go_rows;
     int turn = 0;                       // which of the three lists of largest values
     for (int64_t tile = mine; tile < (mine + 1 == ctas ? tiles : min(tiles, mine + 1)); ++tile) {
         const int64_t row0 = base + tile * a.tile_rows;
@@ -251,39 +264,46 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
         }
         for (int i = tid; i < blocks; i += TEAM) sm.top[0][i] = sm.top[1][i] = sm.top[2][i] = 0;
         sync();
-        const int vecs = (rows - lead) * a.row_vecs;
-        const bool aligned = blocks == 1 || (((lead * a.row_vecs) | (a.row_vecs << a.dst_shift)) & 31) == 0;    // a warp's vectors lie in one block
-        uint8_t* const d_tile = a.dst + row0 * a.dst_token;
-        uint8_t* const ds_tile = a.dst_scales + (row0 >> a.dst_shift);
-        for (int plane = plane0; plane < min(plane0 + a.team_planes, a.planes); ++plane) {
-            const int h = plane % a.num_kv_heads, kv = (plane / a.num_kv_heads) & 1, l = a.layer_begin + plane / (2 * a.num_kv_heads);
-            const char* s = a.src + l * a.src_layer + kv * a.src_kv + h * a.src_head;
-            uint8_t* d = d_tile + l * a.dst_layer + kv * a.dst_kv + h * a.dst_head;
-            uint8_t* ds = ds_tile + l * a.ds_layer + kv * a.ds_kv + h * a.ds_head;
+        const int fresh = rows - lead, go = VECS * a.go_rows;      // rows that are written, and of one go
+        const int planes = min(a.team_planes, a.planes - plane0);
+        int h = plane0 % a.num_kv_heads, kv = (plane0 / a.num_kv_heads) & 1;
+        const int l = a.layer_begin + plane0 / (2 * a.num_kv_heads);
+        const char* s = a.src + a.src_to.at(l, kv, h) + col * 16;
+        const uint8_t* ss = S::kCodes ? a.src_scales + a.ss_to.at(l, kv, h) : nullptr;
+        uint8_t* d = a.dst + row0 * a.dst_token + a.dst_to.at(l, kv, h);
+        uint8_t* ds = a.dst_scales + (row0 >> a.dst_shift) + a.ds_to.at(l, kv, h);
+        for (int plane = 0; plane < planes; ++plane) {
+            if (plane > 0) {                        // to the next plane
+                const int wraps = ++h < a.num_kv_heads ? 0 : 1 + kv;
+                if (wraps) {
+                    h = 0;
+                    kv ^= 1;
+                }
+                s += a.src_to.step[wraps];
+                if constexpr (S::kCodes) ss += a.ss_to.step[wraps];
+                d += a.dst_to.step[wraps];
+                ds += a.ds_to.step[wraps];
+            }
             uint32_t* tops = sm.top[turn];
             const int old = lead > 0 ? scale_exponent(*ds) : kScaleLeast;       // of the first block's rows in front
             uint4 v[VECS];
             int unit[S::kCodes ? VECS : 1];         // exponent of the source's scale
             unsigned there = 0, odd = 0;
-            auto row_of = [&](int q) { return lead + (a.row_inverse ? (int)__umulhi((uint32_t)q, a.row_inverse) : q); };
-            auto load = [&](int q0) {
+            auto load = [&](int y) {                // y: the thread's first row of the go
                 there = 0;
 #pragma unroll
-                for (int u = 0; u < VECS; ++u) {
-                    const int q = q0 + u * TEAM + tid, r = row_of(q);
-                    if (q < vecs) {
-                        const int from = sm.from[r];
-                        if (from >= 0) {
-                            there |= 1u << u;
-                            v[u] = ld_stream(s + from * a.src_token + (q - (r - lead) * a.row_vecs) * 16);
-                            if constexpr (S::kCodes)
-                                unit[u] = scale_exponent(__ldg(a.src_scales + l * a.ss_layer + kv * a.ss_kv + h * a.ss_head + (from >> a.src_shift)));
-                        }
+                for (int u = 0; u < VECS; ++u, y += a.go_rows) {
+                    const int from = y < fresh ? sm.from[lead + y] : -1;
+                    if (from >= 0) {
+                        there |= 1u << u;
+                        v[u] = ld_stream(s + (uint64_t)(uint32_t)from * a.src_token);
+                        if constexpr (S::kCodes) unit[u] = scale_exponent(__ldg(ss + (from >> a.src_shift)));
                     }
                 }
             };
-            for (int q0 = 0; q0 < vecs; q0 += VECS * TEAM) {
-                load(q0);
+            for (int g0 = 0; g0 < fresh; g0 += go) {
+                load(active ? g0 + y0 : fresh);
+                uint32_t all_tops = 0;              // of the tile's only block
 #pragma unroll
                 for (int u = 0; u < VECS; ++u) {
                     uint32_t top = 0;
@@ -293,12 +313,21 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
                         if (strange) odd |= 1u << u;
                         if constexpr (S::kCodes) top = __float_as_uint(__uint_as_float(top) * power_of_two(unit[u]));
                     }
-                    if (aligned) {
-                        top = __reduce_max_sync(0xffffffffu, top);
-                        if (lane == 0 && top) atomicMax(&tops[row_of(q0 + u * TEAM + tid) >> a.dst_shift], top);
-                    } else if (top) {
-                        atomicMax(&tops[row_of(q0 + u * TEAM + tid) >> a.dst_shift], top);
+                    if (blocks == 1) {
+                        all_tops = max(all_tops, top);
+                        continue;
                     }
+                    const int block = (lead + g0 + y0 + u * a.go_rows) >> a.dst_shift, of_first = __shfl_sync(0xffffffffu, block, 0);
+                    if (__all_sync(0xffffffffu, block == of_first || top == 0)) {
+                        top = __reduce_max_sync(0xffffffffu, top);
+                        if (lane == 0 && top) atomicMax(&tops[block], top);
+                    } else if (top) {
+                        atomicMax(&tops[block], top);
+                    }
+                }
+                if (blocks == 1) {
+                    all_tops = __reduce_max_sync(0xffffffffu, all_tops);
+                    if (lane == 0 && all_tops) atomicMax(&tops[0], all_tops);
                 }
             }
             sync();
@@ -309,15 +338,17 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
                 return block == 0 ? max(e, old) : e;
             };
             for (int i = tid; i < blocks; i += TEAM) ds[i] = (uint8_t)(exponent(i) + 127);
-            for (int q0 = 0; q0 < vecs; q0 += VECS * TEAM) {
-                if (vecs > VECS * TEAM) load(q0);
+            const int only = exponent(0);
+            for (int g0 = 0; g0 < fresh; g0 += go) {
+                if (fresh > go) load(active ? g0 + y0 : fresh);
+                // several goes: what was seen in a vector is not kept, so each is taken for strange
+                if (fresh > go) odd = ~0u;
 #pragma unroll
                 for (int u = 0; u < VECS; ++u) {
                     if (!(there >> u & 1)) continue;
-                    const int q = q0 + u * TEAM + tid, r = row_of(q), e = exponent(r >> a.dst_shift);
-                    // several goes: what was seen in a vector is not kept, so each is taken for strange
-                    const bool plain = !(odd >> u & 1) && e < kScaleMost && vecs <= VECS * TEAM;
-                    store_codes<SRC, CODE>(d + r * a.dst_token + (q - (r - lead) * a.row_vecs) * P, v[u], (S::kCodes ? unit[S::kCodes ? u : 0] : 0) - e, plain);
+                    const int r = lead + g0 + y0 + u * a.go_rows, e = blocks == 1 ? only : exponent(r >> a.dst_shift);
+                    const bool plain = !(odd >> u & 1) && e < kScaleMost;
+                    store_codes<SRC, CODE>(d + (uint64_t)(uint32_t)r * a.dst_token + col * P, v[u], (S::kCodes ? unit[S::kCodes ? u : 0] : 0) - e, plain);
                 }
             }
             if (lead > 0 && exponent(0) != old) {                   // rows in front, by the new scale
@@ -329,7 +360,7 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
 #pragma unroll
                     for (int u = 0; u < kAhead; ++u) {
                         const int q = q0 + u * TEAM, r = q / a.code_vecs;
-                        at[u] = d + r * a.dst_token + (q - r * a.code_vecs) * 16;
+                        at[u] = d + (uint64_t)(uint32_t)r * a.dst_token + (q - r * a.code_vecs) * 16;
                         if (q < all_vecs) w[u] = *reinterpret_cast<const uint4*>(at[u]);
                     }
 #pragma unroll
@@ -345,7 +376,8 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
 template <int SRC, int CODE, int TEAM, int VECS>
 sharpv_status launch(AppendQ8Args& a, int sms, cudaStream_t stream) {
     const int block_rows = 1 << a.dst_shift;
-    int rows = VECS * TEAM / a.row_vecs / block_rows * block_rows;      // what a team holds, in whole blocks; one at least
+    a.go_rows = TEAM / a.row_vecs;
+    int rows = VECS * a.go_rows / block_rows * block_rows;      // what a team holds, in whole blocks; one at least
     if (rows < block_rows) rows = block_rows;
     if (rows > kMaxTileRows) rows = kMaxTileRows;
     a.tile_rows = rows;
@@ -369,8 +401,8 @@ sharpv_status by_size(AppendQ8Args& a, int sms, cudaStream_t stream) {
     // a warp a piece where a sequence's rows are no more than a warp takes in two goes; else a CTA, with eight vectors a thread
     // where four do not hold a block
     const int64_t vecs = a.capacity / a.num_seqs * a.row_vecs;
-    if (vecs <= 2 * 4 * 32) return launch<SRC, CODE, 32, 4>(a, sms, stream);
-    if ((a.row_vecs << a.dst_shift) <= 4 * kThreads) return launch<SRC, CODE, kThreads, 4>(a, sms, stream);
+    if (vecs <= 2 * 4 * 32 && a.row_vecs <= 32) return launch<SRC, CODE, 32, 4>(a, sms, stream);
+    if (1 << a.dst_shift <= 4 * (kThreads / a.row_vecs)) return launch<SRC, CODE, kThreads, 4>(a, sms, stream);
     return launch<SRC, CODE, kThreads, 8>(a, sms, stream);
 }
 
@@ -419,7 +451,9 @@ extern "C" sharpv_status sharpv_kv_append_q8(
     if (!src_pos || !src_seq_offsets || !dst_begin) return SHARPV_ERR_INVALID_ARG;
     const int64_t eb = elem_bytes(src_layout->dtype);
     const int row_vecs = (int)(src_layout->head_dim * eb / 16);
-    if (planes > 65535 || src_layout->head_dim > 1024 || row_vecs > 128) return SHARPV_ERR_UNSUPPORTED;
+    if (planes > 65535 || src_layout->head_dim > 1024 || row_vecs > 128 ||
+        src_layout->stride_token * eb >= (int64_t)1 << 31 || dst_layout->stride_token >= (int64_t)1 << 31)
+        return SHARPV_ERR_UNSUPPORTED;
     if (src_tokens > 0 && dst_tokens > 0) {
         uintptr_t s_lo, s_hi, d_lo, d_hi;
         kv_extent(kv_src, src_layout, layer_begin, layer_end, src_tokens, s_lo, s_hi);
@@ -434,25 +468,22 @@ extern "C" sharpv_status sharpv_kv_append_q8(
     AppendQ8Args a = {};
     a.src = (const char*)kv_src;
     a.dst = (uint8_t*)kv_dst;
-    a.src_layer = src_layout->stride_layer * eb; a.src_kv = src_layout->stride_kv * eb;
-    a.src_head = src_layout->stride_head * eb;   a.src_token = src_layout->stride_token * eb;
-    a.dst_layer = dst_layout->stride_layer; a.dst_kv = dst_layout->stride_kv;
-    a.dst_head = dst_layout->stride_head;   a.dst_token = dst_layout->stride_token;
+    const int H = src_layout->num_kv_heads;
+    a.src_to = planes_of(src_layout->stride_layer * eb, src_layout->stride_kv * eb, src_layout->stride_head * eb, H);
+    a.dst_to = planes_of(dst_layout->stride_layer, dst_layout->stride_kv, dst_layout->stride_head, H);
+    a.src_token = (uint32_t)(src_layout->stride_token * eb);
+    a.dst_token = (uint32_t)dst_layout->stride_token;
     a.src_scales = src_scales;
     if (codes) {
-        a.ss_layer = src_scales_layout->stride_layer;
-        a.ss_kv = src_scales_layout->stride_kv;
-        a.ss_head = src_scales_layout->stride_head;
+        a.ss_to = planes_of(src_scales_layout->stride_layer, src_scales_layout->stride_kv, src_scales_layout->stride_head, H);
         a.src_shift = log2_of(src_scales_layout->block_tokens);
     }
     a.dst_scales = dst_scales;
-    a.ds_layer = dst_scales_layout->stride_layer;
-    a.ds_kv = dst_scales_layout->stride_kv;
-    a.ds_head = dst_scales_layout->stride_head;
+    a.ds_to = planes_of(dst_scales_layout->stride_layer, dst_scales_layout->stride_kv, dst_scales_layout->stride_head, H);
     a.dst_shift = log2_of(dst_scales_layout->block_tokens);
     a.src_tokens = src_tokens;
     a.dst_tokens = dst_tokens;
-    a.num_kv_heads = src_layout->num_kv_heads;
+    a.num_kv_heads = H;
     a.layer_begin = layer_begin;
     a.planes = (int)planes;
     a.row_vecs = row_vecs;
@@ -463,7 +494,6 @@ extern "C" sharpv_status sharpv_kv_append_q8(
     a.num_seqs = num_seqs;
     a.capacity = capacity;
     a.status_word = status_word;
-    a.row_inverse = row_vecs == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + row_vecs - 1) / row_vecs);
     int sms = 0;
     st = current_sms(sms);
     if (st != SHARPV_OK) return st;
