@@ -28,6 +28,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxTileRows = 256;
+constexpr int kMaxTeamPlanes = 16;
 
 // Where planes lie, in bytes, and how far the next one is: in the same block, from the last K head to the first of V, from the
 // last of V to the next layer's first.
@@ -69,30 +70,32 @@ __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c
     return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
 
-// What a source's 16-byte vector gives: its largest finite |value| (bits of fp32, without the source's scale), whether something
-// in it is not finite, and its values as fp32.
+// What a source's 16-byte vector gives: a running maximum of its magnitudes in the source's own form (`add`), that as bits of
+// fp32 with whether something was not finite (`top`; without the source's scale), the largest finite magnitude the long way
+// (`finite`), and its values as fp32.
 template <int SRC> struct Source {
     static constexpr int kPerVec = Elem<SRC>::kPerVec;
     static constexpr bool kCodes = false;
     __device__ __forceinline__ static void widen(const uint4& v, float (&x)[kPerVec]) { Elem<SRC>::widen(v, x); }
-    __device__ __forceinline__ static uint32_t top(const uint4& v, bool& odd) {
-        uint32_t m;
-        if constexpr (SRC == SHARPV_F32) {
-            m = max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu));
-        } else {
-            const uint32_t t = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
-            m = max(t & 0xffff0000u, t << 16);
-        }
+    __device__ __forceinline__ static uint32_t add(uint32_t m, const uint4& v) {
+        if constexpr (SRC == SHARPV_F32)
+            return max(max(max(v.x & 0x7fffffffu, v.y & 0x7fffffffu), max(v.z & 0x7fffffffu, v.w & 0x7fffffffu)), m);
+        else
+            return __vmaxu2(__vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)), m);
+    }
+    __device__ __forceinline__ static uint32_t top(uint32_t m, bool& odd) {
+        if constexpr (SRC == SHARPV_BF16) m = max(m & 0xffff0000u, m << 16);
         odd = m >= 0x7f800000u;
-        if (odd) {
-            float x[kPerVec];
-            widen(v, x);
-            m = 0;
+        return m;
+    }
+    __device__ __forceinline__ static uint32_t finite(const uint4& v) {
+        float x[kPerVec];
+        widen(v, x);
+        uint32_t m = 0;
 #pragma unroll
-            for (int e = 0; e < kPerVec; ++e) {
-                const uint32_t y = __float_as_uint(x[e]) & 0x7fffffffu;
-                m = max(m, y < 0x7f800000u ? y : 0u);
-            }
+        for (int e = 0; e < kPerVec; ++e) {
+            const uint32_t y = __float_as_uint(x[e]) & 0x7fffffffu;
+            m = max(m, y < 0x7f800000u ? y : 0u);
         }
         return m;
     }
@@ -110,33 +113,47 @@ template <int CODE> struct CodeSource {
             for (int j = 0; j < 4; ++j) x[4 * i + j] = y[j];
         }
     }
-    __device__ __forceinline__ static uint32_t top(const uint4& v, bool& odd) {
+    // the codes of a vector two at a time in the high bytes of halves, where what stands in the low ones decides nothing
+    __device__ __forceinline__ static uint32_t add(uint32_t m, const uint4& v) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        uint32_t m = 0;                         // two at a time, the larger magnitude of codes in halves of a word
-        odd = false;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (CODE == SHARPV_E4M3) {
-                m = __vmaxu2(__vmaxu2(w[i] & 0x007f007fu, w[i] >> 8 & 0x007f007fu), m);
-            } else {                            // |x| of signed bytes in the high places of halves
-                m = __vmaxu2(__vmaxu2(__vabs2(w[i] & 0xff00ff00u), __vabs2(w[i] << 8 & 0xff00ff00u)), m);
-            }
-        }
-        m = max(m >> 16, m & 0xffffu);
         if constexpr (CODE == SHARPV_E4M3) {
-            odd = m == 0x7fu;
-            if (odd) {                          // NaN: the largest of the others
-                m = 0;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const uint32_t y = w[i / 4] >> (i % 4 * 8) & 0x7fu;
-                    m = max(m, y < 0x7fu ? y : 0u);
-                }
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t x = w[i] & 0x7f7f7f7fu;
+                m = __vmaxu2(__vmaxu2(x, x << 8), m);
             }
+            return m;
+        } else {
+            uint32_t hi = 0, lo = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                hi = __vmaxs2(__vmaxs2(w[i], w[i] << 8), hi);
+                lo = __vmins2(__vmins2(w[i], w[i] << 8), lo);
+            }
+            const int most = max((int)hi >> 24, (int)(hi << 16) >> 24), least = min((int)lo >> 24, (int)(lo << 16) >> 24);
+            return max(m, (uint32_t)max(most, -least));
+        }
+    }
+    __device__ __forceinline__ static uint32_t top(uint32_t m, bool& odd) {
+        if constexpr (CODE == SHARPV_E4M3) {
+            m = max(m >> 24, m >> 8 & 0xffu);
+            odd = m == 0x7fu;
             return __float_as_uint(__half2float(__low2half(as_half2(half2_of_e4m3((uint16_t)m)))));
         } else {
-            return __float_as_uint((float)(m >> 8));
+            odd = false;
+            return __float_as_uint((float)m);
         }
+    }
+    __device__ __forceinline__ static uint32_t finite(const uint4& v) {
+        float x[16];
+        widen(v, x);
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const uint32_t y = __float_as_uint(x[e]) & 0x7fffffffu;
+            m = max(m, y < 0x7f800000u ? y : 0u);
+        }
+        return m;
     }
 };
 template <> struct Source<SHARPV_E4M3> : CodeSource<SHARPV_E4M3> {};
@@ -303,18 +320,42 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
             };
             for (int g0 = 0; g0 < fresh; g0 += go) {
                 load(active ? g0 + y0 : fresh);
-                uint32_t all_tops = 0;              // of the tile's only block
+                auto scaled = [&](uint32_t top, int u) {
+                    return S::kCodes ? __float_as_uint(__uint_as_float(top) * power_of_two(unit[S::kCodes ? u : 0])) : top;
+                };
+                if (blocks == 1 && !S::kCodes) {    // all of a thread's vectors together
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int u = 0; u < VECS; ++u)
+                        if (there >> u & 1) m = S::add(m, v[u]);
+                    bool strange;
+                    uint32_t top = S::top(m, strange);
+                    if (strange) {
+                        odd = ~0u;
+                        top = 0;
+#pragma unroll
+                        for (int u = 0; u < VECS; ++u)
+                            if (there >> u & 1) top = max(top, S::finite(v[u]));
+                    }
+                    top = __reduce_max_sync(0xffffffffu, top);
+                    if (lane == 0 && top) atomicMax(&tops[0], top);
+                    continue;
+                }
+                uint32_t most = 0;                  // of a tile's only block
 #pragma unroll
                 for (int u = 0; u < VECS; ++u) {
                     uint32_t top = 0;
                     if (there >> u & 1) {
                         bool strange;
-                        top = S::top(v[u], strange);
-                        if (strange) odd |= 1u << u;
-                        if constexpr (S::kCodes) top = __float_as_uint(__uint_as_float(top) * power_of_two(unit[u]));
+                        top = S::top(S::add(0, v[u]), strange);
+                        if (strange) {
+                            odd |= 1u << u;
+                            top = S::finite(v[u]);
+                        }
+                        top = scaled(top, u);
                     }
                     if (blocks == 1) {
-                        all_tops = max(all_tops, top);
+                        most = max(most, top);
                         continue;
                     }
                     const int block = (lead + g0 + y0 + u * a.go_rows) >> a.dst_shift, of_first = __shfl_sync(0xffffffffu, block, 0);
@@ -326,8 +367,8 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
                     }
                 }
                 if (blocks == 1) {
-                    all_tops = __reduce_max_sync(0xffffffffu, all_tops);
-                    if (lane == 0 && all_tops) atomicMax(&tops[0], all_tops);
+                    most = __reduce_max_sync(0xffffffffu, most);
+                    if (lane == 0 && most) atomicMax(&tops[0], most);
                 }
             }
             sync();
@@ -382,10 +423,10 @@ sharpv_status launch(AppendQ8Args& a, int sms, cudaStream_t stream) {
     if (rows > kMaxTileRows) rows = kMaxTileRows;
     a.tile_rows = rows;
     const int64_t ctas = a.capacity / rows + a.num_seqs;
-    // several planes a team as long as there are sixteen times as many teams as SMs hold
+    // several planes a team as long as there are eight times as many teams as SMs hold
     constexpr int kTeams = kThreads / TEAM;
     a.team_planes = 1;
-    while (a.team_planes < 8 && ctas * a.planes / (2 * a.team_planes) >= (int64_t)sms * kTeams * 4 * 16) a.team_planes *= 2;
+    while (a.team_planes < kMaxTeamPlanes && ctas * a.planes / (2 * a.team_planes) >= (int64_t)sms * kTeams * 4 * 8) a.team_planes *= 2;
     const int y = (a.planes + kTeams * a.team_planes - 1) / (kTeams * a.team_planes);
     if (ctas >= (int64_t)1 << 31 || y > 65535) return SHARPV_ERR_UNSUPPORTED;
     if (launch_dependent(kv_append_q8_kernel<SRC, CODE, TEAM, VECS>, dim3((unsigned)ctas, (unsigned)y), dim3(kThreads), 0, stream, a) !=
