@@ -219,11 +219,11 @@ __device__ __forceinline__ void store_codes(uint8_t* to, const uint4& v, int k, 
 }
 
 struct Team {
-    int from[kMaxTileRows];             // source row of a row of the tile; -1: none
     uint32_t top[3][kMaxTileRows];      // of the tile's blocks: bits of the largest value; a plane after the other
 };
 
-template <int SRC, int CODE, int TEAM, int VECS>
+// GOES: a tile may hold more rows than the team's threads (VECS vectors each), and is gone through twice a plane.
+template <int SRC, int CODE, int TEAM, int VECS, bool GOES>
 __global__ void __launch_bounds__(kThreads, VECS > 4 ? 3 : 4)
 kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
     using S = Source<SRC>;
@@ -236,12 +236,12 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
     cudaGridDependencySynchronize();
     if (plane0 >= a.planes) return;
     const int64_t all = __ldg(a.offsets + a.num_seqs);
-    const int64_t n = min(max(all, (int64_t)0), a.capacity);
+    const int n = (int)min(max(all, (int64_t)0), a.capacity);
     const bool speaks = plane0 == 0 && tid == 0;
     if (speaks && blockIdx.x == 0 && all > a.capacity) report(a.status_word, SHARPV_ERR_CAPACITY);
     // sequence b has the CTAs from offsets[b] / tile_rows + b on: enough for its tiles but one, which its last CTA takes as well
-    auto offset = [&](int b) { return min(max((int64_t)__ldg(a.offsets + b), (int64_t)0), n); };
-    auto first_cta = [&](int b) { return (int64_t)((uint32_t)offset(b) / (uint32_t)a.tile_rows) + b; };
+    auto offset = [&](int b) { return min(max(__ldg(a.offsets + b), 0), n); };
+    auto first_cta = [&](int b) { return (uint32_t)offset(b) / (uint32_t)a.tile_rows + (uint32_t)b; };
     int b = 0;
     for (int left = a.num_seqs; left > 1;) {                // a warp narrows 32 ways a round
         const int step = (left + 31) / 32, at = lane * step;
@@ -250,45 +250,58 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
         b += skip;
         left = min(step, left - skip);
     }
-    const int64_t j0 = offset(b), j1 = max(offset(b + 1), j0), begin = __ldg(a.dst_begin + b);
+    const int j0 = offset(b), j1 = max(offset(b + 1), j0);
+    const int64_t begin = __ldg(a.dst_begin + b);
     // rows of dst [lo, hi) of this sequence; row t holds list entry j0 + t - begin
     const int64_t lo = min(max(begin, (int64_t)0), a.dst_tokens), hi = min(max(begin + (j1 - j0), lo), a.dst_tokens);
     if (speaks && j1 > j0 && (begin < 0 || begin + (j1 - j0) > a.dst_tokens)) report(a.status_word, SHARPV_ERR_BOUNDS);
-    if (lo >= hi) return;
+    const uint32_t cta0 = (uint32_t)j0 / (uint32_t)a.tile_rows + (uint32_t)b, ctas = first_cta(b + 1) - cta0;
+    if (lo >= hi || blockIdx.x < cta0) return;              // nothing here, or offsets that do not begin at 0
     const int block_rows = 1 << a.dst_shift;
-    const int64_t base = lo >> a.dst_shift << a.dst_shift;         // first row of the sequence's first block
-    const int64_t tiles = ((uint32_t)(hi - base) + a.tile_rows - 1) / (uint32_t)a.tile_rows;
-    const int64_t mine = blockIdx.x - first_cta(b), ctas = first_cta(b + 1) - first_cta(b);
-    if (mine < 0) return;               // offsets that do not begin at 0
-
+    const int64_t base = lo >> a.dst_shift << a.dst_shift;  // first row of the sequence's first block
+    const uint32_t tiles = ((uint32_t)(hi - base) + a.tile_rows - 1) / (uint32_t)a.tile_rows;
+    const uint32_t mine = blockIdx.x - cta0, last_tile = mine + 1 == ctas ? tiles : min(tiles, mine + 1);
     // a thread has one column vector of every go_rows-th row
     const int y0 = tid / a.row_vecs, col = tid - y0 * a.row_vecs;
-    const bool active = y0 < a.go_rows;
-    int turn = 0;                       // which of the three lists of largest values
-    for (int64_t tile = mine; tile < (mine + 1 == ctas ? tiles : min(tiles, mine + 1)); ++tile) {
-        const int64_t row0 = base + tile * a.tile_rows;
+    const int go = VECS * a.go_rows;                        // rows that the team holds
+
+    for (uint32_t tile = mine; tile < last_tile; ++tile) {
+        const int64_t row0 = base + (int64_t)tile * a.tile_rows;
         const int rows = (int)min((int64_t)a.tile_rows, hi - row0), blocks = (rows + block_rows - 1) >> a.dst_shift;
-        const int lead = (int)max(lo - row0, (int64_t)0);           // rows of the first block that lie in front
-        sync();
-        for (int r = tid; r < rows; r += TEAM) {
-            int from = -1;
-            if (r >= lead) {
-                const int64_t f = __ldg(a.src_pos + j0 + (row0 + r - begin));
-                if (f >= 0 && f < a.src_tokens) from = (int)f;
-                else if (plane0 == 0) report(a.status_word, SHARPV_ERR_BOUNDS);
+        const int lead = (int)max(lo - row0, (int64_t)0);   // rows of the first block that lie in front
+        const int fresh = rows - lead;
+        int from[VECS];                                     // source rows of the thread's vectors
+        unsigned there = 0;                                 // which of them there are
+        auto look_up = [&](int g0, bool tell) {
+            there = 0;
+#pragma unroll
+            for (int u = 0; u < VECS; ++u) {
+                const int y = g0 + y0 + u * a.go_rows;
+                from[u] = 0;
+                if (y0 < a.go_rows && y < fresh) {
+                    const int64_t f = __ldg(a.src_pos + j0 + (row0 + lead + y - begin));
+                    if (f >= 0 && f < a.src_tokens) {
+                        from[u] = (int)f;
+                        there |= 1u << u;
+                    } else if (tell && plane0 == 0) {
+                        report(a.status_word, SHARPV_ERR_BOUNDS);
+                    }
+                }
             }
-            sm.from[r] = from;
-        }
+        };
+        sync();                                             // the lists of the tile before are read
         for (int i = tid; i < blocks; i += TEAM) sm.top[0][i] = sm.top[1][i] = sm.top[2][i] = 0;
+        look_up(0, true);
         sync();
-        const int fresh = rows - lead, go = VECS * a.go_rows;      // rows that are written, and of one go
+        int turn = 0;                                       // which of the three lists of largest values
         const int planes = min(a.team_planes, a.planes - plane0);
         int h = plane0 % a.num_kv_heads, kv = (plane0 / a.num_kv_heads) & 1;
         const int l = a.layer_begin + plane0 / (2 * a.num_kv_heads);
         const char* s = a.src + a.src_to.at(l, kv, h) + col * 16;
         const uint8_t* ss = S::kCodes ? a.src_scales + a.ss_to.at(l, kv, h) : nullptr;
-        uint8_t* d = a.dst + row0 * a.dst_token + a.dst_to.at(l, kv, h);
+        uint8_t* d = a.dst + (row0 + lead + y0) * a.dst_token + a.dst_to.at(l, kv, h) + col * P;        // the thread's first vector
         uint8_t* ds = a.dst_scales + (row0 >> a.dst_shift) + a.ds_to.at(l, kv, h);
+        const int64_t d_go = (int64_t)a.go_rows * a.dst_token;
         for (int plane = 0; plane < planes; ++plane) {
             if (plane > 0) {                        // to the next plane
                 const int wraps = ++h < a.num_kv_heads ? 0 : 1 + kv;
@@ -305,24 +318,16 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
             const int old = lead > 0 ? scale_exponent(*ds) : kScaleLeast;       // of the first block's rows in front
             uint4 v[VECS];
             int unit[S::kCodes ? VECS : 1];         // exponent of the source's scale
-            unsigned there = 0, odd = 0;
-            auto load = [&](int y) {                // y: the thread's first row of the go
-                there = 0;
+            auto load = [&] {
 #pragma unroll
-                for (int u = 0; u < VECS; ++u, y += a.go_rows) {
-                    const int from = y < fresh ? sm.from[lead + y] : -1;
-                    if (from >= 0) {
-                        there |= 1u << u;
-                        v[u] = ld_stream(s + (uint64_t)(uint32_t)from * a.src_token);
-                        if constexpr (S::kCodes) unit[u] = scale_exponent(__ldg(ss + (from >> a.src_shift)));
+                for (int u = 0; u < VECS; ++u)
+                    if (there >> u & 1) {
+                        v[u] = ld_stream(s + (uint64_t)(uint32_t)from[u] * a.src_token);
+                        if constexpr (S::kCodes) unit[u] = scale_exponent(__ldg(ss + (from[u] >> a.src_shift)));
                     }
-                }
             };
-            for (int g0 = 0; g0 < fresh; g0 += go) {
-                load(active ? g0 + y0 : fresh);
-                auto scaled = [&](uint32_t top, int u) {
-                    return S::kCodes ? __float_as_uint(__uint_as_float(top) * power_of_two(unit[S::kCodes ? u : 0])) : top;
-                };
+            unsigned odd = 0;                       // vectors with something that is not finite
+            auto largest = [&](int g0) {
                 if (blocks == 1 && !S::kCodes) {    // all of a thread's vectors together
                     uint32_t m = 0;
 #pragma unroll
@@ -339,7 +344,7 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
                     }
                     top = __reduce_max_sync(0xffffffffu, top);
                     if (lane == 0 && top) atomicMax(&tops[0], top);
-                    continue;
+                    return;
                 }
                 uint32_t most = 0;                  // of a tile's only block
 #pragma unroll
@@ -352,7 +357,7 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
                             odd |= 1u << u;
                             top = S::finite(v[u]);
                         }
-                        top = scaled(top, u);
+                        if constexpr (S::kCodes) top = __float_as_uint(__uint_as_float(top) * power_of_two(unit[u]));
                     }
                     if (blocks == 1) {
                         most = max(most, top);
@@ -370,6 +375,16 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
                     most = __reduce_max_sync(0xffffffffu, most);
                     if (lane == 0 && most) atomicMax(&tops[0], most);
                 }
+            };
+            if constexpr (GOES) {
+                for (int g0 = 0; g0 < fresh; g0 += go) {
+                    if (fresh > go) look_up(g0, g0 > 0 && plane == 0);
+                    load();
+                    largest(g0);
+                }
+            } else {
+                load();
+                largest(0);
             }
             sync();
             // the list after the next: nobody reads it any more, and nobody adds to it before the next barrier
@@ -380,20 +395,30 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
             };
             for (int i = tid; i < blocks; i += TEAM) ds[i] = (uint8_t)(exponent(i) + 127);
             const int only = exponent(0);
-            for (int g0 = 0; g0 < fresh; g0 += go) {
-                if (fresh > go) load(active ? g0 + y0 : fresh);
-                // several goes: what was seen in a vector is not kept, so each is taken for strange
-                if (fresh > go) odd = ~0u;
+            auto write = [&](int g0) {
+                uint8_t* to = d + (GOES ? (int64_t)g0 * a.dst_token : 0);
 #pragma unroll
-                for (int u = 0; u < VECS; ++u) {
+                for (int u = 0; u < VECS; ++u, to += d_go) {
                     if (!(there >> u & 1)) continue;
-                    const int r = lead + g0 + y0 + u * a.go_rows, e = blocks == 1 ? only : exponent(r >> a.dst_shift);
-                    const bool plain = !(odd >> u & 1) && e < kScaleMost;
-                    store_codes<SRC, CODE>(d + (uint64_t)(uint32_t)r * a.dst_token + col * P, v[u], (S::kCodes ? unit[S::kCodes ? u : 0] : 0) - e, plain);
+                    const int e = blocks == 1 ? only : exponent((lead + g0 + y0 + u * a.go_rows) >> a.dst_shift);
+                    store_codes<SRC, CODE>(to, v[u], (S::kCodes ? unit[S::kCodes ? u : 0] : 0) - e, !(odd >> u & 1) && e < kScaleMost);
                 }
+            };
+            if constexpr (GOES) {
+                for (int g0 = 0; g0 < fresh; g0 += go) {
+                    if (fresh > go) {
+                        look_up(g0, false);
+                        load();
+                        odd = ~0u;                  // what was seen in a vector is not kept: each is taken for strange
+                    }
+                    write(g0);
+                }
+            } else {
+                write(0);
             }
-            if (lead > 0 && exponent(0) != old) {                   // rows in front, by the new scale
-                const int k = old - exponent(0), all_vecs = lead * a.code_vecs;
+            if (lead > 0 && only != old) {          // rows in front, by the new scale
+                uint8_t* front = d - (int64_t)(lead + y0) * a.dst_token - col * P;
+                const int k = old - only, all_vecs = lead * a.code_vecs;
                 constexpr int kAhead = 4;
                 for (int q0 = tid; q0 < all_vecs; q0 += kAhead * TEAM) {
                     uint4 w[kAhead];
@@ -401,7 +426,7 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
 #pragma unroll
                     for (int u = 0; u < kAhead; ++u) {
                         const int q = q0 + u * TEAM, r = q / a.code_vecs;
-                        at[u] = d + (uint64_t)(uint32_t)r * a.dst_token + (q - r * a.code_vecs) * 16;
+                        at[u] = front + (uint64_t)(uint32_t)r * a.dst_token + (q - r * a.code_vecs) * 16;
                         if (q < all_vecs) w[u] = *reinterpret_cast<const uint4*>(at[u]);
                     }
 #pragma unroll
@@ -414,7 +439,7 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
     }
 }
 
-template <int SRC, int CODE, int TEAM, int VECS>
+template <int SRC, int CODE, int TEAM, int VECS, bool GOES>
 sharpv_status launch(AppendQ8Args& a, int sms, cudaStream_t stream) {
     const int block_rows = 1 << a.dst_shift;
     a.go_rows = TEAM / a.row_vecs;
@@ -423,13 +448,13 @@ sharpv_status launch(AppendQ8Args& a, int sms, cudaStream_t stream) {
     if (rows > kMaxTileRows) rows = kMaxTileRows;
     a.tile_rows = rows;
     const int64_t ctas = a.capacity / rows + a.num_seqs;
-    // several planes a team as long as there are eight times as many teams as SMs hold
+    // several planes a team as long as there are four times as many teams as SMs hold
     constexpr int kTeams = kThreads / TEAM;
     a.team_planes = 1;
-    while (a.team_planes < kMaxTeamPlanes && ctas * a.planes / (2 * a.team_planes) >= (int64_t)sms * kTeams * 4 * 8) a.team_planes *= 2;
+    while (a.team_planes < kMaxTeamPlanes && ctas * a.planes / (2 * a.team_planes) >= (int64_t)sms * kTeams * 4 * 4) a.team_planes *= 2;
     const int y = (a.planes + kTeams * a.team_planes - 1) / (kTeams * a.team_planes);
     if (ctas >= (int64_t)1 << 31 || y > 65535) return SHARPV_ERR_UNSUPPORTED;
-    if (launch_dependent(kv_append_q8_kernel<SRC, CODE, TEAM, VECS>, dim3((unsigned)ctas, (unsigned)y), dim3(kThreads), 0, stream, a) !=
+    if (launch_dependent(kv_append_q8_kernel<SRC, CODE, TEAM, VECS, GOES>, dim3((unsigned)ctas, (unsigned)y), dim3(kThreads), 0, stream, a) !=
         cudaSuccess) {
         (void)cudaGetLastError();
         return SHARPV_ERR_CUDA;
@@ -440,11 +465,13 @@ sharpv_status launch(AppendQ8Args& a, int sms, cudaStream_t stream) {
 template <int SRC, int CODE>
 sharpv_status by_size(AppendQ8Args& a, int sms, cudaStream_t stream) {
     // a warp a piece where a sequence's rows are no more than a warp takes in two goes; else a CTA, with eight vectors a thread
-    // where four do not hold a block
+    // where four do not hold a block, and in several goes where those do not either
     const int64_t vecs = a.capacity / a.num_seqs * a.row_vecs;
-    if (vecs <= 2 * 4 * 32 && a.row_vecs <= 32) return launch<SRC, CODE, 32, 4>(a, sms, stream);
-    if (1 << a.dst_shift <= 4 * (kThreads / a.row_vecs)) return launch<SRC, CODE, kThreads, 4>(a, sms, stream);
-    return launch<SRC, CODE, kThreads, 8>(a, sms, stream);
+    if (vecs <= 2 * 4 * 32 && a.row_vecs <= 32) return launch<SRC, CODE, 32, 4, true>(a, sms, stream);
+    const int block_rows = 1 << a.dst_shift, go_rows = kThreads / a.row_vecs;
+    if (block_rows <= 4 * go_rows) return launch<SRC, CODE, kThreads, 4, false>(a, sms, stream);
+    if (block_rows <= 8 * go_rows) return launch<SRC, CODE, kThreads, 8, false>(a, sms, stream);
+    return launch<SRC, CODE, kThreads, 8, true>(a, sms, stream);
 }
 
 template <int SRC>
