@@ -30,15 +30,11 @@ constexpr int kThreads = 256;
 constexpr int kMaxTileRows = 256;
 constexpr int kMaxTeamPlanes = 16;
 
-// Where planes lie, in bytes, and how far the next one is: in the same block, from the last K head to the first of V, from the
-// last of V to the next layer's first.
+// Where planes lie, in bytes.
 struct Planes {
-    int64_t layer, kv, head, step[3];
+    int64_t layer, kv, head;
     __device__ __forceinline__ int64_t at(int l, int v, int h) const { return l * layer + v * kv + h * head; }
 };
-inline Planes planes_of(int64_t layer, int64_t kv, int64_t head, int heads) {
-    return {layer, kv, head, {head, kv - (heads - 1) * head, layer - kv - (heads - 1) * head}};
-}
 
 struct AppendQ8Args {
     const char* src;
@@ -219,12 +215,15 @@ __device__ __forceinline__ void store_codes(uint8_t* to, const uint4& v, int k, 
 }
 
 struct Team {
+    int64_t plane[kMaxTeamPlanes][4];   // where the team's planes lie: source, its scales, destination, its scales
     uint32_t top[3][kMaxTileRows];      // of the tile's blocks: bits of the largest value; a plane after the other
 };
 
+constexpr int ctas_an_sm(int team, int vecs) { return team == 32 || vecs == 4 ? 3 : 2; }
+
 // GOES: a tile may hold more rows than the team's threads (VECS vectors each), and is gone through twice a plane.
 template <int SRC, int CODE, int TEAM, int VECS, bool GOES>
-__global__ void __launch_bounds__(kThreads, VECS > 4 ? 3 : 4)
+__global__ void __launch_bounds__(kThreads, ctas_an_sm(TEAM, VECS))
 kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
     using S = Source<SRC>;
     constexpr int P = S::kPerVec, kTeams = kThreads / TEAM;
@@ -291,41 +290,55 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
         };
         sync();                                             // the lists of the tile before are read
         for (int i = tid; i < blocks; i += TEAM) sm.top[0][i] = sm.top[1][i] = sm.top[2][i] = 0;
+        const int planes = min(a.team_planes, a.planes - plane0);
+        if (tid < planes) {
+            const int p = plane0 + tid, h = p % a.num_kv_heads, kv = (p / a.num_kv_heads) & 1, l = a.layer_begin + p / (2 * a.num_kv_heads);
+            sm.plane[tid][0] = a.src_to.at(l, kv, h);
+            sm.plane[tid][1] = a.ss_to.at(l, kv, h);
+            sm.plane[tid][2] = a.dst_to.at(l, kv, h);
+            sm.plane[tid][3] = a.ds_to.at(l, kv, h);
+        }
         look_up(0, true);
         sync();
         int turn = 0;                                       // which of the three lists of largest values
-        const int planes = min(a.team_planes, a.planes - plane0);
-        int h = plane0 % a.num_kv_heads, kv = (plane0 / a.num_kv_heads) & 1;
-        const int l = a.layer_begin + plane0 / (2 * a.num_kv_heads);
-        const char* s = a.src + a.src_to.at(l, kv, h) + col * 16;
-        const uint8_t* ss = S::kCodes ? a.src_scales + a.ss_to.at(l, kv, h) : nullptr;
-        uint8_t* d = a.dst + (row0 + lead + y0) * a.dst_token + a.dst_to.at(l, kv, h) + col * P;        // the thread's first vector
-        uint8_t* ds = a.dst_scales + (row0 >> a.dst_shift) + a.ds_to.at(l, kv, h);
+        const char* const s0 = a.src + col * 16;
+        uint8_t* const d0 = a.dst + (row0 + lead + y0) * a.dst_token + col * P;        // the thread's first vector
+        uint8_t* const ds0 = a.dst_scales + (row0 >> a.dst_shift);
         const int64_t d_go = (int64_t)a.go_rows * a.dst_token;
-        for (int plane = 0; plane < planes; ++plane) {
-            if (plane > 0) {                        // to the next plane
-                const int wraps = ++h < a.num_kv_heads ? 0 : 1 + kv;
-                if (wraps) {
-                    h = 0;
-                    kv ^= 1;
+        uint4 v[VECS], next[GOES ? 1 : VECS];
+        int unit[S::kCodes ? VECS : 1];             // exponent of the source's scale
+        uint32_t next_unit[S::kCodes && !GOES ? VECS : 1];
+        auto load = [&](int plane, uint4* to, auto* units) {
+            const char* s = s0 + sm.plane[plane][0];
+            [[maybe_unused]] const uint8_t* ss = S::kCodes ? a.src_scales + sm.plane[plane][1] : nullptr;
+#pragma unroll
+            for (int u = 0; u < VECS; ++u)
+                if (there >> u & 1) {
+                    to[u] = ld_stream(s + (uint64_t)(uint32_t)from[u] * a.src_token);
+                    if constexpr (S::kCodes) units[u] = __ldg(ss + (from[u] >> a.src_shift));
                 }
-                s += a.src_to.step[wraps];
-                if constexpr (S::kCodes) ss += a.ss_to.step[wraps];
-                d += a.dst_to.step[wraps];
-                ds += a.ds_to.step[wraps];
+        };
+        auto exponents = [&] {
+            if constexpr (S::kCodes) {
+#pragma unroll
+                for (int u = 0; u < VECS; ++u) unit[u] = scale_exponent(unit[u]);
             }
+        };
+        if constexpr (!GOES) load(0, next, next_unit);
+        for (int plane = 0; plane < planes; ++plane) {
+            uint8_t* const d = d0 + sm.plane[plane][2];
+            uint8_t* const ds = ds0 + sm.plane[plane][3];
             uint32_t* tops = sm.top[turn];
             const int old = lead > 0 ? scale_exponent(*ds) : kScaleLeast;       // of the first block's rows in front
-            uint4 v[VECS];
-            int unit[S::kCodes ? VECS : 1];         // exponent of the source's scale
-            auto load = [&] {
+            if constexpr (!GOES) {                  // the next plane's are on their way while this one's are worked on
 #pragma unroll
-                for (int u = 0; u < VECS; ++u)
-                    if (there >> u & 1) {
-                        v[u] = ld_stream(s + (uint64_t)(uint32_t)from[u] * a.src_token);
-                        if constexpr (S::kCodes) unit[u] = scale_exponent(__ldg(ss + (from[u] >> a.src_shift)));
-                    }
-            };
+                for (int u = 0; u < VECS; ++u) {
+                    v[u] = next[u];
+                    if constexpr (S::kCodes) unit[u] = next_unit[u];
+                }
+                if (plane + 1 < planes) load(plane + 1, next, next_unit);
+                exponents();
+            }
             unsigned odd = 0;                       // vectors with something that is not finite
             auto largest = [&](int g0) {
                 if (blocks == 1 && !S::kCodes) {    // all of a thread's vectors together
@@ -379,21 +392,31 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
             if constexpr (GOES) {
                 for (int g0 = 0; g0 < fresh; g0 += go) {
                     if (fresh > go) look_up(g0, g0 > 0 && plane == 0);
-                    load();
+                    load(plane, v, unit);
+                    exponents();
                     largest(g0);
                 }
             } else {
-                load();
                 largest(0);
             }
             sync();
             // the list after the next: nobody reads it any more, and nobody adds to it before the next barrier
-            for (int i = tid; i < blocks; i += TEAM) sm.top[turn == 0 ? 2 : turn - 1][i] = 0;
+            auto each_block = [&](auto f) {
+                if constexpr (TEAM >= kMaxTileRows) {
+                    if (tid < blocks) f(tid);
+                } else {
+                    for (int i = tid; i < blocks; i += TEAM) f(i);
+                }
+            };
+            uint32_t* const later = sm.top[turn == 0 ? 2 : turn - 1];
             auto exponent = [&](int block) {
                 const int e = exponent_for<CODE>(tops[block]);
                 return block == 0 ? max(e, old) : e;
             };
-            for (int i = tid; i < blocks; i += TEAM) ds[i] = (uint8_t)(exponent(i) + 127);
+            each_block([&](int i) {
+                later[i] = 0;
+                ds[i] = (uint8_t)(exponent(i) + 127);
+            });
             const int only = exponent(0);
             auto write = [&](int g0) {
                 uint8_t* to = d + (GOES ? (int64_t)g0 * a.dst_token : 0);
@@ -408,7 +431,8 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
                 for (int g0 = 0; g0 < fresh; g0 += go) {
                     if (fresh > go) {
                         look_up(g0, false);
-                        load();
+                        load(plane, v, unit);
+                        exponents();
                         odd = ~0u;                  // what was seen in a vector is not kept: each is taken for strange
                     }
                     write(g0);
@@ -451,7 +475,7 @@ sharpv_status launch(AppendQ8Args& a, int sms, cudaStream_t stream) {
     // several planes a team as long as there are four times as many teams as SMs hold
     constexpr int kTeams = kThreads / TEAM;
     a.team_planes = 1;
-    while (a.team_planes < kMaxTeamPlanes && ctas * a.planes / (2 * a.team_planes) >= (int64_t)sms * kTeams * 4 * 4) a.team_planes *= 2;
+    while (a.team_planes < kMaxTeamPlanes && ctas * a.planes / (2 * a.team_planes) >= (int64_t)sms * kTeams * ctas_an_sm(TEAM, VECS) * 4) a.team_planes *= 2;
     const int y = (a.planes + kTeams * a.team_planes - 1) / (kTeams * a.team_planes);
     if (ctas >= (int64_t)1 << 31 || y > 65535) return SHARPV_ERR_UNSUPPORTED;
     if (launch_dependent(kv_append_q8_kernel<SRC, CODE, TEAM, VECS, GOES>, dim3((unsigned)ctas, (unsigned)y), dim3(kThreads), 0, stream, a) !=
@@ -537,17 +561,17 @@ extern "C" sharpv_status sharpv_kv_append_q8(
     a.src = (const char*)kv_src;
     a.dst = (uint8_t*)kv_dst;
     const int H = src_layout->num_kv_heads;
-    a.src_to = planes_of(src_layout->stride_layer * eb, src_layout->stride_kv * eb, src_layout->stride_head * eb, H);
-    a.dst_to = planes_of(dst_layout->stride_layer, dst_layout->stride_kv, dst_layout->stride_head, H);
+    a.src_to = {src_layout->stride_layer * eb, src_layout->stride_kv * eb, src_layout->stride_head * eb};
+    a.dst_to = {dst_layout->stride_layer, dst_layout->stride_kv, dst_layout->stride_head};
     a.src_token = (uint32_t)(src_layout->stride_token * eb);
     a.dst_token = (uint32_t)dst_layout->stride_token;
     a.src_scales = src_scales;
     if (codes) {
-        a.ss_to = planes_of(src_scales_layout->stride_layer, src_scales_layout->stride_kv, src_scales_layout->stride_head, H);
+        a.ss_to = {src_scales_layout->stride_layer, src_scales_layout->stride_kv, src_scales_layout->stride_head};
         a.src_shift = log2_of(src_scales_layout->block_tokens);
     }
     a.dst_scales = dst_scales;
-    a.ds_to = planes_of(dst_scales_layout->stride_layer, dst_scales_layout->stride_kv, dst_scales_layout->stride_head, H);
+    a.ds_to = {dst_scales_layout->stride_layer, dst_scales_layout->stride_kv, dst_scales_layout->stride_head};
     a.dst_shift = log2_of(dst_scales_layout->block_tokens);
     a.src_tokens = src_tokens;
     a.dst_tokens = dst_tokens;
