@@ -69,7 +69,7 @@ __device__ __forceinline__ uint4 ld_once(const void* p) {
 }
 
 template <int DT, int LP>
-__global__ void __launch_bounds__(kThreads, 4)
+__global__ void __launch_bounds__(kThreads, 3)
 qk_norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
     using E = Elem<DT>;
     constexpr int P = E::kPerVec, kGroups = kThreads / LP, kRound = kGroups * kAhead;
@@ -82,50 +82,72 @@ qk_norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
     cudaGridDependencySynchronize();
     const int64_t token0 = (int64_t)blockIdx.x * a.tile_tokens;
     const int tokens = (int)min((int64_t)a.tile_tokens, a.tokens - token0), rows = tokens * a.all_heads;
-    bool first = true;
+    // the group's rows are every kGroups-th from its first on (several CTAs share a token in turns of kRound)
+    struct At { int r, t, h; };
+    auto place = [&](int r) { return At{r, r / a.all_heads, r % a.all_heads}; };
+    const int turn_rows = (gridDim.y - 1) * kRound;
+    auto next = [&](At p, int by, int dt, int dh) {
+        p.r += by;
+        p.t += dt;
+        p.h += dh;
+        if (p.h >= a.all_heads) {
+            p.h -= a.all_heads;
+            ++p.t;
+        }
+        return p;
+    };
+    const int dt = kGroups / a.all_heads, dh = kGroups % a.all_heads;
+    const int dt_turn = turn_rows / a.all_heads, dh_turn = turn_rows % a.all_heads;
+    auto load = [&](At p, uint4& x0, uint4& x1) {
+        x0 = x1 = make_uint4(0, 0, 0, 0);
+        if (p.r < rows && busy) {
+            const char* row = p.h < a.q_heads ? a.q + (token0 + p.t) * a.q_token + p.h * a.q_head
+                                              : a.k + (token0 + p.t) * a.k_token + (p.h - a.q_heads) * a.k_head;
+            x0 = ld_once(row + v0 * 16);
+            if (second) x1 = ld_once(row + v1 * 16);
+        }
+    };
+    At at[kAhead];                      // of the rows that are loaded
+    uint4 x0[kAhead], x1[kAhead];
+    at[0] = place(blockIdx.y * kRound + group);
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y) {
+        if (y > 0) at[y] = next(at[y - 1], kGroups, dt, dh);
+        load(at[y], x0[y], x1[y]);
+    }
+    if (blockIdx.y * kRound < rows) {   // while the rows are on their way
+        const int step = a.half > 0 ? kThreads / a.half : 0;
+        if (threadIdx.x < step * a.half) {
+            const int i = threadIdx.x % a.half;
+            const double freq = a.freq[i];
+            const int32_t* positions = a.positions + a.axis[i] * a.ld_positions + token0;
+            float2* to = reinterpret_cast<float2*>(table) + ((i % P >> 1) * a.half_vecs + i / P) * 2 + (i & 1);
+            for (int t = threadIdx.x / a.half; t < tokens; t += step) {
+                const double turns = __ldg(positions + t) * freq;
+                float s, c;
+                sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+                to[t * (P / 2) * a.half_vecs * 2] = make_float2(c, s);
+            }
+        }
+    }
+    __syncthreads();
     for (int r0 = blockIdx.y * kRound; r0 < rows; r0 += gridDim.y * kRound) {
-        uint4 x0[kAhead], x1[kAhead];
 #pragma unroll
         for (int y = 0; y < kAhead; ++y) {
-            const int r = r0 + y * kGroups + group;
-            x0[y] = x1[y] = make_uint4(0, 0, 0, 0);
-            if (r < rows && busy) {
-                const int t = r / a.all_heads, h = r - t * a.all_heads;
-                const char* row = h < a.q_heads ? a.q + (token0 + t) * a.q_token + h * a.q_head
-                                                : a.k + (token0 + t) * a.k_token + (h - a.q_heads) * a.k_head;
-                x0[y] = ld_once(row + v0 * 16);
-                if (second) x1[y] = ld_once(row + v1 * 16);
-            }
-        }
-        if (first) {                    // while the rows are on their way
-            first = false;
-            const int step = a.half > 0 ? kThreads / a.half : 0;
-            if (threadIdx.x < step * a.half) {
-                const int i = threadIdx.x % a.half;
-                const double freq = a.freq[i];
-                const int32_t* at = a.positions + a.axis[i] * a.ld_positions + token0;
-                float2* to = reinterpret_cast<float2*>(table) + ((i % P >> 1) * a.half_vecs + i / P) * 2 + (i & 1);
-                for (int t = threadIdx.x / a.half; t < tokens; t += step) {
-                    const double turns = __ldg(at + t) * freq;
-                    float s, c;
-                    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-                    to[t * (P / 2) * a.half_vecs * 2] = make_float2(c, s);
-                }
-            }
-            __syncthreads();
-        }
+            const At p = at[y];
+            float lo[P], hi[P];
+            E::widen(x0[y], lo);
+            E::widen(x1[y], hi);
+            // a place's next row is asked for as soon as its registers are free
+            at[y] = next(next(p, kRound, kAhead * dt, 0), turn_rows, dt_turn, dh_turn);
 #pragma unroll
-        for (int y = 0; y < kAhead; ++y) {
-            const int r = r0 + y * kGroups + group;
-            const int t = r / a.all_heads, h = r - t * a.all_heads;
-            const bool is_q = h < a.q_heads;
-            float p[P], n[P];
-            E::widen(x0[y], p);
-            E::widen(x1[y], n);
+            for (int i = 0; i < kAhead; ++i) at[y] = next(at[y], 0, 0, dh);
+            load(at[y], x0[y], x1[y]);
+            const bool is_q = p.h < a.q_heads;
             if (a.norm) {
                 float sum = 0.f;
 #pragma unroll
-                for (int e = 0; e < P; ++e) sum = fmaf(p[e], p[e], fmaf(n[e], n[e], sum));
+                for (int e = 0; e < P; ++e) sum = fmaf(lo[e], lo[e], fmaf(hi[e], hi[e], sum));
 #pragma unroll
                 for (int o = LP / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                 const float f = rsqrtf(fmaf(sum, a.inv_d, a.eps));
@@ -135,28 +157,28 @@ qk_norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
                 for (int e = 0; e < P; ++e) w[e] = 1.f;
                 if (weight && busy) E::widen(ld_cached(weight + v0 * 16), w);
 #pragma unroll
-                for (int e = 0; e < P; ++e) p[e] *= f * w[e];
+                for (int e = 0; e < P; ++e) lo[e] *= f * w[e];
                 if (weight && second) E::widen(ld_cached(weight + v1 * 16), w);
 #pragma unroll
-                for (int e = 0; e < P; ++e) n[e] *= f * w[e];
+                for (int e = 0; e < P; ++e) hi[e] *= f * w[e];
             }
-            if (r >= rows || !busy) continue;
+            if (p.r >= rows || !busy) continue;
             if (pair) {
-                const float4* cs = table + t * (P / 2) * a.half_vecs + u;
+                const float4* cs = table + p.t * (P / 2) * a.half_vecs + u;
 #pragma unroll
                 for (int e = 0; e < P; e += 2) {
                     const float4 w = cs[(e >> 1) * a.half_vecs];
-                    const float a0 = p[e], a1 = p[e + 1];
-                    p[e] = fmaf(a0, w.x, -n[e] * w.y);
-                    n[e] = fmaf(n[e], w.x, a0 * w.y);
-                    p[e + 1] = fmaf(a1, w.z, -n[e + 1] * w.w);
-                    n[e + 1] = fmaf(n[e + 1], w.z, a1 * w.w);
+                    const float a0 = lo[e], a1 = lo[e + 1];
+                    lo[e] = fmaf(a0, w.x, -hi[e] * w.y);
+                    hi[e] = fmaf(hi[e], w.x, a0 * w.y);
+                    lo[e + 1] = fmaf(a1, w.z, -hi[e + 1] * w.w);
+                    hi[e + 1] = fmaf(hi[e + 1], w.z, a1 * w.w);
                 }
             }
-            char* row = is_q ? a.out_q + (token0 + t) * a.oq_token + h * a.oq_head
-                             : a.out_k + (token0 + t) * a.ok_token + (h - a.q_heads) * a.ok_head;
-            st_stream(row + v0 * 16, narrow<DT>(p));
-            if (second) st_stream(row + v1 * 16, narrow<DT>(n));
+            char* row = is_q ? a.out_q + (token0 + p.t) * a.oq_token + p.h * a.oq_head
+                             : a.out_k + (token0 + p.t) * a.ok_token + (p.h - a.q_heads) * a.ok_head;
+            st_stream(row + v0 * 16, narrow<DT>(lo));
+            if (second) st_stream(row + v1 * 16, narrow<DT>(hi));
         }
     }
 }
@@ -164,9 +186,9 @@ qk_norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
 template <int DT, int LP>
 sharpv_status launch(NormRopeArgs& a, int sms, cudaStream_t stream) {
     constexpr int kRound = kThreads / LP * kAhead;
-    // about four rounds a CTA, so that the angles are formed while others stream; with few tokens a CTA each, and with fewer
+    // about eight rounds a CTA, so that the angles are formed while others stream; with few tokens a CTA each, and with fewer
     // still several CTAs share a token's heads and form its angles each
-    int64_t tile = (4 * kRound + a.all_heads - 1) / a.all_heads;
+    int64_t tile = (8 * kRound + a.all_heads - 1) / a.all_heads;
     const int64_t share = a.tokens / (2 * sms);
     if (tile > share) tile = share;
     if (tile > kMaxTileTokens) tile = kMaxTileTokens;
