@@ -32,7 +32,7 @@ struct NormRopeArgs {
     const char* k;
     char* out_q;
     char* out_k;
-    int64_t q_token, q_head, k_token, k_head, oq_token, oq_head, ok_token, ok_head;     // bytes
+    uint32_t q_token, q_head, k_token, k_head, oq_token, oq_head, ok_token, ok_head;    // bytes
     const char* q_weight;               // or null: ones
     const char* k_weight;
     const int32_t* positions;           // [axes][ld_positions]
@@ -46,19 +46,50 @@ struct NormRopeArgs {
     uint8_t axis[kMaxPairs];
 };
 
+// Two fp32 at a time (one instruction each on this architecture).
+struct Two {
+    uint64_t v;
+    __device__ __forceinline__ Two() : v(0) {}
+    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ float2 parts() const {
+        float2 r;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+        return r;
+    }
+};
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Two fma(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+
 template <int DT>
-__device__ __forceinline__ uint4 narrow(const float (&x)[Elem<DT>::kPerVec]) {
-    if constexpr (DT == SHARPV_F32) {
-        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-    } else {
-        uint32_t w[4];
+__device__ __forceinline__ void widen2(const uint4& v, Two (&x)[Elem<DT>::kPerVec / 2]) {
+    float y[Elem<DT>::kPerVec];
+    Elem<DT>::widen(v, y);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    for (int i = 0; i < Elem<DT>::kPerVec / 2; ++i) x[i] = Two(y[2 * i], y[2 * i + 1]);
+}
+template <int DT>
+__device__ __forceinline__ uint4 narrow(const Two (&x)[Elem<DT>::kPerVec / 2]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < Elem<DT>::kPerVec / 2; ++i) {
+        const float2 p = x[i].parts();
+        if constexpr (DT == SHARPV_F32) {
+            w[2 * i] = __float_as_uint(p.x);
+            w[2 * i + 1] = __float_as_uint(p.y);
+        } else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(p.x, p.y);
             w[i] = *reinterpret_cast<const uint32_t*>(&h);
         }
-        return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // 128 bits that are not read again; not by way of the read-only path, since an output may be its own input
@@ -73,7 +104,7 @@ __global__ void __launch_bounds__(kThreads, 3)
 qk_norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
     using E = Elem<DT>;
     constexpr int P = E::kPerVec, kGroups = kThreads / LP, kRound = kGroups * kAhead;
-    extern __shared__ float4 table[];   // [tokens][P / 2][half_vecs]: cosine and sine of two pairs
+    extern __shared__ float4 table[];   // [tokens][P / 2][half_vecs]: cosines of two pairs, then their sines
     const int u = threadIdx.x % LP, group = threadIdx.x / LP;
     // the lane's two vectors: a pair of the rotated part, or two neighbours behind it
     const bool pair = u < a.half_vecs, busy = u < a.units;
@@ -84,8 +115,6 @@ qk_norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
     const int tokens = (int)min((int64_t)a.tile_tokens, a.tokens - token0), rows = tokens * a.all_heads;
     // the group's rows are every kGroups-th from its first on (several CTAs share a token in turns of kRound)
     struct At { int r, t, h; };
-    auto place = [&](int r) { return At{r, r / a.all_heads, r % a.all_heads}; };
-    const int turn_rows = (gridDim.y - 1) * kRound;
     auto next = [&](At p, int by, int dt, int dh) {
         p.r += by;
         p.t += dt;
@@ -96,23 +125,26 @@ qk_norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
         }
         return p;
     };
-    const int dt = kGroups / a.all_heads, dh = kGroups % a.all_heads;
-    const int dt_turn = turn_rows / a.all_heads, dh_turn = turn_rows % a.all_heads;
+    const int turn = gridDim.y * kRound, dt_turn = turn / a.all_heads, dh_turn = turn % a.all_heads;
+    const char* const q = a.q + token0 * a.q_token;
+    const char* const k = a.k + token0 * a.k_token;
+    char* const out_q = a.out_q + token0 * a.oq_token;
+    char* const out_k = a.out_k + token0 * a.ok_token;
+    auto at_offset = [](auto* base, int t, uint32_t token, int h, uint32_t head) { return base + (uint64_t)(uint32_t)t * token + (uint64_t)(uint32_t)h * head; };
     auto load = [&](At p, uint4& x0, uint4& x1) {
         x0 = x1 = make_uint4(0, 0, 0, 0);
         if (p.r < rows && busy) {
-            const char* row = p.h < a.q_heads ? a.q + (token0 + p.t) * a.q_token + p.h * a.q_head
-                                              : a.k + (token0 + p.t) * a.k_token + (p.h - a.q_heads) * a.k_head;
+            const char* row = p.h < a.q_heads ? at_offset(q, p.t, a.q_token, p.h, a.q_head) : at_offset(k, p.t, a.k_token, p.h - a.q_heads, a.k_head);
             x0 = ld_once(row + v0 * 16);
             if (second) x1 = ld_once(row + v1 * 16);
         }
     };
     At at[kAhead];                      // of the rows that are loaded
     uint4 x0[kAhead], x1[kAhead];
-    at[0] = place(blockIdx.y * kRound + group);
 #pragma unroll
     for (int y = 0; y < kAhead; ++y) {
-        if (y > 0) at[y] = next(at[y - 1], kGroups, dt, dh);
+        const int r = blockIdx.y * kRound + y * kGroups + group;
+        at[y] = At{r, r / a.all_heads, r % a.all_heads};
         load(at[y], x0[y], x1[y]);
     }
     if (blockIdx.y * kRound < rows) {   // while the rows are on their way
@@ -121,12 +153,13 @@ qk_norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
             const int i = threadIdx.x % a.half;
             const double freq = a.freq[i];
             const int32_t* positions = a.positions + a.axis[i] * a.ld_positions + token0;
-            float2* to = reinterpret_cast<float2*>(table) + ((i % P >> 1) * a.half_vecs + i / P) * 2 + (i & 1);
+            float* to = reinterpret_cast<float*>(table) + ((i % P >> 1) * a.half_vecs + i / P) * 4 + (i & 1);
             for (int t = threadIdx.x / a.half; t < tokens; t += step) {
                 const double turns = __ldg(positions + t) * freq;
                 float s, c;
                 sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-                to[t * (P / 2) * a.half_vecs * 2] = make_float2(c, s);
+                to[t * (P / 2) * a.half_vecs * 4] = c;
+                to[t * (P / 2) * a.half_vecs * 4 + 2] = s;
             }
         }
     }
@@ -135,48 +168,53 @@ qk_norm_rope_kernel(const __grid_constant__ NormRopeArgs a) {
 #pragma unroll
         for (int y = 0; y < kAhead; ++y) {
             const At p = at[y];
-            float lo[P], hi[P];
-            E::widen(x0[y], lo);
-            E::widen(x1[y], hi);
-            // a place's next row is asked for as soon as its registers are free
-            at[y] = next(next(p, kRound, kAhead * dt, 0), turn_rows, dt_turn, dh_turn);
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) at[y] = next(at[y], 0, 0, dh);
-            load(at[y], x0[y], x1[y]);
+            Two lo[P / 2], hi[P / 2];
+            widen2<DT>(x0[y], lo);
+            widen2<DT>(x1[y], hi);
+            at[y] = next(p, turn, dt_turn, dh_turn);
+            load(at[y], x0[y], x1[y]);              // as soon as the registers are free
             const bool is_q = p.h < a.q_heads;
             if (a.norm) {
-                float sum = 0.f;
+                Two sum2;
 #pragma unroll
-                for (int e = 0; e < P; ++e) sum = fmaf(lo[e], lo[e], fmaf(hi[e], hi[e], sum));
+                for (int e = 0; e < P / 2; ++e) sum2 = fma(lo[e], lo[e], fma(hi[e], hi[e], sum2));
+                float sum = sum2.parts().x + sum2.parts().y;
 #pragma unroll
                 for (int o = LP / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                 const float f = rsqrtf(fmaf(sum, a.inv_d, a.eps));
+                const Two f2(f, f);
                 const char* weight = is_q ? a.q_weight : a.k_weight;
-                float w[P];
+                if (weight && busy) {
+                    Two w[P / 2];
+                    widen2<DT>(ld_cached(weight + v0 * 16), w);
 #pragma unroll
-                for (int e = 0; e < P; ++e) w[e] = 1.f;
-                if (weight && busy) E::widen(ld_cached(weight + v0 * 16), w);
+                    for (int e = 0; e < P / 2; ++e) lo[e] = lo[e] * (f2 * w[e]);
+                    if (second) {
+                        widen2<DT>(ld_cached(weight + v1 * 16), w);
 #pragma unroll
-                for (int e = 0; e < P; ++e) lo[e] *= f * w[e];
-                if (weight && second) E::widen(ld_cached(weight + v1 * 16), w);
+                        for (int e = 0; e < P / 2; ++e) hi[e] = hi[e] * (f2 * w[e]);
+                    }
+                } else {
 #pragma unroll
-                for (int e = 0; e < P; ++e) hi[e] *= f * w[e];
+                    for (int e = 0; e < P / 2; ++e) {
+                        lo[e] = lo[e] * f2;
+                        hi[e] = hi[e] * f2;
+                    }
+                }
             }
             if (p.r >= rows || !busy) continue;
             if (pair) {
                 const float4* cs = table + p.t * (P / 2) * a.half_vecs + u;
+                const Two minus(-1.f, -1.f);
 #pragma unroll
-                for (int e = 0; e < P; e += 2) {
-                    const float4 w = cs[(e >> 1) * a.half_vecs];
-                    const float a0 = lo[e], a1 = lo[e + 1];
-                    lo[e] = fmaf(a0, w.x, -hi[e] * w.y);
-                    hi[e] = fmaf(hi[e], w.x, a0 * w.y);
-                    lo[e + 1] = fmaf(a1, w.z, -hi[e + 1] * w.w);
-                    hi[e + 1] = fmaf(hi[e + 1], w.z, a1 * w.w);
+                for (int e = 0; e < P / 2; ++e) {
+                    const float4 w = cs[e * a.half_vecs];
+                    const Two c(w.x, w.y), s(w.z, w.w), x = lo[e];
+                    lo[e] = fma(hi[e] * s, minus, x * c);
+                    hi[e] = fma(hi[e], c, x * s);
                 }
             }
-            char* row = is_q ? a.out_q + (token0 + p.t) * a.oq_token + p.h * a.oq_head
-                             : a.out_k + (token0 + p.t) * a.ok_token + (p.h - a.q_heads) * a.ok_head;
+            char* row = is_q ? at_offset(out_q, p.t, a.oq_token, p.h, a.oq_head) : at_offset(out_k, p.t, a.ok_token, p.h - a.q_heads, a.ok_head);
             st_stream(row + v0 * 16, narrow<DT>(lo));
             if (second) st_stream(row + v1 * 16, narrow<DT>(hi));
         }
@@ -247,7 +285,7 @@ extern "C" sharpv_status sharpv_qk_norm_rope(
     const int64_t strides[8] = {ld_q, head_q, ld_k, head_k, ld_out_q, head_out_q, ld_out_k, head_out_k};
     for (int i = 0; i < 8; ++i) {
         if (strides[i] < head_dim) return SHARPV_ERR_INVALID_ARG;
-        if ((strides[i] * eb) % 16) return SHARPV_ERR_UNSUPPORTED;
+        if ((strides[i] * eb) % 16 || strides[i] * eb >= (int64_t)1 << 31) return SHARPV_ERR_UNSUPPORTED;
     }
     if (!aligned16(q) || !aligned16(k) || !aligned16(out_q) || !aligned16(out_k) || !aligned16(q_weight) || !aligned16(k_weight))
         return SHARPV_ERR_UNSUPPORTED;
@@ -256,10 +294,8 @@ extern "C" sharpv_status sharpv_qk_norm_rope(
     a.k = (const char*)k;
     a.out_q = (char*)out_q;
     a.out_k = (char*)out_k;
-    a.q_token = ld_q * eb;      a.q_head = head_q * eb;
-    a.k_token = ld_k * eb;      a.k_head = head_k * eb;
-    a.oq_token = ld_out_q * eb; a.oq_head = head_out_q * eb;
-    a.ok_token = ld_out_k * eb; a.ok_head = head_out_k * eb;
+    uint32_t* const bytes[8] = {&a.q_token, &a.q_head, &a.k_token, &a.k_head, &a.oq_token, &a.oq_head, &a.ok_token, &a.ok_head};
+    for (int i = 0; i < 8; ++i) *bytes[i] = (uint32_t)(strides[i] * eb);
     a.q_weight = (const char*)q_weight;
     a.k_weight = (const char*)k_weight;
     a.positions = positions;
