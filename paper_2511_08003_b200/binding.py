@@ -223,6 +223,16 @@ def _empty(shape, dtype, device, stream, result: bool = True) -> torch.Tensor:
     return t
 
 
+_DENSE = torch.contiguous_format
+
+
+def _like(t: torch.Tensor, stream) -> torch.Tensor:
+    """A dense result of t's shape and type (an allocation by likeness costs half of one by sizes)."""
+    if stream is None:
+        return torch.empty_like(t, memory_format=_DENSE)
+    return _empty(t.shape, t.dtype, t.device, stream)
+
+
 def _workspace(ws: Optional[torch.Tensor], nbytes: int, device, stream=None) -> torch.Tensor:
     if ws is None:
         return _empty(max(nbytes, 256), torch.uint8, device, stream, result=False)
@@ -623,7 +633,7 @@ def _attention_arrays(q, kv, lay, dev, dtype, draft_k, draft_v, tree_mask, out, 
             raise ValueError("tree_mask must be [nodes, words]")
         words, mask = tree_mask.shape[1], _on(tree_mask, "tree_mask", dev, _I32)
     if out is None:
-        o, lse = _empty(q.shape, dtype, dev, stream), _empty((N, HQ), _F32, dev, stream)
+        o, lse = _like(q, stream), _empty((N, HQ), _F32, dev, stream)
         out = {"out": o, "lse": lse}
         po, pl = o.data_ptr(), lse.data_ptr()
     else:
@@ -749,6 +759,16 @@ def sharpv_kv_append(kv_src: torch.Tensor, kv_dst: torch.Tensor, src_pos: torch.
 
 
 # ------------------------------------------------------------------------------- queries and keys of a step
+def _token_rows(t: torch.Tensor, tokens: int, heads: int, d: int):
+    """Address, token stride and head stride of [tokens, heads, d]; a stride that nothing needs is what a dense tensor has."""
+    a, b, c = t.stride()
+    if c != 1 and tokens and heads:
+        raise ValueError("q and k must have a contiguous last axis")
+    if heads < 2:
+        b = d
+    return t.data_ptr(), a if tokens > 1 else heads * b, b
+
+
 def sharpv_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, pair_axis, rope_base: float,
                         norm: bool = False, q_weight: Optional[torch.Tensor] = None,
                         k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -757,40 +777,33 @@ def sharpv_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tenso
     tokens] (or [tokens]): q [tokens, q_heads, head_dim], k [tokens, heads, head_dim], any token and head strides.
     pair_axis: for each of the rotary_dim / 2 pairs the axis whose position turns it (bytes or a sequence of ints).
     Returns dict(q, k), dense unless `out` holds them; out may hold q and k themselves."""
-    if not q.is_cuda:
-        raise ValueError("q must be a CUDA tensor")
-    dev, dtype = q.device, q.dtype
-    if q.dim() != 3 or k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
+    dev, dtype, qs, ks = q.device, q.dtype, q.shape, k.shape
+    if not q.is_cuda or k.device != dev or k.dtype is not dtype:
+        raise ValueError("q and k must be CUDA tensors on the same device and of the same dtype")
+    if len(qs) != 3 or len(ks) != 3 or ks[0] != qs[0] or ks[2] != qs[2]:
         raise ValueError("q and k must be [tokens, heads, head_dim] of the same tokens and head_dim")
-    N, HQ, D = q.shape
-    H = k.shape[1]
-    if k.device != dev or k.dtype is not dtype:
-        raise ValueError("q and k must share device and dtype")
+    N, HQ, D = qs
+    H = ks[1]
     if out is None:
-        out = {"q": _empty(q.shape, dtype, dev, stream), "k": _empty(k.shape, dtype, dev, stream)}
-    oq, ok = out["q"], out["k"]
-    for t, like in ((oq, q), (ok, k)):
-        if t.device != dev or t.dtype is not dtype or t.shape != like.shape:
+        oq, ok = _like(q, stream), _like(k, stream)
+        out = {"q": oq, "k": ok}
+        rows = (oq.data_ptr(), HQ * D, D, ok.data_ptr(), H * D, D)
+    else:
+        oq, ok = out["q"], out["k"]
+        if oq.device != dev or ok.device != dev or oq.dtype is not dtype or ok.dtype is not dtype or oq.shape != qs or ok.shape != ks:
             raise ValueError("out must hold q and k of the inputs' shapes, dtype and device")
-    if positions.dim() == 1:
-        positions = positions[None]
-    if positions.dim() != 2 or positions.shape[1] != N or positions.device != dev or (N > 1 and positions.stride(1) != 1):
+        rows = (*_token_rows(oq, N, HQ, D), *_token_rows(ok, N, H, D))
+    p, ps = positions.shape, positions.stride()
+    axes, far = (p[0], ps[0]) if len(p) == 2 else (1, 0)
+    if positions.device != dev or len(p) not in (1, 2) or p[-1] != N or (N > 1 and ps[-1] != 1):
         raise ValueError(f"positions must be [axes, tokens] on {dev} with a contiguous last axis")
     if positions.dtype is not _I32:
         raise TypeError("positions must be int32")
     pairs = pair_axis if isinstance(pair_axis, bytes) else bytes(pair_axis)
-    rows = []
-    for t in (q, k, oq, ok):
-        s = t.stride()
-        if N and t.shape[1] and s[2] != 1:
-            raise ValueError("q and k must have a contiguous last axis")
-        # a stride that nothing needs may be anything that the call accepts
-        head = s[1] if t.shape[1] > 1 else D
-        rows.append((t.data_ptr(), s[0] if N > 1 else max(D, head), head))
-    w = [None if t is None else _on(t, name, dev, dtype, D) for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight"))]
-    rc = _call("sharpv_qk_norm_rope", q, *rows[0], *rows[1], _dtype_code(q), N, HQ, H, D, 1 if norm else 0, w[0], w[1], eps,
-               positions.data_ptr(), positions.stride(0) if positions.shape[0] > 1 else N, positions.shape[0], pairs, 2 * len(pairs),
-               rope_base, *rows[2], *rows[3], _queue(stream, dev))
+    rc = _call("sharpv_qk_norm_rope", q, *_token_rows(q, N, HQ, D), *_token_rows(k, N, H, D), _dtype_code(q), N, HQ, H, D,
+               1 if norm else 0, None if q_weight is None else _on(q_weight, "q_weight", dev, dtype, D),
+               None if k_weight is None else _on(k_weight, "k_weight", dev, dtype, D), eps, positions.data_ptr(),
+               far if axes > 1 else N, axes, pairs, 2 * len(pairs), rope_base, *rows, _queue(stream, dev))
     if rc:
         _check("sharpv_qk_norm_rope", rc)
     return out
@@ -807,10 +820,11 @@ def _q8_cache(kv: torch.Tensor, scales: torch.Tensor, block_tokens: int, name: s
     if code is None:
         raise TypeError(f"{name} must be float8_e4m3fn or int8")
     lay.dtype = code
-    s, st = scales.shape, scales.stride()
+    s, st, n = scales.shape, scales.stride(), kv.shape
     if scales.device != dev or scales.element_size() != 1:
         raise ValueError(f"the scales of {name} must be one byte each and on {dev}")
-    if len(s) != 4 or s[:3] != kv.shape[:3] or block_tokens < 1 or s[3] * block_tokens < kv.shape[3] or (s[3] > 1 and st[3] != 1):
+    if len(s) != 4 or s[0] != n[0] or s[1] != 2 or s[2] != n[2] or block_tokens < 1 or s[3] * block_tokens < n[3] or \
+            (s[3] > 1 and st[3] != 1):
         raise ValueError(f"the scales of {name} must be [L, 2, H, blocks] with a contiguous last axis and a block for every "
                          "block_tokens rows")
     return lay, KVScales(block_tokens, st[0], st[1], st[2]), dev

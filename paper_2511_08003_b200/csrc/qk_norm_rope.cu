@@ -310,9 +310,12 @@ extern "C" sharpv_status sharpv_qk_norm_rope(
     a.norm = norm;
     a.eps = eps;
     a.inv_d = 1.0f / (float)head_dim;
-    for (int i = 0; i < a.half; ++i) {
+    // powers one after the other, in 64 bits of mantissa: the last of 128 is off by 2^-57
+    const long double ratio = a.half > 0 ? std::pow((long double)rope_base, -1.0L / a.half) : 0.0L;
+    long double freq = 1.0L / 6.283185307179586476925286766559L;
+    for (int i = 0; i < a.half; ++i, freq *= ratio) {
         a.axis[i] = pair_axis[i];
-        a.freq[i] = std::pow(rope_base, -(double)i / a.half) / 6.283185307179586;
+        a.freq[i] = (double)freq;
     }
     int sms = 0;
     const sharpv_status st = current_sms(sms);
