@@ -456,6 +456,7 @@ struct Choice {
 Choice choose(sharpv_dtype dtype, int head_dim, int group, int64_t avg_rows) {
     if (dtype == SHARPV_F32) return avg_rows <= 8 ? Choice{Path::simt, 8, 8, kMaxAttnCtas} : Choice{Path::simt, 32, 32, kMaxAttnCtas};
     if (head_dim <= 128 && group <= 128 && avg_rows > kMaxRowsPath) return {Path::tc, tc_rows(group), kTcPlaces, kMaxTcCtas};
+    if (q8_dtype_ok(dtype) && head_dim <= 128 && avg_rows <= 8) return {Path::rows, 8, 8, kMaxRowsCtas};
     return {Path::rows, kRowsTileRows, kRowsTileRows, kMaxRowsCtas};
 }
 int64_t average_rows(int32_t num_seqs, int64_t total_nodes, int64_t group) {

@@ -53,7 +53,7 @@ sharpv_status encode_attn_maps(const AttnArgs& a, int box_rows, AttnMaps& maps, 
 // Few query rows, bf16: a.split has kRowsTileRows rows and kRowsTileKeys keys a tile.  Sets a.ctas to what it launches.
 constexpr int kRowsTileRows = 16, kRowsTileKeys = 64;
 sharpv_status attn_rows_launch(AttnArgs& a, int sms, cudaStream_t stream);
-// the same for a cache in 8 bits
+// the same for a cache in 8 bits; also with tiles of 8 rows, head_dim of at most 128
 sharpv_status attn_rows_q8_launch(AttnArgs& a, sharpv_dtype code, int sms, cudaStream_t stream);
 
 // Many query rows, bf16 or codes with scales, head_dim and group of at most 128: a.split has tc_rows(group) rows and kTcTileKeys keys a tile.

@@ -26,41 +26,44 @@ namespace sharpv {
 namespace {
 
 constexpr int kKeys = kRowsTileKeys;            // of a tile
-constexpr int kRows = kRowsTileRows;
-constexpr int kWarps = 8;                       // that compute, in two groups of four
-constexpr int kThreads = kWarps * 32 + 32;
-constexpr int kMergeCols = 128;                 // columns that are joined at a time
 constexpr float kHeadroom = 14.f;               // weights reach 2^14
 
-template <int DP>
+template <int DP, int ROWS>
 struct Cfg {
+    static constexpr int kWarps = ROWS == 8 ? 16 : 8;           // that compute, in groups of four
+    static constexpr int kGroups = kWarps / 4, kThreads = kWarps * 32 + 32;
     static constexpr int kBox = DP < 128 ? DP : 128;            // bytes of a row in a TMA box
     static constexpr int kTileBytes = kKeys * DP;               // codes of K or V
     static constexpr int kDraftBytes = kKeys * DP * 2;
-    static constexpr int kStages = DP == 64 ? 12 : (DP == 128 ? 6 : 2);
-    static_assert(kStages % 2 == 0, "a stage belongs to one group");
-    static constexpr bool kQInRegs = DP <= 128;
+    static constexpr int kStages = ROWS == 8 ? (DP == 64 ? 12 : 8) : (DP == 64 ? 12 : (DP == 128 ? 6 : 2));
+    static_assert(kStages % kGroups == 0, "a stage belongs to one group");
     static constexpr int kQPitch = DP * 2 + 16;                 // bytes; 16 more, so that 8 rows fall on 8 bank groups
-    static constexpr int kCols = DP < kMergeCols ? DP : kMergeCols;
+    static constexpr int kCols = ROWS == 8 || DP < 128 ? 64 : 128;      // columns that are joined at a time
 };
 
-template <int DP>
+template <int DP, int ROWS>
 struct Shared {
-    using C = Cfg<DP>;
+    using C = Cfg<DP, ROWS>;
     uint8_t tiles[C::kStages][2][C::kTileBytes];
     uint8_t draft[2][C::kDraftBytes];
-    float merge[kWarps][16][C::kCols + 4];
-    float m[kWarps][16], l[kWarps][16];
-    uint8_t q[2][kRows * C::kQPitch];           // query rows of this portion and the next
-    uint8_t qh[kRows * C::kQPitch];             // this portion's as halves
-    float q_unit[kRows];                        // what a product of them stands for, times the scale of the scores
+    float merge[C::kWarps][ROWS][C::kCols + 4];
+    float m[C::kWarps][ROWS], l[C::kWarps][ROWS];
+    uint8_t q[2][ROWS * C::kQPitch];            // query rows of this portion and the next
+    uint8_t qh[ROWS * C::kQPitch];              // this portion's as halves
+    float q_unit[ROWS];                         // what a product of them stands for, times the scale of the scores
     Portion part[2];                            // kt1 < 0: there are no more
     uint64_t full[C::kStages], empty[C::kStages], part_full[2], part_empty[2], draft_full, draft_empty;
     int poison, dead;
-    PlanScratch<kThreads> plan;
+    PlanScratch<C::kThreads> plan;
 };
 
-__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" :: "n"(kWarps * 32) : "memory"); }
+template <int WARPS>
+__device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;" :: "n"(WARPS * 32) : "memory"); }
+
+// an 8 x 8 block of 16-bit elements, a row every four lanes, transposed
+__device__ __forceinline__ void transpose8(uint32_t& to, uint32_t from) {
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(to) : "r"(from));
+}
 
 // byte offset of 16-byte chunk c of a row of codes
 template <int DP>
@@ -68,12 +71,193 @@ __device__ __forceinline__ uint32_t code_chunk(int row, int c) {
     return DP == 64 ? swizzle64(row, c) : (c >> 3) * (kKeys * 128) + swizzle128(row, c & 7);
 }
 
+// The warp that brings portions, query rows and tiles ahead of the warps that compute.
+template <int DP, int ROWS>
+__device__ __forceinline__ void load_portions(const AttnArgs& a, const AttnMaps& maps, Shared<DP, ROWS>& sm, const PlanStart& plan, int64_t first,
+                                              int64_t end) {
+    using C = Cfg<DP, ROWS>;
+    constexpr int kRows = ROWS, kLanes = 32 / ROWS;     // lanes a query row
+    const int lane = threadIdx.x & 31, D = a.head_dim, G = a.split.group;
+    bool alive = true;                          // a wait that gave up
+    uint32_t ring = 0, drafts = 0, pn = 0;
+    Walk walk(plan, first, end);
+    Portion p, last;
+    for (;; ++pn) {
+        const int slot = pn & 1;
+        last = p;
+        const bool more = walk.next(a.seqs, a.split, p);
+        if (pn >= 2) alive = __all_sync(0xffffffffu, mbar_wait(&sm.part_empty[slot], ((pn >> 1) - 1) & 1));
+        if (!alive) break;                  // the place may still be read: the others give up on the portion that does not come
+        if (more) {
+            const int r_base = p.rt * kRows, r_all = p.s.nodes * G;
+            const int r = lane / kLanes, row = r_base + r;
+            const bool there = row < r_all;
+            const int node = there ? row / G : 0, g = there ? row - node * G : 0;
+            const char* q = a.q + (int64_t)(p.s.node0 + node) * a.q_node + (int64_t)(p.h * G + g) * D * 2;
+            uint8_t* to = sm.q[slot] + r * C::kQPitch;
+#pragma unroll
+            for (int c = lane % kLanes; c < DP / 8; c += kLanes) cp_async16(to + c * 16, c * 8 < D ? q + c * 16 : q, there && c * 8 < D);
+        }
+        cp_async_arrive(&sm.part_full[slot]);
+        if (lane == 0) {
+            if (!more) p.kt1 = -1;
+            sm.part[slot] = p;
+            mbar_arrive(&sm.part_full[slot]);
+        }
+        if (!more) break;
+        if (lane == 0) {
+            for (int kt = p.kt0; kt < p.kt1; ++kt) {
+                if (kt >= p.kt_cache && a.split.draft) {
+                    if (drafts >= 1) alive = mbar_wait(&sm.draft_empty, (drafts - 1) & 1);
+                    if (!alive) break;
+                    mbar_expect(&sm.draft_full, 2 * C::kDraftBytes);
+                    const int row = p.s.node0 + (kt - p.kt_cache) * kKeys;
+#pragma unroll
+                    for (int x = 0; x < DP / 64; ++x) {
+                        tma_load(sm.draft[0] + x * kKeys * 128, &maps.draft_k, &sm.draft_full, x * 64, row, p.h);
+                        tma_load(sm.draft[1] + x * kKeys * 128, &maps.draft_v, &sm.draft_full, x * 64, row, p.h);
+                    }
+                    ++drafts;
+                    continue;
+                }
+                const int stage = ring % C::kStages;
+                if (ring >= C::kStages) alive = mbar_wait(&sm.empty[stage], (ring / C::kStages - 1) & 1);
+                if (!alive) break;
+                ++ring;
+                if (kt >= p.kt_cache) {                     // the empty tile of rows without keys
+                    mbar_arrive(&sm.full[stage]);
+                    continue;
+                }
+                mbar_expect(&sm.full[stage], 2 * C::kTileBytes);
+                const int row = (int)p.s.begin + kt * kKeys;
+#pragma unroll
+                for (int x = 0; x < DP / C::kBox; ++x) {
+                    tma_load(sm.tiles[stage][0] + x * kKeys * C::kBox, &maps.cache_k, &sm.full[stage], x * C::kBox, row, p.h);
+                    tma_load(sm.tiles[stage][1] + x * kKeys * C::kBox, &maps.cache_v, &sm.full[stage], x * C::kBox, row, p.h);
+                }
+            }
+        }
+        alive = __all_sync(0xffffffffu, alive);
+        if (!alive) break;
+    }
+    if (lane == 0) {
+        if (!alive) report(a.status_word, SHARPV_ERR_TIMEOUT);
+        note_shared(a, alive && pn > 0, last, end, plan);
+        // copies in flight land before the CTA ends, also where the warps that wanted them gave up
+        for (int i = 0; i < C::kStages && (uint32_t)i < ring; ++i) {
+            const uint32_t at = ring - 1 - i;
+            (void)mbar_wait(&sm.full[at % C::kStages], (at / C::kStages) & 1);
+        }
+        if (drafts > 0) (void)mbar_wait(&sm.draft_full, (drafts - 1) & 1);
+    }
+    cp_async_wait<0>();
+}
+
+// Query rows as halves in the order of the products' columns, each by one warp.
+template <int DP, int ROWS>
+__device__ __forceinline__ void halve_queries(Shared<DP, ROWS>& sm, int at_part, float scale_log2) {
+    using C = Cfg<DP, ROWS>;
+    const int lane = threadIdx.x & 31;
+    for (int r = threadIdx.x >> 5; r < ROWS; r += C::kWarps) {
+        const uint8_t* from = sm.q[at_part] + r * C::kQPitch;
+        constexpr int N = (DP / 4 + 31) / 32;               // groups of four columns a lane
+        float x[N][4], top = 0.f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int c = n * 32 + lane;
+            const uint2 w = c < DP / 4 ? *reinterpret_cast<const uint2*>(from + c * 8) : make_uint2(0, 0);
+            x[n][0] = __uint_as_float(w.x << 16);
+            x[n][1] = __uint_as_float(w.x & 0xffff0000u);
+            x[n][2] = __uint_as_float(w.y << 16);
+            x[n][3] = __uint_as_float(w.y & 0xffff0000u);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[n][e]));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const int up = min(14 - ((int)(__float_as_uint(top) >> 23) - 127), 126);
+        const float f = power_of_two(up);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int c = n * 32 + lane;
+            if (c < DP / 4) {
+                uint8_t* to = sm.qh + r * C::kQPitch + (c >> 2) * 32 + (c & 3) * 4;
+                *reinterpret_cast<uint32_t*>(to) = pack_f16(x[n][0] * f, x[n][1] * f);
+                *reinterpret_cast<uint32_t*>(to + 16) = pack_f16(x[n][2] * f, x[n][3] * f);
+            }
+        }
+        if (lane == 0) sm.q_unit[r] = power_of_two(-up) * scale_log2;
+    }
+}
+
+// Columns c0 .. of the warps' results joined, and written as the portion's (a partial result, or the rows themselves).
+template <int DP, int ROWS>
+__device__ __forceinline__ void join_warps(const AttnArgs& a, Shared<DP, ROWS>& sm, const Portion& p, int c0) {
+    using C = Cfg<DP, ROWS>;
+    constexpr int kWarps = C::kWarps, kRows = ROWS;
+    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
+    const int r_base = p.rt * ROWS, r_all = p.s.nodes * G;
+    const bool complete = p.kt0 == 0 && p.kt1 == p.kt_all;
+    const int slot = portion_slot(blockIdx.x, p.kt0);
+    constexpr int V = C::kCols / 4;
+    for (int x = threadIdx.x; x < ROWS * V; x += kWarps * 32) {
+        const int r = x / V, c = c0 + (x % V) * 4, row = r_base + r;
+        if (row >= r_all || c >= D) continue;
+        float top = sm.m[0][r];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm.m[w][r]);
+        const float base = top == neg_inf() ? 0.f : top;
+        float sum = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float f = ex2(sm.m[w][r] - base);
+            const float4 v = *reinterpret_cast<const float4*>(&sm.merge[w][r][c - c0]);
+            sum = fmaf(f, sm.l[w][r], sum);
+            acc.x = fmaf(f, v.x, acc.x);
+            acc.y = fmaf(f, v.y, acc.y);
+            acc.z = fmaf(f, v.z, acc.z);
+            acc.w = fmaf(f, v.w, acc.w);
+        }
+        if (sm.poison) {
+            // what was set aside comes back to the rows that see it
+            const int j0 = (max(p.kt0, p.kt_cache) - p.kt_cache) * kKeys, j1 = min(p.s.nodes, (p.kt1 - p.kt_cache) * kKeys);
+            for (int j = j0; j < j1; ++j) {
+                if (!(draft_sees(a, p.s, row / G, j & ~31) >> (j & 31) & 1)) continue;
+                const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(
+                    a.draft_v + (int64_t)(p.s.node0 + j) * a.dv_node) + p.h * D + c;
+                const float v0 = __bfloat162float(v[0]), v1 = __bfloat162float(v[1]);
+                const float v2 = __bfloat162float(v[2]), v3 = __bfloat162float(v[3]);
+                if (!finite_f32(v0)) acc.x += v0;
+                if (!finite_f32(v1)) acc.y += v1;
+                if (!finite_f32(v2)) acc.z += v2;
+                if (!finite_f32(v3)) acc.w += v3;
+            }
+        }
+        const int64_t to = (int64_t)(p.s.node0 + row / G) * HQ + p.h * G + row % G;
+        if (complete) {
+            const float inv = row_scale(sum);
+            *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + to * D + c) =
+                make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+            if (c == 0) a.lse[to] = row_lse(top, sum);
+        } else {
+            *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * kRows + r) * D + c) = acc;
+            if (c == 0) {
+                a.part_ml[(int64_t)slot * 2 * kRows + r] = top;
+                a.part_ml[((int64_t)slot * 2 + 1) * kRows + r] = sum;
+            }
+        }
+    }
+}
+
 template <int CODE, int DP>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Cfg<DP, 16>::kThreads, 1)
 attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnMaps maps) {
-    using C = Cfg<DP>;
+    using C = Cfg<DP, 16>;
+    constexpr int kWarps = C::kWarps, kThreads = C::kThreads, kRows = 16;
+    constexpr bool kQInRegs = DP <= 128;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    auto& sm = *reinterpret_cast<Shared<DP>*>(smem_raw);
+    auto& sm = *reinterpret_cast<Shared<DP, 16>*>(smem_raw);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::kStages; ++i) {
@@ -95,81 +279,10 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     const PlanStart plan = plan_cta<kThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
     bool alive = true;                          // a wait that gave up: nothing is waited for any more, the result is void
     uint32_t ring = 0, drafts = 0, pn = 0;      // tiles in the ring, drafted tiles and portions of this CTA so far
-    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
+    const int G = a.split.group;
 
     if (warp == kWarps) {                       // portions, query rows and tiles ahead of the warps that compute
-        Walk walk(plan, first, end);
-        Portion p, last;
-        for (;; ++pn) {
-            const int slot = pn & 1;
-            last = p;
-            const bool more = walk.next(a.seqs, a.split, p);
-            if (pn >= 2) alive = __all_sync(0xffffffffu, mbar_wait(&sm.part_empty[slot], ((pn >> 1) - 1) & 1));
-            if (!alive) break;                  // the place may still be read: the others give up on the portion that does not come
-            if (more) {
-                const int r_base = p.rt * kRows, r_all = p.s.nodes * G;
-                // two lanes a row, every second chunk each
-                const int r = lane >> 1, row = r_base + r;
-                const bool there = row < r_all;
-                const int node = there ? row / G : 0, g = there ? row - node * G : 0;
-                const char* q = a.q + (int64_t)(p.s.node0 + node) * a.q_node + (int64_t)(p.h * G + g) * D * 2;
-                uint8_t* to = sm.q[slot] + r * C::kQPitch;
-#pragma unroll
-                for (int c = lane & 1; c < DP / 8; c += 2) cp_async16(to + c * 16, c * 8 < D ? q + c * 16 : q, there && c * 8 < D);
-            }
-            cp_async_arrive(&sm.part_full[slot]);
-            if (lane == 0) {
-                if (!more) p.kt1 = -1;
-                sm.part[slot] = p;
-                mbar_arrive(&sm.part_full[slot]);
-            }
-            if (!more) break;
-            if (lane == 0) {
-                for (int kt = p.kt0; kt < p.kt1; ++kt) {
-                    if (kt >= p.kt_cache && a.split.draft) {
-                        if (drafts >= 1) alive = mbar_wait(&sm.draft_empty, (drafts - 1) & 1);
-                        if (!alive) break;
-                        mbar_expect(&sm.draft_full, 2 * C::kDraftBytes);
-                        const int row = p.s.node0 + (kt - p.kt_cache) * kKeys;
-#pragma unroll
-                        for (int x = 0; x < DP / 64; ++x) {
-                            tma_load(sm.draft[0] + x * kKeys * 128, &maps.draft_k, &sm.draft_full, x * 64, row, p.h);
-                            tma_load(sm.draft[1] + x * kKeys * 128, &maps.draft_v, &sm.draft_full, x * 64, row, p.h);
-                        }
-                        ++drafts;
-                        continue;
-                    }
-                    const int stage = ring % C::kStages;
-                    if (ring >= C::kStages) alive = mbar_wait(&sm.empty[stage], (ring / C::kStages - 1) & 1);
-                    if (!alive) break;
-                    ++ring;
-                    if (kt >= p.kt_cache) {                     // the empty tile of rows without keys
-                        mbar_arrive(&sm.full[stage]);
-                        continue;
-                    }
-                    mbar_expect(&sm.full[stage], 2 * C::kTileBytes);
-                    const int row = (int)p.s.begin + kt * kKeys;
-#pragma unroll
-                    for (int x = 0; x < DP / C::kBox; ++x) {
-                        tma_load(sm.tiles[stage][0] + x * kKeys * C::kBox, &maps.cache_k, &sm.full[stage], x * C::kBox, row, p.h);
-                        tma_load(sm.tiles[stage][1] + x * kKeys * C::kBox, &maps.cache_v, &sm.full[stage], x * C::kBox, row, p.h);
-                    }
-                }
-            }
-            alive = __all_sync(0xffffffffu, alive);
-            if (!alive) break;
-        }
-        if (lane == 0) {
-            if (!alive) report(a.status_word, SHARPV_ERR_TIMEOUT);
-            note_shared(a, alive && pn > 0, last, end, plan);
-            // copies in flight land before the CTA ends, also where the warps that wanted them gave up
-            for (int i = 0; i < C::kStages && (uint32_t)i < ring; ++i) {
-                const uint32_t at = ring - 1 - i;
-                (void)mbar_wait(&sm.full[at % C::kStages], (at / C::kStages) & 1);
-            }
-            if (drafts > 0) (void)mbar_wait(&sm.draft_full, (drafts - 1) & 1);
-        }
-        cp_async_wait<0>();
+        load_portions<DP, 16>(a, maps, sm, plan, first, end);
         return;
     }
 
@@ -182,7 +295,7 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             report(a.status_word, SHARPV_ERR_TIMEOUT);
         }
         if (!alive) sm.dead = 1;
-        consumer_sync();                        // all eight warps go on or none does
+        consumer_sync<kWarps>();                        // all eight warps go on or none does
         const Portion p = sm.part[at_part];
         if (p.kt1 < 0 || sm.dead) break;
         const int r_base = p.rt * kRows, r_all = p.s.nodes * G;
@@ -193,45 +306,13 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             return kt < p.kt_cache && key < p.s.len ? (uint32_t)__ldg(scales + ((p.s.begin + key) >> a.scale_shift)) : 127u;
         };
         uint32_t next_scale = scale_of(p.kt0 + (int)((group ^ ring) & 1));
-        // ---- query rows as halves, two a warp
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const int r = warp * 2 + y;
-            const uint8_t* from = sm.q[at_part] + r * C::kQPitch;
-            constexpr int N = (DP / 4 + 31) / 32;               // groups of four columns a lane
-            float x[N][4], top = 0.f;
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int c = n * 32 + lane;
-                const uint2 w = c < DP / 4 ? *reinterpret_cast<const uint2*>(from + c * 8) : make_uint2(0, 0);
-                x[n][0] = __uint_as_float(w.x << 16);
-                x[n][1] = __uint_as_float(w.x & 0xffff0000u);
-                x[n][2] = __uint_as_float(w.y << 16);
-                x[n][3] = __uint_as_float(w.y & 0xffff0000u);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[n][e]));
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const int up = min(14 - ((int)(__float_as_uint(top) >> 23) - 127), 126);
-            const float f = power_of_two(up);
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int c = n * 32 + lane;
-                if (c < DP / 4) {
-                    uint8_t* to = sm.qh + r * C::kQPitch + (c >> 2) * 32 + (c & 3) * 4;
-                    *reinterpret_cast<uint32_t*>(to) = pack_f16(x[n][0] * f, x[n][1] * f);
-                    *reinterpret_cast<uint32_t*>(to + 16) = pack_f16(x[n][2] * f, x[n][3] * f);
-                }
-            }
-            if (lane == 0) sm.q_unit[r] = power_of_two(-up) * a.scale_log2;
-        }
-        consumer_sync();
+        halve_queries<DP, 16>(sm, at_part, a.scale_log2);
+        consumer_sync<kWarps>();
         const uint32_t q_off = (lane & 15) * C::kQPitch + (lane >> 4) * 16;
         const uint32_t qh_base = smem_u32(sm.qh) + q_off, q_base = smem_u32(sm.q[at_part]) + q_off;
         const float unit[2] = {sm.q_unit[qr], sm.q_unit[qr + 8]};
-        uint32_t qf[C::kQInRegs ? DP / 16 : 1][4];
-        if constexpr (C::kQInRegs) {
+        uint32_t qf[kQInRegs ? DP / 16 : 1][4];
+        if constexpr (kQInRegs) {
 #pragma unroll
             for (int ks = 0; ks < DP / 16; ++ks) ldmatrix4(qf[ks], qh_base + ks * 32);
         }
@@ -305,7 +386,7 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
                         uint32_t q4[4], b0, b1;
-                        if constexpr (C::kQInRegs) {
+                        if constexpr (kQInRegs) {
 #pragma unroll
                             for (int i = 0; i < 4; ++i) q4[i] = qf[ks + y][i];
                         } else {
@@ -426,8 +507,6 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         }
 
         // ---- the eight warps' results are joined, up to 128 columns at a time
-        const bool complete = p.kt0 == 0 && p.kt1 == p.kt_all;
-        const int slot = portion_slot(blockIdx.x, p.kt0);
         if (poison) sm.poison = 1;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -444,57 +523,9 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 if (r_base + 8 < r_all)         // rows 8 to 15 hold something
                     *reinterpret_cast<float4*>(&sm.merge[warp][qr + 8][col]) = make_float4(o[j][0][2], o[j][1][2], o[j][0][3], o[j][1][3]);
             }
-            consumer_sync();
-            constexpr int V = C::kCols / 4;
-            for (int x = threadIdx.x; x < 16 * V; x += kWarps * 32) {
-                const int r = x / V, c = c0 + (x % V) * 4, row = r_base + r;
-                if (row >= r_all || c >= D) continue;
-                float top = sm.m[0][r];
-#pragma unroll
-                for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm.m[w][r]);
-                const float base = top == neg_inf() ? 0.f : top;
-                float sum = 0.f;
-                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) {
-                    const float f = ex2(sm.m[w][r] - base);
-                    const float4 v = *reinterpret_cast<const float4*>(&sm.merge[w][r][c - c0]);
-                    sum = fmaf(f, sm.l[w][r], sum);
-                    acc.x = fmaf(f, v.x, acc.x);
-                    acc.y = fmaf(f, v.y, acc.y);
-                    acc.z = fmaf(f, v.z, acc.z);
-                    acc.w = fmaf(f, v.w, acc.w);
-                }
-                if (sm.poison) {
-                    // what was set aside comes back to the rows that see it
-                    const int j0 = (max(p.kt0, p.kt_cache) - p.kt_cache) * kKeys, j1 = min(p.s.nodes, (p.kt1 - p.kt_cache) * kKeys);
-                    for (int j = j0; j < j1; ++j) {
-                        if (!(draft_sees(a, p.s, row / G, j & ~31) >> (j & 31) & 1)) continue;
-                        const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(
-                            a.draft_v + (int64_t)(p.s.node0 + j) * a.dv_node) + p.h * D + c;
-                        const float v0 = __bfloat162float(v[0]), v1 = __bfloat162float(v[1]);
-                        const float v2 = __bfloat162float(v[2]), v3 = __bfloat162float(v[3]);
-                        if (!finite_f32(v0)) acc.x += v0;
-                        if (!finite_f32(v1)) acc.y += v1;
-                        if (!finite_f32(v2)) acc.z += v2;
-                        if (!finite_f32(v3)) acc.w += v3;
-                    }
-                }
-                const int64_t to = (int64_t)(p.s.node0 + row / G) * HQ + p.h * G + row % G;
-                if (complete) {
-                    const float inv = row_scale(sum);
-                    *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + to * D + c) =
-                        make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-                    if (c == 0) a.lse[to] = row_lse(top, sum);
-                } else {
-                    *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * kRows + r) * D + c) = acc;
-                    if (c == 0) {
-                        a.part_ml[(int64_t)slot * 2 * kRows + r] = top;
-                        a.part_ml[((int64_t)slot * 2 + 1) * kRows + r] = sum;
-                    }
-                }
-            }
-            consumer_sync();
+            consumer_sync<kWarps>();
+            join_warps<DP, 16>(a, sm, p, c0);
+            consumer_sync<kWarps>();
         }
         if (threadIdx.x == 0) sm.poison = 0;
         __syncwarp();
@@ -502,16 +533,276 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     }
 }
 
+// Up to eight query rows a tile: keys, and columns of the values, are the rows of the products, query rows their eight columns, so
+// nothing is computed for rows that are not there, and sums take half the registers.  That leaves room for four
+// groups of warps, four warps a scheduler instead of two: the chain from codes to weights is what a warp waits for (one
+// token over 50,432 rows with the kernel of 16 rows, of which seven count, 26.3 us).
+// A thread has the scores of keys lane / 4 and 8 further for query rows 2 (lane % 4) and the next.
 template <int CODE, int DP>
-sharpv_status launch(const AttnArgs& a, cudaStream_t stream) {
-    auto kern = attn_rows_q8_kernel<CODE, DP>;
-    const size_t smem = sizeof(Shared<DP>);
-    static_assert(sizeof(Shared<DP>) <= 227 * 1024, "shared memory of one CTA");
+__global__ void __launch_bounds__(Cfg<DP, 8>::kThreads, 1)
+attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnMaps maps) {
+    using C = Cfg<DP, 8>;
+    constexpr int kWarps = C::kWarps, kThreads = C::kThreads;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    auto& sm = *reinterpret_cast<Shared<DP, 8>*>(smem_raw);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < C::kStages; ++i) {
+            mbar_init(&sm.full[i], 1);
+            mbar_init(&sm.empty[i], 4);
+        }
+        mbar_init(&sm.draft_full, 1);
+        mbar_init(&sm.draft_empty, 4);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sm.part_full[i], 33);        // 32 lanes' query rows have landed, and the portion is written
+            mbar_init(&sm.part_empty[i], kWarps);
+        }
+        mbar_fence_init();
+        sm.poison = sm.dead = 0;
+    }
+    if (warp == kWarps && lane < 4) tma_prefetch(&maps.cache_k + lane);
+    cudaGridDependencySynchronize();
+    int64_t first, end;
+    const PlanStart plan = plan_cta<kThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
+    if (warp == kWarps) {
+        load_portions<DP, 8>(a, maps, sm, plan, first, end);
+        return;
+    }
+    bool alive = true;                                  // a wait that gave up: nothing is waited for any more, the result is void
+    uint32_t ring = 0, drafts = 0;                      // tiles in the ring and drafted tiles so far
+    const int G = a.split.group;
+    const int group = warp >> 2, sub = warp & 3;        // stages of this remainder, 16 keys from sub * 16 on
+    const int kr = lane >> 2, qc = (lane & 3) * 2;      // fragment row (and row + 8), column (and column + 1)
+    for (uint32_t pn = 0;; ++pn) {
+        const int at_part = pn & 1;
+        if (alive && !mbar_wait(&sm.part_full[at_part], (pn >> 1) & 1)) {
+            alive = false;
+            report(a.status_word, SHARPV_ERR_TIMEOUT);
+        }
+        if (!alive) sm.dead = 1;
+        consumer_sync<kWarps>();                        // all warps go on or none does
+        const Portion p = sm.part[at_part];
+        if (p.kt1 < 0 || sm.dead) break;
+        const int r_base = p.rt * 8, r_all = p.s.nodes * G;
+        // lanes 0 to 15: what stands at the scales of the warp's keys; 16 to 31: of its values.  Looked up a tile ahead.
+        const uint8_t* scales = (lane < 16 ? a.k_scales : a.v_scales) + p.h * a.scale_head;
+        auto scale_of = [&](int kt) {
+            const int key = kt * kKeys + sub * 16 + (lane & 15);
+            return kt < p.kt_cache && key < p.s.len ? (uint32_t)__ldg(scales + ((p.s.begin + key) >> a.scale_shift)) : 127u;
+        };
+        uint32_t next_scale = scale_of(p.kt0 + (int)((group - ring) & (C::kGroups - 1)));
+        halve_queries<DP, 8>(sm, at_part, a.scale_log2);
+        consumer_sync<kWarps>();
+        const uint32_t q_off = (lane & 7) * C::kQPitch + (lane >> 3) * 16;
+        const uint32_t q_base = smem_u32(sm.q[at_part]) + q_off;
+        const float unit[2] = {sm.q_unit[qc], sm.q_unit[qc + 1]};
+        uint32_t qf[DP / 32][4];                        // of 32 columns
+#pragma unroll
+        for (int ks = 0; ks < DP / 32; ++ks) ldmatrix4(qf[ks], smem_u32(sm.qh) + q_off + ks * 64);
+        // of 16 columns from 16 j on a thread has the columns 2 kr and 2 kr + 1 of its two query rows
+        float o[DP / 16][4];
+        float m[2] = {neg_inf(), neg_inf()}, l[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < DP / 16; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+        bool poison = false;                            // a drafted value that is not finite was set aside
+
+        // scores (with the values' exponents on top) to weights, relative to the running maximum
+        auto weigh = [&](float (&s)[4]) {
+            float top[2];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                float x = fmaxf(s[y], s[2 + y]);
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                top[y] = fmaxf(x - kHeadroom, m[y]);
+            }
+            if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const float f = m[y] == top[y] ? 1.f : ex2(m[y] - top[y]);
+                    m[y] = top[y];
+                    l[y] *= f;
+#pragma unroll
+                    for (int j = 0; j < DP / 16; ++j) {
+                        o[j][y] *= f;
+                        o[j][2 + y] *= f;
+                    }
+                }
+            }
+            const float b0 = m[0] == neg_inf() ? 0.f : m[0], b1 = m[1] == neg_inf() ? 0.f : m[1];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] = ex2(s[i] - (i & 1 ? b1 : b0));
+        };
+
+        for (int kt = p.kt0; kt < p.kt1; ++kt) {
+            const bool drafted = kt >= p.kt_cache && a.split.draft;
+            const uint32_t at = drafted ? drafts++ : ring++;
+            // a phase that is waited for has to be the next one of its barrier: a stage always has the same group, and so has the
+            // buffer of drafted tiles
+            if ((drafted ? 0 : (int)(at & (C::kGroups - 1))) != group) continue;
+            uint64_t* full = drafted ? &sm.draft_full : &sm.full[at % C::kStages];
+            uint64_t* empty = drafted ? &sm.draft_empty : &sm.empty[at % C::kStages];
+            const uint32_t scale_code = next_scale;
+            next_scale = scale_of(kt + C::kGroups);
+            if (alive && !mbar_wait(full, (drafted ? at : at / C::kStages) & 1)) {
+                alive = false;
+                report(a.status_word, SHARPV_ERR_TIMEOUT);
+            }
+            float s[4] = {};
+            const int vrow = sub * 16 + (lane & 15);
+            if (!drafted) {
+                const int stage = at % C::kStages;
+                const uint32_t ks_base = smem_u32(sm.tiles[stage][0]), vs_base = smem_u32(sm.tiles[stage][1]);
+                const int left = kt < p.kt_cache ? p.s.len - kt * kKeys : 0;        // keys of the tile that are there
+                const int krow = sub * 16 + (lane & 15);
+                float s1[4] = {};               // odd blocks of 16 columns: two chains of products
+#pragma unroll
+                for (int ks = 0; ks < DP / 16; ks += 2) {
+                    uint32_t k4[4], k0[4], k1[4];
+                    ldmatrix4(k4, ks_base + code_chunk<DP>(krow, ks + (lane >> 4)));
+                    halves_of<CODE>(k4[0], k0[0], k0[2]);
+                    halves_of<CODE>(k4[1], k0[1], k0[3]);
+                    halves_of<CODE>(k4[2], k1[0], k1[2]);
+                    halves_of<CODE>(k4[3], k1[1], k1[3]);
+                    mma_f16(s, k0, qf[ks / 2][0], qf[ks / 2][1]);
+                    mma_f16(s1, k1, qf[ks / 2][2], qf[ks / 2][3]);
+                }
+                const int exponent = scale_exponent(scale_code);
+                int ve[2];
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const float kx = power_of_two(__shfl_sync(0xffffffffu, exponent, n * 8 + kr));
+                    ve[n] = __shfl_sync(0xffffffffu, exponent, 16 + n * 8 + kr);
+                    const bool sees = sub * 16 + n * 8 + kr < left;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        s[n * 2 + y] = sees ? fmaf((s[n * 2 + y] + s1[n * 2 + y]) * unit[y], kx, (float)ve[n]) : neg_inf();
+                }
+                weigh(s);
+                const float d0 = power_of_two(-ve[0]), d1 = power_of_two(-ve[1]);
+                l[0] += fmaf(s[0], d0, s[2] * d1);
+                l[1] += fmaf(s[1], d0, s[3] * d1);
+                // weights are rounded to fp16 for the product with the values; their sum is not
+                uint32_t pf[2];
+                transpose8(pf[0], pack_f16(s[0], s[1]));
+                transpose8(pf[1], pack_f16(s[2], s[3]));
+#pragma unroll
+                for (int j = 0; j < DP / 16; j += 2) {
+                    uint32_t v4[4];
+                    ldmatrix4_trans(v4, vs_base + code_chunk<DP>(vrow, j + (lane >> 4)));
+                    if (left < kKeys) {
+                        // rows that are not there may hold anything: 0 times them would not be 0
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = sub * 16 + (i & 1) * 8 + qc;
+                            if (key >= left) v4[i] = 0u;
+                            else if (key + 1 >= left) v4[i] &= 0xffffu;
+                        }
+                    }
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        uint32_t v[4];          // even columns, odd columns of keys 0 to 7, then of keys 8 to 15
+                        halves_of<CODE>(__byte_perm(v4[y * 2], 0u, 0x3120), v[0], v[1]);
+                        halves_of<CODE>(__byte_perm(v4[y * 2 + 1], 0u, 0x3120), v[2], v[3]);
+                        mma_f16(o[j + y], v, pf[0], pf[1]);
+                    }
+                }
+            } else {
+                const uint32_t ks_base = smem_u32(sm.draft[0]), vs_base = smem_u32(sm.draft[1]);
+                const int left = p.s.nodes - (kt - p.kt_cache) * kKeys;
+#pragma unroll
+                for (int ks = 0; ks < DP / 16; ks += 2) {
+                    uint32_t q4[4];
+                    ldmatrix4(q4, q_base + ks * 32);
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        uint32_t k4[4];
+                        ldmatrix4(k4, ks_base + (ks >> 2) * (kKeys * 128) + swizzle128(vrow, ((ks + y) & 3) * 2 + (lane >> 4)));
+                        mma_bf16(s, k4, q4[y * 2], q4[y * 2 + 1]);
+                    }
+                }
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int row = r_base + qc + y;
+                    const int key0 = (kt - p.kt_cache) * kKeys + (sub >> 1) * 32;
+                    const uint32_t sees = row < r_all ? draft_sees(a, p.s, row / G, key0) >> ((sub & 1) * 16) : 0u;
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+                        s[n * 2 + y] = sees >> (n * 8 + kr) & 1 ? s[n * 2 + y] * a.scale_log2 : neg_inf();
+                }
+                weigh(s);
+                l[0] += s[0] + s[2];
+                l[1] += s[1] + s[3];
+                uint32_t pf[2];
+                transpose8(pf[0], pack_bf16(s[0], s[1]));
+                transpose8(pf[1], pack_bf16(s[2], s[3]));
+#pragma unroll
+                for (int j = 0; j < DP / 16; ++j) {
+                    uint32_t v4[4], v[4];
+                    ldmatrix4_trans(v4, vs_base + (j >> 2) * (kKeys * 128) + swizzle128(vrow, (j & 3) * 2 + (lane >> 4)));
+                    // rows that are not there may hold anything, and so may drafted rows that some query rows do not see
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = sub * 16 + (i & 1) * 8 + qc;
+                        if (key >= left) v4[i] = 0u;
+                        else if (key + 1 >= left) v4[i] &= 0xffffu;
+                        const uint32_t off = nonfinite_bf16(v4[i]);
+                        v4[i] &= ~off;
+                        poison |= off != 0;
+                    }
+                    // columns in the order of the sums: even ones, then odd ones
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int from = ((2 * kr + y) & 7) * 4 + (lane & 3);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t low = __shfl_sync(0xffffffffu, v4[i], from), high = __shfl_sync(0xffffffffu, v4[2 + i], from);
+                            v[i * 2 + y] = kr < 4 ? low : high;
+                        }
+                    }
+                    mma_bf16(o[j], v, pf[0], pf[1]);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty);
+        }
+
+        // ---- the warps' results are joined, 64 columns at a time
+        if (poison) sm.poison = 1;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) l[y] += __shfl_xor_sync(0xffffffffu, l[y], w);
+            if (kr == 0) { sm.m[warp][qc + y] = m[y]; sm.l[warp][qc + y] = l[y]; }
+        }
+#pragma unroll
+        for (int c0 = 0; c0 < DP; c0 += C::kCols) {
+#pragma unroll
+            for (int j = c0 / 16; j < (c0 + C::kCols) / 16; ++j)
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+                    *reinterpret_cast<float2*>(&sm.merge[warp][qc + y][j * 16 - c0 + kr * 2]) = make_float2(o[j][y], o[j][2 + y]);
+            consumer_sync<kWarps>();
+            join_warps<DP, 8>(a, sm, p, c0);
+            consumer_sync<kWarps>();
+        }
+        if (threadIdx.x == 0) sm.poison = 0;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.part_empty[at_part]);
+    }
+}
+
+template <int ROWS, int DP>
+sharpv_status launch(void (*kern)(AttnArgs, AttnMaps), const AttnArgs& a, cudaStream_t stream) {
+    using C = Cfg<DP, ROWS>;
+    const size_t smem = sizeof(Shared<DP, ROWS>);
+    static_assert(sizeof(Shared<DP, ROWS>) <= 227 * 1024, "shared memory of one CTA");
     AttnMaps maps;
-    const sharpv_status ms = encode_attn_maps(a, kKeys, maps, Cfg<DP>::kBox);
+    const sharpv_status ms = encode_attn_maps(a, kKeys, maps, C::kBox);
     if (ms != SHARPV_OK) return ms;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
-        launch_dependent(kern, dim3((unsigned)a.ctas), dim3(kThreads), smem, stream, a, maps) != cudaSuccess) {
+        launch_dependent(kern, dim3((unsigned)a.ctas), dim3(C::kThreads), smem, stream, a, maps) != cudaSuccess) {
         (void)cudaGetLastError();
         return SHARPV_ERR_CUDA;
     }
@@ -520,9 +811,11 @@ sharpv_status launch(const AttnArgs& a, cudaStream_t stream) {
 
 template <int CODE>
 sharpv_status by_dim(const AttnArgs& a, cudaStream_t stream) {
-    if (a.head_dim <= 64) return launch<CODE, 64>(a, stream);
-    if (a.head_dim <= 128) return launch<CODE, 128>(a, stream);
-    return launch<CODE, 256>(a, stream);
+    if (a.split.rows == 8)
+        return a.head_dim <= 64 ? launch<8, 64>(attn_rows8_q8_kernel<CODE, 64>, a, stream) : launch<8, 128>(attn_rows8_q8_kernel<CODE, 128>, a, stream);
+    if (a.head_dim <= 64) return launch<16, 64>(attn_rows_q8_kernel<CODE, 64>, a, stream);
+    if (a.head_dim <= 128) return launch<16, 128>(attn_rows_q8_kernel<CODE, 128>, a, stream);
+    return launch<16, 256>(attn_rows_q8_kernel<CODE, 256>, a, stream);
 }
 
 }  // namespace
