@@ -61,7 +61,7 @@ struct Split {
     int rows, keys, group, heads;
     int draft;                  // the drafted tokens' keys take part
     __host__ __device__ int row_tiles(const SeqInfo& s) const {
-        return (int)(((int64_t)s.nodes * group + rows - 1) / rows);
+        return (int)(((uint32_t)s.nodes * (uint32_t)group + (uint32_t)rows - 1) / (uint32_t)rows);     // under 2^31 query rows
     }
     __host__ __device__ int cache_tiles(const SeqInfo& s) const { return (s.len + keys - 1) / keys; }
     // at least one (then empty), so that rows without any key are written as well
@@ -128,73 +128,83 @@ struct PlanScratch {
     PlanStart start;
 };
 
+// The plan of CTA `cta` by one warp, a sequence a lane and all in 32 bits; false where there are more units than that allows.
+// At most 32 sequences.  CTA 0 reports tables that do not fit, by the warp that `tells`.
+template <class S>
+__device__ __forceinline__ bool plan_warp(const SeqTables& t, const S& sp, int cta, int ctas, PlanStart& p, int64_t& first, int64_t& end,
+                                          int32_t* status_word, bool tells) {
+    const int lane = threadIdx.x & 31;
+    bool bad = false;
+    SeqInfo s = {};
+    if (lane < t.num_seqs) s = load_seq(t, lane, bad);
+    const int64_t wide = sp.units(s);
+    if (!__all_sync(0xffffffffu, wide < (1 << 20))) return false;
+    const uint32_t segments = (uint32_t)sp.segments(s), tiles = (uint32_t)sp.tiles(s), units = (uint32_t)wide, cost = sp.cost(s);
+    const uint32_t total = __reduce_add_sync(0xffffffffu, units), costs = __reduce_add_sync(0xffffffffu, units * cost);
+    auto pieces = [&](uint32_t m) { return segments * min(tiles, (tiles * cost + m - 1) / m); };
+    uint32_t lo = costs > (uint32_t)ctas ? (costs + ctas - 1) / ctas : 1, hi = lo + S::kSwitch;
+    const bool cut = __reduce_add_sync(0xffffffffu, pieces(hi)) <= (uint32_t)ctas;
+    while (cut && lo < hi) {
+        const uint32_t m = (lo + hi) >> 1;
+        if (__reduce_add_sync(0xffffffffu, pieces(m)) <= (uint32_t)ctas) hi = m; else lo = m + 1;
+    }
+    // the lane's sequence has the CTAs (pieces) or the units (runs) [inc - mine, inc)
+    const uint32_t mine = cut ? pieces(hi) : units;
+    uint32_t inc = mine, units_inc = units, segments_inc = segments;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t n = __shfl_up_sync(0xffffffffu, inc, o), u = __shfl_up_sync(0xffffffffu, units_inc, o);
+        const uint32_t g = __shfl_up_sync(0xffffffffu, segments_inc, o);
+        if (lane >= o) {
+            inc += n;
+            units_inc += u;
+            segments_inc += g;
+        }
+    }
+    const uint32_t busy = total < (uint32_t)ctas ? total : ctas, each = busy ? total / busy : 0, extra = total - each * busy;
+    auto run_first = [&](uint32_t c) { return c * each + (c < extra ? c : extra); };
+    const uint32_t at = cut ? (uint32_t)cta : ((uint32_t)cta < busy ? run_first(cta) : total);
+    const uint32_t found = __ballot_sync(0xffffffffu, at >= inc - mine && at < inc);
+    const int b = found ? __ffs(found) - 1 : 0;
+    p.s.begin = __shfl_sync(0xffffffffu, s.begin, b);
+    p.s.len = __shfl_sync(0xffffffffu, s.len, b);
+    p.s.node0 = __shfl_sync(0xffffffffu, s.node0, b);
+    p.s.nodes = __shfl_sync(0xffffffffu, s.nodes, b);
+    p.b = b;
+    p.before = __shfl_sync(0xffffffffu, units_inc - units, b);
+    p.units = total;
+    p.segments = cut ? (int)__shfl_sync(0xffffffffu, segments_inc, 31) : -1;
+    p.ordinal = p.last = -1;
+    first = end = total;
+    if (found && !cut) {
+        first = at;
+        end = run_first(cta + 1);
+    }
+    const uint32_t cta_first = __shfl_sync(0xffffffffu, inc - mine, b);
+    const uint32_t segments_before = __shfl_sync(0xffffffffu, segments_inc - segments, b);
+    if (found && cut) {
+        const uint32_t n = (uint32_t)sp.tiles(p.s), of = min(n, (n * sp.cost(p.s) + hi - 1) / hi), local = at - cta_first;
+        const uint32_t segment = local / of, piece = local - segment * of;
+        first = p.before + segment * n + n * piece / of;
+        end = p.before + segment * n + n * (piece + 1) / of;
+        if (piece == 0) {
+            p.ordinal = (int)(segments_before + segment);
+            p.last = cta + (int)of - 1;
+        }
+    }
+    if (cta == 0 && tells && bad) report(status_word, SHARPV_ERR_BOUNDS);
+    return true;
+}
+
 // Every thread of the block (NT threads) gets the plan of this CTA, `first` its first unit and `end` the one behind
 // its last.  CTA 0 reports tables that do not fit.
 template <int NT, class S>
 __device__ __forceinline__ PlanStart plan_cta(const SeqTables& t, const S& sp, int cta, int ctas,
                                               PlanScratch<NT>& sm, int64_t& first, int64_t& end, int32_t* status_word) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (t.num_seqs <= 32) {                     // a sequence a lane, every warp on its own with the same result, in 32 bits
-        bool bad = false;
-        SeqInfo s = {};
-        if (lane < t.num_seqs) s = load_seq(t, lane, bad);
-        const int64_t wide = sp.units(s);
-        if (__all_sync(0xffffffffu, wide < (1 << 20))) {
-            const uint32_t segments = (uint32_t)sp.segments(s), tiles = (uint32_t)sp.tiles(s), units = (uint32_t)wide, cost = sp.cost(s);
-            const uint32_t total = __reduce_add_sync(0xffffffffu, units), costs = __reduce_add_sync(0xffffffffu, units * cost);
-            auto pieces = [&](uint32_t m) { return segments * min(tiles, (tiles * cost + m - 1) / m); };
-            uint32_t lo = costs > (uint32_t)ctas ? (costs + ctas - 1) / ctas : 1, hi = lo + S::kSwitch;
-            const bool cut = __reduce_add_sync(0xffffffffu, pieces(hi)) <= (uint32_t)ctas;
-            while (cut && lo < hi) {
-                const uint32_t m = (lo + hi) >> 1;
-                if (__reduce_add_sync(0xffffffffu, pieces(m)) <= (uint32_t)ctas) hi = m; else lo = m + 1;
-            }
-            // the lane's sequence has the CTAs (pieces) or the units (runs) [inc - mine, inc)
-            const uint32_t mine = cut ? pieces(hi) : units;
-            uint32_t inc = mine, units_inc = units, segments_inc = segments;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t n = __shfl_up_sync(0xffffffffu, inc, o), u = __shfl_up_sync(0xffffffffu, units_inc, o);
-                const uint32_t g = __shfl_up_sync(0xffffffffu, segments_inc, o);
-                if (lane >= o) {
-                    inc += n;
-                    units_inc += u;
-                    segments_inc += g;
-                }
-            }
-            const uint32_t busy = total < (uint32_t)ctas ? total : ctas, each = busy ? total / busy : 0, extra = total - each * busy;
-            auto run_first = [&](uint32_t c) { return c * each + (c < extra ? c : extra); };
-            const uint32_t at = cut ? (uint32_t)cta : ((uint32_t)cta < busy ? run_first(cta) : total);
-            const uint32_t found = __ballot_sync(0xffffffffu, at >= inc - mine && at < inc);
-            const int b = found ? __ffs(found) - 1 : 0;
-            PlanStart p;
-            p.s.begin = __shfl_sync(0xffffffffu, s.begin, b);
-            p.s.len = __shfl_sync(0xffffffffu, s.len, b);
-            p.s.node0 = __shfl_sync(0xffffffffu, s.node0, b);
-            p.s.nodes = __shfl_sync(0xffffffffu, s.nodes, b);
-            p.b = b;
-            p.before = __shfl_sync(0xffffffffu, units_inc - units, b);
-            p.units = total;
-            p.segments = cut ? (int)__shfl_sync(0xffffffffu, segments_inc, 31) : -1;
-            p.ordinal = p.last = -1;
-            first = end = total;
-            if (found && !cut) {
-                first = at;
-                end = run_first(cta + 1);
-            }
-            const uint32_t cta_first = __shfl_sync(0xffffffffu, inc - mine, b);
-            const uint32_t segments_before = __shfl_sync(0xffffffffu, segments_inc - segments, b);
-            if (found && cut) {
-                const uint32_t n = (uint32_t)sp.tiles(p.s), of = min(n, (n * sp.cost(p.s) + hi - 1) / hi), local = at - cta_first;
-                const uint32_t segment = local / of, piece = local - segment * of;
-                first = p.before + segment * n + n * piece / of;
-                end = p.before + segment * n + n * (piece + 1) / of;
-                if (piece == 0) {
-                    p.ordinal = (int)(segments_before + segment);
-                    p.last = cta + (int)of - 1;
-                }
-            }
-            if (cta == 0 && warp == 0 && bad) report(status_word, SHARPV_ERR_BOUNDS);
+    if (t.num_seqs <= 32) {                     // every warp on its own with the same result
+        PlanStart p;
+        if (plan_warp(t, sp, cta, ctas, p, first, end, status_word, warp == 0)) {
             __syncthreads();                    // what was set up in front of the plan is seen
             return p;
         }

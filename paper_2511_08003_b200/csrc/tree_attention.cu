@@ -542,6 +542,9 @@ sharpv_status attend(
         a.v_scales = a.k_scales + scales_layout->stride_kv;
         a.scale_head = scales_layout->stride_head;
         a.scale_shift = log2_of(scales_layout->block_tokens);
+        // units that a sequence can have: key tiles times row tiles times heads
+        const int64_t units = ((cache_tokens + total_nodes) / a.split.keys + 3) * (total_nodes * group / ch.rows + 1) * H;
+        a.warp_plans = num_seqs <= 32 && units < 1 << 20;
     }
     int sms = 0;
     const sharpv_status ss = current_sms(sms);

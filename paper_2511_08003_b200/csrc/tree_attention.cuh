@@ -41,6 +41,7 @@ struct AttnArgs {
     const uint8_t* v_scales;
     int64_t scale_head;
     int scale_shift;
+    int warp_plans;             // few enough sequences and units for the loading warp to plan on its own
 };
 
 // Tensor maps of a call (bf16): boxes of 64 columns and a key tile's rows.  draft_* repeat cache_* where there are none.

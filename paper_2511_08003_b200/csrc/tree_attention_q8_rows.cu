@@ -47,7 +47,7 @@ struct Shared {
     uint8_t tiles[C::kStages][2][C::kTileBytes];
     uint8_t draft[2][C::kDraftBytes];
     float merge[C::kWarps][ROWS][C::kCols + 4];
-    float m[C::kWarps][ROWS], l[C::kWarps][ROWS];
+    float m[C::kWarps][ROWS], l[C::kWarps][ROWS], share[ROWS][16], top[ROWS], sum[ROWS];
     uint8_t q[2][ROWS * C::kQPitch];            // query rows of this portion and the next
     uint8_t qh[ROWS * C::kQPitch];              // this portion's as halves
     float q_unit[ROWS];                         // what a product of them stands for, times the scale of the scores
@@ -190,34 +190,47 @@ __device__ __forceinline__ void halve_queries(Shared<DP, ROWS>& sm, int at_part,
     }
 }
 
+// What every warp's sums count for in the joined ones: by threads of the first ROWS * 16 (half a warp a row).
+template <int DP, int ROWS>
+__device__ __forceinline__ void warp_shares(Shared<DP, ROWS>& sm) {
+    constexpr int kWarps = Cfg<DP, ROWS>::kWarps;
+    if (threadIdx.x >= ROWS * 16) return;
+    const int r = threadIdx.x >> 4, w = threadIdx.x & 15;
+    const float m = w < kWarps ? sm.m[w][r] : neg_inf();
+    float top = m;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float f = ex2(m - (top == neg_inf() ? 0.f : top));
+    float sum = w < kWarps ? f * sm.l[w][r] : 0.f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (w < kWarps) sm.share[r][w] = f;
+    if (w == 0) {
+        sm.top[r] = top;
+        sm.sum[r] = sum;
+    }
+}
+
 // Columns c0 .. of the warps' results joined, and written as the portion's (a partial result, or the rows themselves).
 template <int DP, int ROWS>
 __device__ __forceinline__ void join_warps(const AttnArgs& a, Shared<DP, ROWS>& sm, const Portion& p, int c0) {
     using C = Cfg<DP, ROWS>;
-    constexpr int kWarps = C::kWarps, kRows = ROWS;
+    constexpr int kWarps = C::kWarps;
     const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
     const int r_base = p.rt * ROWS, r_all = p.s.nodes * G;
     const bool complete = p.kt0 == 0 && p.kt1 == p.kt_all;
     const int slot = portion_slot(blockIdx.x, p.kt0);
-    constexpr int V = C::kCols / 4;
+    constexpr int V = C::kCols / 2;                     // two columns a thread
     for (int x = threadIdx.x; x < ROWS * V; x += kWarps * 32) {
-        const int r = x / V, c = c0 + (x % V) * 4, row = r_base + r;
+        const int r = x / V, c = c0 + (x % V) * 2, row = r_base + r;
         if (row >= r_all || c >= D) continue;
-        float top = sm.m[0][r];
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) top = fmaxf(top, sm.m[w][r]);
-        const float base = top == neg_inf() ? 0.f : top;
-        float sum = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float2 acc = make_float2(0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            const float f = ex2(sm.m[w][r] - base);
-            const float4 v = *reinterpret_cast<const float4*>(&sm.merge[w][r][c - c0]);
-            sum = fmaf(f, sm.l[w][r], sum);
+            const float f = sm.share[r][w];
+            const float2 v = *reinterpret_cast<const float2*>(&sm.merge[w][r][c - c0]);
             acc.x = fmaf(f, v.x, acc.x);
             acc.y = fmaf(f, v.y, acc.y);
-            acc.z = fmaf(f, v.z, acc.z);
-            acc.w = fmaf(f, v.w, acc.w);
         }
         if (sm.poison) {
             // what was set aside comes back to the rows that see it
@@ -227,24 +240,21 @@ __device__ __forceinline__ void join_warps(const AttnArgs& a, Shared<DP, ROWS>& 
                 const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(
                     a.draft_v + (int64_t)(p.s.node0 + j) * a.dv_node) + p.h * D + c;
                 const float v0 = __bfloat162float(v[0]), v1 = __bfloat162float(v[1]);
-                const float v2 = __bfloat162float(v[2]), v3 = __bfloat162float(v[3]);
                 if (!finite_f32(v0)) acc.x += v0;
                 if (!finite_f32(v1)) acc.y += v1;
-                if (!finite_f32(v2)) acc.z += v2;
-                if (!finite_f32(v3)) acc.w += v3;
             }
         }
+        const float top = sm.top[r], sum = sm.sum[r];
         const int64_t to = (int64_t)(p.s.node0 + row / G) * HQ + p.h * G + row % G;
         if (complete) {
             const float inv = row_scale(sum);
-            *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + to * D + c) =
-                make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+            *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(a.out) + to * D + c) = pack_bf16(acc.x * inv, acc.y * inv);
             if (c == 0) a.lse[to] = row_lse(top, sum);
         } else {
-            *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * kRows + r) * D + c) = acc;
+            *reinterpret_cast<float2*>(a.part_o + ((int64_t)slot * ROWS + r) * D + c) = acc;
             if (c == 0) {
-                a.part_ml[(int64_t)slot * 2 * kRows + r] = top;
-                a.part_ml[((int64_t)slot * 2 + 1) * kRows + r] = sum;
+                a.part_ml[(int64_t)slot * 2 * ROWS + r] = top;
+                a.part_ml[((int64_t)slot * 2 + 1) * ROWS + r] = sum;
             }
         }
     }
@@ -274,9 +284,13 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         sm.poison = sm.dead = 0;
     }
     if (warp == kWarps && lane < 4) tma_prefetch(&maps.cache_k + lane);
+    __syncthreads();
     cudaGridDependencySynchronize();
+    // the warps that compute are told their portions: where one warp can, the plan is the loading warp's alone
     int64_t first, end;
-    const PlanStart plan = plan_cta<kThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
+    PlanStart plan;
+    if (!a.warp_plans) plan = plan_cta<kThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
+    else if (warp == kWarps) (void)plan_warp(a.seqs, a.split, blockIdx.x, a.ctas, plan, first, end, a.status_word, true);
     bool alive = true;                          // a wait that gave up: nothing is waited for any more, the result is void
     uint32_t ring = 0, drafts = 0, pn = 0;      // tiles in the ring, drafted tiles and portions of this CTA so far
     const int G = a.split.group;
@@ -524,6 +538,10 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     *reinterpret_cast<float4*>(&sm.merge[warp][qr + 8][col]) = make_float4(o[j][0][2], o[j][1][2], o[j][0][3], o[j][1][3]);
             }
             consumer_sync<kWarps>();
+            if (c0 == 0) {
+                warp_shares<DP, 16>(sm);
+                consumer_sync<kWarps>();
+            }
             join_warps<DP, 16>(a, sm, p, c0);
             consumer_sync<kWarps>();
         }
@@ -561,9 +579,13 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
         sm.poison = sm.dead = 0;
     }
     if (warp == kWarps && lane < 4) tma_prefetch(&maps.cache_k + lane);
+    __syncthreads();
     cudaGridDependencySynchronize();
+    // the warps that compute are told their portions: where one warp can, the plan is the loading warp's alone
     int64_t first, end;
-    const PlanStart plan = plan_cta<kThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
+    PlanStart plan;
+    if (!a.warp_plans) plan = plan_cta<kThreads>(a.seqs, a.split, blockIdx.x, a.ctas, sm.plan, first, end, a.status_word);
+    else if (warp == kWarps) (void)plan_warp(a.seqs, a.split, blockIdx.x, a.ctas, plan, first, end, a.status_word, true);
     if (warp == kWarps) {
         load_portions<DP, 8>(a, maps, sm, plan, first, end);
         return;
@@ -784,6 +806,10 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                 for (int y = 0; y < 2; ++y)
                     *reinterpret_cast<float2*>(&sm.merge[warp][qc + y][j * 16 - c0 + kr * 2]) = make_float2(o[j][y], o[j][2 + y]);
             consumer_sync<kWarps>();
+            if (c0 == 0) {
+                warp_shares<DP, 8>(sm);
+                consumer_sync<kWarps>();
+            }
             join_warps<DP, 8>(a, sm, p, c0);
             consumer_sync<kWarps>();
         }
