@@ -27,7 +27,7 @@ namespace {
 
 constexpr int kKeys = kRowsTileKeys;            // of a tile
 // The split with what ending a segment and beginning another costs in these tiles, which take half the time of bf16 ones: the
-// ragged batch of 16 tokens 26.4 -> %.1f us.
+// ragged batch of 16 tokens 26.4 -> 22.2 us.
 struct CodeSplit : Split {
     static constexpr uint32_t kSwitch = 6;
 };
