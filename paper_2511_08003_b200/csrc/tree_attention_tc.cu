@@ -128,6 +128,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     uint64_t r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
@@ -140,60 +145,28 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
-// Four codes times a power of two as bf16, exactly; `f` holds it (and f2 a second factor, where one is not enough).
-//   e4m3: a code's exponent and mantissa in the places of bf16's are 2^-120 of its value, subnormal ones too
+// Four codes times a power of two as bf16, exactly.
+//   e4m3: by way of fp16, which keeps NaN and subnormal codes, and fp32
 //   int8: 128 + the low seven bits, and 128 or 256 by the sign, are bf16 numbers; their difference is the value
-template <int CODE, bool TWICE>
-__device__ __forceinline__ void bf16_of(uint32_t codes, __nv_bfloat162 f, __nv_bfloat162 f2, uint32_t& lo, uint32_t& hi) {
-    __nv_bfloat162 x[2];
+template <int CODE>
+__device__ __forceinline__ void bf16_of(uint32_t codes, float f, uint32_t& lo, uint32_t& hi) {
     if constexpr (CODE == SHARPV_E4M3) {
-        const uint32_t up = (codes >> 4 & 0x07070707u) | (codes & 0x80808080u), down = codes << 4 & 0xf0f0f0f0u;
-        const uint32_t a = __byte_perm(down, up, 0x5140), b = __byte_perm(down, up, 0x7362);
-        x[0] = *reinterpret_cast<const __nv_bfloat162*>(&a);
-        x[1] = *reinterpret_cast<const __nv_bfloat162*>(&b);
+        float x[4];
+        floats_of<CODE>(codes, x);
+        const uint64_t f2 = pack2(f, f);
+        unpack2(mul2(pack2(x[0], x[1]), f2), x[0], x[1]);
+        unpack2(mul2(pack2(x[2], x[3]), f2), x[2], x[3]);
+        lo = pack_bf16(x[0], x[1]);
+        hi = pack_bf16(x[2], x[3]);
     } else {
+        const __nv_bfloat162 f2 = __float2bfloat162_rn(f);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t w = __byte_perm(codes, 0x43434343u, i ? 0x4342 : 0x4140);
             const uint32_t m = w & 0xff7fff7fu, s = w & 0xff80ff80u;
-            x[i] = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&m), *reinterpret_cast<const __nv_bfloat162*>(&s));
+            const __nv_bfloat162 x = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&m), *reinterpret_cast<const __nv_bfloat162*>(&s)), f2);
+            (i ? hi : lo) = *reinterpret_cast<const uint32_t*>(&x);
         }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        x[i] = __hmul2(x[i], f);
-        if constexpr (TWICE) x[i] = __hmul2(x[i], f2);
-    }
-    lo = *reinterpret_cast<const uint32_t*>(&x[0]);
-    hi = *reinterpret_cast<const uint32_t*>(&x[1]);
-}
-
-// e4m3's NaN, which the above takes for 480: a carry into the signs' places of codes that are it, and such halves made NaN
-__device__ __forceinline__ uint32_t nan_carry(uint32_t codes) { return (codes & 0x7f7f7f7fu) + 0x01010101u; }
-__device__ __forceinline__ void keep_nan(uint32_t codes, uint32_t& lo, uint32_t& hi) {
-    const uint32_t n = nan_carry(codes);
-    lo |= (n & 0x80u ? 0x7fffu : 0u) | (n & 0x8000u ? 0x7fff0000u : 0u);
-    hi |= (n & 0x800000u ? 0x7fffu : 0u) | (n & 0x80000000u ? 0x7fff0000u : 0u);
-}
-
-// 64 columns of a row of codes to their places in 64 columns of a tile of bf16.
-template <int CODE, bool TWICE, bool NAN_TOO>
-__device__ __forceinline__ void write_columns(const uint4 (&w)[4], uint8_t* tile, int row, __nv_bfloat162 f, __nv_bfloat162 f2) {
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        uint4 lo, hi;
-        bf16_of<CODE, TWICE>(w[c].x, f, f2, lo.x, lo.y);
-        bf16_of<CODE, TWICE>(w[c].y, f, f2, lo.z, lo.w);
-        bf16_of<CODE, TWICE>(w[c].z, f, f2, hi.x, hi.y);
-        bf16_of<CODE, TWICE>(w[c].w, f, f2, hi.z, hi.w);
-        if constexpr (NAN_TOO) {
-            keep_nan(w[c].x, lo.x, lo.y);
-            keep_nan(w[c].y, lo.z, lo.w);
-            keep_nan(w[c].z, hi.x, hi.y);
-            keep_nan(w[c].w, hi.z, hi.w);
-        }
-        *reinterpret_cast<uint4*>(tile + swizzle128(row, c * 2)) = lo;
-        *reinterpret_cast<uint4*>(tile + swizzle128(row, c * 2 + 1)) = hi;
     }
 }
 
@@ -201,28 +174,25 @@ __device__ __forceinline__ void write_columns(const uint4 (&w)[4], uint8_t* tile
 // called as soon as the codes are in registers.
 template <int DP, int CODE, class Read>
 __device__ __forceinline__ void widen_row(const uint8_t* codes, uint8_t* tile, int row, bool there, int e, Read read) {
-    constexpr int kFree = CODE == SHARPV_E4M3 ? 120 : 0;
-    const int e1 = min(e + kFree, 127), e2 = e + kFree - e1;
-    const __nv_bfloat162 f = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)((e1 + 127) << 7)));
+    const float f = power_of_two(e);
 #pragma unroll
     for (int half = 0; half < DP / 64; ++half) {
         uint4 w[4];
-        uint32_t carry = 0;
 #pragma unroll
         for (int c = 0; c < 4; ++c)
             w[c] = *reinterpret_cast<const uint4*>(codes + (DP == 64 ? swizzle64(row, c) : swizzle128(row, half * 4 + c)));
         if (!there) w[0] = w[1] = w[2] = w[3] = make_uint4(0, 0, 0, 0);
-        if constexpr (CODE == SHARPV_E4M3) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) carry |= nan_carry(w[c].x) | nan_carry(w[c].y) | nan_carry(w[c].z) | nan_carry(w[c].w);
-        }
         if (half == DP / 64 - 1) read();
         uint8_t* to = tile + half * Cfg<DP, CODE>::kHalf;
-        if (__all_sync(0xffffffffu, e2 == 0 && (carry & 0x80808080u) == 0)) {
-            write_columns<CODE, false, false>(w, to, row, f, f);
-        } else {
-            const __nv_bfloat162 f2 = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)((e2 + 127) << 7)));
-            write_columns<CODE, true, CODE == SHARPV_E4M3>(w, to, row, f, f2);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            uint4 lo, hi;
+            bf16_of<CODE>(w[c].x, f, lo.x, lo.y);
+            bf16_of<CODE>(w[c].y, f, lo.z, lo.w);
+            bf16_of<CODE>(w[c].z, f, hi.x, hi.y);
+            bf16_of<CODE>(w[c].w, f, hi.z, hi.w);
+            *reinterpret_cast<uint4*>(to + swizzle128(row, c * 2)) = lo;
+            *reinterpret_cast<uint4*>(to + swizzle128(row, c * 2 + 1)) = hi;
         }
     }
 }
