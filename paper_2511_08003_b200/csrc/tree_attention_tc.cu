@@ -170,30 +170,25 @@ __device__ __forceinline__ void bf16_of(uint32_t codes, float f, uint32_t& lo, u
     }
 }
 
-// The row of a tile of codes that this thread owns, times 2^e, to a tile of bf16; zeros where the row is not there.  `read` is
-// called as soon as the codes are in registers.
-template <int DP, int CODE, class Read>
-__device__ __forceinline__ void widen_row(const uint8_t* codes, uint8_t* tile, int row, bool there, int e, Read read) {
-    const float f = power_of_two(e);
+// 64 columns of a thread's row: its codes, and those times 2^e in their places of a tile of bf16.
+template <int DP>
+__device__ __forceinline__ void read_codes(uint4 (&w)[4], const uint8_t* codes, int row, int half, bool there) {
 #pragma unroll
-    for (int half = 0; half < DP / 64; ++half) {
-        uint4 w[4];
+    for (int c = 0; c < 4; ++c)
+        w[c] = *reinterpret_cast<const uint4*>(codes + (DP == 64 ? swizzle64(row, c) : swizzle128(row, half * 4 + c)));
+    if (!there) w[0] = w[1] = w[2] = w[3] = make_uint4(0, 0, 0, 0);
+}
+template <int CODE>
+__device__ __forceinline__ void write_columns(const uint4 (&w)[4], uint8_t* to, int row, float f) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-            w[c] = *reinterpret_cast<const uint4*>(codes + (DP == 64 ? swizzle64(row, c) : swizzle128(row, half * 4 + c)));
-        if (!there) w[0] = w[1] = w[2] = w[3] = make_uint4(0, 0, 0, 0);
-        if (half == DP / 64 - 1) read();
-        uint8_t* to = tile + half * Cfg<DP, CODE>::kHalf;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            uint4 lo, hi;
-            bf16_of<CODE>(w[c].x, f, lo.x, lo.y);
-            bf16_of<CODE>(w[c].y, f, lo.z, lo.w);
-            bf16_of<CODE>(w[c].z, f, hi.x, hi.y);
-            bf16_of<CODE>(w[c].w, f, hi.z, hi.w);
-            *reinterpret_cast<uint4*>(to + swizzle128(row, c * 2)) = lo;
-            *reinterpret_cast<uint4*>(to + swizzle128(row, c * 2 + 1)) = hi;
-        }
+    for (int c = 0; c < 4; ++c) {
+        uint4 lo, hi;
+        bf16_of<CODE>(w[c].x, f, lo.x, lo.y);
+        bf16_of<CODE>(w[c].y, f, lo.z, lo.w);
+        bf16_of<CODE>(w[c].z, f, hi.x, hi.y);
+        bf16_of<CODE>(w[c].w, f, hi.z, hi.w);
+        *reinterpret_cast<uint4*>(to + swizzle128(row, c * 2)) = lo;
+        *reinterpret_cast<uint4*>(to + swizzle128(row, c * 2 + 1)) = hi;
     }
 }
 
@@ -240,11 +235,23 @@ __device__ __forceinline__ void widen_tiles(const AttnArgs& a, const AttnMaps& m
 #pragma unroll 1
                 for (int v = 0; v < 2; ++v, ++it, ++codes) {
                     const uint32_t from = codes % kCodeStages;
-                    if (!free_tile() || !wait_warp(&sm.c8.full8[from], codes / kCodeStages)) break;
-                    widen_row<DP, CODE>(sm.c8.codes[from], sm.tiles[it % C::kStages], t, there, e, [&] {
+                    if (!wait_warp(&sm.c8.full8[from], codes / kCodeStages)) break;
+                    uint8_t* const tile = sm.tiles[it % C::kStages];
+                    const float f = power_of_two(e);
+                    uint4 w[4];
+                    read_codes<DP>(w, sm.c8.codes[from], t, 0, there);
+                    auto given_back = [&] {             // the codes are in registers
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&sm.c8.empty8[from]);
-                    });
+                    };
+                    if (DP == 64) given_back();
+                    if (!free_tile()) break;
+                    write_columns<CODE>(w, tile, t, f);
+                    if constexpr (DP == 128) {
+                        read_codes<DP>(w, sm.c8.codes[from], t, 1, there);
+                        given_back();
+                        write_columns<CODE>(w, tile + C::kHalf, t, f);
+                    }
                     ready();
                     e = then;
                 }
