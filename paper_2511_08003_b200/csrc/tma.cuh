@@ -103,6 +103,9 @@ __device__ __forceinline__ void tma_load(void* dst, const CUtensorMap* map, uint
                  :: "r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 
+// writes of this thread to shared memory become visible to the tensor cores and to TMA
+__device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 // byte offset of 16-byte chunk c (0..7) of a 128-byte row in a swizzled tile that starts on a 1024-byte boundary
 __device__ __forceinline__ uint32_t swizzle128(int row, int c) { return (uint32_t)(row * 128 + ((c ^ (row & 7)) << 4)); }
 

@@ -44,22 +44,23 @@ struct Cfg {
     static constexpr int kStages = ROWS == 8 ? (DP == 64 ? 12 : 8) : (DP == 64 ? 12 : (DP == 128 ? 6 : 2));
     static_assert(kStages % kGroups == 0, "a stage belongs to one group");
     static constexpr int kQPitch = DP * 2 + 16;                 // bytes; 16 more, so that 8 rows fall on 8 bank groups
-    static constexpr int kCols = ROWS == 8 || DP < 128 ? 64 : 128;      // columns that are joined at a time
+    static constexpr int kCols = DP < 128 ? 64 : 128;           // columns that are joined at a time (16 rows)
 };
 
 template <int DP, int ROWS>
 struct Shared {
     using C = Cfg<DP, ROWS>;
     uint8_t tiles[C::kStages][2][C::kTileBytes];
+    // drafted tiles; 8 rows: the second 64 columns of the warps' sums as well, once a portion's tiles are gone through
     uint8_t draft[2][C::kDraftBytes];
-    float merge[C::kWarps][ROWS][C::kCols + 4];
-    float m[C::kWarps][ROWS], l[C::kWarps][ROWS], share[ROWS][16], top[ROWS], sum[ROWS];
+    float merge[C::kWarps][ROWS][ROWS == 8 ? 64 : C::kCols + 4];
+    float m[C::kWarps][ROWS], l[C::kWarps][ROWS];
     uint8_t q[2][ROWS * C::kQPitch];            // query rows of this portion and the next
     uint8_t qh[ROWS * C::kQPitch];              // this portion's as halves
     float q_unit[ROWS];                         // what a product of them stands for, times the scale of the scores
     Portion part[2];                            // kt1 < 0: there are no more
     uint64_t full[C::kStages], empty[C::kStages], part_full[2], part_empty[2], draft_full, draft_empty;
-    int poison, dead;
+    int poison[2], dead;
     PlanScratch<C::kThreads> plan;
 };
 
@@ -115,6 +116,8 @@ __device__ __forceinline__ void load_portions(const AttnArgs& a, const AttnMaps&
             for (int kt = p.kt0; kt < p.kt1; ++kt) {
                 if (kt >= p.kt_cache && a.split.draft) {
                     if (drafts >= 1) alive = mbar_wait(&sm.draft_empty, (drafts - 1) & 1);
+                    // with 8 rows the warps' sums of the portion before are joined in the same place
+                    if (ROWS == 8 && pn >= 1 && alive) alive = mbar_wait(&sm.part_empty[slot ^ 1], ((pn - 1) >> 1) & 1);
                     if (!alive) break;
                     mbar_expect(&sm.draft_full, 2 * C::kDraftBytes);
                     const int row = p.s.node0 + (kt - p.kt_cache) * kKeys;
@@ -196,74 +199,70 @@ __device__ __forceinline__ void halve_queries(Shared<DP, ROWS>& sm, int at_part,
     }
 }
 
-// What every warp's sums count for in the joined ones: by threads of the first ROWS * 16 (half a warp a row).
-template <int DP, int ROWS>
-__device__ __forceinline__ void warp_shares(Shared<DP, ROWS>& sm) {
-    constexpr int kWarps = Cfg<DP, ROWS>::kWarps;
-    if (threadIdx.x >= ROWS * 16) return;
-    const int r = threadIdx.x >> 4, w = threadIdx.x & 15;
-    const float m = w < kWarps ? sm.m[w][r] : neg_inf();
-    float top = m;
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float f = ex2(m - (top == neg_inf() ? 0.f : top));
-    float sum = w < kWarps ? f * sm.l[w][r] : 0.f;
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (w < kWarps) sm.share[r][w] = f;
-    if (w == 0) {
-        sm.top[r] = top;
-        sm.sum[r] = sum;
+// Two columns of a joined row, written as the portion's (a partial result, or the row itself) with what was set aside of drafted
+// values given back if the row sees it.
+template <int ROWS>
+__device__ __forceinline__ void write_columns(const AttnArgs& a, const Portion& p, int r, int c, float2 acc, float top, float sum, bool poison) {
+    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G, row = p.rt * ROWS + r;
+    if (poison) {
+        const int j0 = (max(p.kt0, p.kt_cache) - p.kt_cache) * kKeys, j1 = min(p.s.nodes, (p.kt1 - p.kt_cache) * kKeys);
+        for (int j = j0; j < j1; ++j) {
+            if (!(draft_sees(a, p.s, row / G, j & ~31) >> (j & 31) & 1)) continue;
+            const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(
+                a.draft_v + (int64_t)(p.s.node0 + j) * a.dv_node) + p.h * D + c;
+            const float v0 = __bfloat162float(v[0]), v1 = __bfloat162float(v[1]);
+            if (!finite_f32(v0)) acc.x += v0;
+            if (!finite_f32(v1)) acc.y += v1;
+        }
+    }
+    if (p.kt0 == 0 && p.kt1 == p.kt_all) {
+        const int64_t to = (int64_t)(p.s.node0 + row / G) * HQ + p.h * G + row % G;
+        const float inv = row_scale(sum);
+        *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(a.out) + to * D + c) = pack_bf16(acc.x * inv, acc.y * inv);
+        if (c == 0) a.lse[to] = row_lse(top, sum);
+    } else {
+        const int64_t slot = portion_slot(blockIdx.x, p.kt0);
+        *reinterpret_cast<float2*>(a.part_o + (slot * ROWS + r) * D + c) = acc;
+        if (c == 0) {
+            a.part_ml[slot * 2 * ROWS + r] = top;
+            a.part_ml[(slot * 2 + 1) * ROWS + r] = sum;
+        }
     }
 }
 
-// Columns c0 .. of the warps' results joined, and written as the portion's (a partial result, or the rows themselves).
+// What warp `lane` (of up to 16) counts for in row r's joined sums, and the row's maximum and sum: by a whole warp.
 template <int DP, int ROWS>
-__device__ __forceinline__ void join_warps(const AttnArgs& a, Shared<DP, ROWS>& sm, const Portion& p, int c0) {
-    using C = Cfg<DP, ROWS>;
-    constexpr int kWarps = C::kWarps;
-    const int D = a.head_dim, G = a.split.group, HQ = a.split.heads * G;
-    const int r_base = p.rt * ROWS, r_all = p.s.nodes * G;
-    const bool complete = p.kt0 == 0 && p.kt1 == p.kt_all;
-    const int slot = portion_slot(blockIdx.x, p.kt0);
-    constexpr int V = C::kCols / 2;                     // two columns a thread
-    for (int x = threadIdx.x; x < ROWS * V; x += kWarps * 32) {
-        const int r = x / V, c = c0 + (x % V) * 2, row = r_base + r;
-        if (row >= r_all || c >= D) continue;
-        float2 acc = make_float2(0.f, 0.f);
+__device__ __forceinline__ float warp_share(const Shared<DP, ROWS>& sm, int r, float& top, float& sum) {
+    constexpr int kWarps = Cfg<DP, ROWS>::kWarps;
+    const int w = threadIdx.x & 15;
+    const float m = w < kWarps ? sm.m[w][r] : neg_inf();
+    top = m;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float f = sm.share[r][w];
-            const float2 v = *reinterpret_cast<const float2*>(&sm.merge[w][r][c - c0]);
-            acc.x = fmaf(f, v.x, acc.x);
-            acc.y = fmaf(f, v.y, acc.y);
-        }
-        if (sm.poison) {
-            // what was set aside comes back to the rows that see it
-            const int j0 = (max(p.kt0, p.kt_cache) - p.kt_cache) * kKeys, j1 = min(p.s.nodes, (p.kt1 - p.kt_cache) * kKeys);
-            for (int j = j0; j < j1; ++j) {
-                if (!(draft_sees(a, p.s, row / G, j & ~31) >> (j & 31) & 1)) continue;
-                const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(
-                    a.draft_v + (int64_t)(p.s.node0 + j) * a.dv_node) + p.h * D + c;
-                const float v0 = __bfloat162float(v[0]), v1 = __bfloat162float(v[1]);
-                if (!finite_f32(v0)) acc.x += v0;
-                if (!finite_f32(v1)) acc.y += v1;
-            }
-        }
-        const float top = sm.top[r], sum = sm.sum[r];
-        const int64_t to = (int64_t)(p.s.node0 + row / G) * HQ + p.h * G + row % G;
-        if (complete) {
-            const float inv = row_scale(sum);
-            *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(a.out) + to * D + c) = pack_bf16(acc.x * inv, acc.y * inv);
-            if (c == 0) a.lse[to] = row_lse(top, sum);
-        } else {
-            *reinterpret_cast<float2*>(a.part_o + ((int64_t)slot * ROWS + r) * D + c) = acc;
-            if (c == 0) {
-                a.part_ml[(int64_t)slot * 2 * ROWS + r] = top;
-                a.part_ml[((int64_t)slot * 2 + 1) * ROWS + r] = sum;
-            }
-        }
+    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float f = ex2(m - (top == neg_inf() ? 0.f : top));
+    sum = w < kWarps ? f * sm.l[w][r] : 0.f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return f;
+}
+
+// 64 columns of a row from c0 on: by a whole warp, two columns a lane.  `at`: where warp w's sums of the lane's columns are.
+template <int DP, int ROWS, class At>
+__device__ __forceinline__ void join_row(const AttnArgs& a, const Shared<DP, ROWS>& sm, const Portion& p, int r, int c0, bool poison, At at) {
+    constexpr int kWarps = Cfg<DP, ROWS>::kWarps;
+    const int c = c0 + (threadIdx.x & 31) * 2;
+    if (p.rt * ROWS + r >= p.s.nodes * a.split.group) return;
+    float top, sum;
+    const float share = warp_share<DP, ROWS>(sm, r, top, sum);
+    float2 acc = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        const float f = __shfl_sync(0xffffffffu, share, w);
+        const float2 v = *reinterpret_cast<const float2*>(at(w));
+        acc.x = fmaf(f, v.x, acc.x);
+        acc.y = fmaf(f, v.y, acc.y);
     }
+    if (c < a.head_dim) write_columns<ROWS>(a, p, r, c, acc, top, sum, poison);
 }
 
 template <int CODE, int DP>
@@ -287,7 +286,7 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             mbar_init(&sm.part_empty[i], kWarps);
         }
         mbar_fence_init();
-        sm.poison = sm.dead = 0;
+        sm.poison[0] = sm.poison[1] = sm.dead = 0;
     }
     if (warp == kWarps && lane < 4) tma_prefetch(&maps.cache_k + lane);
     __syncthreads();
@@ -527,7 +526,7 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         }
 
         // ---- the eight warps' results are joined, up to 128 columns at a time
-        if (poison) sm.poison = 1;
+        if (poison) sm.poison[0] = 1;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
@@ -544,14 +543,13 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     *reinterpret_cast<float4*>(&sm.merge[warp][qr + 8][col]) = make_float4(o[j][0][2], o[j][1][2], o[j][0][3], o[j][1][3]);
             }
             consumer_sync<kWarps>();
-            if (c0 == 0) {
-                warp_shares<DP, 16>(sm);
-                consumer_sync<kWarps>();
+            for (int x = warp; x < 16 * (C::kCols / 64); x += kWarps) {
+                const int r = x / (C::kCols / 64), c = x % (C::kCols / 64) * 64;
+                join_row<DP, 16>(a, sm, p, r, c0 + c, sm.poison[0], [&](int w) { return &sm.merge[w][r][c + lane * 2]; });
             }
-            join_warps<DP, 16>(a, sm, p, c0);
             consumer_sync<kWarps>();
         }
-        if (threadIdx.x == 0) sm.poison = 0;
+        if (threadIdx.x == 0) sm.poison[0] = 0;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.part_empty[at_part]);
     }
@@ -582,7 +580,7 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             mbar_init(&sm.part_empty[i], kWarps);
         }
         mbar_fence_init();
-        sm.poison = sm.dead = 0;
+        sm.poison[0] = sm.poison[1] = sm.dead = 0;
     }
     if (warp == kWarps && lane < 4) tma_prefetch(&maps.cache_k + lane);
     __syncthreads();
@@ -601,26 +599,30 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     const int G = a.split.group;
     const int group = warp >> 2, sub = warp & 3;        // stages of this remainder, 16 keys from sub * 16 on
     const int kr = lane >> 2, qc = (lane & 3) * 2;      // fragment row (and row + 8), column (and column + 1)
-    for (uint32_t pn = 0;; ++pn) {
-        const int at_part = pn & 1;
-        if (alive && !mbar_wait(&sm.part_full[at_part], (pn >> 1) & 1)) {
+    // lanes 0 to 15: what stands at the scales of the warp's keys; 16 to 31: of its values.  Looked up a tile ahead.
+    auto scale_of = [&](const Portion& p, int kt) {
+        const int key = kt * kKeys + sub * 16 + (lane & 15);
+        const uint8_t* scales = (lane < 16 ? a.k_scales : a.v_scales) + p.h * a.scale_head;
+        return kt < p.kt_cache && key < p.s.len ? (uint32_t)__ldg(scales + ((p.s.begin + key) >> a.scale_shift)) : 127u;
+    };
+    auto first_scale = [&](const Portion& p) { return scale_of(p, p.kt0 + (int)((group - ring) & (C::kGroups - 1))); };
+    auto await_portion = [&](uint32_t n) {
+        if (alive && !mbar_wait(&sm.part_full[n & 1], (n >> 1) & 1)) {
             alive = false;
             report(a.status_word, SHARPV_ERR_TIMEOUT);
         }
         if (!alive) sm.dead = 1;
-        consumer_sync<kWarps>();                        // all warps go on or none does
+    };
+    await_portion(0);
+    consumer_sync<kWarps>();                            // all warps go on or none does
+    if (sm.dead || sm.part[0].kt1 < 0) return;
+    uint32_t next_scale = first_scale(sm.part[0]);
+    halve_queries<DP, 8>(sm, 0, a.scale_log2);
+    consumer_sync<kWarps>();
+    for (uint32_t pn = 0;; ++pn) {
+        const int at_part = pn & 1;
         const Portion p = sm.part[at_part];
-        if (p.kt1 < 0 || sm.dead) break;
         const int r_base = p.rt * 8, r_all = p.s.nodes * G;
-        // lanes 0 to 15: what stands at the scales of the warp's keys; 16 to 31: of its values.  Looked up a tile ahead.
-        const uint8_t* scales = (lane < 16 ? a.k_scales : a.v_scales) + p.h * a.scale_head;
-        auto scale_of = [&](int kt) {
-            const int key = kt * kKeys + sub * 16 + (lane & 15);
-            return kt < p.kt_cache && key < p.s.len ? (uint32_t)__ldg(scales + ((p.s.begin + key) >> a.scale_shift)) : 127u;
-        };
-        uint32_t next_scale = scale_of(p.kt0 + (int)((group - ring) & (C::kGroups - 1)));
-        halve_queries<DP, 8>(sm, at_part, a.scale_log2);
-        consumer_sync<kWarps>();
         const uint32_t q_off = (lane & 7) * C::kQPitch + (lane >> 3) * 16;
         const uint32_t q_base = smem_u32(sm.q[at_part]) + q_off;
         const float unit[2] = {sm.q_unit[qc], sm.q_unit[qc + 1]};
@@ -672,7 +674,7 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             uint64_t* full = drafted ? &sm.draft_full : &sm.full[at % C::kStages];
             uint64_t* empty = drafted ? &sm.draft_empty : &sm.empty[at % C::kStages];
             const uint32_t scale_code = next_scale;
-            next_scale = scale_of(kt + C::kGroups);
+            next_scale = scale_of(p, kt + C::kGroups);
             if (alive && !mbar_wait(full, (drafted ? at : at / C::kStages) & 1)) {
                 alive = false;
                 report(a.status_word, SHARPV_ERR_TIMEOUT);
@@ -796,32 +798,39 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             if (lane == 0) mbar_arrive(empty);
         }
 
-        // ---- the warps' results are joined, 64 columns at a time
-        if (poison) sm.poison = 1;
+        // ---- the warps' results are joined; meanwhile the next portion's query rows and first scales
+        if (poison) sm.poison[at_part] = 1;
+        await_portion(pn + 1);
+        const bool more = sm.part[at_part ^ 1].kt1 >= 0 && alive;
+        if (more) next_scale = first_scale(sm.part[at_part ^ 1]);
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
+        for (int y = 0; y < 2; ++y)
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) l[y] += __shfl_xor_sync(0xffffffffu, l[y], w);
+        consumer_sync<kWarps>();                        // the portion before is written, and this one's tiles are gone through
+        if (sm.dead) break;
+        // pairs of columns of every second row lie 64 bytes further round, so that four lanes with the same columns do not meet
+        float (*const late)[8][64] = reinterpret_cast<float (*)[8][64]>(&sm.draft[0][0]);
+        static_assert(DP == 64 || sizeof(sm.merge) <= sizeof(sm.draft), "");
+        auto pair_at = [](int row, int pair) { return (pair ^ (row >> 1 & 3) << 3) * 2; };
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
             if (kr == 0) { sm.m[warp][qc + y] = m[y]; sm.l[warp][qc + y] = l[y]; }
+#pragma unroll
+            for (int j = 0; j < DP / 16; ++j)
+                *reinterpret_cast<float2*>(&(j < 4 ? sm.merge : late)[warp][qc + y][pair_at(qc + y, (j & 3) * 8 + kr)]) = make_float2(o[j][y], o[j][2 + y]);
         }
-#pragma unroll
-        for (int c0 = 0; c0 < DP; c0 += C::kCols) {
-#pragma unroll
-            for (int j = c0 / 16; j < (c0 + C::kCols) / 16; ++j)
-#pragma unroll
-                for (int y = 0; y < 2; ++y)
-                    *reinterpret_cast<float2*>(&sm.merge[warp][qc + y][j * 16 - c0 + kr * 2]) = make_float2(o[j][y], o[j][2 + y]);
-            consumer_sync<kWarps>();
-            if (c0 == 0) {
-                warp_shares<DP, 8>(sm);
-                consumer_sync<kWarps>();
-            }
-            join_warps<DP, 8>(a, sm, p, c0);
-            consumer_sync<kWarps>();
+        if (more) halve_queries<DP, 8>(sm, at_part ^ 1, a.scale_log2);
+        if (threadIdx.x == 0) sm.poison[at_part ^ 1] = 0;
+        consumer_sync<kWarps>();
+        for (int x = warp; x < 8 * (DP / 64); x += kWarps) {
+            const int r = x / (DP / 64), c = x % (DP / 64);
+            join_row<DP, 8>(a, sm, p, r, c * 64, sm.poison[at_part] != 0, [&](int w) { return &(c == 0 ? sm.merge : late)[w][r][pair_at(r, lane)]; });
         }
-        if (threadIdx.x == 0) sm.poison = 0;
+        async_proxy_fence();                            // drafted tiles come by TMA where `late` was
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.part_empty[at_part]);
+        if (!more) break;
     }
 }
 
