@@ -12,8 +12,9 @@
 //   hands two keys of two neighbouring columns: even columns are one product, odd ones another.
 //   A key's scale multiplies its score.  A value's scale 2^e goes to its weight: the softmax runs over s_j + e_j, with m as its
 //   running maximum,   out = sum_j 2^(s_j + e_j - m) code_j / l,   l = sum_j 2^(s_j + e_j - m) 2^-e_j,
-//   so weights never pass what fp16 holds whatever the scales are.  m is kept 14 under the maximum: weights of 2^14 down to
-//   2^-14 are rounded to 11 bits, and what is 2^-28 of the largest loses by 2^-39 of it at most.
+//   so weights never pass what fp16 holds whatever the scales are.  m is set 8 under the maximum and kept until that has grown by
+//   7 more (sums are then rarely rescaled): the largest weight is between 2^8 and 2^15, weights down to 2^-14 are rounded to
+//   11 bits, and smaller ones lose 2^-25, 2^-33 of the largest, at most.
 //
 // Drafted tokens are bf16 and take products of bf16, in a buffer of their own (there are few of them).
 #include "q8.cuh"
@@ -32,7 +33,7 @@ struct CodeSplit : Split {
     static constexpr uint32_t kSwitch = 6;
 };
 
-constexpr float kHeadroom = 14.f;               // weights reach 2^14
+constexpr float kNominal = 8.f, kLazy = 7.f;    // the largest weight is 2^8 when the maximum is set, and stays under 2^15
 
 template <int DP, int ROWS>
 struct Cfg {
@@ -352,13 +353,14 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 float x = fmaxf(fmaxf(s[0][half * 2], s[0][half * 2 + 1]), fmaxf(s[1][half * 2], s[1][half * 2 + 1]));
                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-                top[half] = fmaxf(x - kHeadroom, m[half]);
+                top[half] = x - kNominal;
             }
-            if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
-                const float a0 = m[0] == top[0] ? 1.f : ex2(m[0] - top[0]);
-                const float a1 = m[1] == top[1] ? 1.f : ex2(m[1] - top[1]);
-                m[0] = top[0];
-                m[1] = top[1];
+            const bool grows0 = top[0] > m[0] + kLazy, grows1 = top[1] > m[1] + kLazy;
+            if (__any_sync(0xffffffffu, grows0 || grows1)) {
+                const float a0 = grows0 ? ex2(m[0] - top[0]) : 1.f;         // 0 where nothing was seen yet
+                const float a1 = grows1 ? ex2(m[1] - top[1]) : 1.f;
+                m[0] = grows0 ? top[0] : m[0];
+                m[1] = grows1 ? top[1] : m[1];
                 l[0] *= a0;
                 l[1] *= a1;
 #pragma unroll
@@ -599,13 +601,27 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     const int G = a.split.group;
     const int group = warp >> 2, sub = warp & 3;        // stages of this remainder, 16 keys from sub * 16 on
     const int kr = lane >> 2, qc = (lane & 3) * 2;      // fragment row (and row + 8), column (and column + 1)
-    // lanes 0 to 15: what stands at the scales of the warp's keys; 16 to 31: of its values.  Looked up a tile ahead.
-    auto scale_of = [&](const Portion& p, int kt) {
-        const int key = kt * kKeys + sub * 16 + (lane & 15);
-        const uint8_t* scales = (lane < 16 ? a.k_scales : a.v_scales) + p.h * a.scale_head;
-        return kt < p.kt_cache && key < p.s.len ? (uint32_t)__ldg(scales + ((p.s.begin + key) >> a.scale_shift)) : 127u;
+    // A portion's tiles in the ring (its cached ones, or one for rows without any key), which of them is the group's first, and lanes
+    // 0 to 15: what stands at the scales of the warp's keys in it, 16 to 31: of its values.  Scales are looked up a tile ahead.
+    constexpr int kTurn = C::kGroups * kKeys;           // rows from one of a group's tiles to its next: whole blocks
+    static_assert(kTurn % kMaxBlockTokens == 0, "scales of a group's tiles are a whole number of blocks apart");
+    struct Tiles { int n, first; };
+    auto tiles_of = [&](const Portion& p) {
+        return Tiles{a.split.draft ? max(min(p.kt1, p.kt_cache) - p.kt0, 0) : p.kt1 - p.kt0, (int)((group - ring) & (C::kGroups - 1))};
     };
-    auto first_scale = [&](const Portion& p) { return scale_of(p, p.kt0 + (int)((group - ring) & (C::kGroups - 1))); };
+    const uint8_t* scale_at = nullptr;                  // of the lane's key in the tile that is looked up
+    int scale_key = 0;                                  // that key
+    auto look_up = [&](int len) {
+        const uint32_t code = scale_key < len ? (uint32_t)__ldg(scale_at) : 127u;
+        scale_key += kTurn;
+        scale_at += kTurn >> a.scale_shift;
+        return code;
+    };
+    auto first_scale = [&](const Portion& p) {
+        scale_key = (p.kt0 + tiles_of(p).first) * kKeys + sub * 16 + (lane & 15);
+        scale_at = (lane < 16 ? a.k_scales : a.v_scales) + p.h * a.scale_head + ((p.s.begin + scale_key) >> a.scale_shift);
+        return look_up(p.kt0 < p.kt_cache ? p.s.len : 0);
+    };
     auto await_portion = [&](uint32_t n) {
         if (alive && !mbar_wait(&sm.part_full[n & 1], (n >> 1) & 1)) {
             alive = false;
@@ -645,13 +661,14 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                top[y] = fmaxf(x - kHeadroom, m[y]);
+                top[y] = x - kNominal;
             }
-            if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
+            if (__any_sync(0xffffffffu, top[0] > m[0] + kLazy || top[1] > m[1] + kLazy)) {
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const float f = m[y] == top[y] ? 1.f : ex2(m[y] - top[y]);
-                    m[y] = top[y];
+                    const bool grows = top[y] > m[y] + kLazy;
+                    const float f = grows ? ex2(m[y] - top[y]) : 1.f;       // 0 where nothing was seen yet
+                    m[y] = grows ? top[y] : m[y];
                     l[y] *= f;
 #pragma unroll
                     for (int j = 0; j < DP / 16; ++j) {
@@ -665,137 +682,143 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             for (int i = 0; i < 4; ++i) s[i] = ex2(s[i] - (i & 1 ? b1 : b0));
         };
 
-        for (int kt = p.kt0; kt < p.kt1; ++kt) {
-            const bool drafted = kt >= p.kt_cache && a.split.draft;
-            const uint32_t at = drafted ? drafts++ : ring++;
-            // a phase that is waited for has to be the next one of its barrier: a stage always has the same group, and so has the
-            // buffer of drafted tiles
-            if ((drafted ? 0 : (int)(at & (C::kGroups - 1))) != group) continue;
-            uint64_t* full = drafted ? &sm.draft_full : &sm.full[at % C::kStages];
-            uint64_t* empty = drafted ? &sm.draft_empty : &sm.empty[at % C::kStages];
-            const uint32_t scale_code = next_scale;
-            next_scale = scale_of(p, kt + C::kGroups);
-            if (alive && !mbar_wait(full, (drafted ? at : at / C::kStages) & 1)) {
+        const int vrow = sub * 16 + (lane & 15);
+        auto await_tile = [&](uint64_t* full, uint32_t phase) {
+            if (alive && !mbar_wait(full, phase & 1)) {
                 alive = false;
                 report(a.status_word, SHARPV_ERR_TIMEOUT);
             }
+        };
+        auto give_back = [&](uint64_t* empty) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty);
+        };
+        // a phase that is waited for has to be the next one of its barrier: a stage always has the same group, and so has the
+        // buffer of drafted tiles
+        const Tiles tiles = tiles_of(p);
+        int left = (p.kt0 < p.kt_cache ? p.s.len : 0) - (p.kt0 + tiles.first) * kKeys;        // keys of the tile that are there
+        for (int i = tiles.first; i < tiles.n; i += C::kGroups, left -= kTurn) {
+            const uint32_t at = ring + i;
+            const int stage = at % C::kStages;
+            const uint32_t scale_code = next_scale;
+            next_scale = look_up(p.s.len);
+            await_tile(&sm.full[stage], at / C::kStages);
             float s[4] = {};
-            const int vrow = sub * 16 + (lane & 15);
-            if (!drafted) {
-                const int stage = at % C::kStages;
-                const uint32_t ks_base = smem_u32(sm.tiles[stage][0]), vs_base = smem_u32(sm.tiles[stage][1]);
-                const int left = kt < p.kt_cache ? p.s.len - kt * kKeys : 0;        // keys of the tile that are there
-                const int krow = sub * 16 + (lane & 15);
-                float s1[4] = {};               // odd blocks of 16 columns: two chains of products
+            const uint32_t ks_base = smem_u32(sm.tiles[stage][0]), vs_base = smem_u32(sm.tiles[stage][1]);
+            float s1[4] = {};               // odd blocks of 16 columns: two chains of products
 #pragma unroll
-                for (int ks = 0; ks < DP / 16; ks += 2) {
-                    uint32_t k4[4], k0[4], k1[4];
-                    ldmatrix4(k4, ks_base + code_chunk<DP>(krow, ks + (lane >> 4)));
-                    halves_of<CODE>(k4[0], k0[0], k0[2]);
-                    halves_of<CODE>(k4[1], k0[1], k0[3]);
-                    halves_of<CODE>(k4[2], k1[0], k1[2]);
-                    halves_of<CODE>(k4[3], k1[1], k1[3]);
-                    mma_f16(s, k0, qf[ks / 2][0], qf[ks / 2][1]);
-                    mma_f16(s1, k1, qf[ks / 2][2], qf[ks / 2][3]);
-                }
-                const int exponent = scale_exponent(scale_code);
-                int ve[2];
+            for (int ks = 0; ks < DP / 16; ks += 2) {
+                uint32_t k4[4], k0[4], k1[4];
+                ldmatrix4(k4, ks_base + code_chunk<DP>(vrow, ks + (lane >> 4)));
+                halves_of<CODE>(k4[0], k0[0], k0[2]);
+                halves_of<CODE>(k4[1], k0[1], k0[3]);
+                halves_of<CODE>(k4[2], k1[0], k1[2]);
+                halves_of<CODE>(k4[3], k1[1], k1[3]);
+                mma_f16(s, k0, qf[ks / 2][0], qf[ks / 2][1]);
+                mma_f16(s1, k1, qf[ks / 2][2], qf[ks / 2][3]);
+            }
+            const int exponent = scale_exponent(scale_code);
+            int ve[2];
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    const float kx = power_of_two(__shfl_sync(0xffffffffu, exponent, n * 8 + kr));
-                    ve[n] = __shfl_sync(0xffffffffu, exponent, 16 + n * 8 + kr);
-                    const bool sees = sub * 16 + n * 8 + kr < left;
+            for (int n = 0; n < 2; ++n) {
+                const float kx = power_of_two(__shfl_sync(0xffffffffu, exponent, n * 8 + kr));
+                ve[n] = __shfl_sync(0xffffffffu, exponent, 16 + n * 8 + kr);
+                const bool sees = sub * 16 + n * 8 + kr < left;
 #pragma unroll
-                    for (int y = 0; y < 2; ++y)
-                        s[n * 2 + y] = sees ? fmaf((s[n * 2 + y] + s1[n * 2 + y]) * unit[y], kx, (float)ve[n]) : neg_inf();
-                }
-                weigh(s);
-                const float d0 = power_of_two(-ve[0]), d1 = power_of_two(-ve[1]);
-                l[0] += fmaf(s[0], d0, s[2] * d1);
-                l[1] += fmaf(s[1], d0, s[3] * d1);
-                // weights are rounded to fp16 for the product with the values; their sum is not
-                uint32_t pf[2];
-                transpose8(pf[0], pack_f16(s[0], s[1]));
-                transpose8(pf[1], pack_f16(s[2], s[3]));
+                for (int y = 0; y < 2; ++y)
+                    s[n * 2 + y] = sees ? fmaf((s[n * 2 + y] + s1[n * 2 + y]) * unit[y], kx, (float)ve[n]) : neg_inf();
+            }
+            weigh(s);
+            const float d0 = power_of_two(-ve[0]), d1 = power_of_two(-ve[1]);
+            l[0] += fmaf(s[0], d0, s[2] * d1);
+            l[1] += fmaf(s[1], d0, s[3] * d1);
+            // weights are rounded to fp16 for the product with the values; their sum is not
+            uint32_t pf[2];
+            transpose8(pf[0], pack_f16(s[0], s[1]));
+            transpose8(pf[1], pack_f16(s[2], s[3]));
 #pragma unroll
-                for (int j = 0; j < DP / 16; j += 2) {
-                    uint32_t v4[4];
-                    ldmatrix4_trans(v4, vs_base + code_chunk<DP>(vrow, j + (lane >> 4)));
-                    if (left < kKeys) {
-                        // rows that are not there may hold anything: 0 times them would not be 0
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int key = sub * 16 + (i & 1) * 8 + qc;
-                            if (key >= left) v4[i] = 0u;
-                            else if (key + 1 >= left) v4[i] &= 0xffffu;
-                        }
-                    }
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        uint32_t v[4];          // even columns, odd columns of keys 0 to 7, then of keys 8 to 15
-                        halves_of<CODE>(__byte_perm(v4[y * 2], 0u, 0x3120), v[0], v[1]);
-                        halves_of<CODE>(__byte_perm(v4[y * 2 + 1], 0u, 0x3120), v[2], v[3]);
-                        mma_f16(o[j + y], v, pf[0], pf[1]);
-                    }
-                }
-            } else {
-                const uint32_t ks_base = smem_u32(sm.draft[0]), vs_base = smem_u32(sm.draft[1]);
-                const int left = p.s.nodes - (kt - p.kt_cache) * kKeys;
-#pragma unroll
-                for (int ks = 0; ks < DP / 16; ks += 2) {
-                    uint32_t q4[4];
-                    ldmatrix4(q4, q_base + ks * 32);
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        uint32_t k4[4];
-                        ldmatrix4(k4, ks_base + (ks >> 2) * (kKeys * 128) + swizzle128(vrow, ((ks + y) & 3) * 2 + (lane >> 4)));
-                        mma_bf16(s, k4, q4[y * 2], q4[y * 2 + 1]);
-                    }
-                }
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const int row = r_base + qc + y;
-                    const int key0 = (kt - p.kt_cache) * kKeys + (sub >> 1) * 32;
-                    const uint32_t sees = row < r_all ? draft_sees(a, p.s, row / G, key0) >> ((sub & 1) * 16) : 0u;
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-                        s[n * 2 + y] = sees >> (n * 8 + kr) & 1 ? s[n * 2 + y] * a.scale_log2 : neg_inf();
-                }
-                weigh(s);
-                l[0] += s[0] + s[2];
-                l[1] += s[1] + s[3];
-                uint32_t pf[2];
-                transpose8(pf[0], pack_bf16(s[0], s[1]));
-                transpose8(pf[1], pack_bf16(s[2], s[3]));
-#pragma unroll
-                for (int j = 0; j < DP / 16; ++j) {
-                    uint32_t v4[4], v[4];
-                    ldmatrix4_trans(v4, vs_base + (j >> 2) * (kKeys * 128) + swizzle128(vrow, (j & 3) * 2 + (lane >> 4)));
-                    // rows that are not there may hold anything, and so may drafted rows that some query rows do not see
+            for (int j = 0; j < DP / 16; j += 2) {
+                uint32_t v4[4];
+                ldmatrix4_trans(v4, vs_base + code_chunk<DP>(vrow, j + (lane >> 4)));
+                if (left < kKeys) {
+                    // rows that are not there may hold anything: 0 times them would not be 0
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int key = sub * 16 + (i & 1) * 8 + qc;
                         if (key >= left) v4[i] = 0u;
                         else if (key + 1 >= left) v4[i] &= 0xffffu;
-                        const uint32_t off = nonfinite_bf16(v4[i]);
-                        v4[i] &= ~off;
-                        poison |= off != 0;
                     }
-                    // columns in the order of the sums: even ones, then odd ones
+                }
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const int from = ((2 * kr + y) & 7) * 4 + (lane & 3);
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const uint32_t low = __shfl_sync(0xffffffffu, v4[i], from), high = __shfl_sync(0xffffffffu, v4[2 + i], from);
-                            v[i * 2 + y] = kr < 4 ? low : high;
-                        }
-                    }
-                    mma_bf16(o[j], v, pf[0], pf[1]);
+                for (int y = 0; y < 2; ++y) {
+                    uint32_t v[4];          // even columns, odd columns of keys 0 to 7, then of keys 8 to 15
+                    halves_of<CODE>(__byte_perm(v4[y * 2], 0u, 0x3120), v[0], v[1]);
+                    halves_of<CODE>(__byte_perm(v4[y * 2 + 1], 0u, 0x3120), v[2], v[3]);
+                    mma_f16(o[j + y], v, pf[0], pf[1]);
                 }
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(empty);
+            give_back(&sm.empty[stage]);
+        }
+        ring += tiles.n;
+        for (int kt = max(p.kt0, p.kt_cache); a.split.draft && kt < p.kt1; ++kt, ++drafts) {
+            if (group != 0) continue;
+            await_tile(&sm.draft_full, drafts);
+            float s[4] = {};
+            const uint32_t ks_base = smem_u32(sm.draft[0]), vs_base = smem_u32(sm.draft[1]);
+            const int left = p.s.nodes - (kt - p.kt_cache) * kKeys;
+#pragma unroll
+            for (int ks = 0; ks < DP / 16; ks += 2) {
+                uint32_t q4[4];
+                ldmatrix4(q4, q_base + ks * 32);
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    uint32_t k4[4];
+                    ldmatrix4(k4, ks_base + (ks >> 2) * (kKeys * 128) + swizzle128(vrow, ((ks + y) & 3) * 2 + (lane >> 4)));
+                    mma_bf16(s, k4, q4[y * 2], q4[y * 2 + 1]);
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int row = r_base + qc + y;
+                const int key0 = (kt - p.kt_cache) * kKeys + (sub >> 1) * 32;
+                const uint32_t sees = row < r_all ? draft_sees(a, p.s, row / G, key0) >> ((sub & 1) * 16) : 0u;
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+                    s[n * 2 + y] = sees >> (n * 8 + kr) & 1 ? s[n * 2 + y] * a.scale_log2 : neg_inf();
+            }
+            weigh(s);
+            l[0] += s[0] + s[2];
+            l[1] += s[1] + s[3];
+            uint32_t pf[2];
+            transpose8(pf[0], pack_bf16(s[0], s[1]));
+            transpose8(pf[1], pack_bf16(s[2], s[3]));
+#pragma unroll
+            for (int j = 0; j < DP / 16; ++j) {
+                uint32_t v4[4], v[4];
+                ldmatrix4_trans(v4, vs_base + (j >> 2) * (kKeys * 128) + swizzle128(vrow, (j & 3) * 2 + (lane >> 4)));
+                // rows that are not there may hold anything, and so may drafted rows that some query rows do not see
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = sub * 16 + (i & 1) * 8 + qc;
+                    if (key >= left) v4[i] = 0u;
+                    else if (key + 1 >= left) v4[i] &= 0xffffu;
+                    const uint32_t off = nonfinite_bf16(v4[i]);
+                    v4[i] &= ~off;
+                    poison |= off != 0;
+                }
+                // columns in the order of the sums: even ones, then odd ones
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int from = ((2 * kr + y) & 7) * 4 + (lane & 3);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t low = __shfl_sync(0xffffffffu, v4[i], from), high = __shfl_sync(0xffffffffu, v4[2 + i], from);
+                        v[i * 2 + y] = kr < 4 ? low : high;
+                    }
+                }
+                mma_bf16(o[j], v, pf[0], pf[1]);
+            }
+            give_back(&sm.draft_empty);
         }
 
         // ---- the warps' results are joined; meanwhile the next portion's query rows and first scales

@@ -10,8 +10,8 @@ Bounds, with u = 2^-24 (half a step of fp32) and h half a step of the storage ty
       is a matter of the value alone.
   attention           as in decode_reference, over the values that the codes stand for.  The values' exponents (up to E) are added to
       the scores, and taken out of the sum again: X = max |score| + |lse| + E.  Query rows in fp16: a product is off by 2^-39 of the
-      row's largest element times the code's value.  Weights are rounded to bf16 or finer, those in fp16 that are 2^-28 of the
-      largest (times its scale) by 2^-39 of it: n 2^-39 448 max_j p_j 2^e_j / l.
+      row's largest element times the code's value.  Weights are rounded to bf16 or finer; in fp16 the largest (times its scale) is
+      2^8 at least, and those under 2^-14 are off by half a step of 2^-24, 2^-33 of it: n 2^-33 448 max_j p_j 2^e_j / l.
 """
 import numpy as np
 
@@ -137,7 +137,7 @@ def attention(q, kc, ks, vc, vs, kind, block, begin, length, offsets, dk, dv, tr
                     X = np.abs(s).max() + abs(lse[node, x]) + np.abs(ee).max()
                     e_p = e_s + 8 * U * X + 8 * U
                     A = p @ np.abs(vv) / l
-                    low = m * 2.0 ** -39 * 448 * (p * 2.0 ** ee).max() / l
+                    low = m * 2.0 ** -33 * 448 * (p * 2.0 ** ee).max() / l
                     out_tol[node, x] = (2 * e_p + 2 * m * U) * A + B16 * A + B16 * np.abs(out[node, x]) + low
                     lse_tol[node, x] = e_p + m * U + 2 * U * X
     return out, lse, 1.1 * out_tol, 1.1 * lse_tol
