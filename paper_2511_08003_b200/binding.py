@@ -633,7 +633,7 @@ def _attention_arrays(q, kv, lay, dev, dtype, draft_k, draft_v, tree_mask, out, 
             raise ValueError("tree_mask must be [nodes, words]")
         words, mask = tree_mask.shape[1], _on(tree_mask, "tree_mask", dev, _I32)
     if out is None:
-        o, lse = _like(q, stream), _empty((N, HQ), _F32, dev, stream)
+        o, lse = _like(q, stream), q.new_empty((N, HQ), dtype=_F32) if stream is None else _empty((N, HQ), _F32, dev, stream)
         out = {"out": o, "lse": lse}
         po, pl = o.data_ptr(), lse.data_ptr()
     else:
@@ -815,19 +815,19 @@ _Q8_CODES = {torch.float8_e4m3fn: E4M3, torch.int8: I8}
 
 def _q8_cache(kv: torch.Tensor, scales: torch.Tensor, block_tokens: int, name: str):
     """Layouts of a cache in 8 bits and of its scales [L, 2, H, blocks]: bytes x (uint8 or float8_e8m0fnu) for 2 ** (x - 127)."""
-    lay, dev = _cache(kv)
-    code = _Q8_CODES.get(kv.dtype)
+    code, n, k = _Q8_CODES.get(kv.dtype), kv.shape, kv.stride()
     if code is None:
         raise TypeError(f"{name} must be float8_e4m3fn or int8")
-    lay.dtype = code
-    s, st, n = scales.shape, scales.stride(), kv.shape
+    if not kv.is_cuda or len(n) != 5 or n[1] != 2 or k[4] != 1:
+        raise ValueError(f"{name} must be a [L, 2, H, T, D_h] view on a GPU with a contiguous last axis")
+    dev, s, st = kv.device, scales.shape, scales.stride()
     if scales.device != dev or scales.element_size() != 1:
         raise ValueError(f"the scales of {name} must be one byte each and on {dev}")
     if len(s) != 4 or s[0] != n[0] or s[1] != 2 or s[2] != n[2] or block_tokens < 1 or s[3] * block_tokens < n[3] or \
             (s[3] > 1 and st[3] != 1):
         raise ValueError(f"the scales of {name} must be [L, 2, H, blocks] with a contiguous last axis and a block for every "
                          "block_tokens rows")
-    return lay, KVScales(block_tokens, st[0], st[1], st[2]), dev
+    return KVLayout(n[0], n[2], n[4], code, k[0], k[1], k[2], k[3]), KVScales(block_tokens, st[0], st[1], st[2]), dev
 
 
 def sharpv_kv_append_q8(kv_src: torch.Tensor, kv_dst: torch.Tensor, dst_scales: torch.Tensor, block_tokens: int,
