@@ -255,6 +255,23 @@ def test_kv_append_q8_borders_ties_and_what_is_not_finite(source, kind):
     s.check()
 
 
+@pytest.mark.parametrize("kind", ["e4m3", "i8"])
+@pytest.mark.parametrize("source", ["e4m3", "i8"])
+def test_kv_append_q8_scales_far_apart(source, kind):
+    """Rows of a block whose scales differ by anything, rows of the smallest codes alone, and scales beyond what is used."""
+    s = Store(source, kind, 16, 1, 64, [0, 5], [16 * 40, 70], spare=0, src_block=1)
+    g = np.random.default_rng(7)
+    bits = _bits(s.src).copy()
+    far = g.integers(60, 200, s.src_scales.shape).astype(np.uint8)
+    far[..., 200:400] = g.integers(120, 134, far[..., 200:400].shape)
+    small = np.array([0, 1, 2, 0x81] if source == "e4m3" else [0, 1, 255, 0], np.uint8)
+    bits[..., 100:140, :] = small[g.integers(0, 4, bits[..., 100:140, :].shape)]
+    far[..., 112:128] = 127                     # a block of the smallest codes with one scale
+    s.src, s.src_scales = torch.from_numpy(bits).cuda().view(CODES[source]), torch.from_numpy(far).cuda()
+    s.x = ref.values_of(bits, source) * 2.0 ** ref.clamped(far)[..., None]
+    s.check()
+
+
 def test_kv_append_q8_layer_range_and_twice():
     s = Store("bf16", "e4m3", 32, 2, 64, [5, 40], [100, 9], layers=4)
     s.call(layer_begin=1, layer_end=3)
