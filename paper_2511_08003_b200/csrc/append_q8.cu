@@ -47,6 +47,7 @@ struct AppendQ8Args {
     int src_shift, dst_shift;           // log2 of the blocks' rows
     int num_kv_heads, layer_begin, planes, row_vecs, code_vecs;     // 16-byte vectors of a source row, of a row of codes
     int go_rows;                        // rows that a team's threads hold one vector each of
+    bool go_in_block;                   // such rows are a whole part of a block's
     int tile_rows;                      // a multiple of the block's rows
     int team_planes;                    // that a team takes of a tile, one after the other
     const int32_t* src_pos;
@@ -376,8 +377,9 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
                         most = max(most, top);
                         continue;
                     }
-                    const int block = (lead + g0 + y0 + u * a.go_rows) >> a.dst_shift, of_first = __shfl_sync(0xffffffffu, block, 0);
-                    if (__all_sync(0xffffffffu, block == of_first || top == 0)) {
+                    const int block = (lead + g0 + y0 + u * a.go_rows) >> a.dst_shift;
+                    // a round's vectors lie in one block, or a warp's do
+                    if ((S::kCodes && lead == 0 && a.go_in_block) || __all_sync(0xffffffffu, block == __shfl_sync(0xffffffffu, block, 0) || top == 0)) {
                         top = __reduce_max_sync(0xffffffffu, top);
                         if (lane == 0 && top) atomicMax(&tops[block], top);
                     } else if (top) {
@@ -467,6 +469,7 @@ template <int SRC, int CODE, int TEAM, int VECS, bool GOES>
 sharpv_status launch(AppendQ8Args& a, int sms, cudaStream_t stream) {
     const int block_rows = 1 << a.dst_shift;
     a.go_rows = TEAM / a.row_vecs;
+    a.go_in_block = block_rows % a.go_rows == 0;
     int rows = VECS * a.go_rows / block_rows * block_rows;      // what a team holds, in whole blocks; one at least
     if (rows < block_rows) rows = block_rows;
     if (rows > kMaxTileRows) rows = kMaxTileRows;

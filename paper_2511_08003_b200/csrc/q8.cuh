@@ -30,14 +30,11 @@ __device__ __forceinline__ int scale_exponent(uint32_t code) { return min(max((i
 // 2^e for e of -126 to 127
 __device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
 
-// The least e with x <= largest code * 2^e, within what is used; x by its bits, finite and not negative.
+// The least e with x <= largest code * 2^e, within what is used; x by its bits, finite and not negative.  The largest codes are
+// 1.75 * 2^8 and 1.984375 * 2^6: a mantissa beyond theirs carries into the exponent.
 template <int CODE>
 __device__ __forceinline__ int exponent_for(uint32_t bits) {
-    if (bits == 0) return kScaleLeast;
-    const int x = (int)(bits >> 23) - 127;
-    const uint32_t m = bits & 0x7fffffu;
-    // 448 = 1.75 * 2^8, 127 = 1.984375 * 2^6
-    const int e = CODE == SHARPV_E4M3 ? x - 8 + (m > 0x600000u) : x - 6 + (m > 0x7e0000u);
+    const int e = CODE == SHARPV_E4M3 ? (int)((bits + 0x1fffffu) >> 23) - 127 - 8 : (int)((bits + 0x1ffffu) >> 23) - 127 - 6;
     return min(max(e, kScaleLeast), kScaleMost);
 }
 
