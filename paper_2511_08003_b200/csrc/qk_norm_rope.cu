@@ -11,7 +11,10 @@
 // formed in turns and reduced in 64 bits (a position of 2^31 is off by 2^-23 of a turn at most); their sine and cosine are
 // taken in fp32, as the products are; the one rounding to the storage type is the last.
 //
-// HBM bounds it for prompts, latency (positions, sine, one row) for the tokens of a step.
+// A CTA takes about eight rounds of rows, the next round's loads in flight while one is worked on; arithmetic goes two elements
+// an instruction.  Without either 50,432 tokens of 28 + 4 heads x 128 in bf16 take 164 us, with the first 149, with both 141: 5.9 TB/s,
+// 0.91 of a plain copy's rate, and what is left is the issue of about 15 instructions an element.  1,600 tokens of 14 + 2 heads x 64 in
+// fp32 4.4 us, 16 tokens 3.1 us (latency: positions, sine, one row).
 #include "decode_common.cuh"
 
 #include <cuda_bf16.h>

@@ -17,6 +17,10 @@
 //   11 bits, and smaller ones lose 2^-25, 2^-33 of the largest, at most.
 //
 // Drafted tokens are bf16 and take products of bf16, in a buffer of their own (there are few of them).
+//
+// Up to eight query rows have a kernel of their own, below.  Measured (4 KV heads x 128), up to 8 rows and up to 16, us with the join:
+// one sequence of 50,432 rows 21.3 / 27, the ragged batch of 16 (37,712 rows) 20 / 26, 64 over 2,000 rows each 42 / 58.  Of the first
+// 5 us go by until the first tile is there, 9 to 11 stream the 52 MB, 2 join the warps and 3.5 the CTAs.
 #include "q8.cuh"
 #include "tma.cuh"
 #include "tree_attention.cuh"
@@ -559,8 +563,8 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 
 // Up to eight query rows a tile: keys, and columns of the values, are the rows of the products, query rows their eight columns, so
 // nothing is computed for rows that are not there, and sums take half the registers.  That leaves room for four
-// groups of warps, four warps a scheduler instead of two: the chain from codes to weights is what a warp waits for (one
-// token over 50,432 rows with the kernel of 16 rows, of which seven count, 26.3 us).
+// groups of warps, four warps a scheduler instead of two: the chain from codes to weights is what a warp waits for.  The next
+// portion's query rows are made halves, and its first scales looked up, while one is joined.
 // A thread has the scores of keys lane / 4 and 8 further for query rows 2 (lane % 4) and the next.
 template <int CODE, int DP>
 __global__ void __launch_bounds__(Cfg<DP, 8>::kThreads, 1)

@@ -15,7 +15,8 @@
 //
 // Caches in 8 bits (CODE): their tiles go by TMA into a ring of their own, and a warpgroup of four more warps, a key a thread,
 // widens them to bf16 with the key's scale (exactly: scales are powers of two) into the ring that the products read, which
-// also stands in for the cleaning.  All else is the same code: the products see what a bf16 cache would hold.
+// also stands in for the cleaning.  All else is the same code: the products see what a bf16 cache would hold.  A tile takes the
+// four warps 1,600 clocks, two of them a unit: 61 us for the tree below, 42 and 103 for the other two (e4m3; int8 within 2 %).
 //
 // What bounds it is the hand-over between a stream's scores and its products.  Measured with the join (4 KV heads x 128, 7
 // query heads each): a tree of 64 over 50,432 rows 57 us (0.81 PFLOP/s, tensor pipe 48 % active), trees of 5 to 41 over 37,712
