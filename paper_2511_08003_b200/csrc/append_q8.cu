@@ -18,7 +18,7 @@
 // two at a time in the source's own type, products with powers of two are formed two at a time, and rounding to whole
 // numbers is the addition of a number whose last place is 1.
 //
-// HBM bounds long lists: 37,712 rows of 224 planes x 256 bytes 513 us (6.3 TB/s, 0.98 of a plain copy's rate; 636 without the next
+// HBM bounds long lists: 37,712 rows of 224 planes x 256 bytes 513 to 519 us (6.3 TB/s, 0.97 to 0.98 of a plain copy's rate; 636 without the next
 // plane's loads in flight, 1,634 with every index divided out and elements compared one at a time).  From 8 bits to 8 bits there are
 // more codes a byte, and instructions bound it: half of these rows, int8 to int8, 211 us (0.79).  43 rows 7.1 us: latency
 // (tables, rows, maximum, codes).

@@ -19,8 +19,8 @@
 // Drafted tokens are bf16 and take products of bf16, in a buffer of their own (there are few of them).
 //
 // Up to eight query rows have a kernel of their own, below.  Measured (4 KV heads x 128), up to 8 rows and up to 16, us with the join:
-// one sequence of 50,432 rows 21.3 / 27, the ragged batch of 16 (37,712 rows) 20 / 26, 64 over 2,000 rows each 42 / 58.  Of the first
-// 5 us go by until the first tile is there, 9 to 11 stream the 52 MB, 2 join the warps and 3.5 the CTAs.
+// one sequence of 50,432 rows 21.3 / 27, the ragged batch of 16 (37,712 rows) 20 / 26, 64 over 2,000 rows each 42 / 58.  In the first
+// 5 us go by until the first tile is there, 10 stream the 52 MB, 1.5 join the warps and write (stamped at 22.9 us); the rest joins the CTAs.
 #include "q8.cuh"
 #include "tma.cuh"
 #include "tree_attention.cuh"
