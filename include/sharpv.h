@@ -483,7 +483,7 @@ sharpv_status sharpv_kv_append(
  *   attention or sharpv_kv_append reads them).  An output may be its own input (same pointer and strides); otherwise outputs
  *   overlap neither inputs nor each other.
  * q_weight, k_weight [dev] [head_dim] of the same type, or NULL: ones (they must be NULL where norm = 0).
- * positions [dev] int32[num_axes, num_tokens], row stride ld_positions; any value.  Angles are formed and reduced in
+ * positions [dev] int32[num_axes, num_tokens], row stride ld_positions (0: all axes share one row); any value.  Angles are formed and reduced in
  *   64 bits, their sine and cosine taken in fp32.
  * SHARPV_F32 and SHARPV_BF16; head_dim of at most 256, head_dim and rotary_dim / 2 elements multiples of 16 bytes, strides under
  * 2 GB; at most 8 axes and 4096 heads in all.  rotary_dim = 0 is the norm alone (norm = 0 and rotary_dim = 0: SHARPV_ERR_INVALID_ARG).

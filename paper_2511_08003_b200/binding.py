@@ -774,7 +774,7 @@ def sharpv_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tenso
                         k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
                         out: Optional[Dict[str, torch.Tensor]] = None, stream=None) -> Dict[str, torch.Tensor]:
     """Norm of every head (norm=True; weights [head_dim] or None) and its rotation by the token's positions int32 [axes,
-    tokens] (or [tokens]): q [tokens, q_heads, head_dim], k [tokens, heads, head_dim], any token and head strides.
+    tokens] (or [tokens]; a view that expands one row will do): q [tokens, q_heads, head_dim], k [tokens, heads, head_dim], any token and head strides.
     pair_axis: for each of the rotary_dim / 2 pairs the axis whose position turns it (bytes or a sequence of ints).
     Returns dict(q, k), dense unless `out` holds them; out may hold q and k themselves."""
     dev, dtype, qs, ks = q.device, q.dtype, q.shape, k.shape

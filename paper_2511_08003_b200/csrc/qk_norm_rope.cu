@@ -283,7 +283,7 @@ extern "C" sharpv_status sharpv_qk_norm_rope(
     for (int i = 0; i < rotary_dim / 2; ++i)
         if (pair_axis[i] >= num_axes) return SHARPV_ERR_INVALID_ARG;
     if (num_tokens == 0) return SHARPV_OK;
-    if (!q || !k || !out_q || !out_k || (rotary_dim > 0 && (!positions || (num_axes > 1 && ld_positions < num_tokens))))
+    if (!q || !k || !out_q || !out_k || (rotary_dim > 0 && (!positions || (num_axes > 1 && ld_positions < num_tokens && ld_positions != 0))))
         return SHARPV_ERR_INVALID_ARG;
     const int64_t strides[8] = {ld_q, head_q, ld_k, head_k, ld_out_q, head_out_q, ld_out_k, head_out_k};
     for (int i = 0; i < 8; ++i) {

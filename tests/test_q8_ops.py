@@ -115,6 +115,17 @@ def test_qk_norm_rope_no_tokens_and_outputs_with_strides():
     assert bool((cache[:, :5] == 7).all()) and bool((cache[:, 14:] == 7).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [1, 40, 700])
+def test_qk_norm_rope_of_text_whose_axes_share_their_positions(N, dtype):
+    """A text token's axes all hold the same number: a view without a stride between the axes will do."""
+    q = torch.randn((N, 6, 64), device="cuda").to(DT[dtype])
+    pos, axis = _i32(np.arange(N) * 7 - 3), [i % 3 for i in range(32)]
+    want = sv.sharpv_qk_norm_rope(q, q[:, :2], pos.expand(3, N).contiguous(), axis, 1e6, norm=True)
+    got = sv.sharpv_qk_norm_rope(q, q[:, :2], pos.expand(3, N), axis, 1e6, norm=True)
+    assert torch.equal(got["q"], want["q"]) and torch.equal(got["k"], want["k"])
+
+
 def test_qk_norm_rope_agrees_with_the_compaction():
     """Rotation to a position by this call is the rotation that sharpv_kv_compact_rope adds to keys at position 0."""
     n, D = 6, 64
