@@ -52,6 +52,7 @@ ROPE = dict(q=P, ldq=4608, hsq=128, k=P, ldk=4608, hsk=128, dtype=1, N=9, HQ=28,
     (dict(rot=72), S.ERR_UNSUPPORTED), (dict(axes=9), S.ERR_UNSUPPORTED), (dict(HQ=4093), S.ERR_UNSUPPORTED),
     (dict(N=1 << 31), S.ERR_UNSUPPORTED), (dict(q=P + 8), S.ERR_UNSUPPORTED), (dict(ok=P + 2), S.ERR_UNSUPPORTED),
     (dict(qw=P + 8), S.ERR_UNSUPPORTED), (dict(ldq=4604), S.ERR_UNSUPPORTED), (dict(hsok=132), S.ERR_UNSUPPORTED),
+    (dict(ldq=1 << 30), S.ERR_UNSUPPORTED), (dict(hsok=1 << 30), S.ERR_UNSUPPORTED), (dict(ldp=-1), S.ERR_INVALID_ARG),
     (dict(N=0), S.OK), (dict(N=0, q=None, pos=None), S.OK),
 ])
 def test_qk_norm_rope_refusals(L, change, status):
