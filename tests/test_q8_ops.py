@@ -523,6 +523,24 @@ def test_tree_attention_q8_ignores_what_is_not_seen(value, nodes, kind):
     assert not bool(torch.isfinite(got["out"][last]).all())
 
 
+@pytest.mark.parametrize("kind", ["e4m3", "i8"])
+@pytest.mark.parametrize("HQ,D", [(1, 64), (7, 128), (12, 64), (12, 128), (3, 256)])
+def test_tree_attention_q8_large_queries_over_small_scales(HQ, D, kind):
+    """Few query rows that overflow with the codes alone, where the scale of the key brings the score back.  One key: its weight is
+    relative to its own score, and out is its value.  (With many rows scores and maximum are scaled apart: at scores X a weight's
+    exponent is off by u X, which is past any bound here, over a 16-bit cache as well.)  The products are whole multiples of one power
+    of two and their sum is under 2^24 of them, so the score is rounded with the scale of the scores, with its own product and as
+    lse: 4 u, and 4 more for the logarithms' base."""
+    code, top = (0x7e, 448.0) if kind == "e4m3" else (0x70, 112.0)
+    kv = torch.full((1, 2, 1, 16, D), code, dtype=torch.uint8, device="cuda").view(CODES[kind])
+    scales = torch.full((1, 2, 1, 1), 127 - 48, dtype=torch.uint8, device="cuda")
+    q = torch.full((1, HQ, D), 1.5 * 2.0 ** 118, device="cuda").bfloat16()
+    got = sv.sharpv_tree_attention_q8(q, kv, scales, 16, 0, _i32([5]), _i32([1]), _i32([0, 1]))
+    score = D ** -0.5 * D * 1.5 * 2.0 ** 118 * top * 2.0 ** -48
+    assert bool((got["out"].double() == top * 2.0 ** -48).all())
+    assert float((got["lse"].double() / score - 1).abs().max()) <= 8 * U
+
+
 @pytest.mark.parametrize("nodes", [2, 50])
 def test_tree_attention_q8_shows_what_is_seen(nodes):
     c = Attn("e4m3", 16, 1, 4, 128, [200], [nodes], tree=None, spare=0)
