@@ -542,9 +542,10 @@ sharpv_status sharpv_kv_append_q8(
  * the drafted tokens.  q, draft_k, draft_v and out are SHARPV_BF16; the layout's dtype is SHARPV_E4M3 or SHARPV_I8, head_dim a
  * multiple of 16.  All else as there: tables, masks, rows that see nothing, errors, workspace.
  * Scores, the softmax's maximum and sum, the weighted sums and lse are fp32.  Weights are rounded to 16 bits before they multiply
- * the values, so a component of out is off by up to 2^-8 sum_j p_j |v_j| / sum_j p_j for that and 2^-8 |out| for its own
- * rounding.  (Up to 16 average query rows a sequence and KV head, and where head_dim is over 128, cached values are weighted in
- * fp16 relative to the largest weight times scale, which is eight times as exact.)
+ * the values: a weight p_j is off by up to 2^-8 p_j or 2^-25 max p, so a component of out by up to (2^-8 sum_j p_j |v_j| +
+ * 2^-25 max p sum_j |v_j|) / sum_j p_j for that and 2^-8 |out| for its own rounding.  (Up to 16 average query rows a sequence and KV
+ * head, and where head_dim is over 128, cached values are weighted in fp16, 2^-11 p_j in place of 2^-8 p_j, as long as the scales of
+ * values that are read together are within 2^8 of each other, and in bf16 where they are not.  Elsewhere weights are bf16.)
  */
 size_t sharpv_tree_attention_q8_workspace_bytes(int32_t num_seqs, int64_t total_nodes, int32_t num_q_heads,
                                                 int32_t num_kv_heads, int32_t head_dim);

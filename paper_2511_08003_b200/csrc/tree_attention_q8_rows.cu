@@ -14,7 +14,10 @@
 //   running maximum,   out = sum_j 2^(s_j + e_j - m) code_j / l,   l = sum_j 2^(s_j + e_j - m) 2^-e_j,
 //   so weights never pass what fp16 holds whatever the scales are.  m is set 8 under the maximum and kept until that has grown by
 //   7 more (sums are then rarely rescaled): the largest weight is between 2^8 and 2^15, weights down to 2^-14 are rounded to
-//   11 bits, and smaller ones lose 2^-25, 2^-33 of the largest, at most.
+//   11 bits, and smaller ones lose 2^-25, 2^-33 of the largest, at most.  That is of the largest with its value's scale on it, whatever
+//   the codes there are: a weight p_j itself is off by 2^-33 2^(E - e_j) of the largest p, E being the largest exponent so far.  So a
+//   warp takes a tile with e_j < E - 8 (SpanOfScales) by products of bf16, which has fp32's exponents and holds the codes of both
+//   kinds: weights have 8 bits there, however far the scales are apart.  Elsewhere p_j is off by 2^-25 of the largest at most.
 //
 // Drafted tokens are bf16 and take products of bf16, in a buffer of their own (there are few of them).
 //
@@ -76,6 +79,36 @@ __device__ __forceinline__ void consumer_sync() { asm volatile("bar.sync 1, %0;"
 __device__ __forceinline__ void transpose8(uint32_t& to, uint32_t from) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(to) : "r"(from));
 }
+
+// The exponents that a warp's values have had so far in a portion, as far as fp16 weights go by them.
+struct SpanOfScales {
+    static constexpr int kSpan = 8;
+    int top = kScaleLeast - 1;
+    // Whether values of this tile, whose exponents the lanes that `have` one hold, have weights that fp16 does not hold well.  By a whole
+    // warp, with one vote where nothing is new.
+    __device__ __forceinline__ bool wide(int exponent, bool have) {
+        if (!__any_sync(0xffffffffu, have && (exponent > top || exponent < top - kSpan))) return false;
+        top = max(top, __reduce_max_sync(0xffffffffu, have ? exponent : kScaleLeast - 1));
+        return __any_sync(0xffffffffu, have && exponent < top - kSpan);
+    }
+};
+
+// What a tile's products of weights and values take: fp16, or bf16 where the scales are far apart.
+struct InHalves {
+    __device__ __forceinline__ static uint32_t pack(float lo, float hi) { return pack_f16(lo, hi); }
+    template <int CODE> __device__ __forceinline__ static void codes(uint32_t four, uint32_t& lo, uint32_t& hi) { halves_of<CODE>(four, lo, hi); }
+    __device__ __forceinline__ static void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) { mma_f16(c, a, b0, b1); }
+};
+struct InBf16 {
+    __device__ __forceinline__ static uint32_t pack(float lo, float hi) { return pack_bf16(lo, hi); }
+    template <int CODE> __device__ __forceinline__ static void codes(uint32_t four, uint32_t& lo, uint32_t& hi) {
+        float x[4];
+        floats_of<CODE>(four, x);
+        lo = pack_bf16(x[0], x[1]);
+        hi = pack_bf16(x[2], x[3]);
+    }
+    __device__ __forceinline__ static void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) { mma_bf16(c, a, b0, b1); }
+};
 
 // byte offset of 16-byte chunk c of a row of codes
 template <int DP>
@@ -343,6 +376,7 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         // of 16 columns from 16 j on: o[j][0] the even ones, o[j][1] the odd ones; a thread has columns 4 (lane & 3) .. + 3
         float o[DP / 16][2][4];
         float m[2] = {neg_inf(), neg_inf()}, l[2] = {0.f, 0.f};        // of rows qr and qr + 8
+        SpanOfScales span;
 #pragma unroll
         for (int j = 0; j < DP / 16; ++j)
 #pragma unroll
@@ -436,38 +470,41 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                         s[n][2 + i] = sees ? fmaf(s[n][2 + i], unit[1] * kx, (float)ve[n][i]) : neg_inf();
                     }
                 weigh(s);
-                uint32_t pf[4];
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
                     const float d0 = power_of_two(-ve[n][0]), d1 = power_of_two(-ve[n][1]);
                     l[0] += fmaf(s[n][0], d0, s[n][1] * d1);
                     l[1] += fmaf(s[n][2], d0, s[n][3] * d1);
-                    // weights are rounded to fp16 for the product with the values; their sum is not
-                    pf[n * 2] = pack_f16(s[n][0], s[n][1]);
-                    pf[n * 2 + 1] = pack_f16(s[n][2], s[n][3]);
                 }
+                auto values = [&](auto in) {
+                    using In = decltype(in);
+                    // weights are rounded for the product with the values; their sum is not
+                    const uint32_t pf[4] = {In::pack(s[0][0], s[0][1]), In::pack(s[0][2], s[0][3]), In::pack(s[1][0], s[1][1]), In::pack(s[1][2], s[1][3])};
 #pragma unroll
-                for (int j = 0; j < DP / 16; j += 2) {
-                    uint32_t v4[4];
-                    ldmatrix4_trans(v4, vs_base + code_chunk<DP>(vrow, j + (lane >> 4)));
-                    if (left < kKeys) {
-                        // rows that are not there may hold anything: 0 times them would not be 0
+                    for (int j = 0; j < DP / 16; j += 2) {
+                        uint32_t v4[4];
+                        ldmatrix4_trans(v4, vs_base + code_chunk<DP>(vrow, j + (lane >> 4)));
+                        if (left < kKeys) {
+                            // rows that are not there may hold anything: 0 times them would not be 0
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int key = sub * 16 + (i & 1) * 8 + qc;
-                            if (key >= left) v4[i] = 0u;
-                            else if (key + 1 >= left) v4[i] &= 0xffffu;
+                            for (int i = 0; i < 4; ++i) {
+                                const int key = sub * 16 + (i & 1) * 8 + qc;
+                                if (key >= left) v4[i] = 0u;
+                                else if (key + 1 >= left) v4[i] &= 0xffffu;
+                            }
+                        }
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            uint32_t even0, odd0, even1, odd1;
+                            In::template codes<CODE>(__byte_perm(v4[y * 2], 0u, 0x3120), even0, odd0);
+                            In::template codes<CODE>(__byte_perm(v4[y * 2 + 1], 0u, 0x3120), even1, odd1);
+                            In::mma(o[j + y][0], pf, even0, even1);
+                            In::mma(o[j + y][1], pf, odd0, odd1);
                         }
                     }
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        uint32_t even0, odd0, even1, odd1;
-                        halves_of<CODE>(__byte_perm(v4[y * 2], 0u, 0x3120), even0, odd0);
-                        halves_of<CODE>(__byte_perm(v4[y * 2 + 1], 0u, 0x3120), even1, odd1);
-                        mma_f16(o[j + y][0], pf, even0, even1);
-                        mma_f16(o[j + y][1], pf, odd0, odd1);
-                    }
-                }
+                };
+                if (!span.wide(exponent, lane >= 16 && sub * 16 + (lane & 15) < left)) values(InHalves{});
+                else values(InBf16{});
             } else {
                 const uint32_t ks_base = smem_u32(sm.draft[0]), vs_base = smem_u32(sm.draft[1]);
                 const int left = p.s.nodes - (kt - p.kt_cache) * kKeys;
@@ -652,6 +689,7 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
         // of 16 columns from 16 j on a thread has the columns 2 kr and 2 kr + 1 of its two query rows
         float o[DP / 16][4];
         float m[2] = {neg_inf(), neg_inf()}, l[2] = {0.f, 0.f};
+        SpanOfScales span;
 #pragma unroll
         for (int j = 0; j < DP / 16; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
         bool poison = false;                            // a drafted value that is not finite was set aside
@@ -704,8 +742,9 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
         for (int i = tiles.first; i < tiles.n; i += C::kGroups, left -= kTurn) {
             const uint32_t at = ring + i;
             const int stage = at % C::kStages;
-            const uint32_t scale_code = next_scale;
+            const int exponent = scale_exponent(next_scale);
             next_scale = look_up(p.s.len);
+            const bool wide = span.wide(exponent, lane >= 16 && sub * 16 + (lane & 15) < left);
             await_tile(&sm.full[stage], at / C::kStages);
             float s[4] = {};
             const uint32_t ks_base = smem_u32(sm.tiles[stage][0]), vs_base = smem_u32(sm.tiles[stage][1]);
@@ -721,7 +760,6 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                 mma_f16(s, k0, qf[ks / 2][0], qf[ks / 2][1]);
                 mma_f16(s1, k1, qf[ks / 2][2], qf[ks / 2][3]);
             }
-            const int exponent = scale_exponent(scale_code);
             int ve[2];
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
@@ -736,31 +774,36 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             const float d0 = power_of_two(-ve[0]), d1 = power_of_two(-ve[1]);
             l[0] += fmaf(s[0], d0, s[2] * d1);
             l[1] += fmaf(s[1], d0, s[3] * d1);
-            // weights are rounded to fp16 for the product with the values; their sum is not
-            uint32_t pf[2];
-            transpose8(pf[0], pack_f16(s[0], s[1]));
-            transpose8(pf[1], pack_f16(s[2], s[3]));
+            auto values = [&](auto in) {
+                using In = decltype(in);
+                // weights are rounded for the product with the values; their sum is not
+                uint32_t pf[2];
+                transpose8(pf[0], In::pack(s[0], s[1]));
+                transpose8(pf[1], In::pack(s[2], s[3]));
 #pragma unroll
-            for (int j = 0; j < DP / 16; j += 2) {
-                uint32_t v4[4];
-                ldmatrix4_trans(v4, vs_base + code_chunk<DP>(vrow, j + (lane >> 4)));
-                if (left < kKeys) {
-                    // rows that are not there may hold anything: 0 times them would not be 0
+                for (int j = 0; j < DP / 16; j += 2) {
+                    uint32_t v4[4];
+                    ldmatrix4_trans(v4, vs_base + code_chunk<DP>(vrow, j + (lane >> 4)));
+                    if (left < kKeys) {
+                        // rows that are not there may hold anything: 0 times them would not be 0
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = sub * 16 + (i & 1) * 8 + qc;
-                        if (key >= left) v4[i] = 0u;
-                        else if (key + 1 >= left) v4[i] &= 0xffffu;
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = sub * 16 + (i & 1) * 8 + qc;
+                            if (key >= left) v4[i] = 0u;
+                            else if (key + 1 >= left) v4[i] &= 0xffffu;
+                        }
+                    }
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        uint32_t v[4];          // even columns, odd columns of keys 0 to 7, then of keys 8 to 15
+                        In::template codes<CODE>(__byte_perm(v4[y * 2], 0u, 0x3120), v[0], v[1]);
+                        In::template codes<CODE>(__byte_perm(v4[y * 2 + 1], 0u, 0x3120), v[2], v[3]);
+                        In::mma(o[j + y], v, pf[0], pf[1]);
                     }
                 }
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    uint32_t v[4];          // even columns, odd columns of keys 0 to 7, then of keys 8 to 15
-                    halves_of<CODE>(__byte_perm(v4[y * 2], 0u, 0x3120), v[0], v[1]);
-                    halves_of<CODE>(__byte_perm(v4[y * 2 + 1], 0u, 0x3120), v[2], v[3]);
-                    mma_f16(o[j + y], v, pf[0], pf[1]);
-                }
-            }
+            };
+            if (!wide) values(InHalves{});
+            else values(InBf16{});
             give_back(&sm.empty[stage]);
         }
         ring += tiles.n;

@@ -1,0 +1,63 @@
+"""The operators round a cache in 8 bits at the ends of what their scales, queries and strides may be, on the GPU."""
+import numpy as np
+import pytest
+import torch
+
+import q8_reference as ref
+from decode_reference import B16, U
+from paper_2511_08003_b200 import binding as sv
+from test_q8_ops import CODES, _f64, _i32
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------ scales of values far apart
+def _attention(q, k8, ke, v8, ve, scale):
+    """One head's queries q [rows, D] over keys and values of codes' values k8, v8 [n, D] and exponents ke, ve [n], in 64 bits: out
+    and the bound that the header gives: weights off by 2^-8 of themselves or 2^-25 of the row's largest, out rounded to bf16,
+    and scores, maximum and sums in fp32 (decode_reference: e_p; the values' exponents are added to the scores)."""
+    k, v = k8 * 2.0 ** ke[:, None], v8 * 2.0 ** ve[:, None]
+    n, D = k.shape
+    out, tol = np.zeros((len(q), D)), np.zeros((len(q), D))
+    for i, x in enumerate(q):
+        s = scale * (k @ x)
+        p = np.exp(s - s.max())
+        l = p.sum()
+        out[i] = p @ v / l
+        e_s = (D + 2) * U * scale * (np.abs(k) @ np.abs(x)).max() + scale * 2.0 ** -39 * np.abs(x).max() * np.abs(k).sum(1).max()
+        e_p = e_s + 8 * U * (np.abs(s).max() + abs(s.max() + np.log(l)) + np.abs(ve).max()) + 8 * U
+        A = p @ np.abs(v) / l
+        tol[i] = 1.1 * ((2 * e_p + 2 * n * U + B16) * A + 2.0 ** -25 * np.abs(v).sum(0) / l + B16 * np.abs(out[i]))
+    return out, tol
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "i8"])
+@pytest.mark.parametrize("heads,D", [(2, 64), (7, 128), (12, 64), (12, 128), (3, 256), (40, 64), (40, 128)])
+@pytest.mark.parametrize("gap", [7, 12, 24, 31, 34, 60, 96])
+def test_attention_next_to_a_block_of_far_larger_scale(gap, heads, D, kind):
+    """A block of values whose scale is 2^gap of the others', where nothing of it is in most columns: codes of 0 but for one row of
+    no weight.  What the other blocks hold in those columns is the result.  In the first, a middle and the last block, and
+    in the same 16 keys as others (blocks of 8)."""
+    g = np.random.default_rng(gap)
+    n, least = 200, -48 if gap > 48 else -gap // 2
+    for block, big in ((16, 0), (16, 5), (16, 12), (8, 1), (1, 70)):
+        blocks = -(-n // block)
+        of = np.arange(n) // block
+        scales = np.full((1, 2, 1, blocks), 127, np.uint8)
+        scales[0, 0] = 118
+        scales[0, 1] = 127 + least + g.integers(0, 2, blocks)
+        scales[0, 1, 0, big] = 127 + least + gap
+        k = ref.nearest(g.standard_normal((n, D)) * 60, kind)
+        v = ref.nearest(g.standard_normal((n, D)) * 60, kind)
+        here = np.flatnonzero(of == big)
+        v[here] = 0
+        k[here[-1]] = ref.nearest(np.full(D, -100.0), kind)         # the row of no weight: queries are positive
+        v[here[-1], :3] = ref.nearest(np.array([100.0, -7.0, 1.0]), kind)
+        codes = np.stack([k, v])[None, :, None]
+        q = torch.from_numpy(np.abs(g.standard_normal((1, heads, D))).astype(np.float32)).bfloat16().cuda()
+        kv = torch.from_numpy(np.ascontiguousarray(codes)).cuda().view(CODES[kind])
+        got = sv.sharpv_tree_attention_q8(q, kv, torch.from_numpy(scales).cuda(), block, 0, _i32([0]), _i32([n]), _i32([0, 1]))
+        e = ref.clamped(scales[0, :, 0])
+        want, tol = _attention(_f64(q)[0], ref.values_of(k, kind), e[0][of], ref.values_of(v, kind), e[1][of], D ** -0.5)
+        worst = np.max(np.abs(_f64(got["out"])[0] - want) / tol)
+        assert worst <= 1, f"blocks of {block}, the far one {big}: {worst:.3e} of the bound"
