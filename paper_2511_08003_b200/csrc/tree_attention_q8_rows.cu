@@ -10,8 +10,10 @@
 //   ldmatrix hands a thread four neighbouring codes of a key, so the products take the columns of 16 in the order
 //   0 1 4 5 8 9 12 13 | 2 3 6 7 10 11 14 15, and the query rows are laid out in that order.  Of transposed value tiles it
 //   hands two keys of two neighbouring columns: even columns are one product, odd ones another.
-//   A key's scale multiplies what a product of the row stands for (large queries over small scales would pass fp32 otherwise).  A value's scale 2^e goes to its weight: the softmax runs over s_j + e_j, with m as its
-//   running maximum,   out = sum_j 2^(s_j + e_j - m) code_j / l,   l = sum_j 2^(s_j + e_j - m) 2^-e_j,
+//   A key's scale multiplies the sum of products first: that is between 2^-33 and 2^32, so neither large queries over small scales
+//   nor small codes under large ones pass fp32 before the score itself does (and 0 stays 0).  A value's scale 2^e goes to its
+//   weight: the softmax runs over s_j + e_j, with m as its running maximum,
+//     out = sum_j 2^(s_j + e_j - m) code_j / l,   l = sum_j 2^(s_j + e_j - m) 2^-e_j,
 //   so weights never pass what fp16 holds whatever the scales are.  m is set 8 under the maximum and kept until that has grown by
 //   7 more (sums are then rarely rescaled): the largest weight is between 2^8 and 2^15, weights down to 2^-14 are rounded to
 //   11 bits, and smaller ones lose 2^-25, 2^-33 of the largest, at most.  That is of the largest with its value's scale on it, whatever
@@ -466,8 +468,8 @@ attn_rows_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                         const float kx = power_of_two(__shfl_sync(0xffffffffu, exponent, n * 8 + qc + i));
                         ve[n][i] = __shfl_sync(0xffffffffu, exponent, 16 + n * 8 + qc + i);
                         const bool sees = sub * 16 + n * 8 + qc + i < left;
-                        s[n][i] = sees ? fmaf(s[n][i], unit[0] * kx, (float)ve[n][i]) : neg_inf();
-                        s[n][2 + i] = sees ? fmaf(s[n][2 + i], unit[1] * kx, (float)ve[n][i]) : neg_inf();
+                        s[n][i] = sees ? fmaf(s[n][i] * kx, unit[0], (float)ve[n][i]) : neg_inf();
+                        s[n][2 + i] = sees ? fmaf(s[n][2 + i] * kx, unit[1], (float)ve[n][i]) : neg_inf();
                     }
                 weigh(s);
 #pragma unroll
@@ -768,7 +770,7 @@ attn_rows8_q8_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                 const bool sees = sub * 16 + n * 8 + kr < left;
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
-                    s[n * 2 + y] = sees ? fmaf(s[n * 2 + y] + s1[n * 2 + y], unit[y] * kx, (float)ve[n]) : neg_inf();
+                    s[n * 2 + y] = sees ? fmaf((s[n * 2 + y] + s1[n * 2 + y]) * kx, unit[y], (float)ve[n]) : neg_inf();
             }
             weigh(s);
             const float d0 = power_of_two(-ve[0]), d1 = power_of_two(-ve[1]);

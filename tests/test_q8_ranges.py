@@ -61,3 +61,22 @@ def test_attention_next_to_a_block_of_far_larger_scale(gap, heads, D, kind):
         want, tol = _attention(_f64(q)[0], ref.values_of(k, kind), e[0][of], ref.values_of(v, kind), e[1][of], D ** -0.5)
         worst = np.max(np.abs(_f64(got["out"])[0] - want) / tol)
         assert worst <= 1, f"blocks of {block}, the far one {big}: {worst:.3e} of the bound"
+
+
+# ------------------------------------------------------------------------------------------ large queries, large scales
+@pytest.mark.parametrize("kind", ["e4m3", "i8"])
+@pytest.mark.parametrize("heads,D", [(1, 64), (7, 128), (12, 64), (12, 128), (3, 256), (40, 128)])
+def test_attention_of_large_queries_over_keys_of_zero_with_the_largest_scale(heads, D, kind):
+    """All scores are 0 whatever a query's size times a key's scale is.  Every weight is 1: out is the values' mean, of whole numbers
+    under 2^24, rounded once; their sum is divided by a power of two, or by multiplying with a reciprocal: 2 u more."""
+    n = 61
+    g = np.random.default_rng(D)
+    v = g.integers(1, 9, (n, D)).astype(np.float64)
+    kv = np.zeros((1, 2, 1, 64, D), np.uint8)
+    kv[0, 1, 0, :n] = ref.nearest(v, kind)
+    scales = torch.tensor([[[[175] * 4], [[127] * 4]]], dtype=torch.uint8, device="cuda")
+    q = torch.full((1, heads, D), 1.5 * 2.0 ** 118, device="cuda").bfloat16()
+    got = sv.sharpv_tree_attention_q8(q, torch.from_numpy(kv).cuda().view(CODES[kind]), scales, 16, 0, _i32([0]), _i32([n]), _i32([0, 1]))
+    want = v.mean(0)
+    assert np.all(np.abs(_f64(got["out"])[0] - want) <= (B16 + 8 * U) * want)
+    assert np.all(np.abs(_f64(got["lse"]) - np.log(n)) <= 16 * U * np.log(n))
