@@ -760,13 +760,11 @@ def sharpv_kv_append(kv_src: torch.Tensor, kv_dst: torch.Tensor, src_pos: torch.
 
 # ------------------------------------------------------------------------------- queries and keys of a step
 def _token_rows(t: torch.Tensor, tokens: int, heads: int, d: int):
-    """Address, token stride and head stride of [tokens, heads, d]; a stride that nothing needs is what a dense tensor has."""
+    """Address, token stride and head stride of [tokens, heads, d]; a stride that nothing needs is d, which is always taken."""
     a, b, c = t.stride()
     if c != 1 and tokens and heads:
         raise ValueError("q and k must have a contiguous last axis")
-    if heads < 2:
-        b = d
-    return t.data_ptr(), a if tokens > 1 else heads * b, b
+    return t.data_ptr(), a if tokens > 1 else d, b if heads > 1 else d
 
 
 def sharpv_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, pair_axis, rope_base: float,

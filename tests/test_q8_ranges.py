@@ -80,3 +80,17 @@ def test_attention_of_large_queries_over_keys_of_zero_with_the_largest_scale(hea
     want = v.mean(0)
     assert np.all(np.abs(_f64(got["out"])[0] - want) <= (B16 + 8 * U) * want)
     assert np.all(np.abs(_f64(got["lse"]) - np.log(n)) <= 16 * U * np.log(n))
+
+
+# ------------------------------------------------------------------------------------------ heads far apart
+@pytest.mark.parametrize("n", [1, 2])
+def test_norm_and_rotation_straight_into_a_long_cache(n):
+    """Keys into a plane whose heads are 256 MB apart, one token and two."""
+    cache = torch.zeros((8, 1 << 20, 128), dtype=torch.bfloat16, device="cuda")
+    q, k = (torch.randn((n, 8, 128), device="cuda").bfloat16() for _ in range(2))
+    want = sv.sharpv_qk_norm_rope(q, k, _i32(np.arange(n)[None] + 70000), [0] * 64, 1e6, norm=True)
+    at = 1000003
+    got = sv.sharpv_qk_norm_rope(q, k, _i32(np.arange(n)[None] + 70000), [0] * 64, 1e6, norm=True,
+                                 out={"q": q, "k": cache[:, at:at + n].transpose(0, 1)})
+    assert torch.equal(got["q"], want["q"]) and torch.equal(cache[:, at:at + n].transpose(0, 1), want["k"])
+    assert not bool(cache[:, at - 1].any()) and not bool(cache[:, at + n].any())
