@@ -481,7 +481,8 @@ sharpv_status sharpv_kv_append(
  * q [dev] [num_tokens, num_q_heads, head_dim], token stride ld_q, head stride head_q (elements); k the same with num_kv_heads:
  *   views of a fused projection are fine.  Outputs have strides of their own (keys can go straight to where the
  *   attention or sharpv_kv_append reads them).  An output may be its own input (same pointer and strides); otherwise outputs
- *   overlap neither inputs nor each other.
+ *   must overlap neither inputs nor each other nor themselves (SHARPV_ERR_INVALID_ARG; SHARPV_ERR_UNSUPPORTED where rows interleave
+ *   in so many ways that this cannot be told in a few thousand steps).  Rows that interleave, as a fused projection's do, are fine.
  * q_weight, k_weight [dev] [head_dim] of the same type, or NULL: ones (they must be NULL where norm = 0).
  * positions [dev] int32[num_axes, num_tokens], row stride ld_positions (0: all axes share one row); any value.  Angles are formed and reduced in
  *   64 bits, their sine and cosine taken in fp32.

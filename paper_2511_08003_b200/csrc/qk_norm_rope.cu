@@ -16,6 +16,7 @@
 // 0.91 of a plain copy's rate, and what is left is the issue of about 15 instructions an element.  1,600 tokens of 14 + 2 heads x 64 in
 // fp32 4.4 us, 16 tokens 3.1 us (latency: positions, sine, one row).
 #include "decode_common.cuh"
+#include "overlap.h"
 
 #include <cuda_bf16.h>
 
@@ -259,6 +260,31 @@ sharpv_status by_lanes(NormRopeArgs& a, int sms, cudaStream_t stream) {
     return launch<DT, 32>(a, sms, stream);
 }
 
+// Rows of heads: what an output must not share with what is read, unless it is its own input.
+struct HeadRows {
+    const void* p;
+    int64_t token, head;                // bytes
+    int heads;
+};
+Runs runs_of(const HeadRows& r, int64_t tokens, int64_t row) {
+    return Runs{reinterpret_cast<uintptr_t>(r.p), row, 2, {r.token, r.head}, {tokens, r.heads}};
+}
+bool same_rows(const HeadRows& a, const HeadRows& b, int64_t tokens) {
+    return a.p == b.p && a.heads == b.heads && (tokens == 1 || a.token == b.token) && (a.heads == 1 || a.head == b.head);
+}
+sharpv_status outputs_status(const HeadRows (&in)[2], const HeadRows (&out)[2], int64_t tokens, int64_t row, const Runs (&tables)[3]) {
+    Share worst = share_bytes(runs_of(out[0], tokens, row), runs_of(out[1], tokens, row));
+    auto add = [&](Share s) { if (worst != Share::yes && s != Share::no) worst = s; };
+    for (int i = 0; i < 2; ++i) {
+        const Runs mine = runs_of(out[i], tokens, row);
+        add(shares_own_bytes(mine));
+        add(share_bytes(mine, runs_of(in[1 - i], tokens, row)));
+        if (!same_rows(out[i], in[i], tokens)) add(share_bytes(mine, runs_of(in[i], tokens, row)));
+        for (const Runs& t : tables) add(share_bytes(mine, t));
+    }
+    return worst == Share::no ? SHARPV_OK : (worst == Share::yes ? SHARPV_ERR_INVALID_ARG : SHARPV_ERR_UNSUPPORTED);
+}
+
 }  // namespace
 }  // namespace sharpv
 
@@ -292,6 +318,12 @@ extern "C" sharpv_status sharpv_qk_norm_rope(
     }
     if (!aligned16(q) || !aligned16(k) || !aligned16(out_q) || !aligned16(out_k) || !aligned16(q_weight) || !aligned16(k_weight))
         return SHARPV_ERR_UNSUPPORTED;
+    const HeadRows in[2] = {{q, ld_q * eb, head_q * eb, num_q_heads}, {k, ld_k * eb, head_k * eb, num_kv_heads}};
+    const HeadRows out[2] = {{out_q, ld_out_q * eb, head_out_q * eb, num_q_heads}, {out_k, ld_out_k * eb, head_out_k * eb, num_kv_heads}};
+    const Runs tables[3] = {{reinterpret_cast<uintptr_t>(q_weight), q_weight ? row : 0, 0}, {reinterpret_cast<uintptr_t>(k_weight), k_weight ? row : 0, 0},
+                            {reinterpret_cast<uintptr_t>(positions), rotary_dim > 0 ? num_tokens * 4 : 0, 1, {ld_positions * 4}, {num_axes}}};
+    const sharpv_status os = outputs_status(in, out, num_tokens, row, tables);
+    if (os != SHARPV_OK) return os;
     NormRopeArgs a = {};
     a.q = (const char*)q;
     a.k = (const char*)k;

@@ -94,3 +94,21 @@ def test_norm_and_rotation_straight_into_a_long_cache(n):
                                  out={"q": q, "k": cache[:, at:at + n].transpose(0, 1)})
     assert torch.equal(got["q"], want["q"]) and torch.equal(cache[:, at:at + n].transpose(0, 1), want["k"])
     assert not bool(cache[:, at - 1].any()) and not bool(cache[:, at + n].any())
+
+
+def test_norm_and_rotation_refuse_outputs_that_overlap():
+    """Refused before any launch: the values stay what they are.  Interleaving rows are taken."""
+    qkv = torch.randn((50, 12, 64), device="cuda")
+    before, pos = qkv.clone(), _i32(np.arange(50)[None])
+    q, k = qkv[:, :8], qkv[:, 8:10]
+    for out in ({"q": q, "k": q[:, :2]}, {"q": qkv[:, 1:9], "k": k}, {"q": q, "k": qkv[:, 9:11]}, {"q": torch.empty_like(q), "k": qkv[:, 7:9]},
+                {"q": torch.empty((50, 1, 64), device="cuda").expand(50, 8, 64), "k": k}):
+        with pytest.raises((sv.SharpVError, ValueError)):
+            sv.sharpv_qk_norm_rope(q, k, pos, [0] * 32, 1e4, out=out)
+        assert torch.equal(qkv, before)
+    want = sv.sharpv_qk_norm_rope(q, k, pos, [0] * 32, 1e4)
+    wide = torch.zeros((50, 14, 64), device="cuda")                 # outputs between each other's rows
+    got = sv.sharpv_qk_norm_rope(q, k, pos, [0] * 32, 1e4, out={"q": wide[:, 3:11], "k": wide[:, 11:13]})
+    assert torch.equal(got["q"], want["q"]) and torch.equal(got["k"], want["k"]) and not bool(wide[:, [0, 1, 2, 13]].any())
+    got = sv.sharpv_qk_norm_rope(q, k, pos, [0] * 32, 1e4, out={"q": q, "k": qkv[:, 10:12]})       # keys where the values were
+    assert torch.equal(got["q"], want["q"]) and torch.equal(got["k"], want["k"]) and torch.equal(k, before[:, 8:10])
