@@ -527,7 +527,9 @@ typedef struct {
  * are left as they are: they are free.
  * Tables, capacity, status_word and the disjointness of the two caches as in sharpv_kv_append; src_scales_layout and src_scales
  * are NULL for SHARPV_F32 and SHARPV_BF16 sources.  head_dim is a multiple of 16 and at most 1024 (512 with SHARPV_F32
- * sources), token strides are under 2 GB.  The scales of dst and src must not overlap.
+ * sources), token strides are under 2 GB.  The scales of dst and src must not overlap.  No two rows of dst's planes share bytes, nor
+ * two planes' scales, nor scales of dst with rows of dst or src, nor rows of dst with scales of src; they may interleave, layer by
+ * layer, say (SHARPV_ERR_INVALID_ARG; SHARPV_ERR_UNSUPPORTED where that cannot be told in a few thousand steps).
  */
 sharpv_status sharpv_kv_append_q8(
     const void* kv_src, const sharpv_kv_layout* src_layout /* [host] */, const uint8_t* src_scales,

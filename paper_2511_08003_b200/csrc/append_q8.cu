@@ -22,6 +22,7 @@
 // plane's loads in flight, 1,634 with every index divided out and elements compared one at a time).  From 8 bits to 8 bits there are
 // more codes a byte, and instructions bound it: half of these rows, int8 to int8, 211 us (0.79).  43 rows 7.1 us: latency
 // (tables, rows, maximum, codes).
+#include "overlap.h"
 #include "q8.cuh"
 
 #include <cuda_bf16.h>
@@ -517,6 +518,17 @@ void scales_extent(const uint8_t* scales, const sharpv_kv_scales* s, const sharp
                                                           (L->num_kv_heads - 1) * s->stride_head + (rows - 1) / s->block_tokens + 1);
 }
 
+Runs runs_of(const void* kv, const sharpv_kv_layout* L, int layer_begin, int layer_end, int64_t rows) {
+    const int64_t eb = elem_bytes(L->dtype);
+    return Runs{reinterpret_cast<uintptr_t>(kv) + (uintptr_t)(layer_begin * L->stride_layer * eb), L->head_dim * eb, 4,
+                {L->stride_layer * eb, L->stride_kv * eb, L->stride_head * eb, L->stride_token * eb},
+                {layer_end - layer_begin, 2, L->num_kv_heads, rows}};
+}
+Runs runs_of(const uint8_t* scales, const sharpv_kv_scales* s, const sharpv_kv_layout* L, int layer_begin, int layer_end, int64_t rows) {
+    return Runs{reinterpret_cast<uintptr_t>(scales) + (uintptr_t)(layer_begin * s->stride_layer), rows > 0 ? (rows - 1) / s->block_tokens + 1 : 0, 3,
+                {s->stride_layer, s->stride_kv, s->stride_head}, {layer_end - layer_begin, 2, L->num_kv_heads}};
+}
+
 }  // namespace
 }  // namespace sharpv
 
@@ -563,6 +575,14 @@ extern "C" sharpv_status sharpv_kv_append_q8(
             if (s_lo < d_hi && d_lo < s_hi) return SHARPV_ERR_INVALID_ARG;
         }
     }
+    // what is written: no byte twice, and none that is read
+    const Runs to = runs_of(kv_dst, dst_layout, layer_begin, layer_end, dst_tokens);
+    const Runs to_scales = runs_of(dst_scales, dst_scales_layout, dst_layout, layer_begin, layer_end, dst_tokens);
+    Share shares[5] = {shares_own_bytes(to), shares_own_bytes(to_scales), share_bytes(to, to_scales),
+                       share_bytes(to_scales, runs_of(kv_src, src_layout, layer_begin, layer_end, src_tokens)), Share::no};
+    if (codes) shares[4] = share_bytes(to, runs_of(src_scales, src_scales_layout, src_layout, layer_begin, layer_end, src_tokens));
+    for (const Share s : shares)
+        if (s != Share::no) return s == Share::yes ? SHARPV_ERR_INVALID_ARG : SHARPV_ERR_UNSUPPORTED;
     AppendQ8Args a = {};
     a.src = (const char*)kv_src;
     a.dst = (uint8_t*)kv_dst;

@@ -115,3 +115,34 @@ def test_norm_and_rotation_refuse_outputs_that_overlap(change):
     assert sv.lib().sharpv_qk_norm_rope(
         a["q"], a["ldq"], a["hsq"], a["k"], a["ldk"], a["hsk"], 1, a["N"], 28, 4, 128, 1, a["qw"], a["kw"], 1e-6, a["pos"], a["N"], a["axes"], bytes(64),
         128, 1e6, a["oq"], a["ldoq"], a["hsoq"], a["ok"], a["ldok"], a["hsok"], None) == sv.Status.ERR_INVALID_ARG
+
+
+def _layout(dtype, **kw):
+    lay = sv.KVLayout(2, 4, 128, dtype, 2 * 4 * 100 * 128, 4 * 100 * 128, 100 * 128, 128)
+    for k, v in kw.items():
+        setattr(lay, k, v)
+    return lay
+
+
+def _scales(**kw):
+    s = sv.KVScales(16, 2 * 4 * 8, 4 * 8, 8)
+    for k, v in kw.items():
+        setattr(s, k, v)
+    return s
+
+
+DST = 1 << 40
+
+
+@pytest.mark.parametrize("change", [
+    dict(dsl=_scales(stride_head=0)), dict(dsl=_scales(stride_kv=0)), dict(dsl=_scales(stride_layer=0)),       # planes with one scale
+    dict(dsl=_scales(stride_head=6)),                                                                          # 7 blocks of 100 rows
+    dict(dl=_layout(sv.E4M3, stride_head=0)), dict(dl=_layout(sv.E4M3, stride_layer=99 * 128)),                # planes with one another's rows
+    dict(ds=DST), dict(ds=DST + 2 * 2 * 4 * 100 * 128 - 1), dict(ds=DST - 1), dict(ds=1 << 20), dict(ds=(1 << 20) - 1),    # scales over rows
+    dict(sl=_layout(sv.I8), ss=DST + 128, ssl=_scales()),
+])
+def test_append_refuses_destinations_that_overlap(change):
+    svbuild.build()
+    a = dict(dict(sl=_layout(sv.BF16), ss=None, ssl=None, dl=_layout(sv.E4M3), ds=1 << 41, dsl=_scales()), **change)
+    assert sv.lib().sharpv_kv_append_q8(1 << 20, a["sl"], a["ss"], a["ssl"], 100, DST, a["dl"], a["ds"], a["dsl"], 100, 0, 2, 1 << 16, 1 << 16, 1 << 16,
+                                        2, 10, None, None) == sv.Status.ERR_INVALID_ARG

@@ -112,3 +112,30 @@ def test_norm_and_rotation_refuse_outputs_that_overlap():
     assert torch.equal(got["q"], want["q"]) and torch.equal(got["k"], want["k"]) and not bool(wide[:, [0, 1, 2, 13]].any())
     got = sv.sharpv_qk_norm_rope(q, k, pos, [0] * 32, 1e4, out={"q": q, "k": qkv[:, 10:12]})       # keys where the values were
     assert torch.equal(got["q"], want["q"]) and torch.equal(got["k"], want["k"]) and torch.equal(k, before[:, 8:10])
+
+
+# ------------------------------------------------------------------------------------------ codes and scales in one allocation
+@pytest.mark.parametrize("kind", ["e4m3", "i8"])
+def test_append_and_attention_with_codes_and_scales_layer_by_layer(kind):
+    """Scales behind the codes of their layer: nothing overlaps, and all is as it is with the two apart.  A scale for all heads, or
+    scales over codes, are refused and leave everything as it was."""
+    L, H, T, D, block = 3, 2, 96, 64, 16
+    layer = 2 * H * T * D + 2 * H * 16
+    raw = torch.zeros(L * layer, dtype=torch.uint8, device="cuda")
+    codes = raw.as_strided((L, 2, H, T, D), (layer, H * T * D, T * D, D, 1)).view(CODES[kind])
+    scales = raw.as_strided((L, 2, H, T // block), (layer, 16 * H, 16, 1), 2 * H * T * D)
+    src = torch.randn((L, 2, H, 50, D), device="cuda").bfloat16()
+    apart, its = torch.zeros((L, 2, H, T, D), dtype=CODES[kind], device="cuda"), torch.zeros((L, 2, H, T // block), dtype=torch.uint8, device="cuda")
+    lists = _i32(np.arange(50)), _i32([0, 20, 50]), _i32([0, 48])
+    before = raw.clone()
+    for bad in (scales[:, :, :1].expand(L, 2, H, T // block), raw.as_strided((L, 2, H, T // block), (layer, 16 * H, 16, 1))):
+        with pytest.raises(sv.SharpVError):
+            sv.sharpv_kv_append_q8(src, codes, bad, block, *lists)
+        assert torch.equal(raw, before)
+    sv.sharpv_kv_append_q8(src, codes, scales, block, *lists)
+    sv.sharpv_kv_append_q8(src, apart, its, block, *lists)
+    assert torch.equal(codes.view(torch.uint8), apart.view(torch.uint8)) and torch.equal(scales, its)
+    q, dk = torch.randn((3, 6, D), device="cuda").bfloat16(), torch.randn((3, H, D), device="cuda").bfloat16()
+    got, want = (sv.sharpv_tree_attention_q8(q, c, s, block, 1, _i32([0, 48]), _i32([20, 30]), _i32([0, 1, 3]), dk, dk)
+                 for c, s in ((codes, scales), (apart, its)))
+    assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])
