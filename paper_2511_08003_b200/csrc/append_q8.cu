@@ -260,7 +260,8 @@ kv_append_q8_kernel(const __grid_constant__ AppendQ8Args a) {
     const int64_t lo = min(max(begin, (int64_t)0), a.dst_tokens), hi = min(max(begin + (j1 - j0), lo), a.dst_tokens);
     if (speaks && j1 > j0 && (begin < 0 || begin + (j1 - j0) > a.dst_tokens)) report(a.status_word, SHARPV_ERR_BOUNDS);
     const uint32_t cta0 = (uint32_t)j0 / (uint32_t)a.tile_rows + (uint32_t)b, ctas = first_cta(b + 1) - cta0;
-    if (lo >= hi || blockIdx.x < cta0) return;              // nothing here, or offsets that do not begin at 0
+    // nothing here, offsets that do not begin at 0, or CTAs behind the last sequence's (there are as many as capacity may need)
+    if (lo >= hi || blockIdx.x < cta0 || blockIdx.x - cta0 >= ctas) return;
     const int block_rows = 1 << a.dst_shift;
     const int64_t base = lo >> a.dst_shift << a.dst_shift;  // first row of the sequence's first block
     const uint32_t tiles = ((uint32_t)(hi - base) + a.tile_rows - 1) / (uint32_t)a.tile_rows;

@@ -6,7 +6,7 @@ import torch
 import q8_reference as ref
 from decode_reference import B16, U
 from paper_2511_08003_b200 import binding as sv
-from test_q8_ops import CODES, _f64, _i32
+from test_q8_ops import CODES, Store, _bits, _f64, _i32
 
 pytestmark = pytest.mark.gpu
 
@@ -139,3 +139,22 @@ def test_append_and_attention_with_codes_and_scales_layer_by_layer(kind):
     got, want = (sv.sharpv_tree_attention_q8(q, c, s, block, 1, _i32([0, 48]), _i32([20, 30]), _i32([0, 1, 3]), dk, dk)
                  for c, s in ((codes, scales), (apart, its)))
     assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])
+
+
+# ------------------------------------------------------------------------------------------ lists with room behind them
+@pytest.mark.parametrize("kind", ["e4m3", "i8"])
+@pytest.mark.parametrize("source", ["bf16", "i8"])
+@pytest.mark.parametrize("lens,rows", [([2], [63]), ([2, 62], [64, 127]), ([0, 63, 17], [5, 0, 700]), ([40] * 40, [3] * 39 + [300])])
+def test_append_with_a_list_that_has_room_behind(lens, rows, source, kind):
+    """capacity over the rows there are (a kept list's usual form; what lies behind is no row at all), last sequences that begin late in a
+    block and so need a tile more than their rows fill."""
+    s = Store(source, kind, 64, 2, 128, lens, rows, seed=len(lens))
+    for room in (1, 64, 5000):
+        fresh = Store(source, kind, 64, 2, 128, lens, rows, seed=len(lens))
+        fresh.pos = np.concatenate([s.pos, np.full(room, -7)])
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        fresh.call(status_word=status)
+        fresh.pos = s.pos
+        codes, scales = fresh.expected()
+        assert status.item() == 0
+        assert np.array_equal(fresh.dst_scales.cpu().numpy(), scales) and np.array_equal(_bits(fresh.dst), codes)
