@@ -797,7 +797,7 @@ def sharpv_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tenso
         raise ValueError(f"positions must be [axes, tokens] on {dev} with a contiguous last axis")
     if positions.dtype is not _I32:
         raise TypeError("positions must be int32")
-    pairs = pair_axis if isinstance(pair_axis, bytes) else bytes(pair_axis)
+    pairs = pair_axis if isinstance(pair_axis, bytes) else bytes(list(pair_axis))       # by value, not by an array's memory
     rc = _call("sharpv_qk_norm_rope", q, *_token_rows(q, N, HQ, D), *_token_rows(k, N, H, D), _dtype_code(q), N, HQ, H, D,
                1 if norm else 0, None if q_weight is None else _on(q_weight, "q_weight", dev, dtype, D),
                None if k_weight is None else _on(k_weight, "k_weight", dev, dtype, D), eps, positions.data_ptr(),

@@ -158,3 +158,16 @@ def test_append_with_a_list_that_has_room_behind(lens, rows, source, kind):
         codes, scales = fresh.expected()
         assert status.item() == 0
         assert np.array_equal(fresh.dst_scales.cpu().numpy(), scales) and np.array_equal(_bits(fresh.dst), codes)
+
+
+# ------------------------------------------------------------------------------------------ pairs
+def test_norm_and_rotation_take_axes_by_value():
+    """A list, bytes, an array or a tensor of whole numbers of any width say the same; more than a byte's is refused."""
+    q = torch.randn((5, 4, 128), device="cuda")
+    pos, axis = _i32(np.stack([np.arange(5), 3 * np.arange(5) + 1])), [0, 1, 1, 0, 1, 0, 0, 0]
+    want = sv.sharpv_qk_norm_rope(q, q, pos, axis, 1e4)["q"]
+    for same in (bytes(axis), bytearray(axis), tuple(axis), np.array(axis), np.array(axis, np.uint8), np.array(axis, np.int32), torch.tensor(axis)):
+        assert torch.equal(sv.sharpv_qk_norm_rope(q, q, pos, same, 1e4)["q"], want)
+    for bad in ([0] * 7 + [256], np.array([-1] * 8)):
+        with pytest.raises(ValueError):
+            sv.sharpv_qk_norm_rope(q, q, pos, bad, 1e4)
