@@ -520,7 +520,8 @@ typedef struct {
  *   Every block of dst that receives rows gets the least scale 2^e (e from -48 to 48) with |value| <= 448 * 2^e (SHARPV_E4M3;
  * 127 * 2^e for SHARPV_I8) for all the finite values that it receives; codes are the nearest to value / 2^e, ties to even.
  * Values that are too large for 2^48 and infinities become the largest code of their sign (-128 for SHARPV_I8's negative ones),
- * NaN stays NaN (SHARPV_I8: 0).
+ * NaN stays NaN (SHARPV_I8: 0).  So copying whole blocks from one such cache to another keeps every value, but for blocks of SHARPV_I8 that
+ * hold a code of -128: its 128 passes 127 * 2^e, the copy's scale is twice as large, and odd codes of the block are rounded once more.
  *   Rows that lie in front of dst_begin[b] in the same block are taken to be sequence b's own and keep their values: if their
  * scale is the larger one it stays, otherwise their codes are rounded to the new one.  So sequences begin at multiples of
  * block_tokens, and destination blocks of different sequences must not be the same.  Rows of a block behind the last one written

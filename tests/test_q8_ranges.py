@@ -6,7 +6,7 @@ import torch
 import q8_reference as ref
 from decode_reference import B16, U
 from paper_2511_08003_b200 import binding as sv
-from test_q8_ops import CODES, Store, _bits, _f64, _i32
+from test_q8_ops import CODES, INF, Store, _bits, _f64, _i32
 
 pytestmark = pytest.mark.gpu
 
@@ -171,3 +171,23 @@ def test_norm_and_rotation_take_axes_by_value():
     for bad in ([0] * 7 + [256], np.array([-1] * 8)):
         with pytest.raises(ValueError):
             sv.sharpv_qk_norm_rope(q, q, pos, bad, 1e4)
+
+
+# ------------------------------------------------------------------------------------------ copies
+def test_copies_of_int8_blocks_with_the_code_that_has_no_counterpart():
+    """-128, which a negative infinity becomes, is past 127 * 2^e: a copy of its block has the next scale, and odd codes are rounded to
+    even ones.  Blocks without it, odd codes and all, are the same values."""
+    x = torch.randn((1, 2, 1, 64, 32), device="cuda")
+    x[0, :, 0, 20, 3] = -INF
+    one, two, scales, its = *(torch.zeros((1, 2, 1, 64, 32), dtype=torch.int8, device="cuda") for _ in range(2)), \
+        *(torch.zeros((1, 2, 1, 4), dtype=torch.uint8, device="cuda") for _ in range(2))
+    rows = _i32(np.arange(64)), _i32([0, 64]), _i32([0])
+    sv.sharpv_kv_append_q8(x, one, scales, 16, *rows)
+    sv.sharpv_kv_append_q8(one, two, its, 16, *rows, src_scales=scales)
+    assert bool((one[0, :, 0, 20, 3] == -128).all())
+    same = [0, 2, 3]
+    assert torch.equal(its[..., same], scales[..., same]) and torch.equal(its[..., 1], scales[..., 1] + 1)
+    a, b = one.view(1, 2, 1, 4, 16, 32), two.view(1, 2, 1, 4, 16, 32)
+    assert torch.equal(a[:, :, :, same], b[:, :, :, same])
+    codes = a[:, :, :, 1].cpu().numpy()
+    assert np.any(codes % 2) and np.array_equal(b[:, :, :, 1].cpu().numpy(), np.rint(codes / 2).astype(np.int8))
