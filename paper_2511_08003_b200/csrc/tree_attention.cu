@@ -448,8 +448,8 @@ sharpv_status simt_by_dim(AttnArgs& a, int sms, cudaStream_t stream) {
 // Over an 8-bit cache the bounds are the same, for tiles have to be widened for the tensor cores: 9 to 16 rows, e4m3, us, row kernel against
 // tensor cores' kernel: 50,432 rows 27 / 37, the ragged batch 26 / 35, 6,272 rows 13 / 18, 64 over 2,000 rows each 58 / 77; int8 29 / 36,
 // 28 / 34, 14 / 18, 63 / 76.  Up to 8 rows there is a kernel with keys as the products' rows (21 against 27 at 50,432 rows).
-// 4 x 256 (7 query heads each, 6,272 rows): one token 20, 64 nodes 105, a chunk of 509 872.  63 tokens over 2,000 rows
-// each and a tree of 64 over 50,432: 490 in one call, 42 + 61 in two.
+// 4 x 256 (7 query heads each, 6,272 rows): one token 20, 64 nodes 108, a chunk of 509 888 (int8 125 and 1,024).  63 tokens over
+// 2,000 rows each and a tree of 64 over 50,432: 504 in one call, 41 + 61 in two.
 constexpr int64_t kMaxRowsPath = 16;
 enum class Path { simt, rows, tc };
 struct Choice {

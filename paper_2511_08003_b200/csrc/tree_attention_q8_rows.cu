@@ -21,11 +21,13 @@
 //   warp takes a tile with e_j < E - 8 (SpanOfScales) by products of bf16, which has fp32's exponents and holds the codes of both
 //   kinds: weights have 8 bits there, however far the scales are apart.  Elsewhere p_j is off by 2^-25 of the largest at most.
 //
-// Drafted tokens are bf16 and take products of bf16, in a buffer of their own (there are few of them).
+// Drafted tokens are bf16, which may be anything that fp16 does not hold, so they take products of bf16 and their weights are rounded to
+// 8 bits (both operands of a product are of one type), in a buffer of their own (there are few of them).
 //
 // Up to eight query rows have a kernel of their own, below.  Measured (4 KV heads x 128), up to 8 rows and up to 16, us with the join:
-// one sequence of 50,432 rows 21.3 / 27, the ragged batch of 16 (37,712 rows) 20 / 26, 64 over 2,000 rows each 42 / 58.  In the first
-// 5 us go by until the first tile is there, 10 stream the 52 MB, 1.5 join the warps and write (stamped at 22.9 us); the rest joins the CTAs.
+// one sequence of 50,432 rows 20.8 / 28 (int8 22.4 / 30.5), the ragged batch of 16 (37,712 rows) 20 / 27, 64 over 2,000 rows each 42 / 58.
+// In the first 5.4 us go by until the first tile is there, 8 stream the 52 MB, 2 join the warps and write; the rest joins the CTAs.
+// The vote on the scales is in these: 0.2 to 0.9 us of int8 and of up to 16 rows, nothing of e4m3 up to 8.
 #include "q8.cuh"
 #include "tma.cuh"
 #include "tree_attention.cuh"
@@ -36,8 +38,9 @@ namespace sharpv {
 namespace {
 
 constexpr int kKeys = kRowsTileKeys;            // of a tile
-// The split with what ending a segment and beginning another costs in these tiles, which take half the time of bf16 ones: the
-// ragged batch of 16 tokens 26.4 -> 22.2 us.
+// The split with what ending a segment and beginning another costs in these tiles, which take half the time of bf16 ones.  3 against 6:
+// the ragged batch of 16 tokens 25.5 against 20.5 us (int8 27.2 / 22.1), of pairs 33.3 / 27.0; where segments are even it decides
+// nothing (64 over 2,000 rows each 42.1 / 42.1).
 struct CodeSplit : Split {
     static constexpr uint32_t kSwitch = 6;
 };

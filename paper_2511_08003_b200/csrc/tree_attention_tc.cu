@@ -656,7 +656,8 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnM
                             y0 = ex2(y0);
                             y1 = ex2(y1);
                             sum2[k & 1] = add2(sum2[k & 1], pack2(y0, y1));
-                            // weights are rounded to bf16 for the product with the values; their sum is not
+                            // weights are rounded to bf16 for the product with the values (both operands are of one type, and values
+                            // are bf16, of a cache in 8 bits as well: fp16 does not hold their scales); their sum is not
                             pk[k] = pack_bf16(y0, y1);
                         }
                         tmem_st16(t_scores + i * 16, pk);
