@@ -36,7 +36,7 @@ def needs_build(path: str = LIB_PATH) -> bool:
     if not os.path.exists(path):
         return True
     t = os.path.getmtime(path)
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(INCLUDE, "*.h"))
+    deps = sources() + [p for at in (os.path.join(CSRC, "*.cuh"), os.path.join(CSRC, "*.h"), os.path.join(INCLUDE, "*.h")) for p in glob.glob(at)]
     return any(os.path.getmtime(p) > t for p in deps)
 
 
